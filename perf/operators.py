@@ -82,7 +82,7 @@ def draw(rng):
     seqs = _log(rng, 1, 64) if kind != "chunk" else _log(rng, 1, 8)
     new = 1 if kind == "decode" else rng.randint(2, 17) if kind == "verify" else _log(rng, 33, 2048)
     ctx = new + _log(rng, 1, 8192)
-    seqs = max(1, min(seqs, 2_400_000_000 // (hkv * group * new * ctx)))   # no more pairs than the whole prompt has
+    seqs = max(1, min(seqs, 1_300_000_000 // (hkv * group * new * ctx)))   # no more pairs than the whole prompt has
     return _attn(seqs, new, ctx, hkv * group, hkv, head_dim, rng.choice([16, 24, 64, 128]), rng.choice(["bf16", "bf16", "e4m3"]),
                  rng.choice([0, 0, 1024]), rng.random() < 0.7)
 
