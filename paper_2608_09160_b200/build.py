@@ -25,6 +25,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libqknorm.so")
 
 CHUNKS_PER_THREAD = (1, 2, 3, 4, 6, 8)          # row / ring kernels
 CHUNK_SLOTS_PER_LANE = tuple(range(4, 44, 4))    # warp-per-row kernel
+PADDED_HEAD_DIMS = (64, 128)                     # tensor-core attention kernel
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -51,6 +52,12 @@ def _units() -> List[Tuple[str, str, List[str]]]:
             units.append((f"qknorm_warp_{tag}_l{l}.o", os.path.join(CSRC, "qknorm_warp_inst.cu"),
                           [f"-DQKNORM_L={l}", f"-DQKNORM_IO={io}", f"-DQKNORM_IO_TAG={tag}"]))
     units.append(("qknorm_tp.o", os.path.join(CSRC, "qknorm_tp_inst.cu"), []))
+    units.append(("qknorm_rope.o", os.path.join(CSRC, "qknorm_rope_inst.cu"), []))
+    units.append(("qknorm_attn.o", os.path.join(CSRC, "qknorm_attn_inst.cu"), []))
+    for dp in PADDED_HEAD_DIMS:
+        for f8, tag in (("false", "bf16"), ("true", "e4m3")):
+            units.append((f"qknorm_attn_tc_{tag}_d{dp}.o", os.path.join(CSRC, "qknorm_attn_tc_inst.cu"),
+                          [f"-DQKNORM_DP={dp}", f"-DQKNORM_F8={f8}", f"-DQKNORM_IO_TAG={tag}"]))
     return units
 
 

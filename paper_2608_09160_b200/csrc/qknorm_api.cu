@@ -9,11 +9,14 @@
 #include <mutex>
 
 #include "../../include/qknorm.h"
+#include "../../include/qknorm_attn.h"
+#include "qknorm_attn.cuh"
 #include "qknorm_baselines.cuh"
 #include "qknorm_general.cuh"
 #include "qknorm_head.cuh"
 #include "qknorm_params.h"
 #include "qknorm_ring.cuh"
+#include "qknorm_rope.cuh"
 #include "qknorm_rows.cuh"
 #include "../../include/qknorm_tp.h"
 #include "qknorm_tp.cuh"
@@ -73,6 +76,12 @@ WarpKernel warp_kernel_for(int l, bool exact, int elem_bytes) {
   }
 #undef QKNORM_CASE_L
 }
+
+// per (cache format, padded head_dim), defined in qknorm_attn_tc_inst.cu (one translation unit each)
+AttnKernel attn_tc_kernel_bf1664(bool one_tile, int* smem_bytes);
+AttnKernel attn_tc_kernel_bf16128(bool one_tile, int* smem_bytes);
+AttnKernel attn_tc_kernel_e4m364(bool one_tile, int* smem_bytes);
+AttnKernel attn_tc_kernel_e4m3128(bool one_tile, int* smem_bytes);
 
 // Set by a ring kernel whose bounded wait ran out (0 = never happened).
 __device__ __align__(8) int g_ring_error[8] = {0, 0, 0, 0, 0, 0, 0, 0};  // word 0 is the error word; 1-2: where it happened
@@ -977,10 +986,13 @@ int static_scratch_address(float** out) {
   return QKNORM_OK;
 }
 
+#include "qknorm_attn_host.cuh"  // run_rope, run_append, run_attn
+
 }  // namespace
 }  // namespace qknorm
 
-#include "qknorm_tp_abi.cuh"  // the tensor-parallel entry points (include/qknorm_tp.h)
+#include "qknorm_attn_abi.cuh"  // rotary positions, cache write, attention (include/qknorm_attn.h)
+#include "qknorm_tp_abi.cuh"    // the tensor-parallel entry points (include/qknorm_tp.h)
 
 extern "C" {
 

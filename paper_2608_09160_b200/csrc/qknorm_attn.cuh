@@ -1,0 +1,236 @@
+// Attention of new tokens over a paged cache (include/qknorm_attn.h): what every kernel of it shares --
+// parameters, which keys a row sees, the row-at-a-time routine -- and the general kernel and the join of split results.
+//
+// Mathematics.  For one row, over the keys it sees, with c = scale * log2(e) (times the FP8 cache's k_scale):
+//   s_j = q . k_j,  m = max s_j,  l = sum 2^(c (s_j - m)),  o = sum 2^(c (s_j - m)) v_j / l
+// in one pass with a running m (l and o are multiplied by 2^(c (m_old - m_new)) when it grows).  Two parts
+// (o1, z1), (o2, z2) of one row over different keys, z = c m + log2 l, join to (o1 2^(z1-z) + o2 2^(z2-z), z).
+#pragma once
+#include "qknorm_device.cuh"
+#include "qknorm_ring.cuh"  // ptx helpers
+
+namespace qknorm {
+
+constexpr int kAttnTile = 128;       // keys per tile, rows per query tile
+constexpr int kAttnMaxEpl = 16;      // head_dim elements per lane of the row routine: QKNORM_MAX_HEAD_DIM / 32
+constexpr float kNegInf = -__builtin_huge_valf();
+
+struct AttnSide {
+  const void* base;
+  long long page, token, head;  // strides, elements
+};
+
+struct AttnParams {
+  const uint16_t* q;  // bf16
+  uint16_t* out;      // bf16
+  long long ld_q, ld_out;
+  AttnSide k, v;
+  long long num_pages;
+  int page_size, page_shift;  // page_shift: log2(page_size), or -1
+  const int* table;
+  long long ld_table;
+  const int* kv_lens;
+  const int* q_starts;
+  int seqs;
+  long long T;
+  int max_q;
+  long long max_keys;  // min(max_kv, table_cols * page_size)
+  int heads_q, heads_kv, group, head_dim;
+  float c;             // scale * k_scale * log2(e)
+  float v_scale;
+  int causal, window;
+  float* lse;
+  // split results: part s of (row, head) at [(s*T + row)*heads_q + head]
+  float* part_o;  // [splits, T, heads_q, head_dim], normalised
+  float* part_z;  // [splits, T, heads_q], log2
+  int splits, chunk_tiles;
+  int tok_per_tile;     // tokens of a query tile: 128 / group
+  int tiles_per_item;   // query tiles an item holds: 1 or 2
+  int q_items;          // items per (sequence, key head)
+  int* error;
+};
+
+// What one sequence's place in the batch says; everything clamped to the call's buffers.
+struct AttnSeq {
+  int row0;       // first row of q
+  int n;          // new tokens served (<= max_q)
+  int keys;       // keys that may be looked at
+  long long pos0; // position of the first new token (negative: it sees nothing)
+};
+
+__device__ __forceinline__ AttnSeq attn_seq(const AttnParams& P, int b) {
+  AttnSeq s;
+  const long long T = P.T;
+  long long r0 = P.q_starts[b], r1 = P.q_starts[b + 1];
+  const long long len = P.kv_lens[b];
+  r0 = r0 < 0 ? 0 : r0 > T ? T : r0;
+  r1 = r1 < r0 ? r0 : r1 > T ? T : r1;
+  s.row0 = (int)r0;
+  s.n = (int)(r1 - r0 < P.max_q ? r1 - r0 : P.max_q);
+  s.keys = (int)(len < 0 ? 0 : len < P.max_keys ? len : P.max_keys);
+  s.pos0 = len - (r1 - r0);
+  return s;
+}
+
+// Keys [lo, hi) that new token i sees; hi <= lo: none.  Both grow with i.
+__device__ __forceinline__ int attn_hi(const AttnParams& P, const AttnSeq& s, int i) {
+  if (!P.causal) return s.keys;
+  const long long e = s.pos0 + i + 1;
+  return (int)(e < 0 ? 0 : e < s.keys ? e : s.keys);
+}
+__device__ __forceinline__ int attn_lo(const AttnParams& P, const AttnSeq& s, int i) {
+  if (P.window == 0) return 0;
+  const long long e = s.pos0 + i + 1 - P.window;
+  return (int)(e < 0 ? 0 : e < s.keys ? e : s.keys);
+}
+
+// Page and token inside the page of a key; page < 0: an entry that names no page.
+__device__ __forceinline__ long long attn_page(const AttnParams& P, int b, int key, int& within) {
+  int idx;
+  if (P.page_shift >= 0) {
+    idx = key >> P.page_shift;
+    within = key & (P.page_size - 1);
+  } else {
+    idx = (int)((unsigned)key / (unsigned)P.page_size);
+    within = key - idx * P.page_size;
+  }
+  const int e = P.table[(long long)b * P.ld_table + idx];
+  return (e < 0 || e >= P.num_pages) ? -1 : e;
+}
+
+// One warp, one row and head, keys [lo, hi): o (normalised; lane holds elements lane + 32 e) and z = c m + log2 l.
+// Reads nothing of a key outside the range, so what other keys hold cannot matter.
+// EPL: elements per lane, at least head_dim / 32.
+template <class CIO, int EPL>
+__device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long row, int head, int lo, int hi, float (&o)[EPL],
+                                         float& z_out) {
+  const int lane = threadIdx.x & 31, D = P.head_dim;
+  const int kvh = head / P.group;
+  float q[EPL];
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
+    const int d = lane + 32 * e;
+    q[e] = d < D ? IoBf16::load(P.q, row * P.ld_q + (long long)head * D + d) : 0.f;
+    o[e] = 0.f;
+  }
+  float m = kNegInf, l = 0.f;
+  for (int key = lo; key < hi; ++key) {
+    int within;
+    const long long page = attn_page(P, b, key, within);
+    const long long ka = page * P.k.page + within * P.k.token + kvh * P.k.head;
+    const long long va = page * P.v.page + within * P.v.token + kvh * P.v.head;
+    float s = 0.f;
+    if (page >= 0) {
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) {
+        const int d = lane + 32 * e;
+        if (d < D) s = fmaf(q[e], CIO::load(P.k.base, ka + d), s);
+      }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    if (s == kNegInf) continue;
+    const float mn = fmaxf(m, s);  // a NaN score leaves m as it is and makes p, and the row, NaN
+    const float f = m == kNegInf ? 0.f : exp2f((m - mn) * P.c);
+    const float p = mn == kNegInf ? s : exp2f((s - mn) * P.c);
+    l = fmaf(l, f, p);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      const int d = lane + 32 * e;
+      if (d < D) o[e] = fmaf(o[e], f, p * (page >= 0 ? CIO::load(P.v.base, va + d) : 0.f));
+    }
+    m = mn;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) o[e] *= inv;
+  z_out = l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, P.c, log2f(l));
+}
+
+constexpr float kLn2 = 0.693147180559945309f;
+
+// Any head_dim, group, alignment: a warp per (new token, query head).
+constexpr int kAttnGeneralThreads = 128;
+
+template <class CIO>
+__global__ void __launch_bounds__(kAttnGeneralThreads) attn_general_kernel(const __grid_constant__ AttnParams P) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31;
+  const long long items = (long long)P.seqs * P.max_q * P.heads_q;
+  const long long warps = (long long)gridDim.x * (kAttnGeneralThreads / 32);
+  for (long long it = (long long)blockIdx.x * (kAttnGeneralThreads / 32) + (threadIdx.x >> 5); it < items; it += warps) {
+    const int head = (int)(it % P.heads_q);
+    const long long r = it / P.heads_q;
+    const int i = (int)(r % P.max_q), b = (int)(r / P.max_q);
+    const AttnSeq s = attn_seq(P, b);
+    if (i >= s.n) continue;
+    const long long row = s.row0 + (long long)i;
+    float o[kAttnMaxEpl], z;
+    attn_row<CIO, kAttnMaxEpl>(P, b, row, head, attn_lo(P, s, i), attn_hi(P, s, i), o, z);
+#pragma unroll
+    for (int e = 0; e < kAttnMaxEpl; ++e) {
+      const int d = lane + 32 * e;
+      if (d < P.head_dim) IoBf16::store(P.out, row * P.ld_out + (long long)head * P.head_dim + d, o[e] * P.v_scale);
+    }
+    if (P.lse != nullptr && lane == 0) P.lse[row * P.heads_q + head] = z * kLn2;
+  }
+}
+
+// An item of the tensor-core kernel: query tiles of one sequence and key head, one part of its keys.
+struct AttnItem {
+  AttnSeq s;
+  int b, kvh, split;
+  int tok0;        // first new token
+  int j0, j1;      // key tiles of this part
+  int ulo, uhi;    // keys that some row of the item sees (whole item, not this part only)
+  int parts;       // parts the item's keys are cut into
+};
+
+// Key tiles of the item that starts at token tok0, over all parts: [J0, J1); also ulo, uhi.
+__device__ __forceinline__ void attn_span(const AttnParams& P, const AttnSeq& s, int tok0, int& J0, int& J1, int& ulo, int& uhi) {
+  int last = tok0 + P.tok_per_tile * P.tiles_per_item - 1;
+  if (last >= s.n) last = s.n - 1;
+  ulo = attn_lo(P, s, tok0);
+  uhi = attn_hi(P, s, last);
+  if (uhi <= ulo) {
+    J0 = J1 = 0;
+    return;
+  }
+  J0 = ulo / kAttnTile;
+  J1 = (uhi + kAttnTile - 1) / kAttnTile;
+}
+
+// Item number -> item; false: nothing to do (no such tokens, or a part past the end).  Later tokens first: under a
+// causal mask they see the most keys.  Key heads and parts run fastest.
+__device__ __forceinline__ bool attn_item(const AttnParams& P, long long idx, AttnItem& it) {
+  it.split = (int)(idx % P.splits);
+  idx /= P.splits;
+  it.kvh = (int)(idx % P.heads_kv);
+  idx /= P.heads_kv;
+  it.b = (int)(idx % P.seqs);
+  const int qt = P.q_items - 1 - (int)(idx / P.seqs);
+  it.s = attn_seq(P, it.b);
+  it.tok0 = qt * P.tok_per_tile * P.tiles_per_item;
+  if (it.tok0 >= it.s.n) return false;
+  int J0, J1;
+  attn_span(P, it.s, it.tok0, J0, J1, it.ulo, it.uhi);
+  it.parts = (J1 - J0 + P.chunk_tiles - 1) / P.chunk_tiles;
+  if (it.split > 0 && it.split >= it.parts) return false;
+  it.j0 = J0 + it.split * P.chunk_tiles;
+  it.j1 = it.j0 + P.chunk_tiles < J1 ? it.j0 + P.chunk_tiles : J1;
+  return true;
+}
+
+// Joins the parts of every (row, head): a warp each.
+constexpr int kAttnJoinThreads = 128;
+
+__global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams P);
+
+typedef void (*AttnKernel)(const AttnParams);
+// in qknorm_attn_inst.cu and qknorm_attn_tc_inst.cu
+AttnKernel attn_general_kernel_for(bool e4m3);
+AttnKernel attn_join_kernel_for();
+constexpr int kAttnTcThreads = 512;
+constexpr int kAttnTcRegs = 128;  // registers per thread at launch that the kernel's register split counts on
+
+}  // namespace qknorm

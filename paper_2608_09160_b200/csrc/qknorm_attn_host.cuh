@@ -1,0 +1,537 @@
+// Host side of the entry points of include/qknorm_attn.h: validation, variant choice, launch.
+// Included by qknorm_api.cu INSIDE its unnamed namespace, after the helpers it uses (device cache,
+// occupancy cache, overlap test, launch_overlapped).
+#pragma once
+
+// ---- rotary positions and the cache write ---------------------------------------------------------
+
+int rope_frequencies(int32_t rot_dim, double theta, int32_t scaling, double factor, double original_len, double low,
+                     double high, double* inv_freq, float* mscale) {
+  if (!inv_freq || !mscale) return QKNORM_ERR_NULL;
+  if (rot_dim < 2 || rot_dim % 2 != 0 || rot_dim > QKNORM_MAX_HEAD_DIM) return QKNORM_ERR_SHAPE;
+  if (!(theta > 1.0) || !isfinite(theta)) return QKNORM_ERR_SHAPE;
+  if (scaling < QKNORM_ROPE_PLAIN || scaling > QKNORM_ROPE_BANDS) return QKNORM_ERR_SHAPE;
+  if (scaling != QKNORM_ROPE_PLAIN && !(factor >= 1.0 && isfinite(factor))) return QKNORM_ERR_SHAPE;
+  const bool by_turns = scaling == QKNORM_ROPE_RAMP || scaling == QKNORM_ROPE_BANDS;
+  if (by_turns && !(original_len > 0.0 && isfinite(original_len) && low > 0.0 && high > low && isfinite(high))) return QKNORM_ERR_SHAPE;
+  if (scaling == QKNORM_ROPE_BASE && rot_dim == 2) return QKNORM_ERR_SHAPE;  // its exponent divides by rot_dim - 2
+  const double pi2 = 6.283185307179586476925;
+  const double base = scaling == QKNORM_ROPE_BASE ? theta * pow(factor, (double)rot_dim / (rot_dim - 2)) : theta;
+  *mscale = scaling == QKNORM_ROPE_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+  // pair index (as a real number) that turns `turns` times within original_len
+  auto index_of = [&](double turns) { return rot_dim * log(original_len / (turns * pi2)) / (2.0 * log(theta)); };
+  double first = 0.0, last = 0.0;
+  if (scaling == QKNORM_ROPE_RAMP) {
+    first = fmax(floor(index_of(high)), 0.0);
+    last = fmin(ceil(index_of(low)), rot_dim - 1.0);
+    if (last <= first) last = first + 0.001;
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / rot_dim);
+    double keep = 1.0;  // share of the unscaled frequency
+    if (scaling == QKNORM_ROPE_LINEAR) keep = 0.0;
+    if (scaling == QKNORM_ROPE_RAMP) keep = 1.0 - fmin(fmax((i - first) / (last - first), 0.0), 1.0);
+    if (scaling == QKNORM_ROPE_BANDS) keep = fmin(fmax((original_len * f / pi2 - low) / (high - low), 0.0), 1.0);
+    if (scaling != QKNORM_ROPE_PLAIN && scaling != QKNORM_ROPE_BASE) f = f * keep + f / factor * (1.0 - keep);
+    inv_freq[i] = f;
+  }
+  return QKNORM_OK;
+}
+
+// A rotation of a call; r == nullptr: none.
+int check_rotation(const qknorm_rotation* r, int head_dim, RopeParams& R) {
+  R.rot_dim = 0;
+  R.mscale = 1.0f;
+  if (!r || r->rot_dim == 0) return QKNORM_OK;
+  if (r->rot_dim < 0 || r->rot_dim % 2 != 0 || r->rot_dim > head_dim) return QKNORM_ERR_SHAPE;
+  if (r->interleaved != 0 && r->interleaved != 1) return QKNORM_ERR_SHAPE;
+  if (!isfinite(r->mscale)) return QKNORM_ERR_SHAPE;
+  if (!r->positions || !r->inv_freq) return QKNORM_ERR_NULL;
+  if ((((uintptr_t)r->positions) | ((uintptr_t)r->inv_freq)) & 7u) return QKNORM_ERR_ALIGN;
+  R.rot_dim = r->rot_dim;
+  R.interleaved = r->interleaved;
+  R.mscale = r->mscale;
+  R.positions = (const long long*)r->positions;
+  R.inv_freq = r->inv_freq;
+  R.turns_sign = 0.15915494309189533577;  // 1 / (2 pi)
+  return QKNORM_OK;
+}
+
+struct CallRegions {  // buffers of a call: outputs, and everything an output must not touch
+  Region out[8], in[16];
+  int outs = 0, ins = 0;
+  bool exact_input_ok[8];  // out[i] may be exactly in[own[i]]
+  int own[8];
+};
+
+Region flat(const void* p, uintptr_t bytes) { return Region{(uintptr_t)p, 1, bytes, bytes}; }
+
+// Outputs against every input and every other output; an output may be exactly its own input.
+int check_regions(const CallRegions& c) {
+  for (int i = 0; i < c.outs; ++i) {
+    for (int j = 0; j < c.ins; ++j)
+      if (may_overlap(c.out[i], c.in[j]) && !(c.own[i] == j && same_region(c.out[i], c.in[j]))) return QKNORM_ERR_ALIAS;
+    for (int j = 0; j < c.outs; ++j)
+      if (j != i && may_overlap(c.out[i], c.out[j])) return QKNORM_ERR_ALIAS;
+  }
+  return QKNORM_OK;
+}
+
+int row_stride(int64_t ld, int32_t width, long long* out) {
+  if (ld < 0 || (ld != 0 && ld < width)) return QKNORM_ERR_SHAPE;
+  *out = ld ? ld : width;
+  return QKNORM_OK;
+}
+
+// One side of a paged cache: strides and alignment.  *rows: the tokens of the pool as a region where they can be described
+// as rows of one pitch, else one region from the first to the last element.
+int check_cache_side(const qknorm_paged_cache& c, void* base, int64_t page, int64_t token, int64_t head, Region* region, bool* vec16,
+                     bool* vec8) {
+  const uintptr_t eb = c.e4m3 ? 1 : 2;
+  if (c.num_pages > 0 && !base) return QKNORM_ERR_NULL;
+  if (page < 0 || token < 0 || head < 0) return QKNORM_ERR_SHAPE;
+  if (c.num_pages == 0) {  // an empty pool: nothing in it is ever touched
+    *region = Region{0, 0, 0, 0};
+    *vec16 = *vec8 = true;
+    return QKNORM_OK;
+  }
+  // no two elements of a page in the same place: heads inside a token's stride or tokens inside a head's
+  const int64_t d = c.head_dim;
+  if (c.heads > 1 && head < d) return QKNORM_ERR_SHAPE;
+  if (c.page_size > 1 && token < d) return QKNORM_ERR_SHAPE;
+  if (c.heads > 1 && c.page_size > 1 && (__int128)token < (__int128)(c.heads - 1) * head + d &&
+      (__int128)head < (__int128)(c.page_size - 1) * token + d)
+    return QKNORM_ERR_SHAPE;
+  const __int128 total = (__int128)(c.num_pages > 1 ? c.num_pages - 1 : 0) * page + (__int128)(c.page_size - 1) * token +
+                         (__int128)(c.heads - 1) * head + d;
+  if (total > ((__int128)1 << 60)) return QKNORM_ERR_SHAPE;
+  const int64_t extent = (c.page_size - 1) * token + (c.heads - 1) * head + d;
+  if (c.num_pages > 1 && page < d) return QKNORM_ERR_SHAPE;
+  if (((uintptr_t)base) % eb != 0) return QKNORM_ERR_ALIGN;
+  if (c.num_pages > 1 && page == c.page_size * token && (c.heads - 1) * head + d <= token)
+    *region = Region{(uintptr_t)base, (uintptr_t)(c.num_pages * c.page_size), (uintptr_t)((c.heads - 1) * head + d) * eb, (uintptr_t)token * eb};
+  else if (c.num_pages > 1 && page < extent)
+    *region = Region{(uintptr_t)base, 1, (uintptr_t)((c.num_pages - 1) * page + extent) * eb, (uintptr_t)((c.num_pages - 1) * page + extent) * eb};
+  else
+    *region = Region{(uintptr_t)base, (uintptr_t)c.num_pages, (uintptr_t)extent * eb, (uintptr_t)(c.num_pages > 1 ? page : extent) * eb};
+  const uintptr_t all = (uintptr_t)base | ((uintptr_t)page * eb) | ((uintptr_t)token * eb) | ((uintptr_t)head * eb);
+  *vec16 = all % 16 == 0;
+  *vec8 = all % 8 == 0;
+  return QKNORM_OK;
+}
+
+struct CacheFacts {
+  Region k, v;
+  bool vec16, vec8;
+};
+
+int check_cache(const qknorm_paged_cache* c, CacheFacts* f) {
+  if (!c) return QKNORM_ERR_NULL;
+  if (c->num_pages < 0 || c->num_pages > 0x7fffffff || c->page_size < 1 || c->heads < 1) return QKNORM_ERR_SHAPE;
+  if (c->head_dim < 1 || c->head_dim > QKNORM_MAX_HEAD_DIM) return QKNORM_ERR_HEADS;
+  if ((int64_t)c->heads * c->head_dim > kMaxDim) return QKNORM_ERR_SHAPE;
+  if (c->e4m3 != 0 && c->e4m3 != 1) return QKNORM_ERR_SHAPE;
+  if (c->e4m3 && (!(c->k_scale > 0.0f) || !isfinite(c->k_scale) || !(c->v_scale > 0.0f) || !isfinite(c->v_scale))) return QKNORM_ERR_SHAPE;
+  bool k16, k8, v16, v8;
+  int rc = check_cache_side(*c, c->k, c->k_page, c->k_token, c->k_head, &f->k, &k16, &k8);
+  if (rc != QKNORM_OK) return rc;
+  rc = check_cache_side(*c, c->v, c->v_page, c->v_token, c->v_head, &f->v, &v16, &v8);
+  if (rc != QKNORM_OK) return rc;
+  f->vec16 = k16 && v16;
+  f->vec8 = k8 && v8;
+  return QKNORM_OK;
+}
+
+// Launches R (everything but the launch shape filled in).  cache_bytes 0: no cache.  vec: the vector kernel's alignment holds.
+int launch_rope(RopeParams& R, int elem_bytes, int cache_bytes, int norm, bool vec, cudaStream_t stream) {
+  const DeviceInfo* dev = nullptr;
+  int rc = current_device(&dev);
+  if (rc != QKNORM_OK) return rc;
+  const char* force = env_str("QKNORM_FORCE_VARIANT");
+  if (force && strcmp(force, "general") == 0) vec = false;
+  if (vec) {
+    R.log_lph = 0;
+    while ((16 << R.log_lph) < R.head_dim) ++R.log_lph;
+    const int heads = R.q.heads + R.k.heads + (cache_bytes ? R.v.heads : 0);
+    R.slots_per_token = heads << R.log_lph;
+    // Two units (64 bytes of bf16) per thread keep enough loads in flight without long CTAs; few tokens: one, for latency.
+    int upt = R.T < 2 * dev->sm_count ? 1 : 2;
+    const int forced = env_int("QKNORM_ROPE_UPT", 0);
+    if (forced) upt = forced;
+    if (R.slots_per_token > 1024 * upt) upt = R.slots_per_token > 2048 ? 4 : 2;
+    if (R.slots_per_token <= 4096) {
+      R.threads_per_token = round_up((R.slots_per_token + upt - 1) / upt, 32);
+      // short rows: several tokens share a CTA of about 128 threads
+      R.tokens_per_cta = R.T >= 2 * dev->sm_count && R.threads_per_token < 128 ? 128 / R.threads_per_token : 1;
+      const int smem = R.tokens_per_cta * R.rot_dim * (int)sizeof(float2) / 2;
+      RopeKernel fn = rope_kernel_for(elem_bytes, cache_bytes, norm, upt);
+      const long long grid = (R.T + R.tokens_per_cta - 1) / R.tokens_per_cta;
+      if (fn && grid <= 0x7fffffff) {
+        const cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)(R.tokens_per_cta * R.threads_per_token), (size_t)smem, stream, R);
+        if (e != cudaSuccess) return set_cuda_error(e);
+        return finish_launch(cache_bytes ? "append" : "rope");
+      }
+    }
+  }
+  RopeGeneralKernel gen = rope_general_kernel_for(elem_bytes, cache_bytes);
+  int bres = 1;
+  rc = resident_blocks((const void*)gen, kRopeGeneralThreads, 0, &bres);
+  if (rc != QKNORM_OK) return rc;
+  long long grid = (long long)bres * dev->sm_count;
+  if (grid > R.T) grid = R.T;
+  const cudaError_t e = launch_overlapped(gen, (unsigned)grid, (unsigned)kRopeGeneralThreads, 0, stream, R, norm);
+  if (e != cudaSuccess) return set_cuda_error(e);
+  return finish_launch(cache_bytes ? "append_general" : "rope_general");
+}
+
+int run_rope(int elem_bytes, const void* q, const void* k, const qknorm_rotation* rot, int64_t T, int32_t dq, int32_t dk,
+             int32_t head_dim, int64_t ld_q, int64_t ld_k, int32_t inverse, void* oq, void* ok, int64_t ld_oq, int64_t ld_ok,
+             cudaStream_t stream) {
+  if (T < 0 || dq < 0 || dk < 0 || dq > kMaxDim || dk > kMaxDim) return QKNORM_ERR_SHAPE;
+  if (head_dim < 1 || head_dim > QKNORM_MAX_HEAD_DIM || dq % head_dim != 0 || dk % head_dim != 0) return QKNORM_ERR_HEADS;
+  if (inverse != 0 && inverse != 1) return QKNORM_ERR_SHAPE;
+  if (!rot) return QKNORM_ERR_NULL;
+  RopeParams R;
+  memset(&R, 0, sizeof(R));
+  int rc;
+  if ((rc = row_stride(ld_q, dq, &R.q.ldx)) || (rc = row_stride(ld_k, dk, &R.k.ldx)) || (rc = row_stride(ld_oq, dq, &R.q.ldy)) ||
+      (rc = row_stride(ld_ok, dk, &R.k.ldy)))
+    return rc;
+  if (T == 0) return QKNORM_OK;
+  if (dq == 0 && dk == 0) return QKNORM_ERR_SHAPE;
+  if ((rc = check_rotation(rot, head_dim, R)) != QKNORM_OK) return rc;
+  if (inverse) R.turns_sign = -R.turns_sign;
+  R.T = T;
+  R.head_dim = head_dim;
+  CallRegions c;
+  uintptr_t vec = (uintptr_t)head_dim | (uintptr_t)R.rot_dim;  // multiples of 16, checked together
+  const uintptr_t eb = (uintptr_t)elem_bytes, unit = 8 * eb;
+  bool aligned = vec % 16 == 0;
+  struct Side {
+    RopeSide* s;
+    const void* x;
+    void* y;
+    int d;
+  } sides[2] = {{&R.q, q, oq, dq}, {&R.k, k, ok, dk}};
+  for (Side& sd : sides) {
+    if (sd.d == 0) continue;
+    if (!sd.x || !sd.y) return QKNORM_ERR_NULL;
+    if ((((uintptr_t)sd.x) | ((uintptr_t)sd.y)) % eb != 0) return QKNORM_ERR_ALIGN;
+    sd.s->x = sd.x;
+    sd.s->y = sd.y;
+    sd.s->heads = sd.d / head_dim;
+    aligned = aligned && (((uintptr_t)sd.x) | ((uintptr_t)sd.y) | ((uintptr_t)sd.s->ldx * eb) | ((uintptr_t)sd.s->ldy * eb)) % unit == 0;
+    c.own[c.outs] = c.ins;
+    c.out[c.outs++] = Region{(uintptr_t)sd.y, (uintptr_t)T, (uintptr_t)sd.d * eb, (uintptr_t)sd.s->ldy * eb};
+    c.in[c.ins++] = Region{(uintptr_t)sd.x, (uintptr_t)T, (uintptr_t)sd.d * eb, (uintptr_t)sd.s->ldx * eb};
+  }
+  if (R.rot_dim) {
+    c.in[c.ins++] = flat(R.positions, 8 * (uintptr_t)T);
+    c.in[c.ins++] = flat(R.inv_freq, 4 * (uintptr_t)R.rot_dim);
+  }
+  if ((rc = check_regions(c)) != QKNORM_OK) return rc;
+  return launch_rope(R, elem_bytes, 0, kNormNone, aligned, stream);
+}
+
+int run_append(const void* q, const void* k, const void* v, const void* gq, const void* gk, int32_t norm, float eps,
+               const qknorm_rotation* rot, const int64_t* slots, const qknorm_paged_cache* cache, int64_t T, int32_t dq, int64_t ld_q,
+               int64_t ld_k, int64_t ld_v, void* oq, int64_t ld_oq, cudaStream_t stream) {
+  CacheFacts f;
+  int rc = check_cache(cache, &f);
+  if (rc != QKNORM_OK) return rc;
+  const int hd = cache->head_dim, dk = cache->heads * hd;
+  if (T < 0 || dq < 0 || dq > kMaxDim) return QKNORM_ERR_SHAPE;
+  if (dq % hd != 0) return QKNORM_ERR_HEADS;
+  if (norm < kNormNone || norm > kNormHead) return QKNORM_ERR_SHAPE;
+  if (norm != kNormNone && !(eps >= 0.0f)) return QKNORM_ERR_EPS;
+  RopeParams R;
+  memset(&R, 0, sizeof(R));
+  if ((rc = row_stride(ld_q, dq, &R.q.ldx)) || (rc = row_stride(ld_oq, dq, &R.q.ldy)) || (rc = row_stride(ld_k, dk, &R.k.ldx)) ||
+      (rc = row_stride(ld_v, dk, &R.v.ldx)))
+    return rc;
+  if (T == 0) return QKNORM_OK;
+  if ((rc = check_rotation(rot, hd, R)) != QKNORM_OK) return rc;
+  if (!k || !v || !slots || (norm != kNormNone && !gk)) return QKNORM_ERR_NULL;
+  if (dq > 0 && (!q || !oq || (norm != kNormNone && !gq))) return QKNORM_ERR_NULL;
+  uintptr_t ptrs = (uintptr_t)k | (uintptr_t)v, strides = (uintptr_t)R.k.ldx | (uintptr_t)R.v.ldx;
+  if (norm != kNormNone) ptrs |= (uintptr_t)gk;
+  if (dq > 0) {
+    ptrs |= (uintptr_t)q | (uintptr_t)oq;
+    strides |= (uintptr_t)R.q.ldx | (uintptr_t)R.q.ldy;
+    if (norm != kNormNone) ptrs |= (uintptr_t)gq;
+  }
+  if (ptrs & 1u) return QKNORM_ERR_ALIGN;
+  if (((uintptr_t)slots) & 7u) return QKNORM_ERR_ALIGN;
+  R.T = T;
+  R.head_dim = hd;
+  R.inv_hd = 1.0f / (float)hd;
+  R.eps = eps;
+  if (dq > 0) {
+    R.q.x = q;
+    R.q.y = oq;
+    R.q.gamma = (const uint16_t*)gq;
+    R.q.heads = dq / hd;
+    R.q.inv_d = 1.0f / (float)dq;
+  }
+  R.k.x = k;
+  R.k.gamma = (const uint16_t*)gk;
+  R.k.heads = R.v.heads = cache->heads;
+  R.k.inv_d = 1.0f / (float)dk;
+  R.v.x = v;
+  R.ck = CacheSide{cache->k, cache->k_page, cache->k_token, cache->k_head, cache->e4m3 ? 1.0f / cache->k_scale : 1.0f};
+  R.cv = CacheSide{cache->v, cache->v_page, cache->v_token, cache->v_head, cache->e4m3 ? 1.0f / cache->v_scale : 1.0f};
+  R.slots = (const long long*)slots;
+  R.num_slots = (long long)cache->num_pages * cache->page_size;
+  R.page_size = cache->page_size;
+  const uintptr_t rows = (uintptr_t)T, qb = (uintptr_t)dq * 2, kb = (uintptr_t)dk * 2;
+  CallRegions c;
+  if (dq > 0) {
+    c.own[0] = 0;
+    c.out[c.outs++] = Region{(uintptr_t)oq, rows, qb, (uintptr_t)R.q.ldy * 2};
+    c.in[c.ins++] = Region{(uintptr_t)q, rows, qb, (uintptr_t)R.q.ldx * 2};
+    if (norm != kNormNone) c.in[c.ins++] = flat(gq, qb);
+  }
+  c.own[c.outs] = -1;
+  c.out[c.outs++] = f.k;
+  c.own[c.outs] = -1;
+  c.out[c.outs++] = f.v;
+  c.in[c.ins++] = Region{(uintptr_t)k, rows, kb, (uintptr_t)R.k.ldx * 2};
+  c.in[c.ins++] = Region{(uintptr_t)v, rows, kb, (uintptr_t)R.v.ldx * 2};
+  if (norm != kNormNone) c.in[c.ins++] = flat(gk, kb);
+  c.in[c.ins++] = flat(slots, 8 * rows);
+  if (R.rot_dim) {
+    c.in[c.ins++] = flat(R.positions, 8 * rows);
+    c.in[c.ins++] = flat(R.inv_freq, 4 * (uintptr_t)R.rot_dim);
+  }
+  if ((rc = check_regions(c)) != QKNORM_OK) return rc;
+  const bool vec = (hd | R.rot_dim) % 16 == 0 && ptrs % 16 == 0 && strides % 8 == 0 && (cache->e4m3 ? f.vec8 : f.vec16);
+  return launch_rope(R, 2, cache->e4m3 ? 1 : 2, norm, vec, stream);
+}
+
+// ---- attention over the paged cache ---------------------------------------------------------------
+
+AttnKernel attn_tc_for(int dp, bool e4m3, bool one_tile, int* smem) {
+  if (dp == 64) return e4m3 ? attn_tc_kernel_e4m364(one_tile, smem) : attn_tc_kernel_bf1664(one_tile, smem);
+  return e4m3 ? attn_tc_kernel_e4m3128(one_tile, smem) : attn_tc_kernel_bf16128(one_tile, smem);
+}
+
+// The tensor-core kernel hands registers from its loaders to its softmax warps: it must have been compiled to start with the
+// number the split adds up to, or the warps that ask for more would wait for ever.
+int attn_tc_registers_ok(const void* fn) {
+  static const void* known[16];
+  static int n = 0;
+  std::lock_guard<std::mutex> lock(g_occ_mutex);
+  for (int i = 0; i < n; ++i)
+    if (known[i] == fn) return QKNORM_OK;
+  cudaFuncAttributes a;
+  const cudaError_t e = cudaFuncGetAttributes(&a, fn);
+  if (e != cudaSuccess) return set_cuda_error(e);
+  if (a.numRegs != kAttnTcRegs) return set_cuda_error(cudaErrorLaunchOutOfResources);
+  if (n < 16) known[n++] = fn;
+  return QKNORM_OK;
+}
+
+// How a call is cut: sizes only, so that the workspace can be asked for beforehand.
+struct AttnPlan {
+  bool tc = false;
+  int tok_per_tile = 1, tiles_per_item = 1, q_items = 1, splits = 1, chunk_tiles = 1;
+};
+
+AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, int window, int sms) {
+  AttnPlan p;
+  const int group = heads_q / heads_kv;
+  p.tc = head_dim % 8 == 0 && head_dim <= 128 && group <= kAttnTile;
+  if (!p.tc) return p;
+  p.tok_per_tile = kAttnTile / group;
+  if ((int64_t)max_q > T) max_q = (int)T;
+  p.tiles_per_item = max_q <= p.tok_per_tile ? 1 : 2;
+  const int per_item = p.tok_per_tile * p.tiles_per_item;
+  p.q_items = (max_q + per_item - 1) / per_item;
+  int64_t tiles = (max_keys + kAttnTile - 1) / kAttnTile;
+  if (window > 0) {
+    const int64_t span = ((int64_t)window + per_item - 1 + kAttnTile - 2) / kAttnTile + 1;
+    if (span < tiles) tiles = span;
+  }
+  if (tiles < 1) tiles = 1;
+  // Items that can have rows at all: a batch of T rows has no more than this many query pieces.
+  int64_t pieces = (int64_t)p.q_items * seqs;
+  if (T / per_item + seqs < pieces) pieces = T / per_item + seqs;
+  const int64_t items = pieces * heads_kv;
+  // Parts: waves of CTAs times the tiles each walks, plus what an item costs beside its tiles (start of the
+  // pipeline, end of the rows) and, once there are parts, the second launch.
+  const double per_item_cost = 3.0, join_cost = 6.0;
+  double best = 1e300;
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    const int64_t chunk = (tiles + s - 1) / s;
+    const int64_t used = (tiles + chunk - 1) / chunk;
+    if (used != s) continue;
+    const int64_t waves = (items * s + sms - 1) / sms;
+    const double cost = (double)waves * ((double)chunk + per_item_cost) + (s > 1 ? join_cost + 0.02 * s * items / sms : 0.0);
+    if (cost < best) {
+      best = cost;
+      p.splits = s;
+      p.chunk_tiles = (int)chunk;
+    }
+  }
+  return p;
+}
+
+int64_t attn_workspace(const AttnPlan& p, int64_t T, int heads_q, int head_dim) {
+  if (p.splits <= 1) return 0;
+  const int64_t rows = (int64_t)p.splits * T * heads_q;
+  return ((rows * head_dim * 4 + 15) / 16) * 16 + rows * 4;
+}
+
+int check_attn_sizes(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                     int32_t window) {
+  if (seqs < 0 || T < 0 || T > 0x7fffffff || max_q < 0 || max_kv < 0 || max_kv > QKNORM_MAX_KEYS || window < 0) return QKNORM_ERR_SHAPE;
+  if (head_dim < 1 || head_dim > QKNORM_MAX_HEAD_DIM) return QKNORM_ERR_HEADS;
+  if (heads_q < 1 || heads_kv < 1 || heads_q % heads_kv != 0) return QKNORM_ERR_HEADS;
+  if ((int64_t)heads_q * head_dim > kMaxDim) return QKNORM_ERR_SHAPE;
+  return QKNORM_OK;
+}
+
+int run_attn_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                       int32_t window, int64_t* bytes) {
+  if (!bytes) return QKNORM_ERR_NULL;
+  int rc = check_attn_sizes(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window);
+  if (rc != QKNORM_OK) return rc;
+  *bytes = 0;
+  if (seqs == 0 || T == 0 || max_q == 0) return QKNORM_OK;
+  const DeviceInfo* dev = nullptr;
+  rc = current_device(&dev);
+  if (rc != QKNORM_OK) return rc;
+  *bytes = attn_workspace(plan_attn(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window, dev->sm_count), T, heads_q, head_dim);
+  return QKNORM_OK;
+}
+
+int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* table, int32_t table_cols, int64_t ld_table,
+             const int32_t* kv_lens, const int32_t* q_starts, int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q,
+             float scale, int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* ws, int64_t ws_bytes,
+             cudaStream_t stream) {
+  CacheFacts f;
+  int rc = check_cache(cache, &f);
+  if (rc != QKNORM_OK) return rc;
+  rc = check_attn_sizes(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, window);
+  if (rc != QKNORM_OK) return rc;
+  if (!(scale > 0.0f) || !isfinite(scale)) return QKNORM_ERR_SHAPE;
+  if (causal != 0 && causal != 1) return QKNORM_ERR_SHAPE;
+  if (table_cols < 0 || ld_table < 0 || (ld_table != 0 && ld_table < table_cols)) return QKNORM_ERR_SHAPE;
+  AttnParams P;
+  memset(&P, 0, sizeof(P));
+  const int d = heads_q * cache->head_dim;
+  if ((rc = row_stride(ld_q, d, &P.ld_q)) || (rc = row_stride(ld_out, d, &P.ld_out))) return rc;
+  if (seqs == 0 || T == 0 || max_q == 0) return QKNORM_OK;
+  if (!q || !out || !kv_lens || !q_starts || (table_cols > 0 && !table)) return QKNORM_ERR_NULL;
+  if ((((uintptr_t)q) | ((uintptr_t)out)) & 1u) return QKNORM_ERR_ALIGN;
+  if ((((uintptr_t)table) | ((uintptr_t)kv_lens) | ((uintptr_t)q_starts) | ((uintptr_t)lse)) & 3u) return QKNORM_ERR_ALIGN;
+
+  const DeviceInfo* dev = nullptr;
+  rc = current_device(&dev);
+  if (rc != QKNORM_OK) return rc;
+  AttnPlan plan = plan_attn(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, window, dev->sm_count);
+  const bool aligned = (((uintptr_t)q) | ((uintptr_t)out) | ((uintptr_t)P.ld_q * 2) | ((uintptr_t)P.ld_out * 2)) % 16 == 0 && f.vec16 &&
+                       (!cache->e4m3 || cache->head_dim % 16 == 0);
+  const char* force = env_str("QKNORM_FORCE_VARIANT");
+  if (!aligned || (force && strcmp(force, "general") == 0)) plan.tc = false;
+  if (!plan.tc) plan.splits = 1;
+  const int64_t need = attn_workspace(plan, T, heads_q, cache->head_dim);
+  if (need > 0) {
+    if (!ws || ws_bytes < need || !aligned16(ws)) return QKNORM_ERR_SCRATCH;
+    const Region w = flat(ws, (uintptr_t)need);
+    const Region others[] = {Region{(uintptr_t)q, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_q * 2},
+                             Region{(uintptr_t)out, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_out * 2},
+                             f.k, f.v,
+                             Region{(uintptr_t)table, (uintptr_t)seqs, (uintptr_t)table_cols * 4, (uintptr_t)(ld_table ? ld_table : table_cols) * 4},
+                             flat(kv_lens, 4 * (uintptr_t)seqs), flat(q_starts, 4 * ((uintptr_t)seqs + 1)),
+                             flat(lse, lse ? 4 * (uintptr_t)T * heads_q : 0)};
+    for (const Region& o : others)
+      if (may_overlap(w, o)) return QKNORM_ERR_SCRATCH;
+  }
+  {
+    // q and out stay apart: with the keys in parts, a row of q may still be read after another part has written out
+    CallRegions c;
+    c.own[c.outs] = -1;
+    c.out[c.outs++] = Region{(uintptr_t)out, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_out * 2};
+    if (lse) {
+      c.own[c.outs] = -1;
+      c.out[c.outs++] = flat(lse, 4 * (uintptr_t)T * heads_q);
+    }
+    c.in[c.ins++] = Region{(uintptr_t)q, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_q * 2};
+    c.in[c.ins++] = f.k;
+    c.in[c.ins++] = f.v;
+    if (table_cols > 0)
+      c.in[c.ins++] = Region{(uintptr_t)table, (uintptr_t)seqs, (uintptr_t)table_cols * 4, (uintptr_t)(ld_table ? ld_table : table_cols) * 4};
+    c.in[c.ins++] = flat(kv_lens, 4 * (uintptr_t)seqs);
+    c.in[c.ins++] = flat(q_starts, 4 * ((uintptr_t)seqs + 1));
+    if ((rc = check_regions(c)) != QKNORM_OK) return rc;
+  }
+
+  P.q = (const uint16_t*)q;
+  P.out = (uint16_t*)out;
+  P.k = AttnSide{cache->k, cache->k_page, cache->k_token, cache->k_head};
+  P.v = AttnSide{cache->v, cache->v_page, cache->v_token, cache->v_head};
+  P.num_pages = cache->num_pages;
+  P.page_size = cache->page_size;
+  P.page_shift = -1;
+  for (int s = 0; s < 31; ++s)
+    if (cache->page_size == (1 << s)) P.page_shift = s;
+  P.table = table;
+  P.ld_table = ld_table ? ld_table : table_cols;
+  P.kv_lens = kv_lens;
+  P.q_starts = q_starts;
+  P.seqs = seqs;
+  P.T = T;
+  P.max_q = (int64_t)max_q < T ? max_q : (int)T;
+  P.max_keys = (int64_t)table_cols * cache->page_size < max_kv ? (int64_t)table_cols * cache->page_size : max_kv;
+  P.heads_q = heads_q;
+  P.heads_kv = cache->heads;
+  P.group = heads_q / cache->heads;
+  P.head_dim = cache->head_dim;
+  P.c = scale * (cache->e4m3 ? cache->k_scale : 1.0f) * 1.44269504088896340736f;
+  P.v_scale = cache->e4m3 ? cache->v_scale : 1.0f;
+  P.causal = causal;
+  P.window = window;
+  P.lse = lse;
+  P.tok_per_tile = plan.tok_per_tile;
+  P.tiles_per_item = plan.tiles_per_item;
+  P.q_items = plan.q_items;
+  P.splits = plan.splits;
+  P.chunk_tiles = plan.chunk_tiles;
+  P.error = dev->ring_error;
+  if (plan.splits > 1) {
+    P.part_o = (float*)ws;
+    P.part_z = (float*)((char*)ws + ((int64_t)plan.splits * T * heads_q * cache->head_dim * 4 + 15) / 16 * 16);
+  }
+
+  if (!plan.tc) {
+    AttnKernel gen = attn_general_kernel_for(cache->e4m3 != 0);
+    int bres = 1;
+    rc = resident_blocks((const void*)gen, kAttnGeneralThreads, 0, &bres);
+    if (rc != QKNORM_OK) return rc;
+    long long grid = (long long)bres * dev->sm_count;
+    const long long want = ((long long)seqs * P.max_q * heads_q + kAttnGeneralThreads / 32 - 1) / (kAttnGeneralThreads / 32);
+    if (grid > want) grid = want;
+    const cudaError_t e = launch_overlapped(gen, (unsigned)grid, (unsigned)kAttnGeneralThreads, 0, stream, P);
+    if (e != cudaSuccess) return set_cuda_error(e);
+    return finish_launch("attn_general");
+  }
+  int smem = 0;
+  AttnKernel fn = attn_tc_for(cache->head_dim <= 64 ? 64 : 128, cache->e4m3 != 0, plan.tiles_per_item == 1, &smem);
+  rc = allow_dynamic_smem((const void*)fn, smem);
+  if (rc != QKNORM_OK) return rc;
+  rc = attn_tc_registers_ok((const void*)fn);
+  if (rc != QKNORM_OK) return rc;
+  const long long join_warps = (long long)seqs * P.max_q * heads_q;
+  const long long join_ctas = (join_warps + kAttnJoinThreads / 32 - 1) / (kAttnJoinThreads / 32);
+  if (plan.splits > 1 && join_ctas > 0x7fffffff) return QKNORM_ERR_SHAPE;
+  long long grid = (long long)plan.q_items * seqs * cache->heads * plan.splits;
+  if (grid > dev->sm_count) grid = dev->sm_count;
+  cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P);
+  if (e != cudaSuccess) return set_cuda_error(e);
+  rc = finish_launch("attn_tc");
+  if (rc != QKNORM_OK || plan.splits <= 1) return rc;
+  e = launch_overlapped(attn_join_kernel_for(), (unsigned)join_ctas, (unsigned)kAttnJoinThreads, 0, stream, P);
+  if (e != cudaSuccess) return set_cuda_error(e);
+  return finish_launch("attn_tc");
+}

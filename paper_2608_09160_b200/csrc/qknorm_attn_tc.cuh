@@ -1,0 +1,834 @@
+// Attention over a paged cache on the tensor cores (tcgen05, accumulators in TMEM).
+//
+// A persistent CTA per SM walks over items: the query rows of one sequence that share a key head -- tokens
+// times the group's query heads, packed into tiles of 128 rows -- and a range of key tiles of 128 keys.
+//   warps 0-7    two softmax warpgroups; a thread owns a row of a 128 x 128 score tile
+//   warps 8-11   loaders: gather K and V rows through the page table into a ring of shared-memory tiles
+//   warp 12      issues every tcgen05.mma
+// Scores S_w = Q K^T land in TMEM (128 columns per warpgroup w).  The warpgroup reads them, keeps the running
+// maximum and sum in registers, writes P = 2^(c (s - m)) back over S in 16 bits, and O_w += P V takes P from
+// TMEM and V, keys by head_dim as it lies in the cache, as a transposed operand.  O_w stays in TMEM; it is rescaled only
+// when the maximum has grown by more than 2^8, so P is at most 2^8 and the rescale is rare.
+//
+// Two forms:
+//   two query tiles  (chunks): tile w belongs to warpgroup w, both use every K and V tile;
+//   one query tile   (single tokens, short chunks): key tiles alternate between the warpgroups, each with an O of its
+//                    own over the same rows, joined through TMEM at the end of the item.
+// Both keep the tensor pipe on one warpgroup's tile while the other one is in its exponentials.
+//
+// Rows no token fills, keys outside the item's range and head_dim up to the next multiple of 64 are zeros in
+// shared memory, never memory of somebody else.  Inside a tile that the causal edge or the window cuts, a V row with an
+// infinity or a NaN would reach rows that do not see it (0 * inf): the loader looks at the V rows of such
+// tiles and, if it finds one, has the item's rows done again one by one by attn_row.
+//
+// FP8 cache: K and V are staged raw and widened to fp16, which holds every E4M3 value exactly; Q is
+// brought to fp16 with a power of two per row, which loses nothing but parts below 2^-30 of the row's largest element.
+//
+// Rounding: P to bf16 (fp16 with an FP8 cache), half a step of it relative, is the one rounding besides the output's;
+// sums, maxima and O are fp32.
+#pragma once
+#include "qknorm_attn.cuh"
+
+namespace qknorm {
+
+namespace tc {
+
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46) |
+         (2ull << 61);  // 128-byte swizzle
+}
+// fp32 accumulators, both operands bf16 (or both fp16), M = 128
+__host__ __device__ constexpr uint32_t instr_desc(int n, bool f16, bool b_transposed) {
+  return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((b_transposed ? 1u : 0u) << 16) |
+         ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+#define QKNORM_R8(m, i) m(i), m(i + 1), m(i + 2), m(i + 3), m(i + 4), m(i + 5), m(i + 6), m(i + 7)
+// 32 columns of this lane's row
+__device__ __forceinline__ void ld32(uint32_t addr, uint32_t* r) {
+#define QKNORM_O(i) "=r"(r[i])
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : QKNORM_R8(QKNORM_O, 0), QKNORM_R8(QKNORM_O, 8), QKNORM_R8(QKNORM_O, 16), QKNORM_R8(QKNORM_O, 24)
+      : "r"(addr));
+#undef QKNORM_O
+}
+__device__ __forceinline__ void st32(uint32_t addr, const uint32_t* r) {
+#define QKNORM_I(i) "r"(r[i])
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::QKNORM_R8(QKNORM_I, 0),
+      QKNORM_R8(QKNORM_I, 8), QKNORM_R8(QKNORM_I, 16), QKNORM_R8(QKNORM_I, 24), "r"(addr)
+      : "memory");
+#undef QKNORM_I
+}
+#undef QKNORM_R8
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// 16 bytes from global to shared memory, or 16 zero bytes
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool take) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+}  // namespace tc
+
+// Shared memory, byte offsets from a 1024-byte aligned base.
+template <int DP, bool F8>
+struct AttnSmem {
+  static constexpr int kTile = kAttnTile * DP * 2;  // a 16-bit tile of Q, K or V
+  static constexpr int kRaw = kAttnTile * DP;       // a staged FP8 tile
+  static constexpr int kStages = F8 ? (DP == 128 ? 3 : 6) : (DP == 128 ? 5 : 10);
+  static constexpr int kRawStages = F8 ? 4 : 0;
+  static constexpr int kLag = F8 ? kRawStages - 1 : kStages - 2;  // tiles in flight behind the newest
+  static constexpr int kQ0 = 0;                                   // two Q tiles
+  static constexpr int kRing = 2 * kTile;
+  static constexpr int kRawRing = kRing + kStages * kTile;
+  static constexpr int kFull = kRawRing + kRawStages * kRaw;  // mbarriers, 8 bytes each
+  static constexpr int kEmpty = kFull + 8 * kStages;
+  static constexpr int kQFull = kEmpty + 8 * kStages;
+  static constexpr int kQEmpty = kQFull + 16;
+  static constexpr int kSFull = kQEmpty + 16;
+  static constexpr int kPFull = kSFull + 16;
+  static constexpr int kOFull = kPFull + 16;
+  static constexpr int kOFree = kOFull + 16;
+  static constexpr int kMl = kOFree + 16;
+  static constexpr int kMlFree = kMl + 8;
+  static constexpr int kDrain = kMlFree + 8;
+  static constexpr int kTmem = kDrain + 8;            // TMEM base address
+  static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
+  static constexpr int kPoison = kAbort + 4;          // [4] 1 + number of an item that holds a V row to be careful with
+  // FP8 cache: [4][128] bytes, the exponent taken out of a Q row (0: none).  Four sets, because a set is read until the
+  // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
+  // round again only after the tensor warp has seen the scores of the item before last consumed.
+  static constexpr int kQScale = kPoison + 16;
+  static constexpr int kMlRows = kQScale + (F8 ? 512 : 0);  // [2][128] float2, one-tile form: the warpgroups' (m, l)
+  static constexpr int kBytes = kMlRows + 2048;
+};
+static_assert(AttnSmem<128, false>::kBytes <= 232448 && AttnSmem<128, true>::kBytes <= 232448, "shared memory of one CTA");
+
+// Key tiles [a, b) that query tile w of the item uses, and how its rows' ranges spread.
+struct AttnTileRange {
+  int a, b;
+  int rows;            // rows in use
+  int hi_min, lo_max;  // end of the first token's keys, start of the last token's
+};
+__device__ __forceinline__ AttnTileRange attn_tile_range(const AttnParams& P, const AttnItem& it, int w) {
+  AttnTileRange r;
+  const int t0 = it.tok0 + w * P.tok_per_tile;
+  const int t1 = t0 + P.tok_per_tile < it.s.n ? t0 + P.tok_per_tile : it.s.n;
+  r.a = r.b = r.rows = r.hi_min = r.lo_max = 0;
+  if (t0 >= t1) return r;
+  r.rows = (t1 - t0) * P.group;
+  r.hi_min = attn_hi(P, it.s, t0);
+  r.lo_max = attn_lo(P, it.s, t1 - 1);
+  const int lo = attn_lo(P, it.s, t0), hi = attn_hi(P, it.s, t1 - 1);
+  if (hi <= lo) return r;
+  const int a = lo / kAttnTile, b = (hi + kAttnTile - 1) / kAttnTile;
+  r.a = a > it.j0 ? a : it.j0;
+  r.b = b < it.j1 ? b : it.j1;
+  if (r.b <= r.a) r.a = r.b = 0;
+  return r;
+}
+// Does the causal edge or the window cut through this tile's keys in use for some row of the query tile?
+__device__ __forceinline__ bool attn_cut(const AttnItem& it, const AttnTileRange& r, int j) {
+  const int k0 = j * kAttnTile, k1 = k0 + kAttnTile;
+  return j >= r.a && j < r.b && ((k1 < it.uhi ? k1 : it.uhi) > r.hi_min || (k0 > it.ulo ? k0 : it.ulo) < r.lo_max);
+}
+
+template <int DP, bool F8, bool ONE>
+struct AttnTc {
+  using L = AttnSmem<DP, F8>;
+  static constexpr int kHalf = kAttnTile * 128;  // bytes of a 64-column half of a tile
+
+  const AttnParams& P;
+  uint32_t smem;
+  unsigned char* smem_ptr;
+  long long items;
+
+  __device__ __forceinline__ volatile int* abort_flag() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kAbort); }
+  __device__ __forceinline__ volatile int* poison() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kPoison); }
+
+  // Bounded (two seconds); false: leave.
+  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
+    if (ptx::mbar_try_wait(bar, parity)) return true;
+    return wait_slow(bar, parity);
+  }
+  __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity) const {
+    const unsigned long long t0 = ptx::globaltimer_ns();
+    while (!ptx::mbar_try_wait(bar, parity)) {
+      if (*abort_flag()) return false;
+      if (ptx::globaltimer_ns() - t0 > 2000000000ull) {
+        *abort_flag() = 1;
+        *P.error = 7;
+        return false;
+      }
+    }
+    return true;
+  }
+  // Without a look at the abort flag: what is waited for is on its way whatever else happened.
+  __device__ __forceinline__ void wait_drain() const {
+    const unsigned long long t0 = ptx::globaltimer_ns();
+    while (!ptx::mbar_try_wait(smem + L::kDrain, 0))
+      if (ptx::globaltimer_ns() - t0 > 2000000000ull) {
+        *P.error = 9;
+        return;
+      }
+  }
+  __device__ __forceinline__ uint32_t full(uint32_t pos) const { return smem + L::kFull + 8 * (pos % L::kStages); }
+  __device__ __forceinline__ uint32_t empty(uint32_t pos) const { return smem + L::kEmpty + 8 * (pos % L::kStages); }
+  __device__ __forceinline__ uint32_t stage(uint32_t pos) const { return smem + L::kRing + (pos % L::kStages) * L::kTile; }
+
+  // ---- loaders --------------------------------------------------------------------------------------
+  static constexpr int kChunks = F8 ? DP / 16 : DP / 8;  // 16-byte pieces of a stored row
+  static constexpr int kRowStep = 128 / kChunks;
+
+  struct Loader {
+    uint32_t pos = 0;      // tiles issued
+    int pending = 0;       // issued, not signalled
+    uint64_t qbits = 0;    // per pending tile, oldest lowest, 4 bits: which Q tiles travel with it
+    int cut_item = -1;     // the newest pending tile is V and cut: look through it, name this item
+  };
+
+  __device__ __forceinline__ void signal(uint32_t bar, int lane) const {
+    ptx::fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) tc::arrive(bar);
+  }
+
+  // The oldest pending tile has arrived (its cp.async group is complete): hand it over.
+  __device__ __forceinline__ bool hand_over(Loader& ld, int tid) const {
+    const int lane = tid & 31;
+    const uint32_t pos = ld.pos - ld.pending;
+    const bool look = ld.cut_item >= 0 && ld.pending == 1;
+    bool bad = false;
+    if constexpr (F8) {
+      if (pos >= (uint32_t)L::kStages && !wait(empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
+      const uint32_t raw = smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16;
+      const int c = tid % kChunks, r0 = tid / kChunks;
+      const uint32_t dst = stage(pos) + (c >> 2) * kHalf;
+      const int cc = (2 * c) & 7;
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        const int r = r0 + i * kRowStep;
+        const uint4 v = ptx::lds128(raw + i * 2048);
+        uint32_t h[8];
+        e4m3x4_to_f16x2(v.x, h[0], h[1]);
+        e4m3x4_to_f16x2(v.y, h[2], h[3]);
+        e4m3x4_to_f16x2(v.z, h[4], h[5]);
+        e4m3x4_to_f16x2(v.w, h[6], h[7]);
+        if (look) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) bad |= (h[e] & 0x7c00u) == 0x7c00u || (h[e] & 0x7c000000u) == 0x7c000000u;
+        }
+        const uint32_t row = dst + r * 128;
+        tc::sts128(row + ((cc ^ (r & 7)) << 4), h[0], h[1], h[2], h[3]);
+        tc::sts128(row + (((cc + 1) ^ (r & 7)) << 4), h[4], h[5], h[6], h[7]);
+      }
+    } else if (look) {
+      const int c = tid % kChunks, r0 = tid / kChunks;
+      const uint32_t at = stage(pos) + (c >> 3) * kHalf + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        const uint4 v = ptx::lds128(at + i * kRowStep * 128);
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bad |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
+      }
+    }
+    if (look) {
+      if (bad) poison()[ld.cut_item & 3] = ld.cut_item + 1;
+      ld.cut_item = -1;
+    }
+    signal(full(pos), lane);
+    if (lane == 0) {
+      if (ld.qbits & 1) tc::arrive(smem + L::kQFull);
+      if (ld.qbits & 2) tc::arrive(smem + L::kQFull + 8);
+    }
+    ld.qbits >>= 4;
+    --ld.pending;
+    return true;
+  }
+  __device__ __forceinline__ bool flush(Loader& ld, int tid) const {
+    tc::cp_wait<0>();
+    while (ld.pending > 0)
+      if (!hand_over(ld, tid)) return false;
+    return true;
+  }
+  // Waits, but never while sitting on tiles that somebody else waits for.
+  __device__ __forceinline__ bool wait_or_flush(Loader& ld, int tid, uint32_t bar, uint32_t parity) const {
+    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+    return flush(ld, tid) && wait(bar, parity);
+  }
+
+  // One K or V tile: rows key0 .. key0+127, those outside [ulo, uhi) zeros.
+  __device__ __forceinline__ bool load_tile(Loader& ld, int tid, const AttnItem& it, const AttnSide& side, int key0, int qbits) const {
+    const uint32_t pos = ld.pos;
+    if constexpr (!F8) {
+      if (pos >= (uint32_t)L::kStages && !wait_or_flush(ld, tid, empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
+    }
+    const int c = tid % kChunks, r0 = tid / kChunks;
+    const bool in_head = c * (F8 ? 16 : 8) < P.head_dim;
+    uint32_t dst = F8 ? smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16
+                      : stage(pos) + (c >> 3) * kHalf + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
+    const char* base = reinterpret_cast<const char*>(side.base);
+    const long long in_row = (long long)it.kvh * side.head + c * (F8 ? 16 : 8);
+#pragma unroll 4
+    for (int i = 0; i < kChunks; ++i) {
+      const int key = key0 + r0 + i * kRowStep;
+      const char* src = base;
+      bool take = in_head && key >= it.ulo && key < it.uhi;
+      if (take) {
+        int within;
+        const long long page = attn_page(P, it.b, key, within);
+        take = page >= 0;
+        if (take) src = base + (page * side.page + within * side.token + in_row) * (F8 ? 1 : 2);
+      }
+      tc::cp16(dst + (F8 ? i * 2048 : i * kRowStep * 128), src, take);
+    }
+    tc::cp_commit();
+    ++ld.pos;
+    ld.qbits |= (uint64_t)qbits << (4 * ld.pending);
+    ++ld.pending;
+    if (ld.pending > L::kLag) {
+      tc::cp_wait<L::kLag>();
+      return hand_over(ld, tid);
+    }
+    return true;
+  }
+
+  // Query tile of `rows` rows from token tok0 into Q buffer `buf`.
+  __device__ __forceinline__ void load_q(int tid, const AttnItem& it, int tok0, int rows, int buf, int scale_set) const {
+    constexpr int kQChunks = DP / 8, kStep = 128 / kQChunks;
+    const int c = tid % kQChunks, r0 = tid / kQChunks;
+    const uint32_t dst = smem + L::kQ0 + buf * L::kTile + (c >> 3) * kHalf + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
+    const bool in_head = c * 8 < P.head_dim;
+    for (int i = 0; i < kQChunks; ++i) {
+      const int r = r0 + i * kStep;
+      const int tok = (int)((unsigned)r / (unsigned)P.group), g = r - tok * P.group;
+      const bool take = in_head && r < rows;
+      const uint16_t* src = P.q;
+      if (take)
+        src += (it.s.row0 + (long long)(tok0 + tok)) * P.ld_q + (long long)(it.kvh * P.group + g) * P.head_dim + c * 8;
+      if constexpr (!F8) {
+        tc::cp16(dst + i * kStep * 128, src, take);
+      } else {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (take) v = *reinterpret_cast<const uint4*>(src);
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+        uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t lo = u[e] & 0x7fffu, hi = (u[e] >> 16) & 0x7fffu;
+          mag = max(mag, max(lo, hi));
+        }
+#pragma unroll
+        for (int off = kQChunks / 2; off > 0; off >>= 1) mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, off));
+        // bring the row's largest exponent to 2^8; rows of zeros, tiny rows and rows with infinities or NaN as they are
+        const int e = (int)(mag >> 7);
+        const bool scaled = e > 16 && e < 255;
+        const float f = scaled ? __uint_as_float((uint32_t)(127 + 135 - e) << 23) : 1.f;
+        uint32_t h[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
+        tc::sts128(dst + i * kStep * 128, h[0], h[1], h[2], h[3]);
+        if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void run_loader(int tid) const {
+    Loader ld;
+    uint32_t quse[2] = {0, 0};
+    int count = 0;  // items with keys
+    bool ok = true;
+    for (long long idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
+      AttnItem it;
+      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+      const AttnTileRange r0 = attn_tile_range(P, it, 0);
+      AttnTileRange r1 = r0;
+      if (!ONE) r1 = attn_tile_range(P, it, 1);
+      int qbits = 0;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if (ONE ? w != (count & 1) : (w == 0 ? r0.a >= r0.b : r1.a >= r1.b)) continue;
+        if (quse[w] > 0 && !(ok = wait_or_flush(ld, tid, smem + L::kQEmpty + 8 * w, (quse[w] - 1) & 1))) break;
+        load_q(tid, it, it.tok0 + (ONE ? 0 : w * P.tok_per_tile), w == 0 || ONE ? r0.rows : r1.rows, w,
+               ONE ? count & 3 : w + 2 * (quse[w] & 1));
+        ++quse[w];
+        qbits |= 1 << w;
+      }
+      if (!ok) break;
+      for (int j = it.j0; j < it.j1; ++j) {
+        ok = load_tile(ld, tid, it, P.k, j * kAttnTile, j == it.j0 ? qbits : 0);
+        if (!ok) break;
+        const bool cut = attn_cut(it, r0, j) || (!ONE && attn_cut(it, r1, j));
+        if (cut && !(ok = flush(ld, tid))) break;
+        if (cut) ld.cut_item = count;
+        ok = load_tile(ld, tid, it, P.v, j * kAttnTile, 0);
+        if (!ok) break;
+        if (cut && !(ok = flush(ld, tid))) break;
+      }
+      ++count;
+    }
+    if (ok) flush(ld, tid);
+    tc::cp_wait<0>();
+  }
+
+  // ---- tensor-core issue ----------------------------------------------------------------------------
+  __device__ __forceinline__ void issue_qk(uint32_t tmem, int w, int qbuf, uint32_t pos) const {
+    constexpr uint32_t idesc = tc::instr_desc(kAttnTile, F8, false);
+    const uint32_t q = smem + L::kQ0 + qbuf * L::kTile, k = stage(pos);
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {  // 16 columns of head_dim: 32 bytes inside the 128-byte swizzle span
+      const uint32_t off = (s >> 2) * kHalf + (s & 3) * 32;
+      tc::mma_ss(tmem + w * kAttnTile, tc::smem_desc(q + off, 16, 1024), tc::smem_desc(k + off, 16, 1024), idesc, s > 0);
+    }
+    tc::commit(smem + L::kSFull + 8 * w);
+  }
+  __device__ __forceinline__ void issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc) const {
+    constexpr uint32_t idesc = tc::instr_desc(DP, F8, true);
+    const uint32_t v = stage(pos);
+#pragma unroll
+    for (int s = 0; s < kAttnTile / 16; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
+      tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, tc::smem_desc(v + s * 2048, kHalf, 1024), idesc,
+                 acc || s > 0);
+  }
+
+  __device__ __forceinline__ void run_mma(uint32_t tmem) const {
+    uint32_t pos = 0, count = 0;
+    uint32_t quse[2] = {0, 0}, puse[2] = {0, 0}, ouse[2] = {0, 0};
+    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+      AttnItem it;
+      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+      const int nt = it.j1 - it.j0;
+      if (ONE) {
+        const int qb = count & 1;
+        for (int r = -2; r < nt; ++r) {
+          const int w = r & 1;
+          if (r >= 0) {
+            const uint32_t vp = pos + 2 * r + 1;
+            if (!wait(full(vp), (vp / L::kStages) & 1)) return;
+            if (!wait(smem + L::kPFull + 8 * w, puse[w] & 1)) return;
+            ++puse[w];
+            if (r < 2 && ouse[w] > 0 && !wait(smem + L::kOFree + 8 * w, (ouse[w] - 1) & 1)) return;
+            tc::fence_after();
+            issue_pv(tmem, w, vp, r >= 2);
+            tc::commit(empty(vp));
+            if (r + 2 >= nt) {
+              tc::commit(smem + L::kOFull + 8 * w);
+              ++ouse[w];
+            }
+          }
+          if (r + 2 < nt) {
+            const uint32_t kp = pos + 2 * (r + 2);
+            if (r == -2) {
+              if (!wait(smem + L::kQFull + 8 * qb, quse[qb] & 1)) return;
+              ++quse[qb];
+            }
+            if (!wait(full(kp), (kp / L::kStages) & 1)) return;
+            tc::fence_after();
+            issue_qk(tmem, w, qb, kp);
+            tc::commit(empty(kp));
+            if (r + 2 == nt - 1) tc::commit(smem + L::kQEmpty + 8 * qb);
+          }
+        }
+      } else {
+        AttnTileRange rg[2] = {attn_tile_range(P, it, 0), attn_tile_range(P, it, 1)};
+        for (int j = it.j0 - 1; j < it.j1; ++j) {
+          const uint32_t kp = pos + 2 * (j + 1 - it.j0), vp = kp - 1;
+          if (j >= it.j0 && !wait(full(vp), (vp / L::kStages) & 1)) return;
+          bool have_k = false;
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            if (j >= rg[w].a && j < rg[w].b) {
+              if (!wait(smem + L::kPFull + 8 * w, puse[w] & 1)) return;
+              ++puse[w];
+              if (j == rg[w].a && ouse[w] > 0 && !wait(smem + L::kOFree + 8 * w, (ouse[w] - 1) & 1)) return;
+              tc::fence_after();
+              issue_pv(tmem, w, vp, j > rg[w].a);
+              if (j == rg[w].b - 1) {
+                tc::commit(smem + L::kOFull + 8 * w);
+                ++ouse[w];
+              }
+            }
+            if (j + 1 >= rg[w].a && j + 1 < rg[w].b) {
+              if (j + 1 == rg[w].a) {
+                if (!wait(smem + L::kQFull + 8 * w, quse[w] & 1)) return;
+                ++quse[w];
+              }
+              if (!have_k && !wait(full(kp), (kp / L::kStages) & 1)) return;
+              have_k = true;
+              tc::fence_after();
+              issue_qk(tmem, w, w, kp);
+              if (j + 1 == rg[w].b - 1) tc::commit(smem + L::kQEmpty + 8 * w);
+            }
+          }
+          if (j >= it.j0) tc::commit(empty(vp));
+          if (j + 1 < it.j1) {
+            if (!have_k && !wait(full(kp), (kp / L::kStages) & 1)) return;
+            tc::commit(empty(kp));
+          }
+        }
+      }
+      pos += 2 * nt;
+      ++count;
+    }
+  }
+
+  // c of this row's scores: an FP8 cache's Q rows had an exponent taken out
+  __device__ __forceinline__ float row_c(int set, int row) const {
+    const int e = reinterpret_cast<const volatile unsigned char*>(smem_ptr + L::kQScale)[set * 128 + row];
+    return e == 0 ? P.c : ldexpf(P.c, e - 135);
+  }
+
+  // ---- softmax --------------------------------------------------------------------------------------
+  // O columns of this lane's row times f
+  __device__ __forceinline__ void rescale(uint32_t o, float f) const {
+#pragma unroll
+    for (int k = 0; k < DP; k += 32) {
+      uint32_t r[32];
+      tc::ld32(o + k, r);
+      tc::wait_ld();
+#pragma unroll
+      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+      tc::st32(o + k, r);
+    }
+  }
+  // 32 columns of the result of a row
+  __device__ __forceinline__ void store32(const float* x, long long row, int head, int split, int col) const {
+    if (P.splits > 1) {
+      float* o = P.part_o + (((long long)split * P.T + row) * P.heads_q + head) * P.head_dim + col;
+#pragma unroll
+      for (int e = 0; e < 32; e += 4)
+        if (col + e < P.head_dim) *reinterpret_cast<float4*>(o + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+    } else {
+      uint16_t* o = P.out + row * P.ld_out + (long long)head * P.head_dim + col;
+#pragma unroll
+      for (int e = 0; e < 32; e += 8)
+        if (col + e < P.head_dim)
+          *reinterpret_cast<uint4*>(o + e) = make_uint4(bf_pack(x[e], x[e + 1]), bf_pack(x[e + 2], x[e + 3]),
+                                                        bf_pack(x[e + 4], x[e + 5]), bf_pack(x[e + 6], x[e + 7]));
+    }
+  }
+  __device__ __forceinline__ void store_z(float z, long long row, int head, int split) const {
+    if (P.splits > 1) P.part_z[((long long)split * P.T + row) * P.heads_q + head] = z;
+    else if (P.lse != nullptr) P.lse[row * P.heads_q + head] = z * kLn2;
+  }
+  // The rows of this warp again, one by one, each from the keys it sees and no others.
+  __device__ __forceinline__ void redo(const AttnItem& it, int tok0, int rows, int first) const {
+    const int lane = threadIdx.x & 31;
+    for (int r = first; r < first + 32 && r < rows; ++r) {
+      const int i = tok0 + r / P.group, head = it.kvh * P.group + r % P.group;
+      const long long row = it.s.row0 + (long long)i;
+      int lo = attn_lo(P, it.s, i), hi = attn_hi(P, it.s, i);
+      lo = lo > it.j0 * kAttnTile ? lo : it.j0 * kAttnTile;
+      hi = hi < it.j1 * kAttnTile ? hi : it.j1 * kAttnTile;
+      float o[DP / 32], z;
+      if (F8) attn_row<IoE4m3, DP / 32>(P, it.b, row, head, lo, hi, o, z);
+      else attn_row<IoBf16, DP / 32>(P, it.b, row, head, lo, hi, o, z);
+#pragma unroll
+      for (int e = 0; e < DP / 32; ++e) {
+        const int d = lane + 32 * e;
+        if (d < P.head_dim) {
+          if (P.splits > 1) P.part_o[(((long long)it.split * P.T + row) * P.heads_q + head) * P.head_dim + d] = o[e];
+          else IoBf16::store(P.out, row * P.ld_out + (long long)head * P.head_dim + d, o[e] * P.v_scale);
+        }
+      }
+      if (lane == 0) store_z(z, row, head, it.split);
+    }
+  }
+
+  // One score tile: S -> P, running m and l of this lane's row.
+  __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int k0, int lo, int hi, bool masked, bool first, float c,
+                                       float& m, float& l) const {
+    float s[kAttnTile];
+#pragma unroll
+    for (int k = 0; k < kAttnTile; k += 32) tc::ld32(s_addr + k, reinterpret_cast<uint32_t*>(s) + k);
+    tc::wait_ld();
+    if (masked) {
+      const int a = lo - k0, b = hi - k0;
+#pragma unroll
+      for (int k = 0; k < kAttnTile; ++k) s[k] = k >= a && k < b ? s[k] : kNegInf;
+    }
+    float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+    for (int k = 4; k < kAttnTile; k += 4) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[k + e]);
+    }
+    const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    // m is the maximum that the exponents are taken against; it follows the true one when that is 2^8 ahead
+    const bool grow = mn > m && (m == kNegInf || (mn - m) * c > 8.f);
+    if (__any_sync(0xffffffffu, grow)) {
+      const float f = !grow ? 1.f : m == kNegInf ? 0.f : tc::ex2((m - mn) * c);
+      if (grow) {
+        l = m == kNegInf ? l : l * f;
+        m = mn;
+      }
+      if (!first) rescale(o_addr, f);
+    }
+    const float mc = m == kNegInf ? 0.f : m * c;
+    const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t p[32];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const int k = h * 64 + 2 * e;
+        float2 x = __ffma2_rn(make_float2(s[k], s[k + 1]), c2, mc2);
+        x.x = tc::ex2(x.x);
+        x.y = tc::ex2(x.y);
+        sum[e & 1] = __fadd2_rn(sum[e & 1], x);
+        p[e] = F8 ? tc::pack_f16(x.x, x.y) : bf_pack(x.x, x.y);
+      }
+      tc::st32(s_addr + h * 32, p);
+    }
+    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+    tc::wait_st();
+    tc::fence_before();
+  }
+
+  __device__ __forceinline__ void run_softmax(uint32_t tmem, int w) const {
+    const int wtid = threadIdx.x & 127, lane = threadIdx.x & 31, first_row = wtid & ~31;
+    const uint32_t lanes = (uint32_t)first_row << 16;  // a warp reaches the 32 TMEM lanes of its place in the warpgroup
+    const uint32_t s_addr = tmem + lanes + w * kAttnTile, o_addr = tmem + lanes + 2 * kAttnTile + w * DP;
+    uint32_t suse = 0, ouse[2] = {0, 0}, mluse = 0;
+    int count = 0;
+    const uint32_t all = 0xffffffffu;
+    float2* ml = reinterpret_cast<float2*>(smem_ptr + L::kMlRows);
+    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+      AttnItem it;
+      if (!attn_item(P, idx, it)) continue;
+      const AttnTileRange rg = attn_tile_range(P, it, ONE ? 0 : w);
+      const int tok0 = it.tok0 + (ONE ? 0 : w * P.tok_per_tile);
+      const int i = tok0 + wtid / P.group, head = it.kvh * P.group + wtid % P.group;
+      const bool valid = wtid < rg.rows;
+      const bool busy = first_row < rg.rows;  // some row of this warp is in use
+      const long long row = it.s.row0 + (long long)i;
+      const bool keys = it.j0 < it.j1;
+      const int step = ONE ? 2 : 1;
+      float m = kNegInf, l = 0.f, c = P.c;
+      if (keys) {
+        const int lo = valid ? attn_lo(P, it.s, i) : 0, hi = valid ? attn_hi(P, it.s, i) : 0;
+        for (int j = ONE ? it.j0 + w : rg.a; j < (ONE ? it.j1 : rg.b); j += step) {
+          if (!__all_sync(all, wait(smem + L::kSFull + 8 * w, suse & 1))) return;
+          ++suse;
+          if (busy) {
+            tc::fence_after();
+            if (F8) c = row_c(ONE ? count & 3 : w + 2 * (ouse[w] & 1), wtid);
+            const int k0 = j * kAttnTile;
+            const bool masked = k0 < rg.lo_max || k0 + kAttnTile > rg.hi_min;
+            tile(s_addr, o_addr, k0, lo, hi, masked, j == (ONE ? it.j0 + w : rg.a), c, m, l);
+          }
+          __syncwarp();
+          if (lane == 0) tc::arrive(smem + L::kPFull + 8 * w);
+        }
+      }
+      if (!ONE) {
+        if (rg.a < rg.b) {
+          if (!__all_sync(all, wait(smem + L::kOFull + 8 * w, ouse[w] & 1))) return;
+          ++ouse[w];
+          tc::fence_after();
+        }
+        const bool again = keys && poison()[count & 3] == count + 1;
+        if (busy && !again) {
+          const float inv = l == 0.f ? 0.f : (P.splits > 1 ? 1.f : P.v_scale) / l;
+#pragma unroll
+          for (int k = 0; k < DP; k += 32) {
+            uint32_t o[32];
+            float x[32];
+            if (rg.a < rg.b) {
+              tc::ld32(o_addr + k, o);
+              tc::wait_ld();
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
+            if (valid && !(P.splits > 1 && l == 0.f)) store32(x, row, head, it.split, k);
+          }
+          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), row, head, it.split);
+        }
+        if (again && busy) redo(it, tok0, rg.rows, first_row);
+        if (rg.a < rg.b) {
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) tc::arrive(smem + L::kOFree + 8 * w);
+        }
+      } else if (!keys) {
+        if (w == 0 && valid) {
+          float x[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = 0.f;
+          if (P.splits == 1)
+            for (int k = 0; k < DP; k += 32) store32(x, row, head, 0, k);
+          store_z(kNegInf, row, head, it.split);
+        }
+      } else {
+        // the two warpgroups' parts of the same rows
+        const bool two = it.j1 - it.j0 > 1;
+        if (mluse > 0 && !__all_sync(all, wait(smem + L::kMlFree, (mluse - 1) & 1))) return;
+        ml[w * 128 + wtid] = make_float2(m, l);
+        __syncwarp();
+        if (lane == 0) tc::arrive(smem + L::kMl);
+        if (!__all_sync(all, wait(smem + L::kMl, mluse & 1))) return;
+        const float2 p0 = ml[wtid], p1 = ml[128 + wtid];
+        __syncwarp();
+        if (lane == 0) tc::arrive(smem + L::kMlFree);
+        ++mluse;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          if (k == 1 && !two) break;
+          if (!__all_sync(all, wait(smem + L::kOFull + 8 * k, ouse[k] & 1))) return;
+          ++ouse[k];
+        }
+        tc::fence_after();
+        const bool again = poison()[count & 3] == count + 1;
+        if (busy && !again) {
+          if (F8) c = row_c(count & 3, wtid);
+          const float mm = fmaxf(p0.x, p1.x);
+          // a part without keys counts nothing; one that met only NaN scores makes the row NaN
+          const float f0 = p0.x == kNegInf ? (p0.y != 0.f ? 1.f : 0.f) : tc::ex2((p0.x - mm) * c);
+          const float f1 = p1.x == kNegInf ? (p1.y != 0.f ? 1.f : 0.f) : tc::ex2((p1.x - mm) * c);
+          const float lt = fmaf(f0, p0.y, f1 * p1.y);
+          const float inv = (P.splits > 1 ? 1.f : P.v_scale) / lt;
+          const uint32_t o0 = tmem + lanes + 2 * kAttnTile, o1 = o0 + DP;
+#pragma unroll
+          for (int kk = 0; kk < DP / 2; kk += 32) {
+            const int k = w * (DP / 2) + kk;
+            uint32_t a[32], b[32];
+            tc::ld32(o0 + k, a);
+            if (two) tc::ld32(o1 + k, b);
+            tc::wait_ld();
+            float x[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float v = f0 == 0.f ? 0.f : f0 * __uint_as_float(a[e]);
+              if (two && f1 != 0.f) v = fmaf(f1, __uint_as_float(b[e]), v);
+              x[e] = lt == 0.f ? 0.f : v * inv;
+            }
+            if (valid && !(P.splits > 1 && lt == 0.f)) store32(x, row, head, it.split, k);
+          }
+          if (valid && w == 0) store_z(lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt)), row, head, it.split);
+        }
+        if (again && busy && w == 0) redo(it, tok0, rg.rows, first_row);
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          tc::arrive(smem + L::kOFree);
+          if (two) tc::arrive(smem + L::kOFree + 8);
+        }
+      }
+      if (keys) ++count;
+    }
+  }
+};
+
+template <int DP, bool F8, bool ONE>
+__global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams P) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  using K = AttnTc<DP, F8, ONE>;
+  using L = AttnSmem<DP, F8>;
+  const uint32_t smem = ptx::smem_u32(smem_raw);
+  const int warp = threadIdx.x >> 5;
+  if (smem & 1023u) {  // the swizzle counts on it; no other shared memory is declared, so this does not happen
+    if (threadIdx.x == 0) *P.error = 8;
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < L::kStages; ++i) {
+      ptx::mbar_init(smem + L::kFull + 8 * i, 4);
+      ptx::mbar_init(smem + L::kEmpty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(smem + L::kQFull + 8 * i, 4);
+      ptx::mbar_init(smem + L::kQEmpty + 8 * i, 1);
+      ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
+      ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
+      ptx::mbar_init(smem + L::kOFull + 8 * i, 1);
+      ptx::mbar_init(smem + L::kOFree + 8 * i, ONE ? 8 : 4);
+    }
+    ptx::mbar_init(smem + L::kMl, 8);
+    ptx::mbar_init(smem + L::kMlFree, 8);
+    ptx::mbar_init(smem + L::kDrain, 1);
+    *reinterpret_cast<volatile int*>(smem_raw + L::kAbort) = 0;
+    for (int i = 0; i < 4; ++i) reinterpret_cast<volatile int*>(smem_raw + L::kPoison)[i] = 0;
+    ptx::fence_barrier_init();
+    ptx::fence_proxy_async();
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem + L::kTmem) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    tc::fence_before();
+  }
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = *reinterpret_cast<const volatile uint32_t*>(smem_raw + L::kTmem);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  const long long items = (long long)P.q_items * P.seqs * P.heads_kv * P.splits;
+  const K k{P, smem, smem_raw, items};
+  // 512 threads start with 128 registers each; 2 x 200 + 72 + 40 = 4 x 128
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    k.run_softmax(tmem, warp >> 2);
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    k.run_loader(threadIdx.x - 256);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (threadIdx.x == 384) {
+      k.run_mma(tmem);
+      // every matrix operation has ended before the tiles and TMEM go away, whichever way the loop ended
+      tc::commit(smem + L::kDrain);
+      k.wait_drain();
+    }
+    __syncwarp();
+  }
+  tc::fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    tc::fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  }
+}
+
+}  // namespace qknorm

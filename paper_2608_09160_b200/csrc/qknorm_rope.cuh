@@ -1,0 +1,381 @@
+// Rotary positions, and the fused norm + rotation + write into a paged cache (include/qknorm_attn.h).
+//
+// One kernel template does both: a group of threads owns a token, reads its Q, K (and V) rows once into
+// registers, forms the statistic if there is a norm, rotates, and writes every element once.
+//
+// Mathematics.  The norm is Eq. 1 (layerwise) or its headwise form, as in the other kernels.  Pair
+// (a, b) of a head then turns by angle = position * inv_freq[i]: (a c - b s, b c + a s).  The angle is
+// formed in fp64 as a number of turns and reduced to [-1/2, 1/2] there -- position 10^6 times frequency 1
+// is 1.6e5 turns, of which fp32 keeps only 1/64 -- then cos and sin are taken in fp32.  The rot_dim/2 angles are the same
+// for every head, so a token's cos and sin are made once, in shared memory, not once per head.
+//
+// What bounds it: HBM traffic (each element read once, written once).  The unit of work is 16 elements of one
+// head, the two 8-element chunks whose elements pair up: chunks j and j + rot_dim/16 of the head in the
+// half layout, neighbours in the interleaved one and in the part that does not rotate.  So a pair never
+// crosses a thread, and in-place calls are safe: a unit is read and written by one thread.  A head takes the power of two
+// >= head_dim/16 lanes, which keeps the headwise sum a shuffle tree inside a lane group.
+// The layerwise sum is a shuffle tree plus one slot per warp; the barrier it needs is the one that
+// publishes cos and sin.
+#pragma once
+#include "qknorm_device.cuh"
+#include "qknorm_ring.cuh"  // ptx helpers
+
+namespace qknorm {
+
+struct RopeSide {
+  const void* x;          // [T, heads*head_dim]
+  void* y;                // the same, or nullptr where the result goes to the cache
+  const uint16_t* gamma;  // [heads*head_dim] bf16; nullptr without a norm
+  long long ldx, ldy;     // elements between rows
+  int heads;              // 0 = absent
+  float inv_d;            // 1 / (heads*head_dim)
+};
+
+struct CacheSide {
+  void* base;
+  long long page, token, head;  // strides, elements
+  float inv_scale;
+};
+
+struct RopeParams {
+  RopeSide q, k, v;  // v only with a cache
+  CacheSide ck, cv;
+  const long long* slots;
+  long long num_slots;  // num_pages * page_size
+  int page_size;
+  const long long* positions;
+  const double* inv_freq;
+  float mscale;
+  int rot_dim, interleaved;
+  double turns_sign;  // +-1 / (2 pi)
+  long long T;
+  int head_dim;
+  int log_lph;   // log2 of the lanes per head
+  int slots_per_token;  // (q.heads + k.heads + v.heads) << log_lph
+  int tokens_per_cta, threads_per_token;
+  float eps, inv_hd;
+};
+
+enum { kNormNone = 0, kNormLayer = 1, kNormHead = 2 };
+constexpr int kRopeMaxPairs = 256;  // QKNORM_MAX_HEAD_DIM / 2
+
+// cos and sin of pair i of the token at `pos`
+__device__ __forceinline__ float2 rope_cs(const RopeParams& R, long long pos, int i) {
+  double turns = (double)pos * R.inv_freq[i] * R.turns_sign;
+  turns -= rint(turns);
+  float s, c;
+  sincospif((float)(turns + turns), &s, &c);
+  return make_float2(c * R.mscale, s * R.mscale);
+}
+
+// 8 elements in fp32 <-> storage
+template <class IO>
+struct Chunk8;
+template <>
+struct Chunk8<IoBf16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const void* base, long long i) {
+    w = ld_stream(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(base) + i));
+  }
+  __device__ __forceinline__ void unpack(float* f) const {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[2 * e] = bf_lo(u[e]);
+      f[2 * e + 1] = bf_hi(u[e]);
+    }
+  }
+  static __device__ __forceinline__ void store(void* base, long long i, const float* f) {
+    const uint4 o = make_uint4(bf_pack(f[0], f[1]), bf_pack(f[2], f[3]), bf_pack(f[4], f[5]), bf_pack(f[6], f[7]));
+    st_stream(reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + i), o);
+  }
+};
+template <>
+struct Chunk8<IoE4m3> {
+  uint2 w;
+  __device__ __forceinline__ void load(const void* base, long long i) {
+    w = __ldcs(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(base) + i));
+  }
+  __device__ __forceinline__ void unpack(float* f) const {
+    const uint32_t u[2] = {w.x, w.y};
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint32_t f01, f23;
+      e4m3x4_to_f16x2(u[e], f01, f23);
+      const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&f01));
+      const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&f23));
+      f[4 * e] = a.x;
+      f[4 * e + 1] = a.y;
+      f[4 * e + 2] = b.x;
+      f[4 * e + 3] = b.y;
+    }
+  }
+  static __device__ __forceinline__ void store(void* base, long long i, const float* f) {
+    const uint2 o = make_uint2(e4m3_pack2(f[0], f[1]) | (e4m3_pack2(f[2], f[3]) << 16),
+                               e4m3_pack2(f[4], f[5]) | (e4m3_pack2(f[6], f[7]) << 16));
+    __stcs(reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(base) + i), o);
+  }
+};
+
+// Where element 0 of (token slot, head) of a cache side starts; slot is in range.
+__device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot, int page_size, int head) {
+  const long long page = slot / page_size;
+  return page * c.page + (slot - page * page_size) * c.token + (long long)head * c.head;
+}
+
+// IO: storage of q, k, v and out_q.  CIO: storage of the cache.  UPT: 16-element units per thread.
+template <class IO, class CIO, int NORM, bool CACHE, int UPT>
+__global__ void __launch_bounds__(1024) rope_kernel(const __grid_constant__ RopeParams R) {
+  extern __shared__ float4 cs_all[];  // [tokens_per_cta][4][rot_dim/16]: (c, s) of pairs 8j+2e, 8j+2e+1 at [e][j]
+  __shared__ float red[32][2];        // per warp: sum of squares of Q, of K
+  const int slot_of_token = threadIdx.x / R.threads_per_token;
+  const int tid = threadIdx.x - slot_of_token * R.threads_per_token;
+  const long long t = (long long)blockIdx.x * R.tokens_per_cta + slot_of_token;
+  const bool live = t < R.T;
+  const int r16 = R.rot_dim >> 4;
+  float4* cs = cs_all + slot_of_token * 4 * r16;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  Chunk8<IO> u[UPT][2];
+  int j[UPT], c0[UPT], c1[UPT], head[UPT], side[UPT];  // side: 0 q, 1 k, 2 v, -1 none
+#pragma unroll
+  for (int i = 0; i < UPT; ++i) {
+    const int s = tid + i * R.threads_per_token;
+    int h = s >> R.log_lph;
+    j[i] = s & ((1 << R.log_lph) - 1);
+    side[i] = -1;
+    if (live && s < R.slots_per_token && j[i] * 16 < R.head_dim) {
+      side[i] = 0;
+      if (h >= R.q.heads) {
+        h -= R.q.heads;
+        side[i] = 1;
+        if (CACHE && h >= R.k.heads) {
+          h -= R.k.heads;
+          side[i] = 2;
+        }
+      }
+    }
+    head[i] = h;
+    const bool half = !R.interleaved && j[i] < r16;
+    c0[i] = half ? 8 * j[i] : 16 * j[i];
+    c1[i] = half ? 8 * (j[i] + r16) : 16 * j[i] + 8;
+    if (side[i] >= 0) {
+      const RopeSide& A = side[i] == 0 ? R.q : (!CACHE || side[i] == 1) ? R.k : R.v;
+      const long long row = t * A.ldx + (long long)h * R.head_dim;
+      u[i][0].load(A.x, row + c0[i]);
+      u[i][1].load(A.x, row + c1[i]);
+    }
+  }
+  if (live && r16 > 0) {
+    const long long pos = R.positions[t];
+    for (int p = tid; p < 8 * r16; p += R.threads_per_token)
+      reinterpret_cast<float2*>(cs)[(((p & 7) >> 1) * r16 + (p >> 3)) * 2 + (p & 1)] = rope_cs(R, pos, p);
+  }
+  float rq = 1.f, rk = 1.f;
+  if (NORM == kNormLayer) {
+    float sq = 0.f, sk = 0.f;
+#pragma unroll
+    for (int i = 0; i < UPT; ++i) {
+      if (side[i] == 0 || side[i] == 1) {
+        float f[8], a = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u[i][h].unpack(f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) a = fmaf(f[e], f[e], a);
+        }
+        if (side[i] == 0) sq += a;
+        else sk += a;
+      }
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      sq += __shfl_xor_sync(0xffffffffu, sq, off);
+      sk += __shfl_xor_sync(0xffffffffu, sk, off);
+    }
+    if ((threadIdx.x & 31) == 0) {
+      red[threadIdx.x >> 5][0] = sq;
+      red[threadIdx.x >> 5][1] = sk;
+    }
+  }
+  __syncthreads();
+  if (NORM == kNormLayer) {
+    const int wpt = R.threads_per_token >> 5, w0 = slot_of_token * wpt;
+    float sq = 0.f, sk = 0.f;
+    for (int w = 0; w < wpt; ++w) {  // fixed order
+      sq += red[w0 + w][0];
+      sk += red[w0 + w][1];
+    }
+    rq = rstd_of(sq, R.q.inv_d, R.eps);
+    rk = rstd_of(sk, R.k.inv_d, R.eps);
+  }
+  long long cslot = -1;
+  if (CACHE && live) {
+    cslot = R.slots[t];
+    if (cslot >= R.num_slots) cslot = -1;
+  }
+#pragma unroll
+  for (int i = 0; i < UPT; ++i) {
+    float a[8], b[8];
+    if (side[i] >= 0) {
+      u[i][0].unpack(a);
+      u[i][1].unpack(b);
+    }
+    if (NORM != kNormNone) {
+      float r = side[i] == 0 ? rq : rk;
+      if (NORM == kNormHead) {
+        float ss = 0.f;
+        if (side[i] >= 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
+        }
+        for (int off = 1 << R.log_lph >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+        r = rstd_of(ss, R.inv_hd, R.eps);
+      }
+      if (side[i] == 0 || side[i] == 1) {
+        const uint16_t* g = (side[i] == 0 ? R.q.gamma : R.k.gamma) + (long long)head[i] * R.head_dim;
+        const uint4 g0 = __ldg(reinterpret_cast<const uint4*>(g + c0[i])), g1 = __ldg(reinterpret_cast<const uint4*>(g + c1[i]));
+        const uint32_t ga[4] = {g0.x, g0.y, g0.z, g0.w}, gb[4] = {g1.x, g1.y, g1.z, g1.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[2 * e] *= bf_lo(ga[e]) * r;
+          a[2 * e + 1] *= bf_hi(ga[e]) * r;
+          b[2 * e] *= bf_lo(gb[e]) * r;
+          b[2 * e + 1] *= bf_hi(gb[e]) * r;
+        }
+      }
+    }
+    if (side[i] < 0) continue;
+    if (j[i] < r16 && side[i] != 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float4 f = cs[e * r16 + j[i]];  // pairs 8j+2e, 8j+2e+1
+        if (R.interleaved) {  // pairs 8j..8j+3 lie in a, 8j+4..8j+7 in b
+          float* p = e < 2 ? a + 4 * e : b + 4 * (e - 2);
+          const float x0 = p[0], x1 = p[1], x2 = p[2], x3 = p[3];
+          p[0] = x0 * f.x - x1 * f.y;
+          p[1] = x1 * f.x + x0 * f.y;
+          p[2] = x2 * f.z - x3 * f.w;
+          p[3] = x3 * f.z + x2 * f.w;
+        } else {
+          const float x0 = a[2 * e], y0 = b[2 * e], x1 = a[2 * e + 1], y1 = b[2 * e + 1];
+          a[2 * e] = x0 * f.x - y0 * f.y;
+          b[2 * e] = y0 * f.x + x0 * f.y;
+          a[2 * e + 1] = x1 * f.z - y1 * f.w;
+          b[2 * e + 1] = y1 * f.z + x1 * f.w;
+        }
+      }
+    }
+    if (CACHE && side[i] != 0) {
+      if (cslot < 0) continue;
+      const CacheSide& C = side[i] == 1 ? R.ck : R.cv;
+      if (CIO::kBytes == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          a[e] *= C.inv_scale;
+          b[e] *= C.inv_scale;
+        }
+      }
+      const long long at = cache_at(C, cslot, R.page_size, head[i]);
+      Chunk8<CIO>::store(C.base, at + c0[i], a);
+      Chunk8<CIO>::store(C.base, at + c1[i], b);
+    } else {
+      const RopeSide& A = side[i] == 0 ? R.q : R.k;
+      const long long row = t * A.ldy + (long long)head[i] * R.head_dim;
+      Chunk8<IO>::store(A.y, row + c0[i], a);
+      Chunk8<IO>::store(A.y, row + c1[i], b);
+    }
+  }
+}
+
+// Any head_dim, any alignment, any width: a CTA per token, element-wise.  A lane owns whole pairs, so in-place
+// calls are safe here too.
+constexpr int kRopeGeneralThreads = 256;
+
+template <class IO, class CIO, bool CACHE>
+__global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const __grid_constant__ RopeParams R, int norm) {
+  __shared__ float2 cs[kRopeMaxPairs];
+  __shared__ float red[kRopeGeneralThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int pairs = R.rot_dim >> 1, singles = R.head_dim - R.rot_dim;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (long long t = blockIdx.x; t < R.T; t += gridDim.x) {
+    __syncthreads();  // the previous token's cos and sin are no longer needed
+    if (pairs > 0) {
+      const long long pos = R.positions[t];
+      for (int p = threadIdx.x; p < pairs; p += kRopeGeneralThreads) cs[p] = rope_cs(R, pos, p);
+    }
+    long long cslot = -1;
+    if (CACHE) {
+      cslot = R.slots[t];
+      if (cslot >= R.num_slots) cslot = -1;
+    }
+    for (int side = 0; side < (CACHE ? 3 : 2); ++side) {
+      const RopeSide& A = side == 0 ? R.q : side == 1 ? R.k : R.v;
+      if (A.heads == 0) continue;
+      const bool to_cache = CACHE && side != 0;
+      const CacheSide& C = side == 2 ? R.cv : R.ck;
+      const long long xrow = t * A.ldx;
+      float r = 1.f;
+      if (norm == kNormLayer && side != 2) {
+        float acc = 0.f;
+        const int d = A.heads * R.head_dim;
+        for (int i = threadIdx.x; i < d; i += kRopeGeneralThreads) {
+          const float v = IO::load(A.x, xrow + i);
+          acc = fmaf(v, v, acc);
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
+        __syncthreads();  // the slots of the side before
+        if (lane == 0) red[warp] = acc;
+        __syncthreads();
+        float sum = 0.f;
+        for (int w = 0; w < kRopeGeneralThreads / 32; ++w) sum += red[w];
+        r = rstd_of(sum, A.inv_d, R.eps);
+      } else {
+        __syncthreads();
+      }
+      for (int h = warp; h < A.heads; h += kRopeGeneralThreads / 32) {
+        const long long x0 = xrow + (long long)h * R.head_dim;
+        float rr = r;
+        if (norm == kNormHead && side != 2) {
+          float acc = 0.f;
+          for (int i = lane; i < R.head_dim; i += 32) {
+            const float v = IO::load(A.x, x0 + i);
+            acc = fmaf(v, v, acc);
+          }
+#pragma unroll
+          for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
+          rr = rstd_of(acc, R.inv_hd, R.eps);
+        }
+        auto value = [&](int i) {
+          float v = IO::load(A.x, x0 + i);
+          if (norm != kNormNone && side != 2) v *= IoBf16::load(A.gamma, (long long)h * R.head_dim + i) * rr;
+          return v;
+        };
+        if (to_cache && cslot < 0) continue;
+        const long long y0 = to_cache ? cache_at(C, cslot, R.page_size, h) : t * A.ldy + (long long)h * R.head_dim;
+        auto put = [&](int i, float v) {
+          if (to_cache) CIO::store(C.base, y0 + i, CIO::kBytes == 1 ? v * C.inv_scale : v);
+          else IO::store(A.y, y0 + i, v);
+        };
+        for (int p = lane; p < pairs; p += 32) {
+          const int ia = R.interleaved ? 2 * p : p, ib = R.interleaved ? 2 * p + 1 : p + pairs;
+          const float a = value(ia), b = value(ib);
+          const float2 f = side != 2 ? cs[p] : make_float2(1.f, 0.f);
+          put(ia, side != 2 ? a * f.x - b * f.y : a);
+          put(ib, side != 2 ? b * f.x + a * f.y : b);
+        }
+        for (int i = lane; i < singles; i += 32) put(R.rot_dim + i, value(R.rot_dim + i));
+      }
+    }
+  }
+}
+
+typedef void (*RopeKernel)(const RopeParams);
+typedef void (*RopeGeneralKernel)(const RopeParams, int);
+// in qknorm_rope_inst.cu; upt 1, 2 or 4; cache_bytes 0 = no cache
+RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt);
+RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes);
+
+}  // namespace qknorm

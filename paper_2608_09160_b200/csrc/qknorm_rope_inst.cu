@@ -1,0 +1,38 @@
+// Instantiations of the rotary and cache-write kernels, in a translation unit of their own so that they
+// compile in parallel with the others.
+#include "qknorm_rope.cuh"
+
+namespace qknorm {
+
+namespace {
+template <class IO, class CIO, int NORM, bool CACHE>
+RopeKernel pick(int upt) {
+  switch (upt) {
+    case 1: return rope_kernel<IO, CIO, NORM, CACHE, 1>;
+    case 2: return rope_kernel<IO, CIO, NORM, CACHE, 2>;
+    case 4: return rope_kernel<IO, CIO, NORM, CACHE, 4>;
+    default: return nullptr;
+  }
+}
+template <class CIO>
+RopeKernel pick_cache(int norm, int upt) {
+  switch (norm) {
+    case kNormNone: return pick<IoBf16, CIO, kNormNone, true>(upt);
+    case kNormLayer: return pick<IoBf16, CIO, kNormLayer, true>(upt);
+    case kNormHead: return pick<IoBf16, CIO, kNormHead, true>(upt);
+    default: return nullptr;
+  }
+}
+}  // namespace
+
+RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt) {
+  if (cache_bytes == 0) return elem_bytes == 1 ? pick<IoE4m3, IoE4m3, kNormNone, false>(upt) : pick<IoBf16, IoBf16, kNormNone, false>(upt);
+  return cache_bytes == 1 ? pick_cache<IoE4m3>(norm, upt) : pick_cache<IoBf16>(norm, upt);
+}
+
+RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes) {
+  if (cache_bytes == 0) return elem_bytes == 1 ? rope_general_kernel<IoE4m3, IoE4m3, false> : rope_general_kernel<IoBf16, IoBf16, false>;
+  return cache_bytes == 1 ? rope_general_kernel<IoBf16, IoE4m3, true> : rope_general_kernel<IoBf16, IoBf16, true>;
+}
+
+}  // namespace qknorm

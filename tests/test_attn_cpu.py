@@ -1,0 +1,236 @@
+"""Host side of include/qknorm_attn.h without a GPU: exports, argument checks (all made before any launch), the frequency helper."""
+import ctypes
+import math
+import os
+
+import pytest
+
+from paper_2608_09160_b200 import attn, binding
+from tests.test_abi import ROOT, declared_functions
+
+HEADER_ATTN = os.path.join(ROOT, "include", "qknorm_attn.h")
+A, B, C, D, E, F, G, H = (0x10000000 + i * 0x4000000 for i in range(8))
+
+
+@pytest.fixture(scope="module")
+def lib(libqknorm):
+    return attn.lib()
+
+
+def test_header_and_binding_agree_on_exports(lib):
+    assert declared_functions(HEADER_ATTN) == sorted(attn.EXPORTS)
+    for name in attn.EXPORTS:
+        assert hasattr(lib, name), name
+
+
+def rotation(rot_dim=64, positions=G, inv_freq=G + 0x100000, interleaved=0, mscale=1.0):
+    return attn.CRotation(positions, inv_freq, rot_dim, interleaved, mscale)
+
+
+def rope(lib, q=A, k=B, rot=None, T=4, dq=256, dk=128, hd=64, ldq=0, ldk=0, inverse=0, oq=C, ok=D, ldoq=0, ldok=0, fn="qknorm_rope"):
+    r = rotation() if rot is None else rot
+    return getattr(lib, fn)(q, k, ctypes.byref(r) if r else None, T, dq, dk, hd, ldq, ldk, inverse, oq, ok, ldoq, ldok, None)
+
+
+def test_rope_argument_errors(lib):
+    b = binding
+    assert rope(lib, T=0) == b.QKNORM_OK
+    assert rope(lib, T=-1) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, dq=-64) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, dq=0, dk=0) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, dq=65536 + 64) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, hd=0) == b.QKNORM_ERR_HEADS
+    assert rope(lib, hd=96) == b.QKNORM_ERR_HEADS
+    assert rope(lib, hd=1024, dq=1024, dk=1024) == b.QKNORM_ERR_HEADS
+    assert rope(lib, rot=False) == b.QKNORM_ERR_NULL
+    assert rope(lib, rot=rotation(rot_dim=63)) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, rot=rotation(rot_dim=66)) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, rot=rotation(rot_dim=-2)) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, rot=rotation(interleaved=2)) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, rot=rotation(mscale=math.inf)) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, rot=rotation(positions=None)) == b.QKNORM_ERR_NULL
+    assert rope(lib, rot=rotation(inv_freq=None)) == b.QKNORM_ERR_NULL
+    assert rope(lib, rot=rotation(positions=G + 4)) == b.QKNORM_ERR_ALIGN
+    assert rope(lib, inverse=2) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, q=None) == b.QKNORM_ERR_NULL
+    assert rope(lib, ok=None) == b.QKNORM_ERR_NULL
+    assert rope(lib, q=A + 1) == b.QKNORM_ERR_ALIGN
+    assert rope(lib, ldq=255) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, ldok=-1) == b.QKNORM_ERR_SHAPE
+    assert rope(lib, oq=A + 64) == b.QKNORM_ERR_ALIAS
+    assert rope(lib, oq=B) == b.QKNORM_ERR_ALIAS
+    assert rope(lib, oq=C, ok=C + 64) == b.QKNORM_ERR_ALIAS
+    assert rope(lib, oq=G) == b.QKNORM_ERR_ALIAS                 # on top of the positions
+    assert rope(lib, oq=A, ldoq=512) == b.QKNORM_ERR_ALIAS       # same base, another pitch
+    assert rope(lib, fn="qknorm_rope_e4m3", T=0) == b.QKNORM_OK
+    import torch
+    if not torch.cuda.is_available():                            # legal: gets as far as asking CUDA for the device
+        assert rope(lib, oq=A, ok=B) == b.QKNORM_ERR_CUDA
+        assert rope(lib, q=A, k=A + 512, ldq=512, ldk=512, oq=A, ok=A + 512, ldoq=512, ldok=512, fn="qknorm_rope") == b.QKNORM_ERR_CUDA
+        assert rope(lib, q=A + 1, k=B, oq=A + 1, ok=B, fn="qknorm_rope_e4m3") == b.QKNORM_ERR_CUDA
+
+
+def cache(k=E, v=F, pages=8, page=16, heads=2, hd=64, e4m3=0, ks=1.0, vs=1.0, **kw):
+    c = attn.CPagedCache(k, v, page * heads * hd, heads * hd, hd, page * heads * hd, heads * hd, hd, pages, page, heads, hd, e4m3, ks, vs)
+    for n, x in kw.items():
+        setattr(c, n, x)
+    return c
+
+
+BAD_CACHES = [
+    (dict(pages=-1), "SHAPE"), (dict(page=0), "SHAPE"), (dict(heads=0), "SHAPE"), (dict(hd=0), "HEADS"), (dict(hd=1024), "HEADS"),
+    (dict(e4m3=2), "SHAPE"), (dict(e4m3=1, ks=0.0), "SHAPE"), (dict(e4m3=1, vs=math.nan), "SHAPE"), (dict(k=None), "NULL"),
+    (dict(k=E + 1), "ALIGN"), (dict(k_token=-1), "SHAPE"),
+    (dict(k_head=32), "SHAPE"),                       # heads overlap
+    (dict(v_token=64), "SHAPE"),                      # tokens overlap heads
+    (dict(k_page=8), "SHAPE"),                        # pages overlap
+    (dict(k_page=1 << 60), "SHAPE"),                  # beyond any memory
+]
+
+
+def append(lib, c=None, q=A, k=B, v=B + 0x1000000, gq=C, gk=C + 0x100000, norm=1, eps=1e-6, rot=None, slots=H, T=4, dq=256, ldq=0, ldk=0,
+           ldv=0, oq=D, ldo=0):
+    c = cache() if c is None else c
+    return lib.qknorm_fwd_append(q, k, v, gq, gk, norm, eps, ctypes.byref(rot) if rot else None, slots, ctypes.byref(c) if c else None, T,
+                                 dq, ldq, ldk, ldv, oq, ldo, None)
+
+
+def test_append_argument_errors(lib):
+    b = binding
+    assert append(lib, T=0) == b.QKNORM_OK
+    assert append(lib, c=False) == b.QKNORM_ERR_NULL
+    for kw, name in BAD_CACHES:
+        assert append(lib, c=cache(**kw)) == getattr(b, "QKNORM_ERR_" + name), kw
+    assert append(lib, T=-1) == b.QKNORM_ERR_SHAPE
+    assert append(lib, dq=200) == b.QKNORM_ERR_HEADS
+    assert append(lib, norm=3) == b.QKNORM_ERR_SHAPE
+    assert append(lib, eps=-1.0) == b.QKNORM_ERR_EPS
+    assert append(lib, eps=math.nan) == b.QKNORM_ERR_EPS
+    assert append(lib, rot=rotation(rot_dim=66)) == b.QKNORM_ERR_SHAPE
+    for n in ("q", "k", "v", "gq", "gk", "slots", "oq"):
+        assert append(lib, **{n: None}) == b.QKNORM_ERR_NULL, n
+    assert append(lib, slots=H + 4) == b.QKNORM_ERR_ALIGN
+    assert append(lib, gk=C + 1) == b.QKNORM_ERR_ALIGN
+    assert append(lib, ldk=100) == b.QKNORM_ERR_SHAPE
+    assert append(lib, oq=A + 128) == b.QKNORM_ERR_ALIAS
+    assert append(lib, oq=E + 64) == b.QKNORM_ERR_ALIAS          # q's output inside the K pool
+    assert append(lib, c=cache(v=E + 256)) == b.QKNORM_ERR_ALIAS  # K and V pools overlap
+    assert append(lib, k=E) == b.QKNORM_ERR_ALIAS                # k comes out of the pool it goes to
+    import torch
+    if not torch.cuda.is_available():
+        assert append(lib, norm=0, gq=None, gk=None, eps=-1.0) == b.QKNORM_ERR_CUDA
+        assert append(lib, q=None, oq=None, gq=None, dq=0) == b.QKNORM_ERR_CUDA
+        # K and V side by side: in one page, in one token, heads before tokens
+        assert append(lib, c=cache(v=E + 2 * 2048, k_page=4096, v_page=4096)) == b.QKNORM_ERR_CUDA
+        assert append(lib, c=cache(v=E + 256, k_page=4096, v_page=4096, k_token=256, v_token=256)) == b.QKNORM_ERR_CUDA
+        assert append(lib, c=cache(k_head=1024, k_token=64, v_head=1024, v_token=64)) == b.QKNORM_ERR_CUDA
+
+
+def attention(lib, c=None, q=A, ldq=0, table=G, cols=4, ldt=0, lens=G + 0x100000, starts=G + 0x200000, B_=2, T=4, max_q=2, max_kv=64, hq=4,
+              scale=0.125, causal=1, window=0, out=D, ldo=0, lse=None, ws=H, ws_bytes=1 << 24):
+    c = cache() if c is None else c
+    return lib.qknorm_attn_paged(q, ldq, ctypes.byref(c) if c else None, table, cols, ldt, lens, starts, B_, T, max_q, max_kv, hq, scale,
+                                 causal, window, out, ldo, lse, ws, ws_bytes, None)
+
+
+def test_attention_argument_errors(lib):
+    b = binding
+    for kw in (dict(T=0), dict(B_=0), dict(max_q=0)):
+        assert attention(lib, **kw) == b.QKNORM_OK, kw
+    assert attention(lib, c=False) == b.QKNORM_ERR_NULL
+    for kw, name in BAD_CACHES:
+        assert attention(lib, c=cache(**kw)) == getattr(b, "QKNORM_ERR_" + name), kw
+    for kw in (dict(T=-1), dict(B_=-1), dict(max_q=-1), dict(max_kv=-1), dict(max_kv=0x7fffffff), dict(window=-1), dict(scale=0.0),
+               dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(causal=2), dict(cols=-1), dict(ldt=3), dict(ldq=100),
+               dict(ldo=-4), dict(T=1 << 31)):
+        assert attention(lib, **kw) == b.QKNORM_ERR_SHAPE, kw
+    assert attention(lib, hq=3) == b.QKNORM_ERR_HEADS
+    assert attention(lib, hq=0) == b.QKNORM_ERR_HEADS
+    for n in ("q", "out", "table", "lens", "starts"):
+        assert attention(lib, **{n: None}) == b.QKNORM_ERR_NULL, n
+    for kw in (dict(q=A + 1), dict(out=D + 1), dict(table=G + 2), dict(lens=G + 2), dict(starts=G + 1), dict(lse=C + 2)):
+        assert attention(lib, **kw) == b.QKNORM_ERR_ALIGN, kw
+    import torch
+    if not torch.cuda.is_available():
+        assert attention(lib) == b.QKNORM_ERR_CUDA                     # everything but the device is in order
+        assert attention(lib, cols=0, table=None) == b.QKNORM_ERR_CUDA  # no page at all: every row is empty
+
+
+def test_workspace_argument_errors(lib):
+    out = ctypes.c_int64(-1)
+    ask = lambda seqs=4, T=8, mq=2, mk=64, hq=8, hk=2, hd=64, w=0: lib.qknorm_attn_paged_workspace(seqs, T, mq, mk, hq, hk, hd, w, ctypes.byref(out))
+    assert lib.qknorm_attn_paged_workspace(1, 1, 1, 1, 1, 1, 64, 0, None) == binding.QKNORM_ERR_NULL
+    assert ask(T=0) == binding.QKNORM_OK and out.value == 0
+    assert ask(hq=7) == binding.QKNORM_ERR_HEADS
+    assert ask(hd=513) == binding.QKNORM_ERR_HEADS
+    assert ask(w=-1) == binding.QKNORM_ERR_SHAPE
+    assert ask(mk=-1) == binding.QKNORM_ERR_SHAPE
+
+
+def frequencies(rot_dim, theta, scaling, factor=1.0, orig=0.0, low=1.0, high=32.0):
+    """The scalings of the header, written from their definitions."""
+    out = []
+    for i in range(rot_dim // 2):
+        f = theta ** (-2.0 * i / rot_dim)
+        if scaling == "linear":
+            f /= factor
+        elif scaling == "base":
+            f = (theta * factor ** (rot_dim / (rot_dim - 2))) ** (-2.0 * i / rot_dim)
+        elif scaling == "ramp":
+            at = lambda n: rot_dim * math.log(orig / (n * 2 * math.pi)) / (2 * math.log(theta))
+            a, z = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot_dim - 1)
+            ramp = min(max((i - a) / ((z - a) or 0.001), 0.0), 1.0)
+            f = f / factor * ramp + f * (1 - ramp)
+        elif scaling == "bands":
+            turns = orig * f / (2 * math.pi)
+            if turns <= low:
+                f /= factor
+            elif turns < high:
+                t = (turns - low) / (high - low)
+                f = (1 - t) * f / factor + t * f
+        out.append(f)
+    return out
+
+
+@pytest.mark.parametrize("rot_dim,theta,scaling,kw", [
+    (128, 10000.0, "plain", {}), (2, 500000.0, "plain", {}), (64, 10000.0, "linear", dict(factor=4.0)),
+    (128, 10000.0, "base", dict(factor=8.0)), (128, 10000.0, "ramp", dict(factor=16.0, original_len=4096, low=1.0, high=32.0)),
+    (96, 500000.0, "ramp", dict(factor=2.0, original_len=100.0, low=1.0, high=2.0)),
+    (128, 500000.0, "bands", dict(factor=8.0, original_len=8192, low=1.0, high=4.0)), (128, 10000.0, "linear", dict(factor=1.0)),
+])
+def test_frequencies_against_their_definitions(lib, rot_dim, theta, scaling, kw):
+    got, mscale = attn.rope_frequencies(rot_dim, theta, scaling, device="cpu", **kw)
+    want = frequencies(rot_dim, theta, scaling, kw.get("factor", 1.0), kw.get("original_len", 0.0), kw.get("low", 1.0), kw.get("high", 32.0))
+    assert got.shape == (rot_dim // 2,)
+    for g, w in zip(got.tolist(), want):
+        assert abs(g - w) <= 1e-13 * w
+    assert abs(mscale - (0.1 * math.log(kw["factor"]) + 1 if scaling == "ramp" else 1.0)) < 1e-7
+
+
+def test_frequency_refusals(lib):
+    bad = [dict(rot_dim=3), dict(rot_dim=0), dict(rot_dim=514), dict(rot_dim=64, theta=1.0), dict(rot_dim=64, theta=math.nan),
+           dict(rot_dim=64, scaling="linear", factor=0.5), dict(rot_dim=2, scaling="base", factor=2.0),
+           dict(rot_dim=64, scaling="ramp", factor=2.0), dict(rot_dim=64, scaling="bands", factor=2.0, original_len=64, low=4.0, high=4.0)]
+    for kw in bad:
+        with pytest.raises(binding.QKNormError):
+            attn.rope_frequencies(device="cpu", **kw)
+    with pytest.raises(binding.QKNormError):
+        attn.rope_frequencies(64, scaling="spiral", device="cpu")
+
+
+def test_reference_inverse_rotation_is_the_gradient():
+    """The reference the GPU tests use: rotating back undoes a rotation, and is its gradient by differences."""
+    import torch
+    from tests import attn_reference as R
+    g = torch.Generator().manual_seed(3)
+    x, y = torch.randn(3, 32, generator=g, dtype=torch.float64), torch.randn(3, 32, generator=g, dtype=torch.float64)
+    pos, f = torch.tensor([0, 5, -1000]), torch.tensor([1.0, 0.1, 0.01], dtype=torch.float64)
+    for inter in (False, True):
+        fwd = lambda z: R.rotate(z, pos, f, 16, inter, False, 1.5)[0]
+        assert torch.allclose(R.rotate(fwd(x), pos, f, 16, inter, True, 1 / 1.5)[0][:, :6], x[:, :6], atol=1e-12)
+        grad = R.rotate(y, pos, f, 16, inter, True, 1.5)[0]
+        for e in range(0, 32, 7):
+            h = torch.zeros_like(x)
+            h[:, e] = 1e-6
+            diff = ((fwd(x + h) - fwd(x - h)) * y).sum(1) / 2e-6
+            assert torch.allclose(diff, grad[:, e], atol=1e-7)

@@ -1,0 +1,371 @@
+"""Attention over a paged cache against its 64-bit definition (tests/attn_reference.py says how the bounds come about)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_09160_b200 import attn, binding
+from tests import attn_reference as R
+from tests.attn_reference import BF16, F8
+
+pytestmark = pytest.mark.gpu
+
+
+class Batch:
+    """A seeded batch: lists of new tokens and keys per sequence, a shuffled page pool (unused slots hold NaN), guard rows."""
+
+    def __init__(self, new, kv, hq, hk, hd, page=16, dtype=BF16, seed=0, order="nhd", guard=2, sigma=1.0, pad_cols=0):
+        g = torch.Generator().manual_seed(seed)
+        self.new, self.kv, self.hq, self.hk, self.hd, self.page, self.dtype = list(new), list(kv), hq, hk, hd, page, dtype
+        need = [-(-max(n, 0) // page) for n in kv]
+        self.pages, cols = sum(need) + 3, max(need + [1]) + pad_cols
+        ids = torch.randperm(self.pages, generator=g).tolist()
+        self.table = [[ids.pop() for _ in range(n)] + [10 ** 6] * (cols - n) for n in need]
+        self.ks, self.vs = (0.25, 0.5) if dtype is F8 else (1.0, 1.0)
+        self.k = (torch.randn((self.pages, page, hk, hd), generator=g) * sigma / self.ks).to(dtype)
+        self.v = (torch.randn((self.pages, page, hk, hd), generator=g) / self.vs).to(dtype)
+        used = torch.zeros((self.pages, page), dtype=torch.bool)
+        for row, n in zip(self.table, kv):
+            for j in range(max(n, 0)):
+                used[row[j // page], j % page] = True
+        nan = torch.tensor([0x7F], dtype=torch.uint8).view(F8)[0] if dtype is F8 else torch.tensor(float("nan"), dtype=BF16)
+        for t in (self.k, self.v):
+            raw = t.view(torch.uint8 if dtype is F8 else torch.int16)
+            raw[~used] = nan.view(raw.dtype)
+        self.T = sum(new) + guard
+        self.q = torch.randn((self.T, hq * hd), generator=g).to(BF16)
+        self.q[sum(new):] = float("nan")          # rows of no sequence: not read
+        self.starts = np.concatenate([[0], np.cumsum(new)]).tolist()
+        perm = {"nhd": (0, 1, 2, 3), "hnd": (0, 2, 1, 3), "thd": (1, 0, 2, 3)}[order]
+        inv = [perm.index(i) for i in range(4)]
+        raw = torch.uint8 if dtype is F8 else torch.int16
+        place = lambda t: t.view(raw).permute(perm).contiguous().cuda().permute(inv).view(dtype)
+        self.dk, self.dv = place(self.k), place(self.v)
+        self.dq = self.q.cuda()
+        self.dtable = torch.tensor(self.table, dtype=torch.int32, device="cuda").view(len(new), cols)
+        self.dlens = torch.tensor(kv, dtype=torch.int32, device="cuda")
+        self.dstarts = torch.tensor(self.starts, dtype=torch.int32, device="cuda")
+
+    def call(self, **kw):
+        out = torch.full_like(self.dq, 7.0)
+        lse = torch.full((self.T, self.hq), 7.0, dtype=torch.float32, device="cuda")
+        kw.setdefault("max_q", max(self.new + [1]))
+        kw.setdefault("max_kv", max(self.kv + [1]))
+        attn.qknorm_attn_paged(self.dq, self.dk, self.dv, self.dtable, self.dlens, self.dstarts, kw.pop("max_q"), kw.pop("max_kv"),
+                               k_scale=self.ks, v_scale=self.vs, out=out, lse=lse, **kw)
+        torch.cuda.synchronize()
+        assert binding.device_error_word() == 0
+        return out.cpu(), lse.cpu()
+
+    def reference(self, scale=None, causal=True, window=0, max_kv=None):
+        scale = 1.0 / math.sqrt(self.hd) if scale is None else scale
+        return R.attention(R.widen(self.q), R.widen(self.k), R.widen(self.v), self.table, self.kv, self.starts, self.hq, scale=scale,
+                           causal=causal, window=window, k_scale=self.ks, v_scale=self.vs, max_kv=max_kv)
+
+    def compare(self, out, lse, ref, rows=None):
+        n = self.starts[-1]
+        rows = range(n) if rows is None else rows
+        got, z = out.double().numpy().reshape(self.T, self.hq, self.hd), lse.double().numpy()
+        tol, tol_lse = R.attention_bounds(ref, self.hd, self.dtype is F8)
+        for r in rows:
+            bad = ~(np.abs(got[r] - ref["out"][r]) <= tol[r])
+            assert not bad.any(), (f"row {r}: {int(bad.sum())} of {bad.size} off, first {np.argwhere(bad)[0]}: {got[r][bad][0]} for "
+                                   f"{ref['out'][r][bad][0]} (tolerance {tol[r][bad][0]:.3g})")
+            empty = np.isneginf(ref["lse"][r])
+            assert (np.isneginf(z[r]) == empty).all(), f"row {r}: lse {z[r]} for {ref['lse'][r]}"
+            assert (np.abs(z[r] - ref["lse"][r])[~empty] <= tol_lse[r][~empty]).all(), f"row {r}: lse {z[r]} for {ref['lse'][r]}"
+        assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()     # rows of no sequence: not written
+
+    def check(self, variant=None, **kw):
+        ref = self.reference(**{k: v for k, v in kw.items() if k in ("scale", "causal", "window", "max_kv")})
+        out, lse = self.call(**kw)
+        if variant:
+            assert binding.last_variant() == variant
+        self.compare(out, lse, ref)
+
+
+BOTH = pytest.mark.parametrize("dtype", [BF16, F8], ids=["bf16", "e4m3"])
+
+
+@BOTH
+@pytest.mark.parametrize("hq,hk,hd", [(1, 1, 128), (1, 1, 64), (8, 1, 128), (5, 1, 64), (8, 8, 128), (7, 1, 96), (40, 8, 128)])
+def test_single_tokens(libqknorm, hq, hk, hd, dtype):
+    Batch([1, 1, 1, 1], [1, 130, 33, 128], hq, hk, hd, dtype=dtype).check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("page", [1, 7, 16, 24, 64, 128, 256])
+def test_pages_and_lengths(libqknorm, page, dtype):
+    Batch([1, 2, 1, 3, 1], [127, 129, 255, 257, 384], 4, 2, 64, page=page, dtype=dtype, seed=page).check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("hq,hk,hd,new,kv", [
+    (1, 1, 128, [128], [128]), (1, 1, 128, [129], [129]), (1, 1, 64, [300], [300]), (5, 1, 128, [60, 3, 26], [60, 200, 27]),
+    (8, 2, 64, [16, 17, 33], [300, 17, 129]), (3, 1, 96, [100], [256]), (128, 1, 64, [2, 1], [130, 140]), (2, 2, 128, [257, 1], [500, 129]),
+])
+def test_chunks(libqknorm, hq, hk, hd, new, kv, dtype):
+    Batch(new, kv, hq, hk, hd, dtype=dtype, seed=len(new)).check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("window", [1, 5, 64, 128, 200])
+def test_windows(libqknorm, window, dtype):
+    b = Batch([1, 40, 150], [400, 300, 150], 4, 2, 64, dtype=dtype)
+    b.check("attn_tc", window=window)
+    Batch([1, 1], [300, 77], 4, 2, 64, dtype=dtype).check("attn_tc", window=window)
+
+
+@BOTH
+@pytest.mark.parametrize("one", [True, False])
+def test_not_causal(libqknorm, one, dtype):
+    new = [5, 2] if one else [140, 3]
+    Batch(new, [130, 259], 2, 1, 128, dtype=dtype).check("attn_tc", causal=False)
+    Batch(new, [130, 259], 2, 1, 128, dtype=dtype).check("attn_tc", causal=False, window=30)
+
+
+@BOTH
+def test_rows_without_keys(libqknorm, dtype):
+    """Fewer keys than new tokens (the first rows stand before the first key), no keys at all, an empty sequence between."""
+    Batch([6, 0, 3, 2], [4, 40, 0, 1], 4, 2, 64, dtype=dtype).check("attn_tc")
+    Batch([200, 0, 140], [70, 0, 0], 4, 2, 64, dtype=dtype).check("attn_tc")
+    Batch([1], [0], 4, 2, 64, dtype=dtype).check("attn_tc")
+
+
+@BOTH
+def test_split_keys(libqknorm, dtype):
+    """Long contexts, few rows: parts joined by the second launch; ragged, so that some sequences have fewer parts."""
+    b = Batch([1, 1, 1], [5000, 128, 1], 4, 2, 64, dtype=dtype)
+    n0 = binding.launch_count()
+    b.check("attn_tc")
+    assert binding.launch_count() - n0 == 2
+    Batch([3, 90], [4000, 3000], 2, 1, 128, dtype=dtype).check("attn_tc")
+    Batch([2, 5], [3000, 3], 2, 1, 128, dtype=dtype).check("attn_tc", window=1000)
+    Batch([2, 5], [3000, 0], 2, 1, 128, dtype=dtype).check("attn_tc", max_kv=4000)
+
+
+@BOTH
+def test_large_scores_and_growing_maxima(libqknorm, dtype):
+    """Scores in the hundreds, the maximum rising from tile to tile: the accumulators have to be rescaled."""
+    for new, hd in (([1, 1], 64), ([150], 128)):
+        b = Batch(new, [700] * len(new), 2, 1, hd, dtype=dtype, sigma=1.0)
+        grow = torch.linspace(0.05, 4.0, 700)
+        for row in b.table:
+            for j in range(700):
+                b.k[row[j // 16], j % 16] = (b.k[row[j // 16], j % 16].float() * grow[j]).to(dtype)
+        b.dk.copy_(b.k.cuda())
+        b.check("attn_tc", scale=0.5)
+
+
+@BOTH
+@pytest.mark.parametrize("order", ["hnd", "thd"])
+def test_other_orders_of_the_pool(libqknorm, order, dtype):
+    Batch([1, 70], [200, 150], 4, 2, 128, dtype=dtype, order=order).check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("hq,hk,hd", [(2, 1, 36), (2, 1, 256), (3, 1, 512), (1, 1, 1), (200, 1, 64), (2, 1, 7)])
+def test_general_kernel(libqknorm, hq, hk, hd, dtype):
+    Batch([1, 9], [50, 20], hq, hk, hd, page=5, dtype=dtype).check("attn_general")
+    Batch([3, 4], [2, 33], hq, hk, hd, page=5, dtype=dtype).check("attn_general", window=7)
+
+
+@BOTH
+def test_unaligned_rows_take_the_general_kernel(libqknorm, dtype):
+    b = Batch([1, 9], [50, 20], 2, 1, 64, dtype=dtype)
+    wide = torch.zeros((b.T, 2 * 64 + 1), dtype=BF16, device="cuda")
+    wide[:, 1:] = b.dq
+    b.dq = wide[:, 1:]
+    ref = b.reference()
+    out = torch.full((b.T, 130), 7.0, dtype=BF16, device="cuda")[:, 1:129]
+    lse = torch.full((b.T, 2), 7.0, device="cuda")
+    attn.qknorm_attn_paged(b.dq, b.dk, b.dv, b.dtable, b.dlens, b.dstarts, 9, 50, k_scale=b.ks, v_scale=b.vs, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert binding.last_variant() == "attn_general"
+    b.compare(out.cpu().contiguous(), lse.cpu(), ref)
+
+
+@BOTH
+@pytest.mark.parametrize("new,kv,kw", [([40], [40], {}), ([3, 2], [200, 90], {}), ([150], [150], dict(window=20)), ([1], [300], dict(window=9)),
+                                       ([2, 2], [2500, 2500], {})])
+def test_unseen_values_do_not_matter(libqknorm, new, kv, kw, dtype):
+    """NaN and infinities in K and V at keys that the rows checked do not see -- later tokens of the chunk, keys that left the
+    window -- inside the same tile."""
+    b = Batch(new, kv, 4, 2, 64, dtype=dtype)
+    rows, poison = [], float("nan") if dtype is F8 else float("inf")
+    k, v = b.k.clone(), b.v.clone()
+    for s, row in enumerate(b.table):
+        last = kv[s] - 1                                        # seen by the last new token only (if it is not its own)
+        places = [last] if new[s] > 1 else []
+        if kw.get("window"):
+            places += [kv[s] - new[s] - kw["window"]] if kv[s] > new[s] + kw["window"] else [0]
+        for j in places:
+            for t in (b.k, b.v):
+                t[row[j // b.page], j % b.page] = poison
+        rows += [r for r in range(b.starts[s], b.starts[s + 1])
+                 if not any(R.sees(kv[s] - new[s] + r - b.starts[s], kv[s], True, kw.get("window", 0))[j] for j in places)]
+    b.dk.copy_(b.k.cuda())
+    b.dv.copy_(b.v.cuda())
+    out, lse = b.call(**kw)
+    b.k, b.v = k, v                                             # the rows' own result never involves those keys
+    assert rows
+    b.compare(out, lse, b.reference(**kw), rows)
+
+
+@BOTH
+def test_seen_nan_reaches_the_row(libqknorm, dtype):
+    b = Batch([1, 1], [200, 200], 2, 1, 64, dtype=dtype)
+    b.v[b.table[0][5], 3, 0, 11] = float("nan")
+    b.k[b.table[1][5], 3, 0, 11] = float("nan")
+    b.dk.copy_(b.k.cuda())
+    b.dv.copy_(b.v.cuda())
+    out, lse = b.call()
+    o = out[:2].view(2, 2, 64)
+    assert torch.isnan(o[0, :, 11]).all() and torch.isfinite(o[0, :, :11]).all() and torch.isfinite(lse[0]).all()
+    assert torch.isnan(o[1]).all() and torch.isnan(lse[1]).all()
+
+
+@BOTH
+def test_bad_table_entries_are_pages_of_zeros(libqknorm, dtype):
+    b = Batch([1, 40], [100, 90], 4, 2, 64, dtype=dtype)
+    for s, col, e in ((0, 2, -1), (1, 0, b.pages), (1, 3, 2 ** 31 - 1)):
+        b.table[s][col] = e
+        b.dtable[s, col] = e
+    b.check("attn_tc")
+
+
+def test_lengths_beyond_their_bounds(libqknorm):
+    """kv_lens past the table or max_kv, more new tokens than max_q, q_starts outside the rows: nothing out of the buffers."""
+    b = Batch([1, 4, 2], [100, 60, 40], 4, 2, 64)
+    ref = b.reference(max_kv=48)
+    out, lse = b.call(max_kv=48)
+    b.compare(out, lse, ref)
+    out, lse = b.call(max_q=2)
+    keep = [0, 1, 2, 5, 6]
+    b.compare(out, lse, b.reference(), keep)
+    assert (out[3:5] == 7.0).all() and (lse[3:5] == 7.0).all()
+    b.dlens[1] = -5
+    b.dstarts.copy_(torch.tensor([0, 1, 5, 10 ** 9], dtype=torch.int32))
+    out, lse = b.call(max_q=4)
+    assert (out[1:5] == 0).all() and torch.isneginf(lse[1:5]).all()
+    b.dstarts.copy_(torch.tensor([5, 1, -7, 2], dtype=torch.int32))
+    b.dlens[1] = 60
+    b.call(max_q=4)
+
+
+def test_workspace_is_checked_and_shared_pools_are_safe(libqknorm):
+    b = Batch([1, 1], [4000, 3000], 4, 2, 64)
+    need = attn.attn_paged_workspace(2, b.T, 1, 4000, 4, 2, 64)
+    assert need > 0
+    with pytest.raises(binding.QKNormError) as e:
+        b.call(workspace=torch.empty(need - 16, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == binding.QKNORM_ERR_SCRATCH
+    ws = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")      # NaN everywhere
+    out, lse = b.call(workspace=ws[:need])
+    b.compare(out, lse, b.reference())
+    assert (ws[need:] == 0xFF).all()
+
+
+def test_same_bits_every_time(libqknorm):
+    b = Batch([3, 70], [4000, 300], 8, 2, 128)
+    first = b.call()
+    for _ in range(5):
+        again = b.call()
+        assert torch.equal(first[0].view(torch.int16), again[0].view(torch.int16))
+        assert torch.equal(first[1].view(torch.int32), again[1].view(torch.int32))
+
+
+def test_refusals(libqknorm):
+    b = Batch([2, 1], [50, 20], 4, 2, 64)
+    go = lambda q=b.dq, k=b.dk, v=b.dv, t=b.dtable, n=b.dlens, s=b.dstarts, **kw: attn.qknorm_attn_paged(q, k, v, t, n, s, 2, 50, **kw)
+    out = torch.empty_like(b.dq)
+    bad = [
+        lambda: go(q=b.dq.float()), lambda: go(q=b.dq[:, :100]), lambda: go(q=b.dq[:, ::2]), lambda: go(k=b.dk.half()),
+        lambda: go(v=b.dv[:-1]), lambda: go(t=b.dtable.long()), lambda: go(t=b.dtable[:1]), lambda: go(n=b.dlens.long()),
+        lambda: go(s=b.dstarts[:2]), lambda: go(out=b.dq), lambda: go(out=out[:1]), lambda: go(lse=torch.empty((1, 4), device="cuda")),
+        lambda: go(scale=0.0), lambda: go(window=-1), lambda: go(k=b.k, v=b.v), lambda: go(q=b.dq[:, :192]),
+    ]
+    n0 = binding.launch_count()
+    for i, f in enumerate(bad):
+        with pytest.raises((binding.QKNormError,)):
+            f()
+            pytest.fail(f"call {i} was accepted")
+    assert binding.launch_count() == n0
+
+
+def test_captured_and_replayed_while_lengths_grow(libqknorm):
+    """One graph of a decode step, replayed as the sequences grow: lengths, tables and queries are read when it runs."""
+    b = Batch([1, 1, 1], [600, 40, 10], 4, 2, 64, pad_cols=2)
+    out, lse = torch.full_like(b.dq, 7.0), torch.full((b.T, 4), 7.0, device="cuda")
+    ws = torch.empty(max(16, attn.attn_paged_workspace(3, b.T, 1, 608, 4, 2, 64)), dtype=torch.uint8, device="cuda")
+    go = lambda: attn.qknorm_attn_paged(b.dq, b.dk, b.dv, b.dtable, b.dlens, b.dstarts, 1, 608, out=out, lse=lse, workspace=ws)
+    b.dlens.copy_(torch.tensor([500, 3, 1], dtype=torch.int32))
+    go()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for kv in ([500, 3, 1], [600, 40, 10], [129, 16, 0]):
+        b.kv = kv
+        b.dlens.copy_(torch.tensor(kv, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        b.compare(out.cpu(), lse.cpu(), b.reference())
+
+
+def test_two_streams_at_once(libqknorm):
+    a, b = Batch([1] * 4, [3000] * 4, 8, 2, 128, seed=1), Batch([200], [900], 4, 2, 64, seed=2)
+    want = [a.call(), b.call()]
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        got = []
+        for x, s, mq, mk in ((a, s1, 1, 3000), (b, s2, 200, 900)):
+            with torch.cuda.stream(s):
+                got.append(attn.qknorm_attn_paged(x.dq, x.dk, x.dv, x.dtable, x.dlens, x.dstarts, mq, mk))
+        torch.cuda.synchronize()
+        for x, g, w in zip((a, b), got, want):
+            n = x.starts[-1]
+            assert torch.equal(g.cpu()[:n], w[0][:n])
+
+
+def test_stream_argument(libqknorm):
+    b = Batch([1, 1], [4000, 3000], 4, 2, 64)
+    want = b.call()[0][:2]
+    s = torch.cuda.Stream()
+    for arg in (s, s.cuda_stream):
+        got = attn.qknorm_attn_paged(b.dq, b.dk, b.dv, b.dtable, b.dlens, b.dstarts, 1, 4000, stream=arg)
+        s.synchronize()
+        assert torch.equal(got.cpu()[:2], want)
+
+
+@BOTH
+def test_append_then_attend(libqknorm, dtype):
+    """A layer as it is used: a prompt chunk, then single tokens, each through norm + rotation + cache write and attention; against
+    the 64-bit definition of attention on what the cache and q hold."""
+    g = torch.Generator().manual_seed(8)
+    hq, hk, hd, page = 8, 2, 64, 16
+    ks, vs = (0.03125, 0.0625) if dtype is F8 else (1.0, 1.0)
+    pool = [torch.zeros((32, page, hk, hd), dtype=dtype, device="cuda") for _ in range(2)]
+    lens = [70, 33]
+    table = [list(range(0, 10)), list(range(10, 20))]
+    dtable = torch.tensor(table, dtype=torch.int32, device="cuda")
+    gq, gk = ((torch.rand(n, generator=g) + 0.5).to(BF16).cuda() for n in (hq * hd, hk * hd))
+    inv, m = attn.rope_frequencies(hd, 10000.0, "linear", factor=2.0)
+    seen = [0, 0]
+    for new in (lens, [1, 1], [1, 1], [5, 2]):
+        T = sum(new)
+        x = torch.randn((T, (hq + 2 * hk) * hd), generator=g).to(BF16).cuda()
+        q, k, v = x[:, :hq * hd], x[:, hq * hd:(hq + hk) * hd], x[:, (hq + hk) * hd:]
+        pos = torch.cat([torch.arange(s, s + n) for s, n in zip(seen, new)])
+        slot = torch.tensor([table[b][p // page] * page + p % page for b in range(2) for p in range(seen[b], seen[b] + new[b])])
+        attn.qknorm_fwd_append(q, k, v, gq, gk, pos.cuda(), inv, slot.cuda(), *pool, 1e-6, q, mscale=m, k_scale=ks, v_scale=vs)
+        seen = [s + n for s, n in zip(seen, new)]
+        starts = [0, new[0], T]
+        lse = torch.empty((T, hq), device="cuda")
+        out = attn.qknorm_attn_paged(q, *pool, dtable, torch.tensor(seen, dtype=torch.int32, device="cuda"),
+                                     torch.tensor(starts, dtype=torch.int32, device="cuda"), max(new), 160, k_scale=ks, v_scale=vs, lse=lse)
+        torch.cuda.synchronize()
+        ref = R.attention(R.widen(q), R.widen(pool[0]), R.widen(pool[1]), table, seen, starts, hq, scale=1 / 8, k_scale=ks, v_scale=vs)
+        tol, tol_lse = R.attention_bounds(ref, hd, dtype is F8)
+        assert (np.abs(out.double().cpu().numpy().reshape(T, hq, hd) - ref["out"]) <= tol).all()
+        assert (np.abs(lse.double().cpu().numpy() - ref["lse"]) <= tol_lse).all()
