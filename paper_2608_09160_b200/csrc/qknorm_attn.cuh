@@ -94,7 +94,7 @@ __device__ __forceinline__ long long attn_page(const AttnParams& P, int b, int k
     idx = (int)((unsigned)key / (unsigned)P.page_size);
     within = key - idx * P.page_size;
   }
-  const int e = P.table[(long long)b * P.ld_table + idx];
+  const int e = __ldg(P.table + (long long)b * P.ld_table + idx);
   return (e < 0 || e >= P.num_pages) ? -1 : e;
 }
 

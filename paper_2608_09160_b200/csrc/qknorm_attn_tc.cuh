@@ -33,25 +33,29 @@ namespace qknorm {
 
 namespace tc {
 
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | (1ull << 46) |
-         (2ull << 61);  // 128-byte swizzle
-}
+// Shared-memory matrix descriptor, 128-byte swizzle.  The low word holds the address in 16-byte units (moving on by n
+// bytes adds n / 16 to it) and the leading stride, the high word the stride between groups of 8 rows: a constant.
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return (addr >> 4) | ((lbo >> 4) << 16); }
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 // fp32 accumulators, both operands bf16 (or both fp16), M = 128
 __host__ __device__ constexpr uint32_t instr_desc(int n, bool f16, bool b_transposed) {
   return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((b_transposed ? 1u : 0u) << 16) |
          ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)acc),
+      "r"(kDescHi)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, bool acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)acc)
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"((uint32_t)acc),
+      "r"(kDescHi)
       : "memory");
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
@@ -66,25 +70,32 @@ __device__ __forceinline__ void arrive(uint32_t bar) {
 }
 
 #define QKNORM_R8(m, i) m(i), m(i + 1), m(i + 2), m(i + 3), m(i + 4), m(i + 5), m(i + 6), m(i + 7)
+#define QKNORM_O(i) "=r"(r[i])
+#define QKNORM_I(i) "r"(r[i])
 // 32 columns of this lane's row
 __device__ __forceinline__ void ld32(uint32_t addr, uint32_t* r) {
-#define QKNORM_O(i) "=r"(r[i])
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
       "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : QKNORM_R8(QKNORM_O, 0), QKNORM_R8(QKNORM_O, 8), QKNORM_R8(QKNORM_O, 16), QKNORM_R8(QKNORM_O, 24)
       : "r"(addr));
-#undef QKNORM_O
 }
-__device__ __forceinline__ void st32(uint32_t addr, const uint32_t* r) {
-#define QKNORM_I(i) "r"(r[i])
+// 16 columns
+__device__ __forceinline__ void ld16(uint32_t addr, uint32_t* r) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::QKNORM_R8(QKNORM_I, 0),
-      QKNORM_R8(QKNORM_I, 8), QKNORM_R8(QKNORM_I, 16), QKNORM_R8(QKNORM_I, 24), "r"(addr)
-      : "memory");
-#undef QKNORM_I
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : QKNORM_R8(QKNORM_O, 0), QKNORM_R8(QKNORM_O, 8)
+      : "r"(addr));
 }
+__device__ __forceinline__ void st16(uint32_t addr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15};" ::QKNORM_R8(QKNORM_I, 0),
+      QKNORM_R8(QKNORM_I, 8), "r"(addr)
+      : "memory");
+}
+#undef QKNORM_O
+#undef QKNORM_I
 #undef QKNORM_R8
 
 __device__ __forceinline__ float ex2(float x) {
@@ -95,6 +106,18 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Has the phase completed?  Does not wait: try_wait may suspend the thread for a while.
+__device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 // 16 bytes from global to shared memory, or 16 zero bytes
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool take) {
@@ -140,7 +163,8 @@ struct AttnSmem {
   // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
   // round again only after the tensor warp has seen the scores of the item before last consumed.
   static constexpr int kQScale = kPoison + 16;
-  static constexpr int kMlRows = kQScale + (F8 ? 512 : 0);  // [2][128] float2, one-tile form: the warpgroups' (m, l)
+  static constexpr int kNotes = kQScale + (F8 ? 512 : 0);  // [8 softmax warps][8] ints
+  static constexpr int kMlRows = kNotes + 256;             // [2][128] float2, one-tile form: the warpgroups' (m, l)
   static constexpr int kBytes = kMlRows + 2048;
 };
 static_assert(AttnSmem<128, false>::kBytes <= 232448 && AttnSmem<128, true>::kBytes <= 232448, "shared memory of one CTA");
@@ -218,8 +242,11 @@ struct AttnTc {
   __device__ __forceinline__ uint32_t stage(uint32_t pos) const { return smem + L::kRing + (pos % L::kStages) * L::kTile; }
 
   // ---- loaders --------------------------------------------------------------------------------------
-  static constexpr int kChunks = F8 ? DP / 16 : DP / 8;  // 16-byte pieces of a stored row
-  static constexpr int kRowStep = 128 / kChunks;
+  // A loader warp fills 32 rows of a tile.  A lane looks up one row's place; 32 / kRowsAt lanes then copy that row side by
+  // side, the place handed round by shuffle: one table read per row, and it is made a tile ahead.
+  static constexpr int kChunks = F8 ? DP / 16 : DP / 8;  // 16-byte pieces of a stored row; also steps per tile
+  static constexpr int kRowsAt = 32 / kChunks;           // rows a warp copies in one step
+  __device__ __forceinline__ static int row_of(int tid, int step) { return (tid & ~31) + step * kRowsAt + (tid & 31) / kChunks; }
 
   struct Loader {
     uint32_t pos = 0;      // tiles issued
@@ -243,12 +270,12 @@ struct AttnTc {
     if constexpr (F8) {
       if (pos >= (uint32_t)L::kStages && !wait(empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
       const uint32_t raw = smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16;
-      const int c = tid % kChunks, r0 = tid / kChunks;
+      const int c = tid % kChunks;
       const uint32_t dst = stage(pos) + (c >> 2) * kHalf;
       const int cc = (2 * c) & 7;
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
-        const int r = r0 + i * kRowStep;
+        const int r = row_of(tid, i);
         const uint4 v = ptx::lds128(raw + i * 2048);
         uint32_t h[8];
         e4m3x4_to_f16x2(v.x, h[0], h[1]);
@@ -264,11 +291,11 @@ struct AttnTc {
         tc::sts128(row + (((cc + 1) ^ (r & 7)) << 4), h[4], h[5], h[6], h[7]);
       }
     } else if (look) {
-      const int c = tid % kChunks, r0 = tid / kChunks;
-      const uint32_t at = stage(pos) + (c >> 3) * kHalf + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
+      const int c = tid % kChunks;
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) {
-        const uint4 v = ptx::lds128(at + i * kRowStep * 128);
+        const int r = row_of(tid, i);
+        const uint4 v = ptx::lds128(stage(pos) + (c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4));
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) bad |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
@@ -295,34 +322,34 @@ struct AttnTc {
   }
   // Waits, but never while sitting on tiles that somebody else waits for.
   __device__ __forceinline__ bool wait_or_flush(Loader& ld, int tid, uint32_t bar, uint32_t parity) const {
-    if (__all_sync(0xffffffffu, ptx::mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, tc::test(bar, parity))) return true;
     return flush(ld, tid) && wait(bar, parity);
   }
 
-  // One K or V tile: rows key0 .. key0+127, those outside [ulo, uhi) zeros.
-  __device__ __forceinline__ bool load_tile(Loader& ld, int tid, const AttnItem& it, const AttnSide& side, int key0, int qbits) const {
+  // Page-table entry of the key this lane looks up in tile j (-1: nothing to load).
+  __device__ __forceinline__ int lane_entry(int tid, const AttnItem& it, int j, int& within) const {
+    const int key = j * kAttnTile + tid;
+    within = 0;
+    return key >= it.ulo && key < it.uhi ? (int)attn_page(P, it.b, key, within) : -1;
+  }
+
+  // One K or V tile.  off: where this lane's row starts, elements; negative: a row of zeros.
+  __device__ __forceinline__ bool load_tile(Loader& ld, int tid, const void* from, long long off, int qbits) const {
     const uint32_t pos = ld.pos;
     if constexpr (!F8) {
       if (pos >= (uint32_t)L::kStages && !wait_or_flush(ld, tid, empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
     }
-    const int c = tid % kChunks, r0 = tid / kChunks;
+    const int c = tid % kChunks, src_lane = (tid & 31) / kChunks;
     const bool in_head = c * (F8 ? 16 : 8) < P.head_dim;
-    uint32_t dst = F8 ? smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16
-                      : stage(pos) + (c >> 3) * kHalf + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
-    const char* base = reinterpret_cast<const char*>(side.base);
-    const long long in_row = (long long)it.kvh * side.head + c * (F8 ? 16 : 8);
-#pragma unroll 4
+    const char* base = reinterpret_cast<const char*>(from);
+    const uint32_t dst = F8 ? smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16 : stage(pos) + (c >> 3) * kHalf;
+#pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-      const int key = key0 + r0 + i * kRowStep;
-      const char* src = base;
-      bool take = in_head && key >= it.ulo && key < it.uhi;
-      if (take) {
-        int within;
-        const long long page = attn_page(P, it.b, key, within);
-        take = page >= 0;
-        if (take) src = base + (page * side.page + within * side.token + in_row) * (F8 ? 1 : 2);
-      }
-      tc::cp16(dst + (F8 ? i * 2048 : i * kRowStep * 128), src, take);
+      const int r = row_of(tid, i);
+      const long long at = __shfl_sync(0xffffffffu, off, i * kRowsAt + src_lane);
+      const bool take = in_head && at >= 0;
+      const char* src = take ? base + (at + c * (F8 ? 16 : 8)) * (F8 ? 1 : 2) : base;
+      tc::cp16(F8 ? dst + i * 2048 : dst + r * 128 + (((c ^ r) & 7) << 4), src, take);
     }
     tc::cp_commit();
     ++ld.pos;
@@ -377,8 +404,8 @@ struct AttnTc {
 
   __device__ __forceinline__ void run_loader(int tid) const {
     Loader ld;
-    uint32_t quse[2] = {0, 0};
-    int count = 0;  // items with keys
+    uint32_t qph = 0, qany = 0;  // bit w: phase of Q buffer w, and whether it was in use before
+    int count = 0;               // items with keys
     bool ok = true;
     for (long long idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
       AttnItem it;
@@ -390,20 +417,24 @@ struct AttnTc {
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         if (ONE ? w != (count & 1) : (w == 0 ? r0.a >= r0.b : r1.a >= r1.b)) continue;
-        if (quse[w] > 0 && !(ok = wait_or_flush(ld, tid, smem + L::kQEmpty + 8 * w, (quse[w] - 1) & 1))) break;
+        if (((qany >> w) & 1) && !(ok = wait_or_flush(ld, tid, smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) break;
         load_q(tid, it, it.tok0 + (ONE ? 0 : w * P.tok_per_tile), w == 0 || ONE ? r0.rows : r1.rows, w,
-               ONE ? count & 3 : w + 2 * (quse[w] & 1));
-        ++quse[w];
+               ONE ? count & 3 : w + 2 * ((qph >> w) & 1));
+        qph ^= 1u << w;
+        qany |= 1u << w;
         qbits |= 1 << w;
       }
       if (!ok) break;
+      int within, entry = lane_entry(tid, it, it.j0, within);
       for (int j = it.j0; j < it.j1; ++j) {
-        ok = load_tile(ld, tid, it, P.k, j * kAttnTile, j == it.j0 ? qbits : 0);
+        const int page = entry, tok = within;
+        if (j + 1 < it.j1) entry = lane_entry(tid, it, j + 1, within);
+        ok = load_tile(ld, tid, P.k.base, page < 0 ? -1 : page * P.k.page + tok * P.k.token + it.kvh * P.k.head, j == it.j0 ? qbits : 0);
         if (!ok) break;
         const bool cut = attn_cut(it, r0, j) || (!ONE && attn_cut(it, r1, j));
         if (cut && !(ok = flush(ld, tid))) break;
         if (cut) ld.cut_item = count;
-        ok = load_tile(ld, tid, it, P.v, j * kAttnTile, 0);
+        ok = load_tile(ld, tid, P.v.base, page < 0 ? -1 : page * P.v.page + tok * P.v.token + it.kvh * P.v.head, 0);
         if (!ok) break;
         if (cut && !(ok = flush(ld, tid))) break;
       }
@@ -416,26 +447,25 @@ struct AttnTc {
   // ---- tensor-core issue ----------------------------------------------------------------------------
   __device__ __forceinline__ void issue_qk(uint32_t tmem, int w, int qbuf, uint32_t pos) const {
     constexpr uint32_t idesc = tc::instr_desc(kAttnTile, F8, false);
-    const uint32_t q = smem + L::kQ0 + qbuf * L::kTile, k = stage(pos);
+    const uint32_t q = tc::desc_lo(smem + L::kQ0 + qbuf * L::kTile, 16), k = tc::desc_lo(stage(pos), 16);
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {  // 16 columns of head_dim: 32 bytes inside the 128-byte swizzle span
-      const uint32_t off = (s >> 2) * kHalf + (s & 3) * 32;
-      tc::mma_ss(tmem + w * kAttnTile, tc::smem_desc(q + off, 16, 1024), tc::smem_desc(k + off, 16, 1024), idesc, s > 0);
+      const uint32_t off = ((s >> 2) * kHalf + (s & 3) * 32) >> 4;
+      tc::mma_ss(tmem + w * kAttnTile, q + off, k + off, idesc, s > 0);
     }
     tc::commit(smem + L::kSFull + 8 * w);
   }
   __device__ __forceinline__ void issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc) const {
     constexpr uint32_t idesc = tc::instr_desc(DP, F8, true);
-    const uint32_t v = stage(pos);
+    const uint32_t v = tc::desc_lo(stage(pos), kHalf);
 #pragma unroll
     for (int s = 0; s < kAttnTile / 16; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
-      tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, tc::smem_desc(v + s * 2048, kHalf, 1024), idesc,
-                 acc || s > 0);
+      tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2048 >> 4), idesc, acc || s > 0);
   }
 
   __device__ __forceinline__ void run_mma(uint32_t tmem) const {
     uint32_t pos = 0, count = 0;
-    uint32_t quse[2] = {0, 0}, puse[2] = {0, 0}, ouse[2] = {0, 0};
+    uint32_t qph = 0, pph = 0, oph = 0, oany = 0;  // bit w: phase of a barrier pair's w-th barrier; oany: O_w was in use before
     for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
       AttnItem it;
       if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
@@ -447,22 +477,23 @@ struct AttnTc {
           if (r >= 0) {
             const uint32_t vp = pos + 2 * r + 1;
             if (!wait(full(vp), (vp / L::kStages) & 1)) return;
-            if (!wait(smem + L::kPFull + 8 * w, puse[w] & 1)) return;
-            ++puse[w];
-            if (r < 2 && ouse[w] > 0 && !wait(smem + L::kOFree + 8 * w, (ouse[w] - 1) & 1)) return;
+            if (!wait(smem + L::kPFull + 8 * w, (pph >> w) & 1)) return;
+            pph ^= 1u << w;
+            if (r < 2 && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
             tc::fence_after();
             issue_pv(tmem, w, vp, r >= 2);
             tc::commit(empty(vp));
             if (r + 2 >= nt) {
               tc::commit(smem + L::kOFull + 8 * w);
-              ++ouse[w];
+              oph ^= 1u << w;
+              oany |= 1u << w;
             }
           }
           if (r + 2 < nt) {
             const uint32_t kp = pos + 2 * (r + 2);
             if (r == -2) {
-              if (!wait(smem + L::kQFull + 8 * qb, quse[qb] & 1)) return;
-              ++quse[qb];
+              if (!wait(smem + L::kQFull + 8 * qb, (qph >> qb) & 1)) return;
+              qph ^= 1u << qb;
             }
             if (!wait(full(kp), (kp / L::kStages) & 1)) return;
             tc::fence_after();
@@ -472,34 +503,36 @@ struct AttnTc {
           }
         }
       } else {
-        AttnTileRange rg[2] = {attn_tile_range(P, it, 0), attn_tile_range(P, it, 1)};
+        const AttnTileRange r0 = attn_tile_range(P, it, 0), r1 = attn_tile_range(P, it, 1);
+        const int a[2] = {r0.a, r1.a}, b[2] = {r0.b, r1.b};
         for (int j = it.j0 - 1; j < it.j1; ++j) {
           const uint32_t kp = pos + 2 * (j + 1 - it.j0), vp = kp - 1;
           if (j >= it.j0 && !wait(full(vp), (vp / L::kStages) & 1)) return;
           bool have_k = false;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
-            if (j >= rg[w].a && j < rg[w].b) {
-              if (!wait(smem + L::kPFull + 8 * w, puse[w] & 1)) return;
-              ++puse[w];
-              if (j == rg[w].a && ouse[w] > 0 && !wait(smem + L::kOFree + 8 * w, (ouse[w] - 1) & 1)) return;
+            if (j >= a[w] && j < b[w]) {
+              if (!wait(smem + L::kPFull + 8 * w, (pph >> w) & 1)) return;
+              pph ^= 1u << w;
+              if (j == a[w] && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
               tc::fence_after();
-              issue_pv(tmem, w, vp, j > rg[w].a);
-              if (j == rg[w].b - 1) {
+              issue_pv(tmem, w, vp, j > a[w]);
+              if (j == b[w] - 1) {
                 tc::commit(smem + L::kOFull + 8 * w);
-                ++ouse[w];
+                oph ^= 1u << w;
+                oany |= 1u << w;
               }
             }
-            if (j + 1 >= rg[w].a && j + 1 < rg[w].b) {
-              if (j + 1 == rg[w].a) {
-                if (!wait(smem + L::kQFull + 8 * w, quse[w] & 1)) return;
-                ++quse[w];
+            if (j + 1 >= a[w] && j + 1 < b[w]) {
+              if (j + 1 == a[w]) {
+                if (!wait(smem + L::kQFull + 8 * w, (qph >> w) & 1)) return;
+                qph ^= 1u << w;
               }
               if (!have_k && !wait(full(kp), (kp / L::kStages) & 1)) return;
               have_k = true;
               tc::fence_after();
               issue_qk(tmem, w, w, kp);
-              if (j + 1 == rg[w].b - 1) tc::commit(smem + L::kQEmpty + 8 * w);
+              if (j + 1 == b[w] - 1) tc::commit(smem + L::kQEmpty + 8 * w);
             }
           }
           if (j >= it.j0) tc::commit(empty(vp));
@@ -524,13 +557,13 @@ struct AttnTc {
   // O columns of this lane's row times f
   __device__ __forceinline__ void rescale(uint32_t o, float f) const {
 #pragma unroll
-    for (int k = 0; k < DP; k += 32) {
-      uint32_t r[32];
-      tc::ld32(o + k, r);
+    for (int k = 0; k < DP; k += 16) {
+      uint32_t r[16];
+      tc::ld16(o + k, r);
       tc::wait_ld();
 #pragma unroll
-      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
-      tc::st32(o + k, r);
+      for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * f);
+      tc::st16(o + k, r);
     }
   }
   // 32 columns of the result of a row
@@ -554,8 +587,11 @@ struct AttnTc {
     else if (P.lse != nullptr) P.lse[row * P.heads_q + head] = z * kLn2;
   }
   // The rows of this warp again, one by one, each from the keys it sees and no others.
-  __device__ __forceinline__ void redo(const AttnItem& it, int tok0, int rows, int first) const {
+  __device__ __forceinline__ void redo(long long idx, int w, int first) const {
     const int lane = threadIdx.x & 31;
+    AttnItem it;
+    if (!attn_item(P, idx, it)) return;
+    const int tok0 = it.tok0 + w * P.tok_per_tile, rows = attn_tile_range(P, it, w).rows;
     for (int r = first; r < first + 32 && r < rows; ++r) {
       const int i = tok0 + r / P.group, head = it.kvh * P.group + r % P.group;
       const long long row = it.s.row0 + (long long)i;
@@ -578,16 +614,16 @@ struct AttnTc {
   }
 
   // One score tile: S -> P, running m and l of this lane's row.
-  __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int k0, int lo, int hi, bool masked, bool first, float c,
-                                       float& m, float& l) const {
+  // Columns [from, to) of the tile are keys that the row sees.
+  __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
+                                       float& l) const {
     float s[kAttnTile];
 #pragma unroll
     for (int k = 0; k < kAttnTile; k += 32) tc::ld32(s_addr + k, reinterpret_cast<uint32_t*>(s) + k);
     tc::wait_ld();
     if (masked) {
-      const int a = lo - k0, b = hi - k0;
 #pragma unroll
-      for (int k = 0; k < kAttnTile; ++k) s[k] = k >= a && k < b ? s[k] : kNegInf;
+      for (int k = 0; k < kAttnTile; ++k) s[k] = k >= from && k < to ? s[k] : kNegInf;
     }
     float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
@@ -610,18 +646,18 @@ struct AttnTc {
     const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t p[32];
+    for (int h = 0; h < 4; ++h) {
+      uint32_t p[16];
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const int k = h * 64 + 2 * e;
+      for (int e = 0; e < 16; ++e) {
+        const int k = h * 32 + 2 * e;
         float2 x = __ffma2_rn(make_float2(s[k], s[k + 1]), c2, mc2);
         x.x = tc::ex2(x.x);
         x.y = tc::ex2(x.y);
         sum[e & 1] = __fadd2_rn(sum[e & 1], x);
         p[e] = F8 ? tc::pack_f16(x.x, x.y) : bf_pack(x.x, x.y);
       }
-      tc::st32(s_addr + h * 32, p);
+      tc::st16(s_addr + h * 16, p);
     }
     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
     tc::wait_st();
@@ -631,94 +667,112 @@ struct AttnTc {
   __device__ __forceinline__ void run_softmax(uint32_t tmem, int w) const {
     const int wtid = threadIdx.x & 127, lane = threadIdx.x & 31, first_row = wtid & ~31;
     const uint32_t lanes = (uint32_t)first_row << 16;  // a warp reaches the 32 TMEM lanes of its place in the warpgroup
-    const uint32_t s_addr = tmem + lanes + w * kAttnTile, o_addr = tmem + lanes + 2 * kAttnTile + w * DP;
-    uint32_t suse = 0, ouse[2] = {0, 0}, mluse = 0;
+    uint32_t sph = 0, oph = 0, mlph = 0, ml_any = 0;
     int count = 0;
     const uint32_t all = 0xffffffffu;
-    float2* ml = reinterpret_cast<float2*>(smem_ptr + L::kMlRows);
+    // What the end of an item needs lies in shared memory during its tiles: registers are for the scores.
+    volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 8;
     for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
-      AttnItem it;
-      if (!attn_item(P, idx, it)) continue;
-      const AttnTileRange rg = attn_tile_range(P, it, ONE ? 0 : w);
-      const int tok0 = it.tok0 + (ONE ? 0 : w * P.tok_per_tile);
-      const int i = tok0 + wtid / P.group, head = it.kvh * P.group + wtid % P.group;
-      const bool valid = wtid < rg.rows;
-      const bool busy = first_row < rg.rows;  // some row of this warp is in use
-      const long long row = it.s.row0 + (long long)i;
-      const bool keys = it.j0 < it.j1;
-      const int step = ONE ? 2 : 1;
       float m = kNegInf, l = 0.f, c = P.c;
-      if (keys) {
-        const int lo = valid ? attn_lo(P, it.s, i) : 0, hi = valid ? attn_hi(P, it.s, i) : 0;
-        for (int j = ONE ? it.j0 + w : rg.a; j < (ONE ? it.j1 : rg.b); j += step) {
-          if (!__all_sync(all, wait(smem + L::kSFull + 8 * w, suse & 1))) return;
-          ++suse;
-          if (busy) {
-            tc::fence_after();
-            if (F8) c = row_c(ONE ? count & 3 : w + 2 * (ouse[w] & 1), wtid);
-            const int k0 = j * kAttnTile;
-            const bool masked = k0 < rg.lo_max || k0 + kAttnTile > rg.hi_min;
-            tile(s_addr, o_addr, k0, lo, hi, masked, j == (ONE ? it.j0 + w : rg.a), c, m, l);
+      {
+        AttnItem it;
+        if (!attn_item(P, idx, it)) continue;
+        const AttnTileRange rg = attn_tile_range(P, it, ONE ? 0 : w);
+        const int tok0 = it.tok0 + (ONE ? 0 : w * P.tok_per_tile);
+        __syncwarp();
+        if (lane == 0) {
+          note[0] = it.s.row0;
+          note[1] = tok0;
+          note[2] = it.kvh;
+          note[3] = it.split;
+          note[4] = rg.rows;
+          note[5] = it.j1 - it.j0;
+          note[6] = rg.a < rg.b;
+        }
+        __syncwarp();
+        if (it.j0 < it.j1) {
+          const int i = tok0 + wtid / P.group;
+          const bool valid = wtid < rg.rows, busy = first_row < rg.rows;  // busy: some row of this warp is in use
+          const int lo = valid ? attn_lo(P, it.s, i) : 0, hi = valid ? attn_hi(P, it.s, i) : 0;
+          const int j_first = ONE ? it.j0 + w : rg.a, j_end = ONE ? it.j1 : rg.b;
+          const int plain_from = rg.lo_max, plain_to = rg.hi_min;  // tiles inside [plain_from, plain_to) need no mask
+#pragma unroll 1
+          for (int j = j_first; j < j_end; j += ONE ? 2 : 1) {
+            if (!__all_sync(all, wait(smem + L::kSFull + 8 * w, sph))) return;
+            sph ^= 1;
+            if (busy) {
+              tc::fence_after();
+              if (F8) c = row_c(ONE ? count & 3 : w + 2 * oph, wtid);
+              const int k0 = j * kAttnTile;
+              tile(tmem + lanes + w * kAttnTile, tmem + lanes + 2 * kAttnTile + w * DP, lo - k0, hi - k0,
+                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l);
+            }
+            __syncwarp();
+            if (lane == 0) tc::arrive(smem + L::kPFull + 8 * w);
           }
-          __syncwarp();
-          if (lane == 0) tc::arrive(smem + L::kPFull + 8 * w);
         }
       }
+      const int tiles = note[5], rows = note[4], split = note[3], head = note[2] * P.group + wtid % P.group;
+      const long long row = note[0] + (long long)(note[1] + wtid / P.group);
+      const bool valid = wtid < rows, busy = first_row < rows;
       if (!ONE) {
-        if (rg.a < rg.b) {
-          if (!__all_sync(all, wait(smem + L::kOFull + 8 * w, ouse[w] & 1))) return;
-          ++ouse[w];
+        const bool own = note[6] != 0;  // some tile of the item was this warpgroup's
+        if (own) {
+          if (!__all_sync(all, wait(smem + L::kOFull + 8 * w, oph))) return;
+          oph ^= 1;
           tc::fence_after();
         }
-        const bool again = keys && poison()[count & 3] == count + 1;
+        const bool again = tiles > 0 && poison()[count & 3] == count + 1;
         if (busy && !again) {
           const float inv = l == 0.f ? 0.f : (P.splits > 1 ? 1.f : P.v_scale) / l;
 #pragma unroll
           for (int k = 0; k < DP; k += 32) {
             uint32_t o[32];
             float x[32];
-            if (rg.a < rg.b) {
-              tc::ld32(o_addr + k, o);
+            if (own) {
+              tc::ld32(tmem + lanes + 2 * kAttnTile + w * DP + k, o);
               tc::wait_ld();
             }
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
-            if (valid && !(P.splits > 1 && l == 0.f)) store32(x, row, head, it.split, k);
+            if (valid && !(P.splits > 1 && l == 0.f)) store32(x, row, head, split, k);
           }
-          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), row, head, it.split);
+          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), row, head, split);
         }
-        if (again && busy) redo(it, tok0, rg.rows, first_row);
-        if (rg.a < rg.b) {
+        if (again && busy) redo(idx, w, first_row);
+        if (own) {
           tc::fence_before();
           __syncwarp();
           if (lane == 0) tc::arrive(smem + L::kOFree + 8 * w);
         }
-      } else if (!keys) {
+      } else if (tiles <= 0) {
         if (w == 0 && valid) {
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = 0.f;
           if (P.splits == 1)
             for (int k = 0; k < DP; k += 32) store32(x, row, head, 0, k);
-          store_z(kNegInf, row, head, it.split);
+          store_z(kNegInf, row, head, split);
         }
       } else {
         // the two warpgroups' parts of the same rows
-        const bool two = it.j1 - it.j0 > 1;
-        if (mluse > 0 && !__all_sync(all, wait(smem + L::kMlFree, (mluse - 1) & 1))) return;
+        float2* ml = reinterpret_cast<float2*>(smem_ptr + L::kMlRows);
+        const bool two = tiles > 1;
+        if (ml_any && !__all_sync(all, wait(smem + L::kMlFree, mlph ^ 1))) return;
         ml[w * 128 + wtid] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) tc::arrive(smem + L::kMl);
-        if (!__all_sync(all, wait(smem + L::kMl, mluse & 1))) return;
+        if (!__all_sync(all, wait(smem + L::kMl, mlph))) return;
         const float2 p0 = ml[wtid], p1 = ml[128 + wtid];
         __syncwarp();
         if (lane == 0) tc::arrive(smem + L::kMlFree);
-        ++mluse;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (k == 1 && !two) break;
-          if (!__all_sync(all, wait(smem + L::kOFull + 8 * k, ouse[k] & 1))) return;
-          ++ouse[k];
+        mlph ^= 1;
+        ml_any = 1;
+        if (!__all_sync(all, wait(smem + L::kOFull, oph & 1))) return;
+        oph ^= 1;
+        if (two) {
+          if (!__all_sync(all, wait(smem + L::kOFull + 8, oph >> 1))) return;
+          oph ^= 2;
         }
         tc::fence_after();
         const bool again = poison()[count & 3] == count + 1;
@@ -745,11 +799,11 @@ struct AttnTc {
               if (two && f1 != 0.f) v = fmaf(f1, __uint_as_float(b[e]), v);
               x[e] = lt == 0.f ? 0.f : v * inv;
             }
-            if (valid && !(P.splits > 1 && lt == 0.f)) store32(x, row, head, it.split, k);
+            if (valid && !(P.splits > 1 && lt == 0.f)) store32(x, row, head, split, k);
           }
-          if (valid && w == 0) store_z(lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt)), row, head, it.split);
+          if (valid && w == 0) store_z(lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt)), row, head, split);
         }
-        if (again && busy && w == 0) redo(it, tok0, rg.rows, first_row);
+        if (again && busy && w == 0) redo(idx, 0, first_row);
         tc::fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -757,7 +811,7 @@ struct AttnTc {
           if (two) tc::arrive(smem + L::kOFree + 8);
         }
       }
-      if (keys) ++count;
+      if (tiles > 0) ++count;
     }
   }
 };
@@ -806,15 +860,15 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
 
   const long long items = (long long)P.q_items * P.seqs * P.heads_kv * P.splits;
   const K k{P, smem, smem_raw, items};
-  // 512 threads start with 128 registers each; 2 x 200 + 72 + 40 = 4 x 128
+  // 512 threads start with 128 registers each; 2 x 192 + 64 + 64 = 4 x 128
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     k.run_softmax(tmem, warp >> 2);
   } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     k.run_loader(threadIdx.x - 256);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (threadIdx.x == 384) {
       k.run_mma(tmem);
       // every matrix operation has ended before the tiles and TMEM go away, whichever way the loop ended
