@@ -6,6 +6,8 @@
 // in one pass with a running m (l and o are multiplied by 2^(c (m_old - m_new)) when it grows).  Two parts
 // (o1, z1), (o2, z2) of one row over different keys, z = c m + log2 l, join to (o1 2^(z1-z) + o2 2^(z2-z), z).
 #pragma once
+#include <cuda.h>  // CUtensorMap
+
 #include "qknorm_device.cuh"
 #include "qknorm_ring.cuh"  // ptx helpers
 
@@ -47,7 +49,13 @@ struct AttnParams {
   int tok_per_tile;     // tokens of a query tile: 128 / group
   int tiles_per_item;   // query tiles an item holds: 1 or 2
   int q_items;          // items per (sequence, key head)
+  int box_rows, box_shift;  // tokens of one TMA copy: the largest power of two that divides page_size and a tile; 0: no TMA
   int* error;
+};
+
+// K and V as [page][head][token][d], for the tensor-core kernel's copies.
+struct AttnMaps {
+  CUtensorMap k, v;
 };
 
 // What one sequence's place in the batch says; everything clamped to the call's buffers.
@@ -228,6 +236,7 @@ __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __gri
 
 typedef void (*AttnKernel)(const AttnParams);
 // in qknorm_attn_inst.cu and qknorm_attn_tc_inst.cu
+typedef void (*AttnTcKernel)(const AttnParams, const AttnMaps);
 AttnKernel attn_general_kernel_for(bool e4m3);
 AttnKernel attn_join_kernel_for();
 constexpr int kAttnTcThreads = 512;

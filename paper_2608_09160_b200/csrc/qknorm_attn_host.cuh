@@ -310,9 +310,46 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
 
 // ---- attention over the paged cache ---------------------------------------------------------------
 
-AttnKernel attn_tc_for(int dp, bool e4m3, bool one_tile, int* smem) {
-  if (dp == 64) return e4m3 ? attn_tc_kernel_e4m364(one_tile, smem) : attn_tc_kernel_bf1664(one_tile, smem);
-  return e4m3 ? attn_tc_kernel_e4m3128(one_tile, smem) : attn_tc_kernel_bf16128(one_tile, smem);
+AttnTcKernel attn_tc_for(int dp, bool e4m3, bool one_tile, bool tma, int* smem) {
+  if (dp == 64) return e4m3 ? attn_tc_kernel_e4m364(one_tile, tma, smem) : attn_tc_kernel_bf1664(one_tile, tma, smem);
+  return e4m3 ? attn_tc_kernel_e4m3128(one_tile, tma, smem) : attn_tc_kernel_bf16128(one_tile, tma, smem);
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder, looked up once; nullptr if it cannot be had.
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      p = nullptr;
+    }
+    return (EncodeTiled)p;
+  }();
+  return fn;
+}
+
+// One side of the cache as [page][head][token][d]; a copy takes `rows` tokens of one head and 64 columns, swizzled as the matrix
+// unit reads them (FP8: all columns, as they are, to be widened).  False: no such map (then rows are gathered one by one).
+bool encode_side(CUtensorMap* map, const qknorm_paged_cache& c, const AttnSide& s, int dp, int rows) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t eb = c.e4m3 ? 1 : 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.num_pages};
+  // the stride of an axis of one is never used, but has to look like one
+  const cuuint64_t row = ((cuuint64_t)c.head_dim * eb + 15) / 16 * 16;
+  const cuuint64_t strides[3] = {c.page_size > 1 ? s.token * eb : row, c.heads > 1 ? s.head * eb : row, c.num_pages > 1 ? s.page * eb : row};
+  for (cuuint64_t st : strides)
+    if (st == 0 || st % 16 != 0 || st >= ((cuuint64_t)1 << 40)) return false;
+  const cuuint32_t box[4] = {(cuuint32_t)(c.e4m3 ? dp : 64), (cuuint32_t)rows, 1, 1};
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  return enc(map, c.e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(s.base), dims, strides, box,
+             ones, CU_TENSOR_MAP_INTERLEAVE_NONE, c.e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The tensor-core kernel hands registers from its loaders to its softmax warps: it must have been compiled to start with the
@@ -517,7 +554,17 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
     return finish_launch("attn_general");
   }
   int smem = 0;
-  AttnKernel fn = attn_tc_for(cache->head_dim <= 64 ? 64 : 128, cache->e4m3 != 0, plan.tiles_per_item == 1, &smem);
+  const int dp = cache->head_dim <= 64 ? 64 : 128;
+  AttnMaps maps;
+  memset(&maps, 0, sizeof(maps));
+  int rows = kAttnTile;
+  while (cache->page_size % rows != 0) rows /= 2;
+  const bool tma = rows >= 8 && cache->num_pages > 0 && encode_side(&maps.k, *cache, P.k, dp, rows) && encode_side(&maps.v, *cache, P.v, dp, rows);
+  if (tma) {
+    P.box_rows = rows;
+    while ((1 << P.box_shift) < rows) ++P.box_shift;
+  }
+  AttnTcKernel fn = attn_tc_for(dp, cache->e4m3 != 0, plan.tiles_per_item == 1, tma, &smem);
   rc = allow_dynamic_smem((const void*)fn, smem);
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);
@@ -527,7 +574,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   if (plan.splits > 1 && join_ctas > 0x7fffffff) return QKNORM_ERR_SHAPE;
   long long grid = (long long)plan.q_items * seqs * cache->heads * plan.splits;
   if (grid > dev->sm_count) grid = dev->sm_count;
-  cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P);
+  cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_tc");
   if (rc != QKNORM_OK || plan.splits <= 1) return rc;

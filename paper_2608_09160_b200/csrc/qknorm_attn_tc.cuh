@@ -3,7 +3,10 @@
 // A persistent CTA per SM walks over items: the query rows of one sequence that share a key head -- tokens
 // times the group's query heads, packed into tiles of 128 rows -- and a range of key tiles of 128 keys.
 //   warps 0-7    two softmax warpgroups; a thread owns a row of a 128 x 128 score tile
-//   warps 8-11   loaders: gather K and V rows through the page table into a ring of shared-memory tiles
+//   warp 13      copies K and V tiles into a ring in shared memory with TMA, a box per page and 64 columns
+//   warps 8-11   prepare what has arrived: widen FP8 tiles, blank V rows outside the item's keys; where a page is no
+//                multiple of 8 tokens they gather the rows themselves with cp.async
+//   warps 14-15  gather the query rows
 //   warp 12      issues every tcgen05.mma
 // Scores S_w = Q K^T land in TMEM (128 columns per warpgroup w).  The warpgroup reads them, keeps the running
 // maximum and sum in registers, writes P = 2^(c (s - m)) back over S in 16 bits, and O_w += P V takes P from
@@ -119,6 +122,16 @@ __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+__device__ __forceinline__ void arrive_n(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
+// One box: column x, token t of its page, head h, page p; what lies outside the pool is zeros.
+__device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* map, int x, int t, int h, int p, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(t), "r"(h), "r"(p), "r"(bar)
+      : "memory");
+}
 // 16 bytes from global to shared memory, or 16 zero bytes
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool take) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
@@ -156,7 +169,9 @@ struct AttnSmem {
   static constexpr int kMl = kOFree + 16;
   static constexpr int kMlFree = kMl + 8;
   static constexpr int kDrain = kMlFree + 8;
-  static constexpr int kTmem = kDrain + 8;            // TMEM base address
+  static constexpr int kRawFull = kDrain + 8;         // FP8: a staged tile is there; bf16: a V tile that wants looking at is there
+  static constexpr int kRawEmpty = kRawFull + 8 * (F8 ? kRawStages : kStages);  // FP8: a staged tile has been widened
+  static constexpr int kTmem = kRawEmpty + 8 * kRawStages;  // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
   static constexpr int kPoison = kAbort + 4;          // [4] 1 + number of an item that holds a V row to be careful with
   // FP8 cache: [4][128] bytes, the exponent taken out of a Q row (0: none).  Four sets, because a set is read until the
@@ -198,12 +213,13 @@ __device__ __forceinline__ bool attn_cut(const AttnItem& it, const AttnTileRange
   return j >= r.a && j < r.b && ((k1 < it.uhi ? k1 : it.uhi) > r.hi_min || (k0 > it.ulo ? k0 : it.ulo) < r.lo_max);
 }
 
-template <int DP, bool F8, bool ONE>
+template <int DP, bool F8, bool ONE, bool TMA>
 struct AttnTc {
   using L = AttnSmem<DP, F8>;
   static constexpr int kHalf = kAttnTile * 128;  // bytes of a 64-column half of a tile
 
   const AttnParams& P;
+  const AttnMaps& maps;
   uint32_t smem;
   unsigned char* smem_ptr;
   long long items;
@@ -229,9 +245,9 @@ struct AttnTc {
     return true;
   }
   // Without a look at the abort flag: what is waited for is on its way whatever else happened.
-  __device__ __forceinline__ void wait_drain() const {
+  __device__ __forceinline__ void wait_drain(uint32_t bar, uint32_t parity) const {
     const unsigned long long t0 = ptx::globaltimer_ns();
-    while (!ptx::mbar_try_wait(smem + L::kDrain, 0))
+    while (!ptx::mbar_try_wait(bar, parity))
       if (ptx::globaltimer_ns() - t0 > 2000000000ull) {
         *P.error = 9;
         return;
@@ -241,76 +257,214 @@ struct AttnTc {
   __device__ __forceinline__ uint32_t empty(uint32_t pos) const { return smem + L::kEmpty + 8 * (pos % L::kStages); }
   __device__ __forceinline__ uint32_t stage(uint32_t pos) const { return smem + L::kRing + (pos % L::kStages) * L::kTile; }
 
-  // ---- loaders --------------------------------------------------------------------------------------
-  // A loader warp fills 32 rows of a tile.  A lane looks up one row's place; 32 / kRowsAt lanes then copy that row side by
-  // side, the place handed round by shuffle: one table read per row, and it is made a tile ahead.
-  static constexpr int kChunks = F8 ? DP / 16 : DP / 8;  // 16-byte pieces of a stored row; also steps per tile
-  static constexpr int kRowsAt = 32 / kChunks;           // rows a warp copies in one step
-  __device__ __forceinline__ static int row_of(int tid, int step) { return (tid & ~31) + step * kRowsAt + (tid & 31) / kChunks; }
-
-  struct Loader {
-    uint32_t pos = 0;      // tiles issued
-    int pending = 0;       // issued, not signalled
-    uint64_t qbits = 0;    // per pending tile, oldest lowest, 4 bits: which Q tiles travel with it
-    int cut_item = -1;     // the newest pending tile is V and cut: look through it, name this item
+  // ---- K and V tiles --------------------------------------------------------------------------------
+  // V rows outside the item's keys have to be zeros (a weight of 0 times a NaN would be one), and the rows of a cut tile
+  // looked through.  K may hold anything there: its scores are masked.
+  struct VJob {
+    bool blank, look;
   };
+  __device__ __forceinline__ static VJob v_job(const AttnItem& it, const AttnTileRange& r0, const AttnTileRange& r1, int j) {
+    const int k0 = j * kAttnTile;
+    return VJob{k0 < it.ulo || k0 + kAttnTile > it.uhi, attn_cut(it, r0, j) || (!ONE && attn_cut(it, r1, j))};
+  }
+
+  // Warp 13.  A lane issues one box: the tokens of a page (or 128 of them) times 64 columns (FP8: all columns).
+  __device__ __forceinline__ void run_producer(int lane) const {
+    constexpr int kHalves = F8 ? 1 : DP / 64;
+    const uint32_t all = 0xffffffffu;
+    const int boxes = (kAttnTile >> P.box_shift) * kHalves;  // at most 32: a box has at least 8 tokens
+    const int box = lane / kHalves, half = lane % kHalves;
+    const uint32_t at = F8 ? (uint32_t)(box * P.box_rows * DP) : (uint32_t)(half * kHalf + box * P.box_rows * 128);
+    uint32_t pos = 0, waiting_raw = 0, raw_ph = 0;  // bits by stage: its newest tile went to kRawFull; phase of kRawFull
+    bool ok = true;
+    // page and token of this lane's box of tile j; the page past the last one stands for zeros
+    auto look_up = [&](const AttnItem& it, int j, int& within) {
+      const int key = j * kAttnTile + box * P.box_rows;
+      within = 0;
+      long long page = P.num_pages;
+      if (lane < boxes && key < it.uhi && key + P.box_rows > it.ulo) {
+        const long long e = attn_page(P, it.b, key, within);
+        if (e >= 0) page = e;
+      }
+      return (int)page;
+    };
+    for (long long idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
+      AttnItem it;
+      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+      const AttnTileRange r0 = attn_tile_range(P, it, 0);
+      AttnTileRange r1 = r0;
+      if (!ONE) r1 = attn_tile_range(P, it, 1);
+      int next_within, next = look_up(it, it.j0, next_within);
+      for (int j = it.j0; ok && j < it.j1; ++j) {
+        const int page = next, within = next_within;
+        if (j + 1 < it.j1) next = look_up(it, j + 1, next_within);
+        const VJob job = v_job(it, r0, r1, j);
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          uint32_t bar, dst;
+          if constexpr (F8) {
+            const uint32_t st = pos % L::kRawStages, round = pos / L::kRawStages;
+            if (round > 0 && !(ok = __all_sync(all, wait(smem + L::kRawEmpty + 8 * st, (round - 1) & 1)))) break;
+            bar = smem + L::kRawFull + 8 * st;
+            dst = smem + L::kRawRing + st * L::kRaw;
+            if (lane == 0) ptx::mbar_arrive_expect_tx(bar, L::kRaw);
+          } else {
+            const uint32_t st = pos % L::kStages, round = pos / L::kStages;
+            if (round > 0 && !(ok = __all_sync(all, wait(empty(pos), (round - 1) & 1)))) break;
+            const bool raw = v == 1 && (job.blank || job.look);
+            bar = raw ? smem + L::kRawFull + 8 * st : full(pos);
+            dst = stage(pos);
+            waiting_raw = (waiting_raw & ~(1u << st)) | (raw ? 1u << st : 0u);
+            if (raw) raw_ph ^= 1u << st;
+            if (lane == 0) {
+              if (!raw) tc::arrive_n(bar, 3);  // the four warps that would otherwise have had to look
+              ptx::mbar_arrive_expect_tx(bar, L::kTile);
+            }
+          }
+          __syncwarp();
+          if (lane < boxes) tc::tma4(dst + at, v ? &maps.v : &maps.k, half * 64, within, it.kvh, page, bar);
+          ++pos;
+        }
+      }
+    }
+    if (*abort_flag()) {  // nobody consumes what is still on its way, but it must have landed before the CTA ends
+      const uint32_t n = F8 ? L::kRawStages : L::kStages;
+      for (uint32_t p = pos > n ? pos - n : 0; p < pos; ++p) {
+        if constexpr (F8) wait_drain(smem + L::kRawFull + 8 * (p % n), (p / n) & 1);
+        else if ((waiting_raw >> (p % n)) & 1) wait_drain(smem + L::kRawFull + 8 * (p % n), ((raw_ph >> (p % n)) & 1) ^ 1);
+        else wait_drain(full(p), (p / n) & 1);
+      }
+    }
+  }
 
   __device__ __forceinline__ void signal(uint32_t bar, int lane) const {
     ptx::fence_proxy_async();
     __syncwarp();
     if (lane == 0) tc::arrive(bar);
   }
+  __device__ __forceinline__ static bool odd_bf16(uint32_t u) { return (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u; }
+  __device__ __forceinline__ static bool odd_f16(uint32_t u) { return (u & 0x7c00u) == 0x7c00u || (u & 0x7c000000u) == 0x7c000000u; }
 
-  // The oldest pending tile has arrived (its cp.async group is complete): hand it over.
-  __device__ __forceinline__ bool hand_over(Loader& ld, int tid) const {
-    const int lane = tid & 31;
-    const uint32_t pos = ld.pos - ld.pending;
-    const bool look = ld.cut_item >= 0 && ld.pending == 1;
+  static constexpr int kChunks = F8 ? DP / 16 : DP / 8;  // 16-byte pieces of a stored row; also steps per tile
+  static constexpr int kRowsAt = 32 / kChunks;           // rows a warp handles in one step
+  __device__ __forceinline__ static int row_of(int tid, int step) { return (tid & ~31) + step * kRowsAt + (tid & 31) / kChunks; }
+
+  // Looks through the rows [from, to) of a bf16 tile for infinities and NaN; blanks the others if asked to.
+  __device__ __forceinline__ bool inspect(uint32_t tile_at, int tid, int from, int to, bool blank, bool look) const {
+    const int c = tid % kChunks;
     bool bad = false;
-    if constexpr (F8) {
-      if (pos >= (uint32_t)L::kStages && !wait(empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
-      const uint32_t raw = smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16;
-      const int c = tid % kChunks;
-      const uint32_t dst = stage(pos) + (c >> 2) * kHalf;
-      const int cc = (2 * c) & 7;
+#pragma unroll 4
+    for (int i = 0; i < kChunks; ++i) {
+      const int r = row_of(tid, i);
+      const uint32_t at = tile_at + (c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4);
+      if (r < from || r >= to) {
+        if (blank) tc::sts128(at, 0u, 0u, 0u, 0u);
+      } else if (look) {
+        const uint4 v = ptx::lds128(at);
+        bad |= odd_bf16(v.x) || odd_bf16(v.y) || odd_bf16(v.z) || odd_bf16(v.w);
+      }
+    }
+    return bad;
+  }
+
+  // A staged FP8 tile (row r at raw + r * DP) to fp16; rows outside [from, to) become zeros.
+  __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile_at, int tid, int from, int to, bool look) const {
+    const int c = tid % kChunks, cc = (2 * c) & 7;
+    const uint32_t dst = tile_at + (c >> 2) * kHalf;
+    bool bad = false;
+    constexpr int kBatch = 4 < kChunks ? 4 : kChunks;  // reads ahead of the conversions that wait for them
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i) {
-        const int r = row_of(tid, i);
-        const uint4 v = ptx::lds128(raw + i * 2048);
+    for (int i0 = 0; i0 < kChunks; i0 += kBatch) {
+      uint4 v[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) v[b] = ptx::lds128(raw + row_of(tid, i0 + b) * DP + c * 16);
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int r = row_of(tid, i0 + b);
+        if (r < from || r >= to) v[b] = make_uint4(0u, 0u, 0u, 0u);
         uint32_t h[8];
-        e4m3x4_to_f16x2(v.x, h[0], h[1]);
-        e4m3x4_to_f16x2(v.y, h[2], h[3]);
-        e4m3x4_to_f16x2(v.z, h[4], h[5]);
-        e4m3x4_to_f16x2(v.w, h[6], h[7]);
+        e4m3x4_to_f16x2(v[b].x, h[0], h[1]);
+        e4m3x4_to_f16x2(v[b].y, h[2], h[3]);
+        e4m3x4_to_f16x2(v[b].z, h[4], h[5]);
+        e4m3x4_to_f16x2(v[b].w, h[6], h[7]);
         if (look) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= (h[e] & 0x7c00u) == 0x7c00u || (h[e] & 0x7c000000u) == 0x7c000000u;
+          for (int e = 0; e < 8; ++e) bad |= odd_f16(h[e]);
         }
         const uint32_t row = dst + r * 128;
         tc::sts128(row + ((cc ^ (r & 7)) << 4), h[0], h[1], h[2], h[3]);
         tc::sts128(row + (((cc + 1) ^ (r & 7)) << 4), h[4], h[5], h[6], h[7]);
       }
-    } else if (look) {
-      const int c = tid % kChunks;
-#pragma unroll
-      for (int i = 0; i < kChunks; ++i) {
-        const int r = row_of(tid, i);
-        const uint4 v = ptx::lds128(stage(pos) + (c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4));
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bad |= (u[e] & 0x7f80u) == 0x7f80u || (u[e] & 0x7f800000u) == 0x7f800000u;
+    }
+    return bad;
+  }
+
+  // Warps 8-11 behind TMA copies.
+  __device__ __forceinline__ void run_workers(int tid) const {
+    const uint32_t all = 0xffffffffu;
+    const int lane = tid & 31;
+    uint32_t pos = 0, raw_ph = 0;
+    int count = 0;  // items with keys
+    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+      AttnItem it;
+      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+      const AttnTileRange r0 = attn_tile_range(P, it, 0);
+      AttnTileRange r1 = r0;
+      if (!ONE) r1 = attn_tile_range(P, it, 1);
+      if constexpr (F8) {
+        for (int n = 0; n < 2 * (it.j1 - it.j0); ++n, ++pos) {
+          const int j = it.j0 + (n >> 1), k0 = j * kAttnTile;
+          const bool look = (n & 1) && v_job(it, r0, r1, j).look;
+          const uint32_t st = pos % L::kRawStages;
+          if (!__all_sync(all, wait(smem + L::kRawFull + 8 * st, (pos / L::kRawStages) & 1))) return;
+          if (pos >= (uint32_t)L::kStages && !__all_sync(all, wait(empty(pos), ((pos / L::kStages) - 1) & 1))) return;
+          if (widen(smem + L::kRawRing + st * L::kRaw, stage(pos), tid, it.ulo - k0, it.uhi - k0, look)) poison()[count & 3] = count + 1;
+          signal(full(pos), lane);
+          if (lane == 0) tc::arrive(smem + L::kRawEmpty + 8 * st);
+        }
+      } else {
+        for (int j = it.j0; j < it.j1; ++j) {
+          const VJob job = v_job(it, r0, r1, j);
+          if (!job.blank && !job.look) continue;
+          const uint32_t vp = pos + 2 * (j - it.j0) + 1, st = vp % L::kStages;
+          if (!__all_sync(all, wait(smem + L::kRawFull + 8 * st, (raw_ph >> st) & 1))) return;
+          raw_ph ^= 1u << st;
+          const int k0 = j * kAttnTile;
+          if (inspect(stage(vp), tid, it.ulo - k0, it.uhi - k0, true, job.look)) poison()[count & 3] = count + 1;
+          signal(full(vp), lane);
+        }
+        pos += 2 * (it.j1 - it.j0);
       }
+      ++count;
+    }
+  }
+
+  // Warps 8-11 where a page is no whole number of 8 tokens: they copy the rows themselves.  A warp fills 32 rows of a tile.
+  // A lane looks up one row's place; 32 / kRowsAt lanes then copy that row side by side, the place handed round by
+  // shuffle: one table read per row, and it is made a tile ahead.
+  struct Loader {
+    uint32_t pos = 0;    // tiles issued
+    int pending = 0;     // issued, not handed over
+    int look_item = -1;  // the newest pending tile is V and cut: look through it, name this item
+  };
+
+  // The oldest pending tile has arrived (its cp.async group is complete): hand it over.
+  __device__ __forceinline__ bool hand_over(Loader& ld, int tid) const {
+    const int lane = tid & 31;
+    const uint32_t pos = ld.pos - ld.pending;
+    const bool look = ld.look_item >= 0 && ld.pending == 1;
+    bool bad = false;
+    if constexpr (F8) {
+      if (pos >= (uint32_t)L::kStages && !wait(empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
+      bad = widen(smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw, stage(pos), tid, 0, kAttnTile, look);
+    } else if (look) {
+      bad = inspect(stage(pos), tid, 0, kAttnTile, false, true);
     }
     if (look) {
-      if (bad) poison()[ld.cut_item & 3] = ld.cut_item + 1;
-      ld.cut_item = -1;
+      if (bad) poison()[ld.look_item & 3] = ld.look_item + 1;
+      ld.look_item = -1;
     }
     signal(full(pos), lane);
-    if (lane == 0) {
-      if (ld.qbits & 1) tc::arrive(smem + L::kQFull);
-      if (ld.qbits & 2) tc::arrive(smem + L::kQFull + 8);
-    }
-    ld.qbits >>= 4;
     --ld.pending;
     return true;
   }
@@ -320,40 +474,41 @@ struct AttnTc {
       if (!hand_over(ld, tid)) return false;
     return true;
   }
-  // Waits, but never while sitting on tiles that somebody else waits for.
-  __device__ __forceinline__ bool wait_or_flush(Loader& ld, int tid, uint32_t bar, uint32_t parity) const {
-    if (__all_sync(0xffffffffu, tc::test(bar, parity))) return true;
-    return flush(ld, tid) && wait(bar, parity);
-  }
-
   // Page-table entry of the key this lane looks up in tile j (-1: nothing to load).
   __device__ __forceinline__ int lane_entry(int tid, const AttnItem& it, int j, int& within) const {
     const int key = j * kAttnTile + tid;
     within = 0;
     return key >= it.ulo && key < it.uhi ? (int)attn_page(P, it.b, key, within) : -1;
   }
-
   // One K or V tile.  off: where this lane's row starts, elements; negative: a row of zeros.
-  __device__ __forceinline__ bool load_tile(Loader& ld, int tid, const void* from, long long off, int qbits) const {
+  __device__ __forceinline__ bool load_tile(Loader& ld, int tid, const void* from, long long off) const {
     const uint32_t pos = ld.pos;
     if constexpr (!F8) {
-      if (pos >= (uint32_t)L::kStages && !wait_or_flush(ld, tid, empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
+      // wait, but never while sitting on tiles that somebody else waits for
+      if (pos >= (uint32_t)L::kStages && !__all_sync(0xffffffffu, tc::test(empty(pos), ((pos / L::kStages) - 1) & 1)) &&
+          !(flush(ld, tid) && wait(empty(pos), ((pos / L::kStages) - 1) & 1)))
+        return false;
     }
     const int c = tid % kChunks, src_lane = (tid & 31) / kChunks;
     const bool in_head = c * (F8 ? 16 : 8) < P.head_dim;
     const char* base = reinterpret_cast<const char*>(from);
-    const uint32_t dst = F8 ? smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + tid * 16 : stage(pos) + (c >> 3) * kHalf;
+    const uint32_t dst = F8 ? smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + c * 16 : stage(pos) + (c >> 3) * kHalf;
+    constexpr int kBatch = 8 < kChunks ? 8 : kChunks;  // shuffles ahead of copies: one after the other they would wait in one queue
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-      const int r = row_of(tid, i);
-      const long long at = __shfl_sync(0xffffffffu, off, i * kRowsAt + src_lane);
-      const bool take = in_head && at >= 0;
-      const char* src = take ? base + (at + c * (F8 ? 16 : 8)) * (F8 ? 1 : 2) : base;
-      tc::cp16(F8 ? dst + i * 2048 : dst + r * 128 + (((c ^ r) & 7) << 4), src, take);
+    for (int i0 = 0; i0 < kChunks; i0 += kBatch) {
+      long long at[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) at[b] = __shfl_sync(0xffffffffu, off, (i0 + b) * kRowsAt + src_lane);
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int r = row_of(tid, i0 + b);
+        const bool take = in_head && at[b] >= 0;
+        const char* src = take ? base + (at[b] + c * (F8 ? 16 : 8)) * (F8 ? 1 : 2) : base;
+        tc::cp16(F8 ? dst + r * DP : dst + r * 128 + (((c ^ r) & 7) << 4), src, take);
+      }
     }
     tc::cp_commit();
     ++ld.pos;
-    ld.qbits |= (uint64_t)qbits << (4 * ld.pending);
     ++ld.pending;
     if (ld.pending > L::kLag) {
       tc::cp_wait<L::kLag>();
@@ -362,50 +517,9 @@ struct AttnTc {
     return true;
   }
 
-  // Query tile of `rows` rows from token tok0 into Q buffer `buf`.
-  __device__ __forceinline__ void load_q(int tid, const AttnItem& it, int tok0, int rows, int buf, int scale_set) const {
-    constexpr int kQChunks = DP / 8, kStep = 128 / kQChunks;
-    const int c = tid % kQChunks, r0 = tid / kQChunks;
-    const uint32_t dst = smem + L::kQ0 + buf * L::kTile + (c >> 3) * kHalf + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
-    const bool in_head = c * 8 < P.head_dim;
-    for (int i = 0; i < kQChunks; ++i) {
-      const int r = r0 + i * kStep;
-      const int tok = (int)((unsigned)r / (unsigned)P.group), g = r - tok * P.group;
-      const bool take = in_head && r < rows;
-      const uint16_t* src = P.q;
-      if (take)
-        src += (it.s.row0 + (long long)(tok0 + tok)) * P.ld_q + (long long)(it.kvh * P.group + g) * P.head_dim + c * 8;
-      if constexpr (!F8) {
-        tc::cp16(dst + i * kStep * 128, src, take);
-      } else {
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (take) v = *reinterpret_cast<const uint4*>(src);
-        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-        uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t lo = u[e] & 0x7fffu, hi = (u[e] >> 16) & 0x7fffu;
-          mag = max(mag, max(lo, hi));
-        }
-#pragma unroll
-        for (int off = kQChunks / 2; off > 0; off >>= 1) mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, off));
-        // bring the row's largest exponent to 2^8; rows of zeros, tiny rows and rows with infinities or NaN as they are
-        const int e = (int)(mag >> 7);
-        const bool scaled = e > 16 && e < 255;
-        const float f = scaled ? __uint_as_float((uint32_t)(127 + 135 - e) << 23) : 1.f;
-        uint32_t h[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) h[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
-        tc::sts128(dst + i * kStep * 128, h[0], h[1], h[2], h[3]);
-        if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
-      }
-    }
-  }
-
   __device__ __forceinline__ void run_loader(int tid) const {
     Loader ld;
-    uint32_t qph = 0, qany = 0;  // bit w: phase of Q buffer w, and whether it was in use before
-    int count = 0;               // items with keys
+    int count = 0;  // items with keys
     bool ok = true;
     for (long long idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
       AttnItem it;
@@ -413,35 +527,96 @@ struct AttnTc {
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
       AttnTileRange r1 = r0;
       if (!ONE) r1 = attn_tile_range(P, it, 1);
-      int qbits = 0;
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        if (ONE ? w != (count & 1) : (w == 0 ? r0.a >= r0.b : r1.a >= r1.b)) continue;
-        if (((qany >> w) & 1) && !(ok = wait_or_flush(ld, tid, smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) break;
-        load_q(tid, it, it.tok0 + (ONE ? 0 : w * P.tok_per_tile), w == 0 || ONE ? r0.rows : r1.rows, w,
-               ONE ? count & 3 : w + 2 * ((qph >> w) & 1));
-        qph ^= 1u << w;
-        qany |= 1u << w;
-        qbits |= 1 << w;
-      }
-      if (!ok) break;
       int within, entry = lane_entry(tid, it, it.j0, within);
       for (int j = it.j0; j < it.j1; ++j) {
         const int page = entry, tok = within;
         if (j + 1 < it.j1) entry = lane_entry(tid, it, j + 1, within);
-        ok = load_tile(ld, tid, P.k.base, page < 0 ? -1 : page * P.k.page + tok * P.k.token + it.kvh * P.k.head, j == it.j0 ? qbits : 0);
+        ok = load_tile(ld, tid, P.k.base, page < 0 ? -1 : page * P.k.page + tok * P.k.token + it.kvh * P.k.head);
         if (!ok) break;
-        const bool cut = attn_cut(it, r0, j) || (!ONE && attn_cut(it, r1, j));
-        if (cut && !(ok = flush(ld, tid))) break;
-        if (cut) ld.cut_item = count;
-        ok = load_tile(ld, tid, P.v.base, page < 0 ? -1 : page * P.v.page + tok * P.v.token + it.kvh * P.v.head, 0);
+        const bool look = v_job(it, r0, r1, j).look;
+        if (look && !(ok = flush(ld, tid))) break;
+        if (look) ld.look_item = count;
+        ok = load_tile(ld, tid, P.v.base, page < 0 ? -1 : page * P.v.page + tok * P.v.token + it.kvh * P.v.head);
         if (!ok) break;
-        if (cut && !(ok = flush(ld, tid))) break;
+        if (look && !(ok = flush(ld, tid))) break;
       }
       ++count;
     }
     if (ok) flush(ld, tid);
     tc::cp_wait<0>();
+  }
+
+  // ---- query tiles ----------------------------------------------------------------------------------
+  static constexpr int kQThreads = 64;  // warps 14-15
+
+  // Query tile of `rows` rows from token tok0 into Q buffer `buf`; the rest of the last 32 rows in use is zeros.
+  __device__ __forceinline__ void load_q(int tid, const AttnItem& it, int tok0, int rows, int buf, int scale_set) const {
+    constexpr int kQChunks = DP / 8, kStep = kQThreads / kQChunks, kBatch = 4;
+    const int c = tid % kQChunks, r0 = tid / kQChunks;
+    const uint32_t dst = smem + L::kQ0 + buf * L::kTile + (c >> 3) * kHalf;
+    const bool in_head = c * 8 < P.head_dim;
+    const int end = (rows + 31) & ~31;
+    for (int i0 = r0; i0 < end; i0 += kStep * kBatch) {
+      uint4 v[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int r = i0 + b * kStep;
+        v[b] = make_uint4(0u, 0u, 0u, 0u);
+        if (in_head && r < rows) {
+          const int tok = (int)((unsigned)r / (unsigned)P.group), g = r - tok * P.group;
+          v[b] = *reinterpret_cast<const uint4*>(P.q + (it.s.row0 + (long long)(tok0 + tok)) * P.ld_q +
+                                                 (long long)(it.kvh * P.group + g) * P.head_dim + c * 8);
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        const int r = i0 + b * kStep;  // below 128: kStep * kBatch divides 32
+        const uint32_t at = dst + r * 128 + (((c ^ r) & 7) << 4);
+        if constexpr (!F8) {
+          tc::sts128(at, v[b].x, v[b].y, v[b].z, v[b].w);
+        } else {
+          const uint32_t u[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
+          uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t lo = u[e] & 0x7fffu, hi = (u[e] >> 16) & 0x7fffu;
+            mag = max(mag, max(lo, hi));
+          }
+#pragma unroll
+          for (int off = kQChunks / 2; off > 0; off >>= 1) mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, off));
+          // bring the row's largest exponent to 2^8; rows of zeros, tiny rows and rows with infinities or NaN as they are
+          const int e = (int)(mag >> 7);
+          const bool scaled = e > 16 && e < 255;
+          const float f = scaled ? __uint_as_float((uint32_t)(127 + 135 - e) << 23) : 1.f;
+          uint32_t h[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
+          tc::sts128(at, h[0], h[1], h[2], h[3]);
+          if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
+        }
+      }
+    }
+  }
+
+  __device__ __forceinline__ void run_q(int tid) const {
+    const uint32_t all = 0xffffffffu;
+    uint32_t qph = 0, qany = 0;  // bit w: phase of Q buffer w, and whether it was in use before
+    int count = 0;
+    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+      AttnItem it;
+      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const AttnTileRange r = attn_tile_range(P, it, ONE ? 0 : w);
+        if (ONE ? w != (count & 1) : r.a >= r.b) continue;
+        if (((qany >> w) & 1) && !__all_sync(all, wait(smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) return;
+        load_q(tid, it, it.tok0 + (ONE ? 0 : w * P.tok_per_tile), r.rows, w, ONE ? count & 3 : w + 2 * ((qph >> w) & 1));
+        signal(smem + L::kQFull + 8 * w, tid & 31);
+        qph ^= 1u << w;
+        qany |= 1u << w;
+      }
+      ++count;
+    }
   }
 
   // ---- tensor-core issue ----------------------------------------------------------------------------
@@ -816,10 +991,11 @@ struct AttnTc {
   }
 };
 
-template <int DP, bool F8, bool ONE>
-__global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams P) {
+template <int DP, bool F8, bool ONE, bool TMA>
+__global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams P,
+                                                                    const __grid_constant__ AttnMaps maps) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  using K = AttnTc<DP, F8, ONE>;
+  using K = AttnTc<DP, F8, ONE, TMA>;
   using L = AttnSmem<DP, F8>;
   const uint32_t smem = ptx::smem_u32(smem_raw);
   const int warp = threadIdx.x >> 5;
@@ -831,9 +1007,14 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     for (int i = 0; i < L::kStages; ++i) {
       ptx::mbar_init(smem + L::kFull + 8 * i, 4);
       ptx::mbar_init(smem + L::kEmpty + 8 * i, 1);
+      if (!F8) ptx::mbar_init(smem + L::kRawFull + 8 * i, 1);
+    }
+    for (int i = 0; i < L::kRawStages; ++i) {
+      ptx::mbar_init(smem + L::kRawFull + 8 * i, 1);
+      ptx::mbar_init(smem + L::kRawEmpty + 8 * i, 4);
     }
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(smem + L::kQFull + 8 * i, 4);
+      ptx::mbar_init(smem + L::kQFull + 8 * i, 2);
       ptx::mbar_init(smem + L::kQEmpty + 8 * i, 1);
       ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
@@ -859,23 +1040,26 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   const long long items = (long long)P.q_items * P.seqs * P.heads_kv * P.splits;
-  const K k{P, smem, smem_raw, items};
+  const K k{P, maps, smem, smem_raw, items};
   // 512 threads start with 128 registers each; 2 x 192 + 64 + 64 = 4 x 128
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     k.run_softmax(tmem, warp >> 2);
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    k.run_loader(threadIdx.x - 256);
+    if (TMA) k.run_workers(threadIdx.x - 256);
+    else k.run_loader(threadIdx.x - 256);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (threadIdx.x == 384) {
       k.run_mma(tmem);
       // every matrix operation has ended before the tiles and TMEM go away, whichever way the loop ended
       tc::commit(smem + L::kDrain);
-      k.wait_drain();
+      k.wait_drain(smem + L::kDrain, 0);
     }
     __syncwarp();
+    if (TMA && warp == 13) k.run_producer(threadIdx.x & 31);
+    if (warp >= 14) k.run_q(threadIdx.x - 448);
   }
   tc::fence_before();
   __syncthreads();
