@@ -137,6 +137,7 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool take) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -367,34 +368,33 @@ struct AttnTc {
     return bad;
   }
 
-  // A staged FP8 tile (row r at raw + r * DP) to fp16; rows outside [from, to) become zeros.
-  __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile_at, int tid, int from, int to, bool look) const {
-    const int c = tid % kChunks, cc = (2 * c) & 7;
-    const uint32_t dst = tile_at + (c >> 2) * kHalf;
+  // A staged FP8 tile (row r at raw + r * DP) to fp16.  CARE: rows outside [from, to) become zeros, the others are looked
+  // through for NaN.
+  template <bool CARE>
+  __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile_at, int tid, int from, int to) const {
+    const int c = tid % kChunks, r0 = row_of(tid, 0);
+    const uint32_t src = raw + r0 * DP + c * 16;
+    const uint32_t dst = tile_at + (c >> 2) * kHalf + r0 * 128, turn = (((2 * c) ^ r0) & 7) << 4;
     bool bad = false;
-    constexpr int kBatch = 4 < kChunks ? 4 : kChunks;  // reads ahead of the conversions that wait for them
+    uint4 v[kChunks];  // every read ahead of the conversions that wait for it
 #pragma unroll
-    for (int i0 = 0; i0 < kChunks; i0 += kBatch) {
-      uint4 v[kBatch];
+    for (int i = 0; i < kChunks; ++i) v[i] = ptx::lds128(src + i * kRowsAt * DP);
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) v[b] = ptx::lds128(raw + row_of(tid, i0 + b) * DP + c * 16);
+    for (int i = 0; i < kChunks; ++i) {
+      if (CARE && (r0 + i * kRowsAt < from || r0 + i * kRowsAt >= to)) v[i] = make_uint4(0u, 0u, 0u, 0u);
+      uint32_t h[8];
+      e4m3x4_to_f16x2(v[i].x, h[0], h[1]);
+      e4m3x4_to_f16x2(v[i].y, h[2], h[3]);
+      e4m3x4_to_f16x2(v[i].z, h[4], h[5]);
+      e4m3x4_to_f16x2(v[i].w, h[6], h[7]);
+      if (CARE) {
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int r = row_of(tid, i0 + b);
-        if (r < from || r >= to) v[b] = make_uint4(0u, 0u, 0u, 0u);
-        uint32_t h[8];
-        e4m3x4_to_f16x2(v[b].x, h[0], h[1]);
-        e4m3x4_to_f16x2(v[b].y, h[2], h[3]);
-        e4m3x4_to_f16x2(v[b].z, h[4], h[5]);
-        e4m3x4_to_f16x2(v[b].w, h[6], h[7]);
-        if (look) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= odd_f16(h[e]);
-        }
-        const uint32_t row = dst + r * 128;
-        tc::sts128(row + ((cc ^ (r & 7)) << 4), h[0], h[1], h[2], h[3]);
-        tc::sts128(row + (((cc + 1) ^ (r & 7)) << 4), h[4], h[5], h[6], h[7]);
+        for (int e = 0; e < 8; ++e) bad |= odd_f16(h[e]);
       }
+      // the swizzle of row r0 + i * kRowsAt differs from row r0's by a constant: r0 % 8 < kRowsAt, or kRowsAt is 8
+      const uint32_t at = dst + i * kRowsAt * 128 + (turn ^ (((i * kRowsAt) & 7) << 4));
+      tc::sts128(at, h[0], h[1], h[2], h[3]);
+      tc::sts128(at ^ 16, h[4], h[5], h[6], h[7]);
     }
     return bad;
   }
@@ -414,11 +414,16 @@ struct AttnTc {
       if constexpr (F8) {
         for (int n = 0; n < 2 * (it.j1 - it.j0); ++n, ++pos) {
           const int j = it.j0 + (n >> 1), k0 = j * kAttnTile;
-          const bool look = (n & 1) && v_job(it, r0, r1, j).look;
+          const VJob job = v_job(it, r0, r1, j);
           const uint32_t st = pos % L::kRawStages;
           if (!__all_sync(all, wait(smem + L::kRawFull + 8 * st, (pos / L::kRawStages) & 1))) return;
           if (pos >= (uint32_t)L::kStages && !__all_sync(all, wait(empty(pos), ((pos / L::kStages) - 1) & 1))) return;
-          if (widen(smem + L::kRawRing + st * L::kRaw, stage(pos), tid, it.ulo - k0, it.uhi - k0, look)) poison()[count & 3] = count + 1;
+          const uint32_t raw = smem + L::kRawRing + st * L::kRaw;
+          if ((n & 1) && (job.blank || job.look)) {
+            if (widen<true>(raw, stage(pos), tid, it.ulo - k0, it.uhi - k0) && job.look) poison()[count & 3] = count + 1;
+          } else {
+            widen<false>(raw, stage(pos), tid, 0, 0);
+          }
           signal(full(pos), lane);
           if (lane == 0) tc::arrive(smem + L::kRawEmpty + 8 * st);
         }
@@ -456,7 +461,8 @@ struct AttnTc {
     bool bad = false;
     if constexpr (F8) {
       if (pos >= (uint32_t)L::kStages && !wait(empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
-      bad = widen(smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw, stage(pos), tid, 0, kAttnTile, look);
+      const uint32_t raw = smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw;
+      bad = look ? widen<true>(raw, stage(pos), tid, 0, kAttnTile) : widen<false>(raw, stage(pos), tid, 0, 0);
     } else if (look) {
       bad = inspect(stage(pos), tid, 0, kAttnTile, false, true);
     }
@@ -551,30 +557,33 @@ struct AttnTc {
 
   // Query tile of `rows` rows from token tok0 into Q buffer `buf`; the rest of the last 32 rows in use is zeros.
   __device__ __forceinline__ void load_q(int tid, const AttnItem& it, int tok0, int rows, int buf, int scale_set) const {
-    constexpr int kQChunks = DP / 8, kStep = kQThreads / kQChunks, kBatch = 4;
+    constexpr int kQChunks = DP / 8, kStep = kQThreads / kQChunks;
     const int c = tid % kQChunks, r0 = tid / kQChunks;
     const uint32_t dst = smem + L::kQ0 + buf * L::kTile + (c >> 3) * kHalf;
     const bool in_head = c * 8 < P.head_dim;
     const int end = (rows + 31) & ~31;
-    for (int i0 = r0; i0 < end; i0 += kStep * kBatch) {
-      uint4 v[kBatch];
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int r = i0 + b * kStep;
-        v[b] = make_uint4(0u, 0u, 0u, 0u);
-        if (in_head && r < rows) {
-          const int tok = (int)((unsigned)r / (unsigned)P.group), g = r - tok * P.group;
-          v[b] = *reinterpret_cast<const uint4*>(P.q + (it.s.row0 + (long long)(tok0 + tok)) * P.ld_q +
-                                                 (long long)(it.kvh * P.group + g) * P.head_dim + c * 8);
-        }
+    const uint16_t* from = P.q + (it.s.row0 + (long long)tok0) * P.ld_q + (long long)(it.kvh * P.group) * P.head_dim + c * 8;
+    auto row_at = [&](int r) {
+      const int tok = (int)((unsigned)r / (unsigned)P.group), g = r - tok * P.group;
+      return from + tok * P.ld_q + g * P.head_dim;
+    };
+    if constexpr (!F8) {  // asynchronous: every row is on its way before the first is waited for
+      for (int r = r0; r < end; r += kStep) {
+        const bool take = in_head && r < rows;
+        tc::cp16(dst + r * 128 + (((c ^ r) & 7) << 4), take ? row_at(r) : P.q, take);
       }
+    } else {
+      constexpr int kBatch = 32 / kStep;
+      for (int i0 = r0; i0 < end; i0 += 32) {
+        uint4 v[kBatch];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int r = i0 + b * kStep;  // below 128: kStep * kBatch divides 32
-        const uint32_t at = dst + r * 128 + (((c ^ r) & 7) << 4);
-        if constexpr (!F8) {
-          tc::sts128(at, v[b].x, v[b].y, v[b].z, v[b].w);
-        } else {
+        for (int b = 0; b < kBatch; ++b) {
+          const int r = i0 + b * kStep;
+          v[b] = in_head && r < rows ? *reinterpret_cast<const uint4*>(row_at(r)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int r = i0 + b * kStep;
           const uint32_t u[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
           uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
 #pragma unroll
@@ -591,7 +600,7 @@ struct AttnTc {
           uint32_t h[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) h[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
-          tc::sts128(at, h[0], h[1], h[2], h[3]);
+          tc::sts128(dst + r * 128 + (((c ^ r) & 7) << 4), h[0], h[1], h[2], h[3]);
           if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
         }
       }
@@ -611,6 +620,7 @@ struct AttnTc {
         if (ONE ? w != (count & 1) : r.a >= r.b) continue;
         if (((qany >> w) & 1) && !__all_sync(all, wait(smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) return;
         load_q(tid, it, it.tok0 + (ONE ? 0 : w * P.tok_per_tile), r.rows, w, ONE ? count & 3 : w + 2 * ((qph >> w) & 1));
+        if (!F8) tc::cp_wait_all();
         signal(smem + L::kQFull + 8 * w, tid & 31);
         qph ^= 1u << w;
         qany |= 1u << w;
