@@ -78,10 +78,10 @@ WarpKernel warp_kernel_for(int l, bool exact, int elem_bytes) {
 }
 
 // per (cache format, padded head_dim), defined in qknorm_attn_tc_inst.cu (one translation unit each)
-AttnTcKernel attn_tc_kernel_bf1664(bool one_tile, bool tma, int* smem_bytes);
-AttnTcKernel attn_tc_kernel_bf16128(bool one_tile, bool tma, int* smem_bytes);
-AttnTcKernel attn_tc_kernel_e4m364(bool one_tile, bool tma, int* smem_bytes);
-AttnTcKernel attn_tc_kernel_e4m3128(bool one_tile, bool tma, int* smem_bytes);
+AttnTcKernel attn_tc_kernel_bf1664(int form, bool tma, int* smem_bytes);
+AttnTcKernel attn_tc_kernel_bf16128(int form, bool tma, int* smem_bytes);
+AttnTcKernel attn_tc_kernel_e4m364(int form, bool tma, int* smem_bytes);
+AttnTcKernel attn_tc_kernel_e4m3128(int form, bool tma, int* smem_bytes);
 
 // Set by a ring kernel whose bounded wait ran out (0 = never happened).
 __device__ __align__(8) int g_ring_error[8] = {0, 0, 0, 0, 0, 0, 0, 0};  // word 0 is the error word; 1-2: where it happened

@@ -239,6 +239,8 @@ typedef void (*AttnKernel)(const AttnParams);
 typedef void (*AttnTcKernel)(const AttnParams, const AttnMaps);
 AttnKernel attn_general_kernel_for(bool e4m3);
 AttnKernel attn_join_kernel_for();
+// forms of the tensor-core kernel: two query tiles per item, one, one of at most 32 rows
+constexpr int kAttnTwo = 0, kAttnOne = 1, kAttnQuad = 2;
 constexpr int kAttnTcThreads = 512;
 constexpr int kAttnTcRegs = 128;  // registers per thread at launch that the kernel's register split counts on
 

@@ -310,9 +310,9 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
 
 // ---- attention over the paged cache ---------------------------------------------------------------
 
-AttnTcKernel attn_tc_for(int dp, bool e4m3, bool one_tile, bool tma, int* smem) {
-  if (dp == 64) return e4m3 ? attn_tc_kernel_e4m364(one_tile, tma, smem) : attn_tc_kernel_bf1664(one_tile, tma, smem);
-  return e4m3 ? attn_tc_kernel_e4m3128(one_tile, tma, smem) : attn_tc_kernel_bf16128(one_tile, tma, smem);
+AttnTcKernel attn_tc_for(int dp, bool e4m3, int form, bool tma, int* smem) {
+  if (dp == 64) return e4m3 ? attn_tc_kernel_e4m364(form, tma, smem) : attn_tc_kernel_bf1664(form, tma, smem);
+  return e4m3 ? attn_tc_kernel_e4m3128(form, tma, smem) : attn_tc_kernel_bf16128(form, tma, smem);
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -355,7 +355,7 @@ bool encode_side(CUtensorMap* map, const qknorm_paged_cache& c, const AttnSide& 
 // The tensor-core kernel hands registers from its loaders to its softmax warps: it must have been compiled to start with the
 // number the split adds up to, or the warps that ask for more would wait for ever.
 int attn_tc_registers_ok(const void* fn) {
-  static const void* known[16];
+  static const void* known[32];
   static int n = 0;
   std::lock_guard<std::mutex> lock(g_occ_mutex);
   for (int i = 0; i < n; ++i)
@@ -364,13 +364,14 @@ int attn_tc_registers_ok(const void* fn) {
   const cudaError_t e = cudaFuncGetAttributes(&a, fn);
   if (e != cudaSuccess) return set_cuda_error(e);
   if (a.numRegs != kAttnTcRegs) return set_cuda_error(cudaErrorLaunchOutOfResources);
-  if (n < 16) known[n++] = fn;
+  if (n < 32) known[n++] = fn;
   return QKNORM_OK;
 }
 
 // How a call is cut: sizes only, so that the workspace can be asked for beforehand.
 struct AttnPlan {
   bool tc = false;
+  int form = kAttnTwo;
   int tok_per_tile = 1, tiles_per_item = 1, q_items = 1, splits = 1, chunk_tiles = 1;
 };
 
@@ -382,6 +383,7 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   p.tok_per_tile = kAttnTile / group;
   if ((int64_t)max_q > T) max_q = (int)T;
   p.tiles_per_item = max_q <= p.tok_per_tile ? 1 : 2;
+  p.form = p.tiles_per_item == 2 ? kAttnTwo : max_q * group <= 32 ? kAttnQuad : kAttnOne;
   const int per_item = p.tok_per_tile * p.tiles_per_item;
   p.q_items = (max_q + per_item - 1) / per_item;
   int64_t tiles = (max_keys + kAttnTile - 1) / kAttnTile;
@@ -564,7 +566,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
     P.box_rows = rows;
     while ((1 << P.box_shift) < rows) ++P.box_shift;
   }
-  AttnTcKernel fn = attn_tc_for(dp, cache->e4m3 != 0, plan.tiles_per_item == 1, tma, &smem);
+  AttnTcKernel fn = attn_tc_for(dp, cache->e4m3 != 0, plan.form, tma, &smem);
   rc = allow_dynamic_smem((const void*)fn, smem);
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);

@@ -13,11 +13,15 @@
 // TMEM and V, keys by head_dim as it lies in the cache, as a transposed operand.  O_w stays in TMEM; it is rescaled only
 // when the maximum has grown by more than 2^8, so P is at most 2^8 and the rescale is rare.
 //
-// Two forms:
-//   two query tiles  (chunks): tile w belongs to warpgroup w, both use every K and V tile;
-//   one query tile   (single tokens, short chunks): key tiles alternate between the warpgroups, each with an O of its
-//                    own over the same rows, joined through TMEM at the end of the item.
-// Both keep the tensor pipe on one warpgroup's tile while the other one is in its exponentials.
+// Three forms:
+//   two query tiles     (chunks): tile w belongs to warpgroup w, both use every K and V tile;
+//   one query tile      (short chunks): key tiles alternate between the warpgroups, each with an O of its own over the
+//                       same rows, joined through TMEM at the end of the item;
+//   one tile of 32 rows (single tokens): as before, and the rows stand in all four quarters of the tile's 128 lanes.  A
+//                       warp can only reach its own quarter; so the warp of quarter i takes keys 32 i .. 32 i + 31 of the
+//                       tile (P is zero elsewhere in its quarter), four warps share what one would do alone, and the eight
+//                       parts of a row are joined through shared memory at the end of the item.
+// The first two keep the tensor pipe on one warpgroup's tile while the other one is in its exponentials.
 //
 // Rows no token fills, keys outside the item's range and head_dim up to the next multiple of 64 are zeros in
 // shared memory, never memory of somebody else.  Inside a tile that the causal edge or the window cuts, a V row with an
@@ -152,14 +156,12 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, ui
 template <int DP, bool F8>
 struct AttnSmem {
   static constexpr int kTile = kAttnTile * DP * 2;  // a 16-bit tile of Q, K or V
-  static constexpr int kRaw = kAttnTile * DP;       // a staged FP8 tile
-  static constexpr int kStages = F8 ? (DP == 128 ? 3 : 6) : (DP == 128 ? 5 : 10);
-  static constexpr int kRawStages = F8 ? 4 : 0;
-  static constexpr int kLag = F8 ? kRawStages - 1 : kStages - 2;  // tiles in flight behind the newest
-  static constexpr int kQ0 = 0;                                   // two Q tiles
+  static constexpr int kRaw = kAttnTile * DP;       // an FP8 tile; it lands in the upper half of its stage and is widened over itself
+  static constexpr int kStages = DP == 128 ? 5 : 10;
+  static constexpr int kLag = kStages - 2;  // gathered tiles in flight behind the newest
+  static constexpr int kQ0 = 0;             // two Q tiles
   static constexpr int kRing = 2 * kTile;
-  static constexpr int kRawRing = kRing + kStages * kTile;
-  static constexpr int kFull = kRawRing + kRawStages * kRaw;  // mbarriers, 8 bytes each
+  static constexpr int kFull = kRing + kStages * kTile;  // mbarriers, 8 bytes each
   static constexpr int kEmpty = kFull + 8 * kStages;
   static constexpr int kQFull = kEmpty + 8 * kStages;
   static constexpr int kQEmpty = kQFull + 16;
@@ -170,19 +172,21 @@ struct AttnSmem {
   static constexpr int kMl = kOFree + 16;
   static constexpr int kMlFree = kMl + 8;
   static constexpr int kDrain = kMlFree + 8;
-  static constexpr int kRawFull = kDrain + 8;         // FP8: a staged tile is there; bf16: a V tile that wants looking at is there
-  static constexpr int kRawEmpty = kRawFull + 8 * (F8 ? kRawStages : kStages);  // FP8: a staged tile has been widened
-  static constexpr int kTmem = kRawEmpty + 8 * kRawStages;  // TMEM base address
+  static constexpr int kRawFull = kDrain + 8;         // per stage: an FP8 tile, or a bf16 V tile that wants looking at, is there
+  static constexpr int kWork = kRawFull + 8 * kStages;  // the four warps that widen have all read the tile
+  static constexpr int kPass = kWork + 8;             // the softmax warps' steps through the join of an item
+  static constexpr int kTmem = kPass + 8;             // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
   static constexpr int kPoison = kAbort + 4;          // [4] 1 + number of an item that holds a V row to be careful with
   // FP8 cache: [4][128] bytes, the exponent taken out of a Q row (0: none).  Four sets, because a set is read until the
   // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
   // round again only after the tensor warp has seen the scores of the item before last consumed.
   static constexpr int kQScale = kPoison + 16;
-  static constexpr int kNotes = kQScale + (F8 ? 512 : 0);  // [8 softmax warps][8] ints
-  static constexpr int kMlRows = kNotes + 256;             // [2][128] float2, one-tile form: the warpgroups' (m, l)
+  static constexpr int kNotes = kQScale + (F8 ? 512 : 0);  // [8 softmax warps][7] ints
+  static constexpr int kMlRows = kNotes + 224;             // [8 softmax warps][32] float2, one-tile forms: (m, l) of their parts
   static constexpr int kBytes = kMlRows + 2048;
 };
+
 static_assert(AttnSmem<128, false>::kBytes <= 232448 && AttnSmem<128, true>::kBytes <= 232448, "shared memory of one CTA");
 
 // Key tiles [a, b) that query tile w of the item uses, and how its rows' ranges spread.
@@ -214,9 +218,11 @@ __device__ __forceinline__ bool attn_cut(const AttnItem& it, const AttnTileRange
   return j >= r.a && j < r.b && ((k1 < it.uhi ? k1 : it.uhi) > r.hi_min || (k0 > it.ulo ? k0 : it.ulo) < r.lo_max);
 }
 
-template <int DP, bool F8, bool ONE, bool TMA>
+template <int DP, bool F8, int FORM, bool TMA>
 struct AttnTc {
   using L = AttnSmem<DP, F8>;
+  static constexpr bool ONE = FORM != kAttnTwo;
+  static constexpr bool QUAD = FORM == kAttnQuad;
   static constexpr int kHalf = kAttnTile * 128;  // bytes of a 64-column half of a tile
 
   const AttnParams& P;
@@ -303,24 +309,16 @@ struct AttnTc {
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           uint32_t bar, dst;
-          if constexpr (F8) {
-            const uint32_t st = pos % L::kRawStages, round = pos / L::kRawStages;
-            if (round > 0 && !(ok = __all_sync(all, wait(smem + L::kRawEmpty + 8 * st, (round - 1) & 1)))) break;
-            bar = smem + L::kRawFull + 8 * st;
-            dst = smem + L::kRawRing + st * L::kRaw;
-            if (lane == 0) ptx::mbar_arrive_expect_tx(bar, L::kRaw);
-          } else {
-            const uint32_t st = pos % L::kStages, round = pos / L::kStages;
-            if (round > 0 && !(ok = __all_sync(all, wait(empty(pos), (round - 1) & 1)))) break;
-            const bool raw = v == 1 && (job.blank || job.look);
-            bar = raw ? smem + L::kRawFull + 8 * st : full(pos);
-            dst = stage(pos);
-            waiting_raw = (waiting_raw & ~(1u << st)) | (raw ? 1u << st : 0u);
-            if (raw) raw_ph ^= 1u << st;
-            if (lane == 0) {
-              if (!raw) tc::arrive_n(bar, 3);  // the four warps that would otherwise have had to look
-              ptx::mbar_arrive_expect_tx(bar, L::kTile);
-            }
+          const uint32_t st = pos % L::kStages, round = pos / L::kStages;
+          if (round > 0 && !(ok = __all_sync(all, wait(empty(pos), (round - 1) & 1)))) break;
+          const bool raw = F8 || (v == 1 && (job.blank || job.look));
+          bar = raw ? smem + L::kRawFull + 8 * st : full(pos);
+          dst = stage(pos) + (F8 ? L::kRaw : 0);
+          waiting_raw = (waiting_raw & ~(1u << st)) | (raw ? 1u << st : 0u);
+          if (raw) raw_ph ^= 1u << st;
+          if (lane == 0) {
+            if (!raw) tc::arrive_n(bar, 3);  // the four warps that would otherwise have had to look
+            ptx::mbar_arrive_expect_tx(bar, F8 ? L::kRaw : L::kTile);
           }
           __syncwarp();
           if (lane < boxes) tc::tma4(dst + at, v ? &maps.v : &maps.k, half * 64, within, it.kvh, page, bar);
@@ -329,10 +327,9 @@ struct AttnTc {
       }
     }
     if (*abort_flag()) {  // nobody consumes what is still on its way, but it must have landed before the CTA ends
-      const uint32_t n = F8 ? L::kRawStages : L::kStages;
+      const uint32_t n = L::kStages;
       for (uint32_t p = pos > n ? pos - n : 0; p < pos; ++p) {
-        if constexpr (F8) wait_drain(smem + L::kRawFull + 8 * (p % n), (p / n) & 1);
-        else if ((waiting_raw >> (p % n)) & 1) wait_drain(smem + L::kRawFull + 8 * (p % n), ((raw_ph >> (p % n)) & 1) ^ 1);
+        if ((waiting_raw >> (p % n)) & 1) wait_drain(smem + L::kRawFull + 8 * (p % n), ((raw_ph >> (p % n)) & 1) ^ 1);
         else wait_drain(full(p), (p / n) & 1);
       }
     }
@@ -368,17 +365,20 @@ struct AttnTc {
     return bad;
   }
 
-  // A staged FP8 tile (row r at raw + r * DP) to fp16.  CARE: rows outside [from, to) become zeros, the others are looked
-  // through for NaN.
+  // The FP8 tile in the upper half of a stage (row r at + r * DP) to fp16 over the whole stage: all four warps have read
+  // their rows before any of them writes.  CARE: rows outside [from, to) become zeros, the others are looked through for NaN.
   template <bool CARE>
-  __device__ __forceinline__ bool widen(uint32_t raw, uint32_t tile_at, int tid, int from, int to) const {
+  __device__ __forceinline__ bool widen(uint32_t tile_at, int tid, uint32_t& work_ph, int from, int to, bool& bad) const {
     const int c = tid % kChunks, r0 = row_of(tid, 0);
-    const uint32_t src = raw + r0 * DP + c * 16;
+    const uint32_t src = tile_at + L::kRaw + r0 * DP + c * 16;
     const uint32_t dst = tile_at + (c >> 2) * kHalf + r0 * 128, turn = (((2 * c) ^ r0) & 7) << 4;
-    bool bad = false;
-    uint4 v[kChunks];  // every read ahead of the conversions that wait for it
+    uint4 v[kChunks];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) v[i] = ptx::lds128(src + i * kRowsAt * DP);
+    __syncwarp();
+    if ((tid & 31) == 0) tc::arrive(smem + L::kWork);
+    if (!__all_sync(0xffffffffu, wait(smem + L::kWork, work_ph))) return false;
+    work_ph ^= 1;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (CARE && (r0 + i * kRowsAt < from || r0 + i * kRowsAt >= to)) v[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -396,14 +396,14 @@ struct AttnTc {
       tc::sts128(at, h[0], h[1], h[2], h[3]);
       tc::sts128(at ^ 16, h[4], h[5], h[6], h[7]);
     }
-    return bad;
+    return true;
   }
 
   // Warps 8-11 behind TMA copies.
   __device__ __forceinline__ void run_workers(int tid) const {
     const uint32_t all = 0xffffffffu;
     const int lane = tid & 31;
-    uint32_t pos = 0, raw_ph = 0;
+    uint32_t pos = 0, raw_ph = 0, work_ph = 0;
     int count = 0;  // items with keys
     for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
       AttnItem it;
@@ -415,17 +415,16 @@ struct AttnTc {
         for (int n = 0; n < 2 * (it.j1 - it.j0); ++n, ++pos) {
           const int j = it.j0 + (n >> 1), k0 = j * kAttnTile;
           const VJob job = v_job(it, r0, r1, j);
-          const uint32_t st = pos % L::kRawStages;
-          if (!__all_sync(all, wait(smem + L::kRawFull + 8 * st, (pos / L::kRawStages) & 1))) return;
-          if (pos >= (uint32_t)L::kStages && !__all_sync(all, wait(empty(pos), ((pos / L::kStages) - 1) & 1))) return;
-          const uint32_t raw = smem + L::kRawRing + st * L::kRaw;
+          const uint32_t st = pos % L::kStages;
+          if (!__all_sync(all, wait(smem + L::kRawFull + 8 * st, (pos / L::kStages) & 1))) return;
+          bool bad = false;
           if ((n & 1) && (job.blank || job.look)) {
-            if (widen<true>(raw, stage(pos), tid, it.ulo - k0, it.uhi - k0) && job.look) poison()[count & 3] = count + 1;
-          } else {
-            widen<false>(raw, stage(pos), tid, 0, 0);
+            if (!widen<true>(stage(pos), tid, work_ph, it.ulo - k0, it.uhi - k0, bad)) return;
+            if (bad && job.look) poison()[count & 3] = count + 1;
+          } else if (!widen<false>(stage(pos), tid, work_ph, 0, 0, bad)) {
+            return;
           }
           signal(full(pos), lane);
-          if (lane == 0) tc::arrive(smem + L::kRawEmpty + 8 * st);
         }
       } else {
         for (int j = it.j0; j < it.j1; ++j) {
@@ -450,6 +449,7 @@ struct AttnTc {
   struct Loader {
     uint32_t pos = 0;    // tiles issued
     int pending = 0;     // issued, not handed over
+    uint32_t work_ph = 0;
     int look_item = -1;  // the newest pending tile is V and cut: look through it, name this item
   };
 
@@ -460,9 +460,8 @@ struct AttnTc {
     const bool look = ld.look_item >= 0 && ld.pending == 1;
     bool bad = false;
     if constexpr (F8) {
-      if (pos >= (uint32_t)L::kStages && !wait(empty(pos), ((pos / L::kStages) - 1) & 1)) return false;
-      const uint32_t raw = smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw;
-      bad = look ? widen<true>(raw, stage(pos), tid, 0, kAttnTile) : widen<false>(raw, stage(pos), tid, 0, 0);
+      if (!(look ? widen<true>(stage(pos), tid, ld.work_ph, 0, kAttnTile, bad) : widen<false>(stage(pos), tid, ld.work_ph, 0, 0, bad)))
+        return false;
     } else if (look) {
       bad = inspect(stage(pos), tid, 0, kAttnTile, false, true);
     }
@@ -489,16 +488,14 @@ struct AttnTc {
   // One K or V tile.  off: where this lane's row starts, elements; negative: a row of zeros.
   __device__ __forceinline__ bool load_tile(Loader& ld, int tid, const void* from, long long off) const {
     const uint32_t pos = ld.pos;
-    if constexpr (!F8) {
-      // wait, but never while sitting on tiles that somebody else waits for
-      if (pos >= (uint32_t)L::kStages && !__all_sync(0xffffffffu, tc::test(empty(pos), ((pos / L::kStages) - 1) & 1)) &&
-          !(flush(ld, tid) && wait(empty(pos), ((pos / L::kStages) - 1) & 1)))
-        return false;
-    }
+    // wait, but never while sitting on tiles that somebody else waits for
+    if (pos >= (uint32_t)L::kStages && !__all_sync(0xffffffffu, tc::test(empty(pos), ((pos / L::kStages) - 1) & 1)) &&
+        !(flush(ld, tid) && __all_sync(0xffffffffu, wait(empty(pos), ((pos / L::kStages) - 1) & 1))))
+      return false;
     const int c = tid % kChunks, src_lane = (tid & 31) / kChunks;
     const bool in_head = c * (F8 ? 16 : 8) < P.head_dim;
     const char* base = reinterpret_cast<const char*>(from);
-    const uint32_t dst = F8 ? smem + L::kRawRing + (pos % L::kRawStages) * L::kRaw + c * 16 : stage(pos) + (c >> 3) * kHalf;
+    const uint32_t dst = stage(pos) + (F8 ? L::kRaw + c * 16 : (c >> 3) * kHalf);
     constexpr int kBatch = 8 < kChunks ? 8 : kChunks;  // shuffles ahead of copies: one after the other they would wait in one queue
 #pragma unroll
     for (int i0 = 0; i0 < kChunks; i0 += kBatch) {
@@ -555,7 +552,8 @@ struct AttnTc {
   // ---- query tiles ----------------------------------------------------------------------------------
   static constexpr int kQThreads = 64;  // warps 14-15
 
-  // Query tile of `rows` rows from token tok0 into Q buffer `buf`; the rest of the last 32 rows in use is zeros.
+  // Query tile of `rows` rows from token tok0 into Q buffer `buf`; the rest of the last 32 rows in use is zeros.  QUAD: the
+  // same 32 rows four times.
   __device__ __forceinline__ void load_q(int tid, const AttnItem& it, int tok0, int rows, int buf, int scale_set) const {
     constexpr int kQChunks = DP / 8, kStep = kQThreads / kQChunks;
     const int c = tid % kQChunks, r0 = tid / kQChunks;
@@ -570,11 +568,13 @@ struct AttnTc {
     if constexpr (!F8) {  // asynchronous: every row is on its way before the first is waited for
       for (int r = r0; r < end; r += kStep) {
         const bool take = in_head && r < rows;
-        tc::cp16(dst + r * 128 + (((c ^ r) & 7) << 4), take ? row_at(r) : P.q, take);
+#pragma unroll
+        for (int k = 0; k < (QUAD ? 4 : 1); ++k)
+          tc::cp16(dst + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4), take ? row_at(r) : P.q, take);
       }
     } else {
-      constexpr int kBatch = 32 / kStep;
-      for (int i0 = r0; i0 < end; i0 += 32) {
+      constexpr int kBatch = 4;  // kStep * kBatch divides 32
+      for (int i0 = r0; i0 < end; i0 += kStep * kBatch) {
         uint4 v[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
@@ -600,7 +600,8 @@ struct AttnTc {
           uint32_t h[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) h[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
-          tc::sts128(dst + r * 128 + (((c ^ r) & 7) << 4), h[0], h[1], h[2], h[3]);
+#pragma unroll
+          for (int k = 0; k < (QUAD ? 4 : 1); ++k) tc::sts128(dst + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4), h[0], h[1], h[2], h[3]);
           if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
         }
       }
@@ -767,6 +768,20 @@ struct AttnTc {
                                                         bf_pack(x[e + 4], x[e + 5]), bf_pack(x[e + 6], x[e + 7]));
     }
   }
+  // N (2 or 4) columns of the result of a row
+  template <int N>
+  __device__ __forceinline__ void store_few(const float* x, long long row, int head, int split, int col) const {
+    if (col >= P.head_dim) return;  // head_dim is a multiple of 8, col of N
+    if (P.splits > 1) {
+      float* o = P.part_o + (((long long)split * P.T + row) * P.heads_q + head) * P.head_dim + col;
+#pragma unroll
+      for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(o + e) = make_float2(x[e], x[e + 1]);
+    } else {
+      uint16_t* o = P.out + row * P.ld_out + (long long)head * P.head_dim + col;
+#pragma unroll
+      for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(o + e) = bf_pack(x[e], x[e + 1]);
+    }
+  }
   __device__ __forceinline__ void store_z(float z, long long row, int head, int split) const {
     if (P.splits > 1) P.part_z[((long long)split * P.T + row) * P.heads_q + head] = z;
     else if (P.lse != nullptr) P.lse[row * P.heads_q + head] = z * kLn2;
@@ -798,21 +813,23 @@ struct AttnTc {
     }
   }
 
-  // One score tile: S -> P, running m and l of this lane's row.
+  // One score tile: S -> P, running m and l of this lane's row.  QUAD: the 32 columns of this warp's quarter.
   // Columns [from, to) of the tile are keys that the row sees.
   __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
                                        float& l) const {
-    float s[kAttnTile];
+    constexpr int N = QUAD ? kAttnTile / 4 : kAttnTile;
+    const int first_col = QUAD ? (int)((threadIdx.x >> 5) & 3) * N : 0;
+    float s[N];
 #pragma unroll
-    for (int k = 0; k < kAttnTile; k += 32) tc::ld32(s_addr + k, reinterpret_cast<uint32_t*>(s) + k);
+    for (int k = 0; k < N; k += 32) tc::ld32(s_addr + first_col + k, reinterpret_cast<uint32_t*>(s) + k);
     tc::wait_ld();
     if (masked) {
 #pragma unroll
-      for (int k = 0; k < kAttnTile; ++k) s[k] = k >= from && k < to ? s[k] : kNegInf;
+      for (int k = 0; k < N; ++k) s[k] = first_col + k >= from && first_col + k < to ? s[k] : kNegInf;
     }
     float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-    for (int k = 4; k < kAttnTile; k += 4) {
+    for (int k = 4; k < N; k += 4) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[k + e]);
     }
@@ -831,7 +848,7 @@ struct AttnTc {
     const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
+    for (int h = 0; h < N / 32; ++h) {
       uint32_t p[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -842,7 +859,14 @@ struct AttnTc {
         sum[e & 1] = __fadd2_rn(sum[e & 1], x);
         p[e] = F8 ? tc::pack_f16(x.x, x.y) : bf_pack(x.x, x.y);
       }
-      tc::st16(s_addr + h * 16, p);
+      tc::st16(s_addr + first_col / 2 + h * 16, p);
+    }
+    if (QUAD) {  // the other quarters' keys are not this warp's: zeros in their place
+      uint32_t none[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) none[e] = 0u;
+#pragma unroll
+      for (int h = 1; h < 4; ++h) tc::st16(s_addr + ((first_col / 2 + h * 16) & 63), none);
     }
     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
     tc::wait_st();
@@ -850,13 +874,14 @@ struct AttnTc {
   }
 
   __device__ __forceinline__ void run_softmax(uint32_t tmem, int w) const {
-    const int wtid = threadIdx.x & 127, lane = threadIdx.x & 31, first_row = wtid & ~31;
-    const uint32_t lanes = (uint32_t)first_row << 16;  // a warp reaches the 32 TMEM lanes of its place in the warpgroup
-    uint32_t sph = 0, oph = 0, mlph = 0, ml_any = 0;
+    const int lane = threadIdx.x & 31;
+    const int wtid = QUAD ? lane : threadIdx.x & 127, first_row = wtid & ~31;  // this thread's row, its warp's first
+    const uint32_t lanes = (threadIdx.x & 96) << 16;  // a warp reaches the 32 TMEM lanes of its place in the warpgroup
+    uint32_t sph = 0, oph = 0, mlph = 0, ml_any = 0, pass = 0;
     int count = 0;
     const uint32_t all = 0xffffffffu;
     // What the end of an item needs lies in shared memory during its tiles: registers are for the scores.
-    volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 8;
+    volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 7;
     for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
       float m = kNegInf, l = 0.f, c = P.c;
       {
@@ -931,7 +956,7 @@ struct AttnTc {
           if (lane == 0) tc::arrive(smem + L::kOFree + 8 * w);
         }
       } else if (tiles <= 0) {
-        if (w == 0 && valid) {
+        if (w == 0 && valid && (!QUAD || threadIdx.x < 32)) {
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = 0.f;
@@ -940,15 +965,23 @@ struct AttnTc {
           store_z(kNegInf, row, head, split);
         }
       } else {
-        // the two warpgroups' parts of the same rows
+        // the parts of the same rows: one per warpgroup, QUAD one per warp
         float2* ml = reinterpret_cast<float2*>(smem_ptr + L::kMlRows);
         const bool two = tiles > 1;
         if (ml_any && !__all_sync(all, wait(smem + L::kMlFree, mlph ^ 1))) return;
-        ml[w * 128 + wtid] = make_float2(m, l);
+        ml[threadIdx.x] = make_float2(m, l);
         __syncwarp();
         if (lane == 0) tc::arrive(smem + L::kMl);
         if (!__all_sync(all, wait(smem + L::kMl, mlph))) return;
-        const float2 p0 = ml[wtid], p1 = ml[128 + wtid];
+        constexpr int kParts = QUAD ? 8 : 2;
+        float f[kParts], lp[kParts], mm = kNegInf;
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+          const float2 v = ml[(QUAD ? 32 * p : 128 * p) + wtid];
+          f[p] = v.x;
+          lp[p] = v.y;
+          mm = fmaxf(mm, v.x);
+        }
         __syncwarp();
         if (lane == 0) tc::arrive(smem + L::kMlFree);
         mlph ^= 1;
@@ -961,34 +994,83 @@ struct AttnTc {
         }
         tc::fence_after();
         const bool again = poison()[count & 3] == count + 1;
-        if (busy && !again) {
-          if (F8) c = row_c(count & 3, wtid);
-          const float mm = fmaxf(p0.x, p1.x);
-          // a part without keys counts nothing; one that met only NaN scores makes the row NaN
-          const float f0 = p0.x == kNegInf ? (p0.y != 0.f ? 1.f : 0.f) : tc::ex2((p0.x - mm) * c);
-          const float f1 = p1.x == kNegInf ? (p1.y != 0.f ? 1.f : 0.f) : tc::ex2((p1.x - mm) * c);
-          const float lt = fmaf(f0, p0.y, f1 * p1.y);
-          const float inv = (P.splits > 1 ? 1.f : P.v_scale) / lt;
-          const uint32_t o0 = tmem + lanes + 2 * kAttnTile, o1 = o0 + DP;
+        if (F8) c = row_c(count & 3, wtid);
+        // a part without keys counts nothing; one that met only NaN scores makes the row NaN
+        float lt = 0.f;
 #pragma unroll
-          for (int kk = 0; kk < DP / 2; kk += 32) {
-            const int k = w * (DP / 2) + kk;
-            uint32_t a[32], b[32];
-            tc::ld32(o0 + k, a);
-            if (two) tc::ld32(o1 + k, b);
-            tc::wait_ld();
-            float x[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float v = f0 == 0.f ? 0.f : f0 * __uint_as_float(a[e]);
-              if (two && f1 != 0.f) v = fmaf(f1, __uint_as_float(b[e]), v);
-              x[e] = lt == 0.f ? 0.f : v * inv;
-            }
-            if (valid && !(P.splits > 1 && lt == 0.f)) store32(x, row, head, split, k);
-          }
-          if (valid && w == 0) store_z(lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt)), row, head, split);
+        for (int p = 0; p < kParts; ++p) {
+          f[p] = f[p] == kNegInf ? (lp[p] != 0.f ? 1.f : 0.f) : tc::ex2((f[p] - mm) * c);
+          lt = fmaf(f[p], lp[p], lt);
         }
-        if (again && busy && w == 0) redo(idx, 0, first_row);
+        const float z = lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt));
+        const float inv = lt == 0.f ? 0.f : (P.splits > 1 ? 1.f : P.v_scale) / lt;
+        const bool put = valid && !(P.splits > 1 && lt == 0.f);
+        const uint32_t o0 = tmem + lanes + 2 * kAttnTile, o1 = o0 + DP;
+        if constexpr (QUAD) {
+          // The item's Q tile is done with: its buffer takes the parts, kCols columns of all eight at a time.
+          constexpr int kCols = L::kTile / (8 * 32 * 4);
+          static_assert(kCols == 32 || kCols == 16, "");
+          const int part = threadIdx.x >> 5;
+          float* scratch = reinterpret_cast<float*>(smem_ptr + L::kQ0 + (count & 1) * L::kTile);
+          float mine = 0.f;  // f[part], without indexing registers
+#pragma unroll
+          for (int p = 0; p < kParts; ++p) mine = p == part ? f[p] : mine;
+          const bool has = part < 4 || two;  // the second warpgroup had tiles
+#pragma unroll 1
+          for (int k = 0; k < DP; k += kCols) {
+            uint32_t o[kCols];
+            if (has) {
+#pragma unroll
+              for (int q = 0; q < kCols; q += 16) tc::ld16((part < 4 ? o0 : o1) + k + q, o + q);
+              tc::wait_ld();
+            }
+#pragma unroll
+            for (int e = 0; e < kCols; ++e)
+              scratch[(part * kCols + e) * 32 + lane] = has && mine != 0.f ? mine * __uint_as_float(o[e]) : 0.f;
+            __syncwarp();
+            if (lane == 0) tc::arrive(smem + L::kPass);
+            if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
+            pass ^= 1;
+            constexpr int kMine = kCols / 8;  // columns this warp adds up, its lane's row
+            float x[kMine];
+#pragma unroll
+            for (int e = 0; e < kMine; ++e) {
+              x[e] = 0.f;
+#pragma unroll
+              for (int p = 0; p < 8; ++p) x[e] += scratch[(p * kCols + part * kMine + e) * 32 + lane];
+              x[e] *= inv;
+            }
+            if (put && !again) store_few<kMine>(x, row, head, split, k + part * kMine);
+            __syncwarp();
+            if (lane == 0) tc::arrive(smem + L::kPass);
+            if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
+            pass ^= 1;
+          }
+          if (lane == 0) tc::arrive(smem + L::kQEmpty + 8 * (count & 1));
+          if (valid && part == 0 && !again) store_z(z, row, head, split);
+          if (again && part == 0) redo(idx, 0, 0);
+        } else {
+          if (busy && !again) {
+#pragma unroll
+            for (int kk = 0; kk < DP / 2; kk += 32) {
+              const int k = w * (DP / 2) + kk;
+              uint32_t a[32], b[32];
+              tc::ld32(o0 + k, a);
+              if (two) tc::ld32(o1 + k, b);
+              tc::wait_ld();
+              float x[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                float v = f[0] == 0.f ? 0.f : f[0] * __uint_as_float(a[e]);
+                if (two && f[1] != 0.f) v = fmaf(f[1], __uint_as_float(b[e]), v);
+                x[e] = lt == 0.f ? 0.f : v * inv;
+              }
+              if (put) store32(x, row, head, split, k);
+            }
+            if (valid && w == 0) store_z(z, row, head, split);
+          }
+          if (again && busy && w == 0) redo(idx, 0, first_row);
+        }
         tc::fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -1001,11 +1083,11 @@ struct AttnTc {
   }
 };
 
-template <int DP, bool F8, bool ONE, bool TMA>
+template <int DP, bool F8, int FORM, bool TMA>
 __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams P,
                                                                     const __grid_constant__ AttnMaps maps) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  using K = AttnTc<DP, F8, ONE, TMA>;
+  using K = AttnTc<DP, F8, FORM, TMA>;
   using L = AttnSmem<DP, F8>;
   const uint32_t smem = ptx::smem_u32(smem_raw);
   const int warp = threadIdx.x >> 5;
@@ -1017,23 +1099,21 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     for (int i = 0; i < L::kStages; ++i) {
       ptx::mbar_init(smem + L::kFull + 8 * i, 4);
       ptx::mbar_init(smem + L::kEmpty + 8 * i, 1);
-      if (!F8) ptx::mbar_init(smem + L::kRawFull + 8 * i, 1);
-    }
-    for (int i = 0; i < L::kRawStages; ++i) {
       ptx::mbar_init(smem + L::kRawFull + 8 * i, 1);
-      ptx::mbar_init(smem + L::kRawEmpty + 8 * i, 4);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(smem + L::kQFull + 8 * i, 2);
-      ptx::mbar_init(smem + L::kQEmpty + 8 * i, 1);
+      ptx::mbar_init(smem + L::kQEmpty + 8 * i, K::QUAD ? 9 : 1);
       ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
       ptx::mbar_init(smem + L::kOFull + 8 * i, 1);
-      ptx::mbar_init(smem + L::kOFree + 8 * i, ONE ? 8 : 4);
+      ptx::mbar_init(smem + L::kOFree + 8 * i, K::ONE ? 8 : 4);
     }
     ptx::mbar_init(smem + L::kMl, 8);
     ptx::mbar_init(smem + L::kMlFree, 8);
     ptx::mbar_init(smem + L::kDrain, 1);
+    ptx::mbar_init(smem + L::kWork, 4);
+    ptx::mbar_init(smem + L::kPass, 8);
     *reinterpret_cast<volatile int*>(smem_raw + L::kAbort) = 0;
     for (int i = 0; i < 4; ++i) reinterpret_cast<volatile int*>(smem_raw + L::kPoison)[i] = 0;
     ptx::fence_barrier_init();

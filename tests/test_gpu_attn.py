@@ -74,7 +74,7 @@ class Batch:
                                    f"{ref['out'][r][bad][0]} (tolerance {tol[r][bad][0]:.3g})")
             empty = np.isneginf(ref["lse"][r])
             assert (np.isneginf(z[r]) == empty).all(), f"row {r}: lse {z[r]} for {ref['lse'][r]}"
-            assert (np.abs(z[r] - ref["lse"][r])[~empty] <= tol_lse[r][~empty]).all(), f"row {r}: lse {z[r]} for {ref['lse'][r]}"
+            assert (np.abs(z[r][~empty] - ref["lse"][r][~empty]) <= tol_lse[r][~empty]).all(), f"row {r}: lse {z[r]} for {ref['lse'][r]}"
         assert (out[n:] == 7.0).all() and (lse[n:] == 7.0).all()     # rows of no sequence: not written
 
     def check(self, variant=None, **kw):
@@ -107,6 +107,30 @@ def test_pages_and_lengths(libqknorm, page, dtype):
 ])
 def test_chunks(libqknorm, hq, hk, hd, new, kv, dtype):
     Batch(new, kv, hq, hk, hd, dtype=dtype, seed=len(new)).check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("page", [16, 7])
+@pytest.mark.parametrize("hq,hk,hd,new,kv", [
+    (4, 2, 128, [20, 3, 1], [300, 129, 1]), (8, 1, 64, [9, 16, 4], [500, 16, 130]), (1, 1, 96, [100], [400]), (64, 1, 128, [2], [700]),
+    (7, 1, 64, [18], [3000]), (3, 1, 128, [42, 11, 0], [2000, 11, 5]),
+])
+def test_short_chunks(libqknorm, hq, hk, hd, new, kv, page, dtype):
+    """33 to 128 rows per sequence and key head: one query tile, key tiles alternating between the warpgroups."""
+    assert 32 < max(new) * hq // hk <= 128
+    b = Batch(new, kv, hq, hk, hd, page=page, dtype=dtype, seed=hd)
+    b.check("attn_tc")
+    b.check("attn_tc", causal=False)
+    b.check("attn_tc", window=100)
+
+
+@BOTH
+@pytest.mark.parametrize("rows", [1, 5, 31, 32])
+def test_up_to_32_rows(libqknorm, rows, dtype):
+    """The four-quarter form at its edges: keys that end in each quarter of a tile."""
+    for kv in (31, 32, 33, 64, 65, 96, 97, 128, 129, 225):
+        Batch([rows], [max(kv, 1)], 2, 2, 64, dtype=dtype, seed=kv).check("attn_tc")
+    Batch([rows, 1, rows // 2], [300, 260, 40], 2, 2, 128, page=24, dtype=dtype).check("attn_tc", window=50)
 
 
 @BOTH
@@ -188,7 +212,7 @@ def test_unaligned_rows_take_the_general_kernel(libqknorm, dtype):
 
 @BOTH
 @pytest.mark.parametrize("new,kv,kw", [([40], [40], {}), ([3, 2], [200, 90], {}), ([150], [150], dict(window=20)), ([1], [300], dict(window=9)),
-                                       ([2, 2], [2500, 2500], {})])
+                                       ([2, 2], [2500, 2500], {}), ([20], [300], {}), ([25], [25], dict(window=3)), ([2, 2], [2500, 2500], dict(window=140))])
 def test_unseen_values_do_not_matter(libqknorm, new, kv, kw, dtype):
     """NaN and infinities in K and V at keys that the rows checked do not see -- later tokens of the chunk, keys that left the
     window -- inside the same tile."""
