@@ -14,13 +14,15 @@ A decode step of one layer::
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
+import struct
 from typing import Optional, Tuple
 
 import torch
 
 from . import binding
-from .binding import QKNormError, _check, _expect, _invoke, _ptr
+from .binding import QKNormError, _check, _invoke
 
 EXPORTS = (
     "qknorm_rope_frequencies",
@@ -54,6 +56,11 @@ class CPagedCache(ctypes.Structure):
                 ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
 
 
+# The same two structs as bytes, which is what the wrappers pass: a decode step is a few microseconds long, and filling a
+# ctypes structure takes two of them.
+_ROTATION, _CACHE = struct.Struct("PPiif4x"), struct.Struct("PPqqqqqqqiiiiff")
+assert _ROTATION.size == ctypes.sizeof(CRotation) and _CACHE.size == ctypes.sizeof(CPagedCache)
+
 _ready = False
 
 
@@ -66,10 +73,10 @@ def lib() -> ctypes.CDLL:
     i32, i64, f32, f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double
     L.qknorm_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f32)]
     for fn in (L.qknorm_rope, L.qknorm_rope_e4m3):
-        fn.argtypes = [_vp, _vp, ctypes.POINTER(CRotation), i64, i32, i32, i32, i64, i64, i32, _vp, _vp, i64, i64, _vp]
-    L.qknorm_fwd_append.argtypes = [_vp, _vp, _vp, _vp, _vp, i32, f32, ctypes.POINTER(CRotation), _vp,
-                                    ctypes.POINTER(CPagedCache), i64, i32, i64, i64, i64, _vp, i64, _vp]
-    L.qknorm_attn_paged.argtypes = [_vp, i64, ctypes.POINTER(CPagedCache), _vp, i32, i64, _vp, _vp, i32, i64, i32, i32, i32,
+        fn.argtypes = [_vp, _vp, _vp, i64, i32, i32, i32, i64, i64, i32, _vp, _vp, i64, i64, _vp]
+    L.qknorm_fwd_append.argtypes = [_vp, _vp, _vp, _vp, _vp, i32, f32, _vp, _vp,
+                                    _vp, i64, i32, i64, i64, i64, _vp, i64, _vp]
+    L.qknorm_attn_paged.argtypes = [_vp, i64, _vp, _vp, i32, i64, _vp, _vp, i32, i64, i32, i32, i32,
                                     f32, i32, i32, _vp, i64, _vp, _vp, i64, _vp]
     L.qknorm_attn_paged_workspace.argtypes = [i32, i64, i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
     for name in EXPORTS:
@@ -92,54 +99,76 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "plain
     return torch.tensor(list(host), dtype=torch.float64).to(device), float(mscale.value)
 
 
-def _here(*ts) -> None:
-    """Every tensor on the current device: the library launches there."""
-    cur = torch.cuda.current_device()
-    for t in ts:
-        if t is not None and t.device.index != cur:
-            raise QKNormError(-1, f"a tensor is on {t.device}, the current device is cuda:{cur}")
+def _refuse(status: int, message: str):
+    raise QKNormError(status, message)
 
 
-def _rows(t: torch.Tensor, T: int, what: str, dtype) -> int:
-    """A [T, d] CUDA view of `dtype` with unit column stride; its row stride in elements (0 = contiguous)."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not dtype or t.dim() != 2:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, f"{what}: expected a 2-D {dtype} CUDA tensor")
-    (n, d), (ld, unit) = t.shape, t.stride()
-    if n != T or (unit != 1 and d > 1) or (ld < d and T > 1):
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, f"{what}: expected {T} rows with unit column stride, got {tuple(t.shape)} "
-                                                    f"with strides {tuple(t.stride())}")
-    return ld if T > 1 else d
+_SHAPE = binding.QKNORM_ERR_SHAPE
 
 
-def _rotation(positions, inv_freq, T: int, interleaved: bool, mscale: float) -> Optional[CRotation]:
+def _device() -> int:
+    return torch._C._cuda_getDevice()
+
+
+def _flat(t, shape, dtype, what: str, dev: int) -> int:
+    """A contiguous tensor of that shape on the current device; its address."""
+    if not isinstance(t, torch.Tensor):
+        _refuse(binding.QKNORM_ERR_NULL if t is None else _SHAPE, f"{what}: expected a tensor, got {t!r}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(_SHAPE, f"{what}: expected contiguous {dtype} {tuple(shape)} on cuda:{dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _rows(t, T: int, what: str, dtype, dev: int, width: int = -1):
+    """A [T, d] view of `dtype` with unit column stride on the current device: (address, d, row stride in elements)."""
+    if not isinstance(t, torch.Tensor):
+        _refuse(binding.QKNORM_ERR_NULL if t is None else _SHAPE, f"{what}: expected a tensor, got {t!r}")
+    if t.dtype is dtype and t.dim() == 2 and t.get_device() == dev:
+        (n, d), (ld, unit) = t.shape, t.stride()
+        if T == 1:
+            ld = d
+        if n == T and (unit == 1 or d <= 1) and ld >= d and (width < 0 or d == width):
+            return t.data_ptr(), d, ld
+    _refuse(_SHAPE, f"{what}: expected {dtype} [{T}, {width if width >= 0 else 'd'}] with unit column stride on cuda:{dev}, got "
+                    f"{t.dtype} {tuple(t.shape)} with strides {tuple(t.stride())} on {t.device}")
+
+
+def _rotation(positions, inv_freq, T: int, interleaved: bool, mscale: float, dev: int) -> Optional[bytes]:
     if positions is None and inv_freq is None:
         return None
-    _expect(positions, (T,), torch.int64, "positions")
-    if inv_freq is None or inv_freq.dim() != 1:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "inv_freq: expected a 1-D float64 CUDA tensor")
-    _expect(inv_freq, (inv_freq.shape[0],), torch.float64, "inv_freq")
-    return CRotation(_ptr(positions), _ptr(inv_freq), 2 * inv_freq.shape[0], 1 if interleaved else 0, float(mscale))
+    if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+        _refuse(_SHAPE, "inv_freq: expected a 1-D float64 CUDA tensor")
+    n = inv_freq.shape[0]
+    return _ROTATION.pack(_flat(positions, (T,), torch.int64, "positions", dev), _flat(inv_freq, (n,), torch.float64, "inv_freq", dev),
+                          2 * n, 1 if interleaved else 0, mscale)
 
 
-def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: float, v_scale: float) -> CPagedCache:
-    """k_cache, v_cache [num_pages, page_size, heads, head_dim], any strides over pages, tokens and heads."""
+def _cache(k_cache, v_cache, k_scale: float, v_scale: float, dev: int):
+    """k_cache, v_cache [num_pages, page_size, heads, head_dim], any strides over pages, tokens and heads: (struct, heads,
+    head_dim)."""
     for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if (not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 4 or t.dtype not in (_BF16, _F8)
+        if (not isinstance(t, torch.Tensor) or t.dim() != 4 or t.get_device() != dev or t.dtype not in (_BF16, _F8)
                 or (t.shape[3] > 1 and t.stride(3) != 1)):
-            raise QKNormError(binding.QKNORM_ERR_SHAPE, f"{what}: expected a 4-D bfloat16 or float8_e4m3fn CUDA tensor "
-                                                        f"[pages, page_size, heads, head_dim] with unit stride in head_dim")
-    if k_cache.shape != v_cache.shape or k_cache.dtype is not v_cache.dtype:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "k_cache and v_cache differ in shape or type")
-    pages, page, heads, hd = k_cache.shape
+            _refuse(_SHAPE, f"{what}: expected a 4-D bfloat16 or float8_e4m3fn tensor [pages, page_size, heads, head_dim] on cuda:{dev} "
+                            f"with unit stride in head_dim")
+    shape = k_cache.shape
+    if shape != v_cache.shape or k_cache.dtype is not v_cache.dtype:
+        _refuse(_SHAPE, "k_cache and v_cache differ in shape or type")
+    pages, page, heads, hd = shape
     ks, vs = k_cache.stride(), v_cache.stride()
-    return CPagedCache(_ptr(k_cache), _ptr(v_cache), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages, page, heads, hd,
-                       1 if k_cache.dtype is _F8 else 0, float(k_scale), float(v_scale))
+    return _CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages, page, heads, hd,
+                       1 if k_cache.dtype is _F8 else 0, k_scale, v_scale), heads, hd
+
+
+def _current(stream):
+    """What `_invoke` takes: the current stream as a handle if none is given."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream
 
 
 def _empty(shape, dtype, device, stream) -> torch.Tensor:
     """A new tensor that belongs to the stream the call is made on."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+    if stream is None:  # strides given: a third less time than torch.empty
+        return torch.empty_strided(shape, (shape[1], 1) if len(shape) == 2 else (1,), dtype=dtype, device=device)
     s = torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream
     with torch.cuda.stream(s):
         return torch.empty(shape, dtype=dtype, device=device)
@@ -155,31 +184,26 @@ def qknorm_rope(q, k, positions, inv_freq, head_dim: int, out_q=None, out_k=None
     L = lib()
     ref = q if q is not None else k
     if ref is None:
-        raise QKNormError(binding.QKNORM_ERR_NULL, "q and k are both None")
-    if ref.dim() != 2:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "q and k are 2-D: [tokens, heads * head_dim]")
-    T, act = ref.shape[0], _F8 if ref.dtype is _F8 else _BF16
-    _here(q, k, positions, inv_freq, out_q, out_k)
-    rot = _rotation(positions, inv_freq, T, interleaved, mscale)
+        _refuse(binding.QKNORM_ERR_NULL, "q and k are both None")
+    if not isinstance(ref, torch.Tensor) or ref.dim() != 2:
+        _refuse(_SHAPE, "q and k are 2-D tensors: [tokens, heads * head_dim]")
+    T, act, dev = ref.shape[0], _F8 if ref.dtype is _F8 else _BF16, _device()
+    rot = _rotation(positions, inv_freq, T, interleaved, mscale, dev)
     if rot is None:
-        raise QKNormError(binding.QKNORM_ERR_NULL, "positions and inv_freq are None")
+        _refuse(binding.QKNORM_ERR_NULL, "positions and inv_freq are None")
+    pq = pk = poq = pok = None
     dq = dk = ldq = ldk = ldoq = ldok = 0
     if q is not None:
-        dq, ldq = q.shape[1], _rows(q, T, "q", act)
+        pq, dq, ldq = _rows(q, T, "q", act, dev)
         out_q = _empty((T, dq), act, q.device, stream) if out_q is None else out_q
-        ldoq = _rows(out_q, T, "out_q", act)
-        if out_q.shape[1] != dq:
-            raise QKNormError(binding.QKNORM_ERR_SHAPE, "out_q: another width than q")
+        poq, _, ldoq = _rows(out_q, T, "out_q", act, dev, dq)
     if k is not None:
-        dk, ldk = k.shape[1], _rows(k, T, "k", act)
+        pk, dk, ldk = _rows(k, T, "k", act, dev)
         out_k = _empty((T, dk), act, k.device, stream) if out_k is None else out_k
-        ldok = _rows(out_k, T, "out_k", act)
-        if out_k.shape[1] != dk:
-            raise QKNormError(binding.QKNORM_ERR_SHAPE, "out_k: another width than k")
-    fn = L.qknorm_rope_e4m3 if act is _F8 else L.qknorm_rope
-    _invoke(fn, [_ptr(q), _ptr(k), ctypes.byref(rot), T, dq, dk, int(head_dim), ldq, ldk, 1 if inverse else 0,
-                 _ptr(out_q) if q is not None else None, _ptr(out_k) if k is not None else None, ldoq, ldok], stream,
-            (q, k, positions, inv_freq, out_q, out_k, rot))
+        pok, _, ldok = _rows(out_k, T, "out_k", act, dev, dk)
+    _invoke(L.qknorm_rope_e4m3 if act is _F8 else L.qknorm_rope,
+            (pq, pk, rot, T, dq, dk, int(head_dim), ldq, ldk, 1 if inverse else 0, poq, pok, ldoq, ldok), _current(stream),
+            (q, k, positions, inv_freq, out_q, out_k))
     return out_q, out_k
 
 
@@ -192,44 +216,43 @@ def qknorm_fwd_append(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_c
     [pages, page_size, heads, head_dim] bf16 or float8_e4m3fn (holding x / scale), written in place.
     out_q defaults to a new tensor and may be q.  Returns out_q."""
     L = lib()
-    cache = _cache(k_cache, v_cache, k_scale, v_scale)
+    dev = _device()
+    cache, heads, hd = _cache(k_cache, v_cache, k_scale, v_scale, dev)
     if not isinstance(k, torch.Tensor) or k.dim() != 2:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "k: expected a 2-D bfloat16 CUDA tensor")
-    T, dk = k.shape[0], cache.heads * cache.head_dim
-    _here(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, out_q)
-    ldk, ldv = _rows(k, T, "k", _BF16), _rows(v, T, "v", _BF16)
-    if k.shape[1] != dk or v.shape[1] != dk:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, f"k and v: the cache holds {dk} values per token")
-    _expect(slots, (T,), torch.int64, "slots")
+        _refuse(_SHAPE, "k: expected a 2-D bfloat16 CUDA tensor")
+    T, dk = k.shape[0], heads * hd
+    pk, _, ldk = _rows(k, T, "k", _BF16, dev, dk)
+    pv, _, ldv = _rows(v, T, "v", _BF16, dev, dk)
+    pslots = _flat(slots, (T,), torch.int64, "slots", dev)
     norm = NORM_HEADWISE if headwise else NORM_LAYERWISE
+    pgq = pgk = pq = po = None
     if gamma_q is None and gamma_k is None:
         norm = NORM_NONE
     else:
-        _expect(gamma_k, (dk,), _BF16, "gamma_k")
+        pgk = _flat(gamma_k, (dk,), _BF16, "gamma_k", dev)
     dq = ldq = ldo = 0
     if q is not None:
-        ldq = _rows(q, T, "q", _BF16)
-        dq = q.shape[1]
+        pq, dq, ldq = _rows(q, T, "q", _BF16, dev)
         if norm != NORM_NONE:
-            _expect(gamma_q, (dq,), _BF16, "gamma_q")
+            pgq = _flat(gamma_q, (dq,), _BF16, "gamma_q", dev)
         out_q = _empty((T, dq), _BF16, q.device, stream) if out_q is None else out_q
-        ldo = _rows(out_q, T, "out_q", _BF16)
-        if out_q.shape[1] != dq:
-            raise QKNormError(binding.QKNORM_ERR_SHAPE, "out_q: another width than q")
-    rot = _rotation(positions, inv_freq, T, interleaved, mscale)
-    _invoke(L.qknorm_fwd_append,
-            [_ptr(q), _ptr(k), _ptr(v), _ptr(gamma_q), _ptr(gamma_k), norm, float(eps),
-             ctypes.byref(rot) if rot is not None else None, _ptr(slots), ctypes.byref(cache), T, dq, ldq, ldk, ldv,
-             _ptr(out_q) if q is not None else None, ldo], stream,
-            (q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, out_q, rot, cache))
+        po, _, ldo = _rows(out_q, T, "out_q", _BF16, dev, dq)
+    rot = _rotation(positions, inv_freq, T, interleaved, mscale, dev)
+    _invoke(L.qknorm_fwd_append, (pq, pk, pv, pgq, pgk, norm, eps, rot, pslots, cache, T, dq, ldq, ldk, ldv, po, ldo), _current(stream),
+            (q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, out_q))
     return out_q
 
 
 def attn_paged_workspace(num_seqs: int, tokens: int, max_q: int, max_kv: int, heads_q: int, heads_kv: int, head_dim: int,
                          window: int = 0) -> int:
     """qknorm_attn_paged_workspace: bytes a call of these sizes needs on the current device."""
+    return _workspace(torch.cuda.current_device(), num_seqs, tokens, max_q, max_kv, heads_q, heads_kv, head_dim, window)
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace(device: int, *sizes: int) -> int:
     out = ctypes.c_int64(0)
-    _check(lib().qknorm_attn_paged_workspace(num_seqs, tokens, max_q, max_kv, heads_q, heads_kv, head_dim, window, ctypes.byref(out)))
+    _check(lib().qknorm_attn_paged_workspace(*sizes, ctypes.byref(out)))
     return out.value
 
 
@@ -242,45 +265,35 @@ def qknorm_attn_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q
     out defaults to a new tensor whose rows outside every sequence are not written; lse: fp32 [T, heads_q] to fill;
     workspace: uint8 tensor of attn_paged_workspace(...) bytes, by default a new one per call.  Returns out."""
     L = lib()
-    cache = _cache(k_cache, v_cache, k_scale, v_scale)
+    dev = _device()
+    cache, heads, hd = _cache(k_cache, v_cache, k_scale, v_scale, dev)
     if not isinstance(q, torch.Tensor) or q.dim() != 2:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "q: expected a 2-D bfloat16 CUDA tensor")
-    T, dq = q.shape
-    _here(q, k_cache, v_cache, block_table, kv_lens, q_starts, out, lse, workspace)
-    ldq = _rows(q, T, "q", _BF16)
-    hd = cache.head_dim
+        _refuse(_SHAPE, "q: expected a 2-D bfloat16 CUDA tensor")
+    T = q.shape[0]
+    pq, dq, ldq = _rows(q, T, "q", _BF16, dev)
     if dq == 0 or dq % hd != 0:
-        raise QKNormError(binding.QKNORM_ERR_HEADS, f"q: {dq} columns are no whole number of heads of {hd}")
-    hq = dq // hd
+        _refuse(binding.QKNORM_ERR_HEADS, f"q: {dq} columns are no whole number of heads of {hd}")
+    hq, max_q, max_kv, window = dq // hd, int(max_q), int(max_kv), int(window)
     if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "kv_lens: expected a 1-D int32 CUDA tensor")
+        _refuse(_SHAPE, "kv_lens: expected a 1-D int32 CUDA tensor")
     B = kv_lens.shape[0]
-    _expect(kv_lens, (B,), torch.int32, "kv_lens")
-    _expect(q_starts, (B + 1,), torch.int32, "q_starts")
-    if (not isinstance(block_table, torch.Tensor) or not block_table.is_cuda or block_table.dtype is not torch.int32
-            or block_table.dim() != 2 or block_table.shape[0] != B or (block_table.shape[1] > 1 and block_table.stride(1) != 1)):
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, f"block_table: expected an int32 CUDA tensor [{B}, pages per sequence]")
-    cols = block_table.shape[1]
-    ldt = block_table.stride(0) if B > 1 else 0
-    if out is None:
-        out = _empty((T, dq), _BF16, q.device, stream)
-    elif out.shape != q.shape:
-        raise QKNormError(binding.QKNORM_ERR_SHAPE, "out: another shape than q")
-    ldo = _rows(out, T, "out", _BF16)
-    if lse is not None:
-        _expect(lse, (T, hq), torch.float32, "lse")
+    plens = _flat(kv_lens, (B,), torch.int32, "kv_lens", dev)
+    pstarts = _flat(q_starts, (B + 1,), torch.int32, "q_starts", dev)
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        _refuse(_SHAPE, f"block_table: expected an int32 CUDA tensor [{B}, pages per sequence]")
+    ptable, cols, ldt = _rows(block_table, B, "block_table", torch.int32, dev)
+    out = _empty((T, dq), _BF16, q.device, stream) if out is None else out
+    po, _, ldo = _rows(out, T, "out", _BF16, dev, dq)
+    plse = None if lse is None else _flat(lse, (T, hq), torch.float32, "lse", dev)
     if workspace is None:
-        need = ctypes.c_int64(0)
-        _check(L.qknorm_attn_paged_workspace(B, T, int(max_q), int(max_kv), hq, cache.heads, hd, int(window), ctypes.byref(need)))
-        nbytes = need.value
+        nbytes = _workspace(dev, B, T, max_q, max_kv, hq, heads, hd, window)
         workspace = _empty((nbytes,), torch.uint8, q.device, stream) if nbytes else None
     else:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise QKNormError(binding.QKNORM_ERR_SCRATCH, "workspace must be a contiguous CUDA tensor")
+        if not workspace.is_contiguous() or workspace.get_device() != dev:
+            _refuse(binding.QKNORM_ERR_SCRATCH, f"workspace: expected a contiguous tensor on cuda:{dev}")
         nbytes = workspace.numel() * workspace.element_size()
     _invoke(L.qknorm_attn_paged,
-            [_ptr(q), ldq, ctypes.byref(cache), _ptr(block_table), cols, ldt, _ptr(kv_lens), _ptr(q_starts), B, T, int(max_q),
-             int(max_kv), hq, 1.0 / math.sqrt(hd) if scale is None else float(scale), 1 if causal else 0, int(window),
-             _ptr(out), ldo, _ptr(lse), _ptr(workspace), nbytes], stream,
-            (q, k_cache, v_cache, block_table, kv_lens, q_starts, out, lse, workspace, cache))
+            (pq, ldq, cache, ptable, cols, ldt, plens, pstarts, B, T, max_q, max_kv, hq, 1.0 / math.sqrt(hd) if scale is None else scale,
+             1 if causal else 0, window, po, ldo, plse, workspace.data_ptr() if workspace is not None else None, nbytes),
+            _current(stream), (q, k_cache, v_cache, block_table, kv_lens, q_starts, out, lse, workspace))
     return out
