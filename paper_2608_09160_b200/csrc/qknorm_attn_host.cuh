@@ -64,6 +64,12 @@ struct CallRegions {  // buffers of a call: outputs, and everything an output mu
   int own[8];
 };
 
+int log2_or_minus_one(int v) {
+  for (int s = 0; s < 31; ++s)
+    if (v == (1 << s)) return s;
+  return -1;
+}
+
 Region flat(const void* p, uintptr_t bytes) { return Region{(uintptr_t)p, 1, bytes, bytes}; }
 
 // Outputs against every input and every other output; an output may be exactly its own input.
@@ -154,19 +160,18 @@ int launch_rope(RopeParams& R, int elem_bytes, int cache_bytes, int norm, bool v
     while ((16 << R.log_lph) < R.head_dim) ++R.log_lph;
     const int heads = R.q.heads + R.k.heads + (cache_bytes ? R.v.heads : 0);
     R.slots_per_token = heads << R.log_lph;
-    // Two units (64 bytes of bf16) per thread keep enough loads in flight without long CTAs; few tokens: one, for latency.
-    int upt = R.T < 2 * dev->sm_count ? 1 : 2;
-    const int forced = env_int("QKNORM_ROPE_UPT", 0);
-    if (forced) upt = forced;
-    if (R.slots_per_token > 1024 * upt) upt = R.slots_per_token > 2048 ? 4 : 2;
+    // Few tokens: one unit per thread, for latency.  Many: four, which spread a thread's start (which head, which rows) and the
+    // token's barrier over more elements -- 16384 tokens of 5120 + 1024 + 1024 take 154 us with one, 103 with two, 92 with four.
+    int upt = R.T < 2 * dev->sm_count ? 1 : 4;
+    if (R.slots_per_token > 1024) upt = 4;
     if (R.slots_per_token <= 4096) {
       R.threads_per_token = round_up((R.slots_per_token + upt - 1) / upt, 32);
       // short rows: several tokens share a CTA of about 128 threads
       R.tokens_per_cta = R.T >= 2 * dev->sm_count && R.threads_per_token < 128 ? 128 / R.threads_per_token : 1;
       const int smem = R.tokens_per_cta * R.rot_dim * (int)sizeof(float2) / 2;
-      RopeKernel fn = rope_kernel_for(elem_bytes, cache_bytes, norm, upt);
+      RopeKernel fn = rope_kernel_for(elem_bytes, cache_bytes, norm, upt, R.tokens_per_cta * R.threads_per_token);
       const long long grid = (R.T + R.tokens_per_cta - 1) / R.tokens_per_cta;
-      if (fn && grid <= 0x7fffffff) {
+      if (grid <= 0x7fffffff) {
         const cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)(R.tokens_per_cta * R.threads_per_token), (size_t)smem, stream, R);
         if (e != cudaSuccess) return set_cuda_error(e);
         return finish_launch(cache_bytes ? "append" : "rope");
@@ -283,6 +288,7 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
   R.slots = (const long long*)slots;
   R.num_slots = (long long)cache->num_pages * cache->page_size;
   R.page_size = cache->page_size;
+  R.page_shift = log2_or_minus_one(cache->page_size);
   const uintptr_t rows = (uintptr_t)T, qb = (uintptr_t)dq * 2, kb = (uintptr_t)dk * 2;
   CallRegions c;
   if (dq > 0) {
@@ -512,9 +518,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.v = AttnSide{cache->v, cache->v_page, cache->v_token, cache->v_head};
   P.num_pages = cache->num_pages;
   P.page_size = cache->page_size;
-  P.page_shift = -1;
-  for (int s = 0; s < 31; ++s)
-    if (cache->page_size == (1 << s)) P.page_shift = s;
+  P.page_shift = log2_or_minus_one(cache->page_size);
   P.table = table;
   P.ld_table = ld_table ? ld_table : table_cols;
   P.kv_lens = kv_lens;

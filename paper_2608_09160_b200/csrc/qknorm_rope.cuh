@@ -42,7 +42,7 @@ struct RopeParams {
   CacheSide ck, cv;
   const long long* slots;
   long long num_slots;  // num_pages * page_size
-  int page_size;
+  int page_size, page_shift;  // page_shift: log2(page_size), or -1
   const long long* positions;
   const double* inv_freq;
   float mscale;
@@ -68,65 +68,80 @@ __device__ __forceinline__ float2 rope_cs(const RopeParams& R, long long pos, in
   return make_float2(c * R.mscale, s * R.mscale);
 }
 
-// 8 elements in fp32 <-> storage
+// 8 elements as stored, and as four pairs in fp32 (pairs, because sm_100 multiplies and adds them two at a time)
 template <class IO>
 struct Chunk8;
 template <>
 struct Chunk8<IoBf16> {
   uint4 w;
-  __device__ __forceinline__ void load(const void* base, long long i) {
+  __device__ __forceinline__ void load(const void* base, int i) {
     w = ld_stream(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(base) + i));
   }
-  __device__ __forceinline__ void unpack(float* f) const {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      f[2 * e] = bf_lo(u[e]);
-      f[2 * e + 1] = bf_hi(u[e]);
-    }
+  __device__ __forceinline__ void store(void* base, long long i) const {
+    st_stream(reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + i), w);
   }
-  static __device__ __forceinline__ void store(void* base, long long i, const float* f) {
-    const uint4 o = make_uint4(bf_pack(f[0], f[1]), bf_pack(f[2], f[3]), bf_pack(f[4], f[5]), bf_pack(f[6], f[7]));
-    st_stream(reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(base) + i), o);
+  __device__ __forceinline__ void unpack(float2* f) const {
+    f[0] = bf_unpack2(w.x);
+    f[1] = bf_unpack2(w.y);
+    f[2] = bf_unpack2(w.z);
+    f[3] = bf_unpack2(w.w);
+  }
+  __device__ __forceinline__ void pack(const float2* f) {
+    w = make_uint4(bf_pack(f[0].x, f[0].y), bf_pack(f[1].x, f[1].y), bf_pack(f[2].x, f[2].y), bf_pack(f[3].x, f[3].y));
+  }
+  // (x * gamma) * r; the product is exact
+  __device__ __forceinline__ void scaled(const uint4& g, float2 r, float2* f) const {
+    f[0] = __fmul2_rn(mul_bf16x2(w.x, g.x), r);
+    f[1] = __fmul2_rn(mul_bf16x2(w.y, g.y), r);
+    f[2] = __fmul2_rn(mul_bf16x2(w.z, g.z), r);
+    f[3] = __fmul2_rn(mul_bf16x2(w.w, g.w), r);
+  }
+  __device__ __forceinline__ void sumsq(float& a, float& b) const {
+    IoBf16::sumsq_word(w.x, a, b);
+    IoBf16::sumsq_word(w.y, a, b);
+    IoBf16::sumsq_word(w.z, a, b);
+    IoBf16::sumsq_word(w.w, a, b);
   }
 };
 template <>
 struct Chunk8<IoE4m3> {
   uint2 w;
-  __device__ __forceinline__ void load(const void* base, long long i) {
+  __device__ __forceinline__ void load(const void* base, int i) {
     w = __ldcs(reinterpret_cast<const uint2*>(reinterpret_cast<const uint8_t*>(base) + i));
   }
-  __device__ __forceinline__ void unpack(float* f) const {
+  __device__ __forceinline__ void store(void* base, long long i) const {
+    __stcs(reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(base) + i), w);
+  }
+  __device__ __forceinline__ void unpack(float2* f) const {
     const uint32_t u[2] = {w.x, w.y};
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       uint32_t f01, f23;
       e4m3x4_to_f16x2(u[e], f01, f23);
-      const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&f01));
-      const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&f23));
-      f[4 * e] = a.x;
-      f[4 * e + 1] = a.y;
-      f[4 * e + 2] = b.x;
-      f[4 * e + 3] = b.y;
+      f[2 * e] = __half22float2(*reinterpret_cast<const __half2*>(&f01));
+      f[2 * e + 1] = __half22float2(*reinterpret_cast<const __half2*>(&f23));
     }
   }
-  static __device__ __forceinline__ void store(void* base, long long i, const float* f) {
-    const uint2 o = make_uint2(e4m3_pack2(f[0], f[1]) | (e4m3_pack2(f[2], f[3]) << 16),
-                               e4m3_pack2(f[4], f[5]) | (e4m3_pack2(f[6], f[7]) << 16));
-    __stcs(reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(base) + i), o);
+  __device__ __forceinline__ void pack(const float2* f) {
+    w = make_uint2(e4m3_pack2(f[0].x, f[0].y) | (e4m3_pack2(f[1].x, f[1].y) << 16),
+                   e4m3_pack2(f[2].x, f[2].y) | (e4m3_pack2(f[3].x, f[3].y) << 16));
   }
 };
 
-// Where element 0 of (token slot, head) of a cache side starts; slot is in range.
-__device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot, int page_size, int head) {
-  const long long page = slot / page_size;
-  return page * c.page + (slot - page * page_size) * c.token + (long long)head * c.head;
+// Where token slot `slot` (in range) starts in a cache side.
+__device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot, int page_size, int page_shift) {
+  long long page;
+  if (page_shift >= 0) page = slot >> page_shift;
+  else if (slot <= 0xffffffffll) page = (unsigned)slot / (unsigned)page_size;
+  else page = slot / page_size;
+  return page * c.page + (slot - page * page_size) * c.token;
 }
 
-// IO: storage of q, k, v and out_q.  CIO: storage of the cache.  UPT: 16-element units per thread.
-template <class IO, class CIO, int NORM, bool CACHE, int UPT>
-__global__ void __launch_bounds__(1024) rope_kernel(const __grid_constant__ RopeParams R) {
-  extern __shared__ float4 cs_all[];  // [tokens_per_cta][4][rot_dim/16]: (c, s) of pairs 8j+2e, 8j+2e+1 at [e][j]
+// IO: storage of q, k, v and out_q.  CIO: storage of the cache.  UPT: 16-element units per thread.  MAXT: the largest CTA;
+// CTAs of up to 256 threads get 80 registers a thread, which four units need.
+template <class IO, class CIO, int NORM, bool CACHE, int UPT, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const __grid_constant__ RopeParams R) {
+  extern __shared__ float4 cs_all[];  // [tokens_per_cta][4][rot_dim/16]: (c, c, s, s) of pairs 8j+2e, 8j+2e+1 at [e][j]
   __shared__ float red[32][2];        // per warp: sum of squares of Q, of K
   const int slot_of_token = threadIdx.x / R.threads_per_token;
   const int tid = threadIdx.x - slot_of_token * R.threads_per_token;
@@ -137,14 +152,19 @@ __global__ void __launch_bounds__(1024) rope_kernel(const __grid_constant__ Rope
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
   Chunk8<IO> u[UPT][2];
-  int j[UPT], c0[UPT], c1[UPT], head[UPT], side[UPT];  // side: 0 q, 1 k, 2 v, -1 none
+  int off[UPT];   // of the unit's first chunk in its row
+  int side[UPT];  // 0 q, 1 k, 2 v, -1 none
+  const int j = tid & ((1 << R.log_lph) - 1);  // which 16 elements of its head; threads_per_token is a multiple of 32, so the
+                                               // same in every unit of the thread
+  const bool turns = j < r16;
+  const int c0 = turns && !R.interleaved ? 8 * j : 16 * j;
+  const int step = turns && !R.interleaved ? 8 * r16 : 8;  // from the first chunk to the second
 #pragma unroll
   for (int i = 0; i < UPT; ++i) {
     const int s = tid + i * R.threads_per_token;
     int h = s >> R.log_lph;
-    j[i] = s & ((1 << R.log_lph) - 1);
     side[i] = -1;
-    if (live && s < R.slots_per_token && j[i] * 16 < R.head_dim) {
+    if (live && s < R.slots_per_token && j * 16 < R.head_dim) {
       side[i] = 0;
       if (h >= R.q.heads) {
         h -= R.q.heads;
@@ -155,43 +175,40 @@ __global__ void __launch_bounds__(1024) rope_kernel(const __grid_constant__ Rope
         }
       }
     }
-    head[i] = h;
-    const bool half = !R.interleaved && j[i] < r16;
-    c0[i] = half ? 8 * j[i] : 16 * j[i];
-    c1[i] = half ? 8 * (j[i] + r16) : 16 * j[i] + 8;
+    off[i] = h * R.head_dim + c0;
     if (side[i] >= 0) {
       const RopeSide& A = side[i] == 0 ? R.q : (!CACHE || side[i] == 1) ? R.k : R.v;
-      const long long row = t * A.ldx + (long long)h * R.head_dim;
-      u[i][0].load(A.x, row + c0[i]);
-      u[i][1].load(A.x, row + c1[i]);
+      const char* row = reinterpret_cast<const char*>(A.x) + t * A.ldx * IO::kBytes;
+      u[i][0].load(row, off[i]);
+      u[i][1].load(row, off[i] + step);
     }
   }
   if (live && r16 > 0) {
     const long long pos = R.positions[t];
-    for (int p = tid; p < 8 * r16; p += R.threads_per_token)
-      reinterpret_cast<float2*>(cs)[(((p & 7) >> 1) * r16 + (p >> 3)) * 2 + (p & 1)] = rope_cs(R, pos, p);
+    for (int p = tid; p < 8 * r16; p += R.threads_per_token) {
+      const float2 f = rope_cs(R, pos, p);
+      float* at = reinterpret_cast<float*>(cs + ((p & 7) >> 1) * r16 + (p >> 3)) + (p & 1);
+      at[0] = f.x;
+      at[2] = f.y;
+    }
   }
   float rq = 1.f, rk = 1.f;
-  if (NORM == kNormLayer) {
+  if constexpr (NORM == kNormLayer) {
     float sq = 0.f, sk = 0.f;
 #pragma unroll
     for (int i = 0; i < UPT; ++i) {
       if (side[i] == 0 || side[i] == 1) {
-        float f[8], a = 0.f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          u[i][h].unpack(f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) a = fmaf(f[e], f[e], a);
-        }
-        if (side[i] == 0) sq += a;
-        else sk += a;
+        float a = 0.f, b = 0.f;
+        u[i][0].sumsq(a, b);
+        u[i][1].sumsq(a, b);
+        if (side[i] == 0) sq += a + b;
+        else sk += a + b;
       }
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      sq += __shfl_xor_sync(0xffffffffu, sq, off);
-      sk += __shfl_xor_sync(0xffffffffu, sk, off);
+    for (int o = 16; o > 0; o >>= 1) {
+      sq += __shfl_xor_sync(0xffffffffu, sq, o);
+      sk += __shfl_xor_sync(0xffffffffu, sk, o);
     }
     if ((threadIdx.x & 31) == 0) {
       red[threadIdx.x >> 5][0] = sq;
@@ -199,7 +216,7 @@ __global__ void __launch_bounds__(1024) rope_kernel(const __grid_constant__ Rope
     }
   }
   __syncthreads();
-  if (NORM == kNormLayer) {
+  if constexpr (NORM == kNormLayer) {
     const int wpt = R.threads_per_token >> 5, w0 = slot_of_token * wpt;
     float sq = 0.f, sk = 0.f;
     for (int w = 0; w < wpt; ++w) {  // fixed order
@@ -216,74 +233,86 @@ __global__ void __launch_bounds__(1024) rope_kernel(const __grid_constant__ Rope
   }
 #pragma unroll
   for (int i = 0; i < UPT; ++i) {
-    float a[8], b[8];
-    if (side[i] >= 0) {
-      u[i][0].unpack(a);
-      u[i][1].unpack(b);
-    }
-    if (NORM != kNormNone) {
-      float r = side[i] == 0 ? rq : rk;
-      if (NORM == kNormHead) {
-        float ss = 0.f;
-        if (side[i] >= 0) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) ss = fmaf(a[e], a[e], fmaf(b[e], b[e], ss));
-        }
-        for (int off = 1 << R.log_lph >> 1; off > 0; off >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-        r = rstd_of(ss, R.inv_hd, R.eps);
+    float r = side[i] == 0 ? rq : rk;
+    if constexpr (NORM == kNormHead) {
+      float a = 0.f, b = 0.f;
+      if (side[i] >= 0) {
+        u[i][0].sumsq(a, b);
+        u[i][1].sumsq(a, b);
       }
-      if (side[i] == 0 || side[i] == 1) {
-        const uint16_t* g = (side[i] == 0 ? R.q.gamma : R.k.gamma) + (long long)head[i] * R.head_dim;
-        const uint4 g0 = __ldg(reinterpret_cast<const uint4*>(g + c0[i])), g1 = __ldg(reinterpret_cast<const uint4*>(g + c1[i]));
-        const uint32_t ga[4] = {g0.x, g0.y, g0.z, g0.w}, gb[4] = {g1.x, g1.y, g1.z, g1.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          a[2 * e] *= bf_lo(ga[e]) * r;
-          a[2 * e + 1] *= bf_hi(ga[e]) * r;
-          b[2 * e] *= bf_lo(gb[e]) * r;
-          b[2 * e + 1] *= bf_hi(gb[e]) * r;
-        }
-      }
+      a += b;
+      for (int o = 1 << R.log_lph >> 1; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+      r = rstd_of(a, R.inv_hd, R.eps);
     }
     if (side[i] < 0) continue;
-    if (j[i] < r16 && side[i] != 2) {
+    const bool to_cache = CACHE && side[i] != 0;
+    const bool as_is = (side[i] == 2 || (NORM == kNormNone && !turns)) && (!to_cache || CIO::kBytes == IO::kBytes);
+    float2 a[4], b[4];
+    if (!as_is) {
+      bool scale = false;
+      if constexpr (NORM != kNormNone) {
+        if (side[i] != 2) {
+          const uint16_t* g = (side[i] == 0 ? R.q.gamma : R.k.gamma) + off[i];
+          const uint4 g0 = __ldg(reinterpret_cast<const uint4*>(g)), g1 = __ldg(reinterpret_cast<const uint4*>(g + step));
+          u[i][0].scaled(g0, make_float2(r, r), a);
+          u[i][1].scaled(g1, make_float2(r, r), b);
+          scale = true;
+        }
+      }
+      if (!scale) {
+        u[i][0].unpack(a);
+        u[i][1].unpack(b);
+      }
+      if (turns && side[i] != 2) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float4 f = cs[e * r16 + j[i]];  // pairs 8j+2e, 8j+2e+1
-        if (R.interleaved) {  // pairs 8j..8j+3 lie in a, 8j+4..8j+7 in b
-          float* p = e < 2 ? a + 4 * e : b + 4 * (e - 2);
-          const float x0 = p[0], x1 = p[1], x2 = p[2], x3 = p[3];
-          p[0] = x0 * f.x - x1 * f.y;
-          p[1] = x1 * f.x + x0 * f.y;
-          p[2] = x2 * f.z - x3 * f.w;
-          p[3] = x3 * f.z + x2 * f.w;
-        } else {
-          const float x0 = a[2 * e], y0 = b[2 * e], x1 = a[2 * e + 1], y1 = b[2 * e + 1];
-          a[2 * e] = x0 * f.x - y0 * f.y;
-          b[2 * e] = y0 * f.x + x0 * f.y;
-          a[2 * e + 1] = x1 * f.z - y1 * f.w;
-          b[2 * e + 1] = y1 * f.z + x1 * f.w;
+        for (int e = 0; e < 4; ++e) {
+          const float4 f = cs[e * r16 + j];  // pairs 8j+2e, 8j+2e+1
+          if (R.interleaved) {               // pairs 8j..8j+3 lie in a, 8j+4..8j+7 in b
+            float2& p = e < 2 ? a[2 * e] : b[2 * e - 4];
+            float2& q = e < 2 ? a[2 * e + 1] : b[2 * e - 3];
+            p = __ffma2_rn(make_float2(p.y, p.x), make_float2(-f.z, f.z), __fmul2_rn(p, make_float2(f.x, f.x)));
+            q = __ffma2_rn(make_float2(q.y, q.x), make_float2(-f.w, f.w), __fmul2_rn(q, make_float2(f.y, f.y)));
+          } else {
+            const float2 c = make_float2(f.x, f.y), sn = make_float2(f.z, f.w), x = a[e];
+            a[e] = __ffma2_rn(b[e], make_float2(-sn.x, -sn.y), __fmul2_rn(x, c));
+            b[e] = __ffma2_rn(x, sn, __fmul2_rn(b[e], c));
+          }
         }
       }
     }
-    if (CACHE && side[i] != 0) {
+    if (to_cache) {
       if (cslot < 0) continue;
       const CacheSide& C = side[i] == 1 ? R.ck : R.cv;
-      if (CIO::kBytes == 1) {
+      const int h = (off[i] - c0) / R.head_dim;
+      const long long at = cache_at(C, cslot, R.page_size, R.page_shift) + h * C.head + c0;
+      Chunk8<CIO> o0, o1;
+      if constexpr (CIO::kBytes == 1 || IO::kBytes == 1) {
+        const float2 k = make_float2(C.inv_scale, C.inv_scale);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          a[e] *= C.inv_scale;
-          b[e] *= C.inv_scale;
+        for (int e = 0; e < 4; ++e) {
+          a[e] = __fmul2_rn(a[e], k);
+          b[e] = __fmul2_rn(b[e], k);
         }
+        o0.pack(a);
+        o1.pack(b);
+      } else if (as_is) {
+        o0 = u[i][0];
+        o1 = u[i][1];
+      } else {
+        o0.pack(a);
+        o1.pack(b);
       }
-      const long long at = cache_at(C, cslot, R.page_size, head[i]);
-      Chunk8<CIO>::store(C.base, at + c0[i], a);
-      Chunk8<CIO>::store(C.base, at + c1[i], b);
+      o0.store(C.base, at);
+      o1.store(C.base, at + step);
     } else {
       const RopeSide& A = side[i] == 0 ? R.q : R.k;
-      const long long row = t * A.ldy + (long long)head[i] * R.head_dim;
-      Chunk8<IO>::store(A.y, row + c0[i], a);
-      Chunk8<IO>::store(A.y, row + c1[i], b);
+      char* row = reinterpret_cast<char*>(A.y) + t * A.ldy * IO::kBytes;
+      if (!as_is) {
+        u[i][0].pack(a);
+        u[i][1].pack(b);
+      }
+      u[i][0].store(row, off[i]);
+      u[i][1].store(row, off[i] + step);
     }
   }
 }
@@ -354,7 +383,7 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
           return v;
         };
         if (to_cache && cslot < 0) continue;
-        const long long y0 = to_cache ? cache_at(C, cslot, R.page_size, h) : t * A.ldy + (long long)h * R.head_dim;
+        const long long y0 = to_cache ? cache_at(C, cslot, R.page_size, R.page_shift) + h * C.head : t * A.ldy + (long long)h * R.head_dim;
         auto put = [&](int i, float v) {
           if (to_cache) CIO::store(C.base, y0 + i, CIO::kBytes == 1 ? v * C.inv_scale : v);
           else IO::store(A.y, y0 + i, v);
@@ -374,8 +403,8 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
 
 typedef void (*RopeKernel)(const RopeParams);
 typedef void (*RopeGeneralKernel)(const RopeParams, int);
-// in qknorm_rope_inst.cu; upt 1, 2 or 4; cache_bytes 0 = no cache
-RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt);
+// in qknorm_rope_inst.cu; upt 1 or 4, threads: of the CTA; cache_bytes 0 = no cache
+RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt, int threads);
 RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes);
 
 }  // namespace qknorm

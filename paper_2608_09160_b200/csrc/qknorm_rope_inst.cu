@@ -6,28 +6,24 @@ namespace qknorm {
 
 namespace {
 template <class IO, class CIO, int NORM, bool CACHE>
-RopeKernel pick(int upt) {
-  switch (upt) {
-    case 1: return rope_kernel<IO, CIO, NORM, CACHE, 1>;
-    case 2: return rope_kernel<IO, CIO, NORM, CACHE, 2>;
-    case 4: return rope_kernel<IO, CIO, NORM, CACHE, 4>;
-    default: return nullptr;
-  }
+RopeKernel pick(int upt, int threads) {
+  if (upt == 1) return rope_kernel<IO, CIO, NORM, CACHE, 1, 1024>;
+  return threads <= 256 ? rope_kernel<IO, CIO, NORM, CACHE, 4, 256> : rope_kernel<IO, CIO, NORM, CACHE, 4, 1024>;
 }
 template <class CIO>
-RopeKernel pick_cache(int norm, int upt) {
+RopeKernel pick_cache(int norm, int upt, int threads) {
   switch (norm) {
-    case kNormNone: return pick<IoBf16, CIO, kNormNone, true>(upt);
-    case kNormLayer: return pick<IoBf16, CIO, kNormLayer, true>(upt);
-    case kNormHead: return pick<IoBf16, CIO, kNormHead, true>(upt);
-    default: return nullptr;
+    case kNormNone: return pick<IoBf16, CIO, kNormNone, true>(upt, threads);
+    case kNormLayer: return pick<IoBf16, CIO, kNormLayer, true>(upt, threads);
+    default: return pick<IoBf16, CIO, kNormHead, true>(upt, threads);
   }
 }
 }  // namespace
 
-RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt) {
-  if (cache_bytes == 0) return elem_bytes == 1 ? pick<IoE4m3, IoE4m3, kNormNone, false>(upt) : pick<IoBf16, IoBf16, kNormNone, false>(upt);
-  return cache_bytes == 1 ? pick_cache<IoE4m3>(norm, upt) : pick_cache<IoBf16>(norm, upt);
+RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt, int threads) {
+  if (cache_bytes == 0)
+    return elem_bytes == 1 ? pick<IoE4m3, IoE4m3, kNormNone, false>(upt, threads) : pick<IoBf16, IoBf16, kNormNone, false>(upt, threads);
+  return cache_bytes == 1 ? pick_cache<IoE4m3>(norm, upt, threads) : pick_cache<IoBf16>(norm, upt, threads);
 }
 
 RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes) {
