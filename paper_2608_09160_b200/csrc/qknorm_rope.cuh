@@ -183,6 +183,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
       u[i][1].load(row, off[i] + step);
     }
   }
+  long long cslot = -1;
+  if (CACHE && live) {
+    cslot = R.slots[t];
+    if (cslot >= R.num_slots) cslot = -1;
+  }
   if (live && r16 > 0) {
     const long long pos = R.positions[t];
     for (int p = tid; p < 8 * r16; p += R.threads_per_token) {
@@ -225,11 +230,6 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
     }
     rq = rstd_of(sq, R.q.inv_d, R.eps);
     rk = rstd_of(sk, R.k.inv_d, R.eps);
-  }
-  long long cslot = -1;
-  if (CACHE && live) {
-    cslot = R.slots[t];
-    if (cslot >= R.num_slots) cslot = -1;
   }
 #pragma unroll
   for (int i = 0; i < UPT; ++i) {
