@@ -210,13 +210,13 @@ __device__ __forceinline__ void attn_span(const AttnParams& P, const AttnSeq& s,
 
 // Item number -> item; false: nothing to do (no such tokens, or a part past the end).  Later tokens first: under a
 // causal mask they see the most keys.  Key heads and parts run fastest.
-__device__ __forceinline__ bool attn_item(const AttnParams& P, long long idx, AttnItem& it) {
-  it.split = (int)(idx % P.splits);
+__device__ __forceinline__ bool attn_item(const AttnParams& P, int idx, AttnItem& it) {
+  it.split = idx % P.splits;
   idx /= P.splits;
-  it.kvh = (int)(idx % P.heads_kv);
+  it.kvh = idx % P.heads_kv;
   idx /= P.heads_kv;
-  it.b = (int)(idx % P.seqs);
-  const int qt = P.q_items - 1 - (int)(idx / P.seqs);
+  it.b = idx % P.seqs;
+  const int qt = P.q_items - 1 - idx / P.seqs;
   it.s = attn_seq(P, it.b);
   it.tok0 = qt * P.tok_per_tile * P.tiles_per_item;
   if (it.tok0 >= it.s.n) return false;

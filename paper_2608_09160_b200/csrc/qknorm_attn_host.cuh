@@ -579,6 +579,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   const long long join_ctas = (join_warps + kAttnJoinThreads / 32 - 1) / (kAttnJoinThreads / 32);
   if (plan.splits > 1 && join_ctas > 0x7fffffff) return QKNORM_ERR_SHAPE;
   long long grid = (long long)plan.q_items * seqs * cache->heads * plan.splits;
+  if (grid > 0x7fffffff - dev->sm_count) return QKNORM_ERR_SHAPE;
   if (grid > dev->sm_count) grid = dev->sm_count;
   cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
   if (e != cudaSuccess) return set_cuda_error(e);

@@ -229,7 +229,7 @@ struct AttnTc {
   const AttnMaps& maps;
   uint32_t smem;
   unsigned char* smem_ptr;
-  long long items;
+  int items;
 
   __device__ __forceinline__ volatile int* abort_flag() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kAbort); }
   __device__ __forceinline__ volatile int* poison() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kPoison); }
@@ -295,7 +295,7 @@ struct AttnTc {
       }
       return (int)page;
     };
-    for (long long idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
+    for (int idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
       AttnItem it;
       if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
@@ -405,7 +405,7 @@ struct AttnTc {
     const int lane = tid & 31;
     uint32_t pos = 0, raw_ph = 0, work_ph = 0;
     int count = 0;  // items with keys
-    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
       AttnItem it;
       if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
@@ -524,7 +524,7 @@ struct AttnTc {
     Loader ld;
     int count = 0;  // items with keys
     bool ok = true;
-    for (long long idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
+    for (int idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
       AttnItem it;
       if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
@@ -612,7 +612,7 @@ struct AttnTc {
     const uint32_t all = 0xffffffffu;
     uint32_t qph = 0, qany = 0;  // bit w: phase of Q buffer w, and whether it was in use before
     int count = 0;
-    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
       AttnItem it;
       if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
 #pragma unroll
@@ -652,7 +652,7 @@ struct AttnTc {
   __device__ __forceinline__ void run_mma(uint32_t tmem) const {
     uint32_t pos = 0, count = 0;
     uint32_t qph = 0, pph = 0, oph = 0, oany = 0;  // bit w: phase of a barrier pair's w-th barrier; oany: O_w was in use before
-    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
       AttnItem it;
       if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
       const int nt = it.j1 - it.j0;
@@ -787,7 +787,7 @@ struct AttnTc {
     else if (P.lse != nullptr) P.lse[row * P.heads_q + head] = z * kLn2;
   }
   // The rows of this warp again, one by one, each from the keys it sees and no others.
-  __device__ __forceinline__ void redo(long long idx, int w, int first) const {
+  __device__ __forceinline__ void redo(int idx, int w, int first) const {
     const int lane = threadIdx.x & 31;
     AttnItem it;
     if (!attn_item(P, idx, it)) return;
@@ -882,7 +882,7 @@ struct AttnTc {
     const uint32_t all = 0xffffffffu;
     // What the end of an item needs lies in shared memory during its tiles: registers are for the scores.
     volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 7;
-    for (long long idx = blockIdx.x; idx < items; idx += gridDim.x) {
+    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
       float m = kNegInf, l = 0.f, c = P.c;
       {
         AttnItem it;
@@ -1129,18 +1129,18 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
   const uint32_t tmem = *reinterpret_cast<const volatile uint32_t*>(smem_raw + L::kTmem);
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  const long long items = (long long)P.q_items * P.seqs * P.heads_kv * P.splits;
+  const int items = P.q_items * P.seqs * P.heads_kv * P.splits;  // the host has checked that it fits
   const K k{P, maps, smem, smem_raw, items};
-  // 512 threads start with 128 registers each; 2 x 192 + 64 + 64 = 4 x 128
+  // 512 threads start with 128 registers each; 2 x 184 + 64 + 80 = 4 x 128
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     k.run_softmax(tmem, warp >> 2);
   } else if (warp < 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (TMA) k.run_workers(threadIdx.x - 256);
     else k.run_loader(threadIdx.x - 256);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (threadIdx.x == 384) {
       k.run_mma(tmem);
       // every matrix operation has ended before the tiles and TMEM go away, whichever way the loop ended
