@@ -50,12 +50,13 @@ struct AttnParams {
   int tiles_per_item;   // query tiles an item holds: 1 or 2
   int q_items;          // items per (sequence, key head)
   int box_rows, box_shift;  // tokens of one TMA copy: the largest power of two that divides page_size and a tile; 0: no TMA
+  int q_box_tokens;  // tokens of one TMA copy of q
   int* error;
 };
 
 // K and V as [page][head][token][d], for the tensor-core kernel's copies.
 struct AttnMaps {
-  CUtensorMap k, v;
+  CUtensorMap q, k, v;  // q as [token][head][d]
 };
 
 // What one sequence's place in the batch says; everything clamped to the call's buffers.

@@ -374,6 +374,19 @@ int attn_tc_registers_ok(const void* fn) {
   return QKNORM_OK;
 }
 
+// q as [token][head][d]; a copy takes `tokens` tokens of the `group` query heads of a key head and 64 columns.
+bool encode_q(CUtensorMap* map, const AttnParams& P, int tokens) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)P.head_dim, (cuuint64_t)P.heads_q, (cuuint64_t)P.T};
+  const cuuint64_t strides[2] = {(cuuint64_t)P.head_dim * 2, (cuuint64_t)P.ld_q * 2};
+  if (strides[0] % 16 != 0 || strides[1] % 16 != 0 || strides[1] >= ((cuuint64_t)1 << 40)) return false;
+  const cuuint32_t box[3] = {64, (cuuint32_t)P.group, (cuuint32_t)tokens};
+  const cuuint32_t ones[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(P.q), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // How a call is cut: sizes only, so that the workspace can be asked for beforehand.
 struct AttnPlan {
   bool tc = false;
@@ -565,7 +578,8 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   memset(&maps, 0, sizeof(maps));
   int rows = kAttnTile;
   while (cache->page_size % rows != 0) rows /= 2;
-  const bool tma = rows >= 8 && cache->num_pages > 0 && encode_side(&maps.k, *cache, P.k, dp, rows) && encode_side(&maps.v, *cache, P.v, dp, rows);
+  P.q_box_tokens = plan.form == kAttnQuad ? 32 / P.group : plan.tok_per_tile;
+  const bool tma = rows >= 8 && cache->num_pages > 0 && encode_q(&maps.q, P, P.q_box_tokens) && encode_side(&maps.k, *cache, P.k, dp, rows) && encode_side(&maps.v, *cache, P.v, dp, rows);
   if (tma) {
     P.box_rows = rows;
     while ((1 << P.box_shift) < rows) ++P.box_shift;

@@ -6,7 +6,7 @@
 //   warp 13      copies K and V tiles into a ring in shared memory with TMA, a box per page and 64 columns
 //   warps 8-11   prepare what has arrived: widen FP8 tiles, blank V rows outside the item's keys; where a page is no
 //                multiple of 8 tokens they gather the rows themselves with cp.async
-//   warps 14-15  gather the query rows
+//   warp 14      brings the query rows, by TMA where K and V come that way
 //   warp 12      issues every tcgen05.mma
 // Scores S_w = Q K^T land in TMEM (128 columns per warpgroup w).  The warpgroup reads them, keeps the running
 // maximum and sum in registers, writes P = 2^(c (s - m)) back over S in 16 bits, and O_w += P V takes P from
@@ -136,6 +136,12 @@ __device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* map, int x
       "l"(map), "r"(x), "r"(t), "r"(h), "r"(p), "r"(bar)
       : "memory");
 }
+__device__ __forceinline__ void tma3(uint32_t dst, const CUtensorMap* map, int x, int h, int t, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(h), "r"(t), "r"(bar)
+      : "memory");
+}
 // 16 bytes from global to shared memory, or 16 zero bytes
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool take) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
@@ -174,7 +180,8 @@ struct AttnSmem {
   static constexpr int kDrain = kMlFree + 8;
   static constexpr int kRawFull = kDrain + 8;         // per stage: an FP8 tile, or a bf16 V tile that wants looking at, is there
   static constexpr int kWork = kRawFull + 8 * kStages;  // the four warps that widen have all read the tile
-  static constexpr int kPass = kWork + 8;             // the softmax warps' steps through the join of an item
+  static constexpr int kQRaw = kWork + 8;             // [2] FP8 cache: a bf16 Q tile is there
+  static constexpr int kPass = kQRaw + 16;            // the softmax warps' steps through the join of an item
   static constexpr int kTmem = kPass + 8;             // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
   static constexpr int kPoison = kAbort + 4;          // [4] 1 + number of an item that holds a V row to be careful with
@@ -182,8 +189,8 @@ struct AttnSmem {
   // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
   // round again only after the tensor warp has seen the scores of the item before last consumed.
   static constexpr int kQScale = kPoison + 16;
-  static constexpr int kNotes = kQScale + (F8 ? 512 : 0);  // [8 softmax warps][7] ints
-  static constexpr int kMlRows = kNotes + 224;             // [8 softmax warps][32] float2, one-tile forms: (m, l) of their parts
+  static constexpr int kNotes = kQScale + (F8 ? 512 : 0);  // [8 softmax warps][6] ints
+  static constexpr int kMlRows = kNotes + 192;             // [8 softmax warps][32] float2, one-tile forms: (m, l) of their parts
   static constexpr int kBytes = kMlRows + 2048;
 };
 
@@ -550,7 +557,7 @@ struct AttnTc {
   }
 
   // ---- query tiles ----------------------------------------------------------------------------------
-  static constexpr int kQThreads = 64;  // warps 14-15
+  static constexpr int kQThreads = 32;  // warp 14
 
   // Query tile of `rows` rows from token tok0 into Q buffer `buf`; the rest of the last 32 rows in use is zeros.  QUAD: the
   // same 32 rows four times.
@@ -584,25 +591,54 @@ struct AttnTc {
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
           const int r = i0 + b * kStep;
-          const uint32_t u[4] = {v[b].x, v[b].y, v[b].z, v[b].w};
-          uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
+          q_to_f16(v[b], r, c, scale_set);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t lo = u[e] & 0x7fffu, hi = (u[e] >> 16) & 0x7fffu;
-            mag = max(mag, max(lo, hi));
-          }
+          for (int k = 0; k < (QUAD ? 4 : 1); ++k) tc::sts128(dst + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4), v[b].x, v[b].y, v[b].z, v[b].w);
+        }
+      }
+    }
+  }
+
+  // FP8 cache: 8 elements of Q row r (the row's other pieces are in the neighbouring lanes) from bf16 to fp16, the row's largest
+  // exponent brought to 2^8; rows of zeros, tiny rows and rows with infinities or NaN as they are.
+  __device__ __forceinline__ void q_to_f16(uint4& v, int r, int c, int scale_set) const {
+    uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
 #pragma unroll
-          for (int off = kQChunks / 2; off > 0; off >>= 1) mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, off));
-          // bring the row's largest exponent to 2^8; rows of zeros, tiny rows and rows with infinities or NaN as they are
-          const int e = (int)(mag >> 7);
-          const bool scaled = e > 16 && e < 255;
-          const float f = scaled ? __uint_as_float((uint32_t)(127 + 135 - e) << 23) : 1.f;
-          uint32_t h[4];
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t lo = u[e] & 0x7fffu, hi = (u[e] >> 16) & 0x7fffu;
+      mag = max(mag, max(lo, hi));
+    }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) h[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
+    for (int off = DP / 16; off > 0; off >>= 1) mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, off));
+    const int e = (int)(mag >> 7);
+    const bool scaled = e > 16 && e < 255;
+    const float f = scaled ? __uint_as_float((uint32_t)(127 + 135 - e) << 23) : 1.f;
 #pragma unroll
-          for (int k = 0; k < (QUAD ? 4 : 1); ++k) tc::sts128(dst + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4), h[0], h[1], h[2], h[3]);
-          if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
+    for (int k = 0; k < 4; ++k) u[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
+    v = make_uint4(u[0], u[1], u[2], u[3]);
+    if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
+  }
+
+  // The rows of a Q tile that a TMA copy has brought, to fp16 in place.
+  __device__ __forceinline__ void convert_q(int lane, int rows, int buf, int scale_set) const {
+    constexpr int kQChunks = DP / 8, kStep = 32 / kQChunks, kBatch = 4;
+    const int c = lane % kQChunks;
+    const uint32_t base = smem + L::kQ0 + buf * L::kTile + (c >> 3) * kHalf;
+    const int end = (rows + kStep * kBatch - 1) / (kStep * kBatch) * (kStep * kBatch);  // at most 128, QUAD 32
+    for (int k = 0; k < (QUAD ? 4 : 1); ++k) {
+      for (int i0 = lane / kQChunks; i0 < end; i0 += kStep * kBatch) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int r = i0 + b * kStep;
+          v[b] = ptx::lds128(base + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4));
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+          const int r = i0 + b * kStep;
+          q_to_f16(v[b], r, c, scale_set);
+          tc::sts128(base + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4), v[b].x, v[b].y, v[b].z, v[b].w);
         }
       }
     }
@@ -619,14 +655,48 @@ struct AttnTc {
       for (int w = 0; w < 2; ++w) {
         const AttnTileRange r = attn_tile_range(P, it, ONE ? 0 : w);
         if (ONE ? w != (count & 1) : r.a >= r.b) continue;
-        if (((qany >> w) & 1) && !__all_sync(all, wait(smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) return;
-        load_q(tid, it, it.tok0 + (ONE ? 0 : w * P.tok_per_tile), r.rows, w, ONE ? count & 3 : w + 2 * ((qph >> w) & 1));
-        if (!F8) tc::cp_wait_all();
-        signal(smem + L::kQFull + 8 * w, tid & 31);
+        if (((qany >> w) & 1) && !__all_sync(all, wait(smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) {
+          if (TMA) drain_q(qph, -1);
+          return;
+        }
+        const int tok0 = it.tok0 + (ONE ? 0 : w * P.tok_per_tile), set = ONE ? count & 3 : w + 2 * ((qph >> w) & 1);
+        const uint32_t q_full = smem + L::kQFull + 8 * w;
+        if constexpr (TMA) {
+          // the tile's tokens and heads as one box per 64 columns (QUAD: four times); tokens of other sequences that come
+          // along stand in rows nobody looks at
+          constexpr int kCopies = QUAD ? 4 : 1;
+          const uint32_t bar = F8 ? smem + L::kQRaw + 8 * w : q_full;
+          if (tid == 0) {
+            ptx::mbar_arrive_expect_tx(bar, (DP / 64) * kCopies * P.q_box_tokens * P.group * 128);
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k)
+#pragma unroll
+              for (int h = 0; h < DP / 64; ++h)
+                tc::tma3(smem + L::kQ0 + w * L::kTile + h * kHalf + k * 32 * 128, &maps.q, h * 64, it.kvh * P.group, it.s.row0 + tok0, bar);
+          }
+          if constexpr (F8) {
+            if (!__all_sync(all, wait(bar, (qph >> w) & 1))) return drain_q(qph, w);
+            convert_q(tid, r.rows, w, set);
+            signal(q_full, tid);
+          }
+        } else {
+          load_q(tid, it, tok0, r.rows, w, set);
+          if (!F8) tc::cp_wait_all();
+          signal(q_full, tid);
+        }
         qph ^= 1u << w;
         qany |= 1u << w;
       }
       ++count;
+    }
+    if (TMA && *abort_flag()) drain_q(qph, -1);
+  }
+  // Left early: the copies under way into the Q buffers have to land first.  qph: phases that have been asked for; open: a buffer
+  // whose newest copy is not counted in it yet.
+  __device__ __forceinline__ void drain_q(uint32_t qph, int open) const {
+    for (int w = 0; w < 2; ++w) {
+      const uint32_t bar = smem + (F8 ? L::kQRaw : L::kQFull) + 8 * w;
+      wait_drain(bar, w == open ? (qph >> w) & 1 : ((qph >> w) & 1) ^ 1);
     }
   }
 
@@ -649,6 +719,9 @@ struct AttnTc {
       tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2048 >> 4), idesc, acc || s > 0);
   }
 
+  // One thread issues for both warpgroups, in turn: that keeps one of them in its exponentials while the other's products are
+  // made.  (With a thread for each the products of the two interleave, both warpgroups wait for them and then both compute:
+  // a whole prompt of 8192 took 1024 us instead of 854.)
   __device__ __forceinline__ void run_mma(uint32_t tmem) const {
     uint32_t pos = 0, count = 0;
     uint32_t qph = 0, pph = 0, oph = 0, oany = 0;  // bit w: phase of a barrier pair's w-th barrier; oany: O_w was in use before
@@ -881,7 +954,7 @@ struct AttnTc {
     int count = 0;
     const uint32_t all = 0xffffffffu;
     // What the end of an item needs lies in shared memory during its tiles: registers are for the scores.
-    volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 7;
+    volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 6;
     for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
       float m = kNegInf, l = 0.f, c = P.c;
       {
@@ -893,11 +966,10 @@ struct AttnTc {
         if (lane == 0) {
           note[0] = it.s.row0;
           note[1] = tok0;
-          note[2] = it.kvh;
+          note[2] = it.kvh | (rg.a < rg.b ? 1 << 30 : 0);
           note[3] = it.split;
           note[4] = rg.rows;
           note[5] = it.j1 - it.j0;
-          note[6] = rg.a < rg.b;
         }
         __syncwarp();
         if (it.j0 < it.j1) {
@@ -922,11 +994,11 @@ struct AttnTc {
           }
         }
       }
-      const int tiles = note[5], rows = note[4], split = note[3], head = note[2] * P.group + wtid % P.group;
+      const int tiles = note[5], rows = note[4], split = note[3], head = (note[2] & 0xfffff) * P.group + wtid % P.group;
       const long long row = note[0] + (long long)(note[1] + wtid / P.group);
       const bool valid = wtid < rows, busy = first_row < rows;
       if (!ONE) {
-        const bool own = note[6] != 0;  // some tile of the item was this warpgroup's
+        const bool own = (note[2] >> 30) != 0;  // some tile of the item was this warpgroup's
         if (own) {
           if (!__all_sync(all, wait(smem + L::kOFull + 8 * w, oph))) return;
           oph ^= 1;
@@ -1046,6 +1118,8 @@ struct AttnTc {
             if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
             pass ^= 1;
           }
+          ptx::fence_proxy_async();  // the buffer's next writer is a copy
+          __syncwarp();
           if (lane == 0) tc::arrive(smem + L::kQEmpty + 8 * (count & 1));
           if (valid && part == 0 && !again) store_z(z, row, head, split);
           if (again && part == 0) redo(idx, 0, 0);
@@ -1102,7 +1176,8 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
       ptx::mbar_init(smem + L::kRawFull + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(smem + L::kQFull + 8 * i, 2);
+      ptx::mbar_init(smem + L::kQFull + 8 * i, 1);
+      ptx::mbar_init(smem + L::kQRaw + 8 * i, 1);
       ptx::mbar_init(smem + L::kQEmpty + 8 * i, K::QUAD ? 9 : 1);
       ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
@@ -1141,15 +1216,19 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     else k.run_loader(threadIdx.x - 256);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (threadIdx.x == 384) {
-      k.run_mma(tmem);
-      // every matrix operation has ended before the tiles and TMEM go away, whichever way the loop ended
-      tc::commit(smem + L::kDrain);
-      k.wait_drain(smem + L::kDrain, 0);
+    if (warp == 12) {
+      if ((threadIdx.x & 31) == 0) {
+        k.run_mma(tmem);
+        // every matrix product has ended before the tiles and TMEM go away, whichever way the loop ended
+        tc::commit(smem + L::kDrain);
+        k.wait_drain(smem + L::kDrain, 0);
+      }
+      __syncwarp();
+    } else if (warp == 13) {
+      if (TMA) k.run_producer(threadIdx.x & 31);
+    } else if (warp == 14) {
+      k.run_q(threadIdx.x & 31);
     }
-    __syncwarp();
-    if (TMA && warp == 13) k.run_producer(threadIdx.x & 31);
-    if (warp >= 14) k.run_q(threadIdx.x - 448);
   }
   tc::fence_before();
   __syncthreads();
