@@ -110,6 +110,11 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -173,7 +178,8 @@ struct AttnSmem {
   static constexpr int kQEmpty = kQFull + 16;
   static constexpr int kSFull = kQEmpty + 16;
   static constexpr int kPFull = kSFull + 16;
-  static constexpr int kOFull = kPFull + 16;
+  static constexpr int kPHalf = kPFull + 16;  // the first 64 keys' weights are there (not QUAD)
+  static constexpr int kOFull = kPHalf + 16;
   static constexpr int kOFree = kOFull + 16;
   static constexpr int kMl = kOFree + 16;
   static constexpr int kMlFree = kMl + 8;
@@ -711,12 +717,23 @@ struct AttnTc {
     }
     tc::commit(smem + L::kSFull + 8 * w);
   }
-  __device__ __forceinline__ void issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc) const {
+  // Waits for P as it goes.
+  __device__ __forceinline__ bool issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc, uint32_t p_phase) const {
     constexpr uint32_t idesc = tc::instr_desc(DP, F8, true);
     const uint32_t v = tc::desc_lo(stage(pos), kHalf);
+    if (!QUAD) {
+      if (!wait(smem + L::kPHalf + 8 * w, p_phase)) return false;
+      tc::fence_after();
 #pragma unroll
-    for (int s = 0; s < kAttnTile / 16; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
+      for (int s = 0; s < kAttnTile / 32; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
+        tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2048 >> 4), idesc, acc || s > 0);
+    }
+    if (!wait(smem + L::kPFull + 8 * w, p_phase)) return false;
+    tc::fence_after();
+#pragma unroll
+    for (int s = QUAD ? 0 : kAttnTile / 32; s < kAttnTile / 16; ++s)
       tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2048 >> 4), idesc, acc || s > 0);
+    return true;
   }
 
   // One thread issues for both warpgroups, in turn: that keeps one of them in its exponentials while the other's products are
@@ -736,11 +753,9 @@ struct AttnTc {
           if (r >= 0) {
             const uint32_t vp = pos + 2 * r + 1;
             if (!wait(full(vp), (vp / L::kStages) & 1)) return;
-            if (!wait(smem + L::kPFull + 8 * w, (pph >> w) & 1)) return;
-            pph ^= 1u << w;
             if (r < 2 && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
-            tc::fence_after();
-            issue_pv(tmem, w, vp, r >= 2);
+            if (!issue_pv(tmem, w, vp, r >= 2, (pph >> w) & 1)) return;
+            pph ^= 1u << w;
             tc::commit(empty(vp));
             if (r + 2 >= nt) {
               tc::commit(smem + L::kOFull + 8 * w);
@@ -765,17 +780,16 @@ struct AttnTc {
         const AttnTileRange r0 = attn_tile_range(P, it, 0), r1 = attn_tile_range(P, it, 1);
         const int a[2] = {r0.a, r1.a}, b[2] = {r0.b, r1.b};
         for (int j = it.j0 - 1; j < it.j1; ++j) {
+          // both tiles of this round before anything is issued: a wait between two products leaves the tensor pipe idle
           const uint32_t kp = pos + 2 * (j + 1 - it.j0), vp = kp - 1;
           if (j >= it.j0 && !wait(full(vp), (vp / L::kStages) & 1)) return;
-          bool have_k = false;
+          if (j + 1 < it.j1 && !wait(full(kp), (kp / L::kStages) & 1)) return;
 #pragma unroll
           for (int w = 0; w < 2; ++w) {
             if (j >= a[w] && j < b[w]) {
-              if (!wait(smem + L::kPFull + 8 * w, (pph >> w) & 1)) return;
-              pph ^= 1u << w;
               if (j == a[w] && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
-              tc::fence_after();
-              issue_pv(tmem, w, vp, j > a[w]);
+              if (!issue_pv(tmem, w, vp, j > a[w], (pph >> w) & 1)) return;
+              pph ^= 1u << w;
               if (j == b[w] - 1) {
                 tc::commit(smem + L::kOFull + 8 * w);
                 oph ^= 1u << w;
@@ -786,19 +800,14 @@ struct AttnTc {
               if (j + 1 == a[w]) {
                 if (!wait(smem + L::kQFull + 8 * w, (qph >> w) & 1)) return;
                 qph ^= 1u << w;
+                tc::fence_after();
               }
-              if (!have_k && !wait(full(kp), (kp / L::kStages) & 1)) return;
-              have_k = true;
-              tc::fence_after();
               issue_qk(tmem, w, w, kp);
               if (j + 1 == b[w] - 1) tc::commit(smem + L::kQEmpty + 8 * w);
             }
           }
           if (j >= it.j0) tc::commit(empty(vp));
-          if (j + 1 < it.j1) {
-            if (!have_k && !wait(full(kp), (kp / L::kStages) & 1)) return;
-            tc::commit(empty(kp));
-          }
+          if (j + 1 < it.j1) tc::commit(empty(kp));
         }
       }
       pos += 2 * nt;
@@ -888,8 +897,9 @@ struct AttnTc {
 
   // One score tile: S -> P, running m and l of this lane's row.  QUAD: the 32 columns of this warp's quarter.
   // Columns [from, to) of the tile are keys that the row sees.
+  // Two forms: the first half of P is announced while the second is computed.
   __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
-                                       float& l) const {
+                                       float& l, uint32_t p_half) const {
     constexpr int N = QUAD ? kAttnTile / 4 : kAttnTile;
     const int first_col = QUAD ? (int)((threadIdx.x >> 5) & 3) * N : 0;
     float s[N];
@@ -902,11 +912,11 @@ struct AttnTc {
     }
     float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-    for (int k = 4; k < N; k += 4) {
+    for (int k = 4; k < N - 4; k += 8) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], s[k + e]);
+      for (int e = 0; e < 4; ++e) mx[e] = tc::max3(mx[e], s[k + e], s[k + 4 + e]);
     }
-    const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+    const float mn = fmaxf(tc::max3(mx[0], mx[1], s[N - 4]), tc::max3(mx[2], tc::max3(mx[3], s[N - 3], s[N - 2]), s[N - 1]));
     // m is the maximum that the exponents are taken against; it follows the true one when that is 2^8 ahead
     const bool grow = mn > m && (m == kNegInf || (mn - m) * c > 8.f);
     if (__any_sync(0xffffffffu, grow)) {
@@ -933,6 +943,12 @@ struct AttnTc {
         p[e] = F8 ? tc::pack_f16(x.x, x.y) : bf_pack(x.x, x.y);
       }
       tc::st16(s_addr + first_col / 2 + h * 16, p);
+      if (!QUAD && h == 1) {
+        tc::wait_st();
+        tc::fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) tc::arrive(p_half);
+      }
     }
     if (QUAD) {  // the other quarters' keys are not this warp's: zeros in their place
       uint32_t none[16];
@@ -987,10 +1003,13 @@ struct AttnTc {
               if (F8) c = row_c(ONE ? count & 3 : w + 2 * oph, wtid);
               const int k0 = j * kAttnTile;
               tile(tmem + lanes + w * kAttnTile, tmem + lanes + 2 * kAttnTile + w * DP, lo - k0, hi - k0,
-                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l);
+                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l, smem + L::kPHalf + 8 * w);
             }
             __syncwarp();
-            if (lane == 0) tc::arrive(smem + L::kPFull + 8 * w);
+            if (lane == 0) {
+              if (!QUAD && !busy) tc::arrive(smem + L::kPHalf + 8 * w);
+              tc::arrive(smem + L::kPFull + 8 * w);
+            }
           }
         }
       }
@@ -1181,6 +1200,7 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
       ptx::mbar_init(smem + L::kQEmpty + 8 * i, K::QUAD ? 9 : 1);
       ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
+      ptx::mbar_init(smem + L::kPHalf + 8 * i, 4);
       ptx::mbar_init(smem + L::kOFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kOFree + 8 * i, K::ONE ? 8 : 4);
     }
