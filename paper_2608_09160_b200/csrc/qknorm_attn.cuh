@@ -50,11 +50,16 @@ struct AttnParams {
   int tiles_per_item;   // query tiles an item holds: 1 or 2
   int q_items;          // items per (sequence, key head)
   int box_rows, box_shift;  // tokens of one TMA copy: the largest power of two that divides page_size and a tile; 0: no TMA
+  int box_kind;      // what a TMA copy of K and V takes, below
   int q_box_tokens;  // tokens of one TMA copy of q
   int* error;
 };
 
 // K and V as [page][head][token][d], for the tensor-core kernel's copies.
+// A copy brings tokens of a page times: 64 columns of a head, from [page][head][token][d] (kBoxHalf; FP8: all its columns);
+// a whole head of 128, from [page][8 tokens][head and half][token][64 columns], where heads lie side by side in a token
+// (kBoxHeadInRow), or from [page and head][8 tokens][half][token][64 columns], where a page's heads follow one another (kBoxHeadInPage).
+constexpr int kBoxHalf = 0, kBoxHeadInRow = 1, kBoxHeadInPage = 2;
 struct AttnMaps {
   CUtensorMap q, k, v;  // q as [token][head][d]
 };

@@ -339,21 +339,48 @@ EncodeTiled encode_tiled() {
   return fn;
 }
 
-// One side of the cache as [page][head][token][d]; a copy takes `rows` tokens of one head and 64 columns, swizzled as the matrix
-// unit reads them (FP8: all columns, as they are, to be widened).  False: no such map (then rows are gathered one by one).
-bool encode_side(CUtensorMap* map, const qknorm_paged_cache& c, const AttnSide& s, int dp, int rows) {
+// How copies can take a whole head of 128 bf16 values: both sides have to allow it.
+int whole_head_kind(const qknorm_paged_cache& c) {
+  if (c.e4m3 || c.head_dim != 128) return kBoxHalf;
+  if ((c.heads == 1 || (c.k_head == 128 && c.v_head == 128))) return kBoxHeadInRow;
+  if ((c.num_pages == 1 || (c.k_page == c.heads * c.k_head && c.v_page == c.heads * c.v_head)) && c.num_pages * c.heads < 0x7fffffff)
+    return kBoxHeadInPage;
+  return kBoxHalf;
+}
+
+// One side of the cache, laid out as `kind` says; a copy takes `rows` tokens, swizzled as the matrix unit reads them (FP8: as
+// they are, to be widened).  False: no such map.
+bool encode_side(CUtensorMap* map, const qknorm_paged_cache& c, const AttnSide& s, int kind, int dp, int rows) {
   const EncodeTiled enc = encode_tiled();
   if (!enc) return false;
   const cuuint64_t eb = c.e4m3 ? 1 : 2;
-  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.num_pages};
   // the stride of an axis of one is never used, but has to look like one
   const cuuint64_t row = ((cuuint64_t)c.head_dim * eb + 15) / 16 * 16;
-  const cuuint64_t strides[3] = {c.page_size > 1 ? s.token * eb : row, c.heads > 1 ? s.head * eb : row, c.num_pages > 1 ? s.page * eb : row};
-  for (cuuint64_t st : strides)
-    if (st == 0 || st % 16 != 0 || st >= ((cuuint64_t)1 << 40)) return false;
-  const cuuint32_t box[4] = {(cuuint32_t)(c.e4m3 ? dp : 64), (cuuint32_t)rows, 1, 1};
-  const cuuint32_t ones[4] = {1, 1, 1, 1};
-  return enc(map, c.e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(s.base), dims, strides, box,
+  const cuuint64_t token = c.page_size > 1 ? s.token * eb : row, head = c.heads > 1 ? s.head * eb : row, page = c.num_pages > 1 ? s.page * eb : row;
+  const cuuint64_t pages = (cuuint64_t)c.num_pages, heads = (cuuint64_t)c.heads, tokens = (cuuint64_t)c.page_size;
+  cuuint64_t dims[5], strides[4];
+  cuuint32_t box[5];
+  cuuint32_t n = 4;
+  if (kind == kBoxHalf) {
+    const cuuint64_t d[4] = {(cuuint64_t)c.head_dim, tokens, heads, pages}, st[3] = {token, head, page};
+    const cuuint32_t b[4] = {(cuuint32_t)(c.e4m3 ? dp : 64), (cuuint32_t)rows, 1, 1};
+    memcpy(dims, d, sizeof(d));
+    memcpy(strides, st, sizeof(st));
+    memcpy(box, b, sizeof(b));
+  } else {
+    n = 5;
+    const bool in_row = kind == kBoxHeadInRow;
+    const cuuint64_t d[5] = {64, 8, in_row ? 2 * heads : 2, tokens / 8, in_row ? pages : pages * heads};
+    const cuuint64_t st[4] = {token, 128, 8 * token, in_row ? page : c.heads > 1 ? head : page};
+    const cuuint32_t b[5] = {64, 8, 2, (cuuint32_t)rows / 8, 1};
+    memcpy(dims, d, sizeof(d));
+    memcpy(strides, st, sizeof(st));
+    memcpy(box, b, sizeof(b));
+  }
+  for (cuuint32_t i = 0; i + 1 < n; ++i)
+    if (strides[i] == 0 || strides[i] % 16 != 0 || strides[i] >= ((cuuint64_t)1 << 40)) return false;
+  const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+  return enc(map, c.e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, n, const_cast<void*>(s.base), dims, strides, box,
              ones, CU_TENSOR_MAP_INTERLEAVE_NONE, c.e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -579,7 +606,17 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   int rows = kAttnTile;
   while (cache->page_size % rows != 0) rows /= 2;
   P.q_box_tokens = plan.form == kAttnQuad ? 32 / P.group : plan.tok_per_tile;
-  const bool tma = rows >= 8 && cache->num_pages > 0 && encode_q(&maps.q, P, P.q_box_tokens) && encode_side(&maps.k, *cache, P.k, dp, rows) && encode_side(&maps.v, *cache, P.v, dp, rows);
+  bool tma = rows >= 8 && cache->num_pages > 0 && encode_q(&maps.q, P, P.q_box_tokens);
+  if (tma) {
+    auto both = [&](int kind) {
+      P.box_kind = kind;
+      // a tile's 128-column rows keep their halves side by side in groups of 8 rows: half a head at a time goes there by eights
+      if (kind == kBoxHalf && !cache->e4m3 && dp == 128) rows = 8;
+      return encode_side(&maps.k, *cache, P.k, kind, dp, rows) && encode_side(&maps.v, *cache, P.v, kind, dp, rows);
+    };
+    const int kind = whole_head_kind(*cache);
+    tma = both(kind) || (kind != kBoxHalf && both(kBoxHalf));
+  }
   if (tma) {
     P.box_rows = rows;
     while ((1 << P.box_shift) < rows) ++P.box_shift;

@@ -3,7 +3,7 @@
 // A persistent CTA per SM walks over items: the query rows of one sequence that share a key head -- tokens
 // times the group's query heads, packed into tiles of 128 rows -- and a range of key tiles of 128 keys.
 //   warps 0-7    two softmax warpgroups; a thread owns a row of a 128 x 128 score tile
-//   warp 13      copies K and V tiles into a ring in shared memory with TMA, a box per page and 64 columns
+//   warp 13      copies K and V tiles into a ring in shared memory with TMA, a box per page (and tile)
 //   warps 8-11   prepare what has arrived: widen FP8 tiles, blank V rows outside the item's keys; where a page is no
 //                multiple of 8 tokens they gather the rows themselves with cp.async
 //   warp 14      brings the query rows, by TMA where K and V come that way
@@ -41,28 +41,28 @@ namespace qknorm {
 namespace tc {
 
 // Shared-memory matrix descriptor, 128-byte swizzle.  The low word holds the address in 16-byte units (moving on by n
-// bytes adds n / 16 to it) and the leading stride, the high word the stride between groups of 8 rows: a constant.
+// bytes adds n / 16 to it) and the leading stride, the high word the stride between groups of 8 rows: a constant of the tile.
 __device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lbo) { return (addr >> 4) | ((lbo >> 4) << 16); }
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__host__ __device__ constexpr uint32_t desc_hi(uint32_t group) { return (group >> 4) | (1u << 14) | (2u << 29); }
 // fp32 accumulators, both operands bf16 (or both fp16), M = 128
 __host__ __device__ constexpr uint32_t instr_desc(int n, bool f16, bool b_transposed) {
   return (1u << 4) | ((f16 ? 0u : 1u) << 7) | ((f16 ? 0u : 1u) << 10) | ((b_transposed ? 1u : 0u) << 16) |
          ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool acc) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, bool acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %6};\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)acc),
-      "r"(kDescHi)
+      "r"(a_hi), "r"(b_hi)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, bool acc) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, bool acc) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.u32 p, %4, 0;\n\t"
       "mov.b64 b, {%2, %5};\n\t"
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"((uint32_t)acc),
-      "r"(kDescHi)
+      "r"(b_hi)
       : "memory");
 }
 __device__ __forceinline__ void commit(uint32_t bar) {
@@ -139,6 +139,13 @@ __device__ __forceinline__ void tma4(uint32_t dst, const CUtensorMap* map, int x
   asm volatile(
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
       "l"(map), "r"(x), "r"(t), "r"(h), "r"(p), "r"(bar)
+      : "memory");
+}
+// Whole rows of 128 columns: half column h of the row (or of the head), 8-token group t, page (or page and head) p.
+__device__ __forceinline__ void tma5(uint32_t dst, const CUtensorMap* map, int h, int t, int p, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(h), "r"(t), "r"(p), "r"(bar)
       : "memory");
 }
 __device__ __forceinline__ void tma3(uint32_t dst, const CUtensorMap* map, int x, int h, int t, uint32_t bar) {
@@ -236,7 +243,13 @@ struct AttnTc {
   using L = AttnSmem<DP, F8>;
   static constexpr bool ONE = FORM != kAttnTwo;
   static constexpr bool QUAD = FORM == kAttnQuad;
-  static constexpr int kHalf = kAttnTile * 128;  // bytes of a 64-column half of a tile
+  // Tiles of 64 columns: rows of 128 bytes, 16-byte pieces swizzled within 8 rows.  Q: its 64-column halves one after the
+  // other.  K and V: groups of 8 rows, a group's halves side by side -- so that one TMA box can bring whole rows of a page.
+  static constexpr int kHalf = kAttnTile * 128;
+  static constexpr int kGroup = 8 * 2 * DP;  // bytes of 8 rows of K or V
+  __device__ __forceinline__ static uint32_t kv_at(int r, int c) {  // row r, 16-byte piece c
+    return (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (((c ^ r) & 7) << 4);
+  }
 
   const AttnParams& P;
   const AttnMaps& maps;
@@ -288,13 +301,14 @@ struct AttnTc {
     return VJob{k0 < it.ulo || k0 + kAttnTile > it.uhi, attn_cut(it, r0, j) || (!ONE && attn_cut(it, r1, j))};
   }
 
-  // Warp 13.  A lane issues one box: the tokens of a page (or 128 of them) times 64 columns (FP8: all columns).
+  // Warp 13.  A lane issues one box: tokens of a page, whole heads or 64 columns of them.
   __device__ __forceinline__ void run_producer(int lane) const {
-    constexpr int kHalves = F8 ? 1 : DP / 64;
     const uint32_t all = 0xffffffffu;
-    const int boxes = (kAttnTile >> P.box_shift) * kHalves;  // at most 32: a box has at least 8 tokens
-    const int box = lane / kHalves, half = lane % kHalves;
-    const uint32_t at = F8 ? (uint32_t)(box * P.box_rows * DP) : (uint32_t)(half * kHalf + box * P.box_rows * 128);
+    // at most 32 boxes: one has at least 8 tokens; half heads (kBoxHalf) only come in boxes of 8
+    const int halves = !F8 && P.box_kind == kBoxHalf ? DP / 64 : 1;
+    const int boxes = (kAttnTile >> P.box_shift) * halves;
+    const int box = lane / halves, half = lane % halves;
+    const uint32_t at = box * P.box_rows * (F8 ? DP : 2 * DP) + half * 1024;
     uint32_t pos = 0, waiting_raw = 0, raw_ph = 0;  // bits by stage: its newest tile went to kRawFull; phase of kRawFull
     bool ok = true;
     // page and token of this lane's box of tile j; the page past the last one stands for zeros
@@ -334,7 +348,12 @@ struct AttnTc {
             ptx::mbar_arrive_expect_tx(bar, F8 ? L::kRaw : L::kTile);
           }
           __syncwarp();
-          if (lane < boxes) tc::tma4(dst + at, v ? &maps.v : &maps.k, half * 64, within, it.kvh, page, bar);
+          if (lane < boxes) {
+            const CUtensorMap* map = v ? &maps.v : &maps.k;
+            if (P.box_kind == kBoxHalf) tc::tma4(dst + at, map, half * 64, within, it.kvh, page, bar);
+            else if (P.box_kind == kBoxHeadInRow) tc::tma5(dst + at, map, 2 * it.kvh, within >> 3, page, bar);
+            else tc::tma5(dst + at, map, 0, within >> 3, page * P.heads_kv + it.kvh, bar);
+          }
           ++pos;
         }
       }
@@ -367,7 +386,7 @@ struct AttnTc {
 #pragma unroll 4
     for (int i = 0; i < kChunks; ++i) {
       const int r = row_of(tid, i);
-      const uint32_t at = tile_at + (c >> 3) * kHalf + r * 128 + (((c ^ r) & 7) << 4);
+      const uint32_t at = tile_at + kv_at(r, c);
       if (r < from || r >= to) {
         if (blank) tc::sts128(at, 0u, 0u, 0u, 0u);
       } else if (look) {
@@ -384,7 +403,8 @@ struct AttnTc {
   __device__ __forceinline__ bool widen(uint32_t tile_at, int tid, uint32_t& work_ph, int from, int to, bool& bad) const {
     const int c = tid % kChunks, r0 = row_of(tid, 0);
     const uint32_t src = tile_at + L::kRaw + r0 * DP + c * 16;
-    const uint32_t dst = tile_at + (c >> 2) * kHalf + r0 * 128, turn = (((2 * c) ^ r0) & 7) << 4;
+    // piece 2c of row r0; the next rows of this thread are kRowsAt further each, which is 4 or 8: half a group or one
+    const uint32_t dst = tile_at + kv_at(r0 & ~7, 2 * c & ~7), row = (r0 & 7) * 128, turn = (((2 * c) ^ r0) & 7) << 4;
     uint4 v[kChunks];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) v[i] = ptx::lds128(src + i * kRowsAt * DP);
@@ -404,8 +424,7 @@ struct AttnTc {
 #pragma unroll
         for (int e = 0; e < 8; ++e) bad |= odd_f16(h[e]);
       }
-      // the swizzle of row r0 + i * kRowsAt differs from row r0's by a constant: r0 % 8 < kRowsAt, or kRowsAt is 8
-      const uint32_t at = dst + i * kRowsAt * 128 + (turn ^ (((i * kRowsAt) & 7) << 4));
+      const uint32_t at = dst + (i * kRowsAt >> 3) * kGroup + ((i * kRowsAt) & 7) * 128 + row + (turn ^ (((i * kRowsAt) & 7) << 4));
       tc::sts128(at, h[0], h[1], h[2], h[3]);
       tc::sts128(at ^ 16, h[4], h[5], h[6], h[7]);
     }
@@ -508,7 +527,7 @@ struct AttnTc {
     const int c = tid % kChunks, src_lane = (tid & 31) / kChunks;
     const bool in_head = c * (F8 ? 16 : 8) < P.head_dim;
     const char* base = reinterpret_cast<const char*>(from);
-    const uint32_t dst = stage(pos) + (F8 ? L::kRaw + c * 16 : (c >> 3) * kHalf);
+    const uint32_t dst = stage(pos) + (F8 ? L::kRaw + c * 16 : 0);
     constexpr int kBatch = 8 < kChunks ? 8 : kChunks;  // shuffles ahead of copies: one after the other they would wait in one queue
 #pragma unroll
     for (int i0 = 0; i0 < kChunks; i0 += kBatch) {
@@ -520,7 +539,7 @@ struct AttnTc {
         const int r = row_of(tid, i0 + b);
         const bool take = in_head && at[b] >= 0;
         const char* src = take ? base + (at[b] + c * (F8 ? 16 : 8)) * (F8 ? 1 : 2) : base;
-        tc::cp16(F8 ? dst + r * DP : dst + r * 128 + (((c ^ r) & 7) << 4), src, take);
+        tc::cp16(F8 ? dst + r * DP : dst + kv_at(r, c), src, take);
       }
     }
     tc::cp_commit();
@@ -712,27 +731,27 @@ struct AttnTc {
     const uint32_t q = tc::desc_lo(smem + L::kQ0 + qbuf * L::kTile, 16), k = tc::desc_lo(stage(pos), 16);
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {  // 16 columns of head_dim: 32 bytes inside the 128-byte swizzle span
-      const uint32_t off = ((s >> 2) * kHalf + (s & 3) * 32) >> 4;
-      tc::mma_ss(tmem + w * kAttnTile, q + off, k + off, idesc, s > 0);
+      tc::mma_ss(tmem + w * kAttnTile, q + (((s >> 2) * kHalf + (s & 3) * 32) >> 4), tc::desc_hi(1024), k + (((s >> 2) * 1024 + (s & 3) * 32) >> 4),
+                 tc::desc_hi(kGroup), idesc, s > 0);
     }
     tc::commit(smem + L::kSFull + 8 * w);
   }
   // Waits for P as it goes.
   __device__ __forceinline__ bool issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc, uint32_t p_phase) const {
     constexpr uint32_t idesc = tc::instr_desc(DP, F8, true);
-    const uint32_t v = tc::desc_lo(stage(pos), kHalf);
+    const uint32_t v = tc::desc_lo(stage(pos), 1024);
     if (!QUAD) {
       if (!wait(smem + L::kPHalf + 8 * w, p_phase)) return false;
       tc::fence_after();
 #pragma unroll
       for (int s = 0; s < kAttnTile / 32; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
-        tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2048 >> 4), idesc, acc || s > 0);
+        tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2 * kGroup >> 4), tc::desc_hi(kGroup), idesc, acc || s > 0);
     }
     if (!wait(smem + L::kPFull + 8 * w, p_phase)) return false;
     tc::fence_after();
 #pragma unroll
     for (int s = QUAD ? 0 : kAttnTile / 32; s < kAttnTile / 16; ++s)
-      tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2048 >> 4), idesc, acc || s > 0);
+      tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2 * kGroup >> 4), tc::desc_hi(kGroup), idesc, acc || s > 0);
     return true;
   }
 
