@@ -42,10 +42,12 @@ struct AttnParams {
   float v_scale;
   int causal, window;
   float* lse;
-  // split results: part s of (row, head) at [(s*T + row)*heads_q + head]
-  float* part_o;  // [splits, T, heads_q, head_dim], normalised
-  float* part_z;  // [splits, T, heads_q], log2
-  int splits, chunk_tiles;
+  // where the CTAs of the tensor-core kernel start, and what they leave unfinished (see AttnItem)
+  int* starts;    // [grid][8]
+  float* part_o;  // [grid][2][part_rows][head_dim], normalised
+  float* part_z;  // [grid][2][part_rows], log2
+  int grid, part_rows;
+  int own;  // what an item costs beside its tiles, in tiles
   int tok_per_tile;     // tokens of a query tile: 128 / group
   int tiles_per_item;   // query tiles an item holds: 1 or 2
   int q_items;          // items per (sequence, key head)
@@ -190,17 +192,24 @@ __global__ void __launch_bounds__(kAttnGeneralThreads) attn_general_kernel(const
   }
 }
 
-// An item of the tensor-core kernel: query tiles of one sequence and key head, one part of its keys.
+// The tensor-core kernel's work.  A unit is the query tiles of one item of one sequence (tiles_per_item tiles from token
+// qt * tok_per_tile * tiles_per_item on) and one key head; it weighs as many key tiles as its rows see, and `own` more for its
+// first and last steps.  All units in a row -- sequences, their items, key heads fastest -- are cut into `grid` equal lengths, one for
+// each CTA, wherever the cuts fall: CTAs get the same number of tiles whatever the lengths of the sequences.  A CTA's
+// share of a unit is an item.  A unit that lies in one CTA is finished there; of one that is cut, each CTA leaves its part
+// (normalised rows and their log-sum) in one of its two slots -- 0 if the unit began before the CTA's share, 1 if it goes on
+// behind it -- and the join kernel puts them together.  A cut inside the first `own` of a unit leaves all of it to the later CTA.
 struct AttnItem {
   AttnSeq s;
-  int b, kvh, split;
-  int tok0;        // first new token
-  int j0, j1;      // key tiles of this part
-  int ulo, uhi;    // keys that some row of the item sees (whole item, not this part only)
-  int parts;       // parts the item's keys are cut into
+  int b, kvh;
+  int tok0;      // first new token
+  int j0, j1;    // key tiles of this item; none: j0 == j1
+  int ulo, uhi;  // keys that some row of the unit sees
+  bool whole;    // all of its unit
+  int slot;
 };
 
-// Key tiles of the item that starts at token tok0, over all parts: [J0, J1); also ulo, uhi.
+// Key tiles [J0, J1) of the unit that starts at token tok0, and its keys [ulo, uhi).
 __device__ __forceinline__ void attn_span(const AttnParams& P, const AttnSeq& s, int tok0, int& J0, int& J1, int& ulo, int& uhi) {
   int last = tok0 + P.tok_per_tile * P.tiles_per_item - 1;
   if (last >= s.n) last = s.n - 1;
@@ -213,30 +222,146 @@ __device__ __forceinline__ void attn_span(const AttnParams& P, const AttnSeq& s,
   J0 = ulo / kAttnTile;
   J1 = (uhi + kAttnTile - 1) / kAttnTile;
 }
-
-// Item number -> item; false: nothing to do (no such tokens, or a part past the end).  Later tokens first: under a
-// causal mask they see the most keys.  Key heads and parts run fastest.
-__device__ __forceinline__ bool attn_item(const AttnParams& P, int idx, AttnItem& it) {
-  it.split = idx % P.splits;
-  idx /= P.splits;
-  it.kvh = idx % P.heads_kv;
-  idx /= P.heads_kv;
-  it.b = idx % P.seqs;
-  const int qt = P.q_items - 1 - idx / P.seqs;
-  it.s = attn_seq(P, it.b);
-  it.tok0 = qt * P.tok_per_tile * P.tiles_per_item;
-  if (it.tok0 >= it.s.n) return false;
-  int J0, J1;
-  attn_span(P, it.s, it.tok0, J0, J1, it.ulo, it.uhi);
-  it.parts = (J1 - J0 + P.chunk_tiles - 1) / P.chunk_tiles;
-  if (it.split > 0 && it.split >= it.parts) return false;
-  it.j0 = J0 + it.split * P.chunk_tiles;
-  it.j1 = it.j0 + P.chunk_tiles < J1 ? it.j0 + P.chunk_tiles : J1;
-  return true;
+// What a unit of the sequence's item qt weighs; 0: the sequence has no such rows.
+__device__ __forceinline__ int attn_weight(const AttnParams& P, const AttnSeq& s, int qt) {
+  const int tok0 = qt * P.tok_per_tile * P.tiles_per_item;
+  if (tok0 >= s.n) return 0;
+  int J0, J1, ulo, uhi;
+  attn_span(P, s, tok0, J0, J1, ulo, uhi);
+  return J1 - J0 + P.own;
 }
 
-// Joins the parts of every (row, head): a warp each.
-constexpr int kAttnJoinThreads = 128;
+// Where a CTA's share starts: unit (b, qt, kvh), `off` tiles into it, `left` tiles long.
+struct AttnStart {
+  int b, qt, kvh, off, left;
+};
+
+// Found by the whole CTA (blockDim threads, a multiple of 32 up to 1024): a scan over the weights of (sequence, item).
+// scratch: 33 long longs of shared memory, free again when this returns; `out` is in shared memory too.
+__device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* scratch, AttnStart* out) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const long long n = (long long)P.seqs * P.q_items;
+  const long long per = (n + blockDim.x - 1) / blockDim.x;
+  const long long n0 = per * tid < n ? per * tid : n, n1 = n0 + per < n ? n0 + per : n;
+  long long sum = 0;
+  AttnSeq s;
+  int b = n1 > n0 ? (int)(n0 / P.q_items) : 0, qt = n1 > n0 ? (int)(n0 % P.q_items) : 0;
+  if (n1 > n0) s = attn_seq(P, b);
+  for (long long i = n0; i < n1; ++i) {
+    sum += attn_weight(P, s, qt);
+    if (++qt == P.q_items) {
+      qt = 0;
+      if (i + 1 < n1) s = attn_seq(P, ++b);
+    }
+  }
+  long long incl = sum;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, incl, off);
+    if (lane >= off) incl += v;
+  }
+  if (lane == 31) scratch[warp] = incl;
+  if (tid == 0) out->left = 0;
+  __syncthreads();
+  long long before = incl - sum, total = 0;
+  for (int w = 0; w < warps; ++w) {
+    if (w < warp) before += scratch[w];
+    total += scratch[w];
+  }
+  // shares of at least two tiles: fewer would be more parts than work
+  long long share = (total * P.heads_kv + gridDim.x - 1) / gridDim.x;
+  if (share < P.own + 2) share = P.own + 2;
+  const long long start = blockIdx.x * share, rest = total * P.heads_kv - start;
+  if (rest > 0 && start >= before * P.heads_kv && start < (before + sum) * P.heads_kv) {
+    b = (int)(n0 / P.q_items);
+    qt = (int)(n0 % P.q_items);
+    s = attn_seq(P, b);
+    long long at = before * P.heads_kv;
+    int w = attn_weight(P, s, qt);
+    while (start >= at + (long long)w * P.heads_kv) {
+      at += (long long)w * P.heads_kv;
+      if (++qt == P.q_items) {
+        qt = 0;
+        s = attn_seq(P, ++b);
+      }
+      w = attn_weight(P, s, qt);
+    }
+    AttnStart st = {b, qt, (int)((start - at) / w), (int)((start - at) % w), (int)(rest < share ? rest : share)};
+    if (st.off <= P.own) {
+      st.left += st.off;
+      st.off = 0;
+    }
+    *out = st;
+    int* rec = P.starts + blockIdx.x * 8;
+    rec[0] = st.b;
+    rec[1] = st.qt;
+    rec[2] = st.kvh;
+    rec[3] = st.off;
+    rec[4] = w;
+    rec[5] = (int)share;
+  } else if (tid == 0 && rest <= 0) {
+    P.starts[blockIdx.x * 8 + 3] = 0;  // nothing of this CTA's to join
+  }
+  __syncthreads();
+}
+
+// The items of a share, in order.
+struct AttnWalk {
+  AttnSeq s;
+  int b, qt, kvh, off, left;
+  int J0, J1, ulo, uhi;
+  bool have_seq, known;  // s is b's; the span is that of (b, qt)
+  __device__ __forceinline__ explicit AttnWalk(const AttnStart& st)
+      : b(st.b), qt(st.qt), kvh(st.kvh), off(st.off), left(st.left), have_seq(false), known(false) {}
+  __device__ __forceinline__ bool next(const AttnParams& P, AttnItem& it) {
+    if (left <= 0) return false;
+    const int per_item = P.tok_per_tile * P.tiles_per_item;
+    while (!known) {
+      if (!have_seq) s = attn_seq(P, b);
+      have_seq = true;
+      if (qt * per_item < s.n) {
+        attn_span(P, s, qt * per_item, J0, J1, ulo, uhi);
+        known = true;
+      } else {  // the rest of this sequence's items have no rows
+        qt = 0;
+        have_seq = false;
+        if (++b >= P.seqs) return false;  // cannot be: `left` counts what is there
+      }
+    }
+    const int w = J1 - J0 + P.own;
+    const int take = w - off < left ? w - off : left;
+    if (off == 0 && take <= P.own && take < w) {  // the next CTA does all of this unit
+      left = 0;
+      return false;
+    }
+    it.s = s;
+    it.b = b;
+    it.kvh = kvh;
+    it.tok0 = qt * per_item;
+    it.ulo = ulo;
+    it.uhi = uhi;
+    it.j0 = off > 0 ? J0 + off - P.own : J0;
+    it.j1 = J0 + off + take - P.own;
+    it.whole = off == 0 && take == w;
+    it.slot = off > 0 ? 0 : 1;
+    left -= take;
+    off = 0;
+    if (++kvh == P.heads_kv) {
+      kvh = 0;
+      known = false;
+      if (++qt == P.q_items) {
+        qt = 0;
+        ++b;
+        have_seq = false;
+        if (b >= P.seqs) left = 0;
+      }
+    }
+    return true;
+  }
+};
+
+// Puts the units together that were cut: CTA c does the one that c's share starts inside of, if that cut is the unit's first.
+constexpr int kAttnJoinThreads = 256;
 
 __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams P);
 

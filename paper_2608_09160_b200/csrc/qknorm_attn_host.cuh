@@ -418,7 +418,8 @@ bool encode_q(CUtensorMap* map, const AttnParams& P, int tokens) {
 struct AttnPlan {
   bool tc = false;
   int form = kAttnTwo;
-  int tok_per_tile = 1, tiles_per_item = 1, q_items = 1, splits = 1, chunk_tiles = 1;
+  int tok_per_tile = 1, tiles_per_item = 1, q_items = 1, grid = 1, part_rows = 0;
+  bool cuts = false;  // some unit may be cut between CTAs
 };
 
 AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, int window, int sms) {
@@ -432,45 +433,27 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   p.form = p.tiles_per_item == 2 ? kAttnTwo : max_q * group <= 32 ? kAttnQuad : kAttnOne;
   const int per_item = p.tok_per_tile * p.tiles_per_item;
   p.q_items = (max_q + per_item - 1) / per_item;
-  int64_t tiles = (max_keys + kAttnTile - 1) / kAttnTile;
+  int64_t tiles = (max_keys + kAttnTile - 1) / kAttnTile;  // of a unit, at most
   if (window > 0) {
     const int64_t span = ((int64_t)window + per_item - 1 + kAttnTile - 2) / kAttnTile + 1;
     if (span < tiles) tiles = span;
   }
-  if (tiles < 1) tiles = 1;
-  // Items that can have rows at all: a batch of T rows has no more than this many query pieces.
+  // One CTA per SM, and none for less than two tiles.  Units that a batch of T rows can have:
   int64_t pieces = (int64_t)p.q_items * seqs;
   if (T / per_item + seqs < pieces) pieces = T / per_item + seqs;
-  const int64_t items = pieces * heads_kv;
-  // How many parts.  A CTA takes every sms-th item; an item costs its tiles and about two more (its first and last steps), parts
-  // cost the join: a launch, about two tiles long, and writing and reading their fp32 rows.  The host knows the longest
-  // sequence only, so the time is estimated twice, all sequences as long as that, and lengths spread over the upper three quarters
-  // (0.65 of the parts have keys, and half a part more than the mean falls to the slowest CTA), and the mean of the two is what counts.
-  // Measured on one token of 16 sequences of 8000 to 32000 FP8 keys, 64 + 8 heads: 331 us in 1 part, 262 in 8; of 64
-  // sequences of 2000 to 8192 bf16 keys: 331 us in 1 part, 283 in 2.
-  const double own_tiles = 2.0, join_tiles = 2.0, tile_bytes = 9.6e6;  // a tile takes about 1.5 us
-  double best = 1e300;
-  for (int s = 1; s <= 64 && s <= tiles; ++s) {
-    const int64_t chunk = (tiles + s - 1) / s;
-    if ((tiles + chunk - 1) / chunk != s) continue;
-    const double n = (double)items * s, per_part = (double)chunk + own_tiles;
-    const double even = (double)((items * s + sms - 1) / sms) * per_part;
-    const double spread = fmax(1.0, 0.65 * n / sms + 0.5) * per_part;
-    const double join = s > 1 ? join_tiles + 8.0 * s * (double)T * heads_q * head_dim / tile_bytes : 0.0;
-    const double cost = 0.5 * (even + spread) + join;
-    if (cost < best) {
-      best = cost;
-      p.splits = s;
-      p.chunk_tiles = (int)chunk;
-    }
-  }
+  const double all = (double)pieces * heads_kv * (double)(tiles > 0 ? tiles : 1);
+  p.grid = all >= 2.0 * sms ? sms : (int)((all + 1.0) / 2.0);
+  p.cuts = tiles > 1;
+  p.part_rows = p.form == kAttnQuad ? 32 : kAttnTile * p.tiles_per_item;
   return p;
 }
 
-int64_t attn_workspace(const AttnPlan& p, int64_t T, int heads_q, int head_dim) {
-  if (p.splits <= 1) return 0;
-  const int64_t rows = (int64_t)p.splits * T * heads_q;
-  return ((rows * head_dim * 4 + 15) / 16) * 16 + rows * 4;
+// starts, then parts' rows, then their log-sums
+int64_t attn_starts_bytes(const AttnPlan& p) { return (int64_t)p.grid * 32; }
+int64_t attn_parts(const AttnPlan& p) { return p.cuts ? (int64_t)p.grid * 2 * p.part_rows : 0; }
+int64_t attn_workspace(const AttnPlan& p, int head_dim) {
+  if (!p.tc) return 0;
+  return (attn_starts_bytes(p) + attn_parts(p) * (head_dim + 1) * 4 + 15) / 16 * 16;
 }
 
 int check_attn_sizes(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
@@ -492,7 +475,7 @@ int run_attn_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, i
   const DeviceInfo* dev = nullptr;
   rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
-  *bytes = attn_workspace(plan_attn(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window, dev->sm_count), T, heads_q, head_dim);
+  *bytes = attn_workspace(plan_attn(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window, dev->sm_count), head_dim);
   return QKNORM_OK;
 }
 
@@ -525,8 +508,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
                        (!cache->e4m3 || cache->head_dim % 16 == 0);
   const char* force = env_str("QKNORM_FORCE_VARIANT");
   if (!aligned || (force && strcmp(force, "general") == 0)) plan.tc = false;
-  if (!plan.tc) plan.splits = 1;
-  const int64_t need = attn_workspace(plan, T, heads_q, cache->head_dim);
+  const int64_t need = attn_workspace(plan, cache->head_dim);
   if (need > 0) {
     if (!ws || ws_bytes < need || !aligned16(ws)) return QKNORM_ERR_SCRATCH;
     const Region w = flat(ws, (uintptr_t)need);
@@ -540,7 +522,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
       if (may_overlap(w, o)) return QKNORM_ERR_SCRATCH;
   }
   {
-    // q and out stay apart: with the keys in parts, a row of q may still be read after another part has written out
+    // q and out stay apart: copies of q's rows bring along rows of other sequences, whose results may be written already
     CallRegions c;
     c.own[c.outs] = -1;
     c.out[c.outs++] = Region{(uintptr_t)out, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_out * 2};
@@ -585,12 +567,14 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.tok_per_tile = plan.tok_per_tile;
   P.tiles_per_item = plan.tiles_per_item;
   P.q_items = plan.q_items;
-  P.splits = plan.splits;
-  P.chunk_tiles = plan.chunk_tiles;
+  P.grid = plan.grid;
+  P.part_rows = plan.part_rows;
+  P.own = env_int("QKNORM_OWN", plan.tiles_per_item == 1 ? 1 : 3);
   P.error = dev->ring_error;
-  if (plan.splits > 1) {
-    P.part_o = (float*)ws;
-    P.part_z = (float*)((char*)ws + ((int64_t)plan.splits * T * heads_q * cache->head_dim * 4 + 15) / 16 * 16);
+  if (plan.tc) {
+    P.starts = (int*)ws;
+    P.part_o = (float*)((char*)ws + attn_starts_bytes(plan));
+    P.part_z = P.part_o + attn_parts(plan) * cache->head_dim;
   }
 
   if (!plan.tc) {
@@ -632,17 +616,11 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);
   if (rc != QKNORM_OK) return rc;
-  const long long join_warps = (long long)seqs * P.max_q * heads_q;
-  const long long join_ctas = (join_warps + kAttnJoinThreads / 32 - 1) / (kAttnJoinThreads / 32);
-  if (plan.splits > 1 && join_ctas > 0x7fffffff) return QKNORM_ERR_SHAPE;
-  long long grid = (long long)plan.q_items * seqs * cache->heads * plan.splits;
-  if (grid > 0x7fffffff - dev->sm_count) return QKNORM_ERR_SHAPE;
-  if (grid > dev->sm_count) grid = dev->sm_count;
-  cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
+  cudaError_t e = launch_overlapped(fn, (unsigned)plan.grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_tc");
-  if (rc != QKNORM_OK || plan.splits <= 1) return rc;
-  e = launch_overlapped(attn_join_kernel_for(), (unsigned)join_ctas, (unsigned)kAttnJoinThreads, 0, stream, P);
+  if (rc != QKNORM_OK || !plan.cuts || plan.grid == 1) return rc;
+  e = launch_overlapped(attn_join_kernel_for(), (unsigned)plan.grid, (unsigned)kAttnJoinThreads, 0, stream, P);
   if (e != cudaSuccess) return set_cuda_error(e);
   return finish_launch("attn_tc");
 }

@@ -8,6 +8,7 @@
 //                multiple of 8 tokens they gather the rows themselves with cp.async
 //   warp 14      brings the query rows, by TMA where K and V come that way
 //   warp 12      issues every tcgen05.mma
+//   warp 15      says which items come next
 // Scores S_w = Q K^T land in TMEM (128 columns per warpgroup w).  The warpgroup reads them, keeps the running
 // maximum and sum in registers, writes P = 2^(c (s - m)) back over S in 16 bits, and O_w += P V takes P from
 // TMEM and V, keys by head_dim as it lies in the cache, as a transposed operand.  O_w stays in TMEM; it is rescaled only
@@ -202,8 +203,11 @@ struct AttnSmem {
   // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
   // round again only after the tensor warp has seen the scores of the item before last consumed.
   static constexpr int kQScale = kPoison + 16;
-  static constexpr int kNotes = kQScale + (F8 ? 512 : 0);  // [8 softmax warps][6] ints
-  static constexpr int kMlRows = kNotes + 192;             // [8 softmax warps][32] float2, one-tile forms: (m, l) of their parts
+  static constexpr int kItemSlots = F8 ? 2 : 4;              // items ahead of the slowest reader
+  static constexpr int kItems = kQScale + (F8 ? 512 : 0);    // [kItemSlots][16] ints, see put_item
+  static constexpr int kItemFull = kItems + 64 * kItemSlots;
+  static constexpr int kItemEmpty = kItemFull + 8 * kItemSlots;
+  static constexpr int kMlRows = kItemEmpty + 8 * kItemSlots;             // [8 softmax warps][32] float2, one-tile forms: (m, l) of their parts
   static constexpr int kBytes = kMlRows + 2048;
 };
 
@@ -255,7 +259,6 @@ struct AttnTc {
   const AttnMaps& maps;
   uint32_t smem;
   unsigned char* smem_ptr;
-  int items;
 
   __device__ __forceinline__ volatile int* abort_flag() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kAbort); }
   __device__ __forceinline__ volatile int* poison() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kPoison); }
@@ -290,6 +293,70 @@ struct AttnTc {
   __device__ __forceinline__ uint32_t empty(uint32_t pos) const { return smem + L::kEmpty + 8 * (pos % L::kStages); }
   __device__ __forceinline__ uint32_t stage(uint32_t pos) const { return smem + L::kRing + (pos % L::kStages) * L::kTile; }
 
+  // ---- items ----------------------------------------------------------------------------------------
+  // Warp 15 walks over the CTA's share and lays the items down for everybody else, some ahead.
+  static constexpr int kReaders = 8 + 4 + 1 + 1 + (TMA ? 1 : 0);  // softmax and tile warps, matrix thread, Q, producer
+
+  __device__ __forceinline__ volatile int* item_at(uint32_t i) const {
+    return reinterpret_cast<volatile int*>(smem_ptr + L::kItems) + (i % L::kItemSlots) * 16;
+  }
+  __device__ __forceinline__ void run_walk(const AttnStart& start) const {
+    AttnWalk walk(start);
+    AttnItem it;
+    for (uint32_t i = 0;; ++i) {
+      const bool more = walk.next(P, it);
+      if (i >= (uint32_t)L::kItemSlots &&
+          !wait(smem + L::kItemEmpty + 8 * (i % L::kItemSlots), ((i / L::kItemSlots) - 1) & 1))
+        return;
+      volatile int* at = item_at(i);
+      at[0] = more ? it.b : -1;
+      if (more) {
+        at[1] = it.s.row0;
+        at[2] = it.s.n;
+        at[3] = it.s.keys;
+        at[4] = (int)(it.s.pos0 & 0xffffffffll);
+        at[5] = (int)(it.s.pos0 >> 32);
+        at[6] = it.kvh;
+        at[7] = it.tok0;
+        at[8] = it.j0;
+        at[9] = it.j1;
+        at[10] = it.ulo;
+        at[11] = it.uhi;
+        at[12] = (it.whole ? 1 : 0) | it.slot << 1;
+      }
+      tc::arrive(smem + L::kItemFull + 8 * (i % L::kItemSlots));
+      if (!more) return;
+    }
+  }
+  __device__ __forceinline__ void get_item(uint32_t i, AttnItem& it) const {
+    const volatile int* at = item_at(i);
+    it.b = at[0];
+    it.s.row0 = at[1];
+    it.s.n = at[2];
+    it.s.keys = at[3];
+    it.s.pos0 = (long long)(uint32_t)at[4] | (long long)at[5] << 32;
+    it.kvh = at[6];
+    it.tok0 = at[7];
+    it.j0 = at[8];
+    it.j1 = at[9];
+    it.ulo = at[10];
+    it.uhi = at[11];
+    it.whole = at[12] & 1;
+    it.slot = at[12] >> 1;
+  }
+  __device__ __forceinline__ bool item_wait(uint32_t i) const {
+    return wait(smem + L::kItemFull + 8 * (i % L::kItemSlots), (i / L::kItemSlots) & 1);
+  }
+  __device__ __forceinline__ void item_done(uint32_t i) const { tc::arrive(smem + L::kItemEmpty + 8 * (i % L::kItemSlots)); }
+  // Item i for a whole warp, which keeps it in registers; false: there are no more, or leave.
+  __device__ __forceinline__ bool take_item(uint32_t i, AttnItem& it) const {
+    if (!__all_sync(0xffffffffu, item_wait(i))) return false;
+    get_item(i, it);
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) item_done(i);
+    return it.b >= 0;
+  }
+
   // ---- K and V tiles --------------------------------------------------------------------------------
   // V rows outside the item's keys have to be zeros (a weight of 0 times a NaN would be one), and the rows of a cut tile
   // looked through.  K may hold anything there: its scores are masked.
@@ -322,9 +389,9 @@ struct AttnTc {
       }
       return (int)page;
     };
-    for (int idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
-      AttnItem it;
-      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+    AttnItem it;
+    for (uint32_t n_item = 0; ok && take_item(n_item, it); ++n_item) {
+      if (it.j0 >= it.j1) continue;
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
       AttnTileRange r1 = r0;
       if (!ONE) r1 = attn_tile_range(P, it, 1);
@@ -437,9 +504,9 @@ struct AttnTc {
     const int lane = tid & 31;
     uint32_t pos = 0, raw_ph = 0, work_ph = 0;
     int count = 0;  // items with keys
-    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
-      AttnItem it;
-      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+    AttnItem it;
+    for (uint32_t n_item = 0; take_item(n_item, it); ++n_item) {
+      if (it.j0 >= it.j1) continue;
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
       AttnTileRange r1 = r0;
       if (!ONE) r1 = attn_tile_range(P, it, 1);
@@ -556,9 +623,14 @@ struct AttnTc {
     Loader ld;
     int count = 0;  // items with keys
     bool ok = true;
-    for (int idx = blockIdx.x; ok && idx < items; idx += gridDim.x) {
-      AttnItem it;
-      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+    AttnItem it;
+    for (uint32_t n_item = 0; ok; ++n_item) {
+      // the next item may have to wait for rows that wait for tiles that are pending here
+      if (!__all_sync(0xffffffffu, tc::test(smem + L::kItemFull + 8 * (n_item % L::kItemSlots), (n_item / L::kItemSlots) & 1)) &&
+          !(ok = flush(ld, tid)))
+        break;
+      if (!take_item(n_item, it)) break;
+      if (it.j0 >= it.j1) continue;
       const AttnTileRange r0 = attn_tile_range(P, it, 0);
       AttnTileRange r1 = r0;
       if (!ONE) r1 = attn_tile_range(P, it, 1);
@@ -673,9 +745,9 @@ struct AttnTc {
     const uint32_t all = 0xffffffffu;
     uint32_t qph = 0, qany = 0;  // bit w: phase of Q buffer w, and whether it was in use before
     int count = 0;
-    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
-      AttnItem it;
-      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+    AttnItem it;
+    for (uint32_t n_item = 0; take_item(n_item, it); ++n_item) {
+      if (it.j0 >= it.j1) continue;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         const AttnTileRange r = attn_tile_range(P, it, ONE ? 0 : w);
@@ -761,9 +833,13 @@ struct AttnTc {
   __device__ __forceinline__ void run_mma(uint32_t tmem) const {
     uint32_t pos = 0, count = 0;
     uint32_t qph = 0, pph = 0, oph = 0, oany = 0;  // bit w: phase of a barrier pair's w-th barrier; oany: O_w was in use before
-    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
-      AttnItem it;
-      if (!attn_item(P, idx, it) || it.j0 >= it.j1) continue;
+    AttnItem it;
+    for (uint32_t n_item = 0;; ++n_item) {
+      if (!item_wait(n_item)) return;
+      get_item(n_item, it);
+      item_done(n_item);
+      if (it.b < 0) return;
+      if (it.j0 >= it.j1) continue;
       const int nt = it.j1 - it.j0;
       if (ONE) {
         const int qb = count & 1;
@@ -853,15 +929,27 @@ struct AttnTc {
       tc::st16(o + k, r);
     }
   }
+  // Where a row's result goes: its place in out, or in the parts (place >= 0).
+  struct Dest {
+    long long row, place;
+    int head;
+  };
+  __device__ __forceinline__ Dest dest(const AttnItem& it, int w, int in_tile) const {
+    Dest d;
+    d.row = it.s.row0 + (long long)(it.tok0 + w * P.tok_per_tile + in_tile / P.group);
+    d.head = it.kvh * P.group + in_tile % P.group;
+    d.place = it.whole ? -1 : ((long long)blockIdx.x * 2 + it.slot) * P.part_rows + w * kAttnTile + in_tile;
+    return d;
+  }
   // 32 columns of the result of a row
-  __device__ __forceinline__ void store32(const float* x, long long row, int head, int split, int col) const {
-    if (P.splits > 1) {
-      float* o = P.part_o + (((long long)split * P.T + row) * P.heads_q + head) * P.head_dim + col;
+  __device__ __forceinline__ void store32(const float* x, const Dest& to, int col) const {
+    if (to.place >= 0) {
+      float* o = P.part_o + to.place * P.head_dim + col;
 #pragma unroll
       for (int e = 0; e < 32; e += 4)
         if (col + e < P.head_dim) *reinterpret_cast<float4*>(o + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
     } else {
-      uint16_t* o = P.out + row * P.ld_out + (long long)head * P.head_dim + col;
+      uint16_t* o = P.out + to.row * P.ld_out + (long long)to.head * P.head_dim + col;
 #pragma unroll
       for (int e = 0; e < 32; e += 8)
         if (col + e < P.head_dim)
@@ -871,46 +959,44 @@ struct AttnTc {
   }
   // N (2 or 4) columns of the result of a row
   template <int N>
-  __device__ __forceinline__ void store_few(const float* x, long long row, int head, int split, int col) const {
+  __device__ __forceinline__ void store_few(const float* x, const Dest& to, int col) const {
     if (col >= P.head_dim) return;  // head_dim is a multiple of 8, col of N
-    if (P.splits > 1) {
-      float* o = P.part_o + (((long long)split * P.T + row) * P.heads_q + head) * P.head_dim + col;
+    if (to.place >= 0) {
+      float* o = P.part_o + to.place * P.head_dim + col;
 #pragma unroll
       for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(o + e) = make_float2(x[e], x[e + 1]);
     } else {
-      uint16_t* o = P.out + row * P.ld_out + (long long)head * P.head_dim + col;
+      uint16_t* o = P.out + to.row * P.ld_out + (long long)to.head * P.head_dim + col;
 #pragma unroll
       for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(o + e) = bf_pack(x[e], x[e + 1]);
     }
   }
-  __device__ __forceinline__ void store_z(float z, long long row, int head, int split) const {
-    if (P.splits > 1) P.part_z[((long long)split * P.T + row) * P.heads_q + head] = z;
-    else if (P.lse != nullptr) P.lse[row * P.heads_q + head] = z * kLn2;
+  __device__ __forceinline__ void store_z(float z, const Dest& to) const {
+    if (to.place >= 0) P.part_z[to.place] = z;
+    else if (P.lse != nullptr) P.lse[to.row * P.heads_q + to.head] = z * kLn2;
   }
   // The rows of this warp again, one by one, each from the keys it sees and no others.
-  __device__ __forceinline__ void redo(int idx, int w, int first) const {
+  __device__ __forceinline__ void redo(const AttnItem& it, int w, int first) const {
     const int lane = threadIdx.x & 31;
-    AttnItem it;
-    if (!attn_item(P, idx, it)) return;
     const int tok0 = it.tok0 + w * P.tok_per_tile, rows = attn_tile_range(P, it, w).rows;
     for (int r = first; r < first + 32 && r < rows; ++r) {
-      const int i = tok0 + r / P.group, head = it.kvh * P.group + r % P.group;
-      const long long row = it.s.row0 + (long long)i;
+      const int i = tok0 + r / P.group;
+      const Dest to = dest(it, w, r);
       int lo = attn_lo(P, it.s, i), hi = attn_hi(P, it.s, i);
       lo = lo > it.j0 * kAttnTile ? lo : it.j0 * kAttnTile;
       hi = hi < it.j1 * kAttnTile ? hi : it.j1 * kAttnTile;
       float o[DP / 32], z;
-      if (F8) attn_row<IoE4m3, DP / 32>(P, it.b, row, head, lo, hi, o, z);
-      else attn_row<IoBf16, DP / 32>(P, it.b, row, head, lo, hi, o, z);
+      if (F8) attn_row<IoE4m3, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z);
+      else attn_row<IoBf16, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z);
 #pragma unroll
       for (int e = 0; e < DP / 32; ++e) {
         const int d = lane + 32 * e;
         if (d < P.head_dim) {
-          if (P.splits > 1) P.part_o[(((long long)it.split * P.T + row) * P.heads_q + head) * P.head_dim + d] = o[e];
-          else IoBf16::store(P.out, row * P.ld_out + (long long)head * P.head_dim + d, o[e] * P.v_scale);
+          if (to.place >= 0) P.part_o[to.place * P.head_dim + d] = o[e];
+          else IoBf16::store(P.out, to.row * P.ld_out + (long long)to.head * P.head_dim + d, o[e] * P.v_scale);
         }
       }
-      if (lane == 0) store_z(z, row, head, it.split);
+      if (lane == 0) store_z(z, to);
     }
   }
 
@@ -988,25 +1074,16 @@ struct AttnTc {
     uint32_t sph = 0, oph = 0, mlph = 0, ml_any = 0, pass = 0;
     int count = 0;
     const uint32_t all = 0xffffffffu;
-    // What the end of an item needs lies in shared memory during its tiles: registers are for the scores.
-    volatile int* note = reinterpret_cast<volatile int*>(smem_ptr + L::kNotes) + (threadIdx.x >> 5) * 6;
-    for (int idx = blockIdx.x; idx < items; idx += gridDim.x) {
+    // The item stays in shared memory and is read again at its end: registers are for the scores.
+    for (uint32_t n_item = 0;; ++n_item) {
+      if (!__all_sync(all, item_wait(n_item))) return;
       float m = kNegInf, l = 0.f, c = P.c;
       {
         AttnItem it;
-        if (!attn_item(P, idx, it)) continue;
+        get_item(n_item, it);
+        if (it.b < 0) return;
         const AttnTileRange rg = attn_tile_range(P, it, ONE ? 0 : w);
         const int tok0 = it.tok0 + (ONE ? 0 : w * P.tok_per_tile);
-        __syncwarp();
-        if (lane == 0) {
-          note[0] = it.s.row0;
-          note[1] = tok0;
-          note[2] = it.kvh | (rg.a < rg.b ? 1 << 30 : 0);
-          note[3] = it.split;
-          note[4] = rg.rows;
-          note[5] = it.j1 - it.j0;
-        }
-        __syncwarp();
         if (it.j0 < it.j1) {
           const int i = tok0 + wtid / P.group;
           const bool valid = wtid < rg.rows, busy = first_row < rg.rows;  // busy: some row of this warp is in use
@@ -1032,11 +1109,15 @@ struct AttnTc {
           }
         }
       }
-      const int tiles = note[5], rows = note[4], split = note[3], head = (note[2] & 0xfffff) * P.group + wtid % P.group;
-      const long long row = note[0] + (long long)(note[1] + wtid / P.group);
-      const bool valid = wtid < rows, busy = first_row < rows;
+      AttnItem it;
+      get_item(n_item, it);
+      const AttnTileRange rg = attn_tile_range(P, it, ONE ? 0 : w);
+      const int tiles = it.j1 - it.j0;
+      const bool valid = wtid < rg.rows, busy = first_row < rg.rows;
+      const Dest to = dest(it, ONE ? 0 : w, wtid);
+      const bool cut = to.place >= 0;
       if (!ONE) {
-        const bool own = (note[2] >> 30) != 0;  // some tile of the item was this warpgroup's
+        const bool own = rg.a < rg.b;  // some tile of the item was this warpgroup's
         if (own) {
           if (!__all_sync(all, wait(smem + L::kOFull + 8 * w, oph))) return;
           oph ^= 1;
@@ -1044,7 +1125,7 @@ struct AttnTc {
         }
         const bool again = tiles > 0 && poison()[count & 3] == count + 1;
         if (busy && !again) {
-          const float inv = l == 0.f ? 0.f : (P.splits > 1 ? 1.f : P.v_scale) / l;
+          const float inv = l == 0.f ? 0.f : (cut ? 1.f : P.v_scale) / l;
 #pragma unroll
           for (int k = 0; k < DP; k += 32) {
             uint32_t o[32];
@@ -1055,11 +1136,11 @@ struct AttnTc {
             }
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
-            if (valid && !(P.splits > 1 && l == 0.f)) store32(x, row, head, split, k);
+            if (valid && !(cut && l == 0.f)) store32(x, to, k);
           }
-          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), row, head, split);
+          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), to);
         }
-        if (again && busy) redo(idx, w, first_row);
+        if (again && busy) redo(it, w, first_row);
         if (own) {
           tc::fence_before();
           __syncwarp();
@@ -1070,9 +1151,8 @@ struct AttnTc {
           float x[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] = 0.f;
-          if (P.splits == 1)
-            for (int k = 0; k < DP; k += 32) store32(x, row, head, 0, k);
-          store_z(kNegInf, row, head, split);
+          for (int k = 0; k < DP; k += 32) store32(x, to, k);
+          store_z(kNegInf, to);
         }
       } else {
         // the parts of the same rows: one per warpgroup, QUAD one per warp
@@ -1113,8 +1193,8 @@ struct AttnTc {
           lt = fmaf(f[p], lp[p], lt);
         }
         const float z = lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt));
-        const float inv = lt == 0.f ? 0.f : (P.splits > 1 ? 1.f : P.v_scale) / lt;
-        const bool put = valid && !(P.splits > 1 && lt == 0.f);
+        const float inv = lt == 0.f ? 0.f : (cut ? 1.f : P.v_scale) / lt;
+        const bool put = valid && !(cut && lt == 0.f);
         const uint32_t o0 = tmem + lanes + 2 * kAttnTile, o1 = o0 + DP;
         if constexpr (QUAD) {
           // The item's Q tile is done with: its buffer takes the parts, kCols columns of all eight at a time.
@@ -1150,7 +1230,7 @@ struct AttnTc {
               for (int p = 0; p < 8; ++p) x[e] += scratch[(p * kCols + part * kMine + e) * 32 + lane];
               x[e] *= inv;
             }
-            if (put && !again) store_few<kMine>(x, row, head, split, k + part * kMine);
+            if (put && !again) store_few<kMine>(x, to, k + part * kMine);
             __syncwarp();
             if (lane == 0) tc::arrive(smem + L::kPass);
             if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
@@ -1159,8 +1239,8 @@ struct AttnTc {
           ptx::fence_proxy_async();  // the buffer's next writer is a copy
           __syncwarp();
           if (lane == 0) tc::arrive(smem + L::kQEmpty + 8 * (count & 1));
-          if (valid && part == 0 && !again) store_z(z, row, head, split);
-          if (again && part == 0) redo(idx, 0, 0);
+          if (valid && part == 0 && !again) store_z(z, to);
+          if (again && part == 0) redo(it, 0, 0);
         } else {
           if (busy && !again) {
 #pragma unroll
@@ -1177,11 +1257,11 @@ struct AttnTc {
                 if (two && f[1] != 0.f) v = fmaf(f[1], __uint_as_float(b[e]), v);
                 x[e] = lt == 0.f ? 0.f : v * inv;
               }
-              if (put) store32(x, row, head, split, k);
+              if (put) store32(x, to, k);
             }
-            if (valid && w == 0) store_z(z, row, head, split);
+            if (valid && w == 0) store_z(z, to);
           }
-          if (again && busy && w == 0) redo(idx, 0, first_row);
+          if (again && busy && w == 0) redo(it, 0, first_row);
         }
         tc::fence_before();
         __syncwarp();
@@ -1191,6 +1271,8 @@ struct AttnTc {
         }
       }
       if (tiles > 0) ++count;
+      __syncwarp();
+      if (lane == 0) item_done(n_item);
     }
   }
 };
@@ -1225,6 +1307,10 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     }
     ptx::mbar_init(smem + L::kMl, 8);
     ptx::mbar_init(smem + L::kMlFree, 8);
+    for (int i = 0; i < L::kItemSlots; ++i) {
+      ptx::mbar_init(smem + L::kItemFull + 8 * i, 1);
+      ptx::mbar_init(smem + L::kItemEmpty + 8 * i, K::kReaders);
+    }
     ptx::mbar_init(smem + L::kDrain, 1);
     ptx::mbar_init(smem + L::kWork, 4);
     ptx::mbar_init(smem + L::kPass, 8);
@@ -1243,8 +1329,12 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
   const uint32_t tmem = *reinterpret_cast<const volatile uint32_t*>(smem_raw + L::kTmem);
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  const int items = P.q_items * P.seqs * P.heads_kv * P.splits;  // the host has checked that it fits
-  const K k{P, maps, smem, smem_raw, items};
+  long long* scratch = reinterpret_cast<long long*>(smem_raw + L::kMlRows);  // nobody's yet
+  AttnStart* start = reinterpret_cast<AttnStart*>(smem_raw + L::kMlRows + 512);
+  attn_find_start(P, scratch, start);
+  const AttnStart mine = *start;
+  __syncthreads();
+  const K k{P, maps, smem, smem_raw};
   // 512 threads start with 128 registers each; 2 x 184 + 64 + 80 = 4 x 128
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
@@ -1267,6 +1357,8 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
       if (TMA) k.run_producer(threadIdx.x & 31);
     } else if (warp == 14) {
       k.run_q(threadIdx.x & 31);
+    } else if (threadIdx.x == 480) {
+      k.run_walk(mine);
     }
   }
   tc::fence_before();
