@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kAttnGeneralThreads) attn_general_kernel(const
 // each CTA, wherever the cuts fall: CTAs get the same number of tiles whatever the lengths of the sequences.  A CTA's
 // share of a unit is an item.  A unit that lies in one CTA is finished there; of one that is cut, each CTA leaves its part
 // (normalised rows and their log-sum) in one of its two slots -- 0 if the unit began before the CTA's share, 1 if it goes on
-// behind it -- and the join kernel puts them together.  A cut inside the first `own` of a unit leaves all of it to the later CTA.
+// behind it -- and the join kernel puts them together.  A cut within `snap` of a unit's end or start goes there (attn_snap).
 struct AttnItem {
   AttnSeq s;
   int b, kvh;
@@ -231,27 +231,38 @@ __device__ __forceinline__ int attn_weight(const AttnParams& P, const AttnSeq& s
   return J1 - J0 + P.own;
 }
 
-// Where a CTA's share starts: unit (b, qt, kvh), `off` tiles into it, `left` tiles long.
+// Where a CTA's share starts: unit (b, qt, kvh) of sequence s, `off` into it; and how long it is.
 struct AttnStart {
-  int b, qt, kvh, off, left;
+  AttnSeq s;
+  int b, qt, kvh, off;
+  int left;
 };
 
+// A cut costs its unit a part more and the join; it is worth that where shares are long.  Short shares (few tiles on many SMs) only
+// cut units of more than 16.
+__host__ __device__ __forceinline__ int attn_snap(long long share, int own) { return share >= 32 ? own : 8; }
+
 // Found by the whole CTA (blockDim threads, a multiple of 32 up to 1024): a scan over the weights of (sequence, item).
-// scratch: 33 long longs of shared memory, free again when this returns; `out` is in shared memory too.
+// scratch: 36 long longs of shared memory, free again when this returns; `out` is in shared memory too.
 __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* scratch, AttnStart* out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  const long long n = (long long)P.seqs * P.q_items;
-  const long long per = (n + blockDim.x - 1) / blockDim.x;
-  const long long n0 = per * tid < n ? per * tid : n, n1 = n0 + per < n ? n0 + per : n;
+  const int n = P.seqs * P.q_items;  // the host has checked that it fits
+  const int per = (n + blockDim.x - 1) / blockDim.x;
+  const int n0 = per * tid < n ? per * tid : n, n1 = n0 + per < n ? n0 + per : n;
   long long sum = 0;
-  AttnSeq s;
-  int b = n1 > n0 ? (int)(n0 / P.q_items) : 0, qt = n1 > n0 ? (int)(n0 % P.q_items) : 0;
-  if (n1 > n0) s = attn_seq(P, b);
-  for (long long i = n0; i < n1; ++i) {
-    sum += attn_weight(P, s, qt);
-    if (++qt == P.q_items) {
-      qt = 0;
-      if (i + 1 < n1) s = attn_seq(P, ++b);
+  AttnSeq s = {};
+  int b0 = 0, qt0 = 0;
+  if (n1 > n0) {
+    b0 = P.q_items == 1 ? n0 : n0 / P.q_items;
+    qt0 = n0 - b0 * P.q_items;
+    s = attn_seq(P, b0);
+    int b = b0, qt = qt0;
+    for (int i = n0; i < n1; ++i) {
+      sum += attn_weight(P, s, qt);
+      if (++qt == P.q_items) {
+        qt = 0;
+        if (i + 1 < n1) s = attn_seq(P, ++b);
+      }
     }
   }
   long long incl = sum;
@@ -261,24 +272,32 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
     if (lane >= off) incl += v;
   }
   if (lane == 31) scratch[warp] = incl;
-  if (tid == 0) out->left = 0;
+  if (tid == 0) scratch[33] = scratch[34] = -1;  // snapped end; snapped start
   __syncthreads();
   long long before = incl - sum, total = 0;
   for (int w = 0; w < warps; ++w) {
     if (w < warp) before += scratch[w];
     total += scratch[w];
   }
-  // shares of at least two tiles: fewer would be more parts than work
-  long long share = (total * P.heads_kv + gridDim.x - 1) / gridDim.x;
+  before *= P.heads_kv;
+  total *= P.heads_kv;
+  sum *= P.heads_kv;
+  long long share = total <= 0x7fffffff ? ((unsigned)total + gridDim.x - 1) / gridDim.x : (total + gridDim.x - 1) / gridDim.x;
   if (share < P.own + 2) share = P.own + 2;
-  const long long start = blockIdx.x * share, rest = total * P.heads_kv - start;
-  if (rest > 0 && start >= before * P.heads_kv && start < (before + sum) * P.heads_kv) {
-    b = (int)(n0 / P.q_items);
-    qt = (int)(n0 % P.q_items);
-    s = attn_seq(P, b);
-    long long at = before * P.heads_kv;
+  const int snap = attn_snap(share, P.own);
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {  // this CTA's cut, and the next one's
+    const long long cut = (blockIdx.x + which) * share;
+    if (cut >= total) {
+      if (which == 1 && tid == 0) scratch[33] = total;
+      continue;
+    }
+    if (cut < before || cut >= before + sum) continue;
+    int b = b0, qt = qt0;
+    if (per > 1) s = attn_seq(P, b);
+    long long at = before;
     int w = attn_weight(P, s, qt);
-    while (start >= at + (long long)w * P.heads_kv) {
+    while (cut >= at + (long long)w * P.heads_kv) {
       at += (long long)w * P.heads_kv;
       if (++qt == P.q_items) {
         qt = 0;
@@ -286,21 +305,37 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
       }
       w = attn_weight(P, s, qt);
     }
-    AttnStart st = {b, qt, (int)((start - at) / w), (int)((start - at) % w), (int)(rest < share ? rest : share)};
-    if (st.off <= P.own) {
-      st.left += st.off;
-      st.off = 0;
+    int kvh = 0;
+    for (; cut >= at + w; at += w) ++kvh;
+    int off = (int)(cut - at);
+    const int raw = off;
+    off = off <= snap ? 0 : w - off <= snap ? w : off;
+    scratch[33 + (which ^ 1)] = at + off;
+    if (which == 0) {
+      out->s = s;
+      out->b = b;
+      out->qt = qt;
+      out->kvh = kvh;
+      out->off = off;
+      if (P.starts != nullptr) {
+        int* rec = P.starts + blockIdx.x * 8;
+        const bool inside = off > 0 && off < w;
+        rec[0] = b;
+        rec[1] = qt;
+        rec[2] = kvh;
+        // parts that this cut and those behind it make, if it is the unit's first
+        rec[3] = inside && raw - share <= snap ? 2 + (int)((w - snap - 1 - raw) / share) : 0;
+      }
     }
-    *out = st;
-    int* rec = P.starts + blockIdx.x * 8;
-    rec[0] = st.b;
-    rec[1] = st.qt;
-    rec[2] = st.kvh;
-    rec[3] = st.off;
-    rec[4] = w;
-    rec[5] = (int)share;
-  } else if (tid == 0 && rest <= 0) {
-    P.starts[blockIdx.x * 8 + 3] = 0;  // nothing of this CTA's to join
+  }
+  __syncthreads();
+  if (tid == 0) {
+    if (scratch[34] < 0) {
+      out->left = 0;  // past the last unit
+      if (P.starts != nullptr) P.starts[blockIdx.x * 8 + 3] = 0;
+    } else {
+      out->left = (int)(scratch[33] - scratch[34]);
+    }
   }
   __syncthreads();
 }
@@ -312,51 +347,48 @@ struct AttnWalk {
   int J0, J1, ulo, uhi;
   bool have_seq, known;  // s is b's; the span is that of (b, qt)
   __device__ __forceinline__ explicit AttnWalk(const AttnStart& st)
-      : b(st.b), qt(st.qt), kvh(st.kvh), off(st.off), left(st.left), have_seq(false), known(false) {}
+      : s(st.s), b(st.b), qt(st.qt), kvh(st.kvh), off(st.off), left(st.left), have_seq(true), known(false) {}
   __device__ __forceinline__ bool next(const AttnParams& P, AttnItem& it) {
-    if (left <= 0) return false;
     const int per_item = P.tok_per_tile * P.tiles_per_item;
-    while (!known) {
-      if (!have_seq) s = attn_seq(P, b);
-      have_seq = true;
-      if (qt * per_item < s.n) {
+    while (left > 0 && b < P.seqs) {
+      if (!known) {
+        if (!have_seq) s = attn_seq(P, b);
+        have_seq = true;
+        if (qt * per_item >= s.n) {  // the rest of this sequence's items have no rows
+          qt = 0;
+          ++b;
+          have_seq = false;
+          continue;
+        }
         attn_span(P, s, qt * per_item, J0, J1, ulo, uhi);
         known = true;
-      } else {  // the rest of this sequence's items have no rows
-        qt = 0;
-        have_seq = false;
-        if (++b >= P.seqs) return false;  // cannot be: `left` counts what is there
       }
-    }
-    const int w = J1 - J0 + P.own;
-    const int take = w - off < left ? w - off : left;
-    if (off == 0 && take <= P.own && take < w) {  // the next CTA does all of this unit
-      left = 0;
-      return false;
-    }
-    it.s = s;
-    it.b = b;
-    it.kvh = kvh;
-    it.tok0 = qt * per_item;
-    it.ulo = ulo;
-    it.uhi = uhi;
-    it.j0 = off > 0 ? J0 + off - P.own : J0;
-    it.j1 = J0 + off + take - P.own;
-    it.whole = off == 0 && take == w;
-    it.slot = off > 0 ? 0 : 1;
-    left -= take;
-    off = 0;
-    if (++kvh == P.heads_kv) {
-      kvh = 0;
-      known = false;
-      if (++qt == P.q_items) {
-        qt = 0;
-        ++b;
-        have_seq = false;
-        if (b >= P.seqs) left = 0;
+      const int w = J1 - J0 + P.own;
+      const int take = w - off < left ? w - off : left;  // 0: the share starts at the end of this unit
+      it.s = s;
+      it.b = b;
+      it.kvh = kvh;
+      it.tok0 = qt * per_item;
+      it.ulo = ulo;
+      it.uhi = uhi;
+      it.j0 = off > 0 ? J0 + off - P.own : J0;
+      it.j1 = J0 + off + take - P.own;
+      it.whole = off == 0 && take == w;
+      it.slot = off > 0 ? 0 : 1;
+      left -= take;
+      off = 0;
+      if (++kvh == P.heads_kv) {
+        kvh = 0;
+        known = false;
+        if (++qt == P.q_items) {
+          qt = 0;
+          ++b;
+          have_seq = false;
+        }
       }
+      if (take > 0) return true;
     }
-    return true;
+    return false;
   }
 };
 

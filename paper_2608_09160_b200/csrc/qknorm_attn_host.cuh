@@ -419,6 +419,7 @@ struct AttnPlan {
   bool tc = false;
   int form = kAttnTwo;
   int tok_per_tile = 1, tiles_per_item = 1, q_items = 1, grid = 1, part_rows = 0;
+  int own = 1;
   bool cuts = false;  // some unit may be cut between CTAs
 };
 
@@ -441,15 +442,17 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   // One CTA per SM, and none for less than two tiles.  Units that a batch of T rows can have:
   int64_t pieces = (int64_t)p.q_items * seqs;
   if (T / per_item + seqs < pieces) pieces = T / per_item + seqs;
-  const double all = (double)pieces * heads_kv * (double)(tiles > 0 ? tiles : 1);
+  p.own = env_int("QKNORM_OWN", p.tiles_per_item == 1 ? 1 : 4);
+  const double all = (double)pieces * heads_kv * (double)(tiles + p.own);
   p.grid = all >= 2.0 * sms ? sms : (int)((all + 1.0) / 2.0);
-  p.cuts = tiles > 1;
+  // no cut can fall inside a unit that is shorter than twice the distance at which cuts move to its ends
+  p.cuts = tiles + p.own > 2 * attn_snap((int64_t)(all / p.grid) + 1, p.own);
   p.part_rows = p.form == kAttnQuad ? 32 : kAttnTile * p.tiles_per_item;
   return p;
 }
 
 // starts, then parts' rows, then their log-sums
-int64_t attn_starts_bytes(const AttnPlan& p) { return (int64_t)p.grid * 32; }
+int64_t attn_starts_bytes(const AttnPlan& p) { return p.cuts ? (int64_t)p.grid * 32 : 0; }
 int64_t attn_parts(const AttnPlan& p) { return p.cuts ? (int64_t)p.grid * 2 * p.part_rows : 0; }
 int64_t attn_workspace(const AttnPlan& p, int head_dim) {
   if (!p.tc) return 0;
@@ -458,7 +461,7 @@ int64_t attn_workspace(const AttnPlan& p, int head_dim) {
 
 int check_attn_sizes(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
                      int32_t window) {
-  if (seqs < 0 || T < 0 || T > 0x7fffffff || max_q < 0 || max_kv < 0 || max_kv > QKNORM_MAX_KEYS || window < 0) return QKNORM_ERR_SHAPE;
+  if (seqs < 0 || seqs > 0x3fffffff || T < 0 || T > 0x7fffffff || max_q < 0 || max_kv < 0 || max_kv > QKNORM_MAX_KEYS || window < 0) return QKNORM_ERR_SHAPE;
   if (head_dim < 1 || head_dim > QKNORM_MAX_HEAD_DIM) return QKNORM_ERR_HEADS;
   if (heads_q < 1 || heads_kv < 1 || heads_q % heads_kv != 0) return QKNORM_ERR_HEADS;
   if ((int64_t)heads_q * head_dim > kMaxDim) return QKNORM_ERR_SHAPE;
@@ -569,9 +572,9 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.q_items = plan.q_items;
   P.grid = plan.grid;
   P.part_rows = plan.part_rows;
-  P.own = env_int("QKNORM_OWN", plan.tiles_per_item == 1 ? 1 : 3);
+  P.own = plan.own;
   P.error = dev->ring_error;
-  if (plan.tc) {
+  if (plan.tc && plan.cuts) {
     P.starts = (int*)ws;
     P.part_o = (float*)((char*)ws + attn_starts_bytes(plan));
     P.part_z = P.part_o + attn_parts(plan) * cache->head_dim;
@@ -616,10 +619,11 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);
   if (rc != QKNORM_OK) return rc;
+  if ((int64_t)plan.q_items * seqs > 0x3fffffff) return QKNORM_ERR_SHAPE;
   cudaError_t e = launch_overlapped(fn, (unsigned)plan.grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_tc");
-  if (rc != QKNORM_OK || !plan.cuts || plan.grid == 1) return rc;
+  if (rc != QKNORM_OK || !plan.cuts) return rc;
   e = launch_overlapped(attn_join_kernel_for(), (unsigned)plan.grid, (unsigned)kAttnJoinThreads, 0, stream, P);
   if (e != cudaSuccess) return set_cuda_error(e);
   return finish_launch("attn_tc");

@@ -6,11 +6,9 @@ namespace qknorm {
 __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams P) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int* rec = P.starts + blockIdx.x * 8;
-  const int off = rec[3], share = rec[5];
-  // the share starts with a unit, or the unit was cut before (a cut inside its first `own` is none)
-  if (off <= P.own || off > share + P.own) return;
-  const int b = rec[0], qt = rec[1], kvh = rec[2], weight = rec[4];
-  const int parts = 1 + (weight - off + share - 1) / share;
+  const int parts = rec[3];
+  if (parts == 0) return;  // the share starts with a unit, or the unit was cut before
+  const int b = rec[0], qt = rec[1], kvh = rec[2];
   const AttnSeq s = attn_seq(P, b);
   const int tok0 = qt * P.tok_per_tile * P.tiles_per_item, lane = threadIdx.x & 31;
   // part p of row r lies with CTA blockIdx.x - 1 + p: in its slot 1 if it is the first, else in slot 0
