@@ -146,18 +146,18 @@ def _rotation(positions, inv_freq, T: int, interleaved: bool, mscale: float, dev
 def _cache(k_cache, v_cache, k_scale: float, v_scale: float, dev: int):
     """k_cache, v_cache [num_pages, page_size, heads, head_dim], any strides over pages, tokens and heads: (struct, heads,
     head_dim)."""
-    for t, what in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if (not isinstance(t, torch.Tensor) or t.dim() != 4 or t.get_device() != dev or t.dtype not in (_BF16, _F8)
-                or (t.shape[3] > 1 and t.stride(3) != 1)):
-            _refuse(_SHAPE, f"{what}: expected a 4-D bfloat16 or float8_e4m3fn tensor [pages, page_size, heads, head_dim] on cuda:{dev} "
-                            f"with unit stride in head_dim")
-    shape = k_cache.shape
-    if shape != v_cache.shape or k_cache.dtype is not v_cache.dtype:
-        _refuse(_SHAPE, "k_cache and v_cache differ in shape or type")
-    pages, page, heads, hd = shape
-    ks, vs = k_cache.stride(), v_cache.stride()
-    return _CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], pages, page, heads, hd,
-                       1 if k_cache.dtype is _F8 else 0, k_scale, v_scale), heads, hd
+    if isinstance(k_cache, torch.Tensor) and isinstance(v_cache, torch.Tensor):
+        dtype, shape = k_cache.dtype, k_cache.shape
+        if ((dtype is _BF16 or dtype is _F8) and v_cache.dtype is dtype and len(shape) == 4 and v_cache.shape == shape
+                and k_cache.get_device() == dev and v_cache.get_device() == dev):
+            pages, page, heads, hd = shape
+            kp, kt, kh, k1 = k_cache.stride()
+            vp, vt, vh, v1 = v_cache.stride()
+            if (k1 == 1 and v1 == 1) or hd == 1:
+                return _CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), kp, kt, kh, vp, vt, vh, pages, page, heads, hd,
+                                   1 if dtype is _F8 else 0, k_scale, v_scale), heads, hd
+    _refuse(_SHAPE, f"k_cache, v_cache: expected two bfloat16 or float8_e4m3fn tensors [pages, page_size, heads, head_dim] of one type and "
+                    f"shape on cuda:{dev}, with unit stride in head_dim")
 
 
 def _current(stream):
@@ -195,12 +195,18 @@ def qknorm_rope(q, k, positions, inv_freq, head_dim: int, out_q=None, out_k=None
     dq = dk = ldq = ldk = ldoq = ldok = 0
     if q is not None:
         pq, dq, ldq = _rows(q, T, "q", act, dev)
-        out_q = _empty((T, dq), act, q.device, stream) if out_q is None else out_q
-        poq, _, ldoq = _rows(out_q, T, "out_q", act, dev, dq)
+        if out_q is None:
+            out_q = _empty((T, dq), act, q.device, stream)
+            poq = out_q.data_ptr()
+        else:
+            poq, _, ldoq = _rows(out_q, T, "out_q", act, dev, dq)
     if k is not None:
         pk, dk, ldk = _rows(k, T, "k", act, dev)
-        out_k = _empty((T, dk), act, k.device, stream) if out_k is None else out_k
-        pok, _, ldok = _rows(out_k, T, "out_k", act, dev, dk)
+        if out_k is None:
+            out_k = _empty((T, dk), act, k.device, stream)
+            pok = out_k.data_ptr()
+        else:
+            pok, _, ldok = _rows(out_k, T, "out_k", act, dev, dk)
     _invoke(L.qknorm_rope_e4m3 if act is _F8 else L.qknorm_rope,
             (pq, pk, rot, T, dq, dk, int(head_dim), ldq, ldk, 1 if inverse else 0, poq, pok, ldoq, ldok), _current(stream),
             (q, k, positions, inv_freq, out_q, out_k))
@@ -235,8 +241,11 @@ def qknorm_fwd_append(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_c
         pq, dq, ldq = _rows(q, T, "q", _BF16, dev)
         if norm != NORM_NONE:
             pgq = _flat(gamma_q, (dq,), _BF16, "gamma_q", dev)
-        out_q = _empty((T, dq), _BF16, q.device, stream) if out_q is None else out_q
-        po, _, ldo = _rows(out_q, T, "out_q", _BF16, dev, dq)
+        if out_q is None:
+            out_q = _empty((T, dq), _BF16, q.device, stream)
+            po = out_q.data_ptr()
+        else:
+            po, _, ldo = _rows(out_q, T, "out_q", _BF16, dev, dq)
     rot = _rotation(positions, inv_freq, T, interleaved, mscale, dev)
     _invoke(L.qknorm_fwd_append, (pq, pk, pv, pgq, pgk, norm, eps, rot, pslots, cache, T, dq, ldq, ldk, ldv, po, ldo), _current(stream),
             (q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, out_q))
@@ -282,8 +291,11 @@ def qknorm_attn_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q
     if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
         _refuse(_SHAPE, f"block_table: expected an int32 CUDA tensor [{B}, pages per sequence]")
     ptable, cols, ldt = _rows(block_table, B, "block_table", torch.int32, dev)
-    out = _empty((T, dq), _BF16, q.device, stream) if out is None else out
-    po, _, ldo = _rows(out, T, "out", _BF16, dev, dq)
+    if out is None:
+        out = _empty((T, dq), _BF16, q.device, stream)
+        po, ldo = out.data_ptr(), 0
+    else:
+        po, _, ldo = _rows(out, T, "out", _BF16, dev, dq)
     plse = None if lse is None else _flat(lse, (T, hq), torch.float32, "lse", dev)
     if workspace is None:
         nbytes = _workspace(dev, B, T, max_q, max_kv, hq, heads, hd, window)

@@ -345,9 +345,26 @@ struct AttnWalk {
   AttnSeq s;
   int b, qt, kvh, off, left;
   int J0, J1, ulo, uhi;
+  int unit, step;        // step > 0: no shares, this CTA takes every step-th (sequence, key head), one item per sequence
   bool have_seq, known;  // s is b's; the span is that of (b, qt)
   __device__ __forceinline__ explicit AttnWalk(const AttnStart& st)
-      : s(st.s), b(st.b), qt(st.qt), kvh(st.kvh), off(st.off), left(st.left), have_seq(true), known(false) {}
+      : s(st.s), b(st.b), qt(st.qt), kvh(st.kvh), off(st.off), left(st.left), unit(0), step(0), have_seq(true), known(false) {}
+  __device__ __forceinline__ AttnWalk(int first, int every) : qt(0), off(0), left(0), unit(first), step(every) {}
+  __device__ __forceinline__ bool next_whole(const AttnParams& P, AttnItem& it) {
+    for (; unit < P.seqs * P.heads_kv; unit += step) {
+      it.b = unit / P.heads_kv;
+      it.s = attn_seq(P, it.b);
+      if (it.s.n <= 0) continue;
+      it.kvh = unit - it.b * P.heads_kv;
+      it.tok0 = 0;
+      attn_span(P, it.s, 0, it.j0, it.j1, it.ulo, it.uhi);
+      it.whole = true;
+      it.slot = 0;
+      unit += step;
+      return true;
+    }
+    return false;
+  }
   __device__ __forceinline__ bool next(const AttnParams& P, AttnItem& it) {
     const int per_item = P.tok_per_tile * P.tiles_per_item;
     while (left > 0 && b < P.seqs) {

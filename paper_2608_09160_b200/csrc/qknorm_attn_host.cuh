@@ -598,6 +598,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   memset(&maps, 0, sizeof(maps));
   int rows = kAttnTile;
   while (cache->page_size % rows != 0) rows /= 2;
+  if (cache->e4m3 && rows > 32) rows = 32;  // the rows that one warp widens lie together
   P.q_box_tokens = plan.form == kAttnQuad ? 32 / P.group : plan.tok_per_tile;
   bool tma = rows >= 8 && cache->num_pages > 0 && encode_q(&maps.q, P, P.q_box_tokens);
   if (tma) {
@@ -619,7 +620,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);
   if (rc != QKNORM_OK) return rc;
-  if ((int64_t)plan.q_items * seqs > 0x3fffffff) return QKNORM_ERR_SHAPE;
+  if ((int64_t)plan.q_items * seqs > 0x3fffffff || (int64_t)seqs * cache->heads > 0x3fffffff) return QKNORM_ERR_SHAPE;
   cudaError_t e = launch_overlapped(fn, (unsigned)plan.grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_tc");

@@ -175,7 +175,8 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, ui
 template <int DP, bool F8>
 struct AttnSmem {
   static constexpr int kTile = kAttnTile * DP * 2;  // a 16-bit tile of Q, K or V
-  static constexpr int kRaw = kAttnTile * DP;       // an FP8 tile; it lands in the upper half of its stage and is widened over itself
+  static constexpr int kRaw = kAttnTile * DP;       // an FP8 tile: 32 rows at a time land in the upper half of the place that
+                                                    // their fp16 form takes, and one warp widens them over themselves
   static constexpr int kStages = DP == 128 ? 5 : 10;
   static constexpr int kLag = kStages - 2;  // gathered tiles in flight behind the newest
   static constexpr int kQ0 = 0;             // two Q tiles
@@ -193,8 +194,7 @@ struct AttnSmem {
   static constexpr int kMlFree = kMl + 8;
   static constexpr int kDrain = kMlFree + 8;
   static constexpr int kRawFull = kDrain + 8;         // per stage: an FP8 tile, or a bf16 V tile that wants looking at, is there
-  static constexpr int kWork = kRawFull + 8 * kStages;  // the four warps that widen have all read the tile
-  static constexpr int kQRaw = kWork + 8;             // [2] FP8 cache: a bf16 Q tile is there
+  static constexpr int kQRaw = kRawFull + 8 * kStages;  // [2] FP8 cache: a bf16 Q tile is there
   static constexpr int kPass = kQRaw + 16;            // the softmax warps' steps through the join of an item
   static constexpr int kTmem = kPass + 8;             // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
@@ -251,6 +251,8 @@ struct AttnTc {
   // other.  K and V: groups of 8 rows, a group's halves side by side -- so that one TMA box can bring whole rows of a page.
   static constexpr int kHalf = kAttnTile * 128;
   static constexpr int kGroup = 8 * 2 * DP;  // bytes of 8 rows of K or V
+  // Where row r of a raw FP8 tile lies: with the 31 rows that the same warp widens, behind the start of their fp16 form.
+  __device__ __forceinline__ static uint32_t raw_at(int r) { return (r >> 5) * (64 * DP) + 32 * DP + (r & 31) * DP; }
   __device__ __forceinline__ static uint32_t kv_at(int r, int c) {  // row r, 16-byte piece c
     return (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (((c ^ r) & 7) << 4);
   }
@@ -300,11 +302,10 @@ struct AttnTc {
   __device__ __forceinline__ volatile int* item_at(uint32_t i) const {
     return reinterpret_cast<volatile int*>(smem_ptr + L::kItems) + (i % L::kItemSlots) * 16;
   }
-  __device__ __forceinline__ void run_walk(const AttnStart& start) const {
-    AttnWalk walk(start);
+  __device__ __forceinline__ void run_walk(AttnWalk walk) const {
     AttnItem it;
     for (uint32_t i = 0;; ++i) {
-      const bool more = walk.next(P, it);
+      const bool more = walk.step > 0 ? walk.next_whole(P, it) : walk.next(P, it);
       if (i >= (uint32_t)L::kItemSlots &&
           !wait(smem + L::kItemEmpty + 8 * (i % L::kItemSlots), ((i / L::kItemSlots) - 1) & 1))
         return;
@@ -375,7 +376,7 @@ struct AttnTc {
     const int halves = !F8 && P.box_kind == kBoxHalf ? DP / 64 : 1;
     const int boxes = (kAttnTile >> P.box_shift) * halves;
     const int box = lane / halves, half = lane % halves;
-    const uint32_t at = box * P.box_rows * (F8 ? DP : 2 * DP) + half * 1024;
+    const uint32_t at = F8 ? raw_at(box * P.box_rows) : box * P.box_rows * 2 * DP + half * 1024;
     uint32_t pos = 0, waiting_raw = 0, raw_ph = 0;  // bits by stage: its newest tile went to kRawFull; phase of kRawFull
     bool ok = true;
     // page and token of this lane's box of tile j; the page past the last one stands for zeros
@@ -407,7 +408,7 @@ struct AttnTc {
           if (round > 0 && !(ok = __all_sync(all, wait(empty(pos), (round - 1) & 1)))) break;
           const bool raw = F8 || (v == 1 && (job.blank || job.look));
           bar = raw ? smem + L::kRawFull + 8 * st : full(pos);
-          dst = stage(pos) + (F8 ? L::kRaw : 0);
+          dst = stage(pos);
           waiting_raw = (waiting_raw & ~(1u << st)) | (raw ? 1u << st : 0u);
           if (raw) raw_ph ^= 1u << st;
           if (lane == 0) {
@@ -464,45 +465,48 @@ struct AttnTc {
     return bad;
   }
 
-  // The FP8 tile in the upper half of a stage (row r at + r * DP) to fp16 over the whole stage: all four warps have read
-  // their rows before any of them writes.  CARE: rows outside [from, to) become zeros, the others are looked through for NaN.
+  // This warp's 32 rows of an FP8 tile to fp16, over themselves: all read before any is written.  CARE: rows outside [from, to)
+  // become zeros, the others are looked through for NaN.
   template <bool CARE>
-  __device__ __forceinline__ bool widen(uint32_t tile_at, int tid, uint32_t& work_ph, int from, int to, bool& bad) const {
+  __device__ __forceinline__ bool widen(uint32_t tile_at, int tid, int from, int to) const {
     const int c = tid % kChunks, r0 = row_of(tid, 0);
-    const uint32_t src = tile_at + L::kRaw + r0 * DP + c * 16;
-    // piece 2c of row r0; the next rows of this thread are kRowsAt further each, which is 4 or 8: half a group or one
-    const uint32_t dst = tile_at + kv_at(r0 & ~7, 2 * c & ~7), row = (r0 & 7) * 128, turn = (((2 * c) ^ r0) & 7) << 4;
+    const uint32_t src = tile_at + raw_at(r0) + c * 16;
+    // Pieces 2c and 2c + 1 of row r0; the next rows of this thread are kRowsAt further each, which is 4 or 8: half a group or one.
+    // With 128 columns a quarter of a warp writes one whole row, whose halves lie on the same banks: the upper half writes its odd
+    // pieces first.
+    const bool odd_first = DP == 128 && (c & 4) != 0;
+    const uint32_t dst = tile_at + kv_at(r0 & ~7, 2 * c & ~7), row = (r0 & 7) * 128;
+    const uint32_t turn = (((2 * c) ^ r0) & 7) << 4 ^ (odd_first ? 16 : 0);
+    bool bad = false;
     uint4 v[kChunks];
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) v[i] = ptx::lds128(src + i * kRowsAt * DP);
     __syncwarp();
-    if ((tid & 31) == 0) tc::arrive(smem + L::kWork);
-    if (!__all_sync(0xffffffffu, wait(smem + L::kWork, work_ph))) return false;
-    work_ph ^= 1;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       if (CARE && (r0 + i * kRowsAt < from || r0 + i * kRowsAt >= to)) v[i] = make_uint4(0u, 0u, 0u, 0u);
       uint32_t h[8];
-      e4m3x4_to_f16x2(v[i].x, h[0], h[1]);
-      e4m3x4_to_f16x2(v[i].y, h[2], h[3]);
-      e4m3x4_to_f16x2(v[i].z, h[4], h[5]);
-      e4m3x4_to_f16x2(v[i].w, h[6], h[7]);
+      e4m3x4_to_f16x2(odd_first ? v[i].z : v[i].x, h[0], h[1]);
+      e4m3x4_to_f16x2(odd_first ? v[i].w : v[i].y, h[2], h[3]);
+      e4m3x4_to_f16x2(odd_first ? v[i].x : v[i].z, h[4], h[5]);
+      e4m3x4_to_f16x2(odd_first ? v[i].y : v[i].w, h[6], h[7]);
       if (CARE) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) bad |= odd_f16(h[e]);
       }
+      // the swizzle of row r0 + i * kRowsAt differs from row r0's by a constant: r0 % 8 < kRowsAt, or kRowsAt is 8
       const uint32_t at = dst + (i * kRowsAt >> 3) * kGroup + ((i * kRowsAt) & 7) * 128 + row + (turn ^ (((i * kRowsAt) & 7) << 4));
       tc::sts128(at, h[0], h[1], h[2], h[3]);
       tc::sts128(at ^ 16, h[4], h[5], h[6], h[7]);
     }
-    return true;
+    return bad;
   }
 
   // Warps 8-11 behind TMA copies.
   __device__ __forceinline__ void run_workers(int tid) const {
     const uint32_t all = 0xffffffffu;
     const int lane = tid & 31;
-    uint32_t pos = 0, raw_ph = 0, work_ph = 0;
+    uint32_t pos = 0, raw_ph = 0;
     int count = 0;  // items with keys
     AttnItem it;
     for (uint32_t n_item = 0; take_item(n_item, it); ++n_item) {
@@ -516,12 +520,10 @@ struct AttnTc {
           const VJob job = v_job(it, r0, r1, j);
           const uint32_t st = pos % L::kStages;
           if (!__all_sync(all, wait(smem + L::kRawFull + 8 * st, (pos / L::kStages) & 1))) return;
-          bool bad = false;
           if ((n & 1) && (job.blank || job.look)) {
-            if (!widen<true>(stage(pos), tid, work_ph, it.ulo - k0, it.uhi - k0, bad)) return;
-            if (bad && job.look) poison()[count & 3] = count + 1;
-          } else if (!widen<false>(stage(pos), tid, work_ph, 0, 0, bad)) {
-            return;
+            if (widen<true>(stage(pos), tid, it.ulo - k0, it.uhi - k0) && job.look) poison()[count & 3] = count + 1;
+          } else {
+            widen<false>(stage(pos), tid, 0, 0);
           }
           signal(full(pos), lane);
         }
@@ -548,7 +550,6 @@ struct AttnTc {
   struct Loader {
     uint32_t pos = 0;    // tiles issued
     int pending = 0;     // issued, not handed over
-    uint32_t work_ph = 0;
     int look_item = -1;  // the newest pending tile is V and cut: look through it, name this item
   };
 
@@ -559,8 +560,7 @@ struct AttnTc {
     const bool look = ld.look_item >= 0 && ld.pending == 1;
     bool bad = false;
     if constexpr (F8) {
-      if (!(look ? widen<true>(stage(pos), tid, ld.work_ph, 0, kAttnTile, bad) : widen<false>(stage(pos), tid, ld.work_ph, 0, 0, bad)))
-        return false;
+      bad = look ? widen<true>(stage(pos), tid, 0, kAttnTile) : widen<false>(stage(pos), tid, 0, 0);
     } else if (look) {
       bad = inspect(stage(pos), tid, 0, kAttnTile, false, true);
     }
@@ -594,7 +594,7 @@ struct AttnTc {
     const int c = tid % kChunks, src_lane = (tid & 31) / kChunks;
     const bool in_head = c * (F8 ? 16 : 8) < P.head_dim;
     const char* base = reinterpret_cast<const char*>(from);
-    const uint32_t dst = stage(pos) + (F8 ? L::kRaw + c * 16 : 0);
+    const uint32_t dst = stage(pos) + (F8 ? c * 16 : 0);
     constexpr int kBatch = 8 < kChunks ? 8 : kChunks;  // shuffles ahead of copies: one after the other they would wait in one queue
 #pragma unroll
     for (int i0 = 0; i0 < kChunks; i0 += kBatch) {
@@ -606,7 +606,7 @@ struct AttnTc {
         const int r = row_of(tid, i0 + b);
         const bool take = in_head && at[b] >= 0;
         const char* src = take ? base + (at[b] + c * (F8 ? 16 : 8)) * (F8 ? 1 : 2) : base;
-        tc::cp16(F8 ? dst + r * DP : dst + kv_at(r, c), src, take);
+        tc::cp16(dst + (F8 ? raw_at(r) : kv_at(r, c)), src, take);
       }
     }
     tc::cp_commit();
@@ -1312,7 +1312,6 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
       ptx::mbar_init(smem + L::kItemEmpty + 8 * i, K::kReaders);
     }
     ptx::mbar_init(smem + L::kDrain, 1);
-    ptx::mbar_init(smem + L::kWork, 4);
     ptx::mbar_init(smem + L::kPass, 8);
     *reinterpret_cast<volatile int*>(smem_raw + L::kAbort) = 0;
     for (int i = 0; i < 4; ++i) reinterpret_cast<volatile int*>(smem_raw + L::kPoison)[i] = 0;
@@ -1329,11 +1328,15 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
   const uint32_t tmem = *reinterpret_cast<const volatile uint32_t*>(smem_raw + L::kTmem);
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  long long* scratch = reinterpret_cast<long long*>(smem_raw + L::kMlRows);  // nobody's yet
-  AttnStart* start = reinterpret_cast<AttnStart*>(smem_raw + L::kMlRows + 512);
-  attn_find_start(P, scratch, start);
-  const AttnStart mine = *start;
-  __syncthreads();
+  AttnWalk walk(blockIdx.x, gridDim.x);
+  // Whole units, one per sequence and key head: nothing to work out beforehand, which takes two microseconds.
+  if (!K::ONE || P.starts != nullptr) {
+    long long* scratch = reinterpret_cast<long long*>(smem_raw + L::kMlRows);  // nobody's yet
+    AttnStart* start = reinterpret_cast<AttnStart*>(smem_raw + L::kMlRows + 512);
+    attn_find_start(P, scratch, start);
+    walk = AttnWalk(*start);
+    __syncthreads();
+  }
   const K k{P, maps, smem, smem_raw};
   // 512 threads start with 128 registers each; 2 x 184 + 64 + 80 = 4 x 128
   if (warp < 8) {
@@ -1358,7 +1361,7 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     } else if (warp == 14) {
       k.run_q(threadIdx.x & 31);
     } else if (threadIdx.x == 480) {
-      k.run_walk(mine);
+      k.run_walk(walk);
     }
   }
   tc::fence_before();
