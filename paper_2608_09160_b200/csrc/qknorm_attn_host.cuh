@@ -169,7 +169,7 @@ int launch_rope(RopeParams& R, int elem_bytes, int cache_bytes, int norm, bool v
       // short rows: several tokens share a CTA of about 128 threads
       R.tokens_per_cta = R.T >= 2 * dev->sm_count && R.threads_per_token < 128 ? 128 / R.threads_per_token : 1;
       const int smem = R.tokens_per_cta * R.rot_dim * (int)sizeof(float2) / 2;
-      RopeKernel fn = rope_kernel_for(elem_bytes, cache_bytes, norm, upt, R.tokens_per_cta * R.threads_per_token);
+      RopeKernel fn = rope_kernel_for(elem_bytes, cache_bytes, norm, R.interleaved != 0, upt, R.tokens_per_cta * R.threads_per_token);
       const long long grid = (R.T + R.tokens_per_cta - 1) / R.tokens_per_cta;
       if (grid <= 0x7fffffff) {
         const cudaError_t e = launch_overlapped(fn, (unsigned)grid, (unsigned)(R.tokens_per_cta * R.threads_per_token), (size_t)smem, stream, R);

@@ -139,7 +139,7 @@ __device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot
 
 // IO: storage of q, k, v and out_q.  CIO: storage of the cache.  UPT: 16-element units per thread.  MAXT: the largest CTA;
 // CTAs of up to 256 threads get 80 registers a thread, which four units need.
-template <class IO, class CIO, int NORM, bool CACHE, int UPT, int MAXT>
+template <class IO, class CIO, int NORM, bool CACHE, bool INTER, int UPT, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const __grid_constant__ RopeParams R) {
   extern __shared__ float4 cs_all[];  // [tokens_per_cta][4][rot_dim/16]: (c, c, s, s) of pairs 8j+2e, 8j+2e+1 at [e][j]
   __shared__ float red[32][2];        // per warp: sum of squares of Q, of K
@@ -151,14 +151,18 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
   float4* cs = cs_all + slot_of_token * 4 * r16;
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
+  const char* row_q = reinterpret_cast<const char*>(R.q.x) + t * R.q.ldx * IO::kBytes;
+  const char* row_k = reinterpret_cast<const char*>(R.k.x) + t * R.k.ldx * IO::kBytes;
+  const char* row_v = reinterpret_cast<const char*>(R.v.x) + t * R.v.ldx * IO::kBytes;
   Chunk8<IO> u[UPT][2];
+  int head[UPT];
   int off[UPT];   // of the unit's first chunk in its row
   int side[UPT];  // 0 q, 1 k, 2 v, -1 none
   const int j = tid & ((1 << R.log_lph) - 1);  // which 16 elements of its head; threads_per_token is a multiple of 32, so the
                                                // same in every unit of the thread
   const bool turns = j < r16;
-  const int c0 = turns && !R.interleaved ? 8 * j : 16 * j;
-  const int step = turns && !R.interleaved ? 8 * r16 : 8;  // from the first chunk to the second
+  const int c0 = turns && !INTER ? 8 * j : 16 * j;
+  const int step = turns && !INTER ? 8 * r16 : 8;  // from the first chunk to the second
 #pragma unroll
   for (int i = 0; i < UPT; ++i) {
     const int s = tid + i * R.threads_per_token;
@@ -175,10 +179,10 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
         }
       }
     }
+    head[i] = h;
     off[i] = h * R.head_dim + c0;
     if (side[i] >= 0) {
-      const RopeSide& A = side[i] == 0 ? R.q : (!CACHE || side[i] == 1) ? R.k : R.v;
-      const char* row = reinterpret_cast<const char*>(A.x) + t * A.ldx * IO::kBytes;
+      const char* row = side[i] == 0 ? row_q : (!CACHE || side[i] == 1) ? row_k : row_v;
       u[i][0].load(row, off[i]);
       u[i][1].load(row, off[i] + step);
     }
@@ -187,6 +191,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
   if (CACHE && live) {
     cslot = R.slots[t];
     if (cslot >= R.num_slots) cslot = -1;
+  }
+  long long slot_k = 0, slot_v = 0;  // where the token's slot starts in the pools
+  if (CACHE && cslot >= 0) {
+    slot_k = cache_at(R.ck, cslot, R.page_size, R.page_shift);
+    slot_v = cache_at(R.cv, cslot, R.page_size, R.page_shift);
   }
   if (live && r16 > 0) {
     const long long pos = R.positions[t];
@@ -267,7 +276,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float4 f = cs[e * r16 + j];  // pairs 8j+2e, 8j+2e+1
-          if (R.interleaved) {               // pairs 8j..8j+3 lie in a, 8j+4..8j+7 in b
+          if constexpr (INTER) {             // pairs 8j..8j+3 lie in a, 8j+4..8j+7 in b
             float2& p = e < 2 ? a[2 * e] : b[2 * e - 4];
             float2& q = e < 2 ? a[2 * e + 1] : b[2 * e - 3];
             p = __ffma2_rn(make_float2(p.y, p.x), make_float2(-f.z, f.z), __fmul2_rn(p, make_float2(f.x, f.x)));
@@ -283,8 +292,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const _
     if (to_cache) {
       if (cslot < 0) continue;
       const CacheSide& C = side[i] == 1 ? R.ck : R.cv;
-      const int h = (off[i] - c0) / R.head_dim;
-      const long long at = cache_at(C, cslot, R.page_size, R.page_shift) + h * C.head + c0;
+      const long long at = (side[i] == 1 ? slot_k : slot_v) + head[i] * C.head + c0;
       Chunk8<CIO> o0, o1;
       if constexpr (CIO::kBytes == 1 || IO::kBytes == 1) {
         const float2 k = make_float2(C.inv_scale, C.inv_scale);
@@ -404,7 +412,7 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
 typedef void (*RopeKernel)(const RopeParams);
 typedef void (*RopeGeneralKernel)(const RopeParams, int);
 // in qknorm_rope_inst.cu; upt 1 or 4, threads: of the CTA; cache_bytes 0 = no cache
-RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, int upt, int threads);
+RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, bool interleaved, int upt, int threads);
 RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes);
 
 }  // namespace qknorm
