@@ -137,10 +137,11 @@ __device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot
   return page * c.page + (slot - page * page_size) * c.token;
 }
 
-// IO: storage of q, k, v and out_q.  CIO: storage of the cache.  UPT: 16-element units per thread.  MAXT: the largest CTA;
-// CTAs of up to 256 threads get 80 registers a thread, which four units need.
+// IO: storage of q, k, v and out_q.  CIO: storage of the cache.  INTER: interleaved pairs.  UPT: 16-element units per thread.
+// MAXT: the largest CTA; CTAs of up to 256 threads get 80 registers a thread, which four units need -- 64 with an FP8 cache,
+// whose conversions want more warps instead (8191 tokens of 8192 + 1024 + 1024: 58 us against 64; bf16 cache: 84 against 83).
 template <class IO, class CIO, int NORM, bool CACHE, bool INTER, int UPT, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) rope_kernel(const __grid_constant__ RopeParams R) {
+__global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes == 1 ? 4 : 3) rope_kernel(const __grid_constant__ RopeParams R) {
   extern __shared__ float4 cs_all[];  // [tokens_per_cta][4][rot_dim/16]: (c, c, s, s) of pairs 8j+2e, 8j+2e+1 at [e][j]
   __shared__ float red[32][2];        // per warp: sum of squares of Q, of K
   const int slot_of_token = threadIdx.x / R.threads_per_token;
