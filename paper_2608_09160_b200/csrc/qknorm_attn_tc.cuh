@@ -1005,23 +1005,35 @@ struct AttnTc {
   // Two forms: the first half of P is announced while the second is computed.
   __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
                                        float& l, uint32_t p_half) const {
-    constexpr int N = QUAD ? kAttnTile / 4 : kAttnTile;
+    // The first half stays in registers from the maximum to the exponentials; the second is read again when the first is half
+    // done, so that a thread never holds more than 128 scores and nothing else.
+    constexpr int N = QUAD ? kAttnTile / 4 : kAttnTile / 2;
     const int first_col = QUAD ? (int)((threadIdx.x >> 5) & 3) * N : 0;
-    float s[N];
+    float s[N], t[QUAD ? 1 : N];
+    auto mask = [&](float* x, int col) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] = col + k >= from && col + k < to ? x[k] : kNegInf;
+    };
 #pragma unroll
     for (int k = 0; k < N; k += 32) tc::ld32(s_addr + first_col + k, reinterpret_cast<uint32_t*>(s) + k);
+    if constexpr (!QUAD) {
+#pragma unroll
+      for (int k = 0; k < N; k += 32) tc::ld32(s_addr + N + k, reinterpret_cast<uint32_t*>(t) + k);
+    }
     tc::wait_ld();
     if (masked) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) s[k] = first_col + k >= from && first_col + k < to ? s[k] : kNegInf;
+      mask(s, first_col);
+      if constexpr (!QUAD) mask(t, N);
     }
-    float mx[4] = {s[0], s[1], s[2], s[3]};
+    float mx[8];
 #pragma unroll
-    for (int k = 4; k < N - 4; k += 8) {
+    for (int e = 0; e < 8; ++e) mx[e] = QUAD ? s[e] : fmaxf(s[e], t[e]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mx[e] = tc::max3(mx[e], s[k + e], s[k + 4 + e]);
+    for (int k = 8; k < N; k += 8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx[e] = QUAD ? fmaxf(mx[e], s[k + e]) : tc::max3(mx[e], s[k + e], t[QUAD ? 0 : k + e]);
     }
-    const float mn = fmaxf(tc::max3(mx[0], mx[1], s[N - 4]), tc::max3(mx[2], tc::max3(mx[3], s[N - 3], s[N - 2]), s[N - 1]));
+    const float mn = tc::max3(tc::max3(mx[0], mx[1], mx[2]), tc::max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
     // m is the maximum that the exponents are taken against; it follows the true one when that is 2^8 ahead
     const bool grow = mn > m && (m == kNegInf || (mn - m) * c > 8.f);
     if (__any_sync(0xffffffffu, grow)) {
@@ -1035,25 +1047,31 @@ struct AttnTc {
     const float mc = m == kNegInf ? 0.f : m * c;
     const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-    for (int h = 0; h < N / 32; ++h) {
+    auto weights = [&](const float* x, int col) {  // 32 columns from `col`
       uint32_t p[16];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int k = h * 32 + 2 * e;
-        float2 x = __ffma2_rn(make_float2(s[k], s[k + 1]), c2, mc2);
-        x.x = tc::ex2(x.x);
-        x.y = tc::ex2(x.y);
-        sum[e & 1] = __fadd2_rn(sum[e & 1], x);
-        p[e] = F8 ? tc::pack_f16(x.x, x.y) : bf_pack(x.x, x.y);
+        float2 y = __ffma2_rn(make_float2(x[2 * e], x[2 * e + 1]), c2, mc2);
+        y.x = tc::ex2(y.x);
+        y.y = tc::ex2(y.y);
+        sum[e & 1] = __fadd2_rn(sum[e & 1], y);
+        p[e] = F8 ? tc::pack_f16(y.x, y.y) : bf_pack(y.x, y.y);
       }
-      tc::st16(s_addr + first_col / 2 + h * 16, p);
-      if (!QUAD && h == 1) {
-        tc::wait_st();
-        tc::fence_before();
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) tc::arrive(p_half);
-      }
+      tc::st16(s_addr + col / 2, p);
+    };
+    weights(s, first_col);
+    if constexpr (!QUAD) {
+#pragma unroll
+      for (int k = 0; k < N; k += 32) tc::ld32(s_addr + N + k, reinterpret_cast<uint32_t*>(t) + k);
+      weights(s + 32, 32);
+      tc::wait_st();
+      tc::fence_before();
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) tc::arrive(p_half);
+      tc::wait_ld();
+      if (masked) mask(t, N);
+      weights(t, 64);
+      weights(t + 32, 96);
     }
     if (QUAD) {  // the other quarters' keys are not this warp's: zeros in their place
       uint32_t none[16];
