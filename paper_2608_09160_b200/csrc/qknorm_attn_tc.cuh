@@ -7,8 +7,8 @@
 //   warps 8-11   prepare what has arrived: widen FP8 tiles, blank V rows outside the item's keys; where a page is no
 //                multiple of 8 tokens they gather the rows themselves with cp.async
 //   warp 14      brings the query rows, by TMA where K and V come that way
-//   warp 12      issues every tcgen05.mma
-//   warp 15      says which items come next
+//   warp 12      issues the tcgen05.mma
+//   warp 15      says which items come next; with two query tiles it issues the second one's and warp 14 walks over the items
 // Scores S_w = Q K^T land in TMEM (128 columns per warpgroup w).  The warpgroup reads them, keeps the running
 // maximum and sum in registers, writes P = 2^(c (s - m)) back over S in 16 bits, and O_w += P V takes P from
 // TMEM and V, keys by head_dim as it lies in the cache, as a transposed operand.  O_w stays in TMEM; it is rescaled only
@@ -195,7 +195,8 @@ struct AttnSmem {
   static constexpr int kDrain = kMlFree + 8;
   static constexpr int kRawFull = kDrain + 8;         // per stage: an FP8 tile, or a bf16 V tile that wants looking at, is there
   static constexpr int kQRaw = kRawFull + 8 * kStages;  // [2] FP8 cache: a bf16 Q tile is there
-  static constexpr int kPass = kQRaw + 16;            // the softmax warps' steps through the join of an item
+  static constexpr int kTurn = kQRaw + 16;            // [2] two forms: whose turn it is to issue
+  static constexpr int kPass = kTurn + 16;            // the softmax warps' steps through the join of an item
   static constexpr int kTmem = kPass + 8;             // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
   static constexpr int kPoison = kAbort + 4;          // [4] 1 + number of an item that holds a V row to be careful with
@@ -296,38 +297,35 @@ struct AttnTc {
   __device__ __forceinline__ uint32_t stage(uint32_t pos) const { return smem + L::kRing + (pos % L::kStages) * L::kTile; }
 
   // ---- items ----------------------------------------------------------------------------------------
-  // Warp 15 walks over the CTA's share and lays the items down for everybody else, some ahead.
-  static constexpr int kReaders = 8 + 4 + 1 + 1 + (TMA ? 1 : 0);  // softmax and tile warps, matrix thread, Q, producer
+  // One warp (15; 14 in the two-tile form) walks over the CTA's share and lays the items down for everybody else, some ahead.
+  static constexpr int kReaders = 8 + 4 + 1 + (ONE ? 1 : 2) + (TMA ? 1 : 0);  // softmax and tile warps, Q, matrix threads, producer
 
   __device__ __forceinline__ volatile int* item_at(uint32_t i) const {
     return reinterpret_cast<volatile int*>(smem_ptr + L::kItems) + (i % L::kItemSlots) * 16;
   }
-  __device__ __forceinline__ void run_walk(AttnWalk walk) const {
+  // Lays down item i, or that there are no more; one thread.  False: that was the last, or leave.
+  __device__ __forceinline__ bool put_item(AttnWalk& walk, uint32_t i) const {
     AttnItem it;
-    for (uint32_t i = 0;; ++i) {
-      const bool more = walk.step > 0 ? walk.next_whole(P, it) : walk.next(P, it);
-      if (i >= (uint32_t)L::kItemSlots &&
-          !wait(smem + L::kItemEmpty + 8 * (i % L::kItemSlots), ((i / L::kItemSlots) - 1) & 1))
-        return;
-      volatile int* at = item_at(i);
-      at[0] = more ? it.b : -1;
-      if (more) {
-        at[1] = it.s.row0;
-        at[2] = it.s.n;
-        at[3] = it.s.keys;
-        at[4] = (int)(it.s.pos0 & 0xffffffffll);
-        at[5] = (int)(it.s.pos0 >> 32);
-        at[6] = it.kvh;
-        at[7] = it.tok0;
-        at[8] = it.j0;
-        at[9] = it.j1;
-        at[10] = it.ulo;
-        at[11] = it.uhi;
-        at[12] = (it.whole ? 1 : 0) | it.slot << 1;
-      }
-      tc::arrive(smem + L::kItemFull + 8 * (i % L::kItemSlots));
-      if (!more) return;
+    const bool more = walk.step > 0 ? walk.next_whole(P, it) : walk.next(P, it);
+    if (i >= (uint32_t)L::kItemSlots && !wait(smem + L::kItemEmpty + 8 * (i % L::kItemSlots), ((i / L::kItemSlots) - 1) & 1)) return false;
+    volatile int* at = item_at(i);
+    at[0] = more ? it.b : -1;
+    if (more) {
+      at[1] = it.s.row0;
+      at[2] = it.s.n;
+      at[3] = it.s.keys;
+      at[4] = (int)(it.s.pos0 & 0xffffffffll);
+      at[5] = (int)(it.s.pos0 >> 32);
+      at[6] = it.kvh;
+      at[7] = it.tok0;
+      at[8] = it.j0;
+      at[9] = it.j1;
+      at[10] = it.ulo;
+      at[11] = it.uhi;
+      at[12] = (it.whole ? 1 : 0) | it.slot << 1;
     }
+    tc::arrive(smem + L::kItemFull + 8 * (i % L::kItemSlots));
+    return more;
   }
   __device__ __forceinline__ void get_item(uint32_t i, AttnItem& it) const {
     const volatile int* at = item_at(i);
@@ -741,17 +739,18 @@ struct AttnTc {
     }
   }
 
-  __device__ __forceinline__ void run_q(int tid) const {
+  __device__ __forceinline__ void run_q(int tid, AttnWalk& walk) const {
     const uint32_t all = 0xffffffffu;
+    if (!ONE && tid == 0) put_item(walk, 0);
     uint32_t qph = 0, qany = 0;  // bit w: phase of Q buffer w, and whether it was in use before
     int count = 0;
     AttnItem it;
     for (uint32_t n_item = 0; take_item(n_item, it); ++n_item) {
-      if (it.j0 >= it.j1) continue;
+      const bool keys = it.j0 < it.j1;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         const AttnTileRange r = attn_tile_range(P, it, ONE ? 0 : w);
-        if (ONE ? w != (count & 1) : r.a >= r.b) continue;
+        if (!keys || (ONE ? w != (count & 1) : r.a >= r.b)) continue;
         if (((qany >> w) & 1) && !__all_sync(all, wait(smem + L::kQEmpty + 8 * w, ((qph >> w) & 1) ^ 1))) {
           if (TMA) drain_q(qph, -1);
           return;
@@ -784,7 +783,9 @@ struct AttnTc {
         qph ^= 1u << w;
         qany |= 1u << w;
       }
-      ++count;
+      if (keys) ++count;
+      if (!ONE && tid == 0) put_item(walk, n_item + 1);
+      __syncwarp();
     }
     if (TMA && *abort_flag()) drain_q(qph, -1);
   }
@@ -808,12 +809,11 @@ struct AttnTc {
     }
     tc::commit(smem + L::kSFull + 8 * w);
   }
-  // Waits for P as it goes.
+  // The first half of P has been waited for (not QUAD); waits for the rest.
   __device__ __forceinline__ bool issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc, uint32_t p_phase) const {
     constexpr uint32_t idesc = tc::instr_desc(DP, F8, true);
     const uint32_t v = tc::desc_lo(stage(pos), 1024);
     if (!QUAD) {
-      if (!wait(smem + L::kPHalf + 8 * w, p_phase)) return false;
       tc::fence_after();
 #pragma unroll
       for (int s = 0; s < kAttnTile / 32; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
@@ -827,10 +827,8 @@ struct AttnTc {
     return true;
   }
 
-  // One thread issues for both warpgroups, in turn: that keeps one of them in its exponentials while the other's products are
-  // made.  (With a thread for each the products of the two interleave, both warpgroups wait for them and then both compute:
-  // a whole prompt of 8192 took 1024 us instead of 854.)
-  __device__ __forceinline__ void run_mma(uint32_t tmem) const {
+  // One query tile: one thread issues for both warpgroups.
+  __device__ __forceinline__ void run_mma_one(uint32_t tmem) const {
     uint32_t pos = 0, count = 0;
     uint32_t qph = 0, pph = 0, oph = 0, oany = 0;  // bit w: phase of a barrier pair's w-th barrier; oany: O_w was in use before
     AttnItem it;
@@ -841,72 +839,87 @@ struct AttnTc {
       if (it.b < 0) return;
       if (it.j0 >= it.j1) continue;
       const int nt = it.j1 - it.j0;
-      if (ONE) {
-        const int qb = count & 1;
-        for (int r = -2; r < nt; ++r) {
-          const int w = r & 1;
-          if (r >= 0) {
-            const uint32_t vp = pos + 2 * r + 1;
-            if (!wait(full(vp), (vp / L::kStages) & 1)) return;
-            if (r < 2 && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
-            if (!issue_pv(tmem, w, vp, r >= 2, (pph >> w) & 1)) return;
-            pph ^= 1u << w;
-            tc::commit(empty(vp));
-            if (r + 2 >= nt) {
-              tc::commit(smem + L::kOFull + 8 * w);
-              oph ^= 1u << w;
-              oany |= 1u << w;
-            }
-          }
-          if (r + 2 < nt) {
-            const uint32_t kp = pos + 2 * (r + 2);
-            if (r == -2) {
-              if (!wait(smem + L::kQFull + 8 * qb, (qph >> qb) & 1)) return;
-              qph ^= 1u << qb;
-            }
-            if (!wait(full(kp), (kp / L::kStages) & 1)) return;
-            tc::fence_after();
-            issue_qk(tmem, w, qb, kp);
-            tc::commit(empty(kp));
-            if (r + 2 == nt - 1) tc::commit(smem + L::kQEmpty + 8 * qb);
+      const int qb = count & 1;
+      for (int r = -2; r < nt; ++r) {
+        const int w = r & 1;
+        if (r >= 0) {
+          const uint32_t vp = pos + 2 * r + 1;
+          if (!wait(full(vp), (vp / L::kStages) & 1)) return;
+          if (r < 2 && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
+          if (!QUAD && !wait(smem + L::kPHalf + 8 * w, (pph >> w) & 1)) return;
+          if (!issue_pv(tmem, w, vp, r >= 2, (pph >> w) & 1)) return;
+          pph ^= 1u << w;
+          tc::commit(empty(vp));
+          if (r + 2 >= nt) {
+            tc::commit(smem + L::kOFull + 8 * w);
+            oph ^= 1u << w;
+            oany |= 1u << w;
           }
         }
-      } else {
-        const AttnTileRange r0 = attn_tile_range(P, it, 0), r1 = attn_tile_range(P, it, 1);
-        const int a[2] = {r0.a, r1.a}, b[2] = {r0.b, r1.b};
-        for (int j = it.j0 - 1; j < it.j1; ++j) {
-          // both tiles of this round before anything is issued: a wait between two products leaves the tensor pipe idle
-          const uint32_t kp = pos + 2 * (j + 1 - it.j0), vp = kp - 1;
-          if (j >= it.j0 && !wait(full(vp), (vp / L::kStages) & 1)) return;
-          if (j + 1 < it.j1 && !wait(full(kp), (kp / L::kStages) & 1)) return;
-#pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            if (j >= a[w] && j < b[w]) {
-              if (j == a[w] && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
-              if (!issue_pv(tmem, w, vp, j > a[w], (pph >> w) & 1)) return;
-              pph ^= 1u << w;
-              if (j == b[w] - 1) {
-                tc::commit(smem + L::kOFull + 8 * w);
-                oph ^= 1u << w;
-                oany |= 1u << w;
-              }
-            }
-            if (j + 1 >= a[w] && j + 1 < b[w]) {
-              if (j + 1 == a[w]) {
-                if (!wait(smem + L::kQFull + 8 * w, (qph >> w) & 1)) return;
-                qph ^= 1u << w;
-                tc::fence_after();
-              }
-              issue_qk(tmem, w, w, kp);
-              if (j + 1 == b[w] - 1) tc::commit(smem + L::kQEmpty + 8 * w);
-            }
+        if (r + 2 < nt) {
+          const uint32_t kp = pos + 2 * (r + 2);
+          if (r == -2) {
+            if (!wait(smem + L::kQFull + 8 * qb, (qph >> qb) & 1)) return;
+            qph ^= 1u << qb;
           }
-          if (j >= it.j0) tc::commit(empty(vp));
-          if (j + 1 < it.j1) tc::commit(empty(kp));
+          if (!wait(full(kp), (kp / L::kStages) & 1)) return;
+          tc::fence_after();
+          issue_qk(tmem, w, qb, kp);
+          tc::commit(empty(kp));
+          if (r + 2 == nt - 1) tc::commit(smem + L::kQEmpty + 8 * qb);
         }
       }
       pos += 2 * nt;
       ++count;
+    }
+  }
+
+  // Two query tiles: a thread for each (warps 12 and 15), issuing in turn.  The turns keep one warpgroup in its exponentials while
+  // the other's products are made; if the products of the two interleaved, both would wait for them and then both compute
+  // (measured, 8192 tokens: 1024 us against 768).  Two threads, because what a thread does between products -- waiting for tiles and
+  // weights, announcing what is done -- then lies beside the other's products and not between them.
+  __device__ __forceinline__ void run_mma_two(uint32_t tmem, int w) const {
+    uint32_t pos = 0, round = 0;
+    uint32_t qph = 0, pph = 0, oph = 0, oany = 0;
+    const uint32_t my_turn = smem + L::kTurn + 8 * w, your_turn = smem + L::kTurn + 8 * (w ^ 1);
+    AttnItem it;
+    for (uint32_t n_item = 0;; ++n_item) {
+      if (!item_wait(n_item)) return;
+      get_item(n_item, it);
+      item_done(n_item);
+      if (it.b < 0) return;
+      if (it.j0 >= it.j1) continue;
+      const AttnTileRange rg = attn_tile_range(P, it, w);
+      for (int j = it.j0 - 1; j < it.j1; ++j, ++round) {
+        // P V of tile j, Q K of tile j + 1; everything they need before the turn is taken
+        const uint32_t kp = pos + 2 * (j + 1 - it.j0), vp = kp - 1;
+        const bool pv = j >= rg.a && j < rg.b, qk = j + 1 >= rg.a && j + 1 < rg.b;
+        if (j >= it.j0 && !wait(full(vp), (vp / L::kStages) & 1)) return;
+        if (j + 1 < it.j1 && !wait(full(kp), (kp / L::kStages) & 1)) return;
+        if (qk && j + 1 == rg.a) {
+          if (!wait(smem + L::kQFull + 8 * w, qph)) return;
+          qph ^= 1;
+        }
+        if (pv && j == rg.a && oany && !wait(smem + L::kOFree + 8 * w, oph ^ 1)) return;
+        if (pv && !wait(smem + L::kPHalf + 8 * w, pph)) return;
+        if ((round > 0 || w == 1) && !wait(my_turn, w == 0 ? (round - 1) & 1 : round & 1)) return;
+        tc::fence_after();
+        if (pv) {
+          if (!issue_pv(tmem, w, vp, j > rg.a, pph)) return;
+          pph ^= 1;
+        }
+        if (qk) issue_qk(tmem, w, w, kp);
+        tc::arrive(your_turn);
+        if (pv && j == rg.b - 1) {
+          tc::commit(smem + L::kOFull + 8 * w);
+          oph ^= 1;
+          oany = 1;
+        }
+        if (qk && j + 1 == rg.b - 1) tc::commit(smem + L::kQEmpty + 8 * w);
+        if (j >= it.j0) tc::commit(empty(vp));
+        if (j + 1 < it.j1) tc::commit(empty(kp));
+      }
+      pos += 2 * (it.j1 - it.j0);
     }
   }
 
@@ -1310,12 +1323,13 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
   if (threadIdx.x == 0) {
     for (int i = 0; i < L::kStages; ++i) {
       ptx::mbar_init(smem + L::kFull + 8 * i, 4);
-      ptx::mbar_init(smem + L::kEmpty + 8 * i, 1);
+      ptx::mbar_init(smem + L::kEmpty + 8 * i, K::ONE ? 1 : 2);
       ptx::mbar_init(smem + L::kRawFull + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(smem + L::kQFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kQRaw + 8 * i, 1);
+      ptx::mbar_init(smem + L::kTurn + 8 * i, 1);
       ptx::mbar_init(smem + L::kQEmpty + 8 * i, K::QUAD ? 9 : 1);
       ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
@@ -1329,7 +1343,7 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
       ptx::mbar_init(smem + L::kItemFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kItemEmpty + 8 * i, K::kReaders);
     }
-    ptx::mbar_init(smem + L::kDrain, 1);
+    ptx::mbar_init(smem + L::kDrain, K::ONE ? 1 : 2);
     ptx::mbar_init(smem + L::kPass, 8);
     *reinterpret_cast<volatile int*>(smem_raw + L::kAbort) = 0;
     for (int i = 0; i < 4; ++i) reinterpret_cast<volatile int*>(smem_raw + L::kPoison)[i] = 0;
@@ -1366,9 +1380,10 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     else k.run_loader(threadIdx.x - 256);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 12) {
+    if (warp == 12 || (!K::ONE && warp == 15)) {
       if ((threadIdx.x & 31) == 0) {
-        k.run_mma(tmem);
+        if (K::ONE) k.run_mma_one(tmem);
+        else k.run_mma_two(tmem, warp == 12 ? 0 : 1);
         // every matrix product has ended before the tiles and TMEM go away, whichever way the loop ended
         tc::commit(smem + L::kDrain);
         k.wait_drain(smem + L::kDrain, 0);
@@ -1377,9 +1392,10 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     } else if (warp == 13) {
       if (TMA) k.run_producer(threadIdx.x & 31);
     } else if (warp == 14) {
-      k.run_q(threadIdx.x & 31);
+      k.run_q(threadIdx.x & 31, walk);
     } else if (threadIdx.x == 480) {
-      k.run_walk(walk);
+      for (uint32_t i = 0; k.put_item(walk, i); ++i) {
+      }
     }
   }
   tc::fence_before();
