@@ -187,8 +187,8 @@ struct AttnSmem {
   static constexpr int kQEmpty = kQFull + 16;
   static constexpr int kSFull = kQEmpty + 16;
   static constexpr int kPFull = kSFull + 16;
-  static constexpr int kPHalf = kPFull + 16;  // the first 64 keys' weights are there (not QUAD)
-  static constexpr int kOFull = kPHalf + 16;
+  static constexpr int kPMost = kPFull + 16;  // the first 96 keys' weights are there (not QUAD)
+  static constexpr int kOFull = kPMost + 16;
   static constexpr int kOFree = kOFull + 16;
   static constexpr int kMl = kOFree + 16;
   static constexpr int kMlFree = kMl + 8;
@@ -809,20 +809,20 @@ struct AttnTc {
     }
     tc::commit(smem + L::kSFull + 8 * w);
   }
-  // The first half of P has been waited for (not QUAD); waits for the rest.
+  // The first 96 keys' weights have been waited for (not QUAD); waits for the rest.
   __device__ __forceinline__ bool issue_pv(uint32_t tmem, int w, uint32_t pos, bool acc, uint32_t p_phase) const {
     constexpr uint32_t idesc = tc::instr_desc(DP, F8, true);
     const uint32_t v = tc::desc_lo(stage(pos), 1024);
     if (!QUAD) {
       tc::fence_after();
 #pragma unroll
-      for (int s = 0; s < kAttnTile / 32; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
+      for (int s = 0; s < 6; ++s)  // 16 keys: 8 TMEM columns of P, 16 rows of V
         tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2 * kGroup >> 4), tc::desc_hi(kGroup), idesc, acc || s > 0);
     }
     if (!wait(smem + L::kPFull + 8 * w, p_phase)) return false;
     tc::fence_after();
 #pragma unroll
-    for (int s = QUAD ? 0 : kAttnTile / 32; s < kAttnTile / 16; ++s)
+    for (int s = QUAD ? 0 : 6; s < kAttnTile / 16; ++s)
       tc::mma_ts(tmem + 2 * kAttnTile + w * DP, tmem + w * kAttnTile + s * 8, v + s * (2 * kGroup >> 4), tc::desc_hi(kGroup), idesc, acc || s > 0);
     return true;
   }
@@ -846,7 +846,7 @@ struct AttnTc {
           const uint32_t vp = pos + 2 * r + 1;
           if (!wait(full(vp), (vp / L::kStages) & 1)) return;
           if (r < 2 && ((oany >> w) & 1) && !wait(smem + L::kOFree + 8 * w, ((oph >> w) & 1) ^ 1)) return;
-          if (!QUAD && !wait(smem + L::kPHalf + 8 * w, (pph >> w) & 1)) return;
+          if (!QUAD && !wait(smem + L::kPMost + 8 * w, (pph >> w) & 1)) return;
           if (!issue_pv(tmem, w, vp, r >= 2, (pph >> w) & 1)) return;
           pph ^= 1u << w;
           tc::commit(empty(vp));
@@ -901,7 +901,7 @@ struct AttnTc {
           qph ^= 1;
         }
         if (pv && j == rg.a && oany && !wait(smem + L::kOFree + 8 * w, oph ^ 1)) return;
-        if (pv && !wait(smem + L::kPHalf + 8 * w, pph)) return;
+        if (pv && !wait(smem + L::kPMost + 8 * w, pph)) return;
         if ((round > 0 || w == 1) && !wait(my_turn, w == 0 ? (round - 1) & 1 : round & 1)) return;
         tc::fence_after();
         if (pv) {
@@ -1015,9 +1015,10 @@ struct AttnTc {
 
   // One score tile: S -> P, running m and l of this lane's row.  QUAD: the 32 columns of this warp's quarter.
   // Columns [from, to) of the tile are keys that the row sees.
-  // Two forms: the first half of P is announced while the second is computed.
+  // Not QUAD: the first 96 keys' weights are announced while the last 32 are computed, which takes about as long as the products
+  // of the 96.  (Announced after 64, the products waited in their turn: 755 us for 8192 tokens.)
   __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
-                                       float& l, uint32_t p_half) const {
+                                       float& l, uint32_t p_most) const {
     // The first half stays in registers from the maximum to the exponentials; the second is read again when the first is half
     // done, so that a thread never holds more than 128 scores and nothing else.
     constexpr int N = QUAD ? kAttnTile / 4 : kAttnTile / 2;
@@ -1077,13 +1078,13 @@ struct AttnTc {
 #pragma unroll
       for (int k = 0; k < N; k += 32) tc::ld32(s_addr + N + k, reinterpret_cast<uint32_t*>(t) + k);
       weights(s + 32, 32);
-      tc::wait_st();
-      tc::fence_before();
-      __syncwarp();
-      if ((threadIdx.x & 31) == 0) tc::arrive(p_half);
       tc::wait_ld();
       if (masked) mask(t, N);
       weights(t, 64);
+      tc::wait_st();
+      tc::fence_before();
+      __syncwarp();
+      if ((threadIdx.x & 31) == 0) tc::arrive(p_most);
       weights(t + 32, 96);
     }
     if (QUAD) {  // the other quarters' keys are not this warp's: zeros in their place
@@ -1130,11 +1131,11 @@ struct AttnTc {
               if (F8) c = row_c(ONE ? count & 3 : w + 2 * oph, wtid);
               const int k0 = j * kAttnTile;
               tile(tmem + lanes + w * kAttnTile, tmem + lanes + 2 * kAttnTile + w * DP, lo - k0, hi - k0,
-                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l, smem + L::kPHalf + 8 * w);
+                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l, smem + L::kPMost + 8 * w);
             }
             __syncwarp();
             if (lane == 0) {
-              if (!QUAD && !busy) tc::arrive(smem + L::kPHalf + 8 * w);
+              if (!QUAD && !busy) tc::arrive(smem + L::kPMost + 8 * w);
               tc::arrive(smem + L::kPFull + 8 * w);
             }
           }
@@ -1333,7 +1334,7 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
       ptx::mbar_init(smem + L::kQEmpty + 8 * i, K::QUAD ? 9 : 1);
       ptx::mbar_init(smem + L::kSFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kPFull + 8 * i, 4);
-      ptx::mbar_init(smem + L::kPHalf + 8 * i, 4);
+      ptx::mbar_init(smem + L::kPMost + 8 * i, 4);
       ptx::mbar_init(smem + L::kOFull + 8 * i, 1);
       ptx::mbar_init(smem + L::kOFree + 8 * i, K::ONE ? 8 : 4);
     }
