@@ -417,14 +417,14 @@ int finish_launch(const char* variant) {
 // (griddepcontrol.wait) before its first access to global memory.  QKNORM_PDL=0 (a debug knob)
 // launches the plain way.
 template <class... KArgs, class... Args>
-cudaError_t launch_overlapped(void (*fn)(KArgs...), unsigned grid, unsigned threads, size_t smem, cudaStream_t stream,
+cudaError_t launch_overlapped(void (*fn)(KArgs...), dim3 grid, unsigned threads, size_t smem, cudaStream_t stream,
                               Args... args) {
   if (!env_int("QKNORM_PDL", 1)) {
     fn<<<grid, threads, smem, stream>>>(args...);
     return cudaSuccess;
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

@@ -409,8 +409,10 @@ struct AttnWalk {
   }
 };
 
-// Puts the units together that were cut: CTA c does the one that c's share starts inside of, if that cut is the unit's first.
+// Puts the units together that were cut: CTAs (c, *) do the one that c's share starts inside of, if that cut is the unit's first,
+// 16 rows each, two a warp (a unit's 256 rows in one CTA were one latency after the other: 68 us).
 constexpr int kAttnJoinThreads = 256;
+constexpr int kAttnJoinRows = 16;  // divides part_rows
 
 __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams P);
 

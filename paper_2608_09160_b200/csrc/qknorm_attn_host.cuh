@@ -625,7 +625,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_tc");
   if (rc != QKNORM_OK || !plan.cuts) return rc;
-  e = launch_overlapped(attn_join_kernel_for(), (unsigned)plan.grid, (unsigned)kAttnJoinThreads, 0, stream, P);
+  e = launch_overlapped(attn_join_kernel_for(), dim3((unsigned)plan.grid, (unsigned)(plan.part_rows / kAttnJoinRows)), (unsigned)kAttnJoinThreads, 0, stream, P);
   if (e != cudaSuccess) return set_cuda_error(e);
   return finish_launch("attn_tc");
 }

@@ -13,7 +13,7 @@ __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __gri
   const int tok0 = qt * P.tok_per_tile * P.tiles_per_item, lane = threadIdx.x & 31;
   // part p of row r lies with CTA blockIdx.x - 1 + p: in its slot 1 if it is the first, else in slot 0
   auto place = [&](int p, int r) { return ((long long)(blockIdx.x - 1 + p) * 2 + (p == 0 ? 1 : 0)) * P.part_rows + r; };
-  for (int r = threadIdx.x >> 5; r < P.part_rows; r += kAttnJoinThreads / 32) {
+  for (int r = blockIdx.y * kAttnJoinRows + (threadIdx.x >> 5); r < (blockIdx.y + 1) * kAttnJoinRows; r += kAttnJoinThreads / 32) {
     const int in_tile = r % kAttnTile, i = tok0 + r / kAttnTile * P.tok_per_tile + in_tile / P.group;
     if (in_tile >= P.tok_per_tile * P.group || i >= s.n) continue;
     const long long row = s.row0 + (long long)i;
