@@ -463,18 +463,20 @@ struct AttnTc {
     return bad;
   }
 
+  // The first row of a thread's pieces of FP8 rows.  With 128 columns, 8 lanes take the first half of one row and the second of
+  // its neighbour: the two halves of one widened row lie on the same banks, but the swizzle puts neighbours on different ones.
+  // (Both halves of one row, one of them written in the other order: that choice became branches, 897 cycles a tile against 413.)
+  __device__ __forceinline__ static int raw_row(int tid) { return row_of(tid, 0) ^ (DP == 128 ? (tid >> 2) & 1 : 0); }
+
   // This warp's 32 rows of an FP8 tile to fp16, over themselves: all read before any is written.  CARE: rows outside [from, to)
   // become zeros, the others are looked through for NaN.
   template <bool CARE>
   __device__ __forceinline__ bool widen(uint32_t tile_at, int tid, int from, int to) const {
-    const int c = tid % kChunks, r0 = row_of(tid, 0);
+    const int c = tid % kChunks, r0 = raw_row(tid);
     const uint32_t src = tile_at + raw_at(r0) + c * 16;
     // Pieces 2c and 2c + 1 of row r0; the next rows of this thread are kRowsAt further each, which is 4 or 8: half a group or one.
-    // With 128 columns a quarter of a warp writes one whole row, whose halves lie on the same banks: the upper half writes its odd
-    // pieces first.
-    const bool odd_first = DP == 128 && (c & 4) != 0;
     const uint32_t dst = tile_at + kv_at(r0 & ~7, 2 * c & ~7), row = (r0 & 7) * 128;
-    const uint32_t turn = (((2 * c) ^ r0) & 7) << 4 ^ (odd_first ? 16 : 0);
+    const uint32_t turn = (((2 * c) ^ r0) & 7) << 4;
     bool bad = false;
     uint4 v[kChunks];
 #pragma unroll
@@ -484,10 +486,10 @@ struct AttnTc {
     for (int i = 0; i < kChunks; ++i) {
       if (CARE && (r0 + i * kRowsAt < from || r0 + i * kRowsAt >= to)) v[i] = make_uint4(0u, 0u, 0u, 0u);
       uint32_t h[8];
-      e4m3x4_to_f16x2(odd_first ? v[i].z : v[i].x, h[0], h[1]);
-      e4m3x4_to_f16x2(odd_first ? v[i].w : v[i].y, h[2], h[3]);
-      e4m3x4_to_f16x2(odd_first ? v[i].x : v[i].z, h[4], h[5]);
-      e4m3x4_to_f16x2(odd_first ? v[i].y : v[i].w, h[6], h[7]);
+      e4m3x4_to_f16x2(v[i].x, h[0], h[1]);
+      e4m3x4_to_f16x2(v[i].y, h[2], h[3]);
+      e4m3x4_to_f16x2(v[i].z, h[4], h[5]);
+      e4m3x4_to_f16x2(v[i].w, h[6], h[7]);
       if (CARE) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) bad |= odd_f16(h[e]);
