@@ -9,7 +9,7 @@
  * at the same time on different streams (each attention call with a workspace of its own).
  * All arithmetic is fp32 (angles: fp64), every result is rounded once to its storage format, to nearest even
  * (FP8-E4M3: saturating at +-448).  Results are bitwise reproducible run to run, except where two
- * tokens of one call name the same cache slot (one of them wins).
+ * tokens of one call name the same cache slot (each value there is then one of theirs).
  *
  * Rows are tokens: q is [tokens, dq] with dq = heads * head_dim, row t starts ld_q ELEMENTS after
  * row t-1 (0 = contiguous), so q, k and v may be column blocks of one fused projection output.
@@ -146,8 +146,10 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  *   a row whose every visible score is -inf gets zeros.
  *
  * Kernels: "attn_tc" (tcgen05 tensor cores) for head_dim a multiple of 8 up to 128, 16-byte aligned rows and at most 128 query
- * heads per key head; "attn_general" otherwise.  Where the batch has too few rows to fill the GPU,
- * the keys are split over CTAs and the parts joined by a second launch.
+ * heads per key head; "attn_general" otherwise.  The batch's key tiles are shared out evenly over the SMs; where that can cut
+ * the keys of a row in two or more, the parts lie in the workspace and a second launch joins them (otherwise no workspace
+ * is asked for).  A wait inside "attn_tc" that runs out sets the device's error word (qknorm_device_error_word): 7 a tile
+ * or a product did not come, 9 a copy did not land before the CTA ended; 8: shared memory is not aligned.
  */
 int qknorm_attn_paged(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* block_table,
                       int32_t table_cols, int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts,

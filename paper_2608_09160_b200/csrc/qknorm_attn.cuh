@@ -284,7 +284,9 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
   sum *= P.heads_kv;
   long long share = total <= 0x7fffffff ? ((unsigned)total + gridDim.x - 1) / gridDim.x : (total + gridDim.x - 1) / gridDim.x;
   if (share < P.own + 2) share = P.own + 2;
-  const int snap = attn_snap(share, P.own);
+  // No room for parts: every cut moves to a unit's start.  The host has seen to it that none has to -- for starts that ascend; others
+  // can make more units than the rows allow for.
+  const int snap = P.starts == nullptr ? 0x3fffffff : attn_snap(share, P.own);
 #pragma unroll
   for (int which = 0; which < 2; ++which) {  // this CTA's cut, and the next one's
     const long long cut = (blockIdx.x + which) * share;

@@ -393,3 +393,109 @@ def test_append_then_attend(libqknorm, dtype):
         tol, tol_lse = R.attention_bounds(ref, hd, dtype is F8)
         assert (np.abs(out.double().cpu().numpy().reshape(T, hq, hd) - ref["out"]) <= tol).all()
         assert (np.abs(lse.double().cpu().numpy() - ref["lse"]) <= tol_lse).all()
+
+
+def test_starts_that_go_back_stay_inside_the_buffers(libqknorm):
+    """q_starts that fall name rows twice: more units than the rows allow for, in a call whose lengths need no workspace."""
+    one = Batch([1100], [1500], 1, 1, 64, guard=0)
+    want, want_lse = one.call()
+    seqs = 200
+    assert attn.attn_paged_workspace(seqs, 1100, 1100, 1500, 1, 1, 64) == 0
+    one.dtable = one.dtable.expand(seqs, -1).contiguous()
+    one.dlens = torch.full((seqs,), 1500, dtype=torch.int32, device="cuda")
+    one.dstarts = torch.tensor([0, 1100] * (seqs // 2) + [0], dtype=torch.int32, device="cuda")
+    out, lse = one.call()
+    ref = one.reference()
+    one.compare(out, lse, ref)
+    one.compare(want, want_lse, ref)
+
+
+@BOTH
+@pytest.mark.parametrize("hq,hk,new,kv", [
+    (2, 1, [1] * 900, [1 + 7 * i % 60 for i in range(900)]),                           # more units than CTAs, none of them cut
+    (1, 1, [(i * 5) % 4 for i in range(700)], [(i * 11) % 200 for i in range(700)]),   # some without tokens, without keys, with fewer keys than tokens
+    (1, 1, [140 if i % 50 == 7 else 0 for i in range(400)], [200 if i % 50 == 7 else 0 for i in range(400)]),
+])
+def test_many_sequences(libqknorm, hq, hk, new, kv, dtype):
+    Batch(new, kv, hq, hk, 64, dtype=dtype, seed=3).check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("page", [64, 20])
+@pytest.mark.parametrize("hq,hk,new,kv", [(1, 1, [300], [20000]), (1, 1, [100, 2], [30000, 500]), (4, 2, [1], [40000]), (1, 1, [140, 500], [6000, 9000])])
+def test_units_cut_into_many_parts(libqknorm, hq, hk, new, kv, page, dtype):
+    """Long keys and few rows: a unit's keys over many CTAs, in each form; with a window that leaves whole parts empty too."""
+    b = Batch(new, kv, hq, hk, 64, page=page, dtype=dtype, seed=page)
+    b.check("attn_tc")
+    b.check("attn_tc", causal=False)
+    b.check("attn_tc", window=7000)
+
+
+@BOTH
+def test_pages_shared_by_sequences(libqknorm, dtype):
+    b = Batch([1, 1, 40], [300, 300, 300], 4, 2, 128, dtype=dtype)
+    for row in b.table[1:]:
+        row[:10] = b.table[0][:10]                # 160 keys in common
+    b.dtable = torch.tensor(b.table, dtype=torch.int32, device="cuda")
+    b.check("attn_tc")
+
+
+@BOTH
+@pytest.mark.parametrize("page,hd", [(16, 128), (7, 64), (16, 36)])
+def test_offsets_past_32_bits(libqknorm, page, hd, dtype):
+    """Pages 2^30 and some elements apart, K and V between one another: the last one starts past 2^32 elements."""
+    b = Batch([1, 3], [40, 20], 2, 1, hd, page=page, dtype=dtype)
+    stride = 2 ** 30 + 4096
+    size = stride * (b.pages - 1) + 2 * page * hd
+    assert stride * (b.pages - 1) > 2 ** 32
+    pool = torch.empty(size, dtype=dtype, device="cuda")
+    views = [torch.as_strided(pool, (b.pages, page, 1, hd), (stride, hd, hd, 1), off) for off in (0, page * hd)]
+    for view, src in zip(views, (b.dk, b.dv)):
+        view.view(torch.uint8 if dtype is F8 else torch.int16).copy_(src.view(torch.uint8 if dtype is F8 else torch.int16))
+    b.dk, b.dv = views
+    b.check("attn_general" if hd == 36 else "attn_tc")
+    # written by the cache write, too
+    x = torch.randn(2, hd, device="cuda").to(BF16)
+    slots = torch.tensor([page * (b.pages - 1), 1], device="cuda")
+    q = torch.zeros(2, hd, dtype=BF16, device="cuda")
+    attn.qknorm_fwd_append(q, x, x, None, None, None, None, slots, b.dk, b.dv, 0.0, k_scale=0.5, v_scale=0.5)
+    torch.cuda.synchronize()
+    for view in views:
+        got = torch.stack([view[b.pages - 1, 0, 0], view[0, 1, 0]]).float()
+        want = (x.float() / 0.5).to(F8).float() if dtype is F8 else x.float()
+        assert torch.equal(got, want)
+
+
+def test_first_call_inside_a_capture(libqknorm):
+    """A fresh process whose first call of every entry point is captured."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2608_09160_b200 import attn
+BF16 = torch.bfloat16
+q = torch.randn(2, 256, device="cuda").to(BF16); k = torch.randn(2, 128, device="cuda").to(BF16)
+kc = torch.zeros(40, 16, 1, 128, dtype=BF16, device="cuda"); vc = torch.zeros_like(kc)
+pos = torch.tensor([599, 5], device="cuda"); slots = torch.tensor([16 * 37 + 7, 16 * 39 + 5], device="cuda")
+f = attn.rope_frequencies(128, 10000.0)[0].cuda()
+gq, gk = torch.ones(256, dtype=BF16, device="cuda"), torch.ones(128, dtype=BF16, device="cuda")
+table = torch.stack([torch.arange(38), torch.full((38,), 39)]).int().cuda()
+lens = torch.tensor([600, 6], dtype=torch.int32, device="cuda"); starts = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+def step():
+    a = attn.qknorm_rope(q, k, pos, f, 128)
+    b = attn.qknorm_fwd_append(q, k, k, gq, gk, pos, f, slots, kc, vc, 1e-6)
+    return a[0], b, attn.qknorm_attn_paged(b, kc, vc, table, lens, starts, 1, 600)
+with torch.cuda.graph(g):
+    got = step()
+g.replay(); torch.cuda.synchronize()
+got = [t.clone() for t in got]
+want = step(); torch.cuda.synchronize()
+assert all(torch.equal(x, y) for x, y in zip(got, want)) and bool(want[2].float().abs().sum() > 0)
+print("same")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]

@@ -313,3 +313,25 @@ def test_captured_and_replayed_on_new_inputs(libqknorm):
         torch.cuda.synchronize()
         want, mag = R.rotate(R.widen(new), pos.cpu(), inv.cpu(), hd, False)
         check(out, want, mag, BF16, f"replay {step}")
+
+
+@pytest.mark.parametrize("cdt", [BF16, F8], ids=["bf16", "e4m3"])
+def test_append_tokens_with_one_slot(libqknorm, cdt):
+    """Several tokens of a call name a slot: every value there is one of theirs, all other slots and q are as they would be."""
+    g = gen(17)
+    T, hq, hk, hd = 300, 4, 2, 64
+    q, k, v = (randn(g, (T, n * hd), BF16).cuda() for n in (hq, hk, hk))
+    slots = torch.arange(T, device="cuda")
+    slots[1::3] = 450
+    kp, vp = (torch.zeros((32, 16, hk, hd), dtype=cdt, device="cuda") for _ in range(2))
+    out = attn.qknorm_fwd_append(q, k, v, None, None, None, None, slots, kp, vp, EPS)
+    torch.cuda.synchronize()
+    assert torch.equal(out, q)
+    for pool, x in ((kp, k), (vp, v)):
+        rows, want = pool.view(-1, hk * hd).float(), x.to(cdt).float()
+        alone = slots != 450
+        assert torch.equal(rows[slots[alone]], want[alone])
+        assert (rows[450] == want[~alone]).any(0).all()
+        untouched = torch.ones(len(rows), dtype=torch.bool, device="cuda")
+        untouched[slots] = False
+        assert (rows[untouched] == 0).all()
