@@ -57,10 +57,11 @@ struct AttnParams {
   int* error;
 };
 
-// K and V as [page][head][token][d], for the tensor-core kernel's copies.
-// A copy brings tokens of a page times: 64 columns of a head, from [page][head][token][d] (kBoxHalf; FP8: all its columns);
-// a whole head of 128, from [page][8 tokens][head and half][token][64 columns], where heads lie side by side in a token
-// (kBoxHeadInRow), or from [page and head][8 tokens][half][token][64 columns], where a page's heads follow one another (kBoxHeadInPage).
+// What one of the tensor-core kernel's copies of K or V brings: tokens of a page times
+//   kBoxHalf       64 columns of a head (FP8: all its columns), from [page][head][token][d];
+//   kBoxHeadInRow  a whole head of 128, from [page][8 tokens][head and half][token][64 columns]: heads side by side in a token;
+//   kBoxHeadInPage a whole head of 128, from [page and head][8 tokens][half][token][64 columns]: a page's heads one after the other.
+// Whole heads, because the copy engine's time goes by the box: 64 x 8192 keys took 420 us by halves, 331 by heads.
 constexpr int kBoxHalf = 0, kBoxHeadInRow = 1, kBoxHeadInPage = 2;
 struct AttnMaps {
   CUtensorMap q, k, v;  // q as [token][head][d]
@@ -165,7 +166,8 @@ __device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long r
 
 constexpr float kLn2 = 0.693147180559945309f;
 
-// Any head_dim, group, alignment: a warp per (new token, query head).
+// Any head_dim, group, alignment: a warp per (new token, query head).  For what the tensor-core kernel does not take; each key costs
+// a warp a dependent round trip, where the other kernel takes 128 of them at once.
 constexpr int kAttnGeneralThreads = 128;
 
 template <class CIO>

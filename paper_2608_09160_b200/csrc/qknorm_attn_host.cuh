@@ -442,7 +442,8 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   // One CTA per SM, and none for less than two tiles.  Units that a batch of T rows can have:
   int64_t pieces = (int64_t)p.q_items * seqs;
   if (T / per_item + seqs < pieces) pieces = T / per_item + seqs;
-  // What a unit's start and end take: a tile's time where a step is one score tile, with two query tiles about 8 us of two each.
+  // What a unit's start and end take, in tiles.  Two query tiles, a prompt of 8192: 1106 us with 1, 928 with 2, 897 with 3, 853 with 4,
+  // 852 with 5; one query tile: no difference between 1 and 5.
   p.own = p.tiles_per_item == 1 ? 1 : 4;
   const double all = (double)pieces * heads_kv * (double)(tiles + p.own);
   p.grid = all >= 2.0 * sms ? sms : (int)((all + 1.0) / 2.0);

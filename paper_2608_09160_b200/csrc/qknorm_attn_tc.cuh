@@ -34,6 +34,15 @@
 //
 // Rounding: P to bf16 (fp16 with an FP8 cache), half a step of it relative, is the one rounding besides the output's;
 // sums, maxima and O are fp32.
+//
+// What bounds it (B200; calls in a captured graph, 6448 GB/s and 1676 TFLOP/s measured copy and matrix rates):
+//   single tokens, bf16   HBM: 64 sequences to 8192 keys, 64 query and 8 key heads: 230 us, 5.9 TB/s
+//   single tokens, FP8    the tile workers and shared memory (a K and a V tile are written, read, written as fp16 and read by
+//                         the products: 224 KB of 128-byte-a-cycle traffic): 16 sequences to 32000 keys: 204 us, floor 102
+//   few short sequences   latency: about 5 us until the first product, then a tile each 0.9 us: 8 x 1000 keys: 18 us, floor 3.3
+//   chunks and prompts    exponentials and products of two tiles in turn, 3700 cycles a pair of 128 x 128 (products alone 2048),
+//                         and 8 to 10 thousand cycles a unit for its first and last steps: 8192 tokens, 40 heads: 680 us, floor 410
+// Tiles of 128 x 128: the largest M of one CTA's products, and two score tiles and two O of 128 columns fill the 512 columns of TMEM.
 #pragma once
 #include "qknorm_attn.cuh"
 
@@ -178,7 +187,7 @@ struct AttnSmem {
   static constexpr int kRaw = kAttnTile * DP;       // an FP8 tile: 32 rows at a time land in the upper half of the place that
                                                     // their fp16 form takes, and one warp widens them over themselves
   static constexpr int kStages = DP == 128 ? 5 : 10;
-  static constexpr int kLag = kStages - 2;  // gathered tiles in flight behind the newest
+  static constexpr int kLag = kStages - 2;  // gathered tiles that stay in flight when the next is issued
   static constexpr int kQ0 = 0;             // two Q tiles
   static constexpr int kRing = 2 * kTile;
   static constexpr int kFull = kRing + kStages * kTile;  // mbarriers, 8 bytes each
@@ -717,26 +726,26 @@ struct AttnTc {
     if (c == 0) smem_ptr[L::kQScale + scale_set * 128 + r] = (unsigned char)(scaled ? e : 0);
   }
 
-  // The rows of a Q tile that a TMA copy has brought, to fp16 in place.
+  // The rows of a Q tile that a TMA copy has brought, to fp16 in place; QUAD: and into the other quarters.
   __device__ __forceinline__ void convert_q(int lane, int rows, int buf, int scale_set) const {
     constexpr int kQChunks = DP / 8, kStep = 32 / kQChunks, kBatch = 4;
     const int c = lane % kQChunks;
     const uint32_t base = smem + L::kQ0 + buf * L::kTile + (c >> 3) * kHalf;
     const int end = (rows + kStep * kBatch - 1) / (kStep * kBatch) * (kStep * kBatch);  // at most 128, QUAD 32
-    for (int k = 0; k < (QUAD ? 4 : 1); ++k) {
-      for (int i0 = lane / kQChunks; i0 < end; i0 += kStep * kBatch) {
-        uint4 v[kBatch];
+    for (int i0 = lane / kQChunks; i0 < end; i0 += kStep * kBatch) {
+      uint4 v[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-          const int r = i0 + b * kStep;
-          v[b] = ptx::lds128(base + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4));
-        }
+      for (int b = 0; b < kBatch; ++b) {
+        const int r = i0 + b * kStep;
+        v[b] = ptx::lds128(base + r * 128 + (((c ^ r) & 7) << 4));
+      }
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-          const int r = i0 + b * kStep;
-          q_to_f16(v[b], r, c, scale_set);
+      for (int b = 0; b < kBatch; ++b) {
+        const int r = i0 + b * kStep;
+        q_to_f16(v[b], r, c, scale_set);
+#pragma unroll
+        for (int k = 0; k < (QUAD ? 4 : 1); ++k)
           tc::sts128(base + (r + 32 * k) * 128 + (((c ^ r) & 7) << 4), v[b].x, v[b].y, v[b].z, v[b].w);
-        }
       }
     }
   }
@@ -760,9 +769,9 @@ struct AttnTc {
         const int tok0 = it.tok0 + (ONE ? 0 : w * P.tok_per_tile), set = ONE ? count & 3 : w + 2 * ((qph >> w) & 1);
         const uint32_t q_full = smem + L::kQFull + 8 * w;
         if constexpr (TMA) {
-          // the tile's tokens and heads as one box per 64 columns (QUAD: four times); tokens of other sequences that come
-          // along stand in rows nobody looks at
-          constexpr int kCopies = QUAD ? 4 : 1;
+          // the tile's tokens and heads as one box per 64 columns (QUAD: four times, unless they are written again anyway); tokens of
+          // other sequences that come along stand in rows nobody looks at
+          constexpr int kCopies = QUAD && !F8 ? 4 : 1;
           const uint32_t bar = F8 ? smem + L::kQRaw + 8 * w : q_full;
           if (tid == 0) {
             ptx::mbar_arrive_expect_tx(bar, (DP / 64) * kCopies * P.q_box_tokens * P.group * 128);
@@ -878,7 +887,7 @@ struct AttnTc {
 
   // Two query tiles: a thread for each (warps 12 and 15), issuing in turn.  The turns keep one warpgroup in its exponentials while
   // the other's products are made; if the products of the two interleaved, both would wait for them and then both compute
-  // (measured, 8192 tokens: 1024 us against 768).  Two threads, because what a thread does between products -- waiting for tiles and
+  // (measured at the time, 8192 tokens: 1024 us against 768).  Two threads, because what a thread does between products -- waiting for tiles and
   // weights, announcing what is done -- then lies beside the other's products and not between them.
   __device__ __forceinline__ void run_mma_two(uint32_t tmem, int w) const {
     uint32_t pos = 0, round = 0;
@@ -1018,7 +1027,7 @@ struct AttnTc {
   // One score tile: S -> P, running m and l of this lane's row.  QUAD: the 32 columns of this warp's quarter.
   // Columns [from, to) of the tile are keys that the row sees.
   // Not QUAD: the first 96 keys' weights are announced while the last 32 are computed, which takes about as long as the products
-  // of the 96.  (Announced after 64, the products waited in their turn: 755 us for 8192 tokens.)
+  // of the 96.  (8192 tokens: 726 us; announced after 64, when the products wait in their turn, 755.)
   __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
                                        float& l, uint32_t p_most) const {
     // The first half stays in registers from the maximum to the exponentials; the second is read again when the first is half
