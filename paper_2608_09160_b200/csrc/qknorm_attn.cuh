@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kAttnGeneralThreads) attn_general_kernel(const
 // each CTA, wherever the cuts fall: CTAs get the same number of tiles whatever the lengths of the sequences.  A CTA's
 // share of a unit is an item.  A unit that lies in one CTA is finished there; of one that is cut, each CTA leaves its part
 // (normalised rows and their log-sum) in one of its two slots -- 0 if the unit began before the CTA's share, 1 if it goes on
-// behind it -- and the join kernel puts them together.  A cut within `snap` of a unit's end or start goes there (attn_snap).
+// behind it -- and the join kernel puts them together.  A cut close to a unit's end or start goes there (attn_snap).
 struct AttnItem {
   AttnSeq s;
   int b, kvh;
@@ -241,8 +241,11 @@ struct AttnStart {
 };
 
 // A cut costs its unit a part more and the join; it is worth that where shares are long.  Short shares (few tiles on many SMs) only
-// cut units of more than 16.
-__host__ __device__ __forceinline__ int attn_snap(long long share, int own) { return share >= 32 ? own : 8; }
+// cut units that weigh more than 16: a cut in a shorter one goes to the nearer end.
+constexpr int kAttnWhole = 16;
+__host__ __device__ __forceinline__ int attn_snap(long long share, int own, int weight) {
+  return share < 32 && weight <= kAttnWhole ? (weight + 1) / 2 : own;
+}
 
 // Found by the whole CTA (blockDim threads, a multiple of 32 up to 1024): a scan over the weights of (sequence, item).
 // scratch: 36 long longs of shared memory, free again when this returns; `out` is in shared memory too.
@@ -288,7 +291,7 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
   if (share < P.own + 2) share = P.own + 2;
   // No room for parts: every cut moves to a unit's start.  The host has seen to it that none has to -- for starts that ascend; others
   // can make more units than the rows allow for.
-  const int snap = P.starts == nullptr ? 0x3fffffff : attn_snap(share, P.own);
+  const bool cuts = P.starts != nullptr;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {  // this CTA's cut, and the next one's
     const long long cut = (blockIdx.x + which) * share;
@@ -312,7 +315,7 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
     int kvh = 0;
     for (; cut >= at + w; at += w) ++kvh;
     int off = (int)(cut - at);
-    const int raw = off;
+    const int raw = off, snap = cuts ? attn_snap(share, P.own, w) : 0x3fffffff;
     off = off <= snap ? 0 : w - off <= snap ? w : off;
     scratch[33 + (which ^ 1)] = at + off;
     if (which == 0) {
@@ -321,7 +324,7 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
       out->qt = qt;
       out->kvh = kvh;
       out->off = off;
-      if (P.starts != nullptr) {
+      if (cuts) {
         int* rec = P.starts + blockIdx.x * 8;
         const bool inside = off > 0 && off < w;
         rec[0] = b;
@@ -336,7 +339,7 @@ __device__ __forceinline__ void attn_find_start(const AttnParams& P, long long* 
   if (tid == 0) {
     if (scratch[34] < 0) {
       out->left = 0;  // past the last unit
-      if (P.starts != nullptr) P.starts[blockIdx.x * 8 + 3] = 0;
+      if (cuts) P.starts[blockIdx.x * 8 + 3] = 0;
     } else {
       out->left = (int)(scratch[33] - scratch[34]);
     }

@@ -447,8 +447,9 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   p.own = p.tiles_per_item == 1 ? 1 : 4;
   const double all = (double)pieces * heads_kv * (double)(tiles + p.own);
   p.grid = all >= 2.0 * sms ? sms : (int)((all + 1.0) / 2.0);
-  // no cut can fall inside a unit that is shorter than twice the distance at which cuts move to its ends
-  p.cuts = tiles + p.own > 2 * attn_snap((int64_t)(all / p.grid) + 1, p.own);
+  // no cut can fall inside a unit of at most twice the distance at which cuts move to its ends; shares are at most this long
+  const int longest = tiles + p.own < 0x3fffffff ? (int)(tiles + p.own) : 0x3fffffff;
+  p.cuts = longest > 2 * attn_snap((int64_t)(all / p.grid) + 1, p.own, longest);
   p.part_rows = p.form == kAttnQuad ? 32 : kAttnTile * p.tiles_per_item;
   return p;
 }

@@ -24,17 +24,26 @@ __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __gri
     for (int o = 16; o > 0; o >>= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
     float acc[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
     const int d = lane * 4;
-    for (int p = 0; p < parts; ++p) {
-      const float zp = P.part_z[place(p, r)];
-      if (zp == kNegInf) continue;  // this part saw no key: its row was not written
-      const float w = z == kNegInf ? zp : exp2f(zp - z);
-      sum += w;
-      if (d < P.head_dim) {
-        const float4 x = *reinterpret_cast<const float4*>(P.part_o + place(p, r) * P.head_dim + d);
-        acc[0] = fmaf(w, x.x, acc[0]);
-        acc[1] = fmaf(w, x.y, acc[1]);
-        acc[2] = fmaf(w, x.z, acc[2]);
-        acc[3] = fmaf(w, x.w, acc[3]);
+    for (int p0 = 0; p0 < parts; p0 += 32) {  // a lane each for the parts' weights, then four parts' rows at a time
+      const float zp = p0 + lane < parts ? P.part_z[place(p0 + lane, r)] : kNegInf;
+      const float wp = zp == kNegInf ? 0.f : z == kNegInf ? zp : exp2f(zp - z);
+      const unsigned there = __ballot_sync(0xffffffffu, zp != kNegInf);  // a part that saw no key has written no row
+      const int n = parts - p0 < 32 ? parts - p0 : 32;
+      for (int p = 0; p < n; p += 4) {
+        float4 x[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          x[b] = (there >> (p + b)) & 1 && d < P.head_dim
+                     ? *reinterpret_cast<const float4*>(P.part_o + place(p0 + p + b, r) * P.head_dim + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const float w = __shfl_sync(0xffffffffu, wp, p + b);
+          sum += w;
+          acc[0] = fmaf(w, x[b].x, acc[0]);
+          acc[1] = fmaf(w, x[b].y, acc[1]);
+          acc[2] = fmaf(w, x[b].z, acc[2]);
+          acc[3] = fmaf(w, x[b].w, acc[3]);
+        }
       }
     }
     const float inv = sum == 0.f ? 0.f : P.v_scale / sum;
