@@ -143,7 +143,7 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  *   out and lse may not overlap any other buffer of the call.  scale > 0.
  *   Rows of out and lse outside every sequence are not written, and such rows of q do not matter.
  *   Keys, values that a row does not see have no influence on it, whatever they hold (NaN and infinities too);
- *   a row whose every visible score is -inf gets zeros.
+ *   a row whose every visible score is -inf gets zeros.  An infinite value that a row does see makes that element infinite or NaN.
  *
  * Kernels: "attn_tc" (tcgen05 tensor cores) for head_dim a multiple of 8 up to 128, 16-byte aligned rows and at most 128 query
  * heads per key head; "attn_general" otherwise.  The batch's key tiles are shared out evenly over the SMs; where that can cut

@@ -38,8 +38,8 @@
 // What bounds it (B200; calls in a captured graph, 6448 GB/s and 1676 TFLOP/s measured copy and matrix rates):
 //   single tokens, bf16   HBM: 64 sequences to 8192 keys, 64 query and 8 key heads: 230 us, 5.9 TB/s
 //   single tokens, FP8    the tile workers and shared memory (a K and a V tile are written, read, written as fp16 and read by
-//                         the products: 224 KB of 128-byte-a-cycle traffic): 16 sequences to 32000 keys: 204 us, floor 102
-//   few short sequences   latency: about 5 us until the first product, then a tile each 0.9 us: 8 x 1000 keys: 18 us, floor 3.3
+//                         the products: 224 KB of 128-byte-a-cycle traffic): 16 sequences to 32000 keys: 195 us, floor 102
+//   few short sequences   latency: about 5 us until the first product, then a tile each 0.9 us: 8 x 1000 keys: 17.3 us, floor 3.3
 //   chunks and prompts    exponentials and products of two tiles in turn, 3700 cycles a pair of 128 x 128 (products alone 2048),
 //                         and 8 to 10 thousand cycles a unit for its first and last steps: 8192 tokens, 40 heads: 680 us, floor 410
 // Tiles of 128 x 128: the largest M of one CTA's products, and two score tiles and two O of 128 columns fill the 512 columns of TMEM.
@@ -981,18 +981,18 @@ struct AttnTc {
                                                         bf_pack(x[e + 4], x[e + 5]), bf_pack(x[e + 6], x[e + 7]));
     }
   }
-  // N (2 or 4) columns of the result of a row
+  // N (4 or 8) columns of the result of a row
   template <int N>
   __device__ __forceinline__ void store_few(const float* x, const Dest& to, int col) const {
     if (col >= P.head_dim) return;  // head_dim is a multiple of 8, col of N
     if (to.place >= 0) {
       float* o = P.part_o + to.place * P.head_dim + col;
 #pragma unroll
-      for (int e = 0; e < N; e += 2) *reinterpret_cast<float2*>(o + e) = make_float2(x[e], x[e + 1]);
+      for (int e = 0; e < N; e += 4) *reinterpret_cast<float4*>(o + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
     } else {
       uint16_t* o = P.out + to.row * P.ld_out + (long long)to.head * P.head_dim + col;
 #pragma unroll
-      for (int e = 0; e < N; e += 2) *reinterpret_cast<uint32_t*>(o + e) = bf_pack(x[e], x[e + 1]);
+      for (int e = 0; e < N; e += 4) *reinterpret_cast<uint2*>(o + e) = make_uint2(bf_pack(x[e], x[e + 1]), bf_pack(x[e + 2], x[e + 3]));
     }
   }
   __device__ __forceinline__ void store_z(float z, const Dest& to) const {
@@ -1240,44 +1240,53 @@ struct AttnTc {
         const bool put = valid && !(cut && lt == 0.f);
         const uint32_t o0 = tmem + lanes + 2 * kAttnTile, o1 = o0 + DP;
         if constexpr (QUAD) {
-          // The item's Q tile is done with: its buffer takes the parts, kCols columns of all eight at a time.
-          constexpr int kCols = L::kTile / (8 * 32 * 4);
-          static_assert(kCols == 32 || kCols == 16, "");
-          const int part = threadIdx.x >> 5;
+          // Two warps reach the same rows' quarter: each adds up both warpgroups' parts for half the columns.  The four quarters'
+          // sums meet in the item's Q buffer, which is done with: kCols columns of each half at a time.
+          constexpr int kCols = DP / 4, kMine = kCols / 4;  // kMine: columns this warp puts together, its lane's row
+          static_assert(4 * 2 * kCols * 32 * 4 == L::kTile, "");
+          const int part = threadIdx.x >> 5, quarter = part & 3;
           float* scratch = reinterpret_cast<float*>(smem_ptr + L::kQ0 + (count & 1) * L::kTile);
-          float mine = 0.f;  // f[part], without indexing registers
+          float f0 = 0.f, f1 = 0.f;  // f[quarter], f[4 + quarter], without indexing registers
 #pragma unroll
-          for (int p = 0; p < kParts; ++p) mine = p == part ? f[p] : mine;
-          const bool has = part < 4 || two;  // the second warpgroup had tiles
+          for (int p = 0; p < 4; ++p) {
+            f0 = p == quarter ? f[p] : f0;
+            f1 = p == quarter && two ? f[4 + p] : f1;
+          }
 #pragma unroll 1
-          for (int k = 0; k < DP; k += kCols) {
-            uint32_t o[kCols];
-            if (has) {
-#pragma unroll
-              for (int q = 0; q < kCols; q += 16) tc::ld16((part < 4 ? o0 : o1) + k + q, o + q);
+          for (int k = 0; k < 2; ++k) {
+            const int col = w * (DP / 2) + k * kCols;
+#pragma unroll 1  // small code: unrolled, the FP8 kernel's main loop lost 9 % to instruction fetches (214 us against 195)
+            for (int q = 0; q < kCols; q += 16) {
+              uint32_t a[16], b[16];
+              tc::ld16(o0 + col + q, a);
+              if (two) tc::ld16(o1 + col + q, b);
               tc::wait_ld();
-            }
 #pragma unroll
-            for (int e = 0; e < kCols; ++e)
-              scratch[(part * kCols + e) * 32 + lane] = has && mine != 0.f ? mine * __uint_as_float(o[e]) : 0.f;
+              for (int e = 0; e < 16; ++e) {
+                float x = f0 == 0.f ? 0.f : f0 * __uint_as_float(a[e]);
+                if (f1 != 0.f) x = fmaf(f1, __uint_as_float(b[e]), x);
+                scratch[((quarter * 2 + w) * kCols + q + e) * 32 + lane] = x;
+              }
+            }
             __syncwarp();
             if (lane == 0) tc::arrive(smem + L::kPass);
             if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
             pass ^= 1;
-            constexpr int kMine = kCols / 8;  // columns this warp adds up, its lane's row
             float x[kMine];
 #pragma unroll
             for (int e = 0; e < kMine; ++e) {
               x[e] = 0.f;
 #pragma unroll
-              for (int p = 0; p < 8; ++p) x[e] += scratch[(p * kCols + part * kMine + e) * 32 + lane];
+              for (int p = 0; p < 4; ++p) x[e] += scratch[(p * 2 * kCols + part * kMine + e) * 32 + lane];
               x[e] *= inv;
             }
-            if (put && !again) store_few<kMine>(x, to, k + part * kMine);
-            __syncwarp();
-            if (lane == 0) tc::arrive(smem + L::kPass);
-            if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
-            pass ^= 1;
+            if (put && !again) store_few<kMine>(x, to, col + quarter * kMine);
+            if (k == 0) {  // the second round's sums go where these were
+              __syncwarp();
+              if (lane == 0) tc::arrive(smem + L::kPass);
+              if (!__all_sync(all, wait(smem + L::kPass, pass))) return;
+              pass ^= 1;
+            }
           }
           ptx::fence_proxy_async();  // the buffer's next writer is a copy
           __syncwarp();

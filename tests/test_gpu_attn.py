@@ -411,6 +411,17 @@ def test_starts_that_go_back_stay_inside_the_buffers(libqknorm):
 
 
 @BOTH
+@pytest.mark.parametrize("page", [16, 5])
+@pytest.mark.parametrize("hd", [8, 16, 24, 32, 40, 48, 72, 80, 112, 120])
+def test_head_sizes(libqknorm, hd, page, dtype):
+    """Heads narrower than the tiles' 64 or 128 columns, in each form."""
+    variant = "attn_tc" if dtype is BF16 or hd % 16 == 0 else "attn_general"
+    Batch([1, 3], [200, 70], 4, 2, hd, page=page, dtype=dtype).check(variant)
+    Batch([50, 7], [130, 300], 2, 1, hd, page=page, dtype=dtype).check(variant)
+    Batch([150, 20], [150, 260], 2, 2, hd, page=page, dtype=dtype).check(variant)
+
+
+@BOTH
 @pytest.mark.parametrize("hq,hk,new,kv", [
     (2, 1, [1] * 900, [1 + 7 * i % 60 for i in range(900)]),                           # more units than CTAs, none of them cut
     (1, 1, [(i * 5) % 4 for i in range(700)], [(i * 11) % 200 for i in range(700)]),   # some without tokens, without keys, with fewer keys than tokens
