@@ -578,6 +578,8 @@ struct AttnTc {
       ld.look_item = -1;
     }
     signal(full(pos), lane);
+    // The wait before this call covered this lane's own copies; widen reads pieces that the lanes beside it copied (raw_row).
+    __syncwarp();
     --ld.pending;
     return true;
   }

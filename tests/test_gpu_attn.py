@@ -510,3 +510,24 @@ print("same")
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+@BOTH
+@pytest.mark.parametrize("hd", [64, 96, 128])
+@pytest.mark.parametrize("new,kv", [([1, 3], [900, 130]), ([20, 9], [700, 260]), ([140, 33], [500, 200])])
+def test_gathered_rows_are_the_copied_ones(libqknorm, new, kv, hd, dtype):
+    """The same keys in pages of 16 tokens (boxes) and of 7 (rows gathered by the loader warps): the same bits, every time."""
+    a, b = (Batch(new, kv, 4, 2, hd, page=page, dtype=dtype) for page in (16, 7))
+    for s in range(len(kv)):
+        for j in range(kv[s]):
+            for src, dst in ((a.k, b.k), (a.v, b.v)):
+                raw = torch.uint8 if dtype is F8 else torch.int16
+                dst.view(raw)[b.table[s][j // 7], j % 7] = src.view(raw)[a.table[s][j // 16], j % 16]
+    b.dk.copy_(b.k.cuda())
+    b.dv.copy_(b.v.cuda())
+    b.q, b.dq = a.q, a.dq
+    want, want_lse = a.call()
+    for _ in range(10):
+        out, lse = b.call()
+        assert binding.last_variant() == "attn_tc"
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse, want_lse)
