@@ -148,8 +148,9 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  * Kernels: "attn_tc" (tcgen05 tensor cores) for head_dim a multiple of 8 up to 128, 16-byte aligned rows and at most 128 query
  * heads per key head; "attn_general" otherwise.  The batch's key tiles are shared out evenly over the SMs; where that can cut
  * the keys of a row in two or more, the parts lie in the workspace and a second launch joins them (otherwise no workspace
- * is asked for).  A wait inside "attn_tc" that runs out sets the device's error word (qknorm_device_error_word): 7 a tile
- * or a product did not come, 9 a copy did not land before the CTA ended; 8: shared memory is not aligned.
+ * is asked for).  A wait inside "attn_tc" that runs out -- two seconds in which nothing else in its CTA moved -- sets the device's error
+ * word (qknorm_device_error_word): 7 a tile or a product did not come, 9 a copy did not land before the CTA ended; 8: shared memory is not
+ * aligned.  Rows done again because a tile holds a value that they must not see take about half a microsecond a key.
  */
 int qknorm_attn_paged(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* block_table,
                       int32_t table_cols, int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts,

@@ -54,6 +54,7 @@ struct AttnParams {
   int box_rows, box_shift;  // tokens of one TMA copy: the largest power of two that divides page_size and a tile; 0: no TMA
   int box_kind;      // what a TMA copy of K and V takes, below
   int q_box_tokens;  // tokens of one TMA copy of q
+  unsigned wait_ns;  // how long the tensor-core kernel waits while nothing in the CTA moves; below 2^31
   int* error;
 };
 
@@ -115,12 +116,23 @@ __device__ __forceinline__ long long attn_page(const AttnParams& P, int b, int k
   return (e < 0 || e >= P.num_pages) ? -1 : e;
 }
 
+// The waits of the tensor-core kernel give up when the time that stands in a word of shared memory has passed (low 32 bits of
+// the GPU's clock in ns); whoever gets work done now and then moves it on.
+__device__ __forceinline__ unsigned attn_time() {
+  unsigned t;
+  asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
+  return t;
+}
+__device__ __forceinline__ void attn_moving(const AttnParams& P, uint32_t deadline) {
+  asm volatile("st.volatile.shared::cta.u32 [%0], %1;" ::"r"(deadline), "r"(attn_time() + P.wait_ns) : "memory");
+}
+
 // One warp, one row and head, keys [lo, hi): o (normalised; lane holds elements lane + 32 e) and z = c m + log2 l.
 // Reads nothing of a key outside the range, so what other keys hold cannot matter.
-// EPL: elements per lane, at least head_dim / 32.
+// EPL: elements per lane, at least head_dim / 32.  deadline: the word of attn_moving, or 0.
 template <class CIO, int EPL>
 __device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long row, int head, int lo, int hi, float (&o)[EPL],
-                                         float& z_out) {
+                                         float& z_out, uint32_t deadline = 0) {
   const int lane = threadIdx.x & 31, D = P.head_dim;
   const int kvh = head / P.group;
   float q[EPL];
@@ -132,6 +144,7 @@ __device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long r
   }
   float m = kNegInf, l = 0.f;
   for (int key = lo; key < hi; ++key) {
+    if (deadline != 0 && (key & 63) == 0 && lane == 0) attn_moving(P, deadline);
     int within;
     const long long page = attn_page(P, b, key, within);
     const long long ka = page * P.k.page + within * P.k.token + kvh * P.k.head;
@@ -354,6 +367,7 @@ struct AttnWalk {
   int J0, J1, ulo, uhi;
   int unit, step;        // step > 0: no shares, this CTA takes every step-th (sequence, key head), one item per sequence
   bool have_seq, known;  // s is b's; the span is that of (b, qt)
+  uint32_t deadline = 0;  // the word of attn_moving: many sequences without rows may have to be passed by
   __device__ __forceinline__ explicit AttnWalk(const AttnStart& st)
       : s(st.s), b(st.b), qt(st.qt), kvh(st.kvh), off(st.off), left(st.left), unit(0), step(0), have_seq(true), known(false) {}
   __device__ __forceinline__ AttnWalk(int first, int every) : qt(0), off(0), left(0), unit(first), step(every) {}
@@ -361,7 +375,10 @@ struct AttnWalk {
     for (; unit < P.seqs * P.heads_kv; unit += step) {
       it.b = unit / P.heads_kv;
       it.s = attn_seq(P, it.b);
-      if (it.s.n <= 0) continue;
+      if (it.s.n <= 0) {
+        attn_moving(P, deadline);
+        continue;
+      }
       it.kvh = unit - it.b * P.heads_kv;
       it.tok0 = 0;
       attn_span(P, it.s, 0, it.j0, it.j1, it.ulo, it.uhi);
@@ -382,6 +399,7 @@ struct AttnWalk {
           qt = 0;
           ++b;
           have_seq = false;
+          attn_moving(P, deadline);
           continue;
         }
         attn_span(P, s, qt * per_item, J0, J1, ulo, uhi);

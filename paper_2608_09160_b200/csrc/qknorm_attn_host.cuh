@@ -576,6 +576,8 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.grid = plan.grid;
   P.part_rows = plan.part_rows;
   P.own = plan.own;
+  const int wait_us = env_int("QKNORM_ATTN_WAIT_US", 2000000);  // shorter in tests of the waits
+  P.wait_ns = 1000u * (unsigned)(wait_us < 1 ? 1 : wait_us > 2000000 ? 2000000 : wait_us);
   P.error = dev->ring_error;
   if (plan.tc && plan.cuts) {
     P.starts = (int*)ws;

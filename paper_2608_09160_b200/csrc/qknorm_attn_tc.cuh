@@ -27,7 +27,13 @@
 // Rows no token fills, keys outside the item's range and head_dim up to the next multiple of 64 are zeros in
 // shared memory, never memory of somebody else.  Inside a tile that the causal edge or the window cuts, a V row with an
 // infinity or a NaN would reach rows that do not see it (0 * inf): the loader looks at the V rows of such
-// tiles and, if it finds one, has the item's rows done again one by one by attn_row.
+// tiles and, if it finds one, has the item's rows done again one by one by attn_row, spread over the softmax warps that have them.
+//
+// Every wait is bounded: when for two seconds nothing has moved in the CTA -- 64 score tiles, 64 keys of a row done again, 64 items
+// laid out, a sequence without rows passed by -- it sets the error word, and the CTA leaves.  Waiting for something slow (rows done again over
+// a long context, an item of very many tiles) goes on for as long as that takes.  The time stands in shared memory and not
+// with the one who waits, and there is no other sign to leave: the waiting loop stands in some 30 places between the instructions of
+// the main loops, and with a count of what has moved beside each loop's own start time a prompt of 8192 took 850 to 940 us instead of 770.
 //
 // FP8 cache: K and V are staged raw and widened to fp16, which holds every E4M3 value exactly; Q is
 // brought to fp16 with a power of two per row, which loses nothing but parts below 2^-30 of the row's largest element.
@@ -208,7 +214,8 @@ struct AttnSmem {
   static constexpr int kPass = kTurn + 16;            // the softmax warps' steps through the join of an item
   static constexpr int kTmem = kPass + 8;             // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
-  static constexpr int kPoison = kAbort + 4;          // [4] 1 + number of an item that holds a V row to be careful with
+  static constexpr int kDeadline = kAbort + 4;        // see attn_moving
+  static constexpr int kPoison = kDeadline + 8;       // [4] 1 + number of an item that holds a V row to be careful with
   // FP8 cache: [4][128] bytes, the exponent taken out of a Q row (0: none).  Four sets, because a set is read until the
   // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
   // round again only after the tensor warp has seen the scores of the item before last consumed.
@@ -275,16 +282,17 @@ struct AttnTc {
   __device__ __forceinline__ volatile int* abort_flag() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kAbort); }
   __device__ __forceinline__ volatile int* poison() const { return reinterpret_cast<volatile int*>(smem_ptr + L::kPoison); }
 
-  // Bounded (two seconds); false: leave.
+  __device__ __forceinline__ volatile unsigned* deadline() const { return reinterpret_cast<volatile unsigned*>(smem_ptr + L::kDeadline); }
+  __device__ __forceinline__ void moving() const { attn_moving(P, smem + L::kDeadline); }
+
+  // Bounded (see above); false: leave.
   __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) const {
     if (ptx::mbar_try_wait(bar, parity)) return true;
     return wait_slow(bar, parity);
   }
   __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity) const {
-    const unsigned long long t0 = ptx::globaltimer_ns();
     while (!ptx::mbar_try_wait(bar, parity)) {
-      if (*abort_flag()) return false;
-      if (ptx::globaltimer_ns() - t0 > 2000000000ull) {
+      if ((int)(attn_time() - *deadline()) > 0) {
         *abort_flag() = 1;
         *P.error = 7;
         return false;
@@ -319,6 +327,7 @@ struct AttnTc {
     if (i >= (uint32_t)L::kItemSlots && !wait(smem + L::kItemEmpty + 8 * (i % L::kItemSlots), ((i / L::kItemSlots) - 1) & 1)) return false;
     volatile int* at = item_at(i);
     at[0] = more ? it.b : -1;
+    if ((i & 63) == 63) moving();
     if (more) {
       at[1] = it.s.row0;
       at[2] = it.s.n;
@@ -1001,19 +1010,19 @@ struct AttnTc {
     if (to.place >= 0) P.part_z[to.place] = z;
     else if (P.lse != nullptr) P.lse[to.row * P.heads_q + to.head] = z * kLn2;
   }
-  // The rows of this warp again, one by one, each from the keys it sees and no others.
-  __device__ __forceinline__ void redo(const AttnItem& it, int w, int first) const {
+  // Rows first, first + step, .. below end of query tile w again, one by one, each from the keys it sees and no others.
+  __device__ __forceinline__ void redo(const AttnItem& it, int w, int first, int end, int step) const {
     const int lane = threadIdx.x & 31;
     const int tok0 = it.tok0 + w * P.tok_per_tile, rows = attn_tile_range(P, it, w).rows;
-    for (int r = first; r < first + 32 && r < rows; ++r) {
+    for (int r = first; r < end && r < rows; r += step) {
       const int i = tok0 + r / P.group;
       const Dest to = dest(it, w, r);
       int lo = attn_lo(P, it.s, i), hi = attn_hi(P, it.s, i);
       lo = lo > it.j0 * kAttnTile ? lo : it.j0 * kAttnTile;
       hi = hi < it.j1 * kAttnTile ? hi : it.j1 * kAttnTile;
       float o[DP / 32], z;
-      if (F8) attn_row<IoE4m3, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z);
-      else attn_row<IoBf16, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z);
+      if (F8) attn_row<IoE4m3, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z, smem + L::kDeadline);
+      else attn_row<IoBf16, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z, smem + L::kDeadline);
 #pragma unroll
       for (int e = 0; e < DP / 32; ++e) {
         const int d = lane + 32 * e;
@@ -1149,6 +1158,7 @@ struct AttnTc {
             __syncwarp();
             if (lane == 0) {
               if (!QUAD && !busy) tc::arrive(smem + L::kPMost + 8 * w);
+              if ((j & 62) == 62) moving();
               tc::arrive(smem + L::kPFull + 8 * w);
             }
           }
@@ -1185,7 +1195,7 @@ struct AttnTc {
           }
           if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), to);
         }
-        if (again && busy) redo(it, w, first_row);
+        if (again && busy) redo(it, w, first_row, first_row + 32, 1);
         if (own) {
           tc::fence_before();
           __syncwarp();
@@ -1294,7 +1304,7 @@ struct AttnTc {
           __syncwarp();
           if (lane == 0) tc::arrive(smem + L::kQEmpty + 8 * (count & 1));
           if (valid && part == 0 && !again) store_z(z, to);
-          if (again && part == 0) redo(it, 0, 0);
+          if (again) redo(it, 0, part, 32, 8);  // all eight warps have these rows
         } else {
           if (busy && !again) {
 #pragma unroll
@@ -1315,7 +1325,7 @@ struct AttnTc {
             }
             if (valid && w == 0) store_z(z, to);
           }
-          if (again && busy && w == 0) redo(it, 0, first_row);
+          if (again && busy) redo(it, 0, first_row + w, first_row + 32, 2);  // both warpgroups have them
         }
         tc::fence_before();
         __syncwarp();
@@ -1392,7 +1402,9 @@ __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid
     walk = AttnWalk(*start);
     __syncthreads();
   }
+  walk.deadline = smem + L::kDeadline;
   const K k{P, maps, smem, smem_raw};
+  k.moving();  // every thread: none may look at the word before it holds a time
   // 512 threads start with 128 registers each; 2 x 184 + 64 + 80 = 4 x 128
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");

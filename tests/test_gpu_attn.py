@@ -531,3 +531,70 @@ def test_gathered_rows_are_the_copied_ones(libqknorm, new, kv, hd, dtype):
         out, lse = b.call()
         assert binding.last_variant() == "attn_tc"
         assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse, want_lse)
+
+
+@BOTH
+@pytest.mark.parametrize("new", [4, 10, 40])
+def test_rows_done_again_outlast_no_wait(libqknorm, monkeypatch, new, dtype):
+    """Rows whose tile holds an infinity that they do not see are done again key by key, which takes far longer than the matrix
+    path.  With the limit of a wait lowered to one millisecond, below that: everybody waits on, and the rows of the batch's other
+    sequences come out as ever."""
+    seqs, keys, hq, hk, hd = 20, 6000, 64, 8, 64
+    b = Batch([new] * seqs, [keys] * seqs, hq, hk, hd, dtype=dtype)
+    want, want_lse = b.call()
+    vmax = b.v.float().nan_to_num(0.0).abs().amax().item() * b.vs     # unused slots are NaN
+    b.v[b.table[0][(keys - 1) // 16], (keys - 1) % 16] = float("nan") if dtype is F8 else float("inf")
+    b.dv.copy_(b.v.cuda())                                            # seen by the sequence's last token only
+    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "1000")
+    out, lse = b.call()                                               # looks at the error word, too
+    n = new * seqs
+    assert torch.equal(out[new:n].view(torch.int16), want[new:n].view(torch.int16)) and torch.equal(lse[new:n], want_lse[new:n])
+    # The rows done again have fp32 weights where the others' are rounded: apart by half a step of bf16 of sum p |v| <= max |v|, half a
+    # step of each result, and three times the scores' error on either side (68 2^-24 of 10 at most, as in attention_bounds).
+    x, y = out[:new - 1].double(), want[:new - 1].double()
+    assert ((x - y).abs() <= 2.0 ** -8 * 1.01 * (x.abs() + y.abs() + vmax) + 6 * 68 * 2.0 ** -24 * 10 * vmax).all()
+    # twice 68 2^-24 of 10, and the sum's 6000 / 32 + 16 steps
+    assert ((lse[:new - 1] - want_lse[:new - 1]).abs() <= 2 * (680 + 204) * 2.0 ** -24 + 1e-5).all()
+    assert not torch.isfinite(out[new - 1].view(hq, hd)).any()
+
+
+@BOTH
+@pytest.mark.parametrize("new,group,seqs", [(1, 8, 450), (10, 8, 450), (40, 8, 450)])
+def test_long_items_outlast_no_wait(libqknorm, monkeypatch, new, group, seqs, dtype):
+    """Units of 2048 key tiles (one page over and over), three a CTA: each takes about two milliseconds, and the rows of the one
+    after the next wait for it with a limit of a fifth of a millisecond."""
+    g = torch.Generator().manual_seed(4)
+    keys, page, hd = 1 << 18, 64, 64
+    k, v = (torch.randn((3, page, 1, hd), generator=g).to(dtype).cuda() for _ in range(2))
+    table = torch.arange(keys // page, dtype=torch.int32).remainder(3).expand(seqs, -1).contiguous().cuda()
+    lens = torch.full((seqs,), keys, dtype=torch.int32, device="cuda")
+    starts = torch.arange(0, (seqs + 1) * new, new, dtype=torch.int32, device="cuda")
+    q = torch.randn((seqs * new, group * hd), generator=g).to(BF16).cuda()
+    go = lambda: attn.qknorm_attn_paged(q, k, v, table, lens, starts, new, keys)
+    want = go()
+    torch.cuda.synchronize()
+    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "200")
+    out = go()
+    torch.cuda.synchronize()
+    assert binding.device_error_word() == 0
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("new", [1, 300])
+def test_sequences_without_rows_outlast_no_wait(libqknorm, monkeypatch, new):
+    """Hundreds of thousands of sequences without new tokens between two that have some: passing by them takes milliseconds, the limit
+    of a wait is a fifth of one."""
+    seqs, hd = 400_000, 64
+    g = torch.Generator().manual_seed(5)
+    k, v = (torch.randn((4, 16, 1, hd), generator=g).to(BF16).cuda() for _ in range(2))
+    q = torch.randn((2 * new, hd), generator=g).to(BF16).cuda()
+    starts = torch.full((seqs + 1,), new, dtype=torch.int32, device="cuda")
+    starts[0], starts[-1] = 0, 2 * new
+    lens = torch.full((seqs,), 40, dtype=torch.int32, device="cuda")
+    table = torch.tensor([2, 0, 3], dtype=torch.int32, device="cuda").expand(seqs, -1).contiguous()
+    want = attn.qknorm_attn_paged(q, k, v, table[:2], lens[:2], starts[[0, 1, -1]].contiguous(), new, 40)
+    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "200")
+    out = attn.qknorm_attn_paged(q, k, v, table, lens, starts, new, 40)
+    torch.cuda.synchronize()
+    assert binding.device_error_word() == 0
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
