@@ -82,7 +82,8 @@ int qknorm_rope_e4m3(const void* q, const void* k, const qknorm_rotation* rot, i
 /*
  * A paged cache: pools of num_pages pages, a page holds page_size tokens, a token heads * head_dim
  * values.  Element (page, token, head, d) of K is at k[page*k_page + token*k_token + head*k_head + d], likewise V, in
- * ELEMENTS: any order of the page's axes, K and V in one buffer or in two.
+ * ELEMENTS: any order of the axes, K and V in one buffer or in two, with gaps or between one another (if one lies in the other's
+ * gaps, qknorm_fwd_append asks for the same strides of both; unlike ones are QKNORM_ERR_ALIAS).
  * e4m3 = 0: bf16.  e4m3 = 1: FP8-E4M3 that stands for stored * k_scale (v_scale); the scales are ignored for bf16.
  */
 typedef struct {

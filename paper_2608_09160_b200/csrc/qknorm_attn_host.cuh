@@ -60,8 +60,8 @@ int check_rotation(const qknorm_rotation* r, int head_dim, RopeParams& R) {
 struct CallRegions {  // buffers of a call: outputs, and everything an output must not touch
   Region out[8], in[16];
   int outs = 0, ins = 0;
-  bool exact_input_ok[8];  // out[i] may be exactly in[own[i]]
-  int own[8];
+  int own[8];            // out[i] may be exactly in[own[i]]
+  int pools = -1;        // out[pools] and out[pools + 1] are the two sides of a cache, looked at apart from the others
 };
 
 int log2_or_minus_one(int v) {
@@ -78,7 +78,8 @@ int check_regions(const CallRegions& c) {
     for (int j = 0; j < c.ins; ++j)
       if (may_overlap(c.out[i], c.in[j]) && !(c.own[i] == j && same_region(c.out[i], c.in[j]))) return QKNORM_ERR_ALIAS;
     for (int j = 0; j < c.outs; ++j)
-      if (j != i && may_overlap(c.out[i], c.out[j])) return QKNORM_ERR_ALIAS;
+      if (j != i && !(c.pools >= 0 && i + j == 2 * c.pools + 1 && (i == c.pools || j == c.pools)) && may_overlap(c.out[i], c.out[j]))
+        return QKNORM_ERR_ALIAS;
   }
   return QKNORM_OK;
 }
@@ -89,8 +90,80 @@ int row_stride(int64_t ld, int32_t width, long long* out) {
   return QKNORM_OK;
 }
 
-// One side of a paged cache: strides and alignment.  *rows: the tokens of the pool as a region where they can be described
-// as rows of one pitch, else one region from the first to the last element.
+// Where the elements of one side of a paged cache lie: runs of `width` bytes, along up to three axes from the shortest stride to the
+// longest.  nested: every stride is at least as long as all that lies inside it, so that no two runs meet.
+struct PoolShape {
+  uintptr_t base;
+  int64_t width;
+  int axes;
+  int64_t stride[3], n[3];
+  bool nested;
+};
+
+PoolShape pool_shape(const qknorm_paged_cache& c, void* base, int64_t page, int64_t token, int64_t head) {
+  const int64_t eb = c.e4m3 ? 1 : 2;
+  PoolShape s = {(uintptr_t)base, c.head_dim * eb, 0, {0, 0, 0}, {0, 0, 0}, true};
+  const int64_t stride[3] = {token * eb, head * eb, page * eb}, n[3] = {c.page_size, c.heads, c.num_pages};
+  for (int a = 0; a < 3; ++a) {
+    if (n[a] <= 1) continue;
+    int i = s.axes++;
+    for (; i > 0 && s.stride[i - 1] > stride[a]; --i) {
+      s.stride[i] = s.stride[i - 1];
+      s.n[i] = s.n[i - 1];
+    }
+    s.stride[i] = stride[a];
+    s.n[i] = n[a];
+  }
+  int64_t inside = s.width;
+  for (int i = 0; i < s.axes; ++i) {
+    s.nested = s.nested && s.stride[i] >= inside;
+    inside += (s.n[i] - 1) * s.stride[i];
+  }
+  return s;
+}
+
+// The side as rows of one pitch: axes without gaps become the row, those that go on evenly its repetitions; what an axis
+// beyond them leaves free counts as taken.
+Region pool_region(const PoolShape& s) {
+  int64_t width = s.width, rows = 1, pitch = 0;
+  for (int i = 0; i < s.axes; ++i) {
+    if (rows == 1 && s.stride[i] == width) {
+      width *= s.n[i];
+    } else if (rows == 1 || s.stride[i] == rows * pitch) {
+      pitch = rows == 1 ? s.stride[i] : pitch;
+      rows *= s.n[i];
+    } else {
+      width += (rows - 1) * pitch;
+      pitch = s.stride[i];
+      rows = s.n[i];
+    }
+  }
+  if (!s.nested) {
+    width = s.width;
+    for (int i = 0; i < s.axes; ++i) width += (s.n[i] - 1) * s.stride[i];
+    rows = 1;
+  }
+  return Region{s.base, (uintptr_t)rows, (uintptr_t)width, (uintptr_t)(rows == 1 ? width : pitch)};
+}
+
+// Do two runs of a nested shape, `delta` bytes apart, meet for some steps along axes 0 .. axis of either?
+bool runs_meet(const PoolShape& s, int axis, int64_t delta) {
+  if (axis < 0) return delta < s.width && -delta < s.width;
+  // all that lies inside a stride is no longer than it, so only the two steps that leave less than a stride can do
+  const int64_t q = delta >= 0 ? delta / s.stride[axis] : -((-delta + s.stride[axis] - 1) / s.stride[axis]);
+  for (int64_t step = q; step <= q + 1; ++step)
+    if (step < s.n[axis] && -step < s.n[axis] && runs_meet(s, axis - 1, delta - step * s.stride[axis])) return true;
+  return false;
+}
+
+// Exact where both sides lie alike, as halves of one buffer do; otherwise by their regions.
+bool pools_meet(const PoolShape& a, const PoolShape& b) {
+  bool alike = a.nested && b.nested && a.axes == b.axes;
+  for (int i = 0; alike && i < a.axes; ++i) alike = a.stride[i] == b.stride[i] && a.n[i] == b.n[i];
+  return alike ? runs_meet(a, a.axes - 1, (int64_t)(b.base - a.base)) : may_overlap(pool_region(a), pool_region(b));
+}
+
+// One side of a paged cache: strides and alignment.
 int check_cache_side(const qknorm_paged_cache& c, void* base, int64_t page, int64_t token, int64_t head, Region* region, bool* vec16,
                      bool* vec8) {
   const uintptr_t eb = c.e4m3 ? 1 : 2;
@@ -111,15 +184,9 @@ int check_cache_side(const qknorm_paged_cache& c, void* base, int64_t page, int6
   const __int128 total = (__int128)(c.num_pages > 1 ? c.num_pages - 1 : 0) * page + (__int128)(c.page_size - 1) * token +
                          (__int128)(c.heads - 1) * head + d;
   if (total > ((__int128)1 << 60)) return QKNORM_ERR_SHAPE;
-  const int64_t extent = (c.page_size - 1) * token + (c.heads - 1) * head + d;
   if (c.num_pages > 1 && page < d) return QKNORM_ERR_SHAPE;
   if (((uintptr_t)base) % eb != 0) return QKNORM_ERR_ALIGN;
-  if (c.num_pages > 1 && page == c.page_size * token && (c.heads - 1) * head + d <= token)
-    *region = Region{(uintptr_t)base, (uintptr_t)(c.num_pages * c.page_size), (uintptr_t)((c.heads - 1) * head + d) * eb, (uintptr_t)token * eb};
-  else if (c.num_pages > 1 && page < extent)
-    *region = Region{(uintptr_t)base, 1, (uintptr_t)((c.num_pages - 1) * page + extent) * eb, (uintptr_t)((c.num_pages - 1) * page + extent) * eb};
-  else
-    *region = Region{(uintptr_t)base, (uintptr_t)c.num_pages, (uintptr_t)extent * eb, (uintptr_t)(c.num_pages > 1 ? page : extent) * eb};
+  *region = pool_region(pool_shape(c, base, page, token, head));
   const uintptr_t all = (uintptr_t)base | ((uintptr_t)page * eb) | ((uintptr_t)token * eb) | ((uintptr_t)head * eb);
   *vec16 = all % 16 == 0;
   *vec8 = all % 8 == 0;
@@ -297,6 +364,7 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
     c.in[c.ins++] = Region{(uintptr_t)q, rows, qb, (uintptr_t)R.q.ldx * 2};
     if (norm != kNormNone) c.in[c.ins++] = flat(gq, qb);
   }
+  c.pools = c.outs;
   c.own[c.outs] = -1;
   c.out[c.outs++] = f.k;
   c.own[c.outs] = -1;
@@ -310,6 +378,9 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
     c.in[c.ins++] = flat(R.inv_freq, 4 * (uintptr_t)R.rot_dim);
   }
   if ((rc = check_regions(c)) != QKNORM_OK) return rc;
+  if (cache->num_pages > 0 && pools_meet(pool_shape(*cache, cache->k, cache->k_page, cache->k_token, cache->k_head),
+                                         pool_shape(*cache, cache->v, cache->v_page, cache->v_token, cache->v_head)))
+    return QKNORM_ERR_ALIAS;
   const bool vec = (hd | R.rot_dim) % 16 == 0 && ptrs % 16 == 0 && strides % 8 == 0 && (cache->e4m3 ? f.vec8 : f.vec16);
   return launch_rope(R, 2, cache->e4m3 ? 1 : 2, norm, vec, stream);
 }

@@ -234,3 +234,61 @@ def test_reference_inverse_rotation_is_the_gradient():
             h[:, e] = 1e-6
             diff = ((fwd(x + h) - fwd(x - h)) * y).sum(1) / 2e-6
             assert torch.allclose(diff, grad[:, e], atol=1e-7)
+
+
+# K and V in one buffer: axes of the buffer, the side's place among them.  hd = 64, 2 heads, pages of 16, 8 pages unless said.
+SHARED_BUFFERS = {
+    "tokens, one page": (dict(pages=1), "ptshd"), "heads": ({}, "pthsd"), "heads before tokens": ({}, "phtsd"), "tokens of a head": ({}, "phstd"),
+    "layers between": ({}, "pltshd"), "layers, heads before tokens": ({}, "plhtsd"), "pages inside": ({}, "tpshd"), "one token a page": (dict(page=1), "pthsd"),
+    "one head": (dict(heads=1), "ptshd"), "side by side in a page": ({}, "psthd"), "apart": ({}, "spthd"),
+}
+
+
+def shared(axes, pages=8, page=16, heads=2, hd=64, layers=3):
+    """(K's strides by axis, elements from K to V) of a contiguous buffer [axes]; 's' is K and V, 'l' layers."""
+    size = dict(p=pages, t=page, h=heads, d=hd, s=2, l=layers)
+    stride, n = {}, 1
+    for a in reversed(axes):
+        stride[a] = n
+        n *= size[a]
+    return stride, stride["s"]
+
+
+@pytest.mark.parametrize("name", SHARED_BUFFERS)
+@pytest.mark.parametrize("e4m3", [0, 1])
+def test_append_takes_every_order_of_a_shared_buffer(lib, name, e4m3):
+    """K and V that do not meet are accepted wherever the axes lie; a V that meets K is refused."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("accepted calls would run on made-up addresses")
+    kw, axes = SHARED_BUFFERS[name]
+    st, to_v = shared(axes, **kw)
+    eb = 1 if e4m3 else 2
+    at = dict(k_page=st["p"], k_token=st["t"], k_head=st["h"], v_page=st["p"], v_token=st["t"], v_head=st["h"], e4m3=e4m3, **kw)
+    assert append(lib, c=cache(v=E + to_v * eb, **at), dq=0, q=None, oq=None, gq=None) == binding.QKNORM_ERR_CUDA
+    for off in (0, 8, -8, *([st["t"]] if kw.get("page") != 1 else []), *([st["h"]] if kw.get("heads") != 1 else [])):
+        assert append(lib, c=cache(v=E + off * eb, **at), dq=0, q=None, oq=None, gq=None) == binding.QKNORM_ERR_ALIAS, off
+
+
+def test_append_finds_every_meeting_of_k_and_v(lib):
+    """Small pools of random strides, K and V alike: refused exactly where two elements share a place."""
+    import random
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("accepted calls would run on made-up addresses")
+    rng = random.Random(5)
+    seen = {binding.QKNORM_ERR_CUDA: 0, binding.QKNORM_ERR_ALIAS: 0}
+    for _ in range(4000):
+        hd, n = rng.choice([1, 2, 3]), dict(p=rng.randint(1, 3), t=rng.randint(1, 3), h=rng.randint(1, 3))
+        order, stride, extent = rng.sample("pth", 3), {}, hd
+        for a in order:                                     # nested, with gaps
+            stride[a] = extent + rng.choice([0, 0, hd, rng.randint(0, 9)])
+            extent = (n[a] - 1) * stride[a] + extent
+        k = {p * stride["p"] + t * stride["t"] + h * stride["h"] + d for p in range(n["p"]) for t in range(n["t"]) for h in range(n["h"]) for d in range(hd)}
+        off = rng.randint(-extent - 2, extent + 2)
+        c = cache(v=E + 2 * off, pages=n["p"], page=n["t"], heads=n["h"], hd=hd, k_page=stride["p"], k_token=stride["t"], k_head=stride["h"],
+                  v_page=stride["p"], v_token=stride["t"], v_head=stride["h"])
+        want = binding.QKNORM_ERR_ALIAS if any(e + off in k for e in k) else binding.QKNORM_ERR_CUDA
+        assert append(lib, c=c, dq=0, q=None, oq=None, gq=None) == want, (n, hd, stride, off)
+        seen[want] += 1
+    assert min(seen.values()) > 500

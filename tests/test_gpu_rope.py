@@ -335,3 +335,45 @@ def test_append_tokens_with_one_slot(libqknorm, cdt):
         untouched = torch.ones(len(rows), dtype=torch.bool, device="cuda")
         untouched[slots] = False
         assert (rows[untouched] == 0).all()
+
+
+@pytest.mark.parametrize("cdt", [BF16, F8], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("pages,shape,order", [
+    # a buffer's axes: p pages, t tokens, s K and V, h heads, d head_dim, l layers (the second is used)
+    (1, (1, 64, 2, 2, 64), "ptshd"), (5, (5, 16, 2, 2, 64), "pthsd"), (5, (5, 2, 16, 2, 64), "phtsd"), (5, (5, 2, 2, 16, 64), "phstd"),
+    (5, (5, 3, 16, 2, 2, 64), "pltshd"), (5, (5, 3, 2, 16, 2, 64), "plhtsd"), (5, (16, 5, 2, 2, 64), "tpshd"),
+])
+def test_append_into_every_order_of_a_shared_buffer(libqknorm, pages, shape, order, cdt):
+    """K and V between one another in one buffer: what separate pools get, nothing else in the buffer touched; attention reads it."""
+    g = gen(len(order) + pages)
+    T, hq, hk, hd = 40, 4, 2, 64
+    buf = randn(g, shape, cdt).cuda()
+    raw = torch.uint8 if cdt is F8 else torch.int16
+    before = buf.view(raw).clone()
+
+    def side(b, which):
+        view = b.select(order.index("l"), 1) if "l" in order else b
+        axes = order.replace("l", "")
+        view, axes = view.select(axes.index("s"), which), axes.replace("s", "")
+        return view.permute([axes.index(a) for a in "pthd"])
+    kp, vp = side(buf, 0), side(buf, 1)
+    k2, v2 = kp.contiguous(), vp.contiguous()
+    q, k, v = (randn(g, (T, n * hd), BF16).cuda() for n in (hq, hk, hk))
+    gq, gk = torch.ones(hq * hd, dtype=BF16, device="cuda"), torch.ones(hk * hd, dtype=BF16, device="cuda")
+    inv, _ = attn.rope_frequencies(hd)
+    pos = torch.arange(T, device="cuda")
+    slots = torch.randperm(kp.shape[0] * kp.shape[1], generator=g)[:T].cuda()
+    for a, b in ((kp, vp), (k2, v2)):
+        attn.qknorm_fwd_append(q, k, v, gq, gk, pos, inv, slots, a, b, EPS, k_scale=0.5, v_scale=0.25)
+    torch.cuda.synchronize()
+    assert torch.equal(kp.contiguous().view(raw), k2.view(raw)) and torch.equal(vp.contiguous().view(raw), v2.view(raw))
+    want = before.clone()
+    for which, pool in ((0, k2), (1, v2)):
+        side(want, which).copy_(pool.view(raw))
+    assert torch.equal(buf.view(raw), want)
+    page = kp.shape[1]
+    table = torch.arange(kp.shape[0], dtype=torch.int32, device="cuda")[None]
+    lens, starts = torch.tensor([T], dtype=torch.int32, device="cuda"), torch.tensor([0, T], dtype=torch.int32, device="cuda")
+    outs = [attn.qknorm_attn_paged(q, a, b, table, lens, starts, T, page * kp.shape[0], k_scale=0.5, v_scale=0.25) for a, b in ((kp, vp), (k2, v2))]
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0].view(torch.int16), outs[1].view(torch.int16))
