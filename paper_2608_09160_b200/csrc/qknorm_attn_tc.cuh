@@ -12,7 +12,7 @@
 // Scores S_w = Q K^T land in TMEM (128 columns per warpgroup w).  The warpgroup reads them, keeps the running
 // maximum and sum in registers, writes P = 2^(c (s - m)) back over S in 16 bits, and O_w += P V takes P from
 // TMEM and V, keys by head_dim as it lies in the cache, as a transposed operand.  O_w stays in TMEM; it is rescaled only
-// when the maximum has grown by more than 2^8, so P is at most 2^8 and the rescale is rare.
+// when the maximum has grown by more than 2^8, so a weight is at most 2^8 and the rescale is rare.
 //
 // Three forms:
 //   two query tiles     (chunks): tile w belongs to warpgroup w, both use every K and V tile;
@@ -38,8 +38,10 @@
 // FP8 cache: K and V are staged raw and widened to fp16, which holds every E4M3 value exactly; Q is
 // brought to fp16 with a power of two per row, which loses nothing but parts below 2^-30 of the row's largest element.
 //
-// Rounding: P to bf16 (fp16 with an FP8 cache), half a step of it relative, is the one rounding besides the output's;
-// sums, maxima and O are fp32.
+// Rounding: P is rounded for the second product, to bf16 (2^-8 relative) or, with an FP8 cache, to fp16 (2^-11 relative, and
+// 2^-25 absolute below 2^-14; the sum l takes them unrounded).  So P stands for 2^7 times the weights there: what the maximum may lag
+// behind still fits, and a weight keeps half a step of 2^-32 of the largest one instead of 2^-25.  (With weights as they are, a key that
+// outweighs its row's others by 2^26 left them out of O and in l.)  Otherwise only the output is rounded; sums, maxima and O are fp32.
 //
 // What bounds it (B200; calls in a captured graph, 6448 GB/s and 1676 TFLOP/s measured copy and matrix rates):
 //   single tokens, bf16   HBM: 64 sequences to 8192 keys, 64 query and 8 key heads: 230 us, 5.9 TB/s
@@ -134,6 +136,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The same; what lies beyond the format becomes its largest value (NaN stays NaN).
+__device__ __forceinline__ uint32_t pack_f16_sat(float a, float b) {
+  uint32_t r;
+  asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
 }
 // Has the phase completed?  Does not wait: try_wait may suspend the thread for a while.
 __device__ __forceinline__ bool test(uint32_t bar, uint32_t parity) {
@@ -273,6 +281,8 @@ struct AttnTc {
   __device__ __forceinline__ static uint32_t kv_at(int r, int c) {  // row r, 16-byte piece c
     return (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (((c ^ r) & 7) << 4);
   }
+
+  static constexpr float kUp = F8 ? 7.f : 0.f;  // P = 2^(c (s - m) + kUp), and l is the sum of those
 
   const AttnParams& P;
   const AttnMaps& maps;
@@ -1080,7 +1090,7 @@ struct AttnTc {
       }
       if (!first) rescale(o_addr, f);
     }
-    const float mc = m == kNegInf ? 0.f : m * c;
+    const float mc = m == kNegInf ? 0.f : m * c - kUp;
     const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     auto weights = [&](const float* x, int col) {  // 32 columns from `col`
@@ -1091,7 +1101,7 @@ struct AttnTc {
         y.x = tc::ex2(y.x);
         y.y = tc::ex2(y.y);
         sum[e & 1] = __fadd2_rn(sum[e & 1], y);
-        p[e] = F8 ? tc::pack_f16(y.x, y.y) : bf_pack(y.x, y.y);
+        p[e] = F8 ? tc::pack_f16_sat(y.x, y.y) : bf_pack(y.x, y.y);
       }
       tc::st16(s_addr + col / 2, p);
     };
@@ -1193,7 +1203,7 @@ struct AttnTc {
             for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
             if (valid && !(cut && l == 0.f)) store32(x, to, k);
           }
-          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l)), to);
+          if (valid) store_z(l == 0.f ? kNegInf : m == kNegInf ? l : fmaf(m, c, log2f(l) - kUp), to);
         }
         if (again && busy) redo(it, w, first_row, first_row + 32, 1);
         if (own) {
@@ -1247,7 +1257,7 @@ struct AttnTc {
           f[p] = f[p] == kNegInf ? (lp[p] != 0.f ? 1.f : 0.f) : tc::ex2((f[p] - mm) * c);
           lt = fmaf(f[p], lp[p], lt);
         }
-        const float z = lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt));
+        const float z = lt == 0.f ? kNegInf : mm == kNegInf ? lt : fmaf(mm, c, log2f(lt) - kUp);
         const float inv = lt == 0.f ? 0.f : (cut ? 1.f : P.v_scale) / lt;
         const bool put = valid && !(cut && lt == 0.f);
         const uint32_t o0 = tmem + lanes + 2 * kAttnTile, o1 = o0 + DP;

@@ -598,3 +598,46 @@ def test_sequences_without_rows_outlast_no_wait(libqknorm, monkeypatch, new):
     torch.cuda.synchronize()
     assert binding.device_error_word() == 0
     assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("new", [1, 10, 60])
+def test_small_weights_over_an_fp8_cache(libqknorm, new):
+    """One key outweighs 1499 others by 2^26 each and holds zeros: what comes out is theirs alone.  A weight keeps at least an absolute
+    step of 2^-25 in fp16, where the largest stands for 2^7: 2^-32 of it instead of the 2^-25 that attention_bounds allows."""
+    b = Batch([new], [1500], 8, 1, 64, dtype=F8)
+    b.q.zero_()
+    b.q.view(b.T, 8, 64)[:, :, 0] = 9.0
+    b.k[:], b.v[:] = 0.0, 448.0
+    first = (b.table[0][0], 0)
+    b.k[first][0, 0], b.v[first] = 8.0, 0.0               # 9 * 8 * 0.25 = 18 = 25.97 ln 2
+    for dev, host in ((b.dq, b.q), (b.dk, b.k), (b.dv, b.v)):
+        dev.copy_(host.cuda())
+    kw = dict(scale=1.0, causal=False)
+    ref = b.reference(**kw)
+    out, lse = b.call(**kw)
+    tol, tol_lse = R.attention_bounds(ref, 64, True)
+    tol = tol[:new] - (2.0 ** -25 - 2.0 ** -32) * ref["V"][:new]
+    want = ref["out"][:new]
+    assert (want > 20 * tol).all()
+    assert (np.abs(out[:new].double().numpy().reshape(want.shape) - want) <= tol).all()
+    assert (np.abs(lse[:new].double().numpy() - ref["lse"][:new]) <= tol_lse[:new]).all()
+
+
+@BOTH
+@pytest.mark.parametrize("new", [1, 10, 60])
+def test_scores_beyond_their_own_precision(libqknorm, new, dtype):
+    """Scores of tens of millions, apart by less than their own fp32 step and then by far more: weights are coarse there, but finite and
+    never past the format they are rounded to."""
+    g = torch.Generator().manual_seed(9)
+    b = Batch([new], [700], 8, 1, 64, dtype=dtype)
+    b.q.fill_(2.0 ** 14)
+    grow = 240.0 + 16.0 * torch.arange(44).div(44).repeat_interleave(16)
+    for j in range(700):
+        b.k[b.table[0][j // 16], j % 16] = (grow[j] + torch.randint(0, 3, (64,), generator=g)).to(dtype)
+    b.dq.copy_(b.q.cuda())
+    b.dk.copy_(b.k.cuda())
+    b.dv.copy_(torch.nan_to_num(b.v.float()).to(dtype).cuda())
+    out, lse = b.call(scale=1.0, causal=False)
+    vmax = torch.nan_to_num(b.v.float()).abs().max().item() * b.vs
+    assert torch.isfinite(out[:new].float()).all() and torch.isfinite(lse[:new]).all()
+    assert (out[:new].float().abs() <= vmax * 1.01).all()
