@@ -35,6 +35,7 @@ EXPORTS = (
 
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
 NORM_NONE, NORM_LAYERWISE, NORM_HEADWISE = 0, 1, 2
+MAX_HEAD_DIM = 512  # QKNORM_MAX_HEAD_DIM
 
 _vp = ctypes.c_void_p
 _BF16, _F8 = torch.bfloat16, torch.float8_e4m3fn
@@ -85,6 +86,21 @@ def lib() -> ctypes.CDLL:
     return L
 
 
+def _refuse(status: int, message: str):
+    raise QKNormError(status, message)
+
+
+_SHAPE = binding.QKNORM_ERR_SHAPE
+
+
+def _int32(value, what: str) -> int:
+    """An int the C ABI's int32 holds: ctypes cuts off what it does not."""
+    value = int(value)
+    if not -0x80000000 <= value <= 0x7fffffff:
+        _refuse(_SHAPE, f"{what}: {value} does not fit 32 bits")
+    return value
+
+
 def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "plain", *, factor: float = 1.0,
                      original_len: float = 0.0, low: float = 1.0, high: float = 32.0, device="cuda") -> Tuple[torch.Tensor, float]:
     """qknorm_rope_frequencies: (inv_freq, mscale) -- radians per position of the rot_dim/2 pairs, a float64 tensor on
@@ -92,18 +108,14 @@ def rope_frequencies(rot_dim: int, theta: float = 10000.0, scaling: str = "plain
     original_len; 1 and 32 are usual) or bands (1 and 4 are usual)."""
     if scaling not in SCALINGS:
         raise QKNormError(binding.QKNORM_ERR_SHAPE, f"scaling must be one of {sorted(SCALINGS)}")
-    host = (ctypes.c_double * max(1, int(rot_dim) // 2))()
+    rot_dim = _int32(rot_dim, "rot_dim")
+    if rot_dim > MAX_HEAD_DIM:
+        _refuse(_SHAPE, f"rot_dim: at most {MAX_HEAD_DIM}")
+    host = (ctypes.c_double * max(1, rot_dim // 2))()
     mscale = ctypes.c_float(1.0)
-    _check(lib().qknorm_rope_frequencies(int(rot_dim), float(theta), SCALINGS[scaling], float(factor), float(original_len),
+    _check(lib().qknorm_rope_frequencies(rot_dim, float(theta), SCALINGS[scaling], float(factor), float(original_len),
                                          float(low), float(high), host, ctypes.byref(mscale)))
     return torch.tensor(list(host), dtype=torch.float64).to(device), float(mscale.value)
-
-
-def _refuse(status: int, message: str):
-    raise QKNormError(status, message)
-
-
-_SHAPE = binding.QKNORM_ERR_SHAPE
 
 
 def _device() -> int:
@@ -208,7 +220,7 @@ def qknorm_rope(q, k, positions, inv_freq, head_dim: int, out_q=None, out_k=None
         else:
             pok, _, ldok = _rows(out_k, T, "out_k", act, dev, dk)
     _invoke(L.qknorm_rope_e4m3 if act is _F8 else L.qknorm_rope,
-            (pq, pk, rot, T, dq, dk, int(head_dim), ldq, ldk, 1 if inverse else 0, poq, pok, ldoq, ldok), _current(stream),
+            (pq, pk, rot, T, dq, dk, _int32(head_dim, "head_dim"), ldq, ldk, 1 if inverse else 0, poq, pok, ldoq, ldok), _current(stream),
             (q, k, positions, inv_freq, out_q, out_k))
     return out_q, out_k
 
@@ -255,6 +267,9 @@ def qknorm_fwd_append(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_c
 def attn_paged_workspace(num_seqs: int, tokens: int, max_q: int, max_kv: int, heads_q: int, heads_kv: int, head_dim: int,
                          window: int = 0) -> int:
     """qknorm_attn_paged_workspace: bytes a call of these sizes needs on the current device."""
+    names = ("num_seqs", "max_q", "max_kv", "heads_q", "heads_kv", "head_dim", "window")
+    num_seqs, max_q, max_kv, heads_q, heads_kv, head_dim, window = map(
+        _int32, (num_seqs, max_q, max_kv, heads_q, heads_kv, head_dim, window), names)
     return _workspace(torch.cuda.current_device(), num_seqs, tokens, max_q, max_kv, heads_q, heads_kv, head_dim, window)
 
 
@@ -282,7 +297,7 @@ def qknorm_attn_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q
     pq, dq, ldq = _rows(q, T, "q", _BF16, dev)
     if dq == 0 or dq % hd != 0:
         _refuse(binding.QKNORM_ERR_HEADS, f"q: {dq} columns are no whole number of heads of {hd}")
-    hq, max_q, max_kv, window = dq // hd, int(max_q), int(max_kv), int(window)
+    hq, max_q, max_kv, window = dq // hd, _int32(max_q, "max_q"), _int32(max_kv, "max_kv"), _int32(window, "window")
     if not isinstance(kv_lens, torch.Tensor) or kv_lens.dim() != 1:
         _refuse(_SHAPE, "kv_lens: expected a 1-D int32 CUDA tensor")
     B = kv_lens.shape[0]

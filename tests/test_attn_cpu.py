@@ -292,3 +292,39 @@ def test_append_finds_every_meeting_of_k_and_v(lib):
         assert append(lib, c=c, dq=0, q=None, oq=None, gq=None) == want, (n, hd, stride, off)
         seen[want] += 1
     assert min(seen.values()) > 500
+
+
+def test_python_integers_past_32_bits_are_refused(lib, monkeypatch):
+    """ctypes would cut them off without a word: a window of 2^32 + 1 would be one of 1."""
+    import torch
+    from paper_2608_09160_b200.binding import QKNormError
+    monkeypatch.setattr(attn, "_device", lambda: -1)            # CPU tensors pass the checks; no call gets as far as a kernel
+    monkeypatch.setattr(attn, "_current", lambda stream: 0)
+    monkeypatch.setattr(attn, "_workspace", lambda *sizes: 0)
+    calls = []
+    monkeypatch.setattr(attn, "_invoke", lambda fn, args, stream, keep: calls.append(args))
+    bf, i32 = torch.bfloat16, torch.int32
+    q, pool = torch.zeros((4, 128), dtype=bf), torch.zeros((2, 16, 1, 64), dtype=bf)
+    table, lens, starts = torch.zeros((2, 1), dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(3, dtype=i32)
+    go = lambda max_q=2, max_kv=16, **kw: attn.qknorm_attn_paged(q, pool, pool.clone(), table, lens, starts, max_q, max_kv, **kw)
+    go()
+    assert len(calls) == 1
+    for kw in (dict(window=2 ** 32 + 1), dict(window=2 ** 31), dict(window=-2 ** 40), dict(max_q=2 ** 32), dict(max_kv=2 ** 32 + 16), dict(max_kv=-2 ** 33)):
+        with pytest.raises(QKNormError) as e:
+            go(**kw)
+        assert e.value.status == binding.QKNORM_ERR_SHAPE, kw
+    pos, inv = torch.zeros(4, dtype=torch.int64), torch.zeros(32, dtype=torch.float64)
+    attn.qknorm_rope(q, None, pos, inv, 64)
+    assert len(calls) == 2
+    with pytest.raises(QKNormError):
+        attn.qknorm_rope(q, None, pos, inv, 2 ** 32 + 64)
+    with pytest.raises(QKNormError):
+        attn.rope_frequencies(2 ** 32 + 64, device="cpu")
+    assert len(calls) == 2
+    monkeypatch.undo()
+    for i in (0, 2, 3, 4, 5, 6, 7):
+        sizes = [4, 8, 2, 64, 8, 2, 64, 0]
+        sizes[i] += 2 ** 32
+        with pytest.raises(QKNormError) as e:
+            attn.attn_paged_workspace(*sizes)
+        assert e.value.status == binding.QKNORM_ERR_SHAPE, sizes
