@@ -159,7 +159,7 @@ int qknorm_attn_paged(const void* q, int64_t ld_q, const qknorm_paged_cache* cac
                       int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* workspace,
                       int64_t workspace_bytes, void* stream);
 
-/* Bytes of workspace the call needs on the current device (0 is possible); HOST, written. */
+/* Bytes of workspace that a call of these sizes needs on the current device, causal or not (0 is possible); HOST, written. */
 int qknorm_attn_paged_workspace(int32_t num_seqs, int64_t tokens, int32_t max_q, int32_t max_kv, int32_t heads_q,
                                 int32_t heads_kv, int32_t head_dim, int32_t window, int64_t* bytes);
 

@@ -494,7 +494,8 @@ struct AttnPlan {
   bool cuts = false;  // some unit may be cut between CTAs
 };
 
-AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, int window, int sms) {
+AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, bool causal, int window,
+                   int sms) {
   AttnPlan p;
   const int group = heads_q / heads_kv;
   p.tc = head_dim % 8 == 0 && head_dim <= 128 && group <= kAttnTile;
@@ -507,7 +508,9 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   p.q_items = (max_q + per_item - 1) / per_item;
   int64_t tiles = (max_keys + kAttnTile - 1) / kAttnTile;  // of a unit, at most
   if (window > 0) {
-    const int64_t span = ((int64_t)window + per_item - 1 + kAttnTile - 2) / kAttnTile + 1;
+    // its first row's window, and the keys that its later rows see beyond: as many as there are rows -- or, without the causal edge, all
+    // up to the sequence's end, which the sequence's first unit has the most of
+    const int64_t span = ((int64_t)window + (causal ? per_item : max_q) - 1 + kAttnTile - 2) / kAttnTile + 1;
     if (span < tiles) tiles = span;
   }
   // One CTA per SM, and none for less than two tiles.  Units that a batch of T rows can have:
@@ -552,7 +555,10 @@ int run_attn_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, i
   const DeviceInfo* dev = nullptr;
   rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
-  *bytes = attn_workspace(plan_attn(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window, dev->sm_count), head_dim);
+  for (const bool causal : {true, false}) {  // enough for either
+    const int64_t need = attn_workspace(plan_attn(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, causal, window, dev->sm_count), head_dim);
+    if (need > *bytes) *bytes = need;
+  }
   return QKNORM_OK;
 }
 
@@ -580,7 +586,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   const DeviceInfo* dev = nullptr;
   rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
-  AttnPlan plan = plan_attn(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, window, dev->sm_count);
+  AttnPlan plan = plan_attn(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, causal != 0, window, dev->sm_count);
   const bool aligned = (((uintptr_t)q) | ((uintptr_t)out) | ((uintptr_t)P.ld_q * 2) | ((uintptr_t)P.ld_out * 2)) % 16 == 0 && f.vec16 &&
                        (!cache->e4m3 || cache->head_dim % 16 == 0);
   const char* force = env_str("QKNORM_FORCE_VARIANT");

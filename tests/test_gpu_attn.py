@@ -641,3 +641,20 @@ def test_scores_beyond_their_own_precision(libqknorm, new, dtype):
     vmax = torch.nan_to_num(b.v.float()).abs().max().item() * b.vs
     assert torch.isfinite(out[:new].float()).all() and torch.isfinite(lse[:new]).all()
     assert (out[:new].float().abs() <= vmax * 1.01).all()
+
+
+@BOTH
+def test_window_without_the_causal_edge_is_shared_out(libqknorm, dtype):
+    """With causal=False a row sees every key behind its window's start, so the first of several units has all of the sequence: it is
+    cut (two launches), and a workspace that was asked for without saying causal or not does for both."""
+    b = Batch([2048], [2048], 1, 1, 64, dtype=dtype)
+    n0 = binding.launch_count()
+    b.check("attn_tc", causal=False, window=64)
+    assert binding.launch_count() - n0 == 2
+    need = attn.attn_paged_workspace(1, b.T, 2048, 2048, 1, 1, 64, window=64)
+    assert need > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for causal in (True, False):
+        out, lse = b.call(causal=causal, window=64, workspace=ws)
+        b.compare(out, lse, b.reference(causal=causal, window=64))
+    Batch([700, 3, 500], [900, 40, 500], 4, 2, 64, dtype=dtype).check("attn_tc", causal=False, window=130)
