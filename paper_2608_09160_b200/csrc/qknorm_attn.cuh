@@ -16,6 +16,8 @@ namespace qknorm {
 constexpr int kAttnTile = 128;       // keys per tile, rows per query tile
 constexpr int kAttnMaxEpl = 16;      // head_dim elements per lane of the row routine: QKNORM_MAX_HEAD_DIM / 32
 constexpr float kNegInf = -__builtin_huge_valf();
+// c is never 0, which a product with the -inf of a masked score would make NaN; this is the least fp32 value
+constexpr float kAttnLeastC = 1.401298464e-45f;
 
 struct AttnSide {
   const void* base;

@@ -642,7 +642,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.heads_kv = cache->heads;
   P.group = heads_q / cache->heads;
   P.head_dim = cache->head_dim;
-  P.c = scale * (cache->e4m3 ? cache->k_scale : 1.0f) * 1.44269504088896340736f;
+  P.c = fmaxf((float)((double)scale * (cache->e4m3 ? cache->k_scale : 1.0f) * 1.44269504088896340736), kAttnLeastC);
   P.v_scale = cache->e4m3 ? cache->v_scale : 1.0f;
   P.causal = causal;
   P.window = window;

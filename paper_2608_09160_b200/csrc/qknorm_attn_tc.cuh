@@ -958,7 +958,7 @@ struct AttnTc {
   // c of this row's scores: an FP8 cache's Q rows had an exponent taken out
   __device__ __forceinline__ float row_c(int set, int row) const {
     const int e = reinterpret_cast<const volatile unsigned char*>(smem_ptr + L::kQScale)[set * 128 + row];
-    return e == 0 ? P.c : ldexpf(P.c, e - 135);
+    return e == 0 ? P.c : fmaxf(ldexpf(P.c, e - 135), kAttnLeastC);
   }
 
   // ---- softmax --------------------------------------------------------------------------------------

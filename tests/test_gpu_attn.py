@@ -658,3 +658,28 @@ def test_window_without_the_causal_edge_is_shared_out(libqknorm, dtype):
         out, lse = b.call(causal=causal, window=64, workspace=ws)
         b.compare(out, lse, b.reference(causal=causal, window=64))
     Batch([700, 3, 500], [900, 40, 500], 4, 2, 64, dtype=dtype).check("attn_tc", causal=False, window=130)
+
+
+@pytest.mark.parametrize("variant", ["attn_tc", "attn_general"])
+@pytest.mark.parametrize("new", [1, 10, 60])
+def test_scales_so_small_that_every_key_counts_alike(libqknorm, new, variant):
+    """scale * k_scale below what fp32 holds, or brought there by a tiny query row: the weights of the keys a row sees are equal."""
+    b = Batch([new], [200], 8, 1, 64 if variant == "attn_tc" else 56, dtype=F8)
+    b.check(variant, scale=1e-45)
+    b.q.copy_((b.q.double() * 2.0 ** -112).to(BF16))
+    b.dq.copy_(b.q.cuda())
+    b.check(variant, scale=1e-10)
+    b.check(variant, scale=2.0 ** -30)
+
+
+@BOTH
+@pytest.mark.parametrize("new", [1, 10, 60])
+def test_no_keys_at_all(libqknorm, new, dtype):
+    """max_kv = 0, and a block table without columns: every row is empty."""
+    b = Batch([new, new], [200, 3], 8, 1, 64, dtype=dtype)
+    for _ in range(2):
+        out, lse = b.call(max_kv=0)
+        assert (out[:2 * new] == 0).all() and torch.isneginf(lse[:2 * new]).all() and (out[2 * new:] == 7.0).all()
+        b.dtable = b.dtable[:, :0].contiguous()
+    out, lse = b.call()
+    assert (out[:2 * new] == 0).all() and torch.isneginf(lse[:2 * new]).all() and (out[2 * new:] == 7.0).all()
