@@ -141,7 +141,7 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  *   lse          [tokens, heads_q] fp32 or NULL: log(sum_j exp(scale q.k_j))
  *   workspace    device, 16-byte aligned, at least qknorm_attn_paged_workspace(...) bytes; its contents mean nothing
  *                between calls.  Two calls that may run at the same time need one each.
- *   out and lse may not overlap any other buffer of the call.  scale > 0.
+ *   out and lse may not overlap any other buffer of the call.  scale > 0; scale (times k_scale) times log2(e) has to fit fp32.
  *   Rows of out and lse outside every sequence are not written, and such rows of q do not matter.
  *   Keys, values that a row does not see have no influence on it, whatever they hold (NaN and infinities too);
  *   a row whose every visible score is -inf gets zeros.  An infinite value that a row does see makes that element infinite or NaN.

@@ -572,6 +572,8 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   rc = check_attn_sizes(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, window);
   if (rc != QKNORM_OK) return rc;
   if (!(scale > 0.0f) || !isfinite(scale)) return QKNORM_ERR_SHAPE;
+  const float c = (float)((double)scale * (cache->e4m3 ? cache->k_scale : 1.0f) * 1.44269504088896340736);
+  if (!isfinite(c)) return QKNORM_ERR_SHAPE;
   if (causal != 0 && causal != 1) return QKNORM_ERR_SHAPE;
   if (table_cols < 0 || ld_table < 0 || (ld_table != 0 && ld_table < table_cols)) return QKNORM_ERR_SHAPE;
   AttnParams P;
@@ -642,7 +644,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.heads_kv = cache->heads;
   P.group = heads_q / cache->heads;
   P.head_dim = cache->head_dim;
-  P.c = fmaxf((float)((double)scale * (cache->e4m3 ? cache->k_scale : 1.0f) * 1.44269504088896340736), kAttnLeastC);
+  P.c = fmaxf(c, kAttnLeastC);
   P.v_scale = cache->e4m3 ? cache->v_scale : 1.0f;
   P.causal = causal;
   P.window = window;

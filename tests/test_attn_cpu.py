@@ -328,3 +328,12 @@ def test_python_integers_past_32_bits_are_refused(lib, monkeypatch):
         with pytest.raises(QKNormError) as e:
             attn.attn_paged_workspace(*sizes)
         assert e.value.status == binding.QKNORM_ERR_SHAPE, sizes
+
+
+def test_scales_whose_product_no_float_holds_are_refused(lib):
+    assert attention(lib, c=cache(e4m3=1, ks=1e20), scale=1e30) == binding.QKNORM_ERR_SHAPE
+    assert attention(lib, scale=3e38) == binding.QKNORM_ERR_SHAPE            # times log2 e
+    import torch
+    if not torch.cuda.is_available():
+        assert attention(lib, c=cache(ks=1e20), scale=1e30) == binding.QKNORM_ERR_CUDA      # a bf16 cache has no scale
+        assert attention(lib, c=cache(e4m3=1, ks=1e-30), scale=1e-30) == binding.QKNORM_ERR_CUDA
