@@ -115,7 +115,7 @@ typedef enum {
  *   [0, num_pages * page_size), -1 for instance, writes nothing to the cache (a padded token); its q row is written.
  *   out_q [tokens, dq] bf16; may be exactly q.  dq == 0: no q.
  * Nothing is rounded between the steps: norm, rotation and division by the cache's scale (as a
- * product with its fp32 reciprocal) are fp32.
+ * product with its fp32 reciprocal, which has to be finite) are fp32.
  */
 int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* gamma_q, const void* gamma_k,
                       int32_t norm, float eps, const qknorm_rotation* rot, const int64_t* slots,

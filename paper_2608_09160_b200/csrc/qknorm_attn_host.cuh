@@ -316,6 +316,7 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
   if (dq % hd != 0) return QKNORM_ERR_HEADS;
   if (norm < kNormNone || norm > kNormHead) return QKNORM_ERR_SHAPE;
   if (norm != kNormNone && !(eps >= 0.0f)) return QKNORM_ERR_EPS;
+  if (cache->e4m3 && (!isfinite(1.0f / cache->k_scale) || !isfinite(1.0f / cache->v_scale))) return QKNORM_ERR_SHAPE;
   RopeParams R;
   memset(&R, 0, sizeof(R));
   if ((rc = row_stride(ld_q, dq, &R.q.ldx)) || (rc = row_stride(ld_oq, dq, &R.q.ldy)) || (rc = row_stride(ld_k, dk, &R.k.ldx)) ||

@@ -337,3 +337,14 @@ def test_scales_whose_product_no_float_holds_are_refused(lib):
     if not torch.cuda.is_available():
         assert attention(lib, c=cache(ks=1e20), scale=1e30) == binding.QKNORM_ERR_CUDA      # a bf16 cache has no scale
         assert attention(lib, c=cache(e4m3=1, ks=1e-30), scale=1e-30) == binding.QKNORM_ERR_CUDA
+
+
+def test_append_refuses_scales_without_a_reciprocal(lib):
+    """1 / 1e-39 is no fp32 number: zeros would be written as NaN."""
+    for kw in (dict(ks=1e-39), dict(vs=1e-39)):
+        assert append(lib, c=cache(e4m3=1, **kw)) == binding.QKNORM_ERR_SHAPE, kw
+    import torch
+    if not torch.cuda.is_available():
+        assert append(lib, c=cache(e4m3=1, ks=1e-37)) == binding.QKNORM_ERR_CUDA
+        assert append(lib, c=cache(ks=1e-39)) == binding.QKNORM_ERR_CUDA     # a bf16 cache has no scale
+        assert attention(lib, c=cache(e4m3=1, ks=1e-39)) == binding.QKNORM_ERR_CUDA   # reading multiplies
