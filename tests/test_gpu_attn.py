@@ -533,19 +533,23 @@ def test_gathered_rows_are_the_copied_ones(libqknorm, new, kv, hd, dtype):
         assert torch.equal(out.view(torch.int16), want.view(torch.int16)) and torch.equal(lse, want_lse)
 
 
+# The tests of the waits lower their limit, but not below a few milliseconds: a whole GPU stands still for 1.8 ms now and then (seen
+# once in eight seconds: nothing in any CTA moved for that long), and a wait cannot tell that from something that hangs.
+
+
 @BOTH
 @pytest.mark.parametrize("new", [4, 10, 40])
 def test_rows_done_again_outlast_no_wait(libqknorm, monkeypatch, new, dtype):
     """Rows whose tile holds an infinity that they do not see are done again key by key, which takes far longer than the matrix
-    path.  With the limit of a wait lowered to one millisecond, below that: everybody waits on, and the rows of the batch's other
-    sequences come out as ever."""
+    path: 30 to 300 ms here.  With the limit of a wait below that: everybody waits on, and the rows of the batch's other sequences come
+    out as ever."""
     seqs, keys, hq, hk, hd = 20, 6000, 64, 8, 64
     b = Batch([new] * seqs, [keys] * seqs, hq, hk, hd, dtype=dtype)
     want, want_lse = b.call()
     vmax = b.v.float().nan_to_num(0.0).abs().amax().item() * b.vs     # unused slots are NaN
     b.v[b.table[0][(keys - 1) // 16], (keys - 1) % 16] = float("nan") if dtype is F8 else float("inf")
     b.dv.copy_(b.v.cuda())                                            # seen by the sequence's last token only
-    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "1000")
+    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "10000")
     out, lse = b.call()                                               # looks at the error word, too
     n = new * seqs
     assert torch.equal(out[new:n].view(torch.int16), want[new:n].view(torch.int16)) and torch.equal(lse[new:n], want_lse[new:n])
@@ -561,10 +565,10 @@ def test_rows_done_again_outlast_no_wait(libqknorm, monkeypatch, new, dtype):
 @BOTH
 @pytest.mark.parametrize("new,group,seqs", [(1, 8, 450), (10, 8, 450), (40, 8, 450)])
 def test_long_items_outlast_no_wait(libqknorm, monkeypatch, new, group, seqs, dtype):
-    """Units of 2048 key tiles (one page over and over), three a CTA: each takes about two milliseconds, and the rows of the one
-    after the next wait for it with a limit of a fifth of a millisecond."""
+    """Units of 32768 key tiles (three pages over and over), three a CTA: each takes 16 ms or more, and the rows of the one after the
+    next wait for it with a limit of five."""
     g = torch.Generator().manual_seed(4)
-    keys, page, hd = 1 << 18, 64, 64
+    keys, page, hd = 1 << 22, 64, 64
     k, v = (torch.randn((3, page, 1, hd), generator=g).to(dtype).cuda() for _ in range(2))
     table = torch.arange(keys // page, dtype=torch.int32).remainder(3).expand(seqs, -1).contiguous().cuda()
     lens = torch.full((seqs,), keys, dtype=torch.int32, device="cuda")
@@ -573,18 +577,17 @@ def test_long_items_outlast_no_wait(libqknorm, monkeypatch, new, group, seqs, dt
     go = lambda: attn.qknorm_attn_paged(q, k, v, table, lens, starts, new, keys)
     want = go()
     torch.cuda.synchronize()
-    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "200")
+    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "5000")
     out = go()
     torch.cuda.synchronize()
     assert binding.device_error_word() == 0
     assert torch.equal(out.view(torch.int16), want.view(torch.int16))
 
 
-@pytest.mark.parametrize("new", [1, 300])
-def test_sequences_without_rows_outlast_no_wait(libqknorm, monkeypatch, new):
-    """Hundreds of thousands of sequences without new tokens between two that have some: passing by them takes milliseconds, the limit
-    of a wait is a fifth of one."""
-    seqs, hd = 400_000, 64
+@pytest.mark.parametrize("new,seqs", [(1, 4_000_000), (300, 400_000)])
+def test_sequences_without_rows_outlast_no_wait(libqknorm, monkeypatch, new, seqs):
+    """Millions of sequences without new tokens between two that have some: passing by them takes 20 ms, the limit of a wait is five."""
+    hd = 64
     g = torch.Generator().manual_seed(5)
     k, v = (torch.randn((4, 16, 1, hd), generator=g).to(BF16).cuda() for _ in range(2))
     q = torch.randn((2 * new, hd), generator=g).to(BF16).cuda()
@@ -593,7 +596,7 @@ def test_sequences_without_rows_outlast_no_wait(libqknorm, monkeypatch, new):
     lens = torch.full((seqs,), 40, dtype=torch.int32, device="cuda")
     table = torch.tensor([2, 0, 3], dtype=torch.int32, device="cuda").expand(seqs, -1).contiguous()
     want = attn.qknorm_attn_paged(q, k, v, table[:2], lens[:2], starts[[0, 1, -1]].contiguous(), new, 40)
-    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "200")
+    monkeypatch.setenv("QKNORM_ATTN_WAIT_US", "5000")
     out = attn.qknorm_attn_paged(q, k, v, table, lens, starts, new, 40)
     torch.cuda.synchronize()
     assert binding.device_error_word() == 0
