@@ -7,8 +7,8 @@
  * caller owns every buffer, work is enqueued on `stream` without synchronising, a qknorm_status
  * comes back, nothing is launched on an error, calls may be captured into CUDA graphs and may run
  * at the same time on different streams (each attention call with a workspace of its own).
- * All arithmetic is fp32 (angles: fp64), every result is rounded once to its storage format, to nearest even
- * (FP8-E4M3: saturating at +-448).  Results are bitwise reproducible run to run, except where two
+ * Arithmetic is fp32 (angles: fp64), every result is rounded once to its storage format, to nearest even
+ * (FP8-E4M3: saturating at +-448); the matrix products of attention take rounded softmax weights, see qknorm_attn_paged.  Results are bitwise reproducible run to run, except where two
  * tokens of one call name the same cache slot (each value there is then one of theirs).
  *
  * Rows are tokens: q is [tokens, dq] with dq = heads * head_dim, row t starts ld_q ELEMENTS after
@@ -151,7 +151,12 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  * the keys of a row in two or more, the parts lie in the workspace and a second launch joins them (otherwise no workspace
  * is asked for).  A wait inside "attn_tc" that runs out -- two seconds in which nothing else in its CTA moved -- sets the device's error
  * word (qknorm_device_error_word): 7 a tile or a product did not come, 9 a copy did not land before the CTA ended; 8: shared memory is not
- * aligned.  Rows done again because a tile holds a value that they must not see take about half a microsecond a key.
+ * aligned.  Rows that are done again because a tile holds a value that they must not see take about 1.2 us a key, up to 32 rows in turn.
+ *
+ * Rounding in "attn_tc": scores, maxima, sums and the accumulated output are fp32.  The weights are rounded for the product with V: to
+ * bf16 (half a step: 2^-8 relative) over a bf16 cache, to fp16 over an FP8 one (2^-11 relative, and at least 2^-32 of the row's largest weight).
+ * Over an FP8 cache the queries are brought to fp16, a power of two taken out of each row first: exact but for parts below 2^-30 of
+ * the row's largest element.  "attn_general" rounds neither.
  */
 int qknorm_attn_paged(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* block_table,
                       int32_t table_cols, int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts,

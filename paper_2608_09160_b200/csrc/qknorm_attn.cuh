@@ -256,7 +256,14 @@ struct AttnStart {
 };
 
 // A cut costs its unit a part more and the join; it is worth that where shares are long.  Short shares (few tiles on many SMs) only
-// cut units that weigh more than 16: a cut in a shorter one goes to the nearer end.
+// cut units that weigh more than 16: a cut in a shorter one goes to the nearer end.  Both sides, single tokens, 8 key heads of 8 query heads
+// of 128, us in a captured graph, units whole | cut:
+//   sequences            1            4            8           12           18           19           30           37
+//    500 keys   11.6 | 16.5  12.1 | 17.4  12.3 | 18.3  12.8 | 20.0  14.8 | 18.3  21.4 | 25.2  22.3 | 30.7  22.7 | 27.0
+//   1000 keys   16.6 | 15.7  17.2 | 16.8  18.5 | 20.7  19.4 | 24.7  21.1 | 24.9  31.7 | 30.0  33.1 | 38.5  34.2 | 38.5
+//   1900 keys   25.1 | 17.4  27.2 | 18.7  29.2 | 26.3  29.1 | 31.7  31.6 | 35.0  50.2 | 40.9  52.6 | 54.1  59.4 | 59.2
+// (1 key head: 1000 keys 16.5 | 15.5, 1900 keys 25.5 | 17.5 up to 24 sequences.)  So 16 is right, or within 2 us, for units up to 8 tiles and for batches that
+// give most SMs one unit; for 9 to 16 tiles it loses up to 9 us to cuts where there are fewer than 64 units, and just above one unit an SM.
 constexpr int kAttnWhole = 16;
 __host__ __device__ __forceinline__ int attn_snap(long long share, int own, int weight) {
   return share < 32 && weight <= kAttnWhole ? (weight + 1) / 2 : own;

@@ -24,9 +24,10 @@
 //                       parts of a row are joined through shared memory at the end of the item.
 // The first two keep the tensor pipe on one warpgroup's tile while the other one is in its exponentials.
 //
-// Rows no token fills, keys outside the item's range and head_dim up to the next multiple of 64 are zeros in
-// shared memory, never memory of somebody else.  Inside a tile that the causal edge or the window cuts, a V row with an
-// infinity or a NaN would reach rows that do not see it (0 * inf): the loader looks at the V rows of such
+// What shared memory holds beside the item's own: zeros in V rows outside the item's keys and in the columns behind head_dim, up to the
+// next multiple of 64.  K rows outside the keys hold whatever the page holds there (their scores are masked), Q rows that no token fills
+// hold other sequences' queries or what was there before (their results are stored nowhere).  Inside a tile that the causal
+// edge or the window cuts, a V row with an infinity or a NaN would reach rows that do not see it (0 * inf): the loader looks at the V rows of such
 // tiles and, if it finds one, has the item's rows done again one by one by attn_row, spread over the softmax warps that have them.
 //
 // Every wait is bounded: when for two seconds nothing has moved in the CTA -- 64 score tiles, 64 keys of a row done again, 64 items
@@ -44,12 +45,14 @@
 // outweighs its row's others by 2^26 left them out of O and in l.)  Otherwise only the output is rounded; sums, maxima and O are fp32.
 //
 // What bounds it (B200; calls in a captured graph, 6448 GB/s and 1676 TFLOP/s measured copy and matrix rates):
-//   single tokens, bf16   HBM: 64 sequences to 8192 keys, 64 query and 8 key heads: 230 us, 5.9 TB/s
+//   single tokens, bf16   HBM: 64 sequences to 8192 keys, 64 query and 8 key heads: 233 us, 5.8 TB/s (268 us after a second of nothing
+//                         else, when the power limit has brought the clock from 1965 to 1515 MHz)
 //   single tokens, FP8    the tile workers and shared memory (a K and a V tile are written, read, written as fp16 and read by
-//                         the products: 224 KB of 128-byte-a-cycle traffic): 16 sequences to 32000 keys: 195 us, floor 102
-//   few short sequences   latency: about 5 us until the first product, then a tile each 0.9 us: 8 x 1000 keys: 17.3 us, floor 3.3
-//   chunks and prompts    exponentials and products of two tiles in turn, 3700 cycles a pair of 128 x 128 (products alone 2048),
-//                         and 8 to 10 thousand cycles a unit for its first and last steps: 8192 tokens, 40 heads: 680 us, floor 410
+//                         the products: 224 KB of 128-byte-a-cycle traffic): 16 sequences to 32000 keys: 199 us (217 at 1770 MHz), floor 102
+//   few short sequences   latency: about 5 us until the first product, then a tile each 0.9 us: 8 x 1000 keys: 17.1 us, floor 3.3
+//   chunks and prompts    exponentials and products of two tiles in turn, 3700 cycles a pair of 128 x 128 (products alone 2048,
+//                         exponentials alone as many), and 8 to 10 thousand cycles a unit for its first and last steps: 8192 tokens, 40 heads:
+//                         675 us (765 at 1740 MHz), floor 410; over an FP8 cache 1215, for the widening
 // Tiles of 128 x 128: the largest M of one CTA's products, and two score tiles and two O of 128 columns fill the 512 columns of TMEM.
 #pragma once
 #include "qknorm_attn.cuh"
