@@ -686,3 +686,15 @@ def test_no_keys_at_all(libqknorm, new, dtype):
         b.dtable = b.dtable[:, :0].contiguous()
     out, lse = b.call()
     assert (out[:2 * new] == 0).all() and torch.isneginf(lse[:2 * new]).all() and (out[2 * new:] == 7.0).all()
+
+
+@BOTH
+@pytest.mark.parametrize("new", [[1, 1], [10, 3], [70, 300]])
+def test_the_largest_bounds(libqknorm, new, dtype):
+    """max_q, max_kv and the window at the ends of their ranges say nothing about the batch: the same results, within the workspace asked for."""
+    kv = [300, 500]
+    b = Batch(new, kv, 4, 2, 64, dtype=dtype)
+    for causal in (True, False):
+        for kw in (dict(max_kv=0x7fffff00), dict(max_q=2 ** 31 - 1), dict(window=2 ** 31 - 1), dict(max_q=2 ** 31 - 1, max_kv=0x7fffff00, window=2 ** 31 - 1)):
+            out, lse = b.call(causal=causal, **kw)
+            b.compare(out, lse, b.reference(causal=causal))
