@@ -8,7 +8,8 @@
  * comes back, nothing is launched on an error, calls may be captured into CUDA graphs and may run
  * at the same time on different streams (each attention call with a workspace of its own).
  * Arithmetic is fp32 (angles: fp64), every result is rounded once to its storage format, to nearest even
- * (FP8-E4M3: saturating at +-448); the matrix products of attention take rounded softmax weights, see qknorm_attn_paged.  Results are bitwise reproducible run to run, except where two
+ * (FP8-E4M3: saturating at +-448); the matrix products of attention take rounded softmax weights, see
+ * qknorm_attn_paged.  Results are bitwise reproducible run to run, except where two
  * tokens of one call name the same cache slot (each value there is then one of theirs).
  *
  * Rows are tokens: q is [tokens, dq] with dq = heads * head_dim, row t starts ld_q ELEMENTS after
@@ -141,7 +142,8 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  *   lse          [tokens, heads_q] fp32 or NULL: log(sum_j exp(scale q.k_j))
  *   workspace    device, 16-byte aligned, at least qknorm_attn_paged_workspace(...) bytes; its contents mean nothing
  *                between calls.  Two calls that may run at the same time need one each.
- *   out and lse may not overlap any other buffer of the call.  scale > 0; scale (times k_scale) times log2(e) has to fit fp32.
+ *   out and lse may not overlap any other buffer of the call.  scale > 0; scale (times k_scale) times log2(e) has to fit
+ *   fp32 (QKNORM_ERR_SHAPE), and so have the scores times it, which is not checked.
  *   Rows of out and lse outside every sequence are not written, and such rows of q do not matter.
  *   Keys, values that a row does not see have no influence on it, whatever they hold (NaN and infinities too);
  *   a row whose every visible score is -inf gets zeros.  An infinite value that a row does see makes that element infinite or NaN.
