@@ -30,6 +30,8 @@ extern "C" {
 
 #define QKNORM_MAX_HEAD_DIM 512      /* largest head_dim of the entry points below */
 #define QKNORM_MAX_KEYS 0x7fffff00   /* largest max_kv of qknorm_attn_paged */
+#define QKNORM_MAX_HEAD_DIM_E2M1 256 /* largest head_dim of a 4-bit cache */
+#define QKNORM_MAX_AXES 8            /* largest num_axes of a rotation with several axes */
 
 /* How the frequencies of qknorm_rope_frequencies are scaled for contexts longer than trained on. */
 typedef enum {
@@ -169,6 +171,90 @@ int qknorm_attn_paged(const void* q, int64_t ld_q, const qknorm_paged_cache* cac
 /* Bytes of workspace that a call of these sizes needs on the current device, causal or not (0 is possible); HOST, written. */
 int qknorm_attn_paged_workspace(int32_t num_seqs, int64_t tokens, int32_t max_q, int32_t max_kv, int32_t heads_q,
                                 int32_t heads_kv, int32_t head_dim, int32_t window, int64_t* bytes);
+
+/*
+ * Rotary positions with several axes: images and video place a token by time, height and width at once, and every
+ * pair of a head turns by one of them.  Pair i turns by positions[axis[i]][t] * inv_freq[i]; all else is as in qknorm_rotation.
+ */
+typedef struct {
+  const int64_t* positions; /* [num_axes][tokens], device, an axis' positions ld_positions elements after the last's */
+  int64_t ld_positions;     /* 0 = tokens */
+  const double* inv_freq;   /* [rot_dim/2], device */
+  const uint8_t* axis;      /* [rot_dim/2], device; a pair whose axis is num_axes or more stands at position 0.  NULL: axis 0 for all */
+  int32_t num_axes;         /* 1 .. QKNORM_MAX_AXES */
+  int32_t rot_dim;          /* even, 0 .. head_dim; 0 = no rotation (the pointers are ignored) */
+  int32_t interleaved;
+  float mscale;
+} qknorm_rotation_axes;
+
+/* qknorm_rope, qknorm_rope_e4m3 and qknorm_fwd_append with such a rotation (inverse = 1 is the backward pass here too). */
+int qknorm_rope_axes(const void* q, const void* k, const qknorm_rotation_axes* rot, int64_t tokens, int32_t dq, int32_t dk,
+                     int32_t head_dim, int64_t ld_q, int64_t ld_k, int32_t inverse, void* out_q, void* out_k,
+                     int64_t ld_out_q, int64_t ld_out_k, void* stream);
+int qknorm_rope_axes_e4m3(const void* q, const void* k, const qknorm_rotation_axes* rot, int64_t tokens, int32_t dq,
+                          int32_t dk, int32_t head_dim, int64_t ld_q, int64_t ld_k, int32_t inverse, void* out_q,
+                          void* out_k, int64_t ld_out_q, int64_t ld_out_k, void* stream);
+int qknorm_fwd_append_axes(const void* q, const void* k, const void* v, const void* gamma_q, const void* gamma_k,
+                           int32_t norm, float eps, const qknorm_rotation_axes* rot, const int64_t* slots,
+                           const qknorm_paged_cache* cache, int64_t tokens, int32_t dq, int64_t ld_q, int64_t ld_k,
+                           int64_t ld_v, void* out_q, int64_t ld_out_q, void* stream);
+
+/*
+ * A paged cache in 4 bits.  16 consecutive elements of a head are a block: sixteen E2M1 codes (sign, two exponent bits,
+ * one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) and one E4M3 scale; an element of K stands for
+ * code * scale * k_scale.  k and v hold head_dim/2 bytes per token and head, element 2i in the low four bits of byte i;
+ * k_scales and v_scales head_dim/16 bytes.  All strides are in BYTES; any order of the axes, with gaps, as in qknorm_paged_cache.
+ *   head_dim: a multiple of 16 up to QKNORM_MAX_HEAD_DIM_E2M1.
+ *   k and v with their strides: multiples of 8 bytes (of 16 for the faster copies, head_dim a multiple of 32 then).
+ *   k_scales and v_scales with theirs: multiples of the largest power of two up to 8 that divides head_dim/16.
+ * A page whose heads lie one after the other (strides: head > token) reads fastest.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  void* k_scales;
+  void* v_scales;
+  int64_t k_page, k_token, k_head;
+  int64_t v_page, v_token, v_head;
+  int64_t ks_page, ks_token, ks_head;
+  int64_t vs_page, vs_token, vs_head;
+  int64_t num_pages;
+  int32_t page_size;
+  int32_t heads;
+  int32_t head_dim;
+  float k_scale, v_scale;
+} qknorm_paged_cache_e2m1;
+
+/*
+ * qknorm_fwd_append_e2m1 -- qknorm_fwd_append into a 4-bit cache; rot may be NULL.
+ * With y = x / k_scale (as a product with the fp32 reciprocal, which has to be finite) a block's scale is
+ * f = max |y| / 6 rounded to E4M3, nearest even, saturating at 448; a code is y / f (the correctly rounded quotient) rounded to
+ * E2M1, nearest even, saturating at +-6.  f = 0 (a block of zeros, or too small for E4M3) gives codes of zero.  A block with a NaN gets
+ * the scale NaN and reads back as NaN; infinities saturate.
+ */
+int qknorm_fwd_append_e2m1(const void* q, const void* k, const void* v, const void* gamma_q, const void* gamma_k,
+                           int32_t norm, float eps, const qknorm_rotation_axes* rot, const int64_t* slots,
+                           const qknorm_paged_cache_e2m1* cache, int64_t tokens, int32_t dq, int64_t ld_q, int64_t ld_k,
+                           int64_t ld_v, void* out_q, int64_t ld_out_q, void* stream);
+
+/*
+ * qknorm_attn_paged_e2m1 -- qknorm_attn_paged over a 4-bit cache: the same arguments, the same rows, keys, masks and refusals.
+ * k_scale and v_scale are taken as they stand.  Queries are brought to fp16 with a power of two taken out of each row (exact but for parts
+ * below 2^-30 of the row's largest element); K and V widen exactly; scores, maxima, sums and the output are fp32; the
+ * weights are rounded to fp16 (2^-11 relative, at least 2^-32 of the row's largest weight).
+ *
+ * Kernels: "attn_e2m1" (mma.sync out of registers) for few rows per sequence and key head; for many the visible part of
+ * the cache is widened once into the workspace, to bf16 and exactly, and "attn_tc" reads that (weights rounded to bf16 then, 2^-8).
+ */
+int qknorm_attn_paged_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* cache, const int32_t* block_table,
+                           int32_t table_cols, int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts,
+                           int32_t num_seqs, int64_t tokens, int32_t max_q, int32_t max_kv, int32_t heads_q, float scale,
+                           int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* workspace,
+                           int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that a call of these sizes needs on the current device (0 is possible); HOST, written. */
+int qknorm_attn_paged_e2m1_workspace(int32_t num_seqs, int64_t tokens, int32_t max_q, int32_t max_kv, int32_t heads_q,
+                                     int32_t heads_kv, int32_t head_dim, int32_t window, int64_t* bytes);
 
 #ifdef __cplusplus
 }

@@ -1,5 +1,5 @@
-"""Python side of include/qknorm_attn.h: rotary positions, the fused norm + rotation + cache write,
-attention over a paged cache.
+"""Python side of include/qknorm_attn.h: rotary positions (along one axis or several), the fused norm + rotation + cache
+write, attention over a paged cache (bf16, FP8 or 4 bits).
 
 Argument marshalling only, as in ``binding``: tensors are used for their device pointers, shapes and
 strides, every step runs in the library's kernels, a bad argument raises ``QKNormError``.  Every tensor of a call must
@@ -31,11 +31,19 @@ EXPORTS = (
     "qknorm_fwd_append",
     "qknorm_attn_paged",
     "qknorm_attn_paged_workspace",
+    "qknorm_rope_axes",
+    "qknorm_rope_axes_e4m3",
+    "qknorm_fwd_append_axes",
+    "qknorm_fwd_append_e2m1",
+    "qknorm_attn_paged_e2m1",
+    "qknorm_attn_paged_e2m1_workspace",
 )
 
 SCALINGS = {"plain": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
 NORM_NONE, NORM_LAYERWISE, NORM_HEADWISE = 0, 1, 2
 MAX_HEAD_DIM = 512  # QKNORM_MAX_HEAD_DIM
+MAX_HEAD_DIM_E2M1 = 256  # QKNORM_MAX_HEAD_DIM_E2M1
+MAX_AXES = 8  # QKNORM_MAX_AXES
 
 _vp = ctypes.c_void_p
 _BF16, _F8 = torch.bfloat16, torch.float8_e4m3fn
@@ -57,10 +65,26 @@ class CPagedCache(ctypes.Structure):
                 ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
 
 
-# The same two structs as bytes, which is what the wrappers pass: a decode step is a few microseconds long, and filling a
+class CRotationAxes(ctypes.Structure):
+    """qknorm_rotation_axes"""
+    _fields_ = [("positions", _vp), ("ld_positions", ctypes.c_int64), ("inv_freq", _vp), ("axis", _vp),
+                ("num_axes", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("mscale", ctypes.c_float)]
+
+
+class CPagedCacheE2m1(ctypes.Structure):
+    """qknorm_paged_cache_e2m1"""
+    _fields_ = ([(n, _vp) for n in ("k", "v", "k_scales", "v_scales")]
+                + [(f"{side}_{axis}", ctypes.c_int64) for side in ("k", "v", "ks", "vs") for axis in ("page", "token", "head")]
+                + [("num_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                   ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)])
+
+
+# The same structs as bytes, which is what the wrappers pass: a decode step is a few microseconds long, and filling a
 # ctypes structure takes two of them.
 _ROTATION, _CACHE = struct.Struct("PPiif4x"), struct.Struct("PPqqqqqqqiiiiff")
+_AXES, _CACHE_E2M1 = struct.Struct("PqPPiiif"), struct.Struct("PPPPqqqqqqqqqqqqqiiiff4x")
 assert _ROTATION.size == ctypes.sizeof(CRotation) and _CACHE.size == ctypes.sizeof(CPagedCache)
+assert _AXES.size == ctypes.sizeof(CRotationAxes) and _CACHE_E2M1.size == ctypes.sizeof(CPagedCacheE2m1)
 
 _ready = False
 
@@ -73,13 +97,16 @@ def lib() -> ctypes.CDLL:
         return L
     i32, i64, f32, f64 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double
     L.qknorm_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f32)]
-    for fn in (L.qknorm_rope, L.qknorm_rope_e4m3):
+    for fn in (L.qknorm_rope, L.qknorm_rope_e4m3, L.qknorm_rope_axes, L.qknorm_rope_axes_e4m3):
         fn.argtypes = [_vp, _vp, _vp, i64, i32, i32, i32, i64, i64, i32, _vp, _vp, i64, i64, _vp]
-    L.qknorm_fwd_append.argtypes = [_vp, _vp, _vp, _vp, _vp, i32, f32, _vp, _vp,
-                                    _vp, i64, i32, i64, i64, i64, _vp, i64, _vp]
-    L.qknorm_attn_paged.argtypes = [_vp, i64, _vp, _vp, i32, i64, _vp, _vp, i32, i64, i32, i32, i32,
-                                    f32, i32, i32, _vp, i64, _vp, _vp, i64, _vp]
-    L.qknorm_attn_paged_workspace.argtypes = [i32, i64, i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
+    for fn in (L.qknorm_fwd_append, L.qknorm_fwd_append_axes, L.qknorm_fwd_append_e2m1):
+        fn.argtypes = [_vp, _vp, _vp, _vp, _vp, i32, f32, _vp, _vp,
+                       _vp, i64, i32, i64, i64, i64, _vp, i64, _vp]
+    for fn in (L.qknorm_attn_paged, L.qknorm_attn_paged_e2m1):
+        fn.argtypes = [_vp, i64, _vp, _vp, i32, i64, _vp, _vp, i32, i64, i32, i32, i32,
+                       f32, i32, i32, _vp, i64, _vp, _vp, i64, _vp]
+    for fn in (L.qknorm_attn_paged_workspace, L.qknorm_attn_paged_e2m1_workspace):
+        fn.argtypes = [i32, i64, i32, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
     for name in EXPORTS:
         getattr(L, name).restype = ctypes.c_int
     _ready = True
@@ -155,6 +182,43 @@ def _rotation(positions, inv_freq, T: int, interleaved: bool, mscale: float, dev
                           2 * n, 1 if interleaved else 0, mscale)
 
 
+def _rotation_axes(positions, inv_freq, axis, T: int, interleaved: bool, mscale: float, dev: int) -> Optional[bytes]:
+    """qknorm_rotation_axes: positions [axes, T] with axis, or [T] and axis None."""
+    if axis is None:
+        if positions is None and inv_freq is None:
+            return None
+        if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+            _refuse(_SHAPE, "inv_freq: expected a 1-D float64 CUDA tensor")
+        n = inv_freq.shape[0]
+        return _AXES.pack(_flat(positions, (T,), torch.int64, "positions", dev), 0, _flat(inv_freq, (n,), torch.float64, "inv_freq", dev),
+                          0, 1, 2 * n, 1 if interleaved else 0, mscale)
+    if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+        _refuse(_SHAPE, "inv_freq: expected a 1-D float64 CUDA tensor")
+    if not isinstance(positions, torch.Tensor) or positions.dim() != 2 or not 1 <= positions.shape[0] <= MAX_AXES:
+        _refuse(_SHAPE, f"positions: expected an int64 CUDA tensor [axes, {T}] of 1 to {MAX_AXES} axes to go with axis")
+    n, axes = inv_freq.shape[0], positions.shape[0]
+    ld = positions.stride(0) if axes > 1 else T
+    if (positions.dtype is not torch.int64 or positions.shape[1] != T or positions.get_device() != dev
+            or (T > 1 and positions.stride(1) != 1) or ld < T):
+        _refuse(_SHAPE, f"positions: expected int64 [axes, {T}] with unit stride along the tokens on cuda:{dev}, got {positions.dtype} "
+                        f"{tuple(positions.shape)} with strides {tuple(positions.stride())} on {positions.device}")
+    return _AXES.pack(positions.data_ptr(), ld, _flat(inv_freq, (n,), torch.float64, "inv_freq", dev),
+                      _flat(axis, (n,), torch.uint8, "axis", dev), axes, 2 * n, 1 if interleaved else 0, mscale)
+
+
+def rope_axes(sections, *, turns: bool = False, device="cuda") -> torch.Tensor:
+    """The `axis` tensor of a rotation with several axes: sections[a] pairs turn by axis a, sum(sections) = rot_dim/2.  In blocks,
+    axis 0's pairs first; or (turns) dealt one to each axis in turn for as long as it has any left, from the first pair on."""
+    sections = [int(n) for n in sections]
+    if not 1 <= len(sections) <= MAX_AXES or min(sections) < 0:
+        _refuse(_SHAPE, f"sections: expected 1 to {MAX_AXES} numbers of pairs, got {sections}")
+    if turns:
+        axis = [a for i in range(max(sections)) for a, n in enumerate(sections) if i < n]
+    else:
+        axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    return torch.tensor(axis, dtype=torch.uint8).to(device)
+
+
 def _cache(k_cache, v_cache, k_scale: float, v_scale: float, dev: int):
     """k_cache, v_cache [num_pages, page_size, heads, head_dim], any strides over pages, tokens and heads: (struct, heads,
     head_dim)."""
@@ -172,6 +236,33 @@ def _cache(k_cache, v_cache, k_scale: float, v_scale: float, dev: int):
                     f"shape on cuda:{dev}, with unit stride in head_dim")
 
 
+_CODES = (torch.uint8, torch.float4_e2m1fn_x2)
+_SCALES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _cache_e2m1(k_cache, v_cache, k_scales, v_scales, k_scale: float, v_scale: float, dev: int):
+    """k_cache, v_cache [pages, page_size, heads, head_dim/2] bytes, k_scales, v_scales [pages, page_size, heads, head_dim/16], any
+    strides over pages, tokens and heads: (struct, heads, head_dim)."""
+    four = (k_cache, v_cache, k_scales, v_scales)
+    if all(isinstance(t, torch.Tensor) for t in four):
+        shape, sshape = k_cache.shape, k_scales.shape
+        if (k_cache.dtype in _CODES and v_cache.dtype is k_cache.dtype and k_scales.dtype in _SCALES and v_scales.dtype is k_scales.dtype
+                and len(shape) == 4 and v_cache.shape == shape and len(sshape) == 4 and v_scales.shape == sshape
+                and shape[:3] == sshape[:3] and shape[3] == 8 * sshape[3] and shape[3] > 0
+                and k_cache.get_device() == dev and v_cache.get_device() == dev and k_scales.get_device() == dev and v_scales.get_device() == dev):
+            kp, kt, kh, k1 = k_cache.stride()
+            vp, vt, vh, v1 = v_cache.stride()
+            ap, at, ah, a1 = k_scales.stride()
+            bp, bt, bh, b1 = v_scales.stride()
+            if k1 == 1 and v1 == 1 and ((a1 == 1 and b1 == 1) or sshape[3] == 1):
+                pages, page, heads, half = shape
+                return _CACHE_E2M1.pack(k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), kp, kt, kh, vp, vt, vh,
+                                        ap, at, ah, bp, bt, bh, pages, page, heads, 2 * half, k_scale, v_scale), heads, 2 * half
+    _refuse(_SHAPE, "k_cache, v_cache, k_scales, v_scales: expected two uint8 or float4_e2m1fn_x2 tensors [pages, page_size, heads, head_dim/2] of "
+                    "one type and shape and two float8_e4m3fn or uint8 tensors [pages, page_size, heads, head_dim/16], head_dim a multiple of 16, "
+                    f"on cuda:{dev}, with unit stride in the last axis")
+
+
 def _current(stream):
     """What `_invoke` takes: the current stream as a handle if none is given."""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream
@@ -187,10 +278,11 @@ def _empty(shape, dtype, device, stream) -> torch.Tensor:
 
 
 def qknorm_rope(q, k, positions, inv_freq, head_dim: int, out_q=None, out_k=None, *, interleaved: bool = False,
-                inverse: bool = False, mscale: float = 1.0, stream=None):
+                inverse: bool = False, mscale: float = 1.0, axis=None, stream=None):
     """qknorm_rope / qknorm_rope_e4m3 (chosen by the activations' dtype): rotary positions on q [T, dq] and k [T, dk]
     (either may be None; rows may be strided).  positions int64 [T]; inv_freq float64 [rot_dim/2]; rot_dim <= head_dim,
-    the rest of a head passes through.  interleaved: pairs (2i, 2i+1), else (i, i + rot_dim/2).
+    the rest of a head passes through.  axis uint8 [rot_dim/2] (qknorm_rope_axes): positions are int64 [axes, T], and pair i turns by those
+    of axis[i]; see rope_axes.  interleaved: pairs (2i, 2i+1), else (i, i + rot_dim/2).
     inverse=True turns back: the backward pass, from the gradient of the outputs to that of the inputs.
     out_* default to new tensors and may be the inputs.  Returns (out_q, out_k)."""
     L = lib()
@@ -200,7 +292,8 @@ def qknorm_rope(q, k, positions, inv_freq, head_dim: int, out_q=None, out_k=None
     if not isinstance(ref, torch.Tensor) or ref.dim() != 2:
         _refuse(_SHAPE, "q and k are 2-D tensors: [tokens, heads * head_dim]")
     T, act, dev = ref.shape[0], _F8 if ref.dtype is _F8 else _BF16, _device()
-    rot = _rotation(positions, inv_freq, T, interleaved, mscale, dev)
+    rot = (_rotation(positions, inv_freq, T, interleaved, mscale, dev) if axis is None
+           else _rotation_axes(positions, inv_freq, axis, T, interleaved, mscale, dev))
     if rot is None:
         _refuse(binding.QKNORM_ERR_NULL, "positions and inv_freq are None")
     pq = pk = poq = pok = None
@@ -219,23 +312,43 @@ def qknorm_rope(q, k, positions, inv_freq, head_dim: int, out_q=None, out_k=None
             pok = out_k.data_ptr()
         else:
             pok, _, ldok = _rows(out_k, T, "out_k", act, dev, dk)
-    _invoke(L.qknorm_rope_e4m3 if act is _F8 else L.qknorm_rope,
+    _invoke((L.qknorm_rope_e4m3 if act is _F8 else L.qknorm_rope) if axis is None else
+            (L.qknorm_rope_axes_e4m3 if act is _F8 else L.qknorm_rope_axes),
             (pq, pk, rot, T, dq, dk, _int32(head_dim, "head_dim"), ldq, ldk, 1 if inverse else 0, poq, pok, ldoq, ldok), _current(stream),
-            (q, k, positions, inv_freq, out_q, out_k))
+            (q, k, positions, inv_freq, axis, out_q, out_k))
     return out_q, out_k
 
 
 def qknorm_fwd_append(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, eps: float, out_q=None, *,
                       headwise: bool = False, interleaved: bool = False, mscale: float = 1.0, k_scale: float = 1.0,
-                      v_scale: float = 1.0, stream=None):
+                      v_scale: float = 1.0, axis=None, stream=None):
     """qknorm_fwd_append: norm (layerwise, or headwise; none if gamma_q and gamma_k are None), rotation (none if positions and
     inv_freq are None) and cache write in one pass.  q [T, dq] (or None), k and v [T, heads * head_dim] bf16, rows may
     be strided; slots int64 [T] (page * page_size + token; outside the pool: not written); k_cache and v_cache
-    [pages, page_size, heads, head_dim] bf16 or float8_e4m3fn (holding x / scale), written in place.
+    [pages, page_size, heads, head_dim] bf16 or float8_e4m3fn (holding x / scale), written in place.  axis: as in qknorm_rope.
     out_q defaults to a new tensor and may be q.  Returns out_q."""
     L = lib()
     dev = _device()
     cache, heads, hd = _cache(k_cache, v_cache, k_scale, v_scale, dev)
+    return _append(L.qknorm_fwd_append if axis is None else L.qknorm_fwd_append_axes, axis is not None, (k_cache, v_cache), cache, heads, hd, q, k, v,
+                   gamma_q, gamma_k, positions, inv_freq, axis, slots, eps, out_q, headwise, interleaved, mscale, stream, dev)
+
+
+def qknorm_fwd_append_e2m1(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, k_scales, v_scales, eps: float, out_q=None,
+                           *, headwise: bool = False, interleaved: bool = False, mscale: float = 1.0, k_scale: float = 1.0,
+                           v_scale: float = 1.0, axis=None, stream=None):
+    """qknorm_fwd_append_e2m1: qknorm_fwd_append into a 4-bit cache, codes [pages, page_size, heads, head_dim/2] (uint8 or
+    float4_e2m1fn_x2, the even element in the low four bits) and scales [pages, page_size, heads, head_dim/16] (float8_e4m3fn or
+    uint8), written in place; an element reads back as code * scale * k_scale (v_scale).  Returns out_q."""
+    L = lib()
+    dev = _device()
+    cache, heads, hd = _cache_e2m1(k_cache, v_cache, k_scales, v_scales, k_scale, v_scale, dev)
+    return _append(L.qknorm_fwd_append_e2m1, True, (k_cache, v_cache, k_scales, v_scales), cache, heads, hd, q, k, v, gamma_q, gamma_k, positions,
+                   inv_freq, axis, slots, eps, out_q, headwise, interleaved, mscale, stream, dev)
+
+
+def _append(cfunc, several: bool, pools, cache, heads: int, hd: int, q, k, v, gamma_q, gamma_k, positions, inv_freq, axis, slots, eps, out_q,
+            headwise, interleaved, mscale, stream, dev: int):
     if not isinstance(k, torch.Tensor) or k.dim() != 2:
         _refuse(_SHAPE, "k: expected a 2-D bfloat16 CUDA tensor")
     T, dk = k.shape[0], heads * hd
@@ -258,9 +371,10 @@ def qknorm_fwd_append(q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_c
             po = out_q.data_ptr()
         else:
             po, _, ldo = _rows(out_q, T, "out_q", _BF16, dev, dq)
-    rot = _rotation(positions, inv_freq, T, interleaved, mscale, dev)
-    _invoke(L.qknorm_fwd_append, (pq, pk, pv, pgq, pgk, norm, eps, rot, pslots, cache, T, dq, ldq, ldk, ldv, po, ldo), _current(stream),
-            (q, k, v, gamma_q, gamma_k, positions, inv_freq, slots, k_cache, v_cache, out_q))
+    rot = (_rotation_axes(positions, inv_freq, axis, T, interleaved, mscale, dev) if several
+           else _rotation(positions, inv_freq, T, interleaved, mscale, dev))
+    _invoke(cfunc, (pq, pk, pv, pgq, pgk, norm, eps, rot, pslots, cache, T, dq, ldq, ldk, ldv, po, ldo), _current(stream),
+            (q, k, v, gamma_q, gamma_k, positions, inv_freq, axis, slots, *pools, out_q))
     return out_q
 
 
@@ -273,10 +387,26 @@ def attn_paged_workspace(num_seqs: int, tokens: int, max_q: int, max_kv: int, he
     return _workspace(torch.cuda.current_device(), num_seqs, tokens, max_q, max_kv, heads_q, heads_kv, head_dim, window)
 
 
+def attn_paged_e2m1_workspace(num_seqs: int, tokens: int, max_q: int, max_kv: int, heads_q: int, heads_kv: int, head_dim: int,
+                              window: int = 0) -> int:
+    """qknorm_attn_paged_e2m1_workspace: bytes a call of these sizes needs on the current device."""
+    names = ("num_seqs", "max_q", "max_kv", "heads_q", "heads_kv", "head_dim", "window")
+    num_seqs, max_q, max_kv, heads_q, heads_kv, head_dim, window = map(
+        _int32, (num_seqs, max_q, max_kv, heads_q, heads_kv, head_dim, window), names)
+    return _workspace_e2m1(torch.cuda.current_device(), num_seqs, tokens, max_q, max_kv, heads_q, heads_kv, head_dim, window)
+
+
 @functools.lru_cache(maxsize=256)
 def _workspace(device: int, *sizes: int) -> int:
     out = ctypes.c_int64(0)
     _check(lib().qknorm_attn_paged_workspace(*sizes, ctypes.byref(out)))
+    return out.value
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_e2m1(device: int, *sizes: int) -> int:
+    out = ctypes.c_int64(0)
+    _check(lib().qknorm_attn_paged_e2m1_workspace(*sizes, ctypes.byref(out)))
     return out.value
 
 
@@ -291,6 +421,24 @@ def qknorm_attn_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q
     L = lib()
     dev = _device()
     cache, heads, hd = _cache(k_cache, v_cache, k_scale, v_scale, dev)
+    return _attend(L.qknorm_attn_paged, _workspace, (k_cache, v_cache), cache, heads, hd, q, block_table, kv_lens, q_starts, max_q, max_kv, scale,
+                   causal, window, out, lse, workspace, stream, dev)
+
+
+def qknorm_attn_paged_e2m1(q, k_cache, v_cache, k_scales, v_scales, block_table, kv_lens, q_starts, max_q: int, max_kv: int, *,
+                           scale: Optional[float] = None, causal: bool = True, window: int = 0, k_scale: float = 1.0,
+                           v_scale: float = 1.0, out=None, lse=None, workspace=None, stream=None):
+    """qknorm_attn_paged_e2m1: qknorm_attn_paged over a 4-bit cache (codes and scales as in qknorm_fwd_append_e2m1).
+    workspace: uint8 tensor of attn_paged_e2m1_workspace(...) bytes, by default a new one per call.  Returns out."""
+    L = lib()
+    dev = _device()
+    cache, heads, hd = _cache_e2m1(k_cache, v_cache, k_scales, v_scales, k_scale, v_scale, dev)
+    return _attend(L.qknorm_attn_paged_e2m1, _workspace_e2m1, (k_cache, v_cache, k_scales, v_scales), cache, heads, hd, q, block_table, kv_lens,
+                   q_starts, max_q, max_kv, scale, causal, window, out, lse, workspace, stream, dev)
+
+
+def _attend(cfunc, bytes_of, pools, cache, heads: int, hd: int, q, block_table, kv_lens, q_starts, max_q, max_kv, scale, causal, window, out, lse,
+            workspace, stream, dev: int):
     if not isinstance(q, torch.Tensor) or q.dim() != 2:
         _refuse(_SHAPE, "q: expected a 2-D bfloat16 CUDA tensor")
     T = q.shape[0]
@@ -313,14 +461,14 @@ def qknorm_attn_paged(q, k_cache, v_cache, block_table, kv_lens, q_starts, max_q
         po, _, ldo = _rows(out, T, "out", _BF16, dev, dq)
     plse = None if lse is None else _flat(lse, (T, hq), torch.float32, "lse", dev)
     if workspace is None:
-        nbytes = _workspace(dev, B, T, max_q, max_kv, hq, heads, hd, window)
+        nbytes = bytes_of(dev, B, T, max_q, max_kv, hq, heads, hd, window)
         workspace = _empty((nbytes,), torch.uint8, q.device, stream) if nbytes else None
     else:
         if not workspace.is_contiguous() or workspace.get_device() != dev:
             _refuse(binding.QKNORM_ERR_SCRATCH, f"workspace: expected a contiguous tensor on cuda:{dev}")
         nbytes = workspace.numel() * workspace.element_size()
-    _invoke(L.qknorm_attn_paged,
+    _invoke(cfunc,
             (pq, ldq, cache, ptable, cols, ldt, plens, pstarts, B, T, max_q, max_kv, hq, 1.0 / math.sqrt(hd) if scale is None else scale,
              1 if causal else 0, window, po, ldo, plse, workspace.data_ptr() if workspace is not None else None, nbytes),
-            _current(stream), (q, k_cache, v_cache, block_table, kv_lens, q_starts, out, lse, workspace))
+            _current(stream), (q, *pools, block_table, kv_lens, q_starts, out, lse, workspace))
     return out

@@ -26,6 +26,7 @@ LIB_PATH = os.path.join(PKG_DIR, "libqknorm.so")
 CHUNKS_PER_THREAD = (1, 2, 3, 4, 6, 8)          # row / ring kernels
 CHUNK_SLOTS_PER_LANE = tuple(range(4, 44, 4))    # warp-per-row kernel
 PADDED_HEAD_DIMS = (64, 128)                     # tensor-core attention kernel
+PADDED_HEAD_DIMS_E2M1 = (64, 128, 256)           # attention over a 4-bit cache
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -58,6 +59,8 @@ def _units() -> List[Tuple[str, str, List[str]]]:
         for f8, tag in (("false", "bf16"), ("true", "e4m3")):
             units.append((f"qknorm_attn_tc_{tag}_d{dp}.o", os.path.join(CSRC, "qknorm_attn_tc_inst.cu"),
                           [f"-DQKNORM_DP={dp}", f"-DQKNORM_F8={f8}", f"-DQKNORM_IO_TAG={tag}"]))
+    for dp in PADDED_HEAD_DIMS_E2M1:
+        units.append((f"qknorm_attn_e2m1_d{dp}.o", os.path.join(CSRC, "qknorm_attn_e2m1_inst.cu"), [f"-DQKNORM_DP={dp}"]))
     return units
 
 

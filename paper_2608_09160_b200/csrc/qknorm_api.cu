@@ -11,6 +11,7 @@
 #include "../../include/qknorm.h"
 #include "../../include/qknorm_attn.h"
 #include "qknorm_attn.cuh"
+#include "qknorm_attn_e2m1.cuh"
 #include "qknorm_baselines.cuh"
 #include "qknorm_general.cuh"
 #include "qknorm_head.cuh"

@@ -57,11 +57,27 @@ int check_rotation(const qknorm_rotation* r, int head_dim, RopeParams& R) {
   return QKNORM_OK;
 }
 
+// The same with several axes.
+int check_rotation(const qknorm_rotation_axes* r, int head_dim, RopeParams& R, int64_t T) {
+  if (r && r->rot_dim != 0) {
+    if (r->num_axes < 1 || r->num_axes > QKNORM_MAX_AXES) return QKNORM_ERR_SHAPE;
+    if (r->ld_positions < 0 || (r->ld_positions != 0 && r->ld_positions < T)) return QKNORM_ERR_SHAPE;
+    R.axis = r->axis;
+    R.axes = r->num_axes;
+    R.ld_pos = r->ld_positions ? r->ld_positions : T;
+    const qknorm_rotation one = {r->positions, r->inv_freq, r->rot_dim, r->interleaved, r->mscale};
+    return check_rotation(&one, head_dim, R);
+  }
+  return check_rotation((const qknorm_rotation*)nullptr, head_dim, R);
+}
+int check_rotation(const qknorm_rotation* r, int head_dim, RopeParams& R, int64_t) { return check_rotation(r, head_dim, R); }
+
 struct CallRegions {  // buffers of a call: outputs, and everything an output must not touch
   Region out[8], in[16];
   int outs = 0, ins = 0;
   int own[8];            // out[i] may be exactly in[own[i]]
-  int pools = -1;        // out[pools] and out[pools + 1] are the two sides of a cache, looked at apart from the others
+  int pools = -1, num_pools = 2;  // out[pools] and the num_pools - 1 behind it are the sides of a cache, looked at apart from the others
+  bool both_pools(int i, int j) const { return pools >= 0 && i >= pools && j >= pools && i < pools + num_pools && j < pools + num_pools; }
 };
 
 int log2_or_minus_one(int v) {
@@ -78,10 +94,18 @@ int check_regions(const CallRegions& c) {
     for (int j = 0; j < c.ins; ++j)
       if (may_overlap(c.out[i], c.in[j]) && !(c.own[i] == j && same_region(c.out[i], c.in[j]))) return QKNORM_ERR_ALIAS;
     for (int j = 0; j < c.outs; ++j)
-      if (j != i && !(c.pools >= 0 && i + j == 2 * c.pools + 1 && (i == c.pools || j == c.pools)) && may_overlap(c.out[i], c.out[j]))
-        return QKNORM_ERR_ALIAS;
+      if (j != i && !c.both_pools(i, j) && may_overlap(c.out[i], c.out[j])) return QKNORM_ERR_ALIAS;
   }
   return QKNORM_OK;
+}
+
+// What a rotation reads.
+void rotation_regions(const RopeParams& R, CallRegions& c) {
+  if (!R.rot_dim) return;
+  const uintptr_t bytes = 8 * (uintptr_t)R.T;
+  c.in[c.ins++] = R.axis ? Region{(uintptr_t)R.positions, (uintptr_t)R.axes, bytes, 8 * (uintptr_t)R.ld_pos} : flat(R.positions, bytes);
+  c.in[c.ins++] = flat(R.inv_freq, 4 * (uintptr_t)R.rot_dim);
+  if (R.axis) c.in[c.ins++] = flat(R.axis, (uintptr_t)R.rot_dim / 2);
 }
 
 int row_stride(int64_t ld, int32_t width, long long* out) {
@@ -215,6 +239,51 @@ int check_cache(const qknorm_paged_cache* c, CacheFacts* f) {
   return QKNORM_OK;
 }
 
+// A 4-bit cache: codes of K, of V, scales of K, of V.
+struct E2m1Facts {
+  Region region[4];
+  PoolShape shape[4];
+  bool vec16;  // 16-byte copies of the codes
+};
+
+// One side of it, in bytes, as check_cache_side and pool_shape look at it.
+qknorm_paged_cache e2m1_side(const qknorm_paged_cache_e2m1& c, int i) {
+  qknorm_paged_cache s = {};
+  s.num_pages = c.num_pages;
+  s.page_size = c.page_size;
+  s.heads = c.heads;
+  s.head_dim = i < 2 ? c.head_dim / 2 : c.head_dim / 16;
+  s.e4m3 = 1;
+  s.k = i == 0 ? c.k : i == 1 ? c.v : i == 2 ? c.k_scales : c.v_scales;
+  s.k_page = i == 0 ? c.k_page : i == 1 ? c.v_page : i == 2 ? c.ks_page : c.vs_page;
+  s.k_token = i == 0 ? c.k_token : i == 1 ? c.v_token : i == 2 ? c.ks_token : c.vs_token;
+  s.k_head = i == 0 ? c.k_head : i == 1 ? c.v_head : i == 2 ? c.ks_head : c.vs_head;
+  return s;
+}
+
+int check_cache(const qknorm_paged_cache_e2m1* c, E2m1Facts* f) {
+  if (!c) return QKNORM_ERR_NULL;
+  if (c->num_pages < 0 || c->num_pages > 0x7fffffff || c->page_size < 1 || c->heads < 1) return QKNORM_ERR_SHAPE;
+  if (c->head_dim < 16 || c->head_dim > QKNORM_MAX_HEAD_DIM_E2M1 || c->head_dim % 16 != 0) return QKNORM_ERR_HEADS;
+  if ((int64_t)c->heads * c->head_dim > kMaxDim) return QKNORM_ERR_SHAPE;
+  if (!(c->k_scale > 0.0f) || !isfinite(c->k_scale) || !(c->v_scale > 0.0f) || !isfinite(c->v_scale)) return QKNORM_ERR_SHAPE;
+  f->vec16 = c->head_dim % 32 == 0;
+  const int blocks = c->head_dim / 16;
+  const uintptr_t low = blocks & -blocks, unit = low > 8 ? 8 : low;
+  for (int i = 0; i < 4; ++i) {
+    const qknorm_paged_cache s = e2m1_side(*c, i);
+    bool v16, v8;
+    const int rc = check_cache_side(s, s.k, s.k_page, s.k_token, s.k_head, &f->region[i], &v16, &v8);
+    if (rc != QKNORM_OK) return rc;
+    f->shape[i] = pool_shape(s, s.k, s.k_page, s.k_token, s.k_head);
+    if (c->num_pages == 0) continue;
+    const uintptr_t all = (uintptr_t)s.k | (uintptr_t)s.k_page | (uintptr_t)s.k_token | (uintptr_t)s.k_head;
+    if (i < 2 ? !v8 : all % unit != 0) return QKNORM_ERR_ALIGN;
+    if (i < 2) f->vec16 = f->vec16 && v16;
+  }
+  return QKNORM_OK;
+}
+
 // Launches R (everything but the launch shape filled in).  cache_bytes 0: no cache.  vec: the vector kernel's alignment holds.
 int launch_rope(RopeParams& R, int elem_bytes, int cache_bytes, int norm, bool vec, cudaStream_t stream) {
   const DeviceInfo* dev = nullptr;
@@ -256,7 +325,8 @@ int launch_rope(RopeParams& R, int elem_bytes, int cache_bytes, int norm, bool v
   return finish_launch(cache_bytes ? "append_general" : "rope_general");
 }
 
-int run_rope(int elem_bytes, const void* q, const void* k, const qknorm_rotation* rot, int64_t T, int32_t dq, int32_t dk,
+template <class Rotation>
+int run_rope(int elem_bytes, const void* q, const void* k, const Rotation* rot, int64_t T, int32_t dq, int32_t dk,
              int32_t head_dim, int64_t ld_q, int64_t ld_k, int32_t inverse, void* oq, void* ok, int64_t ld_oq, int64_t ld_ok,
              cudaStream_t stream) {
   if (T < 0 || dq < 0 || dk < 0 || dq > kMaxDim || dk > kMaxDim) return QKNORM_ERR_SHAPE;
@@ -271,7 +341,7 @@ int run_rope(int elem_bytes, const void* q, const void* k, const qknorm_rotation
     return rc;
   if (T == 0) return QKNORM_OK;
   if (dq == 0 && dk == 0) return QKNORM_ERR_SHAPE;
-  if ((rc = check_rotation(rot, head_dim, R)) != QKNORM_OK) return rc;
+  if ((rc = check_rotation(rot, head_dim, R, T)) != QKNORM_OK) return rc;
   if (inverse) R.turns_sign = -R.turns_sign;
   R.T = T;
   R.head_dim = head_dim;
@@ -297,33 +367,74 @@ int run_rope(int elem_bytes, const void* q, const void* k, const qknorm_rotation
     c.out[c.outs++] = Region{(uintptr_t)sd.y, (uintptr_t)T, (uintptr_t)sd.d * eb, (uintptr_t)sd.s->ldy * eb};
     c.in[c.ins++] = Region{(uintptr_t)sd.x, (uintptr_t)T, (uintptr_t)sd.d * eb, (uintptr_t)sd.s->ldx * eb};
   }
-  if (R.rot_dim) {
-    c.in[c.ins++] = flat(R.positions, 8 * (uintptr_t)T);
-    c.in[c.ins++] = flat(R.inv_freq, 4 * (uintptr_t)R.rot_dim);
-  }
+  rotation_regions(R, c);
   if ((rc = check_regions(c)) != QKNORM_OK) return rc;
   return launch_rope(R, elem_bytes, 0, kNormNone, aligned, stream);
 }
 
-int run_append(const void* q, const void* k, const void* v, const void* gq, const void* gk, int32_t norm, float eps,
-               const qknorm_rotation* rot, const int64_t* slots, const qknorm_paged_cache* cache, int64_t T, int32_t dq, int64_t ld_q,
-               int64_t ld_k, int64_t ld_v, void* oq, int64_t ld_oq, cudaStream_t stream) {
+// What an append needs to know of a cache: its sides, 2 of them or (with a 4-bit cache's scales) 4.
+struct AppendCache {
+  int bytes, sides;  // bytes: of an element, or kCacheE2m1
+  CacheSide side[4];
+  Region region[4];
+  PoolShape shape[4];
+  bool vec;
+};
+
+int append_cache(const qknorm_paged_cache* c, AppendCache* a) {
   CacheFacts f;
-  int rc = check_cache(cache, &f);
+  const int rc = check_cache(c, &f);
+  if (rc != QKNORM_OK) return rc;
+  a->bytes = c->e4m3 ? 1 : 2;
+  a->sides = 2;
+  a->side[0] = CacheSide{c->k, c->k_page, c->k_token, c->k_head, c->e4m3 ? 1.0f / c->k_scale : 1.0f};
+  a->side[1] = CacheSide{c->v, c->v_page, c->v_token, c->v_head, c->e4m3 ? 1.0f / c->v_scale : 1.0f};
+  a->region[0] = f.k;
+  a->region[1] = f.v;
+  if (c->num_pages > 0) {
+    a->shape[0] = pool_shape(*c, c->k, c->k_page, c->k_token, c->k_head);
+    a->shape[1] = pool_shape(*c, c->v, c->v_page, c->v_token, c->v_head);
+  }
+  a->vec = c->e4m3 ? f.vec8 : f.vec16;
+  return QKNORM_OK;
+}
+
+int append_cache(const qknorm_paged_cache_e2m1* c, AppendCache* a) {
+  E2m1Facts f;
+  const int rc = check_cache(c, &f);
+  if (rc != QKNORM_OK) return rc;
+  a->bytes = kCacheE2m1;
+  a->sides = 4;
+  for (int i = 0; i < 4; ++i) {
+    const qknorm_paged_cache s = e2m1_side(*c, i);
+    a->side[i] = CacheSide{s.k, s.k_page, s.k_token, s.k_head, i == 0 ? 1.0f / c->k_scale : i == 1 ? 1.0f / c->v_scale : 1.0f};
+    a->region[i] = f.region[i];
+    a->shape[i] = f.shape[i];
+  }
+  a->vec = true;  // what a vector store needs, check_cache has asked for
+  return QKNORM_OK;
+}
+
+template <class Rotation, class Cache>
+int run_append(const void* q, const void* k, const void* v, const void* gq, const void* gk, int32_t norm, float eps,
+               const Rotation* rot, const int64_t* slots, const Cache* cache, int64_t T, int32_t dq, int64_t ld_q,
+               int64_t ld_k, int64_t ld_v, void* oq, int64_t ld_oq, cudaStream_t stream) {
+  AppendCache f;
+  int rc = append_cache(cache, &f);
   if (rc != QKNORM_OK) return rc;
   const int hd = cache->head_dim, dk = cache->heads * hd;
   if (T < 0 || dq < 0 || dq > kMaxDim) return QKNORM_ERR_SHAPE;
   if (dq % hd != 0) return QKNORM_ERR_HEADS;
   if (norm < kNormNone || norm > kNormHead) return QKNORM_ERR_SHAPE;
   if (norm != kNormNone && !(eps >= 0.0f)) return QKNORM_ERR_EPS;
-  if (cache->e4m3 && (!isfinite(1.0f / cache->k_scale) || !isfinite(1.0f / cache->v_scale))) return QKNORM_ERR_SHAPE;
+  if (!isfinite(f.side[0].inv_scale) || !isfinite(f.side[1].inv_scale)) return QKNORM_ERR_SHAPE;
   RopeParams R;
   memset(&R, 0, sizeof(R));
   if ((rc = row_stride(ld_q, dq, &R.q.ldx)) || (rc = row_stride(ld_oq, dq, &R.q.ldy)) || (rc = row_stride(ld_k, dk, &R.k.ldx)) ||
       (rc = row_stride(ld_v, dk, &R.v.ldx)))
     return rc;
   if (T == 0) return QKNORM_OK;
-  if ((rc = check_rotation(rot, hd, R)) != QKNORM_OK) return rc;
+  if ((rc = check_rotation(rot, hd, R, T)) != QKNORM_OK) return rc;
   if (!k || !v || !slots || (norm != kNormNone && !gk)) return QKNORM_ERR_NULL;
   if (dq > 0 && (!q || !oq || (norm != kNormNone && !gq))) return QKNORM_ERR_NULL;
   uintptr_t ptrs = (uintptr_t)k | (uintptr_t)v, strides = (uintptr_t)R.k.ldx | (uintptr_t)R.v.ldx;
@@ -351,8 +462,12 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
   R.k.heads = R.v.heads = cache->heads;
   R.k.inv_d = 1.0f / (float)dk;
   R.v.x = v;
-  R.ck = CacheSide{cache->k, cache->k_page, cache->k_token, cache->k_head, cache->e4m3 ? 1.0f / cache->k_scale : 1.0f};
-  R.cv = CacheSide{cache->v, cache->v_page, cache->v_token, cache->v_head, cache->e4m3 ? 1.0f / cache->v_scale : 1.0f};
+  R.ck = f.side[0];
+  R.cv = f.side[1];
+  if (f.sides == 4) {
+    R.cks = f.side[2];
+    R.cvs = f.side[3];
+  }
   R.slots = (const long long*)slots;
   R.num_slots = (long long)cache->num_pages * cache->page_size;
   R.page_size = cache->page_size;
@@ -366,24 +481,25 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
     if (norm != kNormNone) c.in[c.ins++] = flat(gq, qb);
   }
   c.pools = c.outs;
-  c.own[c.outs] = -1;
-  c.out[c.outs++] = f.k;
-  c.own[c.outs] = -1;
-  c.out[c.outs++] = f.v;
+  c.num_pools = f.sides;
+  for (int i = 0; i < f.sides; ++i) {
+    c.own[c.outs] = -1;
+    c.out[c.outs++] = f.region[i];
+  }
   c.in[c.ins++] = Region{(uintptr_t)k, rows, kb, (uintptr_t)R.k.ldx * 2};
   c.in[c.ins++] = Region{(uintptr_t)v, rows, kb, (uintptr_t)R.v.ldx * 2};
   if (norm != kNormNone) c.in[c.ins++] = flat(gk, kb);
   c.in[c.ins++] = flat(slots, 8 * rows);
-  if (R.rot_dim) {
-    c.in[c.ins++] = flat(R.positions, 8 * rows);
-    c.in[c.ins++] = flat(R.inv_freq, 4 * (uintptr_t)R.rot_dim);
-  }
+  rotation_regions(R, c);
   if ((rc = check_regions(c)) != QKNORM_OK) return rc;
-  if (cache->num_pages > 0 && pools_meet(pool_shape(*cache, cache->k, cache->k_page, cache->k_token, cache->k_head),
-                                         pool_shape(*cache, cache->v, cache->v_page, cache->v_token, cache->v_head)))
-    return QKNORM_ERR_ALIAS;
-  const bool vec = (hd | R.rot_dim) % 16 == 0 && ptrs % 16 == 0 && strides % 8 == 0 && (cache->e4m3 ? f.vec8 : f.vec16);
-  return launch_rope(R, 2, cache->e4m3 ? 1 : 2, norm, vec, stream);
+  if (cache->num_pages > 0)
+    for (int i = 0; i < f.sides; ++i)
+      for (int j = 0; j < i; ++j)
+        if (pools_meet(f.shape[i], f.shape[j])) return QKNORM_ERR_ALIAS;
+  bool vec = (hd | R.rot_dim) % 16 == 0 && ptrs % 16 == 0 && strides % 8 == 0 && f.vec;
+  // a block of 16 elements lies with two neighbouring lanes in the half layout: both have to be of the part that turns
+  if (f.bytes == kCacheE2m1 && R.rot_dim % 32 != 0 && !R.interleaved) vec = false;
+  return launch_rope(R, 2, f.bytes, norm, vec, stream);
 }
 
 // ---- attention over the paged cache ---------------------------------------------------------------
@@ -563,10 +679,11 @@ int run_attn_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, i
   return QKNORM_OK;
 }
 
+// v_scale: what V of a bf16 cache is multiplied by (an FP8 one has its own).
 int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* table, int32_t table_cols, int64_t ld_table,
              const int32_t* kv_lens, const int32_t* q_starts, int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q,
              float scale, int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* ws, int64_t ws_bytes,
-             cudaStream_t stream) {
+             cudaStream_t stream, float v_scale = 1.0f) {
   CacheFacts f;
   int rc = check_cache(cache, &f);
   if (rc != QKNORM_OK) return rc;
@@ -646,7 +763,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.group = heads_q / cache->heads;
   P.head_dim = cache->head_dim;
   P.c = fmaxf(c, kAttnLeastC);
-  P.v_scale = cache->e4m3 ? cache->v_scale : 1.0f;
+  P.v_scale = cache->e4m3 ? cache->v_scale : v_scale;
   P.causal = causal;
   P.window = window;
   P.lse = lse;
@@ -713,4 +830,222 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   e = launch_overlapped(attn_join_kernel_for(), dim3((unsigned)plan.grid, (unsigned)(plan.part_rows / kAttnJoinRows)), (unsigned)kAttnJoinThreads, 0, stream, P);
   if (e != cudaSuccess) return set_cuda_error(e);
   return finish_launch("attn_tc");
+}
+
+// ---- attention over a 4-bit cache --------------------------------------------------------------------
+
+// How a call over a 4-bit cache is cut: sizes only, so that the workspace can be asked for beforehand.
+struct E2m1Plan {
+  bool widen = false;
+  int nt = 1, row_tiles = 1, chunk = 0, splits = 1, cols = 0;
+  int64_t parts = 0;         // of a head's row
+  int64_t side_bytes = 0;    // widened K, or V
+  int64_t table_bytes = 0, rest = 0;  // rest: what attn_tc asks for itself
+  int64_t bytes() const { return widen ? 2 * side_bytes + table_bytes + rest : (parts * 4 + 15) / 16 * 16; }
+};
+
+constexpr int kE2m1WidenRows = 64;                      // rows of a sequence and key head from which widening pays
+constexpr int64_t kE2m1WidenMost = (int64_t)2 << 30;    // bytes of the widened cache
+
+int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, bool causal, int window, int sms,
+              E2m1Plan* out) {
+  E2m1Plan p;
+  const int group = heads_q / heads_kv;
+  if ((int64_t)max_q > T) max_q = (int)T;
+  const int64_t rows = (int64_t)max_q * group;
+  p.cols = (int)((max_keys + kE2m1Page - 1) / kE2m1Page);
+  p.side_bytes = (int64_t)seqs * p.cols * kE2m1Page * heads_kv * head_dim * 2;
+  const AttnPlan tc = plan_attn(seqs, T, max_q, max_keys, heads_q, heads_kv, head_dim, causal, window, sms);
+  if (rows > kE2m1WidenRows && tc.tc && 2 * p.side_bytes <= kE2m1WidenMost) {
+    p.widen = true;
+    p.table_bytes = ((int64_t)seqs * p.cols * 4 + 15) / 16 * 16;
+    p.rest = attn_workspace(tc, head_dim);
+    *out = p;
+    return QKNORM_OK;
+  }
+  p.nt = rows <= 8 ? 1 : rows <= 16 || head_dim > 128 ? 2 : 4;
+  const int64_t row_tiles = (rows + 8 * p.nt - 1) / (8 * p.nt);
+  int64_t span = max_keys;
+  if (window > 0) {  // the first row's window, and what the later ones see behind it
+    const int64_t w = (int64_t)window + (causal ? max_q : T) - 1;
+    if (w < span) span = w;
+  }
+  // Equal chunks, about six CTAs for each place on the GPU, and four tiles of 32 keys at least.
+  const int64_t units = row_tiles * heads_kv * seqs, want = (6 * 3 * (int64_t)sms + units - 1) / units;
+  int64_t chunk = (span + want - 1) / want;
+  chunk = (chunk + 127) / 128 * 128;
+  if (chunk < 128) chunk = 128;
+  const int64_t splits = span > 0 ? (span + chunk - 1) / chunk : 1;
+  if (row_tiles * heads_kv > 0x7fffffff / splits || row_tiles * heads_kv * splits > 0x7fffffff / seqs) return QKNORM_ERR_SHAPE;
+  p.row_tiles = (int)row_tiles;
+  p.chunk = (int)chunk;
+  p.splits = (int)splits;
+  if (splits > 1) p.parts = T * heads_q * splits * (head_dim + 1);
+  *out = p;
+  return QKNORM_OK;
+}
+
+int check_e2m1_sizes(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                     int32_t window) {
+  const int rc = check_attn_sizes(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window);
+  if (rc != QKNORM_OK) return rc;
+  return head_dim % 16 != 0 || head_dim > QKNORM_MAX_HEAD_DIM_E2M1 ? QKNORM_ERR_HEADS : QKNORM_OK;
+}
+
+int run_attn_e2m1_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                            int32_t window, int64_t* bytes) {
+  if (!bytes) return QKNORM_ERR_NULL;
+  int rc = check_e2m1_sizes(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, window);
+  if (rc != QKNORM_OK) return rc;
+  *bytes = 0;
+  if (seqs == 0 || T == 0 || max_q == 0) return QKNORM_OK;
+  const DeviceInfo* dev = nullptr;
+  rc = current_device(&dev);
+  if (rc != QKNORM_OK) return rc;
+  for (const bool causal : {true, false}) {  // enough for either
+    E2m1Plan p;
+    rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, causal, window, dev->sm_count, &p);
+    if (rc != QKNORM_OK) return rc;
+    if (p.bytes() > *bytes) *bytes = p.bytes();
+  }
+  return QKNORM_OK;
+}
+
+int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* cache, const int32_t* table, int32_t table_cols,
+                  int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts, int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv,
+                  int32_t heads_q, float scale, int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* ws,
+                  int64_t ws_bytes, cudaStream_t stream) {
+  E2m1Facts f;
+  int rc = check_cache(cache, &f);
+  if (rc != QKNORM_OK) return rc;
+  const int hd = cache->head_dim;
+  rc = check_e2m1_sizes(seqs, T, max_q, max_kv, heads_q, cache->heads, hd, window);
+  if (rc != QKNORM_OK) return rc;
+  if (!(scale > 0.0f) || !isfinite(scale)) return QKNORM_ERR_SHAPE;
+  const float c = (float)((double)scale * cache->k_scale * 1.44269504088896340736);
+  if (!isfinite(c)) return QKNORM_ERR_SHAPE;
+  if (causal != 0 && causal != 1) return QKNORM_ERR_SHAPE;
+  if (table_cols < 0 || ld_table < 0 || (ld_table != 0 && ld_table < table_cols)) return QKNORM_ERR_SHAPE;
+  AttnE2m1Params E;
+  memset(&E, 0, sizeof(E));
+  AttnParams& P = E.A;
+  const int d = heads_q * hd;
+  if ((rc = row_stride(ld_q, d, &P.ld_q)) || (rc = row_stride(ld_out, d, &P.ld_out))) return rc;
+  if (seqs == 0 || T == 0 || max_q == 0) return QKNORM_OK;
+  if (!q || !out || !kv_lens || !q_starts || (table_cols > 0 && !table)) return QKNORM_ERR_NULL;
+  if ((((uintptr_t)q) | ((uintptr_t)out)) & 1u) return QKNORM_ERR_ALIGN;
+  if ((((uintptr_t)table) | ((uintptr_t)kv_lens) | ((uintptr_t)q_starts) | ((uintptr_t)lse)) & 3u) return QKNORM_ERR_ALIGN;
+  const DeviceInfo* dev = nullptr;
+  rc = current_device(&dev);
+  if (rc != QKNORM_OK) return rc;
+  P.max_keys = (int64_t)table_cols * cache->page_size < max_kv ? (int64_t)table_cols * cache->page_size : max_kv;
+  // the plan goes by max_kv, which the workspace was asked for with
+  E2m1Plan plan;
+  rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, cache->heads, hd, causal != 0, window, dev->sm_count, &plan);
+  if (rc != QKNORM_OK) return rc;
+  const int64_t need = plan.bytes();
+  CallRegions r;
+  r.own[r.outs] = -1;
+  r.out[r.outs++] = Region{(uintptr_t)out, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_out * 2};
+  if (lse) {
+    r.own[r.outs] = -1;
+    r.out[r.outs++] = flat(lse, 4 * (uintptr_t)T * heads_q);
+  }
+  r.in[r.ins++] = Region{(uintptr_t)q, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_q * 2};
+  for (const Region& pool : f.region) r.in[r.ins++] = pool;
+  if (table_cols > 0)
+    r.in[r.ins++] = Region{(uintptr_t)table, (uintptr_t)seqs, (uintptr_t)table_cols * 4, (uintptr_t)(ld_table ? ld_table : table_cols) * 4};
+  r.in[r.ins++] = flat(kv_lens, 4 * (uintptr_t)seqs);
+  r.in[r.ins++] = flat(q_starts, 4 * ((uintptr_t)seqs + 1));
+  if ((rc = check_regions(r)) != QKNORM_OK) return rc;
+  if (need > 0) {
+    if (!ws || ws_bytes < need || !aligned16(ws)) return QKNORM_ERR_SCRATCH;
+    const Region w = flat(ws, (uintptr_t)need);
+    for (int i = 0; i < r.ins; ++i)
+      if (may_overlap(w, r.in[i])) return QKNORM_ERR_SCRATCH;
+    for (int i = 0; i < r.outs; ++i)
+      if (may_overlap(w, r.out[i])) return QKNORM_ERR_SCRATCH;
+  }
+  P.q = (const uint16_t*)q;
+  P.out = (uint16_t*)out;
+  P.k = AttnSide{cache->k, cache->k_page, cache->k_token, cache->k_head};
+  P.v = AttnSide{cache->v, cache->v_page, cache->v_token, cache->v_head};
+  E.ks = AttnSide{cache->k_scales, cache->ks_page, cache->ks_token, cache->ks_head};
+  E.vs = AttnSide{cache->v_scales, cache->vs_page, cache->vs_token, cache->vs_head};
+  P.num_pages = cache->num_pages;
+  P.page_size = cache->page_size;
+  P.page_shift = log2_or_minus_one(cache->page_size);
+  P.table = table;
+  P.ld_table = ld_table ? ld_table : table_cols;
+  P.kv_lens = kv_lens;
+  P.q_starts = q_starts;
+  P.seqs = seqs;
+  P.T = T;
+  P.max_q = (int64_t)max_q < T ? max_q : (int)T;
+  P.heads_q = heads_q;
+  P.heads_kv = cache->heads;
+  P.group = heads_q / cache->heads;
+  P.head_dim = hd;
+  P.c = c;
+  P.v_scale = cache->v_scale;
+  P.causal = causal;
+  P.window = window;
+  P.lse = lse;
+
+  if (plan.widen) {
+    WidenParams W;
+    W.P = E;
+    W.k = (uint16_t*)ws;
+    W.v = (uint16_t*)((char*)ws + plan.side_bytes);
+    W.table = (int*)((char*)ws + 2 * plan.side_bytes);
+    W.cols = plan.cols;
+    const int64_t ctas = (int64_t)seqs * plan.cols * cache->heads * 2;
+    if (ctas > 0) {
+      const cudaError_t e = launch_overlapped(e2m1_widen_kernel_for(), (unsigned)ctas, (unsigned)kE2m1WidenThreads, 0, stream, W);
+      if (e != cudaSuccess) return set_cuda_error(e);
+      rc = finish_launch("attn_e2m1");
+      if (rc != QKNORM_OK) return rc;
+    }
+    qknorm_paged_cache wide = {};
+    wide.k = W.k;
+    wide.v = W.v;
+    wide.k_token = wide.v_token = hd;
+    wide.k_head = wide.v_head = (int64_t)kE2m1Page * hd;
+    wide.k_page = wide.v_page = (int64_t)cache->heads * kE2m1Page * hd;
+    wide.num_pages = (int64_t)seqs * plan.cols;
+    wide.page_size = kE2m1Page;
+    wide.heads = cache->heads;
+    wide.head_dim = hd;
+    const float s = fmaxf((float)((double)scale * cache->k_scale), 1.401298464e-45f);
+    return run_attn(q, ld_q, &wide, W.table, plan.cols, 0, kv_lens, q_starts, seqs, T, max_q, (int)P.max_keys, heads_q, s, causal, window,
+                    out, ld_out, lse, (char*)W.table + plan.table_bytes, plan.rest, stream, cache->v_scale);
+  }
+
+  E.chunk = plan.chunk;
+  E.splits = plan.splits;
+  E.row_tiles = plan.row_tiles;
+  E.tile_rows = 8 * plan.nt;
+  const int blocks = hd / 16, low = blocks & -blocks;
+  E.scale_unit = low > 8 ? 8 : low;
+  E.q_vec = ((uintptr_t)q | (uintptr_t)P.ld_q * 2) % 16 == 0;
+  if (plan.splits > 1) {
+    E.part_o = (float*)ws;
+    E.part_z = E.part_o + T * heads_q * plan.splits * hd;
+  }
+  int smem = 0, per_sm = 0;
+  const int copy = f.vec16 ? 16 : 8;
+  AttnE2m1Kernel fn = hd <= 64 ? attn_e2m1_kernel_64(plan.nt, copy, &smem, &per_sm)
+                      : hd <= 128 ? attn_e2m1_kernel_128(plan.nt, copy, &smem, &per_sm) : attn_e2m1_kernel_256(plan.nt, copy, &smem, &per_sm);
+  rc = allow_dynamic_smem((const void*)fn, smem);
+  if (rc != QKNORM_OK) return rc;
+  const int64_t ctas = (int64_t)seqs * plan.splits * cache->heads * plan.row_tiles;
+  cudaError_t e = launch_overlapped(fn, (unsigned)ctas, (unsigned)kE2m1Threads, (size_t)smem, stream, E);
+  if (e != cudaSuccess) return set_cuda_error(e);
+  rc = finish_launch("attn_e2m1");
+  if (rc != QKNORM_OK || plan.splits == 1) return rc;
+  int64_t joins = ((int64_t)seqs * P.max_q * heads_q + kE2m1JoinThreads / 32 - 1) / (kE2m1JoinThreads / 32);
+  if (joins > 16 * (int64_t)dev->sm_count) joins = 16 * (int64_t)dev->sm_count;
+  e = launch_overlapped(attn_e2m1_join_kernel_for(), (unsigned)joins, (unsigned)kE2m1JoinThreads, 0, stream, E);
+  if (e != cudaSuccess) return set_cuda_error(e);
+  return finish_launch("attn_e2m1");
 }

@@ -72,6 +72,32 @@ __device__ __forceinline__ uint32_t e4m3_pack2(float lo, float hi) {
   return (uint32_t)r;
 }
 
+// Eight E2M1 codes of a word -> four fp16 pairs, byte by byte, the low four bits in the low half (exact: every E2M1 value is an
+// fp16 value).
+__device__ __forceinline__ void e2m1x8_to_f16x2(uint32_t w, uint32_t (&f)[4]) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+      : "=r"(f[0]), "=r"(f[1]), "=r"(f[2]), "=r"(f[3])
+      : "r"(w));
+}
+// Eight fp32 -> eight E2M1 codes, element 0 in the low four bits; nearest even, saturating at +-6.
+__device__ __forceinline__ uint32_t e2m1_pack8(const float2 (&v)[4]) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+      : "=r"(r)
+      : "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y));
+  return r;
+}
+
 // ---- storage formats --------------------------------------------------------------------------
 
 struct IoBf16 {

@@ -33,17 +33,26 @@ struct RopeSide {
 
 struct CacheSide {
   void* base;
-  long long page, token, head;  // strides, elements
+  long long page, token, head;  // strides, elements (4-bit cache: bytes)
   float inv_scale;
+};
+
+// The 4-bit cache as the template's CIO: its stores work on blocks of 16, below.
+struct IoE2m1 {
+  static constexpr int kBytes = 0;
 };
 
 struct RopeParams {
   RopeSide q, k, v;  // v only with a cache
   CacheSide ck, cv;
+  CacheSide cks, cvs;  // the block scales of a 4-bit cache
   const long long* slots;
   long long num_slots;  // num_pages * page_size
   int page_size, page_shift;  // page_shift: log2(page_size), or -1
-  const long long* positions;
+  const long long* positions;  // [T], or with several axes [axes][T], ld_pos apart
+  const unsigned char* axis;   // which axis turns a pair; nullptr: the first
+  long long ld_pos;
+  int axes;
   const double* inv_freq;
   float mscale;
   int rot_dim, interleaved;
@@ -58,6 +67,13 @@ struct RopeParams {
 
 enum { kNormNone = 0, kNormLayer = 1, kNormHead = 2 };
 constexpr int kRopeMaxPairs = 256;  // QKNORM_MAX_HEAD_DIM / 2
+
+// The position at which pair i of token t stands; `first` is its position along the first axis.
+__device__ __forceinline__ long long rope_pos(const RopeParams& R, long long t, int i, long long first) {
+  if (R.axis == nullptr) return first;
+  const int a = R.axis[i];
+  return a < R.axes ? R.positions[a * R.ld_pos + t] : 0;
+}
 
 // cos and sin of pair i of the token at `pos`
 __device__ __forceinline__ float2 rope_cs(const RopeParams& R, long long pos, int i) {
@@ -128,6 +144,42 @@ struct Chunk8<IoE4m3> {
   }
 };
 
+// What goes into a 4-bit cache (include/qknorm_attn.h: qknorm_fwd_append_e2m1).
+
+// The larger magnitude, or NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float absmax8(const float2 (&v)[4]) {
+  float m = max_nan(fabsf(v[0].x), fabsf(v[0].y));
+#pragma unroll
+  for (int e = 1; e < 4; ++e) m = max_nan(m, max_nan(fabsf(v[e].x), fabsf(v[e].y)));
+  return m;
+}
+// The E4M3 scale of a block whose largest magnitude is amax, as its byte, and its value.
+__device__ __forceinline__ float e2m1_scale(float amax, uint32_t& byte) {
+  byte = e4m3_pack2(__fdiv_rn(amax, 6.0f), 0.f) & 0xffu;
+  uint32_t f01, f23;
+  e4m3x4_to_f16x2(byte, f01, f23);
+  return __half2float(__ushort_as_half((unsigned short)(f01 & 0xffffu)));
+}
+// Codes of eight elements of a block with that scale f, r = 1/f (0 for f = 0).  A tie between two codes is common (bf16 values over a
+// scale of four bits), so the quotient is the correctly rounded one: a product with r and one correction by its remainder (Markstein).
+// Magnitudes beyond 1e30, whose remainder may overflow, are far beyond +-6.
+__device__ __forceinline__ uint32_t e2m1_codes8(const float2 (&v)[4], float f, float r) {
+  const float2 rr = make_float2(r, r), ff = make_float2(-f, -f);
+  float2 y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 x = make_float2(fminf(fmaxf(v[e].x, -1e30f), 1e30f), fminf(fmaxf(v[e].y, -1e30f), 1e30f));
+    const float2 q = __fmul2_rn(x, rr);
+    y[e] = __ffma2_rn(__ffma2_rn(q, ff, x), rr, q);
+  }
+  return e2m1_pack8(y);
+}
+
 // Where token slot `slot` (in range) starts in a cache side.
 __device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot, int page_size, int page_shift) {
   long long page;
@@ -193,15 +245,20 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
     cslot = R.slots[t];
     if (cslot >= R.num_slots) cslot = -1;
   }
-  long long slot_k = 0, slot_v = 0;  // where the token's slot starts in the pools
+  constexpr bool kBlocks = CACHE && CIO::kBytes == 0;
+  long long slot_k = 0, slot_v = 0, slot_ks = 0, slot_vs = 0;  // where the token's slot starts in the pools
   if (CACHE && cslot >= 0) {
     slot_k = cache_at(R.ck, cslot, R.page_size, R.page_shift);
     slot_v = cache_at(R.cv, cslot, R.page_size, R.page_shift);
+    if constexpr (kBlocks) {
+      slot_ks = cache_at(R.cks, cslot, R.page_size, R.page_shift);
+      slot_vs = cache_at(R.cvs, cslot, R.page_size, R.page_shift);
+    }
   }
   if (live && r16 > 0) {
     const long long pos = R.positions[t];
     for (int p = tid; p < 8 * r16; p += R.threads_per_token) {
-      const float2 f = rope_cs(R, pos, p);
+      const float2 f = rope_cs(R, rope_pos(R, t, p, pos), p);
       float* at = reinterpret_cast<float*>(cs + ((p & 7) >> 1) * r16 + (p >> 3)) + (p & 1);
       at[0] = f.x;
       at[2] = f.y;
@@ -293,6 +350,36 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
     if (to_cache) {
       if (cslot < 0) continue;
       const CacheSide& C = side[i] == 1 ? R.ck : R.cv;
+      if constexpr (kBlocks) {
+        // A chunk of the half layout is half a block; the other half is the neighbouring lane's (rot_dim is a multiple of 32
+        // then, so it is a lane of the same head, and of the same part of it).
+        const CacheSide& S = side[i] == 1 ? R.cks : R.cvs;
+        const bool split = turns && !INTER;
+        const float2 k2 = make_float2(C.inv_scale, C.inv_scale);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[e] = __fmul2_rn(a[e], k2);
+          b[e] = __fmul2_rn(b[e], k2);
+        }
+        float ma = absmax8(a), mb = absmax8(b);
+        if (split) {
+          const unsigned pair = 3u << (threadIdx.x & 30);
+          ma = max_nan(ma, __shfl_xor_sync(pair, ma, 1));
+          mb = max_nan(mb, __shfl_xor_sync(pair, mb, 1));
+        } else {
+          ma = mb = max_nan(ma, mb);
+        }
+        uint32_t sa, sb;
+        const float fa = e2m1_scale(ma, sa), fb = e2m1_scale(mb, sb);
+        const float ra = fa > 0.f ? __frcp_rn(fa) : 0.f, rb = fb > 0.f ? __frcp_rn(fb) : 0.f;
+        char* codes = reinterpret_cast<char*>(C.base) + (side[i] == 1 ? slot_k : slot_v) + head[i] * C.head + (c0 >> 1);
+        __stcs(reinterpret_cast<uint32_t*>(codes), e2m1_codes8(a, fa, ra));
+        __stcs(reinterpret_cast<uint32_t*>(codes + (step >> 1)), e2m1_codes8(b, fb, rb));
+        unsigned char* sc = reinterpret_cast<unsigned char*>(S.base) + (side[i] == 1 ? slot_ks : slot_vs) + head[i] * S.head;
+        if (!split || !(j & 1)) sc[c0 >> 4] = (unsigned char)sa;
+        else sc[(c0 + step) >> 4] = (unsigned char)sb;
+        continue;
+      } else {
       const long long at = (side[i] == 1 ? slot_k : slot_v) + head[i] * C.head + c0;
       Chunk8<CIO> o0, o1;
       if constexpr (CIO::kBytes == 1 || IO::kBytes == 1) {
@@ -313,6 +400,7 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
       }
       o0.store(C.base, at);
       o1.store(C.base, at + step);
+      }
     } else {
       const RopeSide& A = side[i] == 0 ? R.q : R.k;
       char* row = reinterpret_cast<char*>(A.y) + t * A.ldy * IO::kBytes;
@@ -334,6 +422,8 @@ template <class IO, class CIO, bool CACHE>
 __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const __grid_constant__ RopeParams R, int norm) {
   __shared__ float2 cs[kRopeMaxPairs];
   __shared__ float red[kRopeGeneralThreads / 32];
+  constexpr bool kBlocks = CACHE && CIO::kBytes == 0;
+  __shared__ float whole[kBlocks ? kRopeGeneralThreads / 32 : 1][kBlocks ? kRopeMaxPairs : 1];  // a warp's head, before it is cut into blocks
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int pairs = R.rot_dim >> 1, singles = R.head_dim - R.rot_dim;
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -341,7 +431,7 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
     __syncthreads();  // the previous token's cos and sin are no longer needed
     if (pairs > 0) {
       const long long pos = R.positions[t];
-      for (int p = threadIdx.x; p < pairs; p += kRopeGeneralThreads) cs[p] = rope_cs(R, pos, p);
+      for (int p = threadIdx.x; p < pairs; p += kRopeGeneralThreads) cs[p] = rope_cs(R, rope_pos(R, t, p, pos), p);
     }
     long long cslot = -1;
     if (CACHE) {
@@ -394,8 +484,16 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
         if (to_cache && cslot < 0) continue;
         const long long y0 = to_cache ? cache_at(C, cslot, R.page_size, R.page_shift) + h * C.head : t * A.ldy + (long long)h * R.head_dim;
         auto put = [&](int i, float v) {
-          if (to_cache) CIO::store(C.base, y0 + i, CIO::kBytes == 1 ? v * C.inv_scale : v);
-          else IO::store(A.y, y0 + i, v);
+          if constexpr (kBlocks) {
+            if (to_cache) {
+              whole[warp][i] = v * C.inv_scale;
+              return;
+            }
+          } else if (to_cache) {
+            CIO::store(C.base, y0 + i, CIO::kBytes == 1 ? v * C.inv_scale : v);
+            return;
+          }
+          IO::store(A.y, y0 + i, v);
         };
         for (int p = lane; p < pairs; p += 32) {
           const int ia = R.interleaved ? 2 * p : p, ib = R.interleaved ? 2 * p + 1 : p + pairs;
@@ -405,6 +503,27 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
           put(ib, side != 2 ? b * f.x + a * f.y : b);
         }
         for (int i = lane; i < singles; i += 32) put(R.rot_dim + i, value(R.rot_dim + i));
+        if constexpr (kBlocks) {
+          if (to_cache) {
+            const CacheSide& S = side == 2 ? R.cvs : R.cks;
+            unsigned char* sc = reinterpret_cast<unsigned char*>(S.base) + cache_at(S, cslot, R.page_size, R.page_shift) + h * S.head;
+            __syncwarp();
+            for (int blk = lane; blk < R.head_dim / 16; blk += 32) {
+              float2 lo[4], hi[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                lo[e] = make_float2(whole[warp][16 * blk + 2 * e], whole[warp][16 * blk + 2 * e + 1]);
+                hi[e] = make_float2(whole[warp][16 * blk + 8 + 2 * e], whole[warp][16 * blk + 9 + 2 * e]);
+              }
+              uint32_t byte;
+              const float f = e2m1_scale(max_nan(absmax8(lo), absmax8(hi)), byte), r1 = f > 0.f ? __frcp_rn(f) : 0.f;
+              *reinterpret_cast<uint2*>(reinterpret_cast<char*>(C.base) + y0 + 8 * blk) =
+                  make_uint2(e2m1_codes8(lo, f, r1), e2m1_codes8(hi, f, r1));
+              sc[blk] = (unsigned char)byte;
+            }
+            __syncwarp();
+          }
+        }
       }
     }
   }
@@ -412,7 +531,8 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
 
 typedef void (*RopeKernel)(const RopeParams);
 typedef void (*RopeGeneralKernel)(const RopeParams, int);
-// in qknorm_rope_inst.cu; upt 1 or 4, threads: of the CTA; cache_bytes 0 = no cache
+// in qknorm_rope_inst.cu; upt 1 or 4, threads: of the CTA; cache_bytes 0 = no cache, kCacheE2m1 = the 4-bit one
+constexpr int kCacheE2m1 = 4;
 RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, bool interleaved, int upt, int threads);
 RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes);
 

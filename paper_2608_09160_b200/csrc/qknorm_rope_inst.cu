@@ -28,11 +28,13 @@ RopeKernel rope_kernel_for(int elem_bytes, int cache_bytes, int norm, bool inter
   if (cache_bytes == 0)
     return elem_bytes == 1 ? pick<IoE4m3, IoE4m3, kNormNone, false>(interleaved, upt, threads)
                            : pick<IoBf16, IoBf16, kNormNone, false>(interleaved, upt, threads);
+  if (cache_bytes == kCacheE2m1) return pick_cache<IoE2m1>(norm, interleaved, upt, threads);
   return cache_bytes == 1 ? pick_cache<IoE4m3>(norm, interleaved, upt, threads) : pick_cache<IoBf16>(norm, interleaved, upt, threads);
 }
 
 RopeGeneralKernel rope_general_kernel_for(int elem_bytes, int cache_bytes) {
   if (cache_bytes == 0) return elem_bytes == 1 ? rope_general_kernel<IoE4m3, IoE4m3, false> : rope_general_kernel<IoBf16, IoBf16, false>;
+  if (cache_bytes == kCacheE2m1) return rope_general_kernel<IoBf16, IoE2m1, true>;
   return cache_bytes == 1 ? rope_general_kernel<IoBf16, IoE4m3, true> : rope_general_kernel<IoBf16, IoBf16, true>;
 }
 
