@@ -207,7 +207,8 @@ int qknorm_fwd_append_axes(const void* q, const void* k, const void* v, const vo
  *   head_dim: a multiple of 16 up to QKNORM_MAX_HEAD_DIM_E2M1.
  *   k and v with their strides: multiples of 8 bytes (of 16 for the faster copies, head_dim a multiple of 32 then).
  *   k_scales and v_scales with theirs: multiples of the largest power of two up to 8 that divides head_dim/16.
- * A page whose heads lie one after the other (strides: head > token) reads fastest.
+ * Fastest to read: a head's tokens one after the other in a page (k_token = head_dim/2, ks_token = head_dim/16), head_dim 64 or 128,
+ * pages of a multiple of 8 tokens, addresses and the other strides multiples of 16 bytes.
  */
 typedef struct {
   void* k;

@@ -8,66 +8,67 @@ namespace qknorm {
 #define QKNORM_PASTE(a, b) QKNORM_PASTE_(a, b)
 
 namespace {
+template <int NT, int COPY>
+E2m1Launch one() {
+  return E2m1Launch{attn_e2m1_kernel<QKNORM_DP, NT, COPY>, E2m1Cta<QKNORM_DP, NT, COPY>::kSmem, E2m1Cta<QKNORM_DP, NT, COPY>::kWarps,
+                    E2m1Cta<QKNORM_DP, NT, COPY>::kPerSm};
+}
 template <int NT>
-AttnE2m1Kernel pick(int copy, int* smem, int* per_sm) {
-  *smem = E2m1Cta<QKNORM_DP, NT>::kSmem;
-  *per_sm = E2m1Cta<QKNORM_DP, NT>::kPerSm;
-  return copy == 16 ? attn_e2m1_kernel<QKNORM_DP, NT, 16> : attn_e2m1_kernel<QKNORM_DP, NT, 8>;
+E2m1Launch pick(int copy) {
+#if QKNORM_DP < 256
+  if (copy == 0) return one<NT, 0>();
+#endif
+  return copy == 16 ? one<NT, 16>() : one<NT, 8>();
 }
 }  // namespace
 
-AttnE2m1Kernel QKNORM_PASTE(attn_e2m1_kernel_, QKNORM_DP)(int nt, int copy, int* smem, int* per_sm) {
-  switch (nt) {
-    case 1: return pick<1>(copy, smem, per_sm);
-    case 2: return pick<2>(copy, smem, per_sm);
-#if QKNORM_DP < 256
-    case 4: return pick<4>(copy, smem, per_sm);
-#endif
-    default: return nullptr;
-  }
+E2m1Launch QKNORM_PASTE(attn_e2m1_kernel_, QKNORM_DP)(int nt, int copy) {
+  return nt == 1 ? pick<1>(copy) : pick<2>(copy);
 }
 
 #if QKNORM_DP == 64
 __global__ void __launch_bounds__(kE2m1JoinThreads) attn_e2m1_join_kernel(const __grid_constant__ AttnE2m1Params P) {
   const AttnParams& A = P.A;
-  const int lane = threadIdx.x & 31;
-  const long long warps = (long long)gridDim.x * (kE2m1JoinThreads / 32), items = (long long)A.seqs * A.max_q * A.heads_q;
+  const int lane = threadIdx.x & 31, rows = P.heads_cta * P.tile_rows;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (long long it = (long long)blockIdx.x * (kE2m1JoinThreads / 32) + (threadIdx.x >> 5); it < items; it += warps) {
-    const int head = (int)(it % A.heads_q), i = (int)(it / A.heads_q % A.max_q), b = (int)(it / A.heads_q / A.max_q);
-    const AttnSeq s = attn_seq(A, b);
-    if (i >= s.n) continue;
-    const long long r = (long long)i * A.group + head % A.group;
-    const E2m1Span u = e2m1_span(P, s, r - r % P.tile_rows);
-    if (u.c0 == u.c1) continue;
+  const int* cut = P.cuts + blockIdx.x * 8;
+  const int b = cut[0];
+  if (b < 0) return;
+  const int rt = cut[1], hg = cut[2], c0 = cut[3], slot0 = cut[4], parts = blockIdx.x - c0 + 1;
+  const AttnSeq s = attn_seq(A, b);
+  // part p of row k lies with CTA c0 + p, in slot 0 but for the first
+  auto place = [&](int p, int k) { return ((long long)(c0 + p) * 2 + (p == 0 ? slot0 : 0)) * rows + k; };
+  for (int k = blockIdx.y * (kE2m1JoinThreads / 32) + (threadIdx.x >> 5); k < rows; k += gridDim.y * (kE2m1JoinThreads / 32)) {
+    const unsigned rr = (unsigned)rt * (unsigned)P.tile_rows + (unsigned)(k % P.tile_rows);
+    if (rr >= (unsigned)s.n * (unsigned)A.group) continue;
+    const int i = (int)(rr / (unsigned)A.group), head = (hg * P.heads_cta + k / P.tile_rows) * A.group + (int)(rr - (unsigned)i * (unsigned)A.group);
     const long long row = s.row0 + (long long)i;
-    const long long at = (row * A.heads_q + head) * P.splits;
     float z = kNegInf;
-    for (int c = u.c0 + lane; c <= u.c1; c += 32) z = fmaxf(z, P.part_z[at + c]);  // NaN passes by; its weight below will be NaN
+    for (int p = lane; p < parts; p += 32) z = fmaxf(z, P.part_z[place(p, k)]);  // NaN passes by; its weight below will be NaN
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, o));
     for (int d0 = 0; d0 < A.head_dim; d0 += 128) {
       const int d = d0 + 4 * lane;
       float acc[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-      for (int c0 = u.c0; c0 <= u.c1; c0 += 32) {  // a lane each for the parts' weights, then four parts' rows at a time
-        const float zp = c0 + lane <= u.c1 ? P.part_z[at + c0 + lane] : kNegInf;
+      for (int p0 = 0; p0 < parts; p0 += 32) {  // a lane each for the parts' weights, then four parts' rows at a time
+        const float zp = p0 + lane < parts ? P.part_z[place(p0 + lane, k)] : kNegInf;
         const float wp = zp == kNegInf ? 0.f : z == kNegInf ? zp : exp2f(zp - z);
-        const int n = u.c1 - c0 + 1 < 32 ? u.c1 - c0 + 1 : 32;
+        const int n = parts - p0 < 32 ? parts - p0 : 32;
         for (int p = 0; p < n; p += 4) {
           float4 x[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            x[k] = p + k < n && d < A.head_dim ? *reinterpret_cast<const float4*>(P.part_o + (at + c0 + p + k) * A.head_dim + d)
+          for (int e = 0; e < 4; ++e)
+            x[e] = p + e < n && d < A.head_dim ? *reinterpret_cast<const float4*>(P.part_o + place(p0 + p + e, k) * A.head_dim + d)
                                                : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float w = __shfl_sync(0xffffffffu, wp, (p + k) & 31);
-            if (p + k >= n) continue;
+          for (int e = 0; e < 4; ++e) {
+            const float w = __shfl_sync(0xffffffffu, wp, (p + e) & 31);
+            if (p + e >= n) continue;
             sum += w;
-            acc[0] = fmaf(w, x[k].x, acc[0]);
-            acc[1] = fmaf(w, x[k].y, acc[1]);
-            acc[2] = fmaf(w, x[k].z, acc[2]);
-            acc[3] = fmaf(w, x[k].w, acc[3]);
+            acc[0] = fmaf(w, x[e].x, acc[0]);
+            acc[1] = fmaf(w, x[e].y, acc[1]);
+            acc[2] = fmaf(w, x[e].z, acc[2]);
+            acc[3] = fmaf(w, x[e].w, acc[3]);
           }
         }
       }
@@ -75,13 +76,13 @@ __global__ void __launch_bounds__(kE2m1JoinThreads) attn_e2m1_join_kernel(const 
       if (d < A.head_dim) {
         uint16_t* out = A.out + row * A.ld_out + (long long)head * A.head_dim + d;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) IoBf16::store(out, k, acc[k] * inv);
+        for (int e = 0; e < 4; ++e) IoBf16::store(out, e, acc[e] * inv);
       }
       if (A.lse != nullptr && lane == 0 && d == 0) A.lse[row * A.heads_q + head] = sum == 0.f ? kNegInf : (z + log2f(sum)) * kLn2;
     }
   }
 }
-AttnE2m1Kernel attn_e2m1_join_kernel_for() { return attn_e2m1_join_kernel; }
+AttnE2m1JoinKernel attn_e2m1_join_kernel_for() { return attn_e2m1_join_kernel; }
 
 // A CTA per (sequence, page, head, side).
 __global__ void __launch_bounds__(kE2m1WidenThreads) e2m1_widen_kernel(const __grid_constant__ WidenParams W) {
@@ -103,33 +104,45 @@ __global__ void __launch_bounds__(kE2m1WidenThreads) e2m1_widen_kernel(const __g
   const AttnSide& C = side ? A.v : A.k;
   const AttnSide& S = side ? W.P.vs : W.P.ks;
   uint16_t* out = (side ? W.v : W.k) + (((long long)b * W.cols + j) * A.heads_kv + h) * kE2m1Page * A.head_dim;
-  for (int i = threadIdx.x; i < kE2m1Page * blocks; i += kE2m1WidenThreads) {
-    const int in = i / blocks, blk = i - in * blocks;
-    const long long key = first + in;
-    uint32_t y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (key >= lo && key < hi) {
-      int within;
-      const long long page = attn_page(A, b, (int)key, within);
-      if (page >= 0) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const char*>(C.base) + page * C.page + within * C.token + h * C.head) + blk);
-        const uint32_t byte = __ldg(reinterpret_cast<const unsigned char*>(S.base) + page * S.page + within * S.token + h * S.head + blk);
-        uint32_t f[4], sc, none;
-        e4m3x4_to_f16x2(byte, sc, none);
-        const float scale = __half2float(__ushort_as_half((unsigned short)(sc & 0xffffu)));
+  constexpr int kAhead = 4;  // blocks of a thread whose loads are under way together
+  for (int i0 = threadIdx.x; i0 < kE2m1Page * blocks; i0 += kAhead * kE2m1WidenThreads) {
+    uint2 w[kAhead];
+    uint32_t byte[kAhead];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          e2m1x8_to_f16x2(half ? w.y : w.x, f);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&f[k]));
-            y[4 * half + k] = bf_pack(v.x * scale, v.y * scale);
-          }
+    for (int a = 0; a < kAhead; ++a) {
+      const int i = i0 + a * kE2m1WidenThreads, in = i / blocks, blk = i - in * blocks;
+      const long long key = first + in;
+      w[a] = make_uint2(0, 0);
+      byte[a] = 0;
+      if (i < kE2m1Page * blocks && key >= lo && key < hi) {
+        int within;
+        const long long page = attn_page(A, b, (int)key, within);
+        if (page >= 0) {
+          w[a] = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const char*>(C.base) + page * C.page + within * C.token + h * C.head) + blk);
+          byte[a] = __ldg(reinterpret_cast<const unsigned char*>(S.base) + page * S.page + within * S.token + h * S.head + blk);
         }
       }
     }
-    uint4* to = reinterpret_cast<uint4*>(out + (long long)in * A.head_dim + 16 * blk);
-    to[0] = make_uint4(y[0], y[1], y[2], y[3]);
-    to[1] = make_uint4(y[4], y[5], y[6], y[7]);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) {
+      const int i = i0 + a * kE2m1WidenThreads;
+      if (i >= kE2m1Page * blocks) break;
+      uint32_t f[4], sc, none, y[8];
+      e4m3x4_to_f16x2(byte[a], sc, none);
+      const float scale = __half2float(__ushort_as_half((unsigned short)(sc & 0xffffu)));
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        e2m1x8_to_f16x2(half ? w[a].y : w[a].x, f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&f[k]));
+          y[4 * half + k] = bf_pack(v.x * scale, v.y * scale);
+        }
+      }
+      uint4* to = reinterpret_cast<uint4*>(out + 16ll * i);  // rows lie one after the other
+      to[0] = make_uint4(y[0], y[1], y[2], y[3]);
+      to[1] = make_uint4(y[4], y[5], y[6], y[7]);
+    }
   }
 }
 WidenKernel e2m1_widen_kernel_for() { return e2m1_widen_kernel; }

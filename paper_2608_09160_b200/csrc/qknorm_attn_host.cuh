@@ -837,15 +837,30 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
 // How a call over a 4-bit cache is cut: sizes only, so that the workspace can be asked for beforehand.
 struct E2m1Plan {
   bool widen = false;
-  int nt = 1, row_tiles = 1, chunk = 0, splits = 1, cols = 0;
-  int64_t parts = 0;         // of a head's row
-  int64_t side_bytes = 0;    // widened K, or V
+  // TMA, where the layout allows it: for whole heads' copies of several heads, and long shares.  us, single tokens of 8 query heads a key
+  // head, TMA with 8 (4, 2) heads a copy | cp.async: 64 x 8192 keys 102 | 123, 16 x 32000 keys 97 (102, 106) | 109, 256 x 500 keys 53 | 59, but
+  // 64 x 1000 keys 33 | 31, 16 x 2000 keys 27 | 21, 4 x 8192 keys 43 | 23; 2 key heads, 32 x 4000 keys 45 | 32.
+  bool tma = false;
+  int nt = 1, row_tiles = 1, cols = 0;
+  struct Way {  // by cp.async, by TMA
+    int heads = 1, grid = 1;
+    bool shares = false;
+  } way[2];
+  int64_t parts = 0;                  // rows of parts, at most
+  int64_t side_bytes = 0;             // widened K, or V
   int64_t table_bytes = 0, rest = 0;  // rest: what attn_tc asks for itself
-  int64_t bytes() const { return widen ? 2 * side_bytes + table_bytes + rest : (parts * 4 + 15) / 16 * 16; }
+  int64_t cut_bytes = 0;
+  int64_t need = 0;
 };
 
-constexpr int kE2m1WidenRows = 64;                      // rows of a sequence and key head from which widening pays
+// Rows of a sequence and key head from which widening pays: 16 sequences of 4096 keys, 8 key heads, 60 rows 74 us against 112 widened, 85 rows
+// about 105 against 114; 4 sequences of 8192 keys with 2560 rows 1074 against 245.
+constexpr int kE2m1WidenRows = 96;
 constexpr int64_t kE2m1WidenMost = (int64_t)2 << 30;    // bytes of the widened cache
+
+E2m1Launch e2m1_kernel(int head_dim, int nt, int copy) {
+  return head_dim <= 64 ? attn_e2m1_kernel_64(nt, copy) : head_dim <= 128 ? attn_e2m1_kernel_128(nt, copy) : attn_e2m1_kernel_256(nt, copy);
+}
 
 int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, bool causal, int window, int sms,
               E2m1Plan* out) {
@@ -860,29 +875,60 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
     p.widen = true;
     p.table_bytes = ((int64_t)seqs * p.cols * 4 + 15) / 16 * 16;
     p.rest = attn_workspace(tc, head_dim);
+    p.need = 2 * p.side_bytes + p.table_bytes + p.rest;
     *out = p;
     return QKNORM_OK;
   }
-  p.nt = rows <= 8 ? 1 : rows <= 16 || head_dim > 128 ? 2 : 4;
+  if (rows > 0x7fffffff) return QKNORM_ERR_SHAPE;
+  p.nt = rows <= 8 ? 1 : 2;
   const int64_t row_tiles = (rows + 8 * p.nt - 1) / (8 * p.nt);
   int64_t span = max_keys;
   if (window > 0) {  // the first row's window, and what the later ones see behind it
     const int64_t w = (int64_t)window + (causal ? max_q : T) - 1;
     if (w < span) span = w;
   }
-  // Equal chunks, about six CTAs for each place on the GPU, and four tiles of 32 keys at least.
-  const int64_t units = row_tiles * heads_kv * seqs, want = (6 * 3 * (int64_t)sms + units - 1) / units;
-  int64_t chunk = (span + want - 1) / want;
-  chunk = (chunk + 127) / 128 * 128;
-  if (chunk < 128) chunk = 128;
-  const int64_t splits = span > 0 ? (span + chunk - 1) / chunk : 1;
-  if (row_tiles * heads_kv > 0x7fffffff / splits || row_tiles * heads_kv * splits > 0x7fffffff / seqs) return QKNORM_ERR_SHAPE;
+  span += kE2m1Tile - 1;  // units start at a multiple of a tile
+  if (row_tiles > 0x3fffffff / seqs) return QKNORM_ERR_SHAPE;
   p.row_tiles = (int)row_tiles;
-  p.chunk = (int)chunk;
-  p.splits = (int)splits;
-  if (splits > 1) p.parts = T * heads_q * splits * (head_dim + 1);
+  for (int k = 0; k < 2; ++k) {
+    if (k == 1 && head_dim != 64 && head_dim != 128) continue;
+    const E2m1Launch kernel = e2m1_kernel(head_dim, p.nt, k == 1 ? 0 : 16);
+    E2m1Plan::Way& w = p.way[k];
+    while (k == 1 && 2 * w.heads <= kernel.warps && heads_kv % (2 * w.heads) == 0) w.heads *= 2;
+    const int round = kE2m1Tile * kernel.warps / w.heads;
+    const int64_t places = (int64_t)sms * kernel.per_sm, rounds = (span + round - 1) / round;
+    const int64_t units = row_tiles * seqs * (heads_kv / w.heads);
+    if (units > 0x7fffffff) return QKNORM_ERR_SHAPE;
+    w.shares = rounds > kE2m1Whole;
+    w.grid = (int)(!w.shares || units * rounds < places ? (w.shares ? units * rounds : units) : places);
+    if (k == 1) p.tma = w.heads >= 4 && units * rounds >= 8 * places;
+    if (!w.shares) continue;
+    const int64_t parts = (int64_t)w.grid * 2 * w.heads * 8 * p.nt;
+    if (parts > p.parts) p.parts = parts;
+    if (w.grid * 32 > p.cut_bytes) p.cut_bytes = w.grid * 32;
+  }
+  p.need = p.cut_bytes + (p.parts * (head_dim + 1) * 4 + 15) / 16 * 16;
   *out = p;
   return QKNORM_OK;
+}
+
+// One side of a 4-bit cache as [page][head][bytes of a page's tokens], in elements of `element` bytes; a copy takes `run` tokens of
+// `heads` heads.  False: no such map.
+bool encode_e2m1(CUtensorMap* map, const qknorm_paged_cache_e2m1& c, const AttnSide& s, int token_bytes, int element, int heads, int run) {
+  const EncodeTiled enc = encode_tiled();
+  if (!enc) return false;
+  // the stride of an axis of one is never used, but has to look like one
+  const cuuint64_t all = ((cuuint64_t)c.page_size * token_bytes + 15) / 16 * 16;
+  const cuuint64_t dims[3] = {(cuuint64_t)c.page_size * token_bytes / element, (cuuint64_t)c.heads, (cuuint64_t)c.num_pages};
+  const cuuint64_t strides[2] = {c.heads > 1 ? (cuuint64_t)s.head : all, c.num_pages > 1 ? (cuuint64_t)s.page : all};
+  if ((uintptr_t)s.base % 16 != 0) return false;
+  for (const cuuint64_t st : strides)
+    if (st == 0 || st % 16 != 0 || st >= ((cuuint64_t)1 << 40)) return false;
+  const cuuint32_t box[3] = {(cuuint32_t)(run * token_bytes / element), (cuuint32_t)heads, 1};
+  const cuuint32_t ones[3] = {1, 1, 1};
+  return enc(map, element == 8 ? CU_TENSOR_MAP_DATA_TYPE_INT64 : CU_TENSOR_MAP_DATA_TYPE_INT32, 3, const_cast<void*>(s.base), dims, strides, box, ones,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 int check_e2m1_sizes(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
@@ -906,7 +952,7 @@ int run_attn_e2m1_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_
     E2m1Plan p;
     rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, causal, window, dev->sm_count, &p);
     if (rc != QKNORM_OK) return rc;
-    if (p.bytes() > *bytes) *bytes = p.bytes();
+    if (p.need > *bytes) *bytes = p.need;
   }
   return QKNORM_OK;
 }
@@ -943,7 +989,7 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   E2m1Plan plan;
   rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, cache->heads, hd, causal != 0, window, dev->sm_count, &plan);
   if (rc != QKNORM_OK) return rc;
-  const int64_t need = plan.bytes();
+  const int64_t need = plan.need;
   CallRegions r;
   r.own[r.outs] = -1;
   r.out[r.outs++] = Region{(uintptr_t)out, (uintptr_t)T, (uintptr_t)d * 2, (uintptr_t)P.ld_out * 2};
@@ -991,6 +1037,7 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   P.causal = causal;
   P.window = window;
   P.lse = lse;
+  P.error = dev->ring_error;
 
   if (plan.widen) {
     WidenParams W;
@@ -1021,31 +1068,43 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
                     out, ld_out, lse, (char*)W.table + plan.table_bytes, plan.rest, stream, cache->v_scale);
   }
 
-  E.chunk = plan.chunk;
-  E.splits = plan.splits;
   E.row_tiles = plan.row_tiles;
   E.tile_rows = 8 * plan.nt;
   const int blocks = hd / 16, low = blocks & -blocks;
   E.scale_unit = low > 8 ? 8 : low;
   E.q_vec = ((uintptr_t)q | (uintptr_t)P.ld_q * 2) % 16 == 0;
-  if (plan.splits > 1) {
-    E.part_o = (float*)ws;
-    E.part_z = E.part_o + T * heads_q * plan.splits * hd;
+  E.out_vec = ((uintptr_t)out | (uintptr_t)P.ld_out * 2) % 16 == 0;
+  if (plan.parts > 0) {
+    E.cuts = (int*)ws;
+    E.part_o = (float*)((char*)ws + plan.cut_bytes);
+    E.part_z = E.part_o + plan.parts * hd;
   }
-  int smem = 0, per_sm = 0;
-  const int copy = f.vec16 ? 16 : 8;
-  AttnE2m1Kernel fn = hd <= 64 ? attn_e2m1_kernel_64(plan.nt, copy, &smem, &per_sm)
-                      : hd <= 128 ? attn_e2m1_kernel_128(plan.nt, copy, &smem, &per_sm) : attn_e2m1_kernel_256(plan.nt, copy, &smem, &per_sm);
-  rc = allow_dynamic_smem((const void*)fn, smem);
+  E2m1Maps maps;
+  memset(&maps, 0, sizeof(maps));
+  int copy = f.vec16 ? 16 : 8;
+  // TMA: tokens of a head one after the other in codes and scales, everything on 16 bytes, pages of whole runs of 16 tokens; copies go to
+  // multiples of 128 bytes.
+  const int heads = plan.way[1].heads, tma = env_int("QKNORM_E2M1_TMA", -1);  // 0, 1: for tests
+  E.run_shift = cache->page_size % 32 == 0 ? 5 : 4;
+  if ((hd == 64 || hd == 128) && cache->page_size % 16 == 0 && cache->num_pages > 0 && P.k.token == hd / 2 && P.v.token == hd / 2 &&
+      E.ks.token == hd / 16 && E.vs.token == hd / 16 && (heads << E.run_shift) * (hd / 16) % 128 == 0 && (tma < 0 ? plan.tma : tma != 0) &&
+      encode_e2m1(&maps.k, *cache, P.k, hd / 2, 8, heads, 1 << E.run_shift) && encode_e2m1(&maps.v, *cache, P.v, hd / 2, 8, heads, 1 << E.run_shift) &&
+      encode_e2m1(&maps.ks, *cache, E.ks, hd / 16, 4, heads, 1 << E.run_shift) &&
+      encode_e2m1(&maps.vs, *cache, E.vs, hd / 16, 4, heads, 1 << E.run_shift))
+    copy = 0;
+  const E2m1Plan::Way& way = plan.way[copy == 0];
+  E.heads_cta = way.heads;
+  E.shares = way.shares;
+  P.grid = way.grid;
+  const E2m1Launch kernel = e2m1_kernel(hd, plan.nt, copy);
+  rc = allow_dynamic_smem((const void*)kernel.fn, kernel.smem);
   if (rc != QKNORM_OK) return rc;
-  const int64_t ctas = (int64_t)seqs * plan.splits * cache->heads * plan.row_tiles;
-  cudaError_t e = launch_overlapped(fn, (unsigned)ctas, (unsigned)kE2m1Threads, (size_t)smem, stream, E);
+  cudaError_t e = launch_overlapped(kernel.fn, (unsigned)way.grid, (unsigned)(32 * kernel.warps), (size_t)kernel.smem, stream, E, maps);
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_e2m1");
-  if (rc != QKNORM_OK || plan.splits == 1) return rc;
-  int64_t joins = ((int64_t)seqs * P.max_q * heads_q + kE2m1JoinThreads / 32 - 1) / (kE2m1JoinThreads / 32);
-  if (joins > 16 * (int64_t)dev->sm_count) joins = 16 * (int64_t)dev->sm_count;
-  e = launch_overlapped(attn_e2m1_join_kernel_for(), (unsigned)joins, (unsigned)kE2m1JoinThreads, 0, stream, E);
+  if (rc != QKNORM_OK || !way.shares) return rc;
+  e = launch_overlapped(attn_e2m1_join_kernel_for(), dim3((unsigned)way.grid, (unsigned)((way.heads * 8 * plan.nt + 7) / 8)),
+                        (unsigned)kE2m1JoinThreads, 0, stream, E);
   if (e != cudaSuccess) return set_cuda_error(e);
   return finish_launch("attn_e2m1");
 }

@@ -232,15 +232,21 @@ class Batch:
         return out, lse
 
 
+@pytest.fixture(params=["tma", "cp.async"])
+def copies(request, monkeypatch):
+    """Both ways of bringing tiles in, whichever the sizes would choose; a layout that TMA cannot bring takes the other."""
+    monkeypatch.setenv("QKNORM_E2M1_TMA", "1" if request.param == "tma" else "0")
+
+
 @pytest.mark.parametrize("order", ["hnd", "nhd"])
 @pytest.mark.parametrize("hq,hk,hd", [(1, 1, 128), (1, 1, 64), (8, 1, 128), (5, 1, 64), (8, 8, 128), (7, 1, 96), (40, 8, 128), (6, 2, 32),
                                       (3, 1, 16), (16, 1, 128), (9, 1, 64), (32, 1, 128), (4, 2, 256), (12, 1, 208), (2, 1, 80), (2, 2, 112)])
-def test_single_tokens(libqknorm, hq, hk, hd, order):
+def test_single_tokens(libqknorm, copies, hq, hk, hd, order):
     Batch([1, 1, 1, 1], [1, 130, 33, 128], hq, hk, hd, order=order, seed=hd).check()
 
 
 @pytest.mark.parametrize("page", [1, 7, 16, 24, 64, 128, 256])
-def test_pages_and_lengths(libqknorm, page):
+def test_pages_and_lengths(libqknorm, copies, page):
     Batch([1, 2, 1, 3, 1], [127, 129, 255, 257, 384], 4, 2, 64, page=page, seed=page).check()
 
 
@@ -248,7 +254,7 @@ def test_pages_and_lengths(libqknorm, page):
     (4, 2, 128, [16, 3, 1], [300, 129, 1]), (8, 1, 64, [7, 6, 4], [500, 16, 130]), (1, 1, 96, [50], [400]), (32, 1, 128, [2], [700]),
     (7, 1, 64, [9, 0, 2], [3000, 0, 5]), (3, 1, 256, [20, 11, 0], [2000, 11, 5]), (40, 8, 128, [5, 5], [1000, 5]), (2, 1, 160, [17], [40]),
 ])
-def test_several_new_tokens(libqknorm, hq, hk, hd, new, kv):
+def test_several_new_tokens(libqknorm, copies, hq, hk, hd, new, kv):
     Batch(new, kv, hq, hk, hd, seed=len(new)).check()
 
 
@@ -256,29 +262,41 @@ def test_several_new_tokens(libqknorm, hq, hk, hd, new, kv):
     (5, 1, 128, [60, 3, 26], [60, 200, 27]), (8, 2, 64, [16, 17, 33], [300, 17, 129]), (3, 1, 96, [100, 1, 0], [256, 300, 9]), (1, 1, 128, [300], [300]),
     (2, 2, 16, [70], [500]), (128, 1, 64, [2, 1], [130, 140]),
 ])
-def test_chunks_over_a_widened_cache(libqknorm, hq, hk, hd, new, kv):
-    Batch(new, kv, hq, hk, hd, seed=len(new)).check("attn_tc")
+def test_chunks(libqknorm, hq, hk, hd, new, kv):
+    """More than 96 rows of a sequence and key head: over a widened cache."""
+    Batch(new, kv, hq, hk, hd, seed=len(new)).check("attn_tc" if max(new) * hq // hk > 96 else "attn_e2m1")
 
 
 @pytest.mark.parametrize("new,variant", [([1, 1, 1], "attn_e2m1"), ([9, 4, 2], "attn_e2m1"), ([80, 1, 33], "attn_tc")])
 @pytest.mark.parametrize("window", [1, 31, 100, 1000])
 @pytest.mark.parametrize("causal", [True, False])
-def test_windows(libqknorm, causal, window, new, variant):
+def test_windows(libqknorm, copies, causal, window, new, variant):
     Batch(new, [400, 257, 90], 4, 2, 128, seed=window).check(variant, causal=causal, window=window)
 
 
 @pytest.mark.parametrize("new,kv,variant", [([3, 5], [1, 3], "attn_e2m1"), ([100, 4], [40, 0], "attn_tc"), ([1, 1], [0, 7], "attn_e2m1")])
-def test_rows_that_see_nothing(libqknorm, new, kv, variant):
+def test_rows_that_see_nothing(libqknorm, copies, new, kv, variant):
     """More new tokens than keys: the first rows stand before key 0."""
     out, lse = Batch(new, kv, 2, 1, 64, seed=1).check(variant)
 
 
-def test_long_rows_are_cut_and_joined(libqknorm):
+def test_long_rows_are_cut_and_joined(libqknorm, copies):
     b = Batch([1, 4], [20000, 5001], 8, 1, 128, seed=2)
     assert attn.attn_paged_e2m1_workspace(2, b.T, 4, 20000, 8, 1, 128) > 0
     out, lse = b.check()
     again, _ = b.call()
     assert torch.equal(out.view(torch.int16), again.view(torch.int16))
+
+
+@pytest.mark.parametrize("hq,hk,hd,new,kv", [
+    (8, 8, 64, [1] * 40, [3000 - 70 * i for i in range(40)]),             # many units, ragged, some without a key
+    (16, 4, 128, [1, 3, 0, 2], [9000, 17, 40, 2500]),                     # units over one share, several in one
+    (4, 1, 64, [1] * 300, [(37 * i) % 400 for i in range(300)]),          # more sequences than threads look for a share
+    (6, 2, 256, [1, 2], [5000, 700]), (5, 1, 96, [1, 1], [6000, 1500]), (24, 2, 64, [4], [70000]),
+])
+def test_shares(libqknorm, copies, hq, hk, hd, new, kv):
+    """Units cut wherever equal shares end, in every way that they can be."""
+    Batch(new, kv, hq, hk, hd, seed=len(kv), pad_cols=3).check(max_kv=max(kv) + 5000)
 
 
 def test_bounds_smaller_than_the_batch(libqknorm):
@@ -288,7 +306,7 @@ def test_bounds_smaller_than_the_batch(libqknorm):
     assert (out[3] == 7.0).all() and not (out[2] == 7.0).all()
 
 
-def test_bad_pages_read_as_zeros(libqknorm):
+def test_bad_pages_read_as_zeros(libqknorm, copies):
     b = Batch([1, 2], [100, 70], 8, 2, 128, seed=5)
     for row, j, e in ((0, 1, -1), (0, 3, 2 ** 31 - 1), (1, 2, b.pages)):
         b.table[row][j] = e
@@ -302,7 +320,7 @@ def test_bad_pages_read_as_zeros(libqknorm):
 
 
 @pytest.mark.parametrize("hd", [64, 128, 256])
-def test_values_not_seen_do_not_matter(libqknorm, hd):
+def test_values_not_seen_do_not_matter(libqknorm, copies, hd):
     """NaN in K and V blocks that only some rows of a tile see: those rows have it, the others are as they were."""
     b = Batch([6], [200], 2, 1, hd, seed=6)
     page, token = b.table[0][197 // 16], 197 % 16                # seen by rows 3, 4, 5
@@ -330,7 +348,7 @@ def test_extreme_queries_and_scales(libqknorm):
     b.check(scale=1e-38)
 
 
-def test_small_weights_are_kept(libqknorm):
+def test_small_weights_are_kept(libqknorm, copies):
     """One key far above the rest: 30000 others share 2^-20 of its weight each."""
     b = Batch([1], [30000], 1, 1, 64, seed=8)
     b.k[:], b.ks.view(torch.uint8)[:] = 0, 0x38
@@ -360,7 +378,7 @@ def test_strided_rows_and_other_streams(libqknorm):
 
 
 @pytest.mark.parametrize("new,kv", [([1, 1], [700, 900]), ([70, 2], [700, 300])])
-def test_capture_and_replay(libqknorm, new, kv):
+def test_capture_and_replay(libqknorm, copies, new, kv):
     b = Batch(new, kv, 8, 2, 128, seed=10)
     want, _ = b.call()
     out = torch.zeros_like(b.dq)
