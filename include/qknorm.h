@@ -298,7 +298,7 @@ int qknorm_device_error_word(int* out);
 
 /* Name of the kernel variant the last successful call on this thread launched
  * ("warp", "tile", "ring", "rows", "wide", "general", "head", "head_general", "two_pass", "tp",
- * "rope", "rope_general", "append", "append_general", "attn_tc", "attn_general", "none"); static storage.  For tests and benchmarks. */
+ * "rope", "rope_general", "append", "append_general", "attn_tc", "attn_general", "attn_e2m1", "pages", "none"); static storage.  For tests and benchmarks. */
 const char* qknorm_last_variant(void);
 
 /* Number of kernel launches this thread has enqueued through the library. */

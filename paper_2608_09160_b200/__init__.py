@@ -4,4 +4,4 @@ The CUDA library is loaded on first use (see ``binding``); importing this
 package never touches it, so the seeded input generators in ``workloads`` can
 be used on a machine without the built library.
 """
-__all__ = ["workloads", "binding", "build", "attn", "tp"]
+__all__ = ["workloads", "binding", "build", "attn", "pages", "tp"]

@@ -54,6 +54,7 @@ def _units() -> List[Tuple[str, str, List[str]]]:
                           [f"-DQKNORM_L={l}", f"-DQKNORM_IO={io}", f"-DQKNORM_IO_TAG={tag}"]))
     units.append(("qknorm_tp.o", os.path.join(CSRC, "qknorm_tp_inst.cu"), []))
     units.append(("qknorm_rope.o", os.path.join(CSRC, "qknorm_rope_inst.cu"), []))
+    units.append(("qknorm_pages.o", os.path.join(CSRC, "qknorm_pages_inst.cu"), []))
     units.append(("qknorm_attn.o", os.path.join(CSRC, "qknorm_attn_inst.cu"), []))
     for dp in PADDED_HEAD_DIMS:
         for f8, tag in (("false", "bf16"), ("true", "e4m3")):

@@ -10,11 +10,13 @@
 
 #include "../../include/qknorm.h"
 #include "../../include/qknorm_attn.h"
+#include "../../include/qknorm_pages.h"
 #include "qknorm_attn.cuh"
 #include "qknorm_attn_e2m1.cuh"
 #include "qknorm_baselines.cuh"
 #include "qknorm_general.cuh"
 #include "qknorm_head.cuh"
+#include "qknorm_pages.cuh"
 #include "qknorm_params.h"
 #include "qknorm_ring.cuh"
 #include "qknorm_rope.cuh"
@@ -988,11 +990,13 @@ int static_scratch_address(float** out) {
 }
 
 #include "qknorm_attn_host.cuh"  // run_rope, run_append, run_attn
+#include "qknorm_pages_host.cuh"  // run_pages_*
 
 }  // namespace
 }  // namespace qknorm
 
 #include "qknorm_attn_abi.cuh"  // rotary positions, cache write, attention (include/qknorm_attn.h)
+#include "qknorm_pages_abi.cuh"  // the pages of a cache (include/qknorm_pages.h)
 #include "qknorm_tp_abi.cuh"    // the tensor-parallel entry points (include/qknorm_tp.h)
 
 extern "C" {

@@ -1,0 +1,50 @@
+// Pages of a paged cache: copying, forking, freeing, compacting (include/qknorm_pages.h).
+//
+// The bookkeeping is a few thousand integers and bound by latency: which page is free, and which moves where, are prefix sums over
+// refs, done by one CTA (fork: it stops as soon as it has found the pages it needs) or by one cluster of eight that exchanges its counts
+// through distributed shared memory (compact: it has to see all of refs).  The k-th fork takes the k-th free page whichever thread finds it,
+// so that nothing depends on the order of atomics; those that remain only add to refs.
+// A second launch moves the data, bound by HBM (each byte read once, written once), and brings the tables up to date beside it.
+#pragma once
+#include <stdint.h>
+
+namespace qknorm {
+
+constexpr int kPagePools = 48;  // pools of a launch: what its parameters hold
+constexpr int kPageThreads = 256, kPlanThreads = 1024, kPlanCluster = 8;
+constexpr int kPageChunk = 16384;  // bytes that a CTA copies at a time: four vectors of 16 bytes a thread
+constexpr int kPlanAhead = 8;      // refs that a thread looks at together
+
+struct PagePool {
+  char* base;
+  long long page, stride0, stride1, bytes;
+  long long pieces;  // count[0] * count[1]
+  int count1;
+  int unit;          // 16, 4 or 1: what divides everything
+};
+
+struct PageParams {
+  PagePool pool[kPagePools];
+  int pools;
+  long long num_pages;
+  int* refs;
+  int* table;
+  int cols;
+  long long ld;
+  int* lens;
+  int rows, page_size;
+  const int *from, *to;  // pairs of pages
+  const int *parents, *children;  // fork; free: the rows are children
+  int n;                 // of pairs, forks or rows
+  const int* n_device;   // compact: how many pairs there are
+  int* ok;               // fork
+  int* live;             // compact
+  int *claim, *free_page, *src, *dst, *len, *map, *count;  // workspace
+  int books;             // the launch keeps the tables, too: 1 fork, 2 compact
+};
+
+typedef void (*PageKernel)(const PageParams);
+enum { kPagesForkPlan, kPagesCompactPlan, kPagesFree, kPagesMove };
+PageKernel pages_kernel_for(int which);  // in qknorm_pages_inst.cu
+
+}  // namespace qknorm
