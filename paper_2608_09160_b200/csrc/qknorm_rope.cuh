@@ -158,24 +158,35 @@ __device__ __forceinline__ float absmax8(const float2 (&v)[4]) {
   for (int e = 1; e < 4; ++e) m = max_nan(m, max_nan(fabsf(v[e].x), fabsf(v[e].y)));
   return m;
 }
-// The E4M3 scale of a block whose largest magnitude is amax, as its byte, and its value.
-__device__ __forceinline__ float e2m1_scale(float amax, uint32_t& byte) {
-  byte = e4m3_pack2(__fdiv_rn(amax, 6.0f), 0.f) & 0xffu;
+// x / d correctly rounded, r = 1/d to half a step: a product and one correction by its remainder (Markstein).  Ties between two codes
+// are common (bf16 values over a scale of four bits), and an ulp would decide them wrongly.
+__device__ __forceinline__ float2 quotient(float2 x, float d, float r) {
+  const float2 rr = make_float2(r, r), q = __fmul2_rn(x, rr);
+  return __ffma2_rn(__ffma2_rn(q, make_float2(-d, -d), x), rr, q);
+}
+// The E4M3 scale of a block whose largest magnitude is amax, as its byte; its value f and 1/f (0 for f = 0).
+__device__ __forceinline__ float e2m1_scale(float amax, uint32_t& byte, float& r) {
+  float most;
+  asm("min.NaN.f32 %0, %1, 0f7E967699;" : "=f"(most) : "f"(amax));  // 1e38: an infinity has no remainder
+  byte = e4m3_pack2(quotient(make_float2(most, most), 6.0f, 1.0f / 6.0f).x, 0.f) & 0xffu;
   uint32_t f01, f23;
   e4m3x4_to_f16x2(byte, f01, f23);
-  return __half2float(__ushort_as_half((unsigned short)(f01 & 0xffffu)));
+  const float f = __half2float(__ushort_as_half((unsigned short)(f01 & 0xffffu)));
+  // a scale has four significant bits, its reciprocal is found by one of Newton's steps from an estimate
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(f));
+  r = fmaf(r, fmaf(-f, r, 1.0f), r);
+  if (!(f > 0.f)) r = 0.f;
+  return f;
 }
-// Codes of eight elements of a block with that scale f, r = 1/f (0 for f = 0).  A tie between two codes is common (bf16 values over a
-// scale of four bits), so the quotient is the correctly rounded one: a product with r and one correction by its remainder (Markstein).
-// Magnitudes beyond 1e30, whose remainder may overflow, are far beyond +-6.
-__device__ __forceinline__ uint32_t e2m1_codes8(const float2 (&v)[4], float f, float r) {
-  const float2 rr = make_float2(r, r), ff = make_float2(-f, -f);
+// Codes of eight elements of a block with that scale.
+__device__ __forceinline__ uint32_t e2m1_codes8(const float2 (&v)[4], float amax, float f, float r) {
   float2 y[4];
+  if (amax < 1e30f) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 x = make_float2(fminf(fmaxf(v[e].x, -1e30f), 1e30f), fminf(fmaxf(v[e].y, -1e30f), 1e30f));
-    const float2 q = __fmul2_rn(x, rr);
-    y[e] = __ffma2_rn(__ffma2_rn(q, ff, x), rr, q);
+    for (int e = 0; e < 4; ++e) y[e] = quotient(v[e], f, r);
+  } else {  // far beyond +-6 times the largest scale, where a remainder may overflow
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = make_float2(v[e].x * r, v[e].y * r);
   }
   return e2m1_pack8(y);
 }
@@ -370,11 +381,14 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
           ma = mb = max_nan(ma, mb);
         }
         uint32_t sa, sb;
-        const float fa = e2m1_scale(ma, sa), fb = e2m1_scale(mb, sb);
-        const float ra = fa > 0.f ? __frcp_rn(fa) : 0.f, rb = fb > 0.f ? __frcp_rn(fb) : 0.f;
+        float ra, rb;
+        const float fa = e2m1_scale(ma, sa, ra);
+        float fb = fa;
+        rb = ra, sb = sa;
+        if (split) fb = e2m1_scale(mb, sb, rb);
         char* codes = reinterpret_cast<char*>(C.base) + (side[i] == 1 ? slot_k : slot_v) + head[i] * C.head + (c0 >> 1);
-        __stcs(reinterpret_cast<uint32_t*>(codes), e2m1_codes8(a, fa, ra));
-        __stcs(reinterpret_cast<uint32_t*>(codes + (step >> 1)), e2m1_codes8(b, fb, rb));
+        __stcs(reinterpret_cast<uint32_t*>(codes), e2m1_codes8(a, ma, fa, ra));
+        __stcs(reinterpret_cast<uint32_t*>(codes + (step >> 1)), e2m1_codes8(b, mb, fb, rb));
         unsigned char* sc = reinterpret_cast<unsigned char*>(S.base) + (side[i] == 1 ? slot_ks : slot_vs) + head[i] * S.head;
         if (!split || !(j & 1)) sc[c0 >> 4] = (unsigned char)sa;
         else sc[(c0 + step) >> 4] = (unsigned char)sb;
@@ -516,9 +530,10 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
                 hi[e] = make_float2(whole[warp][16 * blk + 8 + 2 * e], whole[warp][16 * blk + 9 + 2 * e]);
               }
               uint32_t byte;
-              const float f = e2m1_scale(max_nan(absmax8(lo), absmax8(hi)), byte), r1 = f > 0.f ? __frcp_rn(f) : 0.f;
+              float r1;
+              const float most = max_nan(absmax8(lo), absmax8(hi)), f = e2m1_scale(most, byte, r1);
               *reinterpret_cast<uint2*>(reinterpret_cast<char*>(C.base) + y0 + 8 * blk) =
-                  make_uint2(e2m1_codes8(lo, f, r1), e2m1_codes8(hi, f, r1));
+                  make_uint2(e2m1_codes8(lo, most, f, r1), e2m1_codes8(hi, most, f, r1));
               sc[blk] = (unsigned char)byte;
             }
             __syncwarp();
