@@ -229,9 +229,9 @@ typedef struct {
 /*
  * qknorm_fwd_append_e2m1 -- qknorm_fwd_append into a 4-bit cache; rot may be NULL.
  * With y = x / k_scale (as a product with the fp32 reciprocal, which has to be finite) a block's scale is
- * f = max |y| / 6 rounded to E4M3, nearest even, saturating at 448; a code is y / f (the correctly rounded quotient) rounded to
+ * f = max |y| / 6 (the correctly rounded quotient) rounded to E4M3, nearest even, saturating at 448; a code is y / f (the correctly rounded quotient) rounded to
  * E2M1, nearest even, saturating at +-6.  f = 0 (a block of zeros, or too small for E4M3) gives codes of zero.  A block with a NaN gets
- * the scale NaN and reads back as NaN; infinities saturate.
+ * the scale NaN and reads back as NaN; infinities saturate.  Two tokens of a call that name the same slot leave codes and scales of either.
  */
 int qknorm_fwd_append_e2m1(const void* q, const void* k, const void* v, const void* gamma_q, const void* gamma_k,
                            int32_t norm, float eps, const qknorm_rotation_axes* rot, const int64_t* slots,
@@ -244,8 +244,10 @@ int qknorm_fwd_append_e2m1(const void* q, const void* k, const void* v, const vo
  * below 2^-30 of the row's largest element); K and V widen exactly; scores, maxima, sums and the output are fp32; the
  * weights are rounded to fp16 (2^-11 relative, at least 2^-32 of the row's largest weight).
  *
- * Kernels: "attn_e2m1" (mma.sync out of registers) for few rows per sequence and key head; for many the visible part of
- * the cache is widened once into the workspace, to bf16 and exactly, and "attn_tc" reads that (weights rounded to bf16 then, 2^-8).
+ * Kernels: "attn_e2m1" (mma.sync out of registers) for up to 96 rows (new tokens times query heads) per sequence and key head; for more the
+ * visible part of the cache is widened once into the workspace, to bf16 and exactly, and "attn_tc" reads that (weights rounded to bf16
+ * then, 2^-8) -- where head_dim is at most 128 and the widened cache, 4 bytes an element of max_kv keys of every sequence, at most 2 GB.  A wait
+ * inside "attn_e2m1" that runs out after a second sets the device's error word to 10.
  */
 int qknorm_attn_paged_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* cache, const int32_t* block_table,
                            int32_t table_cols, int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts,

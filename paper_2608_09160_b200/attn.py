@@ -236,28 +236,28 @@ def _cache(k_cache, v_cache, k_scale: float, v_scale: float, dev: int):
                     f"shape on cuda:{dev}, with unit stride in head_dim")
 
 
-_CODES = (torch.uint8, torch.float4_e2m1fn_x2)
-_SCALES = (torch.float8_e4m3fn, torch.uint8)
+_U8, _F4 = torch.uint8, torch.float4_e2m1fn_x2
 
 
 def _cache_e2m1(k_cache, v_cache, k_scales, v_scales, k_scale: float, v_scale: float, dev: int):
     """k_cache, v_cache [pages, page_size, heads, head_dim/2] bytes, k_scales, v_scales [pages, page_size, heads, head_dim/16], any
     strides over pages, tokens and heads: (struct, heads, head_dim)."""
-    four = (k_cache, v_cache, k_scales, v_scales)
-    if all(isinstance(t, torch.Tensor) for t in four):
-        shape, sshape = k_cache.shape, k_scales.shape
-        if (k_cache.dtype in _CODES and v_cache.dtype is k_cache.dtype and k_scales.dtype in _SCALES and v_scales.dtype is k_scales.dtype
-                and len(shape) == 4 and v_cache.shape == shape and len(sshape) == 4 and v_scales.shape == sshape
-                and shape[:3] == sshape[:3] and shape[3] == 8 * sshape[3] and shape[3] > 0
-                and k_cache.get_device() == dev and v_cache.get_device() == dev and k_scales.get_device() == dev and v_scales.get_device() == dev):
+    try:
+        shape, sshape, dtype, sdtype = k_cache.shape, k_scales.shape, k_cache.dtype, k_scales.dtype
+        if ((dtype is _U8 or dtype is _F4) and v_cache.dtype is dtype and (sdtype is _F8 or sdtype is _U8) and v_scales.dtype is sdtype
+                and v_cache.shape == shape and v_scales.shape == sshape
+                and k_cache.get_device() == v_cache.get_device() == k_scales.get_device() == v_scales.get_device() == dev):
+            pages, page, heads, half = shape
             kp, kt, kh, k1 = k_cache.stride()
             vp, vt, vh, v1 = v_cache.stride()
             ap, at, ah, a1 = k_scales.stride()
             bp, bt, bh, b1 = v_scales.stride()
-            if k1 == 1 and v1 == 1 and ((a1 == 1 and b1 == 1) or sshape[3] == 1):
-                pages, page, heads, half = shape
+            if (half > 0 and half % 8 == 0 and sshape == (pages, page, heads, half // 8) and k1 == 1 and v1 == 1
+                    and ((a1 == 1 and b1 == 1) or half == 8)):
                 return _CACHE_E2M1.pack(k_cache.data_ptr(), v_cache.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), kp, kt, kh, vp, vt, vh,
                                         ap, at, ah, bp, bt, bh, pages, page, heads, 2 * half, k_scale, v_scale), heads, 2 * half
+    except (AttributeError, ValueError):  # no tensor, or not four axes
+        pass
     _refuse(_SHAPE, "k_cache, v_cache, k_scales, v_scales: expected two uint8 or float4_e2m1fn_x2 tensors [pages, page_size, heads, head_dim/2] of "
                     "one type and shape and two float8_e4m3fn or uint8 tensors [pages, page_size, heads, head_dim/16], head_dim a multiple of 16, "
                     f"on cuda:{dev}, with unit stride in the last axis")

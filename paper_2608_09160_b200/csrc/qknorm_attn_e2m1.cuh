@@ -708,200 +708,199 @@ __global__ void __launch_bounds__(E2m1Cta<DP, NT, COPY>::kThreads, E2m1Cta<DP, N
   }
 
   for (;;) {
-  uint2* const qs = reinterpret_cast<uint2*>(smem + h * C::kQHead);
-  core.start(P, w.s, w.hg * HP + h, (unsigned)w.rt * (8 * NT), w.u.rows, qs, slice == 0);
-  if constexpr (C::kQShared) __syncthreads();
-  // keys that every row sees
-  const int all_lo = attn_lo(A, w.s, w.u.tok1), all_hi = attn_hi(A, w.s, w.u.tok0), k1 = w.u.uhi;
-  // the tile's place in a stage, in tokens of a head
-  const int tile_at = kTma ? ((slice * kE2m1Tile >> P.run_shift) * HP + h) << P.run_shift : 0;
-  const int jump = kTma && P.run_shift == 4 ? 16 * HP : 16;
+    uint2* const qs = reinterpret_cast<uint2*>(smem + h * C::kQHead);
+    core.start(P, w.s, w.hg * HP + h, (unsigned)w.rt * (8 * NT), w.u.rows, qs, slice == 0);
+    if constexpr (C::kQShared) __syncthreads();
+    // keys that every row sees
+    const int all_lo = attn_lo(A, w.s, w.u.tok1), all_hi = attn_hi(A, w.s, w.u.tok0), k1 = w.u.uhi;
+    // the tile's place in a stage, in tokens of a head
+    const int tile_at = kTma ? ((slice * kE2m1Tile >> P.run_shift) * HP + h) << P.run_shift : 0;
+    const int jump = kTma && P.run_shift == 4 ? 16 * HP : 16;
 
-  while (w.u.uhi > w.u.ulo) {
-    const int end = seg_end;
-    for (int it = seg; it < end; ++it) {
-      if constexpr (kTma) {
-        if (__any_sync(0xffffffffu, !ptx::mbar_wait_bounded(bar32 + 8 * stage, parity))) {
-          // never seen: the rows come out wrong and the error word says so; what is still on its way gets the same time again
-          if (lane == 0) *A.error = kE2m1Error;
-          for (int i = 0; i < C::kStages; ++i)
-            if (it + i < end) ptx::mbar_wait_bounded(bar32 + 8 * ((stage + i) % C::kStages), parity ^ (stage + i >= C::kStages ? 1u : 0u));
-          failed = true;
-          break;
-        }
-      } else {
-        asm volatile("cp.async.wait_group %0;" ::"n"(C::kStages - 2) : "memory");
-        __syncwarp();  // every lane's copies have landed, and nobody reads the stage that is filled next
-        int next = stage + C::kStages - 1;
-        if (next >= C::kStages) next -= C::kStages;
-        issue(it + C::kStages - 1, next);
-        look(it + C::kStages);
-      }
-      char* const st = ring + stage * C::kBytes;
-      const int key0 = w.u.from + it * round + slice * kE2m1Tile;
-      if (key0 < k1)
-        core.tile(st + tile_at * C::kKPitch, st + C::kV + tile_at * C::kVPitch, st + C::kKs + tile_at * C::kSPitch, st + C::kVs + tile_at * C::kSPitch,
-                  jump, key0, key0 >= all_lo && key0 + kE2m1Tile <= all_hi, qs);
-      if constexpr (kTma) {  // the last warp that has read a stage fills it again: nobody waits for the others
-        __syncwarp();
-        if (it + C::kStages < end) {
-          unsigned before = 0;
-          if (lane == 0)
-            asm volatile("atom.acq_rel.cta.shared::cta.inc.u32 %0, [%1], %2;" : "=r"(before) : "r"(done32 + 4 * stage), "r"(kWarps - 1) : "memory");
-          if (__shfl_sync(0xffffffffu, before, 0) == kWarps - 1) fill(it + C::kStages, stage);
-        }
-      }
-      if (++stage == C::kStages) {
-        stage = 0;
-        parity ^= 1;
-      }
-    }
-    if constexpr (kTma) {
-      if (__syncthreads_or(failed)) return;  // everybody has seen the stretch's copies land, or has given up on them
-    }
-    if (end == w.r1) break;
-    prime(end);
-  }
-  if constexpr (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
-
-
-  // ---- the next unit; where a warp has its head to itself, its first copies come while the results of this one leave
-  const E2m1Item now = w;
-  const int now_slot = first_item ? 0 : 1;
-  left -= w.r1 - w.r0;
-  if (left > 0) {
-    first_item = false;
-    w.r0 = 0;
-    do {
-      if (++w.hg == groups) {
-        w.hg = 0;
-        if (++w.rt == P.row_tiles) {
-          w.rt = 0;
-          if (++w.b == A.seqs) return;  // never: the shares add up to the units
-          w.s = attn_seq(A, w.b);
-        }
-        w.u = e2m1_span(P, w.s, w.rt, round);
-      }
-    } while (w.u.rounds == 0);
-    w.r1 = left < w.u.rounds ? (int)left : w.u.rounds;
-    if (kTma && slices == 1) prime(0);
-  }
-  const AttnSeq& s = now.s;
-  const E2m1Span& u = now.u;
-  const unsigned first = (unsigned)now.rt * (8 * NT);
-  const bool whole = now.r0 == 0 && now.r1 == u.rounds;
-  if (slices == 1) {  // ---- a warp has its head to itself: straight from its registers
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float sum = k ? core.l[nt].y : core.l[nt].x;
-        sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 16);
-        const float top = k ? core.m[nt].y : core.m[nt].x, c = k ? core.cl[nt].y : core.cl[nt].x;
-        const unsigned r = nt * 8 + 2 * t + k, rr = first + r;
-        if (rr >= u.rows) continue;
-        const float z = sum == 0.f ? kNegInf : fmaf(top == kNegInf ? 0.f : top, c, log2f(sum)) - kE2m1Lift, inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int i = (int)(rr / group), head = (now.hg * HP + h) * A.group + (int)(rr - i * group);
-        const long long row = s.row0 + (long long)i;
-        const long long part = ((long long)blockIdx.x * 2 + now_slot) * (HP * 8 * NT) + h * 8 * NT + r;
-        if (whole) {
-          const float scale = inv * A.v_scale;
-          uint16_t* out = A.out + row * A.ld_out + (long long)head * A.head_dim + g * Core::PG;
-#pragma unroll
-          for (int j = 0; j < Core::KS; j += 4) {
-            uint32_t v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = bf_pack(core.o[j + e][nt][k] * scale, core.o[j + e][nt][2 + k] * scale);
-            if (P.out_vec) {
-              *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(v[0], v[1], v[2], v[3]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) out[2 * j + e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
-            }
+    while (w.u.uhi > w.u.ulo) {
+      const int end = seg_end;
+      for (int it = seg; it < end; ++it) {
+        if constexpr (kTma) {
+          if (__any_sync(0xffffffffu, !ptx::mbar_wait_bounded(bar32 + 8 * stage, parity))) {
+            // never seen: the rows come out wrong and the error word says so; what is still on its way gets the same time again
+            if (lane == 0) *A.error = kE2m1Error;
+            for (int i = 0; i < C::kStages; ++i)
+              if (it + i < end) ptx::mbar_wait_bounded(bar32 + 8 * ((stage + i) % C::kStages), parity ^ (stage + i >= C::kStages ? 1u : 0u));
+            failed = true;
+            break;
           }
         } else {
-          float* po = P.part_o + part * A.head_dim + g * Core::PG;
-#pragma unroll
-          for (int j = 0; j < Core::KS; j += 2)
-            *reinterpret_cast<float4*>(po + 2 * j) = make_float4(core.o[j][nt][k] * inv, core.o[j][nt][2 + k] * inv, core.o[j + 1][nt][k] * inv,
-                                                                 core.o[j + 1][nt][2 + k] * inv);
+          asm volatile("cp.async.wait_group %0;" ::"n"(C::kStages - 2) : "memory");
+          __syncwarp();  // every lane's copies have landed, and nobody reads the stage that is filled next
+          int next = stage + C::kStages - 1;
+          if (next >= C::kStages) next -= C::kStages;
+          issue(it + C::kStages - 1, next);
+          look(it + C::kStages);
         }
-        if (g == 0) {
+        char* const st = ring + stage * C::kBytes;
+        const int key0 = w.u.from + it * round + slice * kE2m1Tile;
+        if (key0 < k1)
+          core.tile(st + tile_at * C::kKPitch, st + C::kV + tile_at * C::kVPitch, st + C::kKs + tile_at * C::kSPitch, st + C::kVs + tile_at * C::kSPitch,
+                    jump, key0, key0 >= all_lo && key0 + kE2m1Tile <= all_hi, qs);
+        if constexpr (kTma) {  // the last warp that has read a stage fills it again: nobody waits for the others
+          __syncwarp();
+          if (it + C::kStages < end) {
+            unsigned before = 0;
+            if (lane == 0)
+              asm volatile("atom.acq_rel.cta.shared::cta.inc.u32 %0, [%1], %2;" : "=r"(before) : "r"(done32 + 4 * stage), "r"(kWarps - 1) : "memory");
+            if (__shfl_sync(0xffffffffu, before, 0) == kWarps - 1) fill(it + C::kStages, stage);
+          }
+        }
+        if (++stage == C::kStages) {
+          stage = 0;
+          parity ^= 1;
+        }
+      }
+      if constexpr (kTma) {
+        if (__syncthreads_or(failed)) return;  // everybody has seen the stretch's copies land, or has given up on them
+      }
+      if (end == w.r1) break;
+      prime(end);
+    }
+    if constexpr (!kTma) asm volatile("cp.async.wait_all;" ::: "memory");
+
+    // ---- the next unit; where a warp has its head to itself, its first copies come while the results of this one leave
+    const E2m1Item now = w;
+    const int now_slot = first_item ? 0 : 1;
+    left -= w.r1 - w.r0;
+    if (left > 0) {
+      first_item = false;
+      w.r0 = 0;
+      do {
+        if (++w.hg == groups) {
+          w.hg = 0;
+          if (++w.rt == P.row_tiles) {
+            w.rt = 0;
+            if (++w.b == A.seqs) return;  // never: the shares add up to the units
+            w.s = attn_seq(A, w.b);
+          }
+          w.u = e2m1_span(P, w.s, w.rt, round);
+        }
+      } while (w.u.rounds == 0);
+      w.r1 = left < w.u.rounds ? (int)left : w.u.rounds;
+      if (kTma && slices == 1) prime(0);
+    }
+    const AttnSeq& s = now.s;
+    const E2m1Span& u = now.u;
+    const unsigned first = (unsigned)now.rt * (8 * NT);
+    const bool whole = now.r0 == 0 && now.r1 == u.rounds;
+    if (slices == 1) {  // ---- a warp has its head to itself: straight from its registers
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float sum = k ? core.l[nt].y : core.l[nt].x;
+          sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+          const float top = k ? core.m[nt].y : core.m[nt].x, c = k ? core.cl[nt].y : core.cl[nt].x;
+          const unsigned r = nt * 8 + 2 * t + k, rr = first + r;
+          if (rr >= u.rows) continue;
+          const float z = sum == 0.f ? kNegInf : fmaf(top == kNegInf ? 0.f : top, c, log2f(sum)) - kE2m1Lift, inv = sum == 0.f ? 0.f : 1.f / sum;
+          const int i = (int)(rr / group), head = (now.hg * HP + h) * A.group + (int)(rr - i * group);
+          const long long row = s.row0 + (long long)i;
+          const long long part = ((long long)blockIdx.x * 2 + now_slot) * (HP * 8 * NT) + h * 8 * NT + r;
+          if (whole) {
+            const float scale = inv * A.v_scale;
+            uint16_t* out = A.out + row * A.ld_out + (long long)head * A.head_dim + g * Core::PG;
+#pragma unroll
+            for (int j = 0; j < Core::KS; j += 4) {
+              uint32_t v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = bf_pack(core.o[j + e][nt][k] * scale, core.o[j + e][nt][2 + k] * scale);
+              if (P.out_vec) {
+                *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(v[0], v[1], v[2], v[3]);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) out[2 * j + e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+              }
+            }
+          } else {
+            float* po = P.part_o + part * A.head_dim + g * Core::PG;
+#pragma unroll
+            for (int j = 0; j < Core::KS; j += 2)
+              *reinterpret_cast<float4*>(po + 2 * j) = make_float4(core.o[j][nt][k] * inv, core.o[j][nt][2 + k] * inv, core.o[j + 1][nt][k] * inv,
+                                                                   core.o[j + 1][nt][2 + k] * inv);
+          }
+          if (g == 0) {
+            if (!whole) P.part_z[part] = z;
+            else if (A.lse != nullptr) A.lse[row * A.heads_q + head] = z * kLn2;
+          }
+        }
+    } else {  // ---- the parts of the warps of a head
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float v = k ? core.l[nt].y : core.l[nt].x;
+          v += __shfl_xor_sync(0xffffffffu, v, 4);
+          v += __shfl_xor_sync(0xffffffffu, v, 8);
+          v += __shfl_xor_sync(0xffffffffu, v, 16);
+          if (g == 0) {
+            row_m[warp][nt * 8 + 2 * t + k] = k ? core.m[nt].y : core.m[nt].x;
+            row_c[warp][nt * 8 + 2 * t + k] = k ? core.cl[nt].y : core.cl[nt].x;
+            row_l[warp][nt * 8 + 2 * t + k] = v;
+          }
+        }
+      __syncthreads();  // nobody reads tiles any more
+      float* const all = reinterpret_cast<float*>(smem + C::kQBytes);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float* at = all + ((warp * NT + nt) * 8 + 2 * t + k) * C::kOPitch + g * Core::PG;
+#pragma unroll
+          for (int j = 0; j < Core::KS; ++j) *reinterpret_cast<float2*>(at + 2 * j) = make_float2(core.o[j][nt][k], core.o[j][nt][2 + k]);
+        }
+      __syncthreads();
+      for (int item = warp; item < HP * 8 * NT; item += kWarps) {
+        const int r = item / HP, w0 = item % HP;  // the head's warps: w0, w0 + HP, ...
+        const unsigned rr = first + r;
+        if (rr >= u.rows) break;
+        float top = row_m[w0][r];
+        for (int w = w0 + HP; w < kWarps; w += HP) top = fmaxf(top, row_m[w][r]);
+        const float against = top == kNegInf ? 0.f : top, c = row_c[w0][r];
+        float sum = 0.f;
+        for (int w = w0; w < kWarps; w += HP) sum = fmaf(row_l[w][r], ex2((row_m[w][r] - against) * c), sum);
+        const float z = sum == 0.f ? kNegInf : fmaf(against, c, log2f(sum)) - kE2m1Lift, inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int i = (int)(rr / group), head = (now.hg * HP + w0) * A.group + (int)(rr - i * group);
+        const long long row = s.row0 + (long long)i;
+        const long long part = ((long long)blockIdx.x * 2 + now_slot) * (HP * 8 * NT) + w0 * 8 * NT + r;
+        for (int d = 2 * lane; d < A.head_dim; d += 64) {
+          float2 v = make_float2(0.f, 0.f);
+          for (int w = w0; w < kWarps; w += HP) {
+            const float2 a = *reinterpret_cast<const float2*>(all + (w * 8 * NT + r) * C::kOPitch + d);
+            const float share = ex2((row_m[w][r] - against) * c);
+            v.x = fmaf(a.x, share, v.x);
+            v.y = fmaf(a.y, share, v.y);
+          }
+          v.x *= inv;
+          v.y *= inv;
+          if (whole) {
+            uint16_t* out = A.out + row * A.ld_out + (long long)head * A.head_dim + d;
+            IoBf16::store(out, 0, v.x * A.v_scale);
+            IoBf16::store(out, 1, v.y * A.v_scale);
+          } else {
+            *reinterpret_cast<float2*>(P.part_o + part * A.head_dim + d) = v;
+          }
+        }
+        if (lane == 0) {
           if (!whole) P.part_z[part] = z;
           else if (A.lse != nullptr) A.lse[row * A.heads_q + head] = z * kLn2;
         }
       }
-  } else {  // ---- the parts of the warps of a head
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float v = k ? core.l[nt].y : core.l[nt].x;
-      v += __shfl_xor_sync(0xffffffffu, v, 4);
-      v += __shfl_xor_sync(0xffffffffu, v, 8);
-      v += __shfl_xor_sync(0xffffffffu, v, 16);
-      if (g == 0) {
-        row_m[warp][nt * 8 + 2 * t + k] = k ? core.m[nt].y : core.m[nt].x;
-        row_c[warp][nt * 8 + 2 * t + k] = k ? core.cl[nt].y : core.cl[nt].x;
-        row_l[warp][nt * 8 + 2 * t + k] = v;
-      }
     }
-  __syncthreads();  // nobody reads tiles any more
-  float* const all = reinterpret_cast<float*>(smem + C::kQBytes);
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      float* at = all + ((warp * NT + nt) * 8 + 2 * t + k) * C::kOPitch + g * Core::PG;
-#pragma unroll
-      for (int j = 0; j < Core::KS; ++j) *reinterpret_cast<float2*>(at + 2 * j) = make_float2(core.o[j][nt][k], core.o[j][nt][2 + k]);
+    if (left <= 0) break;
+    if (!kTma || slices != 1) {
+      if constexpr (kTma) ptx::fence_proxy_async();  // copies go where the parts were
+      __syncthreads();
+      prime(0);
     }
-  __syncthreads();
-  for (int item = warp; item < HP * 8 * NT; item += kWarps) {
-    const int r = item / HP, w0 = item % HP;  // the head's warps: w0, w0 + HP, ...
-    const unsigned rr = first + r;
-    if (rr >= u.rows) break;
-    float top = row_m[w0][r];
-    for (int w = w0 + HP; w < kWarps; w += HP) top = fmaxf(top, row_m[w][r]);
-    const float against = top == kNegInf ? 0.f : top, c = row_c[w0][r];
-    float sum = 0.f;
-    for (int w = w0; w < kWarps; w += HP) sum = fmaf(row_l[w][r], ex2((row_m[w][r] - against) * c), sum);
-    const float z = sum == 0.f ? kNegInf : fmaf(against, c, log2f(sum)) - kE2m1Lift, inv = sum == 0.f ? 0.f : 1.f / sum;
-    const int i = (int)(rr / group), head = (now.hg * HP + w0) * A.group + (int)(rr - i * group);
-    const long long row = s.row0 + (long long)i;
-    const long long part = ((long long)blockIdx.x * 2 + now_slot) * (HP * 8 * NT) + w0 * 8 * NT + r;
-    for (int d = 2 * lane; d < A.head_dim; d += 64) {
-      float2 v = make_float2(0.f, 0.f);
-      for (int w = w0; w < kWarps; w += HP) {
-        const float2 a = *reinterpret_cast<const float2*>(all + (w * 8 * NT + r) * C::kOPitch + d);
-        const float share = ex2((row_m[w][r] - against) * c);
-        v.x = fmaf(a.x, share, v.x);
-        v.y = fmaf(a.y, share, v.y);
-      }
-      v.x *= inv;
-      v.y *= inv;
-      if (whole) {
-        uint16_t* out = A.out + row * A.ld_out + (long long)head * A.head_dim + d;
-        IoBf16::store(out, 0, v.x * A.v_scale);
-        IoBf16::store(out, 1, v.y * A.v_scale);
-      } else {
-        *reinterpret_cast<float2*>(P.part_o + part * A.head_dim + d) = v;
-      }
-    }
-    if (lane == 0) {
-      if (!whole) P.part_z[part] = z;
-      else if (A.lse != nullptr) A.lse[row * A.heads_q + head] = z * kLn2;
-    }
-  }
-  }
-  if (left <= 0) break;
-  if (!kTma || slices != 1) {
-    if constexpr (kTma) ptx::fence_proxy_async();  // copies go where the parts were
-    __syncthreads();
-    prime(0);
-  }
   }
 }
 

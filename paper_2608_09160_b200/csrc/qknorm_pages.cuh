@@ -23,9 +23,7 @@ struct PagePool {
   int unit;          // 16, 4 or 1: what divides everything
 };
 
-struct PageParams {
-  PagePool pool[kPagePools];
-  int pools;
+struct PageParams {  // the books
   long long num_pages;
   int* refs;
   int* table;
@@ -40,11 +38,18 @@ struct PageParams {
   int* ok;               // fork
   int* live;             // compact
   int *claim, *free_page, *src, *dst, *len, *map, *count;  // workspace
-  int books;             // the launch keeps the tables, too: 1 fork, 2 compact
+  int books;             // the launch that moves pages keeps the tables, too: 1 fork, 2 compact
+};
+struct MoveParams {
+  PageParams P;
+  int pools;
+  PagePool pool[kPagePools];
 };
 
 typedef void (*PageKernel)(const PageParams);
-enum { kPagesForkPlan, kPagesCompactPlan, kPagesFree, kPagesMove };
+typedef void (*MoveKernel)(const MoveParams);
+enum { kPagesForkPlan, kPagesCompactPlan, kPagesFree };
 PageKernel pages_kernel_for(int which);  // in qknorm_pages_inst.cu
+MoveKernel pages_move_kernel_for();
 
 }  // namespace qknorm

@@ -102,16 +102,18 @@ int check_pages_workspace(const PageParams& P, int n, void* ws, int64_t ws_bytes
 }
 
 // Moves the pairs' pages, pairs: their number, or at most; the first launch keeps the books.
-int launch_moves(PageParams& P, const qknorm_page_pool* pools, int num_pools, int64_t pairs, cudaStream_t stream) {
+int launch_moves(const PageParams& P, const qknorm_page_pool* pools, int num_pools, int64_t pairs, cudaStream_t stream) {
   const DeviceInfo* dev = nullptr;
   int rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
+  MoveParams M;
+  M.P = P;
   for (int k0 = 0; k0 == 0 || k0 < num_pools; k0 += kPagePools) {
-    P.pools = num_pools - k0 < kPagePools ? num_pools - k0 : kPagePools;
+    M.pools = num_pools - k0 < kPagePools ? num_pools - k0 : kPagePools;
     int64_t most = 1;  // items of a pool
-    for (int k = 0; k < P.pools; ++k) {
+    for (int k = 0; k < M.pools; ++k) {
       const qknorm_page_pool& p = pools[k0 + k];
-      PagePool& q = P.pool[k];
+      PagePool& q = M.pool[k];
       q.base = (char*)p.base;
       q.page = p.page;
       q.stride0 = p.stride[0];
@@ -126,15 +128,15 @@ int launch_moves(PageParams& P, const qknorm_page_pool* pools, int num_pools, in
       most = items > most ? (items < 0x7fffffff ? (int64_t)items : 0x7fffffff) : most;
     }
     // eight CTAs for every SM, shared between the pools
-    int64_t x = (8 * (int64_t)dev->sm_count + P.pools - 1) / (P.pools > 0 ? P.pools : 1);
-    const int64_t books = P.books == 1 ? P.n : P.books == 2 ? P.rows : 0;
+    int64_t x = (8 * (int64_t)dev->sm_count + M.pools - 1) / (M.pools > 0 ? M.pools : 1);
+    const int64_t books = M.P.books == 1 ? P.n : M.P.books == 2 ? P.rows : 0;
     if (most < books) most = books;
     if (x > most) x = most;
-    const cudaError_t e = launch_overlapped(pages_kernel_for(kPagesMove), dim3((unsigned)x, (unsigned)(P.pools + (P.books ? 1 : 0))),
-                                            (unsigned)kPageThreads, 0, stream, P);
+    const cudaError_t e = launch_overlapped(pages_move_kernel_for(), dim3((unsigned)x, (unsigned)(M.pools + (M.P.books ? 1 : 0))),
+                                            (unsigned)kPageThreads, 0, stream, M);
     if (e != cudaSuccess) return set_cuda_error(e);
     if ((rc = finish_launch("pages")) != QKNORM_OK) return rc;
-    P.books = 0;
+    M.P.books = 0;
   }
   return QKNORM_OK;
 }

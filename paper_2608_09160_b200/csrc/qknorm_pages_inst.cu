@@ -247,11 +247,12 @@ __device__ __forceinline__ void copy_run(char* dst, const char* src, int n) {
 }
 
 // blockIdx.y: a pool, or behind the last one the books.
-__global__ void __launch_bounds__(kPageThreads) pages_move_kernel(const __grid_constant__ PageParams P) {
+__global__ void __launch_bounds__(kPageThreads) pages_move_kernel(const __grid_constant__ MoveParams M) {
+  const PageParams& P = M.P;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int pairs = P.n_device != nullptr ? *P.n_device : P.n;
-  if ((int)blockIdx.y < P.pools) {
-    const PagePool& pool = P.pool[blockIdx.y];
+  if ((int)blockIdx.y < M.pools) {
+    const PagePool& pool = M.pool[blockIdx.y];
     const long long chunks = (pool.bytes + kPageChunk - 1) / kPageChunk, per = pool.pieces * chunks;
     for (long long it = blockIdx.x; it < per * pairs; it += gridDim.x) {
       const int i = (int)(it / per);
@@ -307,9 +308,9 @@ PageKernel pages_kernel_for(int which) {
   switch (which) {
     case kPagesForkPlan: return pages_fork_plan_kernel;
     case kPagesCompactPlan: return pages_compact_plan_kernel;
-    case kPagesFree: return pages_free_kernel;
-    default: return pages_move_kernel;
+    default: return pages_free_kernel;
   }
 }
+MoveKernel pages_move_kernel_for() { return pages_move_kernel; }
 
 }  // namespace qknorm
