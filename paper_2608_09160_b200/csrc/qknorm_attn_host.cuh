@@ -890,6 +890,7 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
   span += kE2m1Tile - 1;  // units start at a multiple of a tile
   if (row_tiles > 0x3fffffff / seqs) return QKNORM_ERR_SHAPE;
   p.row_tiles = (int)row_tiles;
+  const int tma = env_int("QKNORM_E2M1_TMA", -1);  // 0, 1: for tests
   for (int k = 0; k < 2; ++k) {
     if (k == 1 && head_dim != 64 && head_dim != 128) continue;
     const E2m1Launch kernel = e2m1_kernel(head_dim, p.nt, k == 1 ? 0 : 16);
@@ -901,8 +902,8 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
     if (units > 0x7fffffff) return QKNORM_ERR_SHAPE;
     w.shares = rounds > kE2m1Whole;
     w.grid = (int)(!w.shares || units * rounds < places ? (w.shares ? units * rounds : units) : places);
-    if (k == 1) p.tma = w.heads >= 4 && units * rounds >= 8 * places;
-    if (!w.shares) continue;
+    if (k == 1) p.tma = tma < 0 ? w.heads >= 4 && units * rounds >= 8 * places : tma != 0;
+    if (!w.shares || (k == 1 && !p.tma)) continue;
     const int64_t parts = (int64_t)w.grid * 2 * w.heads * 8 * p.nt;
     if (parts > p.parts) p.parts = parts;
     if (w.grid * 32 > p.cut_bytes) p.cut_bytes = w.grid * 32;
@@ -1084,10 +1085,10 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   int copy = f.vec16 ? 16 : 8;
   // TMA: tokens of a head one after the other in codes and scales, everything on 16 bytes, pages of whole runs of 16 tokens; copies go to
   // multiples of 128 bytes.
-  const int heads = plan.way[1].heads, tma = env_int("QKNORM_E2M1_TMA", -1);  // 0, 1: for tests
+  const int heads = plan.way[1].heads;
   E.run_shift = cache->page_size % 32 == 0 ? 5 : 4;
   if ((hd == 64 || hd == 128) && cache->page_size % 16 == 0 && cache->num_pages > 0 && P.k.token == hd / 2 && P.v.token == hd / 2 &&
-      E.ks.token == hd / 16 && E.vs.token == hd / 16 && (heads << E.run_shift) * (hd / 16) % 128 == 0 && (tma < 0 ? plan.tma : tma != 0) &&
+      E.ks.token == hd / 16 && E.vs.token == hd / 16 && (heads << E.run_shift) * (hd / 16) % 128 == 0 && plan.tma &&
       encode_e2m1(&maps.k, *cache, P.k, hd / 2, 8, heads, 1 << E.run_shift) && encode_e2m1(&maps.v, *cache, P.v, hd / 2, 8, heads, 1 << E.run_shift) &&
       encode_e2m1(&maps.ks, *cache, E.ks, hd / 16, 4, heads, 1 << E.run_shift) &&
       encode_e2m1(&maps.vs, *cache, E.vs, hd / 16, 4, heads, 1 << E.run_shift))

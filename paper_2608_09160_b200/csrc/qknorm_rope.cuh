@@ -45,14 +45,10 @@ struct IoE2m1 {
 struct RopeParams {
   RopeSide q, k, v;  // v only with a cache
   CacheSide ck, cv;
-  CacheSide cks, cvs;  // the block scales of a 4-bit cache
   const long long* slots;
   long long num_slots;  // num_pages * page_size
   int page_size, page_shift;  // page_shift: log2(page_size), or -1
   const long long* positions;  // [T], or with several axes [axes][T], ld_pos apart
-  const unsigned char* axis;   // which axis turns a pair; nullptr: the first
-  long long ld_pos;
-  int axes;
   const double* inv_freq;
   float mscale;
   int rot_dim, interleaved;
@@ -63,6 +59,10 @@ struct RopeParams {
   int slots_per_token;  // (q.heads + k.heads + v.heads) << log_lph
   int tokens_per_cta, threads_per_token;
   float eps, inv_hd;
+  const unsigned char* axis;   // which axis turns a pair; nullptr: the first
+  long long ld_pos;
+  int axes;
+  CacheSide cks, cvs;  // the block scales of a 4-bit cache
 };
 
 enum { kNormNone = 0, kNormLayer = 1, kNormHead = 2 };
@@ -267,12 +267,16 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
     }
   }
   if (live && r16 > 0) {
-    const long long pos = R.positions[t];
-    for (int p = tid; p < 8 * r16; p += R.threads_per_token) {
-      const float2 f = rope_cs(R, rope_pos(R, t, p, pos), p);
+    auto put = [&](int p, float2 f) {
       float* at = reinterpret_cast<float*>(cs + ((p & 7) >> 1) * r16 + (p >> 3)) + (p & 1);
       at[0] = f.x;
       at[2] = f.y;
+    };
+    const long long pos = R.positions[t];
+    if (R.axis == nullptr) {
+      for (int p = tid; p < 8 * r16; p += R.threads_per_token) put(p, rope_cs(R, pos, p));
+    } else {
+      for (int p = tid; p < 8 * r16; p += R.threads_per_token) put(p, rope_cs(R, rope_pos(R, t, p, pos), p));
     }
   }
   float rq = 1.f, rk = 1.f;

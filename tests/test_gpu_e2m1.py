@@ -236,6 +236,9 @@ class Batch:
 def copies(request, monkeypatch):
     """Both ways of bringing tiles in, whichever the sizes would choose; a layout that TMA cannot bring takes the other."""
     monkeypatch.setenv("QKNORM_E2M1_TMA", "1" if request.param == "tma" else "0")
+    attn._workspace_e2m1.cache_clear()       # the two need different sizes
+    yield
+    attn._workspace_e2m1.cache_clear()
 
 
 @pytest.mark.parametrize("order", ["hnd", "nhd"])
