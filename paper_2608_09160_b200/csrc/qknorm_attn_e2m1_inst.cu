@@ -84,42 +84,51 @@ __global__ void __launch_bounds__(kE2m1JoinThreads) attn_e2m1_join_kernel(const 
 }
 AttnE2m1JoinKernel attn_e2m1_join_kernel_for() { return attn_e2m1_join_kernel; }
 
-// A CTA per (sequence, page, head, side).
+// A CTA per (sequence, page, head): blocks of K and of V together, so that a page is looked up once for both.
 __global__ void __launch_bounds__(kE2m1WidenThreads) e2m1_widen_kernel(const __grid_constant__ WidenParams W) {
   const AttnParams& A = W.P.A;
   const int blocks = A.head_dim >> 4;
   unsigned idx = blockIdx.x;
-  const int side = idx & 1;
-  idx >>= 1;
   const int h = idx % (unsigned)A.heads_kv;
   idx /= (unsigned)A.heads_kv;
   const int j = idx % (unsigned)W.cols, b = idx / (unsigned)W.cols;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (side == 0 && h == 0 && threadIdx.x == 0) W.table[(long long)b * W.cols + j] = b * W.cols + j;
+  if (h == 0 && threadIdx.x == 0) W.table[(long long)b * W.cols + j] = b * W.cols + j;
   const AttnSeq s = attn_seq(A, b);
   if (s.n == 0) return;
   const int lo = attn_lo(A, s, 0), hi = attn_hi(A, s, s.n - 1);
   const long long first = (long long)j * kE2m1Page;
   if (hi <= lo || first >= hi || first + kE2m1Page <= lo) return;
-  const AttnSide& C = side ? A.v : A.k;
-  const AttnSide& S = side ? W.P.vs : W.P.ks;
-  uint16_t* out = (side ? W.v : W.k) + (((long long)b * W.cols + j) * A.heads_kv + h) * kE2m1Page * A.head_dim;
-  constexpr int kAhead = 4;  // blocks of a thread whose loads are under way together
-  for (int i0 = threadIdx.x; i0 < kE2m1Page * blocks; i0 += kAhead * kE2m1WidenThreads) {
-    uint2 w[kAhead];
-    uint32_t byte[kAhead];
+  const long long to = (((long long)b * W.cols + j) * A.heads_kv + h) * kE2m1Page * A.head_dim;
+  const char* const codes[2] = {reinterpret_cast<const char*>(A.k.base) + h * A.k.head, reinterpret_cast<const char*>(A.v.base) + h * A.v.head};
+  const unsigned char* const scales[2] = {reinterpret_cast<const unsigned char*>(W.P.ks.base) + h * W.P.ks.head,
+                                          reinterpret_cast<const unsigned char*>(W.P.vs.base) + h * W.P.vs.head};
+  constexpr int kAhead = 4;  // blocks of a thread, of K and of V, whose loads are under way together
+  const bool even = kE2m1WidenThreads % blocks == 0;  // a thread stays at its block of a token
+  const int in0 = (int)threadIdx.x / blocks, blk0 = (int)threadIdx.x - in0 * blocks, step = kE2m1WidenThreads / blocks;
+  for (int i0 = threadIdx.x, turn = 0; i0 < kE2m1Page * blocks; i0 += kAhead * kE2m1WidenThreads, ++turn) {
+    uint2 w[kAhead][2];
+    uint32_t byte[kAhead][2];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
-      const int i = i0 + a * kE2m1WidenThreads, in = i / blocks, blk = i - in * blocks;
+      const int i = i0 + a * kE2m1WidenThreads;
+      int in = in0 + (turn * kAhead + a) * step, blk = blk0;
+      if (!even) {
+        in = i / blocks;
+        blk = i - in * blocks;
+      }
       const long long key = first + in;
-      w[a] = make_uint2(0, 0);
-      byte[a] = 0;
+      w[a][0] = w[a][1] = make_uint2(0, 0);
+      byte[a][0] = byte[a][1] = 0;
       if (i < kE2m1Page * blocks && key >= lo && key < hi) {
         int within;
-        const long long page = attn_page(A, b, (int)key, within);
+        const int page = (int)attn_page(A, b, (int)key, within);
         if (page >= 0) {
-          w[a] = __ldg(reinterpret_cast<const uint2*>(reinterpret_cast<const char*>(C.base) + page * C.page + within * C.token + h * C.head) + blk);
-          byte[a] = __ldg(reinterpret_cast<const unsigned char*>(S.base) + page * S.page + within * S.token + h * S.head + blk);
+          const unsigned long long p = (unsigned)page, n = (unsigned)within;
+          w[a][0] = __ldg(reinterpret_cast<const uint2*>(codes[0] + p * A.k.page + n * A.k.token) + blk);
+          w[a][1] = __ldg(reinterpret_cast<const uint2*>(codes[1] + p * A.v.page + n * A.v.token) + blk);
+          byte[a][0] = __ldg(scales[0] + p * W.P.ks.page + n * W.P.ks.token + blk);
+          byte[a][1] = __ldg(scales[1] + p * W.P.vs.page + n * W.P.vs.token + blk);
         }
       }
     }
@@ -127,21 +136,25 @@ __global__ void __launch_bounds__(kE2m1WidenThreads) e2m1_widen_kernel(const __g
     for (int a = 0; a < kAhead; ++a) {
       const int i = i0 + a * kE2m1WidenThreads;
       if (i >= kE2m1Page * blocks) break;
-      uint32_t f[4], sc, none, y[8];
-      e4m3x4_to_f16x2(byte[a], sc, none);
-      const float scale = __half2float(__ushort_as_half((unsigned short)(sc & 0xffffu)));
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        e2m1x8_to_f16x2(half ? w[a].y : w[a].x, f);
+      for (int side = 0; side < 2; ++side) {
+        uint32_t f[4], sc, none, y[8];
+        e4m3x4_to_f16x2(byte[a][side], sc, none);
+        const float scale = __half2float(__ushort_as_half((unsigned short)(sc & 0xffffu)));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&f[k]));
-          y[4 * half + k] = bf_pack(v.x * scale, v.y * scale);
+        for (int half = 0; half < 2; ++half) {
+          e2m1x8_to_f16x2(half ? w[a][side].y : w[a][side].x, f);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float2 v = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&f[k])), make_float2(scale, scale));
+            y[4 * half + k] = bf_pack(v.x, v.y);
+          }
         }
+        // rows lie one after the other; 32 bytes at a time, a whole sector
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"((side ? W.v : W.k) + to + 16ll * i), "r"(y[0]), "r"(y[1]), "r"(y[2]),
+                     "r"(y[3]), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7])
+                     : "memory");
       }
-      uint4* to = reinterpret_cast<uint4*>(out + 16ll * i);  // rows lie one after the other
-      to[0] = make_uint4(y[0], y[1], y[2], y[3]);
-      to[1] = make_uint4(y[4], y[5], y[6], y[7]);
     }
   }
 }

@@ -875,7 +875,7 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
     p.widen = true;
     p.table_bytes = ((int64_t)seqs * p.cols * 4 + 15) / 16 * 16;
     p.rest = attn_workspace(tc, head_dim);
-    p.need = 2 * p.side_bytes + p.table_bytes + p.rest;
+    p.need = 2 * p.side_bytes + p.table_bytes + p.rest + 16;  // 16: the widened cache starts at a multiple of 32 bytes, which its stores take at a time
     *out = p;
     return QKNORM_OK;
   }
@@ -886,8 +886,8 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
   if (window > 0) {  // the first row's window, and what the later ones see behind it
     const int64_t w = (int64_t)window + (causal ? max_q : T) - 1;
     if (w < span) span = w;
+    span += kE2m1Tile - 1;  // units start at a multiple of a tile
   }
-  span += kE2m1Tile - 1;  // units start at a multiple of a tile
   if (row_tiles > 0x3fffffff / seqs) return QKNORM_ERR_SHAPE;
   p.row_tiles = (int)row_tiles;
   const int tma = env_int("QKNORM_E2M1_TMA", -1);  // 0, 1: for tests
@@ -1043,11 +1043,11 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   if (plan.widen) {
     WidenParams W;
     W.P = E;
-    W.k = (uint16_t*)ws;
-    W.v = (uint16_t*)((char*)ws + plan.side_bytes);
-    W.table = (int*)((char*)ws + 2 * plan.side_bytes);
+    W.k = (uint16_t*)(((uintptr_t)ws + 31) & ~(uintptr_t)31);
+    W.v = (uint16_t*)((char*)W.k + plan.side_bytes);
+    W.table = (int*)((char*)W.k + 2 * plan.side_bytes);
     W.cols = plan.cols;
-    const int64_t ctas = (int64_t)seqs * plan.cols * cache->heads * 2;
+    const int64_t ctas = (int64_t)seqs * plan.cols * cache->heads;
     if (ctas > 0) {
       const cudaError_t e = launch_overlapped(e2m1_widen_kernel_for(), (unsigned)ctas, (unsigned)kE2m1WidenThreads, 0, stream, W);
       if (e != cudaSuccess) return set_cuda_error(e);

@@ -380,6 +380,17 @@ def test_strided_rows_and_other_streams(libqknorm):
     b.compare(out.cpu(), lse.cpu(), ref, True)
 
 
+@pytest.mark.parametrize("skew", [0, 16])
+@pytest.mark.parametrize("new,kv", [([60, 1], [300, 77]), ([1, 1], [3000, 50])])
+def test_workspaces_anywhere(libqknorm, new, kv, skew):
+    """A workspace of exactly the bytes asked for, at any multiple of 16: what lies around it stays."""
+    b = Batch(new, kv, 8, 2, 128, seed=12)
+    n = attn.attn_paged_e2m1_workspace(2, b.T, max(new), max(kv), 8, 2, 128)
+    around = torch.full((n + 64,), 77, dtype=torch.uint8, device="cuda")
+    b.check("attn_tc" if max(new) > 24 else "attn_e2m1", workspace=around[skew:skew + n]) if n else b.check()
+    assert (around[:skew] == 77).all() and (around[skew + n:] == 77).all()
+
+
 @pytest.mark.parametrize("new,kv", [([1, 1], [700, 900]), ([70, 2], [700, 300])])
 def test_capture_and_replay(libqknorm, copies, new, kv):
     b = Batch(new, kv, 8, 2, 128, seed=10)
