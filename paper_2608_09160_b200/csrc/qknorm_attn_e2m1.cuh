@@ -17,6 +17,13 @@
 // Scores come out with keys along g and rows along t, and go back in transposed by movmatrix; a thread's output columns are the
 // rows of its scores, so that maxima and rescaling need no exchange beyond the maximum itself.
 //
+// What holds it then, at 64 sequences of up to 8192 keys, 64 / 8 heads of 128 (102 us; its 382 MB take 58 at the copy rate): without its copies the kernel
+// takes 83 us, without its arithmetic 76.  A tile of 32 keys is 136 widening conversions at two cycles each on one pipe, 128 packed products
+// at two cycles on another, 32 matrix instructions at 8.8 and about 180 others; four warps of a scheduler alone with the K and V steps, out of registers, take
+// 612 cycles a tile, all of it together 1018.  Tried and dropped: 64 keys a tile by cp.async (124 us against 123), V's words
+// loaded before the weights (no difference), the scores of the next tile beside the weights and products of this one (101 against 99), four tiles of
+// eight rows (spills; 60 rows 97 us against 74 with two), copies of one head's 16 tokens (124: the copy engine's time goes by the copy).
+//
 // Work: a unit is up to 8 NT query rows of a sequence and one key head for each warp as far as the CTA has heads; further warps take
 // other keys of the same heads, and their parts are joined in shared memory.  A round is 32 keys for every warp.  With many heads to a CTA a
 // copy brings a page's tokens of all of them.  See E2m1Item for how units come to CTAs.
