@@ -138,7 +138,7 @@ __device__ __forceinline__ int e2m1_share_of(long long total, int grid, long lon
   const long long q = total / grid, more = total - q * grid;
   return (int)(at < more * (q + 1) ? at / (q + 1) : more + (at - more * (q + 1)) / q);
 }
-// By the whole CTA.  scratch: 33 long longs; both in shared memory.
+// By the whole CTA.  scratch: a long long for every warp; both in shared memory.
 __device__ __forceinline__ void e2m1_find(const AttnE2m1Params& P, int groups, int round, long long* scratch, E2m1Start* out) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int n = P.A.seqs * P.row_tiles;  // the host has checked that it fits

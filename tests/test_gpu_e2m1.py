@@ -437,3 +437,89 @@ def test_append_then_attend(libqknorm):
         tol, tol_lse = R.attention_bounds(ref, hd, n == 1)
         assert (np.abs(out.cpu().double().numpy().reshape(n, hq, hd) - ref["out"]) <= tol).all()
         assert (np.abs(lse.cpu().double().numpy() - ref["lse"]) <= tol_lse).all()
+
+
+@pytest.mark.parametrize("new", [[1, 2], [60, 2]])
+def test_no_keys_to_look_at(libqknorm, copies, new):
+    """Bounds of 0 keys, tables without columns, a pool without pages: zeros (a page that is none reads as zeros)."""
+    b = Batch(new, [50, 40], 4, 2, 64, seed=13)
+    n = b.starts[-1]
+    out, lse = b.call(max_kv=0)
+    assert (out[:n] == 0).all() and torch.isneginf(lse[:n]).all() and (out[n:] == 7.0).all()
+    b.dtable = b.dtable[:, :0]
+    out, lse = b.call()
+    assert (out[:n] == 0).all() and torch.isneginf(lse[:n]).all()
+    c = Batch(new, [50, 40], 4, 2, 64, seed=13)
+    c.pools = [t[:0] for t in c.pools]
+    out, lse = c.call()
+    seen = torch.tensor([max(0, L - m + i + 1) for m, L in zip(new, [50, 40]) for i in range(m)]).double()
+    assert (out[:n] == 0).all() and ((lse[:n].double() - torch.log(seen)[:, None]).abs()[seen > 0] < 1e-5).all()
+
+
+def test_more_query_heads_than_the_widened_path_takes(libqknorm):
+    Batch([1, 2], [300, 40], 130, 1, 64, seed=14).check()
+    Batch([3], [500], 300, 2, 128, seed=15).check()
+
+
+@pytest.mark.parametrize("hq,hk", [(8, 8), (16, 8), (4, 1)])
+def test_results_at_odd_addresses(libqknorm, copies, hq, hk):
+    b = Batch([1, 3], [77, 2000], hq, hk, 128, seed=16)
+    ref = b.reference()
+    wide = torch.full((b.T, hq * 128 + 3), 7.0, dtype=BF16, device="cuda")
+    out, lse = wide[:, 1:1 + hq * 128], torch.full((b.T, hq), 7.0, device="cuda")
+    attn.qknorm_attn_paged_e2m1(b.dq, *b.pools, b.dtable, b.dlens, b.dstarts, 3, 2000, k_scale=b.unit[0], v_scale=b.unit[1], out=out, lse=lse)
+    torch.cuda.synchronize()
+    b.compare(out.cpu(), lse.cpu(), ref, True)
+    assert (wide[:, 0] == 7.0).all() and (wide[:, 1 + hq * 128:] == 7.0).all()
+
+
+def test_two_streams_at_once(libqknorm, copies):
+    """Calls that run beside one another, each with a workspace of its own, give what they give alone."""
+    b, c = Batch([1] * 8, [2500] * 8, 8, 8, 128, seed=17), Batch([1] * 3, [4000, 50, 3000], 16, 2, 64, seed=18)
+    want = [x.call()[0] for x in (b, c)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.zeros_like(x.dq) for _ in range(6)] for x in (b, c)]
+    torch.cuda.synchronize()
+    for i in range(6):
+        for x, s, o in zip((b, c), streams, outs):
+            attn.qknorm_attn_paged_e2m1(x.dq, *x.pools, x.dtable, x.dlens, x.dstarts, 1, max(x.kv), k_scale=x.unit[0], v_scale=x.unit[1], out=o[i], stream=s)
+    torch.cuda.synchronize()
+    for x, w, o in zip((b, c), want, outs):
+        n = x.starts[-1]
+        for y in o:
+            assert torch.equal(y.cpu()[:n].view(torch.int16), w[:n].view(torch.int16))
+
+
+def test_lengths_grow_between_replays(libqknorm, copies):
+    b = Batch([1, 1], [700, 3000], 8, 4, 128, seed=19)
+    out = torch.zeros_like(b.dq)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attn.qknorm_attn_paged_e2m1(b.dq, *b.pools, b.dtable, b.dlens, b.dstarts, 1, 3000, k_scale=b.unit[0], v_scale=b.unit[1], out=out)
+    for lens in ([1, 1], [0, 2999], [700, 3000], [33, 128]):
+        b.dlens.copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        want, _ = b.call(max_kv=3000)
+        assert torch.equal(out.cpu()[:2].view(torch.int16), want[:2].view(torch.int16))
+
+
+def test_python_refusals(libqknorm):
+    b = Batch([1], [20], 2, 1, 64, seed=20)
+    k, v, ks, vs = b.pools
+    bad = [(k[..., :16], v, ks, vs), (k, v, ks[..., :2], vs), (k.view(torch.int8), v, ks, vs), (k, v, ks.view(torch.int8), vs), (k, v.cpu(), ks, vs),
+           (k, v, ks, None), (k.transpose(2, 3), v.transpose(2, 3), ks, vs), (k[:1], v, ks, vs), (k, v, ks.view(torch.uint8), vs), (k[0], v[0], ks[0], vs[0])]
+    for pools in bad:
+        with pytest.raises(binding.QKNormError):
+            attn.qknorm_attn_paged_e2m1(b.dq, *pools, b.dtable, b.dlens, b.dstarts, 1, 20)
+    x = torch.zeros((2, 64), dtype=BF16, device="cuda")
+    slots = torch.zeros(2, dtype=torch.int64, device="cuda")
+    for pools in bad:
+        with pytest.raises(binding.QKNormError):
+            attn.qknorm_fwd_append_e2m1(None, x, x, None, None, None, None, slots, *pools, 1e-6)
+    four = torch.zeros((1, 16, 1, 32), dtype=torch.uint8, device="cuda").view(torch.float4_e2m1fn_x2)     # torch's own type for two codes
+    byte = torch.zeros((1, 16, 1, 4), dtype=torch.uint8, device="cuda")
+    x[0], x[1] = 3.0, -1.5
+    attn.qknorm_fwd_append_e2m1(None, x, x, None, None, None, None, torch.tensor([4, 7], device="cuda"), four, torch.zeros_like(four.view(torch.uint8)).view(four.dtype),
+                                byte, torch.zeros_like(byte), 1e-6)
+    torch.cuda.synchronize()
+    assert (four.view(torch.uint8)[0, 4] == 0x77).all() and (four.view(torch.uint8)[0, 7] == 0xFF).all() and (byte[0, [4, 7]] != 0).all()
