@@ -4,7 +4,7 @@
 // has six and is exact in fp16; the products are fp16 in, fp32 out.
 //
 // What bounds it: single tokens read 9/16 byte per element of K and V, a quarter of a bf16 cache, and have to widen every one of
-// them.  So nothing is staged for the matrix unit: a warp brings 32 keys at a time into shared memory by cp.async, widens them out of
+// them.  So nothing is staged for the matrix unit: a warp takes 32 keys at a time as they lie in the cache, from shared memory, widens them in
 // registers straight into the operands of mma.sync, and no widened element touches memory.  K and V are the 16-row operand and the query
 // rows the 8-column one, S^T = K Q^T and O^T = V^T P^T: eight query heads of a key head fill a matrix instruction, where they would
 // leave half (mma.sync) or fifteen sixteenths (tcgen05) of it empty as its rows.

@@ -50,20 +50,20 @@ __global__ void __launch_bounds__(kE2m1JoinThreads) attn_e2m1_join_kernel(const 
     for (int d0 = 0; d0 < A.head_dim; d0 += 128) {
       const int d = d0 + 4 * lane;
       float acc[4] = {0.f, 0.f, 0.f, 0.f}, sum = 0.f;
-      for (int p0 = 0; p0 < parts; p0 += 32) {  // a lane each for the parts' weights, then four parts' rows at a time
+      for (int p0 = 0; p0 < parts; p0 += 32) {  // a lane each for the parts' weights, then eight parts' rows at a time
         const float zp = p0 + lane < parts ? P.part_z[place(p0 + lane, k)] : kNegInf;
         const float wp = zp == kNegInf ? 0.f : z == kNegInf ? zp : exp2f(zp - z);
         const int n = parts - p0 < 32 ? parts - p0 : 32;
-        for (int p = 0; p < n; p += 4) {
-          float4 x[4];
+        constexpr int kAhead = 8;
+        for (int p = 0; p < n; p += kAhead) {
+          float4 x[kAhead];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int e = 0; e < kAhead; ++e)
             x[e] = p + e < n && d < A.head_dim ? *reinterpret_cast<const float4*>(P.part_o + place(p0 + p + e, k) * A.head_dim + d)
                                                : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float w = __shfl_sync(0xffffffffu, wp, (p + e) & 31);
-            if (p + e >= n) continue;
+          for (int e = 0; e < kAhead; ++e) {
+            const float w = __shfl_sync(0xffffffffu, wp, p + e);  // 0 behind the last part
             sum += w;
             acc[0] = fmaf(w, x[e].x, acc[0]);
             acc[1] = fmaf(w, x[e].y, acc[1]);
