@@ -61,10 +61,11 @@ struct E2m1Maps {  // [page][head][a page's tokens, one after the other]; elemen
 
 // How tiles come and lie in shared memory.  COPY 0: by TMA, runs of 16 or 32 tokens of all the CTA's heads per copy; a stage holds a tile
 // for every warp, [run][head][token].  COPY 8, 16: any layout, by cp.async of that many bytes; stages are a warp's own.  The pitches keep
-// the reads free of bank conflicts, but for V by TMA (two ways; see key_of).
-template <int DP, int NT, int COPY>
+// the reads free of bank conflicts, but for V by TMA (two ways; see key_of).  WARPS: eight by cp.async for few short units, one CTA an SM.
+constexpr int e2m1_warps(int nt, int copy) { return copy == 0 && nt == 1 ? 8 : 4; }
+template <int DP, int NT, int COPY, int WARPS = e2m1_warps(NT, COPY)>
 struct E2m1Cta {
-  static constexpr int kWarps = COPY == 0 && NT == 1 ? 8 : 4, kThreads = 32 * kWarps;
+  static constexpr int kWarps = WARPS, kThreads = 32 * kWarps;
   static constexpr int kStages = DP == 256 ? 2 : 3;
   static constexpr int kTiles = COPY == 0 ? kWarps : 1;  // of a stage
   static constexpr int kKPitch = DP == 256 ? 144 : DP / 2;
@@ -82,7 +83,7 @@ struct E2m1Cta {
   static constexpr int kOPitch = DP + 8;           // floats
   static constexpr int kJoin = kWarps * 8 * NT * kOPitch * 4;
   static constexpr int kSmem = 128 + kQBytes + (kJoin > kAll ? kJoin : kAll);
-  static constexpr int kPerSm = DP == 256 || kWarps == 8 ? 2 : 3;
+  static constexpr int kPerSm = COPY != 0 && kWarps == 8 ? 1 : DP == 256 || kWarps == 8 ? 2 : 3;
 };
 constexpr int kE2m1Runs = 256;  // runs whose pages are looked up at a time
 
@@ -518,11 +519,11 @@ struct E2m1Core {
   }
 };
 
-// DP: head_dim padded; NT: tiles of 8 query rows; COPY: see E2m1Cta.
-template <int DP, int NT, int COPY>
-__global__ void __launch_bounds__(E2m1Cta<DP, NT, COPY>::kThreads, E2m1Cta<DP, NT, COPY>::kPerSm)
+// DP: head_dim padded; NT: tiles of 8 query rows; COPY, WARPS: see E2m1Cta.
+template <int DP, int NT, int COPY, int WARPS>
+__global__ void __launch_bounds__(E2m1Cta<DP, NT, COPY, WARPS>::kThreads, E2m1Cta<DP, NT, COPY, WARPS>::kPerSm)
     attn_e2m1_kernel(const __grid_constant__ AttnE2m1Params P, const __grid_constant__ E2m1Maps maps) {
-  using C = E2m1Cta<DP, NT, COPY>;
+  using C = E2m1Cta<DP, NT, COPY, WARPS>;
   using Core = E2m1Core<DP, NT, COPY>;
   constexpr bool kTma = COPY == 0;
   constexpr int kWarps = C::kWarps;
@@ -921,10 +922,10 @@ struct E2m1Launch {
   AttnE2m1Kernel fn;
   int smem, warps, per_sm;
 };
-// in qknorm_attn_e2m1_inst.cu; nt 1 or 2; copy 0 (not for dp 256), 8 or 16
-E2m1Launch attn_e2m1_kernel_64(int nt, int copy);
-E2m1Launch attn_e2m1_kernel_128(int nt, int copy);
-E2m1Launch attn_e2m1_kernel_256(int nt, int copy);
+// in qknorm_attn_e2m1_inst.cu; nt 1 or 2; copy 0 (not for dp 256), 8 or 16; wide: eight warps by cp.async, nt 1
+E2m1Launch attn_e2m1_kernel_64(int nt, int copy, bool wide);
+E2m1Launch attn_e2m1_kernel_128(int nt, int copy, bool wide);
+E2m1Launch attn_e2m1_kernel_256(int nt, int copy, bool wide);
 AttnE2m1JoinKernel attn_e2m1_join_kernel_for();
 
 // The visible part of a 4-bit cache as bf16 -- exact, the largest product of a code and a scale has six significant bits -- in pages of

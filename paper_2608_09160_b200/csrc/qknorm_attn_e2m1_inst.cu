@@ -8,10 +8,10 @@ namespace qknorm {
 #define QKNORM_PASTE(a, b) QKNORM_PASTE_(a, b)
 
 namespace {
-template <int NT, int COPY>
+template <int NT, int COPY, int WARPS = e2m1_warps(NT, COPY)>
 E2m1Launch one() {
-  return E2m1Launch{attn_e2m1_kernel<QKNORM_DP, NT, COPY>, E2m1Cta<QKNORM_DP, NT, COPY>::kSmem, E2m1Cta<QKNORM_DP, NT, COPY>::kWarps,
-                    E2m1Cta<QKNORM_DP, NT, COPY>::kPerSm};
+  using C = E2m1Cta<QKNORM_DP, NT, COPY, WARPS>;
+  return E2m1Launch{attn_e2m1_kernel<QKNORM_DP, NT, COPY, WARPS>, C::kSmem, C::kWarps, C::kPerSm};
 }
 template <int NT>
 E2m1Launch pick(int copy) {
@@ -22,7 +22,8 @@ E2m1Launch pick(int copy) {
 }
 }  // namespace
 
-E2m1Launch QKNORM_PASTE(attn_e2m1_kernel_, QKNORM_DP)(int nt, int copy) {
+E2m1Launch QKNORM_PASTE(attn_e2m1_kernel_, QKNORM_DP)(int nt, int copy, bool wide) {
+  if (wide) return copy == 16 ? one<1, 16, 8>() : one<1, 8, 8>();
   return nt == 1 ? pick<1>(copy) : pick<2>(copy);
 }
 

@@ -841,6 +841,9 @@ struct E2m1Plan {
   // head, TMA with 8 (4, 2) heads a copy | cp.async: 64 x 8192 keys 102 | 123, 16 x 32000 keys 97 (102, 106) | 109, 256 x 500 keys 53 | 59, but
   // 64 x 1000 keys 33 | 31, 16 x 2000 keys 27 | 21, 4 x 8192 keys 43 | 23; 2 key heads, 32 x 4000 keys 45 | 32.
   bool tma = false;
+  // Eight warps a CTA by cp.async instead of four: where units are no more than SMs, and short enough to be taken whole.  us, eight warps
+  // | four: 8 x 1000 keys, 8 key heads of 5 11.4 | 14.8, 16 x 2000 keys, 8 of 8 17.8 | 21.5, 4 x 500 keys 8.3 | 10.3.
+  bool wide = false;
   int nt = 1, row_tiles = 1, cols = 0;
   struct Way {  // by cp.async, by TMA
     int heads = 1, grid = 1;
@@ -858,8 +861,8 @@ struct E2m1Plan {
 constexpr int kE2m1WidenRows = 96;
 constexpr int64_t kE2m1WidenMost = (int64_t)2 << 30;    // bytes of the widened cache
 
-E2m1Launch e2m1_kernel(int head_dim, int nt, int copy) {
-  return head_dim <= 64 ? attn_e2m1_kernel_64(nt, copy) : head_dim <= 128 ? attn_e2m1_kernel_128(nt, copy) : attn_e2m1_kernel_256(nt, copy);
+E2m1Launch e2m1_kernel(int head_dim, int nt, int copy, bool wide) {
+  return head_dim <= 64 ? attn_e2m1_kernel_64(nt, copy, wide) : head_dim <= 128 ? attn_e2m1_kernel_128(nt, copy, wide) : attn_e2m1_kernel_256(nt, copy, wide);
 }
 
 int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, bool causal, int window, int sms,
@@ -893,8 +896,12 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
   const int tma = env_int("QKNORM_E2M1_TMA", -1);  // 0, 1: for tests
   for (int k = 0; k < 2; ++k) {
     if (k == 1 && head_dim != 64 && head_dim != 128) continue;
-    const E2m1Launch kernel = e2m1_kernel(head_dim, p.nt, k == 1 ? 0 : 16);
     E2m1Plan::Way& w = p.way[k];
+    if (k == 0) {
+      const int wide_round = 8 * kE2m1Tile;
+      p.wide = p.nt == 1 && row_tiles * seqs * heads_kv <= sms && (span + wide_round - 1) / wide_round <= kE2m1Whole;
+    }
+    const E2m1Launch kernel = e2m1_kernel(head_dim, p.nt, k == 1 ? 0 : 16, k == 0 && p.wide);
     while (k == 1 && 2 * w.heads <= kernel.warps && heads_kv % (2 * w.heads) == 0) w.heads *= 2;
     const int round = kE2m1Tile * kernel.warps / w.heads;
     const int64_t places = (int64_t)sms * kernel.per_sm, rounds = (span + round - 1) / round;
@@ -1098,7 +1105,7 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   E.heads_cta = way.heads;
   E.shares = way.shares;
   P.grid = way.grid;
-  const E2m1Launch kernel = e2m1_kernel(hd, plan.nt, copy);
+  const E2m1Launch kernel = e2m1_kernel(hd, plan.nt, copy, copy != 0 && plan.wide);
   rc = allow_dynamic_smem((const void*)kernel.fn, kernel.smem);
   if (rc != QKNORM_OK) return rc;
   cudaError_t e = launch_overlapped(kernel.fn, (unsigned)way.grid, (unsigned)(32 * kernel.warps), (size_t)kernel.smem, stream, E, maps);

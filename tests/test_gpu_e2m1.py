@@ -456,6 +456,12 @@ def test_no_keys_to_look_at(libqknorm, copies, new):
     assert (out[:n] == 0).all() and ((lse[:n].double() - torch.log(seen)[:, None]).abs()[seen > 0] < 1e-5).all()
 
 
+@pytest.mark.parametrize("hd", [64, 96, 128, 256])
+def test_many_short_sequences(libqknorm, copies, hd):
+    """More units than SMs, each taken whole."""
+    Batch([1] * 160, [(53 * i) % 290 for i in range(160)], 2, 1, hd, seed=21).check()
+
+
 def test_more_query_heads_than_the_widened_path_takes(libqknorm):
     Batch([1, 2], [300, 40], 130, 1, 64, seed=14).check()
     Batch([3], [500], 300, 2, 128, seed=15).check()
