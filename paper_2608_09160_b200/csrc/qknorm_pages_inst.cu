@@ -136,6 +136,7 @@ __global__ void __cluster_dims__(kPlanCluster, 1, 1) __launch_bounds__(kPlanThre
   constexpr int kStep = kPlanThreads * kPlanAhead;
   const long long per = ((P.num_pages + kPlanCluster - 1) / kPlanCluster + kPlanAhead - 1) / kPlanAhead * kPlanAhead;
   const long long begin = per * rank < P.num_pages ? per * rank : P.num_pages, end = begin + per < P.num_pages ? begin + per : P.num_pages;
+  const bool once = per <= kStep;  // a thread's pages are looked at once and stay in its registers
   int r[kPlanAhead], total;
   // held pages
   int mine = 0;
@@ -150,43 +151,17 @@ __global__ void __cluster_dims__(kPlanCluster, 1, 1) __launch_bounds__(kPlanThre
   cluster_sync();
   int live = 0;
   for (int c = 0; c < kPlanCluster; ++c) live += cluster_read(&held, c);
-  // free pages before `live`, held ones from there on
-  int n_holes = 0, n_movers = 0;
-  for (long long p0 = begin + tid * kPlanAhead; p0 < end; p0 += kStep) {
-    plan_refs(P, p0, end, r);
+  // free pages before `live`, and held ones from there on, of a thread's kPlanAhead pages: in the lower and the upper half of a word
+  auto both = [&](long long p0) {
+    int n = 0;
 #pragma unroll
     for (int k = 0; k < kPlanAhead; ++k) {
       if (p0 + k >= end) continue;
-      n_holes += r[k] <= 0 && p0 + k < live;
-      n_movers += r[k] > 0 && p0 + k >= live;
+      n += r[k] <= 0 && p0 + k < live ? 1 : r[k] > 0 && p0 + k >= live ? 1 << 16 : 0;
     }
-  }
-  plan_scan(n_holes, scratch, total);
-  if (tid == 0) holes = total;
-  plan_scan(n_movers, scratch, total);
-  if (tid == 0) movers = total;
-  __syncthreads();
-  cluster_sync();
-  int hole = 0, mover = 0, moves = 0;
-  for (int c = 0; c < kPlanCluster; ++c) {
-    const int a = cluster_read(&holes, c), b = cluster_read(&movers, c);
-    if (c < rank) hole += a, mover += b;
-    moves += b;
-  }
-  for (long long at = begin; at < end; at += kStep) {
-    const long long p0 = at + tid * kPlanAhead;
-    if (p0 < end) plan_refs(P, p0, end, r);
-    int a = 0, b = 0;
-#pragma unroll
-    for (int k = 0; k < kPlanAhead; ++k) {
-      if (p0 + k >= end) continue;
-      a += r[k] <= 0 && p0 + k < live;
-      b += r[k] > 0 && p0 + k >= live;
-    }
-    int ia = hole + plan_scan(a, scratch, total);
-    hole += total;
-    int ib = mover + plan_scan(b, scratch, total);
-    mover += total;
+    return n;
+  };
+  auto list = [&](long long p0, int ia, int ib) {
 #pragma unroll
     for (int k = 0; k < kPlanAhead; ++k) {
       const long long p = p0 + k;
@@ -197,15 +172,47 @@ __global__ void __cluster_dims__(kPlanCluster, 1, 1) __launch_bounds__(kPlanThre
         if (r[k] > 0) P.src[ib++] = (int)p;
       }
     }
+  };
+  int before = 0, n_holes = 0, n_movers = 0;
+  const long long mine0 = begin + tid * kPlanAhead;
+  for (long long at = begin; at < end; at += kStep) {
+    const long long p0 = at + tid * kPlanAhead;
+    if (!once && p0 < end) plan_refs(P, p0, end, r);
+    before = plan_scan(both(p0), scratch, total);
+    n_holes += total & 0xffff;
+    n_movers += total >> 16;
+  }
+  if (tid == 0) {
+    holes = n_holes;
+    movers = n_movers;
+  }
+  __syncthreads();
+  cluster_sync();
+  int hole = 0, mover = 0, moves = 0;
+  for (int c = 0; c < kPlanCluster; ++c) {
+    const int a = cluster_read(&holes, c), b = cluster_read(&movers, c);
+    if (c < rank) hole += a, mover += b;
+    moves += b;
+  }
+  if (once) {
+    list(mine0, hole + (before & 0xffff), mover + (before >> 16));
+  } else {
+    for (long long at = begin; at < end; at += kStep) {
+      const long long p0 = at + tid * kPlanAhead;
+      if (p0 < end) plan_refs(P, p0, end, r);
+      before = plan_scan(both(p0), scratch, total);
+      list(p0, hole + (before & 0xffff), mover + (before >> 16));
+      hole += total & 0xffff;
+      mover += total >> 16;
+    }
   }
   __threadfence();
-  cluster_sync();
+  cluster_sync();  // the lists are complete, and nobody reads another's shared memory any more
   for (int k = rank * kPlanThreads + tid; k < moves; k += kPlanCluster * kPlanThreads) P.map[__ldcg(P.src + k)] = __ldcg(P.dst + k);
   if (rank == 0 && tid == 0) {
     *P.count = moves;
     *P.live = live;
   }
-  cluster_sync();  // nobody leaves while its shared memory may be read
 }
 
 // Rows give up their pages: a CTA per row.

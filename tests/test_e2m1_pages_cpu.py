@@ -206,7 +206,7 @@ def test_pages_argument_errors(lib):
         assert fn(lib, cols=-1) == b.QKNORM_ERR_SHAPE
         assert fn(lib, rows=-1) == b.QKNORM_ERR_SHAPE
         assert fn(lib, N=1 << 31) == b.QKNORM_ERR_SHAPE
-        assert fn(lib, lens=C + 16) == b.QKNORM_ERR_ALIAS                        # inside the table
+        assert fn(lib, lens=C + 16) == b.QKNORM_ERR_ALIAS                        # inside the table: one of the two is written
         assert fn(lib, refs=D) == b.QKNORM_ERR_ALIAS
         if CPU:
             assert fn(lib) == LEGAL
@@ -220,6 +220,9 @@ def test_pages_argument_errors(lib):
         assert fn(lib, ws=G + 4) == b.QKNORM_ERR_SCRATCH
         assert fn(lib, ws=C) == b.QKNORM_ERR_SCRATCH                             # on the table
         assert fn(lib, ws=A) == b.QKNORM_ERR_SCRATCH                             # on the pages
+    if CPU:
+        assert fork(lib, parents=E, children=E + 4) == LEGAL                     # lists that are only read may overlap
+        assert fork(lib, parents=E, children=E) == LEGAL
     n = ctypes.c_int64(0)
     assert lib.qknorm_pages_workspace(100, 4, 2, None) == b.QKNORM_ERR_NULL
     assert lib.qknorm_pages_workspace(0, 4, 2, ctypes.byref(n)) == b.QKNORM_ERR_SHAPE

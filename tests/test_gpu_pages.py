@@ -127,7 +127,7 @@ class Model:
             assert torch.equal(a.cpu().view(torch.uint8) if a.dtype.itemsize == 1 else a.cpu(), b.view(torch.uint8) if b.dtype.itemsize == 1 else b)
 
 
-@pytest.mark.parametrize("page,cols,N", [(16, 9, 64), (1, 30, 200), (24, 5, 40), (64, 4, 20000)])
+@pytest.mark.parametrize("page,cols,N", [(16, 9, 64), (1, 30, 200), (24, 5, 40), (64, 4, 20000), (2, 300, 70001), (1, 9, 131073)])
 def test_a_life(libqknorm, page, cols, N):
     """Sequences come, are forked, grow, end, and the pool is packed, over and over."""
     m = Model(N, 12, cols, page, seed=N)
