@@ -144,52 +144,57 @@ struct Chunk8<IoE4m3> {
   }
 };
 
-// What goes into a 4-bit cache (include/qknorm_attn.h: qknorm_fwd_append_e2m1).  16384 tokens of 5120 + 1024 + 1024 take 98 us, where 64 would move the
-// bytes and a bf16 cache takes 83: the conversions of a block are about 100 instructions in warps that issue in two cycles of three.
-// With 64 registers a thread for four CTAs an SM instead of 80 for three the compiler spills.
+// What goes into a 4-bit cache (include/qknorm_attn.h: qknorm_fwd_append_e2m1).  16384 tokens of 5120 + 1024 + 1024 take 88 us, where 64 would move the
+// bytes and a bf16 cache takes 81; the issue slots are 70 % full.
 
-// The larger magnitude, or NaN if either is.
+// The largest of three, or NaN if any is.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ float absmax8(const float2 (&v)[4]) {
   float m = max_nan(fabsf(v[0].x), fabsf(v[0].y));
 #pragma unroll
-  for (int e = 1; e < 4; ++e) m = max_nan(m, max_nan(fabsf(v[e].x), fabsf(v[e].y)));
+  for (int e = 1; e < 4; ++e) m = max_nan(m, fabsf(v[e].x), fabsf(v[e].y));
   return m;
 }
-// x / d correctly rounded, r = 1/d to half a step: a product and one correction by its remainder (Markstein).  Ties between two codes
-// are common (bf16 values over a scale of four bits), and an ulp would decide them wrongly.
-__device__ __forceinline__ float2 quotient(float2 x, float d, float r) {
-  const float2 rr = make_float2(r, r), q = __fmul2_rn(x, rr);
-  return __ffma2_rn(__ffma2_rn(q, make_float2(-d, -d), x), rr, q);
+// x / d correctly rounded, for a d of at most four significant bits: its reciprocal is r, rounded down, and what is left.  The sum of
+// the two products is off by 2^-45 of itself before its one rounding, and these quotients stay 2^-29 away from the middle between two
+// fp32 numbers.  Ties between two codes are common (bf16 values over such a scale), and an ulp would decide them wrongly.
+struct Reciprocal {
+  float r, rest;
+};
+__device__ __forceinline__ float2 quotient(float2 x, Reciprocal d) {
+  return __ffma2_rn(x, make_float2(d.r, d.r), __fmul2_rn(x, make_float2(d.rest, d.rest)));
 }
-// The E4M3 scale of a block whose largest magnitude is amax, as its byte; its value f and 1/f (0 for f = 0).
-__device__ __forceinline__ float e2m1_scale(float amax, uint32_t& byte, float& r) {
+// The E4M3 scale of a block whose largest magnitude is amax, as its byte; returns the scale's reciprocal, 0 for a scale of 0 or NaN.
+// For the scale 448, which infinities have, rest > 0: they stay infinite.
+__device__ __forceinline__ Reciprocal e2m1_scale(float amax, uint32_t& byte) {
   float most;
-  asm("min.NaN.f32 %0, %1, 0f7E967699;" : "=f"(most) : "f"(amax));  // 1e38: an infinity has no remainder
-  byte = e4m3_pack2(quotient(make_float2(most, most), 6.0f, 1.0f / 6.0f).x, 0.f) & 0xffu;
+  asm("min.NaN.f32 %0, %1, 0f7E967699;" : "=f"(most) : "f"(amax));  // 1e38
+  byte = e4m3_pack2(quotient(make_float2(most, most), {0x1.555554p-3f, 0x1.555556p-27f}).x, 0.f) & 0xffu;
   uint32_t f01, f23;
   e4m3x4_to_f16x2(byte, f01, f23);
   const float f = __half2float(__ushort_as_half((unsigned short)(f01 & 0xffffu)));
-  // a scale has four significant bits, its reciprocal is found by one of Newton's steps from an estimate
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(f));
-  r = fmaf(r, fmaf(-f, r, 1.0f), r);
-  if (!(f > 0.f)) r = 0.f;
-  return f;
+  // from an estimate by one of Newton's steps, rounded down; the remainder f*r - 1 is exact
+  Reciprocal d;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d.r) : "f"(f));
+  d.r = __fmaf_rz(d.r, fmaf(-f, d.r, 1.0f), d.r);
+  d.rest = d.r * fmaf(-f, d.r, 1.0f);
+  if (!(f > 0.f)) d.r = d.rest = 0.f;
+  return d;
 }
 // Codes of eight elements of a block with that scale.
-__device__ __forceinline__ uint32_t e2m1_codes8(const float2 (&v)[4], float amax, float f, float r) {
+__device__ __forceinline__ uint32_t e2m1_codes8(const float2 (&v)[4], Reciprocal d) {
   float2 y[4];
-  if (amax < 1e30f) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = quotient(v[e], f, r);
-  } else {  // far beyond +-6 times the largest scale, where a remainder may overflow
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = make_float2(v[e].x * r, v[e].y * r);
-  }
+  for (int e = 0; e < 4; ++e) y[e] = quotient(v[e], d);
   return e2m1_pack8(y);
 }
 
@@ -205,8 +210,10 @@ __device__ __forceinline__ long long cache_at(const CacheSide& c, long long slot
 // IO: storage of q, k, v and out_q.  CIO: storage of the cache.  INTER: interleaved pairs.  UPT: 16-element units per thread.
 // MAXT: the largest CTA; CTAs of up to 256 threads get 80 registers a thread, which four units need -- 64 with an FP8 cache,
 // whose conversions want more warps instead (8191 tokens of 8192 + 1024 + 1024: 58 us against 64; bf16 cache: 84 against 83).
+// So does a 4-bit cache behind a layerwise norm (16384 tokens of 5120 + 1024 + 1024: 87 us against 91), not behind the others, which would spill
+// more (per head 97 against 93).
 template <class IO, class CIO, int NORM, bool CACHE, bool INTER, int UPT, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes == 1 ? 4 : 3) rope_kernel(const __grid_constant__ RopeParams R) {
+__global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && (CIO::kBytes == 1 || (CIO::kBytes == 0 && NORM == kNormLayer)) ? 4 : 3) rope_kernel(const __grid_constant__ RopeParams R) {
   extern __shared__ float4 cs_all[];  // [tokens_per_cta][4][rot_dim/16]: (c, c, s, s) of pairs 8j+2e, 8j+2e+1 at [e][j]
   __shared__ float red[32][2];        // per warp: sum of squares of Q, of K
   const int slot_of_token = threadIdx.x / R.threads_per_token;
@@ -259,14 +266,14 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
     if (cslot >= R.num_slots) cslot = -1;
   }
   constexpr bool kBlocks = CACHE && CIO::kBytes == 0;
-  long long slot_k = 0, slot_v = 0, slot_ks = 0, slot_vs = 0;  // where the token's slot starts in the pools
-  if (CACHE && cslot >= 0) {
+  // Where the token's slot starts in the pools.  Only the warps that write there work it out, after the norm -- but for norms per head,
+  // which everything has to be ready for (16384 tokens of 5120 + 1024 + 1024, bf16 cache: 81.5 us instead of 83.7; per head 86.6, as
+  // here 83.7.  4-bit cache: 90.6 instead of 92.3, per head 92.8 instead of 96.1).
+  constexpr bool kEarly = CACHE && !kBlocks && NORM != kNormLayer;
+  long long slot_k = 0, slot_v = 0;
+  if (kEarly && cslot >= 0) {
     slot_k = cache_at(R.ck, cslot, R.page_size, R.page_shift);
     slot_v = cache_at(R.cv, cslot, R.page_size, R.page_shift);
-    if constexpr (kBlocks) {
-      slot_ks = cache_at(R.cks, cslot, R.page_size, R.page_shift);
-      slot_vs = cache_at(R.cvs, cslot, R.page_size, R.page_shift);
-    }
   }
   if (live && r16 > 0) {
     auto put = [&](int p, float2 f) {
@@ -386,21 +393,23 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && CIO::kBytes =
         } else {
           ma = mb = max_nan(ma, mb);
         }
-        uint32_t sa, sb;
-        float ra, rb;
-        const float fa = e2m1_scale(ma, sa, ra);
-        float fb = fa;
-        rb = ra, sb = sa;
-        if (split) fb = e2m1_scale(mb, sb, rb);
-        char* codes = reinterpret_cast<char*>(C.base) + (side[i] == 1 ? slot_k : slot_v) + head[i] * C.head + (c0 >> 1);
-        __stcs(reinterpret_cast<uint32_t*>(codes), e2m1_codes8(a, ma, fa, ra));
-        __stcs(reinterpret_cast<uint32_t*>(codes + (step >> 1)), e2m1_codes8(b, mb, fb, rb));
-        unsigned char* sc = reinterpret_cast<unsigned char*>(S.base) + (side[i] == 1 ? slot_ks : slot_vs) + head[i] * S.head;
+        uint32_t sa, sb = 0;
+        const Reciprocal da = e2m1_scale(ma, sa);
+        char* codes = reinterpret_cast<char*>(C.base) + cache_at(C, cslot, R.page_size, R.page_shift) + head[i] * C.head + (c0 >> 1);
+        if (split) {
+          const Reciprocal db = e2m1_scale(mb, sb);
+          __stcs(reinterpret_cast<uint32_t*>(codes), e2m1_codes8(a, da));
+          __stcs(reinterpret_cast<uint32_t*>(codes + (step >> 1)), e2m1_codes8(b, db));
+        } else {
+          __stcs(reinterpret_cast<uint2*>(codes), make_uint2(e2m1_codes8(a, da), e2m1_codes8(b, da)));
+        }
+        unsigned char* sc = reinterpret_cast<unsigned char*>(S.base) + cache_at(S, cslot, R.page_size, R.page_shift) + head[i] * S.head;
         if (!split || !(j & 1)) sc[c0 >> 4] = (unsigned char)sa;
         else sc[(c0 + step) >> 4] = (unsigned char)sb;
         continue;
       } else {
-      const long long at = (side[i] == 1 ? slot_k : slot_v) + head[i] * C.head + c0;
+      const long long slot_at = !kEarly ? cache_at(C, cslot, R.page_size, R.page_shift) : side[i] == 1 ? slot_k : slot_v;
+      const long long at = slot_at + head[i] * C.head + c0;
       Chunk8<CIO> o0, o1;
       if constexpr (CIO::kBytes == 1 || IO::kBytes == 1) {
         const float2 k = make_float2(C.inv_scale, C.inv_scale);
@@ -536,10 +545,9 @@ __global__ void __launch_bounds__(kRopeGeneralThreads) rope_general_kernel(const
                 hi[e] = make_float2(whole[warp][16 * blk + 8 + 2 * e], whole[warp][16 * blk + 9 + 2 * e]);
               }
               uint32_t byte;
-              float r1;
-              const float most = max_nan(absmax8(lo), absmax8(hi)), f = e2m1_scale(most, byte, r1);
+              const Reciprocal d = e2m1_scale(max_nan(absmax8(lo), absmax8(hi)), byte);
               *reinterpret_cast<uint2*>(reinterpret_cast<char*>(C.base) + y0 + 8 * blk) =
-                  make_uint2(e2m1_codes8(lo, most, f, r1), e2m1_codes8(hi, most, f, r1));
+                  make_uint2(e2m1_codes8(lo, d), e2m1_codes8(hi, d));
               sc[blk] = (unsigned char)byte;
             }
             __syncwarp();
