@@ -872,10 +872,11 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
   if ((int64_t)max_q > T) max_q = (int)T;
   const int64_t rows = (int64_t)max_q * group;
   p.cols = (int)((max_keys + kE2m1Page - 1) / kE2m1Page);
-  p.side_bytes = (int64_t)seqs * p.cols * kE2m1Page * heads_kv * head_dim * 2;
+  const __int128 wide = (__int128)seqs * p.cols * kE2m1Page * heads_kv * head_dim * 4;  // sizes that a call may have go beyond 64 bits
   const AttnPlan tc = plan_attn(seqs, T, max_q, max_keys, heads_q, heads_kv, head_dim, causal, window, sms);
-  if (rows > kE2m1WidenRows && tc.tc && 2 * p.side_bytes <= kE2m1WidenMost) {
+  if (rows > kE2m1WidenRows && tc.tc && wide <= kE2m1WidenMost) {
     p.widen = true;
+    p.side_bytes = (int64_t)(wide / 2);
     p.table_bytes = ((int64_t)seqs * p.cols * 4 + 15) / 16 * 16;
     p.rest = attn_workspace(tc, head_dim);
     p.need = 2 * p.side_bytes + p.table_bytes + p.rest + 16;  // 16: the widened cache starts at a multiple of 32 bytes, which its stores take at a time
