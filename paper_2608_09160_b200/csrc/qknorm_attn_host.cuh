@@ -1077,7 +1077,10 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
                     out, ld_out, lse, (char*)W.table + plan.table_bytes, plan.rest, stream, cache->v_scale);
   }
 
-  if (cache->num_pages == 0) P.k.base = P.v.base = E.ks.base = E.vs.base = q;  // never read, but an address that copies of no bytes can name
+  if (cache->num_pages == 0) {  // never read, but copies of no bytes name an address, too, and one that their size divides
+    const AttnSide none = {(const void*)((uintptr_t)q & ~(uintptr_t)15), 0, 0, 0};
+    P.k = P.v = E.ks = E.vs = none;
+  }
   E.row_tiles = plan.row_tiles;
   E.tile_rows = 8 * plan.nt;
   const int blocks = hd / 16, low = blocks & -blocks;
