@@ -747,6 +747,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   P.out = (uint16_t*)out;
   P.k = AttnSide{cache->k, cache->k_page, cache->k_token, cache->k_head};
   P.v = AttnSide{cache->v, cache->v_page, cache->v_token, cache->v_head};
+  if (cache->num_pages == 0) P.k = P.v = AttnSide{(const void*)((uintptr_t)q & ~(uintptr_t)15), 0, 0, 0};  // never read, but copies of no bytes name it
   P.num_pages = cache->num_pages;
   P.page_size = cache->page_size;
   P.page_shift = log2_or_minus_one(cache->page_size);
