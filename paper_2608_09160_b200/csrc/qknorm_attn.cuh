@@ -453,7 +453,8 @@ __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __gri
 typedef void (*AttnKernel)(const AttnParams);
 // in qknorm_attn_inst.cu and qknorm_attn_tc_inst.cu
 typedef void (*AttnTcKernel)(const AttnParams, const AttnMaps);
-AttnKernel attn_general_kernel_for(bool e4m3);
+enum AttnFormat { kAttnBf16, kAttnE4m3, kAttnF16Cache };  // how a cache's elements are stored; the last: a 4-bit one, widened
+AttnKernel attn_general_kernel_for(AttnFormat format);
 AttnKernel attn_join_kernel_for();
 // forms of the tensor-core kernel: two query tiles per item, one, one of at most 32 rows
 constexpr int kAttnTwo = 0, kAttnOne = 1, kAttnQuad = 2;

@@ -139,17 +139,14 @@ __global__ void __launch_bounds__(kE2m1WidenThreads) e2m1_widen_kernel(const __g
       if (i >= kE2m1Page * blocks) break;
 #pragma unroll
       for (int side = 0; side < 2; ++side) {
-        uint32_t f[4], sc, none, y[8];
-        e4m3x4_to_f16x2(byte[a][side], sc, none);
-        const float scale = __half2float(__ushort_as_half((unsigned short)(sc & 0xffffu)));
+        uint32_t y[8], twice, none;  // the block's scale in both halves
+        e4m3x4_to_f16x2(byte[a][side] * 0x101u, twice, none);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
+          uint32_t f[4];
           e2m1x8_to_f16x2(half ? w[a][side].y : w[a][side].x, f);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 v = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&f[k])), make_float2(scale, scale));
-            y[4 * half + k] = bf_pack(v.x, v.y);
-          }
+          for (int k = 0; k < 4; ++k) y[4 * half + k] = hmul2(f[k], twice);
         }
         // rows lie one after the other; 32 bytes at a time, a whole sector
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"((side ? W.v : W.k) + to + 16ll * i), "r"(y[0]), "r"(y[1]), "r"(y[2]),

@@ -504,9 +504,10 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
 
 // ---- attention over the paged cache ---------------------------------------------------------------
 
-AttnTcKernel attn_tc_for(int dp, bool e4m3, int form, bool tma, int* smem) {
-  if (dp == 64) return e4m3 ? attn_tc_kernel_e4m364(form, tma, smem) : attn_tc_kernel_bf1664(form, tma, smem);
-  return e4m3 ? attn_tc_kernel_e4m3128(form, tma, smem) : attn_tc_kernel_bf16128(form, tma, smem);
+AttnTcKernel attn_tc_for(int dp, AttnFormat format, int form, bool tma, int* smem) {
+  if (format == kAttnE4m3) return dp == 64 ? attn_tc_kernel_e4m364(form, tma, smem) : attn_tc_kernel_e4m3128(form, tma, smem);
+  if (format == kAttnF16Cache) return dp == 64 ? attn_tc_kernel_f1664(form, tma, smem) : attn_tc_kernel_f16128(form, tma, smem);
+  return dp == 64 ? attn_tc_kernel_bf1664(form, tma, smem) : attn_tc_kernel_bf16128(form, tma, smem);
 }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -679,11 +680,11 @@ int run_attn_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, i
   return QKNORM_OK;
 }
 
-// v_scale: what V of a bf16 cache is multiplied by (an FP8 one has its own).
+// widened: `cache` says bf16, but holds fp16, a 4-bit cache's codes times their scales, and V is multiplied by v_scale (an FP8 cache has its own).
 int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* table, int32_t table_cols, int64_t ld_table,
              const int32_t* kv_lens, const int32_t* q_starts, int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q,
              float scale, int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* ws, int64_t ws_bytes,
-             cudaStream_t stream, float v_scale = 1.0f) {
+             cudaStream_t stream, bool widened = false, float v_scale = 1.0f) {
   CacheFacts f;
   int rc = check_cache(cache, &f);
   if (rc != QKNORM_OK) return rc;
@@ -706,6 +707,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   const DeviceInfo* dev = nullptr;
   rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
+  const AttnFormat format = widened ? kAttnF16Cache : cache->e4m3 ? kAttnE4m3 : kAttnBf16;
   AttnPlan plan = plan_attn(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, causal != 0, window, dev->sm_count);
   const bool aligned = (((uintptr_t)q) | ((uintptr_t)out) | ((uintptr_t)P.ld_q * 2) | ((uintptr_t)P.ld_out * 2)) % 16 == 0 && f.vec16 &&
                        (!cache->e4m3 || cache->head_dim % 16 == 0);
@@ -784,7 +786,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   }
 
   if (!plan.tc) {
-    AttnKernel gen = attn_general_kernel_for(cache->e4m3 != 0);
+    AttnKernel gen = attn_general_kernel_for(format);
     int bres = 1;
     rc = resident_blocks((const void*)gen, kAttnGeneralThreads, 0, &bres);
     if (rc != QKNORM_OK) return rc;
@@ -818,7 +820,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
     P.box_rows = rows;
     while ((1 << P.box_shift) < rows) ++P.box_shift;
   }
-  AttnTcKernel fn = attn_tc_for(dp, cache->e4m3 != 0, plan.form, tma, &smem);
+  AttnTcKernel fn = attn_tc_for(dp, format, plan.form, tma, &smem);
   rc = allow_dynamic_smem((const void*)fn, smem);
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);
@@ -1075,7 +1077,7 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
     wide.head_dim = hd;
     const float s = fmaxf((float)((double)scale * cache->k_scale), 1.401298464e-45f);
     return run_attn(q, ld_q, &wide, W.table, plan.cols, 0, kv_lens, q_starts, seqs, T, max_q, (int)P.max_keys, heads_q, s, causal, window,
-                    out, ld_out, lse, (char*)W.table + plan.table_bytes, plan.rest, stream, cache->v_scale);
+                    out, ld_out, lse, (char*)W.table + plan.table_bytes, plan.rest, stream, true, cache->v_scale);
   }
 
   if (cache->num_pages == 0) {  // never read, but copies of no bytes name an address, too, and one that their size divides

@@ -158,6 +158,14 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {  // exact when
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// fp16: a 4-bit cache that has been widened.
+struct IoF16 {
+  static constexpr int kBytes = 2;
+  static __device__ __forceinline__ float load(const void* base, long long i) {
+    return __half2float(__ushort_as_half(reinterpret_cast<const unsigned short*>(base)[i]));
+  }
+};
+
 struct IoE4m3 {
   static constexpr int kBytes = 1;
   static constexpr int kGammaVecs = 2;   // 16 elements per chunk need 32 bytes of bf16 gamma

@@ -56,3 +56,92 @@ def test_an_empty_pool_beside_queries_at_odd_addresses(libqknorm, copies, hq, hk
     some = seen > 0
     assert (out == 0).all() and torch.isneginf(lse[~some.cuda()]).all()
     assert ((lse.cpu().double() - torch.log(seen.clamp(min=1))[:, None]).abs()[some] < 1e-5).all()
+
+
+def weights_in_fp16(b, variant="attn_tc", **kw):
+    """The call's rows within the bounds that weights in fp16 have."""
+    ref = b.reference(**{k: v for k, v in kw.items() if k in ("scale", "causal", "window", "max_kv")})
+    out, lse = b.call(**kw)
+    assert binding.last_variant() == variant
+    b.compare(out, lse, ref, True)
+    return out, lse
+
+
+@pytest.mark.parametrize("hq,hk,hd,new,kv", [
+    (5, 1, 128, [60, 3, 26], [60, 200, 27]), (8, 2, 64, [26, 17, 33], [300, 17, 129]), (3, 1, 96, [100, 1, 0], [256, 300, 9]), (1, 1, 128, [300], [300]),
+    (2, 2, 16, [120], [500]), (128, 1, 64, [2, 1], [130, 140]), (4, 2, 80, [80, 130], [80, 130]), (1, 1, 128, [101], [9000]), (6, 2, 64, [40, 1], [40, 20000]),
+])
+def test_weights_do_not_get_coarser_with_more_rows(libqknorm, hq, hk, hd, new, kv):
+    """Short rows among them, where a weight's rounding shows: 2^-9 of a value that others nearly cancel."""
+    weights_in_fp16(Batch(new, kv, hq, hk, hd, seed=31 + hd))
+
+
+@pytest.mark.parametrize("window", [1, 31, 100])
+@pytest.mark.parametrize("causal", [True, False])
+def test_weights_of_windowed_chunks(libqknorm, causal, window):
+    weights_in_fp16(Batch([80, 1, 53], [400, 257, 90], 4, 2, 128, seed=window), causal=causal, window=window)
+
+
+def test_a_row_is_rounded_the_same_beside_a_chunk(libqknorm):
+    """Two decode rows alone, and in a batch with a chunk: both within the bounds of fp16 weights."""
+    weights_in_fp16(Batch([1, 1], [5, 40], 8, 2, 128, seed=33), "attn_e2m1")
+    weights_in_fp16(Batch([1, 1, 64], [5, 40, 64], 8, 2, 128, seed=33))
+
+
+def test_extreme_queries_of_a_chunk(libqknorm):
+    b = Batch([60, 60], [64, 64], 4, 2, 128, seed=34)
+    for row, e in ((0, 10), (3, 14), (5, -100), (9, -112), (11, -120), (20, -130), (21, -126), (60, 9), (61, -133)):
+        b.q[row] = (b.q[row].double() * 2.0 ** e).to(BF16)
+    b.q[30] = 0
+    b.q[31, 5], b.q[32, 7] = float("nan"), float("inf")
+    b.dq = b.q.cuda()
+    keep = [r for r in range(120) if r not in (31, 32)]
+    for scale in (2.0 ** -3, 1e-38, 2.0 ** 100):       # the last: rows so small that without it every score would be 0
+        if scale > 1:
+            big = torch.ones(b.T, dtype=torch.bool)
+            big[[5, 9, 11, 20, 21, 61]] = False
+            b.q[big] = 0
+            b.dq = b.q.cuda()
+            keep = list(range(120))
+        ref = b.reference(scale=scale)
+        out, lse = b.call(scale=scale)
+        assert binding.last_variant() == "attn_tc"
+        got, z = out.double().numpy().reshape(b.T, 4, 128), lse.double().numpy()
+        tol, tol_lse = R.attention_bounds(ref, 128, True)
+        for r in keep:
+            assert (np.abs(got[r] - ref["out"][r]) <= tol[r]).all() and (np.abs(z[r] - ref["lse"][r]) <= tol_lse[r]).all(), (scale, r)
+        if scale < 1:
+            assert np.isnan(got[31, 0]).all() and np.isnan(got[32, 0]).all()     # of the head that has them; the others
+            for r in (31, 32):
+                assert (np.abs(got[r, 1:] - ref["out"][r, 1:]) <= tol[r, 1:]).all()
+
+
+def test_small_weights_of_a_chunk_are_kept(libqknorm):
+    """One key far above the rest of a long row: 30000 others share 2^-20 of its weight each."""
+    b = Batch([100], [30000], 1, 1, 64, seed=35)
+    b.k[:], b.ks.view(torch.uint8)[:] = 0, 0x38
+    b.k[b.table[0][0], 0, 0, 0] = 0x04
+    b.q[:] = 0
+    b.q[:100, 0] = 20 * np.log(2) / (2 * 0.25) * 8.0
+    b.dq = b.q.cuda()
+    b.place()
+    weights_in_fp16(b)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_a_chunk_does_not_see_do_not_matter(libqknorm, hd):
+    """NaN in blocks of K and V that only the later rows of a chunk see."""
+    b = Batch([120], [200], 2, 1, hd, seed=36)
+    for pool, key, blk in ((b.vs, 150, hd // 16 - 1), (b.ks, 180, 0)):        # seen from rows 70 and 100 on
+        pool.view(torch.uint8)[b.table[0][key // 16], key % 16, 0, blk] = 0xFF
+    b.place()
+    out, lse = b.call()
+    assert binding.last_variant() == "attn_tc"
+    ref = b.reference()
+    got = out.double().numpy().reshape(b.T, 2, hd)
+    tol, _ = R.attention_bounds(ref, hd, True)
+    for r in range(100):
+        first = 0 if r < 70 else hd - 16
+        assert (np.abs(got[r] - ref["out"][r]) <= tol[r])[:, :hd if r < 70 else first].all(), r
+        assert r < 70 or np.isnan(got[r][:, hd - 16:]).all()
+    assert np.isnan(got[100:120]).all()
