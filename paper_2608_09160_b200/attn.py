@@ -236,7 +236,7 @@ def _cache(k_cache, v_cache, k_scale: float, v_scale: float, dev: int):
                     f"shape on cuda:{dev}, with unit stride in head_dim")
 
 
-_U8, _F4 = torch.uint8, torch.float4_e2m1fn_x2
+_U8, _F4 = torch.uint8, getattr(torch, "float4_e2m1fn_x2", None)  # a torch without the type has no tensors of it
 
 
 def _cache_e2m1(k_cache, v_cache, k_scales, v_scales, k_scale: float, v_scale: float, dev: int):

@@ -2,6 +2,8 @@
 import ctypes
 import math
 import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -242,3 +244,12 @@ def test_how_a_page_lies():
     assert f(t[:, :1, :, ::2, :, :8], 2) is None                                 # three axes of pieces
     assert f(torch.zeros((5, 7), dtype=torch.uint8), 0) == (7, 1, 1, 0, 0, 7)
     assert f(torch.zeros((5, 1, 1)), 0) == (4, 1, 1, 0, 0, 4)
+
+
+def test_a_torch_without_a_4_bit_type_will_do():
+    """Everything but tensors of that type works there: bf16 and FP8 calls need no more than before."""
+    code = ("import torch\n"
+            "del torch.float4_e2m1fn_x2\n"
+            "from paper_2608_09160_b200 import attn, pages\n"
+            "assert attn._F4 is None\n")
+    subprocess.run([sys.executable, "-c", code], cwd=ROOT, check=True)
