@@ -240,12 +240,12 @@ int qknorm_fwd_append_e2m1(const void* q, const void* k, const void* v, const vo
 
 /*
  * qknorm_attn_paged_e2m1 -- qknorm_attn_paged over a 4-bit cache: the same arguments, the same rows, keys, masks and refusals.
- * k_scale and v_scale are taken as they stand.  Queries are brought to fp16 with a power of two taken out of each row (exact but for parts
- * below 2^-30 of the row's largest element); K and V widen exactly; scores, maxima, sums and the output are fp32; the
- * weights are rounded to fp16 (2^-11 relative, at least 2^-32 of the row's largest weight).  All of this is so whichever kernel runs.
+ * k_scale and v_scale are taken as they stand.  K and V widen exactly; scores, maxima, sums and the output are fp32; the
+ * weights are rounded to fp16 (2^-11 relative, at least 2^-32 of the row's largest weight), whichever kernel runs.  "attn_e2m1" brings queries to fp16
+ * with a power of two taken out of each row (exact but for parts below 2^-30 of the row's largest element).
  *
  * Kernels: "attn_e2m1" (mma.sync out of registers) for up to 96 rows (new tokens times query heads) per sequence and key head; for more the
- * visible part of the cache is widened once into the workspace, to fp16, and "attn_tc" reads that -- where head_dim is at most 128
+ * visible part of the cache is widened once into the workspace, K to bf16 and V to fp16, and "attn_tc" reads that -- where head_dim is at most 128
  * and the widened cache, 4 bytes an element of max_kv keys of every sequence (with a window, too), at most 2 GB.  A wait
  * inside "attn_e2m1" that runs out after a second sets the device's error word to 10.
  */

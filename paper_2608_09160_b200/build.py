@@ -57,9 +57,9 @@ def _units() -> List[Tuple[str, str, List[str]]]:
     units.append(("qknorm_pages.o", os.path.join(CSRC, "qknorm_pages_inst.cu"), []))
     units.append(("qknorm_attn.o", os.path.join(CSRC, "qknorm_attn_inst.cu"), []))
     for dp in PADDED_HEAD_DIMS:
-        for io, tag in (("IoBf16", "bf16"), ("IoE4m3", "e4m3"), ("IoF16", "f16")):
+        for kio, vio, tag in (("IoBf16", "IoBf16", "bf16"), ("IoE4m3", "IoE4m3", "e4m3"), ("IoBf16", "IoF16", "wide")):
             units.append((f"qknorm_attn_tc_{tag}_d{dp}.o", os.path.join(CSRC, "qknorm_attn_tc_inst.cu"),
-                          [f"-DQKNORM_DP={dp}", f"-DQKNORM_CIO={io}", f"-DQKNORM_IO_TAG={tag}"]))
+                          [f"-DQKNORM_DP={dp}", f"-DQKNORM_KIO={kio}", f"-DQKNORM_VIO={vio}", f"-DQKNORM_IO_TAG={tag}"]))
     for dp in PADDED_HEAD_DIMS_E2M1:
         units.append((f"qknorm_attn_e2m1_d{dp}.o", os.path.join(CSRC, "qknorm_attn_e2m1_inst.cu"), [f"-DQKNORM_DP={dp}"]))
     return units

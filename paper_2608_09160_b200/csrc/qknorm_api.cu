@@ -83,8 +83,8 @@ WarpKernel warp_kernel_for(int l, bool exact, int elem_bytes) {
 // per (cache format, padded head_dim), defined in qknorm_attn_tc_inst.cu (one translation unit each)
 AttnTcKernel attn_tc_kernel_bf1664(int form, bool tma, int* smem_bytes);
 AttnTcKernel attn_tc_kernel_bf16128(int form, bool tma, int* smem_bytes);
-AttnTcKernel attn_tc_kernel_f1664(int form, bool tma, int* smem_bytes);
-AttnTcKernel attn_tc_kernel_f16128(int form, bool tma, int* smem_bytes);
+AttnTcKernel attn_tc_kernel_wide64(int form, bool tma, int* smem_bytes);
+AttnTcKernel attn_tc_kernel_wide128(int form, bool tma, int* smem_bytes);
 AttnTcKernel attn_tc_kernel_e4m364(int form, bool tma, int* smem_bytes);
 AttnTcKernel attn_tc_kernel_e4m3128(int form, bool tma, int* smem_bytes);
 

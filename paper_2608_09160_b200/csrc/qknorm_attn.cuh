@@ -132,7 +132,7 @@ __device__ __forceinline__ void attn_moving(const AttnParams& P, uint32_t deadli
 // One warp, one row and head, keys [lo, hi): o (normalised; lane holds elements lane + 32 e) and z = c m + log2 l.
 // Reads nothing of a key outside the range, so what other keys hold cannot matter.
 // EPL: elements per lane, at least head_dim / 32.  deadline: the word of attn_moving, or 0.
-template <class CIO, int EPL>
+template <class KIO, class VIO, int EPL>
 __device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long row, int head, int lo, int hi, float (&o)[EPL],
                                          float& z_out, uint32_t deadline = 0) {
   const int lane = threadIdx.x & 31, D = P.head_dim;
@@ -156,7 +156,7 @@ __device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long r
 #pragma unroll
       for (int e = 0; e < EPL; ++e) {
         const int d = lane + 32 * e;
-        if (d < D) s = fmaf(q[e], CIO::load(P.k.base, ka + d), s);
+        if (d < D) s = fmaf(q[e], KIO::load(P.k.base, ka + d), s);
       }
     }
 #pragma unroll
@@ -169,7 +169,7 @@ __device__ __forceinline__ void attn_row(const AttnParams& P, int b, long long r
 #pragma unroll
     for (int e = 0; e < EPL; ++e) {
       const int d = lane + 32 * e;
-      if (d < D) o[e] = fmaf(o[e], f, p * (page >= 0 ? CIO::load(P.v.base, va + d) : 0.f));
+      if (d < D) o[e] = fmaf(o[e], f, p * (page >= 0 ? VIO::load(P.v.base, va + d) : 0.f));
     }
     m = mn;
   }
@@ -185,7 +185,7 @@ constexpr float kLn2 = 0.693147180559945309f;
 // a warp a dependent round trip, where the other kernel takes 128 of them at once.
 constexpr int kAttnGeneralThreads = 128;
 
-template <class CIO>
+template <class KIO, class VIO>
 __global__ void __launch_bounds__(kAttnGeneralThreads) attn_general_kernel(const __grid_constant__ AttnParams P) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kAttnGeneralThreads) attn_general_kernel(const
     if (i >= s.n) continue;
     const long long row = s.row0 + (long long)i;
     float o[kAttnMaxEpl], z;
-    attn_row<CIO, kAttnMaxEpl>(P, b, row, head, attn_lo(P, s, i), attn_hi(P, s, i), o, z);
+    attn_row<KIO, VIO, kAttnMaxEpl>(P, b, row, head, attn_lo(P, s, i), attn_hi(P, s, i), o, z);
 #pragma unroll
     for (int e = 0; e < kAttnMaxEpl; ++e) {
       const int d = lane + 32 * e;
@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __gri
 typedef void (*AttnKernel)(const AttnParams);
 // in qknorm_attn_inst.cu and qknorm_attn_tc_inst.cu
 typedef void (*AttnTcKernel)(const AttnParams, const AttnMaps);
-enum AttnFormat { kAttnBf16, kAttnE4m3, kAttnF16Cache };  // how a cache's elements are stored; the last: a 4-bit one, widened
+enum AttnFormat { kAttnBf16, kAttnE4m3, kAttnWidened };  // how a cache's elements are stored; the last: a 4-bit one, as K in bf16 and V in fp16
 AttnKernel attn_general_kernel_for(AttnFormat format);
 AttnKernel attn_join_kernel_for();
 // forms of the tensor-core kernel: two query tiles per item, one, one of at most 32 rows

@@ -928,7 +928,8 @@ E2m1Launch attn_e2m1_kernel_128(int nt, int copy, bool wide);
 E2m1Launch attn_e2m1_kernel_256(int nt, int copy, bool wide);
 AttnE2m1JoinKernel attn_e2m1_join_kernel_for();
 
-// The visible part of a 4-bit cache as fp16 -- exact, the product of a code and a scale has six significant bits, and is 2^-10 at least and 2688 at most -- in pages of
+// The visible part of a 4-bit cache, K as bf16 and V as fp16 -- exact, the product of a code and a scale has six significant bits, and is 2^-10 at least and
+// 2688 at most -- in pages of
 // kE2m1Page tokens, heads one after the other in a page, the sequences' pages in a row: what "attn_tc" reads fastest.
 constexpr int kE2m1Page = 128, kE2m1WidenThreads = 256;
 struct WidenParams {

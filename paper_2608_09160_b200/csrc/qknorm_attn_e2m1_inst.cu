@@ -146,7 +146,13 @@ __global__ void __launch_bounds__(kE2m1WidenThreads) e2m1_widen_kernel(const __g
           uint32_t f[4];
           e2m1x8_to_f16x2(half ? w[a][side].y : w[a][side].x, f);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) y[4 * half + k] = hmul2(f[k], twice);
+          for (int k = 0; k < 4; ++k) {
+            y[4 * half + k] = hmul2(f[k], twice);
+            if (side == 0) {
+              const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&y[4 * half + k]));
+              y[4 * half + k] = bf_pack(v.x, v.y);
+            }
+          }
         }
         // rows lie one after the other; 32 bytes at a time, a whole sector
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"((side ? W.v : W.k) + to + 16ll * i), "r"(y[0]), "r"(y[1]), "r"(y[2]),

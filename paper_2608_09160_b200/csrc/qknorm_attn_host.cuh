@@ -506,7 +506,7 @@ int run_append(const void* q, const void* k, const void* v, const void* gq, cons
 
 AttnTcKernel attn_tc_for(int dp, AttnFormat format, int form, bool tma, int* smem) {
   if (format == kAttnE4m3) return dp == 64 ? attn_tc_kernel_e4m364(form, tma, smem) : attn_tc_kernel_e4m3128(form, tma, smem);
-  if (format == kAttnF16Cache) return dp == 64 ? attn_tc_kernel_f1664(form, tma, smem) : attn_tc_kernel_f16128(form, tma, smem);
+  if (format == kAttnWidened) return dp == 64 ? attn_tc_kernel_wide64(form, tma, smem) : attn_tc_kernel_wide128(form, tma, smem);
   return dp == 64 ? attn_tc_kernel_bf1664(form, tma, smem) : attn_tc_kernel_bf16128(form, tma, smem);
 }
 
@@ -680,7 +680,7 @@ int run_attn_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, i
   return QKNORM_OK;
 }
 
-// widened: `cache` says bf16, but holds fp16, a 4-bit cache's codes times their scales, and V is multiplied by v_scale (an FP8 cache has its own).
+// widened: a 4-bit cache's codes times their scales, V in fp16, though `cache` says bf16; V is multiplied by v_scale (an FP8 cache has its own).
 int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* table, int32_t table_cols, int64_t ld_table,
              const int32_t* kv_lens, const int32_t* q_starts, int32_t seqs, int64_t T, int32_t max_q, int32_t max_kv, int32_t heads_q,
              float scale, int32_t causal, int32_t window, void* out, int64_t ld_out, float* lse, void* ws, int64_t ws_bytes,
@@ -707,7 +707,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   const DeviceInfo* dev = nullptr;
   rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
-  const AttnFormat format = widened ? kAttnF16Cache : cache->e4m3 ? kAttnE4m3 : kAttnBf16;
+  const AttnFormat format = widened ? kAttnWidened : cache->e4m3 ? kAttnE4m3 : kAttnBf16;
   AttnPlan plan = plan_attn(seqs, T, max_q, max_kv, heads_q, cache->heads, cache->head_dim, causal != 0, window, dev->sm_count);
   const bool aligned = (((uintptr_t)q) | ((uintptr_t)out) | ((uintptr_t)P.ld_q * 2) | ((uintptr_t)P.ld_out * 2)) % 16 == 0 && f.vec16 &&
                        (!cache->e4m3 || cache->head_dim % 16 == 0);

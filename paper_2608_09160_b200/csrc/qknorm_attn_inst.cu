@@ -56,7 +56,8 @@ __global__ void __launch_bounds__(kAttnJoinThreads) attn_join_kernel(const __gri
 }
 
 AttnKernel attn_general_kernel_for(AttnFormat format) {
-  return format == kAttnE4m3 ? attn_general_kernel<IoE4m3> : format == kAttnF16Cache ? attn_general_kernel<IoF16> : attn_general_kernel<IoBf16>;
+  return format == kAttnE4m3 ? attn_general_kernel<IoE4m3, IoE4m3>
+                             : format == kAttnWidened ? attn_general_kernel<IoBf16, IoF16> : attn_general_kernel<IoBf16, IoBf16>;
 }
 AttnKernel attn_join_kernel_for() { return attn_join_kernel; }
 

@@ -38,9 +38,10 @@
 //
 // FP8 cache: K and V are staged raw and widened to fp16, which holds every E4M3 value exactly; Q is
 // brought to fp16 with a power of two per row, which loses nothing but parts below 2^-30 of the row's largest element.
-// fp16 cache (a 4-bit one, widened beforehand, qknorm_attn_e2m1.cuh): tiles as in a bf16 one, Q as with an FP8 one.
+// A 4-bit cache, widened beforehand (qknorm_attn_e2m1.cuh), comes as K in bf16 and V in fp16, both exact: so the first product takes Q as it
+// is, and the second one has weights in fp16.  (K in fp16, too, with Q brought to it by warp 14, 24 us a tile: a prompt of 8192 1160 us, 40 / 8 heads; so 735.)
 //
-// Rounding: P is rounded for the second product, to bf16 (2^-8 relative) or, with an FP8 or fp16 cache, to fp16 (2^-11 relative, and
+// Rounding: P is rounded for the second product, to bf16 (2^-8 relative) or, with an FP8 or a widened cache, to fp16 (2^-11 relative, and
 // 2^-25 absolute below 2^-14; the sum l takes them unrounded).  So P stands for 2^7 times the weights there: what the maximum may lag
 // behind still fits, and a weight keeps half a step of 2^-32 of the largest one instead of 2^-25.  (With weights as they are, a key that
 // outweighs its row's others by 2^26 left them out of O and in l.)  Otherwise only the output is rounded; sums, maxima and O are fp32.
@@ -56,15 +57,11 @@
 //                         675 us (765 at 1740 MHz), floor 410; over an FP8 cache 1215, for the widening
 // Tiles of 128 x 128: the largest M of one CTA's products, and two score tiles and two O of 128 columns fill the 512 columns of TMEM.
 #pragma once
+#include <type_traits>
+
 #include "qknorm_attn.cuh"
 
 namespace qknorm {
-
-// Caches whose products are of fp16, and those of bf16.
-template <class CIO>
-inline constexpr bool kAttnF16 = true;
-template <>
-inline constexpr bool kAttnF16<IoBf16> = false;
 
 namespace tc {
 
@@ -205,7 +202,7 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, ui
 }  // namespace tc
 
 // Shared memory, byte offsets from a 1024-byte aligned base.
-template <int DP, class CIO>
+template <int DP, bool F8>
 struct AttnSmem {
   static constexpr int kTile = kAttnTile * DP * 2;  // a 16-bit tile of Q, K or V
   static constexpr int kRaw = kAttnTile * DP;       // an FP8 tile: 32 rows at a time land in the upper half of the place that
@@ -227,26 +224,26 @@ struct AttnSmem {
   static constexpr int kMlFree = kMl + 8;
   static constexpr int kDrain = kMlFree + 8;
   static constexpr int kRawFull = kDrain + 8;         // per stage: an FP8 tile, or a 16-bit V tile that wants looking at, is there
-  static constexpr int kQRaw = kRawFull + 8 * kStages;  // [2] products in fp16: a bf16 Q tile is there
+  static constexpr int kQRaw = kRawFull + 8 * kStages;  // [2] FP8 cache: a bf16 Q tile is there
   static constexpr int kTurn = kQRaw + 16;            // [2] two forms: whose turn it is to issue
   static constexpr int kPass = kTurn + 16;            // the softmax warps' steps through the join of an item
   static constexpr int kTmem = kPass + 8;             // TMEM base address
   static constexpr int kAbort = kTmem + 4;            // a wait ran out: everybody leaves
   static constexpr int kDeadline = kAbort + 4;        // see attn_moving
   static constexpr int kPoison = kDeadline + 8;       // [4] 1 + number of an item that holds a V row to be careful with
-  // Products in fp16: [4][128] bytes, the exponent taken out of a Q row (0: none).  Four sets, because a set is read until the
+  // FP8 cache: [4][128] bytes, the exponent taken out of a Q row (0: none).  Four sets, because a set is read until the
   // item's last score tile is done with, which can be after its Q buffer has been given to a later item; a set comes
   // round again only after the tensor warp has seen the scores of the item before last consumed.
   static constexpr int kQScale = kPoison + 16;
-  static constexpr int kItemSlots = kAttnF16<CIO> ? 2 : 4;              // items ahead of the slowest reader
-  static constexpr int kItems = kQScale + (kAttnF16<CIO> ? 512 : 0);    // [kItemSlots][16] ints, see put_item
+  static constexpr int kItemSlots = F8 ? 2 : 4;              // items ahead of the slowest reader
+  static constexpr int kItems = kQScale + (F8 ? 512 : 0);    // [kItemSlots][16] ints, see put_item
   static constexpr int kItemFull = kItems + 64 * kItemSlots;
   static constexpr int kItemEmpty = kItemFull + 8 * kItemSlots;
   static constexpr int kMlRows = kItemEmpty + 8 * kItemSlots;             // [8 softmax warps][32] float2, one-tile forms: (m, l) of their parts
   static constexpr int kBytes = kMlRows + 2048;
 };
 
-static_assert(AttnSmem<128, IoBf16>::kBytes <= 232448 && AttnSmem<128, IoE4m3>::kBytes <= 232448, "shared memory of one CTA");
+static_assert(AttnSmem<128, false>::kBytes <= 232448 && AttnSmem<128, true>::kBytes <= 232448, "shared memory of one CTA");
 
 // Key tiles [a, b) that query tile w of the item uses, and how its rows' ranges spread.
 struct AttnTileRange {
@@ -277,11 +274,11 @@ __device__ __forceinline__ bool attn_cut(const AttnItem& it, const AttnTileRange
   return j >= r.a && j < r.b && ((k1 < it.uhi ? k1 : it.uhi) > r.hi_min || (k0 > it.ulo ? k0 : it.ulo) < r.lo_max);
 }
 
-template <int DP, class CIO, int FORM, bool TMA>
+template <int DP, class KIO, class VIO, int FORM, bool TMA>
 struct AttnTc {
-  using L = AttnSmem<DP, CIO>;
-  static constexpr bool F8 = CIO::kBytes == 1;      // tiles are staged raw and widened
-  static constexpr bool F16 = kAttnF16<CIO>;        // the products are of fp16: Q has to be brought to it
+  static constexpr bool F8 = KIO::kBytes == 1;                      // tiles are staged raw and widened, Q is brought to fp16
+  static constexpr bool F16 = !std::is_same<VIO, IoBf16>::value;    // V and the weights are fp16
+  using L = AttnSmem<DP, F8>;
   static constexpr bool ONE = FORM != kAttnTwo;
   static constexpr bool QUAD = FORM == kAttnQuad;
   // Tiles of 64 columns: rows of 128 bytes, 16-byte pieces swizzled within 8 rows.  Q: its 64-column halves one after the
@@ -487,7 +484,7 @@ struct AttnTc {
   static constexpr int kRowsAt = 32 / kChunks;           // rows a warp handles in one step
   __device__ __forceinline__ static int row_of(int tid, int step) { return (tid & ~31) + step * kRowsAt + (tid & 31) / kChunks; }
 
-  // Looks through the rows [from, to) of a 16-bit tile for infinities and NaN; blanks the others if asked to.
+  // Looks through the rows [from, to) of a 16-bit V tile for infinities and NaN; blanks the others if asked to.
   __device__ __forceinline__ bool inspect(uint32_t tile_at, int tid, int from, int to, bool blank, bool look) const {
     const int c = tid % kChunks;
     bool bad = false;
@@ -713,7 +710,7 @@ struct AttnTc {
       const int tok = (int)((unsigned)r / (unsigned)P.group), g = r - tok * P.group;
       return from + tok * P.ld_q + g * P.head_dim;
     };
-    if constexpr (!F16) {  // asynchronous: every row is on its way before the first is waited for
+    if constexpr (!F8) {  // asynchronous: every row is on its way before the first is waited for
       for (int r = r0; r < end; r += kStep) {
         const bool take = in_head && r < rows;
 #pragma unroll
@@ -740,9 +737,8 @@ struct AttnTc {
     }
   }
 
-  // Products in fp16: 8 elements of Q row r (the row's other pieces are in the neighbouring lanes) from bf16 to fp16, the row's largest
-  // exponent brought to 2^8.  FP8 cache: rows of zeros, tiny rows and rows with infinities or NaN as they are.  fp16 cache: every row,
-  // a tiny one by at most 2^119 and one with an infinity or NaN as if its finite elements were the largest, as attn_e2m1_kernel takes them.
+  // FP8 cache: 8 elements of Q row r (the row's other pieces are in the neighbouring lanes) from bf16 to fp16, the row's largest
+  // exponent brought to 2^8; rows of zeros, tiny rows and rows with infinities or NaN as they are.
   __device__ __forceinline__ void q_to_f16(uint4& v, int r, int c, int scale_set) const {
     uint32_t u[4] = {v.x, v.y, v.z, v.w};
     uint32_t mag = 0;  // largest magnitude of the row, as bf16 bits
@@ -753,9 +749,8 @@ struct AttnTc {
     }
 #pragma unroll
     for (int off = DP / 16; off > 0; off >>= 1) mag = max(mag, __shfl_xor_sync(0xffffffffu, mag, off));
-    int e = (int)(mag >> 7);
-    if (!F8) e = e < 16 ? 16 : e > 254 ? 254 : e;
-    const bool scaled = !F8 || (e > 16 && e < 255);
+    const int e = (int)(mag >> 7);
+    const bool scaled = e > 16 && e < 255;
     const float f = scaled ? __uint_as_float((uint32_t)(127 + 135 - e) << 23) : 1.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) u[k] = tc::pack_f16(bf_lo(u[k]) * f, bf_hi(u[k]) * f);
@@ -808,8 +803,8 @@ struct AttnTc {
         if constexpr (TMA) {
           // the tile's tokens and heads as one box per 64 columns (QUAD: four times, unless they are written again anyway); tokens of
           // other sequences that come along stand in rows nobody looks at
-          constexpr int kCopies = QUAD && !F16 ? 4 : 1;
-          const uint32_t bar = F16 ? smem + L::kQRaw + 8 * w : q_full;
+          constexpr int kCopies = QUAD && !F8 ? 4 : 1;
+          const uint32_t bar = F8 ? smem + L::kQRaw + 8 * w : q_full;
           if (tid == 0) {
             ptx::mbar_arrive_expect_tx(bar, (DP / 64) * kCopies * P.q_box_tokens * P.group * 128);
 #pragma unroll
@@ -818,14 +813,14 @@ struct AttnTc {
               for (int h = 0; h < DP / 64; ++h)
                 tc::tma3(smem + L::kQ0 + w * L::kTile + h * kHalf + k * 32 * 128, &maps.q, h * 64, it.kvh * P.group, it.s.row0 + tok0, bar);
           }
-          if constexpr (F16) {
+          if constexpr (F8) {
             if (!__all_sync(all, wait(bar, (qph >> w) & 1))) return drain_q(qph, w);
             convert_q(tid, r.rows, w, set);
             signal(q_full, tid);
           }
         } else {
           load_q(tid, it, tok0, r.rows, w, set);
-          if (!F16) tc::cp_wait_all();
+          if (!F8) tc::cp_wait_all();
           signal(q_full, tid);
         }
         qph ^= 1u << w;
@@ -841,14 +836,14 @@ struct AttnTc {
   // whose newest copy is not counted in it yet.
   __device__ __forceinline__ void drain_q(uint32_t qph, int open) const {
     for (int w = 0; w < 2; ++w) {
-      const uint32_t bar = smem + (F16 ? L::kQRaw : L::kQFull) + 8 * w;
+      const uint32_t bar = smem + (F8 ? L::kQRaw : L::kQFull) + 8 * w;
       wait_drain(bar, w == open ? (qph >> w) & 1 : ((qph >> w) & 1) ^ 1);
     }
   }
 
   // ---- tensor-core issue ----------------------------------------------------------------------------
   __device__ __forceinline__ void issue_qk(uint32_t tmem, int w, int qbuf, uint32_t pos) const {
-    constexpr uint32_t idesc = tc::instr_desc(kAttnTile, F16, false);
+    constexpr uint32_t idesc = tc::instr_desc(kAttnTile, F8, false);
     const uint32_t q = tc::desc_lo(smem + L::kQ0 + qbuf * L::kTile, 16), k = tc::desc_lo(stage(pos), 16);
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {  // 16 columns of head_dim: 32 bytes inside the 128-byte swizzle span
@@ -971,10 +966,9 @@ struct AttnTc {
     }
   }
 
-  // c of this row's scores: with products in fp16 the Q rows had an exponent taken out.  Positive and finite
+  // c of this row's scores: an FP8 cache's Q rows had an exponent taken out
   __device__ __forceinline__ float row_c(int set, int row) const {
     const int e = reinterpret_cast<const volatile unsigned char*>(smem_ptr + L::kQScale)[set * 128 + row];
-    if (!F8) return fminf(fmaxf(ldexpf(P.c, e - 135), kAttnLeastC), 3.4e38f);
     return e == 0 ? P.c : fmaxf(ldexpf(P.c, e - 135), kAttnLeastC);
   }
 
@@ -1048,7 +1042,7 @@ struct AttnTc {
       lo = lo > it.j0 * kAttnTile ? lo : it.j0 * kAttnTile;
       hi = hi < it.j1 * kAttnTile ? hi : it.j1 * kAttnTile;
       float o[DP / 32], z;
-      attn_row<CIO, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z, smem + L::kDeadline);
+      attn_row<KIO, VIO, DP / 32>(P, it.b, to.row, to.head, lo, hi, o, z, smem + L::kDeadline);
 #pragma unroll
       for (int e = 0; e < DP / 32; ++e) {
         const int d = lane + 32 * e;
@@ -1176,7 +1170,7 @@ struct AttnTc {
             sph ^= 1;
             if (busy) {
               tc::fence_after();
-              if (F16) c = row_c(ONE ? count & 3 : w + 2 * oph, wtid);
+              if (F8) c = row_c(ONE ? count & 3 : w + 2 * oph, wtid);
               const int k0 = j * kAttnTile;
               tile(tmem + lanes + w * kAttnTile, tmem + lanes + 2 * kAttnTile + w * DP, lo - k0, hi - k0,
                    k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l, smem + L::kPMost + 8 * w);
@@ -1265,7 +1259,7 @@ struct AttnTc {
         }
         tc::fence_after();
         const bool again = poison()[count & 3] == count + 1;
-        if (F16) c = row_c(count & 3, wtid);
+        if (F8) c = row_c(count & 3, wtid);
         // a part without keys counts nothing; one that met only NaN scores makes the row NaN
         float lt = 0.f;
 #pragma unroll
@@ -1367,12 +1361,12 @@ struct AttnTc {
   }
 };
 
-template <int DP, class CIO, int FORM, bool TMA>
+template <int DP, class KIO, class VIO, int FORM, bool TMA>
 __global__ void __launch_bounds__(kAttnTcThreads, 1) attn_tc_kernel(const __grid_constant__ AttnParams P,
                                                                     const __grid_constant__ AttnMaps maps) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  using K = AttnTc<DP, CIO, FORM, TMA>;
-  using L = AttnSmem<DP, CIO>;
+  using K = AttnTc<DP, KIO, VIO, FORM, TMA>;
+  using L = typename K::L;
   const uint32_t smem = ptx::smem_u32(smem_raw);
   const int warp = threadIdx.x >> 5;
   if (smem & 1023u) {  // the swizzle counts on it; no other shared memory is declared, so this does not happen

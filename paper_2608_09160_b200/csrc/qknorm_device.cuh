@@ -158,7 +158,7 @@ __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {  // exact when
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// fp16: a 4-bit cache that has been widened.
+// fp16: V of a 4-bit cache that has been widened.
 struct IoF16 {
   static constexpr int kBytes = 2;
   static __device__ __forceinline__ float load(const void* base, long long i) {
