@@ -245,8 +245,9 @@ int qknorm_fwd_append_e2m1(const void* q, const void* k, const void* v, const vo
  * with a power of two taken out of each row (exact but for parts below 2^-30 of the row's largest element).
  *
  * Kernels: "attn_e2m1" (mma.sync out of registers) for up to 96 rows (new tokens times query heads) per sequence and key head; for more the
- * visible part of the cache is widened once into the workspace, K to bf16 and V to fp16, and "attn_tc" reads that -- where head_dim is at most 128
- * and the widened cache, 4 bytes an element of max_kv keys of every sequence (with a window, too), at most 2 GB.  A wait
+ * visible part of the cache is widened once into the workspace, K to bf16 and V to fp16, and "attn_tc" reads that -- where rows of q and out
+ * are 16-byte aligned, head_dim is at most 128 and the widened cache, 4 bytes an element of max_kv keys of every sequence (with a window, too),
+ * at most 2 GB.  A wait
  * inside "attn_e2m1" that runs out after a second sets the device's error word to 10.
  */
 int qknorm_attn_paged_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* cache, const int32_t* block_table,

@@ -868,8 +868,9 @@ E2m1Launch e2m1_kernel(int head_dim, int nt, int copy, bool wide) {
   return head_dim <= 64 ? attn_e2m1_kernel_64(nt, copy, wide) : head_dim <= 128 ? attn_e2m1_kernel_128(nt, copy, wide) : attn_e2m1_kernel_256(nt, copy, wide);
 }
 
-int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, bool causal, int window, int sms,
-              E2m1Plan* out) {
+// aligned: rows of q and out are, as "attn_tc" wants them.  Rows that are not would be left to the row-at-a-time kernel behind a widened cache.
+int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int heads_kv, int head_dim, bool causal, int window, bool aligned,
+              int sms, E2m1Plan* out) {
   E2m1Plan p;
   const int group = heads_q / heads_kv;
   if ((int64_t)max_q > T) max_q = (int)T;
@@ -877,7 +878,10 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
   p.cols = (int)((max_keys + kE2m1Page - 1) / kE2m1Page);
   const __int128 wide = (__int128)seqs * p.cols * kE2m1Page * heads_kv * head_dim * 4;  // sizes that a call may have go beyond 64 bits
   const AttnPlan tc = plan_attn(seqs, T, max_q, max_keys, heads_q, heads_kv, head_dim, causal, window, sms);
-  if (rows > kE2m1WidenRows && tc.tc && wide <= kE2m1WidenMost) {
+  p.nt = rows <= 8 ? 1 : 2;
+  const int64_t row_tiles = (rows + 8 * p.nt - 1) / (8 * p.nt);
+  const bool countable = rows <= 0x7fffffff && row_tiles <= 0x3fffffff / seqs && row_tiles * seqs * heads_kv <= 0x7fffffff;
+  if (rows > kE2m1WidenRows && tc.tc && wide <= kE2m1WidenMost && (aligned || !countable)) {
     p.widen = true;
     p.side_bytes = (int64_t)(wide / 2);
     p.table_bytes = ((int64_t)seqs * p.cols * 4 + 15) / 16 * 16;
@@ -886,16 +890,13 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
     *out = p;
     return QKNORM_OK;
   }
-  if (rows > 0x7fffffff) return QKNORM_ERR_SHAPE;
-  p.nt = rows <= 8 ? 1 : 2;
-  const int64_t row_tiles = (rows + 8 * p.nt - 1) / (8 * p.nt);
+  if (!countable) return QKNORM_ERR_SHAPE;
   int64_t span = max_keys;
   if (window > 0) {  // the first row's window, and what the later ones see behind it
     const int64_t w = (int64_t)window + (causal ? max_q : T) - 1;
     if (w < span) span = w;
     span += kE2m1Tile - 1;  // units start at a multiple of a tile
   }
-  if (row_tiles > 0x3fffffff / seqs) return QKNORM_ERR_SHAPE;
   p.row_tiles = (int)row_tiles;
   const int tma = env_int("QKNORM_E2M1_TMA", -1);  // 0, 1: for tests
   for (int k = 0; k < 2; ++k) {
@@ -910,7 +911,6 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
     const int round = kE2m1Tile * kernel.warps / w.heads;
     const int64_t places = (int64_t)sms * kernel.per_sm, rounds = (span + round - 1) / round;
     const int64_t units = row_tiles * seqs * (heads_kv / w.heads);
-    if (units > 0x7fffffff) return QKNORM_ERR_SHAPE;
     w.shares = rounds > kE2m1Whole;
     w.grid = (int)(!w.shares || units * rounds < places ? (w.shares ? units * rounds : units) : places);
     if (k == 1) p.tma = tma < 0 ? w.heads >= 4 && units * rounds >= 8 * places : tma != 0;
@@ -960,12 +960,13 @@ int run_attn_e2m1_workspace(int32_t seqs, int64_t T, int32_t max_q, int32_t max_
   const DeviceInfo* dev = nullptr;
   rc = current_device(&dev);
   if (rc != QKNORM_OK) return rc;
-  for (const bool causal : {true, false}) {  // enough for either
-    E2m1Plan p;
-    rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, causal, window, dev->sm_count, &p);
-    if (rc != QKNORM_OK) return rc;
-    if (p.need > *bytes) *bytes = p.need;
-  }
+  for (const bool causal : {true, false})  // enough for either, and wherever q and out lie
+    for (const bool aligned : {true, false}) {
+      E2m1Plan p;
+      rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, heads_kv, head_dim, causal, window, aligned, dev->sm_count, &p);
+      if (rc != QKNORM_OK) return rc;
+      if (p.need > *bytes) *bytes = p.need;
+    }
   return QKNORM_OK;
 }
 
@@ -999,7 +1000,9 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   P.max_keys = (int64_t)table_cols * cache->page_size < max_kv ? (int64_t)table_cols * cache->page_size : max_kv;
   // the plan goes by max_kv, which the workspace was asked for with
   E2m1Plan plan;
-  rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, cache->heads, hd, causal != 0, window, dev->sm_count, &plan);
+  E.q_vec = ((uintptr_t)q | (uintptr_t)P.ld_q * 2) % 16 == 0;
+  E.out_vec = ((uintptr_t)out | (uintptr_t)P.ld_out * 2) % 16 == 0;
+  rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, cache->heads, hd, causal != 0, window, E.q_vec && E.out_vec, dev->sm_count, &plan);
   if (rc != QKNORM_OK) return rc;
   const int64_t need = plan.need;
   CallRegions r;
@@ -1088,8 +1091,6 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   E.tile_rows = 8 * plan.nt;
   const int blocks = hd / 16, low = blocks & -blocks;
   E.scale_unit = low > 8 ? 8 : low;
-  E.q_vec = ((uintptr_t)q | (uintptr_t)P.ld_q * 2) % 16 == 0;
-  E.out_vec = ((uintptr_t)out | (uintptr_t)P.ld_out * 2) % 16 == 0;
   if (plan.parts > 0) {
     E.cuts = (int*)ws;
     E.part_o = (float*)((char*)ws + plan.cut_bytes);

@@ -145,3 +145,31 @@ def test_values_a_chunk_does_not_see_do_not_matter(libqknorm, hd):
         assert (np.abs(got[r] - ref["out"][r]) <= tol[r])[:, :hd if r < 70 else first].all(), r
         assert r < 70 or np.isnan(got[r][:, hd - 16:]).all()
     assert np.isnan(got[100:120]).all()
+
+
+@pytest.mark.parametrize("which", ["q", "out", "ld_q", "ld_out"])
+@pytest.mark.parametrize("hq,hk,hd,new,kv", [(8, 2, 128, [60, 1], [300, 77]), (3, 1, 64, [200, 40], [700, 2000]), (5, 1, 96, [30], [30])])
+def test_chunks_at_odd_addresses(libqknorm, copies, hq, hk, hd, new, kv, which):
+    """More than 96 rows whose q or out "attn_tc" cannot take: row tiles, not a row at a time over a widened cache."""
+    b = Batch(new, kv, hq, hk, hd, seed=51)
+    ref = b.reference()
+    n, at = hq * hd, {"q": 1, "out": 1}.get(which, 0)
+    gap = 8 if at else 3
+    q, out = b.dq, torch.full_like(b.dq, 7.0)
+    around = torch.full((b.T, n + gap), 7.0, dtype=BF16, device="cuda")
+    if which in ("q", "ld_q"):
+        around[:, at:at + n] = q
+        q = around[:, at:at + n]
+    else:
+        out = around[:, at:at + n]
+    lse = torch.full((b.T, hq), 7.0, device="cuda")
+    need = attn.attn_paged_e2m1_workspace(len(new), b.T, max(new), max(kv), hq, hk, hd)
+    ws = torch.full((need + 32,), 77, dtype=torch.uint8, device="cuda")
+    attn.qknorm_attn_paged_e2m1(q, *b.pools, b.dtable, b.dlens, b.dstarts, max(new), max(kv), k_scale=b.unit[0], v_scale=b.unit[1], out=out, lse=lse,
+                                workspace=ws[:need])
+    torch.cuda.synchronize()
+    assert binding.last_variant() == "attn_e2m1" and binding.device_error_word() == 0
+    b.compare(out.cpu(), lse.cpu(), ref, True)
+    assert (ws[need:] == 77).all()
+    if which in ("out", "ld_out"):
+        assert (around[:, :at] == 7.0).all() and (around[:, at + n:] == 7.0).all()
