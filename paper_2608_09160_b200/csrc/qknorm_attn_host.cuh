@@ -646,6 +646,9 @@ AttnPlan plan_attn(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q
   return p;
 }
 
+// Can the kernel count the call's items in 32 bits?
+bool attn_countable(const AttnPlan& p, int seqs, int heads_kv) { return (int64_t)p.q_items * seqs <= 0x3fffffff && (int64_t)seqs * heads_kv <= 0x3fffffff; }
+
 // starts, then parts' rows, then their log-sums
 int64_t attn_starts_bytes(const AttnPlan& p) { return p.cuts ? (int64_t)p.grid * 32 : 0; }
 int64_t attn_parts(const AttnPlan& p) { return p.cuts ? (int64_t)p.grid * 2 * p.part_rows : 0; }
@@ -825,7 +828,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
   if (rc != QKNORM_OK) return rc;
   rc = attn_tc_registers_ok((const void*)fn);
   if (rc != QKNORM_OK) return rc;
-  if ((int64_t)plan.q_items * seqs > 0x3fffffff || (int64_t)seqs * cache->heads > 0x3fffffff) return QKNORM_ERR_SHAPE;
+  if (!attn_countable(plan, seqs, cache->heads)) return QKNORM_ERR_SHAPE;
   cudaError_t e = launch_overlapped(fn, (unsigned)plan.grid, (unsigned)kAttnTcThreads, (size_t)smem, stream, P, maps);
   if (e != cudaSuccess) return set_cuda_error(e);
   rc = finish_launch("attn_tc");
@@ -840,6 +843,7 @@ int run_attn(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const
 // How a call over a 4-bit cache is cut: sizes only, so that the workspace can be asked for beforehand.
 struct E2m1Plan {
   bool widen = false;
+  bool refused = false;  // widen: by "attn_tc", which has to be known before the first launch
   // TMA, where the layout allows it: for whole heads' copies of several heads, and long shares.  us, single tokens of 8 query heads a key
   // head, TMA with 8 (4, 2) heads a copy | cp.async: 64 x 8192 keys 102 | 123, 16 x 32000 keys 97 (102, 106) | 109, 256 x 500 keys 53 | 59, but
   // 64 x 1000 keys 33 | 31, 16 x 2000 keys 27 | 21, 4 x 8192 keys 43 | 23; 2 key heads, 32 x 4000 keys 45 | 32.
@@ -883,6 +887,7 @@ int plan_e2m1(int seqs, int64_t T, int max_q, int64_t max_keys, int heads_q, int
   const bool countable = rows <= 0x7fffffff && row_tiles <= 0x3fffffff / seqs && row_tiles * seqs * heads_kv <= 0x7fffffff;
   if (rows > kE2m1WidenRows && tc.tc && wide <= kE2m1WidenMost && (aligned || !countable)) {
     p.widen = true;
+    p.refused = aligned && !attn_countable(tc, seqs, heads_kv);
     p.side_bytes = (int64_t)(wide / 2);
     p.table_bytes = ((int64_t)seqs * p.cols * 4 + 15) / 16 * 16;
     p.rest = attn_workspace(tc, head_dim);
@@ -1004,6 +1009,7 @@ int run_attn_e2m1(const void* q, int64_t ld_q, const qknorm_paged_cache_e2m1* ca
   E.out_vec = ((uintptr_t)out | (uintptr_t)P.ld_out * 2) % 16 == 0;
   rc = plan_e2m1(seqs, T, max_q, max_kv, heads_q, cache->heads, hd, causal != 0, window, E.q_vec && E.out_vec, dev->sm_count, &plan);
   if (rc != QKNORM_OK) return rc;
+  if (plan.refused) return QKNORM_ERR_SHAPE;
   const int64_t need = plan.need;
   CallRegions r;
   r.own[r.outs] = -1;

@@ -173,3 +173,14 @@ def test_chunks_at_odd_addresses(libqknorm, copies, hq, hk, hd, new, kv, which):
     assert (ws[need:] == 77).all()
     if which in ("out", "ld_out"):
         assert (around[:, :at] == 7.0).all() and (around[:, at + n:] == 7.0).all()
+
+
+def test_what_the_second_kernel_refuses_is_refused_before_the_first(libqknorm):
+    """More items than "attn_tc" can count: told before the cache is widened."""
+    lib, seqs, new = attn.lib(), 2 ** 16, 2 ** 16
+    need = attn.attn_paged_e2m1_workspace(seqs, new, new, 16, 128, 1, 64)
+    assert need > 2 ** 31
+    before = lib.qknorm_launch_count()
+    assert attend(lib, cache(pages_=8, heads=1, hd=64), q=0x100000000, out=0x200000000, seqs=seqs, T=new, max_q=new, max_kv=16, cols=1, hq=128,
+                  ws=0x300000000, wsb=need) == binding.QKNORM_ERR_SHAPE
+    assert lib.qknorm_launch_count() == before
