@@ -184,3 +184,26 @@ def test_what_the_second_kernel_refuses_is_refused_before_the_first(libqknorm):
     assert attend(lib, cache(pages_=8, heads=1, hd=64), q=0x100000000, out=0x200000000, seqs=seqs, T=new, max_q=new, max_kv=16, cols=1, hq=128,
                   ws=0x300000000, wsb=need) == binding.QKNORM_ERR_SHAPE
     assert lib.qknorm_launch_count() == before
+
+
+@pytest.mark.parametrize("hq,hk,hd", [(8, 8, 128), (16, 8, 64), (8, 4, 128), (64, 4, 128), (12, 4, 64), (4, 1, 128)])
+@pytest.mark.parametrize("page", [16, 64])
+def test_shares_of_several_stretches_of_pages(libqknorm, copies, page, hq, hk, hd):
+    """Shares of more rounds than pages are looked up for at a time: 160 sequences over the same 20000 keys, the last of them of other lengths.
+    (Keys of a round: 32 for 8 / hk heads' warps; pages in runs of 16 or 32 tokens, 256 at a time.)"""
+    S, lens = 160, [20000, 19999, 15003, 17]
+    b = Batch([1], [20000], hq, hk, hd, page=page, seed=41)
+    g = torch.Generator().manual_seed(42)
+    q = torch.randn((4, hq * hd), generator=g).to(BF16)
+    ref = R.attention(R.widen(q), E.widen(b.k, b.ks), E.widen(b.v, b.vs), b.table * 4, lens, [0, 1, 2, 3, 4], hq, scale=hd ** -0.5, k_scale=b.unit[0],
+                      v_scale=b.unit[1])
+    tol, tol_lse = R.attention_bounds(ref, hd, True)
+    which = torch.tensor([i % 3 if i < S - 8 else i % 4 for i in range(S)])
+    out, lse = torch.full((S, hq * hd), 7.0, dtype=BF16, device="cuda"), torch.full((S, hq), 7.0, device="cuda")
+    attn.qknorm_attn_paged_e2m1(q[which].cuda(), *b.pools, b.dtable.expand(S, -1).contiguous(), torch.tensor(lens, dtype=torch.int32)[which].cuda(),
+                                torch.arange(S + 1, dtype=torch.int32, device="cuda"), 1, 20000, k_scale=b.unit[0], v_scale=b.unit[1], out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert binding.device_error_word() == 0 and binding.last_variant() == "attn_e2m1"
+    got, z = out.cpu().double().numpy().reshape(S, hq, hd), lse.cpu().double().numpy()
+    for r, n in enumerate(which.tolist()):
+        assert (np.abs(got[r] - ref["out"][n]) <= tol[n]).all() and (np.abs(z[r] - ref["lse"][n]) <= tol_lse[n]).all(), r
