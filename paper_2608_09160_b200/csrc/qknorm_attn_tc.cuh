@@ -1059,8 +1059,8 @@ struct AttnTc {
   // Columns [from, to) of the tile are keys that the row sees.
   // Not QUAD: the first 96 keys' weights are announced while the last 32 are computed, which takes about as long as the products
   // of the 96.  (8192 tokens: 726 us; announced after 64, when the products wait in their turn, 755.)
-  __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& m,
-                                       float& l, uint32_t p_most) const {
+  __device__ __forceinline__ void tile(uint32_t s_addr, uint32_t o_addr, int from, int to, bool masked, bool first, float c, float& cw,
+                                       float& m, float& l, uint32_t p_most) const {
     // The first half stays in registers from the maximum to the exponentials; the second is read again when the first is half
     // done, so that a thread never holds more than 128 scores and nothing else.
     constexpr int N = QUAD ? kAttnTile / 4 : kAttnTile / 2;
@@ -1091,7 +1091,7 @@ struct AttnTc {
     }
     const float mn = tc::max3(tc::max3(mx[0], mx[1], mx[2]), tc::max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
     // m is the maximum that the exponents are taken against; it follows the true one when that is 2^8 ahead
-    const bool grow = mn > m && (m == kNegInf || (mn - m) * c > 8.f);
+    const bool grow = mn > m && (m == kNegInf || (mn - m) * cw > 8.f);
     if (__any_sync(0xffffffffu, grow)) {
       const float f = !grow ? 1.f : m == kNegInf ? 0.f : tc::ex2((m - mn) * c);
       if (grow) {
@@ -1099,9 +1099,13 @@ struct AttnTc {
         m = mn;
       }
       if (!first) rescale(o_addr, f);
+      // A weight is 2^(cw s - mc).  What the rounding of mc adds is common to a row's weights: harmless up to scores of 2^22, where it is 2^-2 at
+      // most.  Larger ones are brought there: neighbouring fp32 scores, which is as well as they are known, are still 2^-2 apart then.
+      const float far = m == kNegInf ? 0.f : fabsf(m) * c;
+      cw = far > 0x1p22f ? c * __fdividef(4.f, far * 0x1p-20f) : c;
     }
-    const float mc = m == kNegInf ? 0.f : m * c - kUp;
-    const float2 c2 = make_float2(c, c), mc2 = make_float2(-mc, -mc);
+    const float mc = m == kNegInf ? 0.f : m * cw - kUp;
+    const float2 c2 = make_float2(cw, cw), mc2 = make_float2(-mc, -mc);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     auto weights = [&](const float* x, int col) {  // 32 columns from `col`
       uint32_t p[16];
@@ -1151,7 +1155,7 @@ struct AttnTc {
     // The item stays in shared memory and is read again at its end: registers are for the scores.
     for (uint32_t n_item = 0;; ++n_item) {
       if (!__all_sync(all, item_wait(n_item))) return;
-      float m = kNegInf, l = 0.f, c = P.c;
+      float m = kNegInf, l = 0.f, c = P.c, cw = P.c;
       {
         AttnItem it;
         get_item(n_item, it);
@@ -1173,7 +1177,7 @@ struct AttnTc {
               if (F8) c = row_c(ONE ? count & 3 : w + 2 * oph, wtid);
               const int k0 = j * kAttnTile;
               tile(tmem + lanes + w * kAttnTile, tmem + lanes + 2 * kAttnTile + w * DP, lo - k0, hi - k0,
-                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, m, l, smem + L::kPMost + 8 * w);
+                   k0 < plain_from || k0 + kAttnTile > plain_to, j == j_first, c, cw, m, l, smem + L::kPMost + 8 * w);
             }
             __syncwarp();
             if (lane == 0) {

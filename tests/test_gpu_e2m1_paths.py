@@ -207,3 +207,31 @@ def test_shares_of_several_stretches_of_pages(libqknorm, copies, page, hq, hk, h
     got, z = out.cpu().double().numpy().reshape(S, hq, hd), lse.cpu().double().numpy()
     for r, n in enumerate(which.tolist()):
         assert (np.abs(got[r] - ref["out"][n]) <= tol[n]).all() and (np.abs(z[r] - ref["lse"][n]) <= tol_lse[n]).all(), r
+
+
+@pytest.mark.parametrize("e", [20, 30, 60, 100, 112])
+@pytest.mark.parametrize("new,variant", [([1, 2], "attn_e2m1"), ([60, 30], "attn_tc")])
+def test_scores_of_any_size(libqknorm, copies, new, variant, e):
+    """Queries of 2^e: where the largest score is ahead of the next by more than fp32 sums of D products are off, the result is its key's value."""
+    hd = 128
+    b = Batch(new, [500, 300], 4, 2, hd, seed=61)
+    b.q = (b.q.double() * 2.0 ** e).to(BF16)
+    b.dq = b.q.cuda()
+    ref = b.reference()
+    out, lse = b.call()
+    assert binding.last_variant() == variant
+    b.compare(out, lse, ref, True)                        # no NaN, and lse
+    k, v = (E.widen(c, s).numpy() * u for c, s, u in zip((b.k, b.v), (b.ks, b.vs), b.unit))
+    q, got, clear = R.widen(b.q).numpy().reshape(b.T, 4, hd), out.double().numpy().reshape(b.T, 4, hd), 0
+    for s, L in enumerate(b.kv):
+        kk, vv = (x[b.table[s][:-(-L // b.page)]].reshape(-1, 2, hd) for x in (k, v))
+        for r in range(b.starts[s], b.starts[s + 1]):
+            seen = L - (b.starts[s + 1] - r) + 1
+            for h in range(4):
+                score = kk[:seen, h // 2] @ q[r, h] * hd ** -0.5
+                top = int(score.argmax())
+                second = np.delete(score, top).max()
+                if score[top] - second > 2 * (hd + 4) * 2.0 ** -24 * ref["S"][r, h] + 30:
+                    clear += 1
+                    assert (np.abs(got[r, h] - vv[top, h // 2]) <= 2.0 ** -7 * np.abs(vv[top, h // 2]) + 1e-6).all(), (r, h)
+    assert clear > 0
