@@ -86,9 +86,8 @@ def _pieces(shape: Tuple[int, ...], stride: Tuple[int, ...], item: int, page_dim
 
 
 def _pools(pools, page_dim: int, dev: int, num_pages: int = -1):
-    """The pools as the C ABI takes them: (structs, how many, pages)."""
-    if isinstance(pools, torch.Tensor):
-        pools = (pools,)
+    """The pools as the C ABI takes them: (structs, how many, pages), and the tensors themselves, to be kept as long as the call is."""
+    pools = (pools,) if isinstance(pools, torch.Tensor) else tuple(pools)
     packed = []
     for t in pools:
         if not isinstance(t, torch.Tensor) or t.get_device() != dev or not -t.dim() <= page_dim < t.dim():
@@ -102,7 +101,7 @@ def _pools(pools, page_dim: int, dev: int, num_pages: int = -1):
         if how is None:
             _refuse(_SHAPE, f"pools: a page of {tuple(t.shape)} with strides {t.stride()} is more than two axes of contiguous pieces")
         packed.append(_POOL.pack(t.data_ptr(), *how))
-    return b"".join(packed), len(packed), num_pages
+    return b"".join(packed), len(packed), num_pages, pools
 
 
 def _books(refs, block_table, lens, dev: int):
@@ -149,7 +148,7 @@ def qknorm_pages_copy(pools, src, dst, *, page_dim: int = 0, stream=None) -> Non
     """qknorm_pages_copy: page src[i] to page dst[i] in every pool; src, dst int32 [n].  Pairs outside the pool copy nothing."""
     L = lib()
     dev = _device()
-    packed, k, n = _pools(pools, page_dim, dev)
+    packed, k, n, pools = _pools(pools, page_dim, dev)
     psrc, pdst = _list(src, "src", dev), _list(dst, "dst", dev)
     if src.shape != dst.shape:
         _refuse(_SHAPE, f"src, dst: {src.shape[0]} and {dst.shape[0]} pages")
@@ -166,7 +165,7 @@ def qknorm_pages_fork(pools, refs, block_table, lens, parents, children, page_si
     L = lib()
     dev = _device()
     N, prefs, ptable, cols, ld, plens, rows = _books(refs, block_table, lens, dev)
-    packed, k, _ = _pools(pools, page_dim, dev, N)
+    packed, k, _, pools = _pools(pools, page_dim, dev, N)
     pp, pc = _list(parents, "parents", dev), _list(children, "children", dev)
     n = parents.shape[0]
     if children.shape[0] != n:
@@ -195,7 +194,7 @@ def qknorm_pages_compact(pools, refs, block_table, lens, page_size: int, *, page
     L = lib()
     dev = _device()
     N, prefs, ptable, cols, ld, plens, R = _books(refs, block_table, lens, dev)
-    packed, k, _ = _pools(pools, page_dim, dev, N)
+    packed, k, _, pools = _pools(pools, page_dim, dev, N)
     if live is None:
         live = _empty((1,), torch.int32, refs.device, stream)
     plive = _flat(live, (1,), torch.int32, "live", dev)
