@@ -244,7 +244,7 @@ int qknorm_fwd_append_e2m1(const void* q, const void* k, const void* v, const vo
  * weights are rounded to fp16 (2^-11 relative, at least 2^-32 of the row's largest weight), whichever kernel runs.  "attn_e2m1" brings queries to fp16
  * with a power of two taken out of each row (exact but for parts below 2^-30 of the row's largest element).
  *
- * Kernels: "attn_e2m1" (mma.sync out of registers) for up to 96 rows (new tokens times query heads) per sequence and key head; for more the
+ * Kernels: "attn_e2m1" (mma.sync out of registers) for up to 96 rows (max_q times the query heads of a key head) per sequence; for more the
  * visible part of the cache is widened once into the workspace, K to bf16 and V to fp16, and "attn_tc" reads that -- where rows of q and out
  * are 16-byte aligned, head_dim is at most 128 and the widened cache, 4 bytes an element of max_kv keys of every sequence (with a window, too),
  * at most 2 GB.  A wait

@@ -863,8 +863,8 @@ struct E2m1Plan {
   int64_t need = 0;
 };
 
-// Rows of a sequence and key head from which widening pays: 16 sequences of 4096 keys, 8 key heads, 60 rows 74 us against 112 widened, 85 rows
-// about 105 against 114; 4 sequences of 8192 keys with 2560 rows 1074 against 245.
+// Rows of a sequence and key head from which widening pays: 16 sequences of 4096 keys, 8 key heads, 60 rows 76 us against 112 widened, 95 rows
+// 97, 100 rows widened 105; 4 sequences of 8192 keys with 2560 rows 1074 against 252.
 constexpr int kE2m1WidenRows = 96;
 constexpr int64_t kE2m1WidenMost = (int64_t)2 << 30;    // bytes of the widened cache
 

@@ -54,7 +54,7 @@
 //   few short sequences   latency: about 5 us until the first product, then a tile each 0.9 us: 8 x 1000 keys: 17.1 us, floor 3.3
 //   chunks and prompts    exponentials and products of two tiles in turn, 3700 cycles a pair of 128 x 128 (products alone 2048,
 //                         exponentials alone as many), and 8 to 10 thousand cycles a unit for its first and last steps: 8192 tokens, 40 heads:
-//                         675 us (765 at 1740 MHz), floor 410; over an FP8 cache 1215, for the widening
+//                         682 to 700 us (780 at 1740 MHz), floor 410; over an FP8 cache 1215, 868 if the queries need not be brought to fp16
 // Tiles of 128 x 128: the largest M of one CTA's products, and two score tiles and two O of 128 columns fill the 512 columns of TMEM.
 #pragma once
 #include <type_traits>

@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(MAXT, MAXT != 256 ? 1 : CACHE && (CIO::kBytes 
   constexpr bool kBlocks = CACHE && CIO::kBytes == 0;
   // Where the token's slot starts in the pools.  Only the warps that write there work it out, after the norm -- but for norms per head,
   // which everything has to be ready for (16384 tokens of 5120 + 1024 + 1024, bf16 cache: 81.5 us instead of 83.7; per head 86.6, as
-  // here 83.7.  4-bit cache: 90.6 instead of 92.3, per head 92.8 instead of 96.1).
+  // here 83.7.  4-bit cache: 88.5 instead of 94.3, per head 93.8 instead of 97.2, without a norm 86.5 instead of 92.3).
   constexpr bool kEarly = CACHE && !kBlocks && NORM != kNormLayer;
   long long slot_k = 0, slot_v = 0;
   if (kEarly && cslot >= 0) {
