@@ -235,3 +235,63 @@ def test_scores_of_any_size(libqknorm, copies, new, variant, e):
                     clear += 1
                     assert (np.abs(got[r, h] - vv[top, h // 2]) <= 2.0 ** -7 * np.abs(vv[top, h // 2]) + 1e-6).all(), (r, h)
     assert clear > 0
+
+
+@pytest.mark.parametrize("hq,hk,hd,new,kv", [(8, 2, 128, [60, 1], [300, 77]), (2, 2, 48, [120], [500])])
+def test_a_widened_cache_read_a_row_at_a_time(libqknorm, monkeypatch, hq, hk, hd, new, kv):
+    """What unaligned rows come to where the row tiles cannot be counted."""
+    monkeypatch.setenv("QKNORM_FORCE_VARIANT", "general")
+    b = Batch(new, kv, hq, hk, hd, seed=81)
+    weights_in_fp16(b, "attn_general")
+
+
+@pytest.mark.parametrize("hd", [64, 128, 96])
+def test_rows_too_far_apart_for_boxes(libqknorm, hd):
+    """One row whose stride no tensor map takes: K, V and Q are gathered."""
+    b = Batch([1], [700], 128, 1, hd, seed=82, guard=0)
+    ref = b.reference()
+    lib = attn.lib()
+    need = attn.attn_paged_e2m1_workspace(1, 1, 1, 700, 128, 1, hd)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(b.dq, 7.0), torch.full((1, 128), 7.0, device="cuda")
+    k, v, ks, vs = b.pools
+    strides = [t.stride(d) for t in (k, v, ks, vs) for d in range(3)]
+    c = attn.CPagedCacheE2m1(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), *strides, b.pages, b.page, 1, hd, *b.unit)
+    rc = lib.qknorm_attn_paged_e2m1(b.dq.data_ptr(), 2 ** 40, ctypes.byref(c), b.dtable.data_ptr(), b.dtable.shape[1], 0, b.dlens.data_ptr(),
+                                    b.dstarts.data_ptr(), 1, 1, 1, 700, 128, hd ** -0.5, 1, 0, out.data_ptr(), 0, lse.data_ptr(), ws.data_ptr(), need,
+                                    torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == binding.QKNORM_OK and binding.last_variant() == "attn_tc" and binding.device_error_word() == 0
+    b.compare(out.cpu(), lse.cpu(), ref, True)
+
+
+def test_two_chunks_at_once(libqknorm):
+    """Chunks on two streams, each with a workspace of its own, give what they give alone; so do chunks beside single tokens."""
+    batches = [Batch([80, 33, 1], [900, 33, 2500], 8, 4, 128, seed=83), Batch([130], [4000], 4, 2, 64, seed=84), Batch([1] * 8, [2500] * 8, 8, 8, 128, seed=85)]
+    want = [b.call()[0] for b in batches]
+    streams = [torch.cuda.Stream() for _ in batches]
+    outs = [[torch.zeros_like(b.dq) for _ in range(5)] for b in batches]
+    torch.cuda.synchronize()
+    for i in range(5):
+        for b, s, o in zip(batches, streams, outs):
+            attn.qknorm_attn_paged_e2m1(b.dq, *b.pools, b.dtable, b.dlens, b.dstarts, max(b.new), max(b.kv), k_scale=b.unit[0], v_scale=b.unit[1], out=o[i], stream=s)
+    torch.cuda.synchronize()
+    for b, w, o in zip(batches, want, outs):
+        n = b.starts[-1]
+        for y in o:
+            assert torch.equal(y.cpu()[:n].view(torch.int16), w[:n].view(torch.int16))
+
+
+def test_lengths_grow_between_replays_of_a_chunk(libqknorm):
+    b = Batch([64, 64], [700, 1500], 4, 2, 128, seed=86)
+    out = torch.zeros_like(b.dq)
+    ws = torch.empty(attn.attn_paged_e2m1_workspace(2, b.T, 64, 1500, 4, 2, 128), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attn.qknorm_attn_paged_e2m1(b.dq, *b.pools, b.dtable, b.dlens, b.dstarts, 64, 1500, k_scale=b.unit[0], v_scale=b.unit[1], out=out, workspace=ws)
+    for lens in ([64, 64], [0, 1499], [700, 1500], [33, 128]):
+        b.dlens.copy_(torch.tensor(lens, dtype=torch.int32))
+        ws.fill_(255)                                   # NaN in every place that nothing is widened into
+        graph.replay()
+        want, _ = b.call(max_kv=1500)
+        assert torch.equal(out.cpu()[:128].view(torch.int16), want[:128].view(torch.int16)) and not torch.isnan(out).any()
