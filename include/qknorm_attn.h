@@ -160,7 +160,8 @@ int qknorm_fwd_append(const void* q, const void* k, const void* v, const void* g
  * Rounding in "attn_tc": scores, maxima, sums and the accumulated output are fp32.  The weights are rounded for the product with V: to
  * bf16 (half a step: 2^-8 relative) over a bf16 cache, to fp16 over an FP8 one (2^-11 relative, and at least 2^-32 of the row's largest weight).
  * Over an FP8 cache the queries are brought to fp16, a power of two taken out of each row first: exact but for parts below 2^-30 of
- * the row's largest element.  "attn_general" rounds neither.
+ * the row's largest element.  "attn_general" rounds neither.  In "attn_tc" a row whose scores (times log2(e)) pass 2^22 tells those apart that differ by more
+ * than a few fp32 steps; closer ones share the weight.
  */
 int qknorm_attn_paged(const void* q, int64_t ld_q, const qknorm_paged_cache* cache, const int32_t* block_table,
                       int32_t table_cols, int64_t ld_table, const int32_t* kv_lens, const int32_t* q_starts,

@@ -39,7 +39,7 @@
 // FP8 cache: K and V are staged raw and widened to fp16, which holds every E4M3 value exactly; Q is
 // brought to fp16 with a power of two per row, which loses nothing but parts below 2^-30 of the row's largest element.
 // A 4-bit cache, widened beforehand (qknorm_attn_e2m1.cuh), comes as K in bf16 and V in fp16, both exact: so the first product takes Q as it
-// is, and the second one has weights in fp16.  (K in fp16, too, with Q brought to it by warp 14, 24 us a tile: a prompt of 8192 1160 us, 40 / 8 heads; so 735.)
+// is, and the second one has weights in fp16.  (K in fp16, too, with Q brought to it by warp 14, 24 us a tile: a prompt of 8192, 40 / 8 heads, 1160 us; so 715.)
 //
 // Rounding: P is rounded for the second product, to bf16 (2^-8 relative) or, with an FP8 or a widened cache, to fp16 (2^-11 relative, and
 // 2^-25 absolute below 2^-14; the sum l takes them unrounded).  So P stands for 2^7 times the weights there: what the maximum may lag
